@@ -10,7 +10,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB_PATH = os.path.join(PKG, "libccdpp.so")
-SOURCES = ("sweep.hip", "build.hip", "host_copy.hip", "api.hip")
+SOURCES = ("sweep.hip", "build.hip", "host_copy.hip", "api.hip", "ops_api.hip",
+           "softmax_loss.hip", "grad_clip.hip")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 

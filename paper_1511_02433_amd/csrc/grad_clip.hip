@@ -1,0 +1,206 @@
+// Global norm of many gradient tensors, and their clipping (gfx950).
+//
+//   norm = sqrt(sum_i sum_j g_ij^2),   out_i = c g_i,   c = min(1, max_norm / (norm + eps))
+//
+// Bound by memory: the gradients are read once for the norm, and once more and written for the clipping.  The tensors
+// of a launch come as a table in the kernel's arguments, cut into chunks of kChunk values that the blocks take in
+// turn; squares are summed in 64 bits, so no gradient that its type can hold overflows them.  Every block leaves one
+// partial sum, and later launches (more than kTable tensors) add to it, in stream order: the result does not depend on timing.
+#include <algorithm>
+#include <cmath>
+
+#include "ops_internal.hpp"
+
+namespace ccdops {
+namespace {
+
+constexpr int kTable = 64;      // tensors per launch
+constexpr int kBlocks = 1024;   // partial sums
+constexpr int64_t kChunk = 8192;
+
+struct Table {
+    const void* in[kTable];
+    void* out[kTable];
+    int64_t size[kTable];
+    int64_t first[kTable];   // first chunk of each tensor
+    uint8_t dtype[kTable];
+    uint8_t wide[kTable];    // both pointers aligned to 16 bytes
+    int n;
+    int64_t chunks;
+};
+
+template <class T> struct alignas(16) Vec { T v[16 / sizeof(T)]; };
+
+template <class T>
+__device__ __forceinline__ double chunk_squares(const void* base, int64_t lo, int64_t n, bool wide) {
+    const T* g = (const T*)base + lo;
+    constexpr int W = 16 / sizeof(T);
+    double s = 0.0;
+    int64_t i = 0;
+    if (wide) {
+        for (int64_t k = threadIdx.x; k < n / W; k += blockDim.x) {
+            const Vec<T> q = ((const Vec<T>*)g)[k];
+            for (int j = 0; j < W; ++j) s += (double)(float)q.v[j] * (double)(float)q.v[j];
+        }
+        i = n / W * W;
+    }
+    for (i += threadIdx.x; i < n; i += blockDim.x) s += (double)(float)g[i] * (double)(float)g[i];
+    return s;
+}
+
+template <class T>
+__device__ __forceinline__ void chunk_scale(const void* base, void* out, int64_t lo, int64_t n, bool wide, float c) {
+    const T* g = (const T*)base + lo;
+    T* o = (T*)out + lo;
+    constexpr int W = 16 / sizeof(T);
+    int64_t i = 0;
+    if (wide) {
+        for (int64_t k = threadIdx.x; k < n / W; k += blockDim.x) {
+            Vec<T> q = ((const Vec<T>*)g)[k];
+            for (int j = 0; j < W; ++j) q.v[j] = (T)((float)q.v[j] * c);
+            ((Vec<T>*)o)[k] = q;
+        }
+        i = n / W * W;
+    }
+    for (i += threadIdx.x; i < n; i += blockDim.x) o[i] = (T)((float)g[i] * c);
+}
+
+// The tensor that a chunk belongs to.
+__device__ __forceinline__ int find(const Table& t, int64_t chunk) {
+    int lo = 0, hi = t.n - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (t.first[mid] <= chunk) lo = mid;
+        else hi = mid - 1;
+    }
+    return lo;
+}
+
+__device__ __forceinline__ double block_sum(double s, double* red) {
+    for (int k = 32; k > 0; k >>= 1) s += __shfl_xor(s, k);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+    __syncthreads();
+    double all = 0.0;
+    for (int w = 0; w < (int)blockDim.x / 64; ++w) all += red[w];
+    return all;
+}
+
+__global__ __launch_bounds__(256) void k_squares(Table t, double* parts, int add) {
+    __shared__ double red[4];
+    double s = 0.0;
+    for (int64_t c = blockIdx.x; c < t.chunks; c += gridDim.x) {
+        const int i = find(t, c);
+        const int64_t lo = (c - t.first[i]) * kChunk, n = min(kChunk, t.size[i] - lo);
+        if (t.dtype[i] == CCDPP_F32) s += chunk_squares<float>(t.in[i], lo, n, t.wide[i]);
+        else if (t.dtype[i] == CCDPP_BF16) s += chunk_squares<__bf16>(t.in[i], lo, n, t.wide[i]);
+        else s += chunk_squares<_Float16>(t.in[i], lo, n, t.wide[i]);
+    }
+    s = block_sum(s, red);
+    if (threadIdx.x == 0) parts[blockIdx.x] = add ? parts[blockIdx.x] + s : s;
+}
+
+// norm[0], from partial sums in a fixed order; no tensors: 0.
+__global__ __launch_bounds__(256) void k_norm(const double* parts, int n, float* norm) {
+    __shared__ double red[4];
+    double s = 0.0;
+    for (int i = threadIdx.x; i < n; i += 256) s += parts[i];
+    s = block_sum(s, red);
+    if (threadIdx.x == 0) *norm = (float)sqrt(s);
+}
+
+// min(1, max_norm / (norm + eps)); NaN for a norm that is NaN, 1 without a limit.
+__device__ __forceinline__ float clip_factor(float norm, float max_norm, float eps) {
+    if (norm != norm) return norm;
+    return isinf(max_norm) || norm + eps <= max_norm ? 1.f : max_norm / (norm + eps);
+}
+
+__global__ __launch_bounds__(256) void k_scale(Table t, const float* norm, float max_norm, float eps) {
+    const float c = clip_factor(*norm, max_norm, eps);
+    for (int64_t k = blockIdx.x; k < t.chunks; k += gridDim.x) {
+        const int i = find(t, k);
+        if (c == 1.f && t.out[i] == t.in[i]) continue;
+        const int64_t lo = (k - t.first[i]) * kChunk, n = min(kChunk, t.size[i] - lo);
+        if (t.dtype[i] == CCDPP_F32) chunk_scale<float>(t.in[i], t.out[i], lo, n, t.wide[i], c);
+        else if (t.dtype[i] == CCDPP_BF16) chunk_scale<__bf16>(t.in[i], t.out[i], lo, n, t.wide[i], c);
+        else chunk_scale<_Float16>(t.in[i], t.out[i], lo, n, t.wide[i], c);
+    }
+}
+
+int run(bool clip, int32_t n, const void* const* in, void* const* out, const int64_t* sizes, const int32_t* dtypes, float max_norm, float eps,
+        float* norm, void* ws, int64_t ws_bytes, void* stream) {
+    if (n < 0) return fail(CCDPP_EINVAL, "n must be >= 0");
+    if (n > 0 && (!in || !sizes || !dtypes || (clip && !out))) return fail(CCDPP_EINVAL, "the tables of tensors must be non-NULL");
+    if (!norm) return fail(CCDPP_EINVAL, "norm must be non-NULL");
+    if (clip && (!(max_norm >= 0.f) || !(eps >= 0.f) || std::isinf(eps))) return fail(CCDPP_EINVAL, "max_norm must be >= 0 and eps finite and >= 0");
+    for (int32_t i = 0; i < n; ++i) {
+        if (sizes[i] < 0) return fail(CCDPP_EINVAL, "a tensor's size is negative");
+        if (dtypes[i] < CCDPP_F32 || dtypes[i] > CCDPP_F16) return fail(CCDPP_EINVAL, "dtypes must be CCDPP_F32, CCDPP_BF16 or CCDPP_F16");
+        if (sizes[i] > 0 && (!in[i] || (clip && !out[i]))) return fail(CCDPP_EINVAL, "a tensor is NULL");
+        const uintptr_t es = dtypes[i] == CCDPP_F32 ? 4 : 2;
+        if (sizes[i] > 0 && ((uintptr_t)in[i] % es || (clip && (uintptr_t)out[i] % es))) return fail(CCDPP_EINVAL, "a tensor is not aligned to its type");
+    }
+    if (!ws || (uintptr_t)ws % 256 || ws_bytes < kBlocks * 8) return fail(CCDPP_EINVAL, "the workspace is too small or not aligned to 256 bytes");
+    if (int rc = check_device()) return rc;
+    hipStream_t st = (hipStream_t)stream;
+    double* parts = (double*)ws;
+    const auto launch = [&](bool scale) -> int {
+        int filled = 0;
+        bool first = true;
+        Table t = {};
+        const auto go = [&]() -> int {
+            if (!t.n) return CCDPP_OK;
+            if (scale) {
+                k_scale<<<(unsigned)std::min<int64_t>(4 * kBlocks, t.chunks), 256, 0, st>>>(t, norm, max_norm, eps);
+            } else {
+                const int blocks = first ? kBlocks : (int)std::min<int64_t>(kBlocks, t.chunks);
+                k_squares<<<blocks, 256, 0, st>>>(t, parts, !first);
+                first = false;
+            }
+            const hipError_t e = hipGetLastError();
+            t.n = 0, t.chunks = 0;
+            return e == hipSuccess ? CCDPP_OK : hip_fail(e, "gradient norm");
+        };
+        for (int32_t i = 0; i < n; ++i) {
+            if (!sizes[i]) continue;
+            t.in[t.n] = in[i], t.out[t.n] = clip ? out[i] : nullptr;
+            t.size[t.n] = sizes[i], t.first[t.n] = t.chunks, t.dtype[t.n] = (uint8_t)dtypes[i];
+            t.wide[t.n] = (uintptr_t)in[i] % 16 == 0 && (!clip || (uintptr_t)out[i] % 16 == 0);
+            t.chunks += (sizes[i] + kChunk - 1) / kChunk;
+            ++filled;
+            if (++t.n == kTable)
+                if (int rc = go()) return rc;
+        }
+        if (int rc = go()) return rc;
+        if (!scale) {
+            k_norm<<<1, 256, 0, st>>>(parts, filled ? kBlocks : 0, norm);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return hip_fail(e, "gradient norm");
+        }
+        return CCDPP_OK;
+    };
+    if (int rc = launch(false)) return rc;
+    return clip ? launch(true) : CCDPP_OK;
+}
+
+}  // namespace
+}  // namespace ccdops
+
+extern "C" {
+
+int ccdpp_grad_norm_workspace(int64_t* bytes) {
+    if (!bytes) return ccdops::fail(CCDPP_EINVAL, "bytes is NULL");
+    *bytes = ccdops::kBlocks * 8;
+    return CCDPP_OK;
+}
+
+int ccdpp_grad_norm(int32_t n, const void* const* tensors, const int64_t* sizes, const int32_t* dtypes, float* norm, void* workspace,
+                    int64_t workspace_bytes, void* stream) {
+    return ccdops::run(false, n, tensors, nullptr, sizes, dtypes, 0.f, 0.f, norm, workspace, workspace_bytes, stream);
+}
+
+int ccdpp_clip_grads(int32_t n, const void* const* tensors, void* const* out, const int64_t* sizes, const int32_t* dtypes, float max_norm,
+                     float eps, float* norm, void* workspace, int64_t workspace_bytes, void* stream) {
+    return ccdops::run(true, n, tensors, out, sizes, dtypes, max_norm, eps, norm, workspace, workspace_bytes, stream);
+}
+
+}  // extern "C"

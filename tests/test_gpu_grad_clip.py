@@ -1,0 +1,130 @@
+"""Global gradient norm and clipping against float64.
+
+Tolerances: squares are summed in 64 bits, the norm is rounded once (2^-24) and the factor's division and product
+round twice more in 32 bits: 4 x 2^-24 relative; 16-bit outputs round once more (2^-9, 2^-11)."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+TOL = {torch.float32: 4 * 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -10}
+
+
+def ops():
+    from paper_1511_02433_amd import ops as o
+    return o
+
+
+def make(sizes, dtypes, seed=0, size=1.0):
+    gen = torch.Generator().manual_seed(seed)
+    return [(torch.randn(n, generator=gen) * size).to(dtypes[i % len(dtypes)]).cuda() for i, n in enumerate(sizes)]
+
+
+def exact_norm(ts):
+    return math.sqrt(sum(float((a.double() ** 2).sum()) for a in ts))
+
+
+CASES = [[1], [0], [], [1, 0, 7], [8192], [8191, 8193, 3], [100_003, 5, 64], [3] * 200, [1000, 1_000_003, 17, 65536, 2]]
+
+
+@pytest.mark.parametrize("dtypes", [["f32"], ["bf16"], ["f16"], ["f32", "bf16", "f16"]])
+@pytest.mark.parametrize("sizes", CASES)
+@pytest.mark.parametrize("over", [0.5, 3.0])
+def test_norm_and_clip(sizes, dtypes, over):
+    ts = make(sizes, [DT[d] for d in dtypes], seed=len(sizes))
+    want = exact_norm(ts)
+    limit = want / over if want else 1.0
+    norm = ops().grad_norm(ts)
+    assert abs(float(norm) - want) <= 2e-7 * want
+    c = min(1.0, limit / (want + 1e-6))
+    out = [torch.empty_like(a) for a in ts]
+    n2 = ops().clip_grads(ts, limit, out=out)
+    assert torch.equal(n2, norm)
+    for a, o in zip(ts, out):
+        w = a.double() * c
+        # subnormal results of 16-bit types round absolutely
+        slack = 2.0 ** -25 if a.dtype == torch.float16 else 0.0
+        assert bool(((o.double() - w).abs() <= TOL[a.dtype] * w.abs() + slack).all())
+    kept = [a.clone() for a in ts]
+    n3 = ops().clip_grads(ts, limit)  # in place
+    assert torch.equal(n3, norm)
+    for a, o, k in zip(ts, out, kept):
+        assert torch.equal(a, o)
+        if over < 1:
+            assert torch.equal(a, k)
+
+
+def test_misaligned_and_permuted():
+    base = torch.randn(10_007, device="cuda")
+    half = torch.randn(5001, device="cuda").half()
+    ts = [base[1:], half[3:], torch.randn(30, 50, device="cuda").t(), torch.randn(4, 5, 6, device="cuda").permute(2, 0, 1)]
+    want = exact_norm(ts)
+    assert abs(float(ops().grad_norm(ts)) - want) <= 2e-7 * want
+    before = [a.clone() for a in ts]
+    first = float(base[0])
+    ops().clip_grads(ts, want / 2)
+    for a, b in zip(ts, before):
+        assert float((a.double() - b.double() / 2).abs().max()) <= 2e-3 if a.dtype == torch.float16 else 1e-5
+    assert float(base[0]) == first
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_large_values_do_not_overflow(dtype):
+    ts = make([1000, 33], [DT[dtype]], size=1e30)
+    want = exact_norm(ts)
+    assert abs(float(ops().grad_norm(ts)) - want) <= 1e-6 * want
+    ops().clip_grads(ts, 1.0)
+    assert abs(exact_norm(ts) - 1.0) <= 1e-2
+
+
+def test_not_finite():
+    ts = make([100, 50], [torch.float32])
+    ts[0][3] = math.nan
+    n = ops().clip_grads(ts, 1.0)
+    assert math.isnan(float(n)) and all(bool(torch.isnan(a).all()) for a in ts)
+    ts = make([100, 50], [torch.float32])
+    ts[0][3] = math.inf
+    n = ops().clip_grads(ts, 1.0)
+    assert math.isinf(float(n)) and float(ts[1].abs().max()) == 0.0 and math.isnan(float(ts[0][3]))
+    ts = make([100, 50], [torch.float32])
+    kept = [a.clone() for a in ts]
+    ops().clip_grads(ts, math.inf)
+    assert all(torch.equal(a, b) for a, b in zip(ts, kept))
+    ops().clip_grads(ts, 0.0)
+    assert all(float(a.abs().max()) == 0 for a in ts)
+
+
+def test_zero_gradients():
+    ts = [torch.zeros(100, device="cuda")]
+    assert float(ops().clip_grads(ts, 1.0)) == 0.0 and float(ts[0].abs().max()) == 0.0
+
+
+def test_identical_runs_and_streams():
+    ts = make([100_003, 5, 64], [torch.float32])
+    a = ops().grad_norm(ts)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        b = ops().grad_norm(ts)
+    s.synchronize()
+    assert torch.equal(a, b)
+
+
+def test_refusals():
+    o = ops()
+    a = torch.ones(4, 6, device="cuda")
+    for bad, kind in (([a.double()], TypeError), ([a.cpu()], ValueError), ([a[:, :3]], ValueError)):
+        with pytest.raises(kind):
+            o.grad_norm(bad)
+    with pytest.raises(ValueError):
+        o.clip_grads([a], 1.0, out=[])
+    with pytest.raises(ValueError):
+        o.clip_grads([a], 1.0, out=[a.t()])
+    from paper_1511_02433_amd.ccdpp import CCDPPError
+    for kw in (dict(max_norm=-1.0), dict(max_norm=math.nan), dict(max_norm=1.0, eps=-1.0)):
+        with pytest.raises(CCDPPError):
+            o.clip_grads([a], **kw)
