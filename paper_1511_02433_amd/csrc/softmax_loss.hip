@@ -178,6 +178,7 @@ struct PackArgs {
     int target_bits;
     int64_t v;
     const float* offset;
+    float* o2;                        // of the table: offsets in base 2, padded with -inf
 };
 
 // One block: 32 rows x 128 columns through LDS.
@@ -206,6 +207,10 @@ __global__ __launch_bounds__(256) void k_pack(PackArgs a) {
             }
         }
         mul[threadIdx.x] = m, mult[threadIdx.x] = mt;
+        if (a.o2 && blockIdx.y == 0) {
+            const float o = r < a.rows && a.offset ? a.offset[r] : 0.f;
+            a.o2[r] = r >= a.rows || o < kExcluded ? -INFINITY : o * kLog2e;
+        }
     }
     for (int i = threadIdx.x; i < 32 * 128; i += 256) {
         const int r = i >> 7, c = i & 127;
@@ -265,9 +270,11 @@ struct GemmArgs {
     // logits
     int64_t v0;                  // table entry of row 0 of A
     int64_t t, v;
-    const int32_t *x_row, *fin;  // exponents (32-bit inputs), or NULL
+    int scaled;                  // 32-bit inputs: x_row, fin[0] hold
+    const int32_t *x_row, *fin;  // exponents; fin is NULL where nothing is scaled
     float scale;
     const float* offset;
+    const float* o2;             // offsets of A's rows in base 2, -inf for excluded and missing ones
     float2* part;                // [blocks of 256 table entries][t] (max, sum), base 2
     const void* target;
     int target_bits;
@@ -277,91 +284,189 @@ struct GemmArgs {
     int64_t ksv, kst;
     // other products
     float* out;                  // [split][M][ldo]
+    void* last;                  // or the result itself
     int64_t out_split, rows, cols, ldo;
-    int add;
+    int add, which;              // which: the exponent in fin of the other operand, or -1
 };
 
-template <class P, int NPL, int EPI>
+constexpr int kStages = 4;          // of LDS, each a step of 32 over K of both operands
+constexpr int kStage = 32 * kBlk;
+
+// 1 KB from global memory into LDS, 16 bytes per lane, without passing through registers.
+__device__ __forceinline__ void fetch(const char* from, char* to) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
+
+template <class P, int NPL, int EPI, class T>
 __global__ __launch_bounds__(512) void k_gemm(GemmArgs a) {
     constexpr int NSEG = NPL == 2 ? 3 : 1;
-    __shared__ __align__(16) char lds[2][16][kBlk];  // A, B: 8 blocks of 32 rows x 2 steps
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    __shared__ __align__(16) char lds[kStages * kStage];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave >> 2, wn = wave & 3;
-    const int64_t mb = (a.m_tiles + 7) / 8;
-    const int64_t bm = blockIdx.x % mb, bn = blockIdx.x / mb;
     const int split = blockIdx.y;
+    // Blocks b, b + 8, .. share an XCD and its L2: each gets a contiguous run of tiles, eight rows of tiles at a time.
+    const int64_t mb = (a.m_tiles + 7) / 8, nb = (a.n_tiles + 7) / 8;
+    int64_t bm, bn;
+    {
+        const int64_t all = mb * nb, x = blockIdx.x & 7, per = all >> 3, more = all & 7;
+        const int64_t id = x * per + min(x, more) + (blockIdx.x >> 3);
+        const int64_t band = id / (8 * nb), first = band * 8, height = min((int64_t)8, mb - first);
+        const int64_t in = id - band * 8 * nb;
+        bm = first + in % height, bn = in / height;
+    }
     const int64_t k0 = a.kb * split / a.splits, k1 = a.kb * (split + 1) / a.splits;
     f32x16 acc[4][2];
+#pragma unroll
     for (int i = 0; i < 4; ++i)
+#pragma unroll
         for (int j = 0; j < 2; ++j)
+#pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-    const int64_t am = min(bm * 8 + wave, a.m_tiles - 1), bt = min(bn * 8 + wave, a.n_tiles - 1);
-    for (int seg = 0; seg < NSEG; ++seg) {
-        const char* pa = a.a + (seg == 2 ? a.a_plane : 0) + am * a.a_tile + lane * 16;
-        const char* pb = a.b + (seg == 1 ? a.b_plane : 0) + bt * a.b_tile + lane * 16;
-        for (int64_t k = k0; k < k1; ++k) {
-            const u32x4 a0 = *(const u32x4*)(pa + k * 2 * kBlk), a1 = *(const u32x4*)(pa + k * 2 * kBlk + kBlk);
-            const u32x4 b0 = *(const u32x4*)(pb + k * 2 * kBlk), b1 = *(const u32x4*)(pb + k * 2 * kBlk + kBlk);
-            __syncthreads();
-            *(u32x4*)&lds[0][wave * 2][lane * 16] = a0;
-            *(u32x4*)&lds[0][wave * 2 + 1][lane * 16] = a1;
-            *(u32x4*)&lds[1][wave * 2][lane * 16] = b0;
-            *(u32x4*)&lds[1][wave * 2 + 1][lane * 16] = b1;
-            __syncthreads();
-            for (int s = 0; s < 2; ++s) {
-                typename P::vec fa[4], fb[2];
-                for (int i = 0; i < 4; ++i) fa[i] = *(const typename P::vec*)&lds[0][(wm * 4 + i) * 2 + s][lane * 16];
-                for (int j = 0; j < 2; ++j) fb[j] = *(const typename P::vec*)&lds[1][(wn * 2 + j) * 2 + s][lane * 16];
-                for (int i = 0; i < 4; ++i)
-                    for (int j = 0; j < 2; ++j) acc[i][j] = P::mfma(fa[i], fb[j], acc[i][j]);
+
+    // A wave brings one block of 32 rows of either operand, 2 KB a stage each.
+    const int64_t steps = k1 - k0, total = steps * NSEG;
+    if (total > 0) {
+        const char* const a0 = a.a + min(bm * 8 + wave, a.m_tiles - 1) * a.a_tile + k0 * 2 * kBlk + lane * 16;
+        const char* const b0 = a.b + min(bn * 8 + wave, a.n_tiles - 1) * a.b_tile + k0 * 2 * kBlk + lane * 16;
+        const char *pa = a0, *pb = b0;
+        int64_t left = steps;
+        int seg = 0;
+        char* const to = lds + wave * 2 * kBlk;
+        int slot = 0;
+        // Past the last step the last one is fetched again, so that the count of loads in flight stays the same.
+        const auto next = [&]() {
+            char* const s = to + slot * kStage;
+            fetch(pa, s);
+            fetch(pa + kBlk, s + kBlk);
+            fetch(pb, s + 16 * kBlk);
+            fetch(pb + kBlk, s + 17 * kBlk);
+            slot = (slot + 1) & (kStages - 1);
+            if (--left > 0) {
+                pa += 2 * kBlk, pb += 2 * kBlk;
+            } else if (seg < NSEG - 1) {
+                ++seg;
+                pa = a0 + (seg == 2 ? a.a_plane : 0), pb = b0 + (seg == 1 ? a.b_plane : 0);
+                left = steps;
+            } else {
+                left = 1;
             }
+        };
+        typename P::vec fa[2][4], fb[2][2];
+        const char* const ra = lds + wm * 8 * kBlk + lane * 16;
+        const char* const rb = lds + (16 + wn * 4) * kBlk + lane * 16;
+        const auto read = [&](int s, int at, int buf) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) fa[buf][i] = *(const typename P::vec*)(ra + at * kStage + (2 * i + s) * kBlk);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) fb[buf][j] = *(const typename P::vec*)(rb + at * kStage + (2 * j + s) * kBlk);
+        };
+        // Eight products; the reads (and fetches) issued with them go in between, one after each.
+        const auto multiply = [&](int buf, bool fetched) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) acc[i][j] = P::mfma(fa[buf][i], fb[buf][j], acc[i][j]);
+#pragma unroll
+            for (int i = 0; i < 6; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                if (fetched && i < 4) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            asm volatile("" ::: "memory");
+        };
+        next(), next(), next(), next();
+        asm volatile("s_waitcnt vmcnt(12)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        read(0, 0, 0);
+        int at = 0;
+        for (int64_t k = total; k > 0; --k) {
+            read(1, at, 1);
+            multiply(0, false);
+            // Everybody is done with this stage and has the next one: fetch into this one, read on in the next.
+            asm volatile("s_waitcnt vmcnt(8) lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            next();
+            at = (at + 1) & (kStages - 1);
+            read(0, at, 0);
+            multiply(1, true);
         }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
     const int n = lane & 31, h = lane >> 5;
     if constexpr (EPI == EPI_OUT) {
-        float* out = a.out + split * a.out_split;
+        // Last piece and only share: the caller's type.  Else 32 bits, added to what earlier pieces left.
+        const float fg = a.fin ? ldexpf(1.f, -a.fin[2]) : 1.f, f = a.fin && a.which >= 0 ? ldexpf(a.scale, -a.fin[a.which]) : a.scale;
+        float* const part = a.out + split * a.out_split;
+#pragma unroll
         for (int i = 0; i < 4; ++i)
+#pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const int64_t col = (bn * 8 + wn * 2 + j) * 32 + n;
+                const int64_t row0 = (bm * 8 + wm * 4 + i) * 32 + 4 * h;
                 if (col >= a.cols) continue;
+#pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    const int64_t row = (bm * 8 + wm * 4 + i) * 32 + 8 * (r >> 2) + 4 * h + (r & 3);
+                    const int64_t row = row0 + 8 * (r >> 2) + (r & 3);
                     if (row >= a.rows) continue;
-                    float* o = out + row * a.ldo + col;
-                    *o = a.add ? *o + acc[i][j][r] : acc[i][j][r];
+                    if (a.last) {
+                        ((T*)a.last)[row * a.ldo + col] = (T)(acc[i][j][r] * fg * f);
+                    } else {
+                        float* o = part + row * a.ldo + col;
+                        *o = a.add ? *o + acc[i][j][r] : acc[i][j][r];
+                    }
                 }
             }
         return;
     }
-    // Logits in base 2; excluded and missing entries are -inf.
-    const int ee = a.fin ? a.fin[0] : 0;
+    // Logits in base 2: accumulator times the row's factor, plus offset.
+    const int ee = a.scaled ? a.fin[0] : 0;
+    const auto factor = [&](int64_t t) {
+        const int xe = a.scaled ? a.x_row[min(t, a.t - 1)] : 0;
+        return ldexpf(a.scale * kLog2e, -(xe + ee));
+    };
+    const auto offsets = [&](int64_t tile, f32x4* o) {  // of a block of 32 entries, those of this lane's rows
+        const float* at = a.o2 + tile * 32 + 4 * h;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) o[q] = *(const f32x4*)(at + 8 * q);
+    };
     if constexpr (EPI == EPI_LSE) {
-        __shared__ float2 share[2][256];
-        for (int j = 0; j < 2; ++j) {
-            const int64_t t = (bn * 8 + wn * 2 + j) * 32 + n;
-            const int xe = a.x_row && t < a.t ? a.x_row[t] : 0;
-            const float f = ldexpf(a.scale * kLog2e, -(xe + ee));
-            float top = -INFINITY;
-            for (int i = 0; i < 4; ++i)
+        float2(*share)[256] = (float2(*)[256])lds;
+        float f[2], top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < 2; ++j) f[j] = factor((bn * 8 + wn * 2 + j) * 32 + n);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t tile = bm * 8 + wm * 4 + i;
+            f32x4 o[4];
+            if (tile < a.m_tiles) {
+                offsets(tile, o);
+            } else {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) o[q] = -INFINITY;
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    const int64_t v = a.v0 + (bm * 8 + wm * 4 + i) * 32 + 8 * (r >> 2) + 4 * h + (r & 3);
-                    float z = -INFINITY;
-                    if (v < a.v) {
-                        const float o = a.offset ? a.offset[v] : 0.f;
-                        if (!(o < kExcluded)) z = fmaf(acc[i][j][r], f, o * kLog2e);
-                    }
-                    acc[i][j][r] = z;
-                    top = fmaxf(top, z);
+                    acc[i][j][r] = fmaf(acc[i][j][r], f[j], o[r >> 2][r & 3]);
+                    top[j] = fmaxf(top[j], acc[i][j][r]);
                 }
-            float sum = 0.f;
-            const float ref = top == -INFINITY ? 0.f : top;
+        }
+        __syncthreads();  // LDS is free
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            top[j] = fmaxf(top[j], __shfl_xor(top[j], 32));
+            const float ref = top[j] == -INFINITY ? 0.f : top[j];
+#pragma unroll
             for (int i = 0; i < 4; ++i)
-                for (int r = 0; r < 16; ++r) sum += exp2_fast(acc[i][j][r] - ref);
-            const float top2 = __shfl_xor(top, 32), sum2 = __shfl_xor(sum, 32);
-            const float m = fmaxf(top, top2);
-            const float mr = m == -INFINITY ? 0.f : m;
-            sum = sum * exp2_fast(top - mr) + sum2 * exp2_fast(top2 - mr);
-            if (h == 0) share[wm][(wn * 2 + j) * 32 + n] = make_float2(m, sum);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) sum[j] += exp2_fast(acc[i][j][r] - ref);
+            sum[j] += __shfl_xor(sum[j], 32);
+            if (h == 0) share[wm][(wn * 2 + j) * 32 + n] = make_float2(top[j], sum[j]);
         }
         __syncthreads();
         if (threadIdx.x < 256) {
@@ -376,57 +481,74 @@ __global__ __launch_bounds__(512) void k_gemm(GemmArgs a) {
     if constexpr (EPI == EPI_G) {
         // identity in B-operand order for the two steps of 16 entries
         typename P::vec eye[2];
+#pragma unroll
         for (int s = 0; s < 2; ++s)
-            for (int k = 0; k < 8; ++k) {
-                const int v = 16 * s + (k < 4 ? 4 * h + k : 8 + 4 * h + k - 4);
-                eye[s][k] = (typename P::elem)(v == n ? 1.f : 0.f);
-            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) eye[s][k] = (typename P::elem)(16 * s + (k < 4 ? 4 * h + k : 8 + 4 * h + k - 4) == n ? 1.f : 0.f);
+        float w[2], l2[2], f[2];
+        int64_t y[2];        // target, from the piece's first entry
+        uint32_t keep[2];    // all ones in rows that count: others are cut off as bits, whatever they hold
+#pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const int64_t tt = bn * 8 + wn * 2 + j, t = tt * 32 + n;
-            if (tt >= a.n_tiles) continue;
-            float w = 0.f, l2 = 0.f, f = 0.f;
-            int64_t y = -1;
+            const int64_t t = (bn * 8 + wn * 2 + j) * 32 + n;
+            w[j] = 0.f, l2[j] = 0.f, f[j] = 0.f, y[j] = -1, keep[j] = 0;
             if (t < a.t) {
-                y = load_target(a.target, a.target_bits, t);
-                const int xe = a.x_row ? a.x_row[t] : 0;
-                f = ldexpf(a.scale * kLog2e, -(xe + ee));
-                if (row_counts(y, a.v, a.offset)) {
-                    w = a.grad ? a.grad[t] : 1.f;
-                    if (a.fin) w = ldexpf(w, a.fin[2]);
-                    if (y >= a.v) w = NAN;
-                    l2 = a.lse[t] * kLog2e;
+                const int64_t yt = load_target(a.target, a.target_bits, t);
+                f[j] = factor(t);
+                if (row_counts(yt, a.v, a.offset)) {
+                    keep[j] = ~0u;
+                    w[j] = a.grad ? a.grad[t] : 1.f;
+                    if (a.fin) w[j] = ldexpf(w[j], a.fin[2]);
+                    if (yt >= a.v) w[j] = NAN;
+                    l2[j] = a.lse[t] * kLog2e;
+                    y[j] = yt - a.v0;
                 }
             }
-            const bool dead = t >= a.t || !row_counts(y, a.v, a.offset);
-            for (int i = 0; i < 4; ++i) {
-                const int64_t vt = bm * 8 + wm * 4 + i;
-                if (vt >= a.m_tiles) continue;
-                typename P::vec hi[NPL][2];
-                for (int r = 0; r < 16; ++r) {
-                    const int64_t v = a.v0 + vt * 32 + 8 * (r >> 2) + 4 * h + (r & 3);
-                    float g = 0.f;
-                    if (v < a.v && !dead) {
-                        const float o = a.offset ? a.offset[v] : 0.f;
-                        const float pr = o < kExcluded ? 0.f : exp2_fast(fmaf(acc[i][j][r], f, o * kLog2e) - l2);
-                        g = w * (pr - (v == y ? 1.f : 0.f));
-                    }
-                    typename P::elem o2[2];
-                    to_planes<P, NPL>(g, o2);
-                    for (int pl = 0; pl < NPL; ++pl) hi[pl][r >> 3][r & 7] = o2[pl];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t vt = bm * 8 + wm * 4 + i;
+            if (vt >= a.m_tiles) continue;
+            f32x4 o[4];
+            offsets(vt, o);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int64_t tt = bn * 8 + wn * 2 + j;
+                if (tt >= a.n_tiles) continue;
+                float g[16];
+#pragma unroll
+                for (int r = 0; r < 16; ++r) g[r] = w[j] * exp2_fast(fmaf(acc[i][j][r], f[j], o[r >> 2][r & 3]) - l2[j]);
+                const int64_t at = y[j] - vt * 32;
+                if (__any(at >= 0 && at < 32)) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (at == 8 * (r >> 2) + 4 * h + (r & 3)) g[r] -= w[j];
                 }
-                for (int pl = 0; pl < NPL; ++pl) {
-                    char* g = a.g + pl * a.g_plane + (tt * a.ksv + vt * 2) * kBlk + lane * 16;
-                    *(typename P::vec*)g = hi[pl][0];
-                    *(typename P::vec*)(g + kBlk) = hi[pl][1];
-                    f32x16 tr;
-                    for (int r = 0; r < 16; ++r) tr[r] = 0.f;
-                    tr = P::mfma(hi[pl][0], eye[0], tr);
-                    tr = P::mfma(hi[pl][1], eye[1], tr);
-                    typename P::vec o[2];
-                    for (int r = 0; r < 16; ++r) o[r >> 3][r & 7] = (typename P::elem)tr[r];
-                    char* gt = a.gt + pl * a.gt_plane + (vt * a.kst + tt * 2) * kBlk + lane * 16;
-                    *(typename P::vec*)gt = o[0];
-                    *(typename P::vec*)(gt + kBlk) = o[1];
+                typename P::vec pl[NPL][2];
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    typename P::elem e2[2];
+                    to_planes<P, NPL>(g[r], e2);
+#pragma unroll
+                    for (int k = 0; k < NPL; ++k) pl[k][r >> 3][r & 7] = e2[k];
+                }
+#pragma unroll
+                for (int k = 0; k < NPL; ++k) {
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        u32x4 bits = __builtin_bit_cast(u32x4, pl[k][s]);
+                        bits &= keep[j];
+                        pl[k][s] = __builtin_bit_cast(typename P::vec, bits);
+                        *(u32x4*)(a.g + k * a.g_plane + (tt * a.ksv + vt * 2 + s) * kBlk + lane * 16) = bits;
+                    }
+                    f32x16 tr = {};
+                    tr = P::mfma(pl[k][0], eye[0], tr);
+                    tr = P::mfma(pl[k][1], eye[1], tr);
+                    typename P::vec to[2];
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) to[r >> 3][r & 7] = (typename P::elem)tr[r];
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) *(typename P::vec*)(a.gt + k * a.gt_plane + (vt * a.kst + tt * 2 + s) * kBlk + lane * 16) = to[s];
                 }
             }
         }
@@ -500,7 +622,7 @@ struct Plan {
     int64_t vc;              // table entries per piece of the gradients (a multiple of 256)
     int sx, se;              // splits of the two gradients' contractions
     // offsets into the workspace
-    int64_t o_scale, o_xrow, o_fin, o_xf, o_ef, o_xt, o_et, o_g, o_gt, o_part, o_dx, o_de, o_lse, bytes;
+    int64_t o_scale, o_xrow, o_fin, o_xf, o_ef, o_o2, o_xt, o_et, o_g, o_gt, o_part, o_dx, o_de, o_lse, bytes;
 };
 
 constexpr int64_t kPieceBytes = int64_t(128) << 20;  // of G
@@ -535,14 +657,15 @@ Plan make_plan(const ccdpp_softmax_t& p, int call) {
     w.o_xrow = take(w.scaled ? p.t * 4 : 0);
     w.o_xf = take(w.planes * w.tt * w.ksd * kBlk);
     w.o_ef = take(w.planes * w.vt * w.ksd * kBlk);
+    w.o_o2 = take(w.vt * 32 * 4);
     w.o_part = take(w.forward ? (w.vt + 7) / 8 * p.t * 8 : 0);
     if (w.grads) {
         w.o_xt = take(w.planes * w.dt * w.kst * kBlk);
         w.o_et = take(w.planes * w.dt * w.ksv * kBlk);
         w.o_g = take(w.planes * w.tt * (w.vc / 16) * kBlk);
         w.o_gt = take(w.planes * (w.vc / 32) * w.kst * kBlk);
-        w.o_dx = take(w.sx * p.t * p.d * 4);
-        w.o_de = take(w.se * w.vc * p.d * 4);
+        w.o_dx = take(p.v <= w.vc && w.sx == 1 ? 0 : w.sx * p.t * p.d * 4);
+        w.o_de = take(w.se == 1 ? 0 : w.se * w.vc * p.d * 4);
     } else {
         w.o_xt = w.o_et = w.o_g = w.o_gt = w.o_dx = w.o_de = 0;
     }
@@ -585,6 +708,7 @@ int run(const ccdpp_softmax_t& p, int call, float* loss, float* lse, const float
     pk.src = p.table, pk.ld = p.ldt, pk.rows = p.v, pk.ksr = w.ksv, pk.which = 0, pk.row_exp = nullptr;
     pk.nat = ws + w.o_ef, pk.nat_plane = w.vt * w.ksd * kBlk;
     pk.turned = w.grads ? ws + w.o_et : nullptr, pk.turned_plane = w.dt * w.ksv * kBlk;
+    pk.o2 = (float*)(ws + w.o_o2);
     k_pack<DT><<<dim3((unsigned)w.vt, (p.d + 127) / 128), 256, 0, st>>>(pk);
     OPS_LAUNCH("pack table");
 
@@ -593,15 +717,12 @@ int run(const ccdpp_softmax_t& p, int call, float* loss, float* lse, const float
     z.a_plane = w.vt * w.ksd * kBlk, z.b_plane = w.tt * w.ksd * kBlk;
     z.a_tile = z.b_tile = (int64_t)w.ksd * kBlk;
     z.m_tiles = w.vt, z.n_tiles = w.tt, z.kb = w.ksd / 2, z.splits = 1;
-    z.t = p.t, z.v = p.v, z.x_row = w.scaled ? sc.x_row : nullptr, z.fin = fin;
+    z.t = p.t, z.v = p.v, z.scaled = w.scaled, z.x_row = sc.x_row, z.fin = fin, z.o2 = (const float*)(ws + w.o_o2);
     z.scale = p.scale, z.offset = p.offset, z.target = p.target, z.target_bits = p.target_bits;
-    // the table's exponent is part of the logits' factor for 32-bit inputs alone
     if (w.forward) {
         z.part = (float2*)(ws + w.o_part);
-        GemmArgs f = z;
-        if (!w.scaled) f.fin = nullptr;
         const int64_t blocks = (w.vt + 7) / 8 * ((w.tt + 7) / 8);
-        k_gemm<P, NPL, EPI_LSE><<<(unsigned)blocks, 512, 0, st>>>(f);
+        k_gemm<P, NPL, EPI_LSE, T><<<(unsigned)blocks, 512, 0, st>>>(z);
         OPS_LAUNCH("logits");
         k_loss<T><<<(unsigned)((p.t + 3) / 4), 256, 0, st>>>(p, z.part, (w.vt + 7) / 8, loss, lse);
         OPS_LAUNCH("loss");
@@ -613,30 +734,36 @@ int run(const ccdpp_softmax_t& p, int call, float* loss, float* lse, const float
     for (int64_t v0 = 0; v0 < p.v; v0 += w.vc) {
         const int64_t n = std::min(w.vc, p.v - v0), nt = (n + 31) / 32;
         GemmArgs q = z;
-        q.v0 = v0, q.a = z.a + v0 / 32 * z.a_tile, q.m_tiles = nt;
+        q.v0 = v0, q.a = z.a + v0 / 32 * z.a_tile, q.o2 = z.o2 + v0, q.m_tiles = nt;
         q.ksv = nt * 2, q.g_plane = w.tt * q.ksv * kBlk, q.gt_plane = nt * w.kst * kBlk;
-        k_gemm<P, NPL, EPI_G><<<(unsigned)((nt + 7) / 8 * ((w.tt + 7) / 8)), 512, 0, st>>>(q);
+        k_gemm<P, NPL, EPI_G, T><<<(unsigned)((nt + 7) / 8 * ((w.tt + 7) / 8)), 512, 0, st>>>(q);
         OPS_LAUNCH("G");
         GemmArgs o = {};
-        o.n_tiles = w.dt, o.cols = o.ldo = p.d;
+        o.n_tiles = w.dt, o.cols = p.d, o.scale = p.scale, o.fin = fin;
         if (dx) {
             o.a = z.g, o.a_plane = q.g_plane, o.a_tile = q.ksv * kBlk, o.m_tiles = w.tt, o.rows = p.t;
             o.b = ws + w.o_et + v0 / 16 * kBlk, o.b_plane = w.dt * w.ksv * kBlk, o.b_tile = w.ksv * kBlk;
             o.kb = nt, o.splits = w.sx, o.out = (float*)(ws + w.o_dx), o.out_split = p.t * p.d, o.add = v0 > 0;
-            k_gemm<P, NPL, EPI_OUT><<<dim3((unsigned)((w.tt + 7) / 8 * ((w.dt + 7) / 8)), w.sx), 512, 0, st>>>(o);
+            o.which = w.scaled ? 0 : -1;
+            o.last = p.v <= w.vc && w.sx == 1 ? dx : nullptr, o.ldo = o.last ? lddx : p.d;
+            k_gemm<P, NPL, EPI_OUT, T><<<dim3((unsigned)((w.tt + 7) / 8 * ((w.dt + 7) / 8)), w.sx), 512, 0, st>>>(o);
             OPS_LAUNCH("dx");
         }
         if (de) {
             o.a = z.gt, o.a_plane = q.gt_plane, o.a_tile = w.kst * kBlk, o.m_tiles = nt, o.rows = n;
             o.b = ws + w.o_xt, o.b_plane = w.dt * w.kst * kBlk, o.b_tile = w.kst * kBlk;
             o.kb = w.tt, o.splits = w.se, o.out = (float*)(ws + w.o_de), o.out_split = w.vc * p.d, o.add = 0;
-            k_gemm<P, NPL, EPI_OUT><<<dim3((unsigned)((nt + 7) / 8 * ((w.dt + 7) / 8)), w.se), 512, 0, st>>>(o);
+            o.which = w.scaled ? 1 : -1;
+            o.last = w.se == 1 ? (T*)de + v0 * ldde : nullptr, o.ldo = o.last ? ldde : p.d;
+            k_gemm<P, NPL, EPI_OUT, T><<<dim3((unsigned)((nt + 7) / 8 * ((w.dt + 7) / 8)), w.se), 512, 0, st>>>(o);
             OPS_LAUNCH("dtable");
-            k_finish<T><<<2048, 256, 0, st>>>(o.out, w.se, o.out_split, n, p.d, p.d, (T*)de + v0 * ldde, ldde, p.scale, fin, w.scaled ? 1 : -1);
-            OPS_LAUNCH("dtable");
+            if (!o.last) {
+                k_finish<T><<<2048, 256, 0, st>>>(o.out, w.se, o.out_split, n, p.d, p.d, (T*)de + v0 * ldde, ldde, p.scale, fin, o.which);
+                OPS_LAUNCH("dtable");
+            }
         }
     }
-    if (dx) {
+    if (dx && !(p.v <= w.vc && w.sx == 1)) {
         k_finish<T><<<2048, 256, 0, st>>>((const float*)(ws + w.o_dx), w.sx, p.t * p.d, p.t, p.d, p.d, (T*)dx, lddx, p.scale, fin, w.scaled ? 0 : -1);
         OPS_LAUNCH("dx");
     }
