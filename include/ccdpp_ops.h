@@ -43,7 +43,7 @@ enum ccdpp_dtype {
 
 /*
  * Rows against a table.  Logits z_tv = scale * (x_t . e_v) + offset_v.
- *   t, v, d  : rows (0 <= t < 2^31 - 256), table length (1 <= v < 2^31 - 256), factors
+ *   t, v, d  : rows (0 <= t < 2^26), table length (1 <= v < 2^28), factors
  *              (1 <= d <= 65536); t * v < 2^39
  *   dtype    : enum ccdpp_dtype of x, table and their gradients
  *   x, ldx   : t rows of d values, ldx >= d values apart

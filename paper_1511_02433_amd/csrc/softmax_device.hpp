@@ -1,0 +1,103 @@
+// Device code that the softmax loss's kernels share (gfx950).
+#pragma once
+
+#include "ops_internal.hpp"
+
+namespace ccdops {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kExcluded = -1e38f;  // offsets below this exclude an item
+constexpr int kParts = 256;          // partial maxima of k_scales per quantity
+constexpr int kBlk = 1024;           // bytes of one operand fragment
+
+// The 16-bit type that the matrix instructions read.
+struct BF {
+    typedef __bf16 elem;
+    typedef bf16x8 vec;
+    static __device__ f32x16 mfma(vec a, vec b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+};
+struct HF {
+    typedef _Float16 elem;
+    typedef f16x8 vec;
+    static __device__ f32x16 mfma(vec a, vec b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+};
+
+// Input type -> operand type and number of planes.
+template <int DT> struct Types;
+template <> struct Types<CCDPP_F32> { typedef float in; typedef HF op; static constexpr int planes = 2; };
+template <> struct Types<CCDPP_BF16> { typedef __bf16 in; typedef BF op; static constexpr int planes = 1; };
+template <> struct Types<CCDPP_F16> { typedef _Float16 in; typedef HF op; static constexpr int planes = 1; };
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float pow2i(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }  // -126 <= e <= 127
+__device__ __forceinline__ bool finite(float v) { return (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u; }
+
+// Power of two that brings values up to `top` below 2^15 (the result's exponent).
+__device__ __forceinline__ int scale_exp(float top) {
+    if (!(top > 0.f)) return 0;
+    const int e = (int)(__float_as_uint(top) >> 23) - 127;  // subnormals: -127
+    return min(126, 14 - e);
+}
+
+// Value in planes: hi + lo, 22 bits; lo stays 0 where hi is not finite.
+template <class P, int NPL>
+__device__ __forceinline__ void to_planes(float v, typename P::elem* out) {
+    out[0] = (typename P::elem)v;
+    if constexpr (NPL == 2) {
+        const float hi = (float)out[0];
+        out[1] = (typename P::elem)(finite(hi) ? v - hi : 0.f);
+    }
+}
+
+__device__ __forceinline__ int64_t load_target(const void* y, int bits, int64_t t) {
+    return bits == 64 ? ((const int64_t*)y)[t] : (int64_t)((const int32_t*)y)[t];
+}
+
+// Whether row t takes part in the gradients: its target is neither negative nor an excluded item.
+__device__ __forceinline__ bool row_counts(int64_t y, int64_t v, const float* offset) {
+    if (y < 0) return false;
+    return !(y < v && offset && offset[y] < kExcluded);
+}
+
+__device__ __forceinline__ float wave_max(float m) {
+    for (int k = 32; k > 0; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
+    return m;
+}
+
+// 1 KB from global memory into LDS, 16 bytes per lane, without passing through registers.
+__device__ __forceinline__ void fetch(const char* from, char* to) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
+
+// ---- few factors (d <= kSmallD) ------------------------------------------------------------
+// Everything about 32 rows of x or of the table in one piece of memory, in blocks of 1 KB: the operand fragments of the
+// rows [plane][step of 16 over d]; the rows' numbers (32 floats each: factor of the logits, or a table entry's
+// offset in base 2; lse in base 2; weight; target, as int32); the fragments of the turned rows
+// [plane][32 columns][2 steps of 16 rows].
+constexpr int kSmallD = 128;
+
+struct SmallArgs {
+    const char *x, *xlive, *e;          // bundles: x without turned rows; x with them, rows that do not count zeroed; the table
+    int64_t x_tile, xlive_tile, e_tile; // bytes of one bundle
+    int64_t tt, vt;                     // bundles
+    int64_t t, v;
+    int splits, splits_x, splits_e;     // shares of the streamed side: logits, dx, de
+    int64_t blocks_x;                   // blocks of k_small_grads that compute dx; the others compute de
+    int64_t blocks_e;
+    float2* part;                       // [split][t]
+    float *dxp, *dep;                   // [split][32 tiles][32 columns of d each]
+};
+
+// ksd: steps of 16 over d that the kernels were built for (small_steps).  Return launch errors.
+int small_steps(int d);
+template <class P, int NPL> hipError_t launch_small_lse(int ksd, const SmallArgs& a, hipStream_t st);
+template <class P, int NPL> hipError_t launch_small_grads(int ksd, const SmallArgs& a, hipStream_t st);
+
+}  // namespace ccdops

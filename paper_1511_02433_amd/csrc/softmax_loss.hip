@@ -22,238 +22,240 @@
 #include <cmath>
 #include <type_traits>
 
-#include "ops_internal.hpp"
+#include "softmax_device.hpp"
 
 namespace ccdops {
 namespace {
 
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
-constexpr float kExcluded = -1e38f;  // offsets below this exclude an item
-constexpr int kParts = 256;          // partial maxima of k_scales per quantity
-constexpr int kBlk = 1024;           // bytes of one operand fragment
-
-// The 16-bit type that the matrix instructions read.
-struct BF {
-    typedef __bf16 elem;
-    typedef bf16x8 vec;
-    static __device__ f32x16 mfma(vec a, vec b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
-};
-struct HF {
-    typedef _Float16 elem;
-    typedef f16x8 vec;
-    static __device__ f32x16 mfma(vec a, vec b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
-};
-
-// Input type -> operand type and number of planes.
-template <int DT> struct Types;
-template <> struct Types<CCDPP_F32> { typedef float in; typedef HF op; static constexpr int planes = 2; };
-template <> struct Types<CCDPP_BF16> { typedef __bf16 in; typedef BF op; static constexpr int planes = 1; };
-template <> struct Types<CCDPP_F16> { typedef _Float16 in; typedef HF op; static constexpr int planes = 1; };
-
-__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
-__device__ __forceinline__ float pow2i(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }  // -126 <= e <= 127
-__device__ __forceinline__ bool finite(float v) { return (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u; }
-
-// Power of two that brings values up to `top` below 2^15 (the result's exponent).
-__device__ __forceinline__ int scale_exp(float top) {
-    if (!(top > 0.f)) return 0;
-    const int e = (int)(__float_as_uint(top) >> 23) - 127;  // subnormals: -127
-    return min(126, 14 - e);
-}
-
-// Value in planes: hi + lo, 22 bits; lo stays 0 where hi is not finite.
-template <class P, int NPL>
-__device__ __forceinline__ void to_planes(float v, typename P::elem* out) {
-    out[0] = (typename P::elem)v;
-    if constexpr (NPL == 2) {
-        const float hi = (float)out[0];
-        out[1] = (typename P::elem)(finite(hi) ? v - hi : 0.f);
-    }
-}
-
-__device__ __forceinline__ int64_t load_target(const void* y, int bits, int64_t t) {
-    return bits == 64 ? ((const int64_t*)y)[t] : (int64_t)((const int32_t*)y)[t];
-}
-
-// Whether row t takes part in the gradients: its target is neither negative nor an excluded item.
-__device__ __forceinline__ bool row_counts(int64_t y, int64_t v, const float* offset) {
-    if (y < 0) return false;
-    return !(y < v && offset && offset[y] < kExcluded);
-}
-
-__device__ __forceinline__ float wave_max(float m) {
-    for (int k = 32; k > 0; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
-    return m;
-}
-
 // ---- scales of 32-bit inputs ----------------------------------------------------------
 // Exponents of the powers of two that x's rows (their own, for the logits; one for all rows that count, for de), the
 // table and the rows' weights are multiplied with.  Only finite values count.
+constexpr int kParts = 256;  // blocks of k_scales, and partial maxima of each quantity
+
 struct Scales {
-    float* e_part;   // [kParts] largest |table| value (items that are not excluded)
-    float* x_part;   // [kParts] largest |x| value of rows that count
-    float* g_part;   // [kParts] largest |grad|
-    int32_t* x_row;  // [t] exponent of each row of x
-    int32_t* fin;    // [3] exponents: table, x, G
+    float *e_part, *x_part, *g_part;  // [kParts] largest |table| (excluded items apart), |x| of rows that count, |grad|
+    int32_t* x_row;                   // [t] exponent of each row of x
+    int32_t* fin;                     // [3] exponents: table, x, G
 };
 
-// Blocks 0 .. kParts - 1 take the table's rows in turn (a wave per row), blocks kParts .. the rows of x.
 template <class T>
-__global__ __launch_bounds__(256) void k_scales(ccdpp_softmax_t p, const float* grad, Scales sc, int with_mats, int grads) {
-    __shared__ float red[4][3];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    float em = 0.f, xm = 0.f, gm = 0.f;
-    const int b = blockIdx.x < kParts ? blockIdx.x : blockIdx.x - kParts;
-    if (blockIdx.x < kParts) {
-        if (with_mats)
-            for (int64_t v = b * 4 + wave; v < p.v; v += kParts * 4) {
-                if (p.offset && p.offset[v] < kExcluded) continue;
-                const T* row = (const T*)p.table + v * p.ldt;
-                for (int d = lane; d < p.d; d += 64) {
-                    const float a = fabsf((float)row[d]);
-                    if (finite(a)) em = fmaxf(em, a);
-                }
-            }
-    } else {
-        for (int64_t t = b * 4 + wave; t < p.t; t += kParts * 4) {
-            const bool counts = row_counts(load_target(p.target, p.target_bits, t), p.v, p.offset);
-            if (with_mats) {
-                const T* row = (const T*)p.x + t * p.ldx;
-                float m = 0.f;
-                for (int d = lane; d < p.d; d += 64) {
-                    const float a = fabsf((float)row[d]);
-                    if (finite(a)) m = fmaxf(m, a);
-                }
-                m = wave_max(m);
-                if (lane == 0) sc.x_row[t] = scale_exp(m);
-                if (counts) xm = fmaxf(xm, m);
-            }
-            if (grads && counts) {
-                const float g = grad ? fabsf(grad[t]) : 1.f;
-                if (finite(g)) gm = fmaxf(gm, g);
-            }
+__device__ __forceinline__ float abs_finite(T v) {
+    const float a = fabsf((float)v);
+    return finite(a) ? a : 0.f;
+}
+
+// Largest finite |value| of a row, by 16 lanes.
+template <class T>
+__device__ __forceinline__ float row_max(const T* row, int d, bool wide) {
+    const int l = threadIdx.x & 15;
+    float m = 0.f;
+    int c = 0;
+    if (wide) {
+        for (; c + 64 <= d; c += 64) {
+            const f32x4 q = *(const f32x4*)(row + c + 4 * l);
+            for (int j = 0; j < 4; ++j) m = fmaxf(m, abs_finite(q[j]));
         }
     }
+    for (c += l; c < d; c += 16) m = fmaxf(m, abs_finite(row[c]));
+    for (int k = 8; k > 0; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
+    return m;
+}
+
+// MATS: the table and x (32-bit inputs), 16 lanes a row.  The rows' weights where `grads` is set.
+template <bool MATS>
+__global__ __launch_bounds__(1024) void k_scales(ccdpp_softmax_t p, const float* grad, Scales sc, int grads) {
+    __shared__ float red[16][3];
+    float em = 0.f, xm = 0.f, gm = 0.f;
+    const int64_t stride = (int64_t)kParts * 64;
+    if constexpr (MATS) {
+        const bool we = ((uintptr_t)p.table | (p.ldt * 4)) % 16 == 0, wx = ((uintptr_t)p.x | (p.ldx * 4)) % 16 == 0;
+        for (int64_t v = (int64_t)blockIdx.x * 64 + (threadIdx.x >> 4); v < p.v; v += stride) {
+            if (p.offset && p.offset[v] < kExcluded) continue;
+            em = fmaxf(em, row_max((const float*)p.table + v * p.ldt, p.d, we));
+        }
+        for (int64_t t = (int64_t)blockIdx.x * 64 + (threadIdx.x >> 4); t < p.t; t += stride) {
+            const float m = row_max((const float*)p.x + t * p.ldx, p.d, wx);
+            if ((threadIdx.x & 15) == 0) sc.x_row[t] = scale_exp(m);
+            if (row_counts(load_target(p.target, p.target_bits, t), p.v, p.offset)) xm = fmaxf(xm, m);
+        }
+    }
+    if (grads)
+        for (int64_t t = (int64_t)blockIdx.x * 1024 + threadIdx.x; t < p.t; t += (int64_t)kParts * 1024)
+            if (row_counts(load_target(p.target, p.target_bits, t), p.v, p.offset)) gm = fmaxf(gm, grad ? abs_finite(grad[t]) : 1.f);
     em = wave_max(em), xm = wave_max(xm), gm = wave_max(gm);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     if (lane == 0) red[wave][0] = em, red[wave][1] = xm, red[wave][2] = gm;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < 4; ++w) {
-            em = fmaxf(em, red[w][0]), xm = fmaxf(xm, red[w][1]), gm = fmaxf(gm, red[w][2]);
-        }
-        if (blockIdx.x < kParts) sc.e_part[b] = em;
-        else sc.x_part[b] = xm, sc.g_part[b] = gm;
+    if (wave == 0) {
+        em = lane < 16 ? red[lane][0] : 0.f, xm = lane < 16 ? red[lane][1] : 0.f, gm = lane < 16 ? red[lane][2] : 0.f;
+        em = wave_max(em), xm = wave_max(xm), gm = wave_max(gm);
+        if (lane == 0) sc.e_part[blockIdx.x] = em, sc.x_part[blockIdx.x] = xm, sc.g_part[blockIdx.x] = gm;
     }
 }
 
-// G lies within its row's weight, or a few times that where lse is the caller's own: two bits are left for it.
-__global__ __launch_bounds__(64) void k_scales_final(Scales sc) {
-    float em = 0.f, xm = 0.f, gm = 0.f;
-    for (int i = threadIdx.x; i < kParts; i += 64) em = fmaxf(em, sc.e_part[i]), xm = fmaxf(xm, sc.x_part[i]), gm = fmaxf(gm, sc.g_part[i]);
-    em = wave_max(em), xm = wave_max(xm), gm = wave_max(gm);
-    if (threadIdx.x == 0) sc.fin[0] = scale_exp(em), sc.fin[1] = scale_exp(xm), sc.fin[2] = scale_exp(gm) - 2;
+// Largest of kParts partial maxima, by 256 threads.
+__device__ __forceinline__ float parts_max(const float* part, float* red) {
+    const float m = wave_max(part[threadIdx.x]);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+    __syncthreads();
+    return fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
 }
 
 // ---- operands in fragment order ----------------------------------------------------------
-struct PackArgs {
+// Where the fragments of one matrix go; pointers that are NULL are not written.
+struct PackSide {
     const void* src;
-    int64_t ld, rows;
-    int d;
-    int ksd;              // 16-wide steps over d (even)
-    int64_t ksr;          // 16-wide steps over rows (even)
-    char* nat;            // [plane][rows/32][ksd] fragments of the matrix, or NULL
-    char* turned;         // [plane][d/32][ksr] fragments of its transpose, or NULL
-    int64_t nat_plane, turned_plane;  // bytes
-    const int32_t* row_exp;           // exponent per row for `nat` (x), or NULL
-    const int32_t* fin;               // exponents of k_scales_final, or NULL: no scaling
-    int which;                        // 0: the table, 1: x
+    int64_t ld, rows, tiles;                  // tiles: blocks of 32 rows
+    int wide;                                 // rows aligned to 16 bytes
+    char* nat;                                // the matrix as it is
+    int64_t nat_row, nat_plane;               // bytes per block of 32 rows, per plane
+    char* live;                               // the same with rows that do not count zeroed (x)
+    int64_t live_row;
+    char* turned;                             // its transpose, without the rows that do not count
+    int64_t turned_row, turned_d, turned_plane;  // per block of 32 rows, per block of 32 columns, per plane
+    char *num, *live_num;                     // numbers of the rows (see softmax_device.hpp) of the first block of 32
+    int64_t num_row, live_num_row;
+    float* o2;                                // or the table's offsets in base 2 alone
+};
+struct PackArgs {
+    PackSide x, e;
+    Scales sc;
+    int scaled;    // 32-bit inputs
+    int weights;   // g_part holds
+    int d, ksd;    // ksd: steps of 16 over d
     const void* target;
     int target_bits;
     int64_t v;
+    float scale;
     const float* offset;
-    float* o2;                        // of the table: offsets in base 2, padded with -inf
 };
 
-// One block: 32 rows x 128 columns through LDS.
+// One block: 32 rows x 128 columns, blocks of x first.  A wave takes 16 columns at a time: a lane's 8 values of a
+// fragment are 8 neighbours in memory; the turned ones are picked out of LDS.
 template <int DT>
 __global__ __launch_bounds__(256) void k_pack(PackArgs a) {
     typedef typename Types<DT>::in T;
     typedef typename Types<DT>::op P;
     constexpr int NPL = Types<DT>::planes;
-    __shared__ float tile[32][129];
-    __shared__ float mul[32];   // natural
-    __shared__ float mult[32];  // turned
-    const int64_t r0 = (int64_t)blockIdx.x * 32;
+    constexpr int kPitch = 128 + 16 / sizeof(T);
+    __shared__ __align__(16) T tile[32][kPitch];
+    __shared__ float live[32], red[4];
+    const bool is_x = blockIdx.x < a.x.tiles;
+    const PackSide& side = is_x ? a.x : a.e;
+    const int64_t rt = is_x ? blockIdx.x : blockIdx.x - a.x.tiles, r0 = rt * 32;
     const int c0 = blockIdx.y * 128;
+    int exp = 0;  // of the whole matrix
+    if (a.scaled) exp = scale_exp(parts_max(is_x ? a.sc.x_part : a.sc.e_part, red));
+    if (blockIdx.x == 0 && blockIdx.y == 0 && (a.scaled || a.weights)) {
+        const float em = a.scaled ? parts_max(a.sc.e_part, red) : 0.f, xm = a.scaled ? parts_max(a.sc.x_part, red) : 0.f;
+        const float gm = a.weights ? parts_max(a.sc.g_part, red) : 0.f;
+        // G lies within its row's weight, or a few times that where lse is the caller's own: two bits are left for it.
+        if (threadIdx.x == 0) a.sc.fin[0] = scale_exp(em), a.sc.fin[1] = scale_exp(xm), a.sc.fin[2] = scale_exp(gm) - 2;
+    }
     if (threadIdx.x < 32) {
         const int64_t r = r0 + threadIdx.x;
-        float m = 1.f, mt = 1.f;
-        if (r < a.rows) {
-            if (a.fin) {
-                m = pow2i(a.row_exp ? a.row_exp[r] : a.fin[a.which]);
-                mt = pow2i(a.fin[a.which]);
+        const bool in = r < side.rows;
+        bool counts = in;
+        if (is_x) counts = in && row_counts(load_target(a.target, a.target_bits, r), a.v, a.offset);
+        else counts = in && !(a.offset && a.offset[r] < kExcluded);
+        live[threadIdx.x] = counts ? 1.f : 0.f;
+        if (blockIdx.y == 0) {
+            if (!is_x) {
+                const float o = counts ? (a.offset ? a.offset[r] * kLog2e : 0.f) : -INFINITY;
+                if (side.o2) side.o2[r] = o;
+                if (side.num) *(float*)(side.num + rt * side.num_row + threadIdx.x * 4) = o;
             }
-            if (a.which == 0) {
-                if (a.offset && a.offset[r] < kExcluded) m = mt = 0.f;
-            } else if (a.turned && !row_counts(load_target(a.target, a.target_bits, r), a.v, a.offset)) {
-                mt = 0.f;
-            }
-        }
-        mul[threadIdx.x] = m, mult[threadIdx.x] = mt;
-        if (a.o2 && blockIdx.y == 0) {
-            const float o = r < a.rows && a.offset ? a.offset[r] : 0.f;
-            a.o2[r] = r >= a.rows || o < kExcluded ? -INFINITY : o * kLog2e;
         }
     }
-    for (int i = threadIdx.x; i < 32 * 128; i += 256) {
-        const int r = i >> 7, c = i & 127;
-        float v = 0.f;
-        if (r0 + r < a.rows && c0 + c < a.d) v = (float)((const T*)a.src)[(r0 + r) * a.ld + c0 + c];
-        tile[r][c] = v;
+    if (is_x && blockIdx.y == 0 && (side.num || side.live_num)) {
+        const int ee = a.scaled ? scale_exp(parts_max(a.sc.e_part, red)) : 0;
+        __syncthreads();
+        if (threadIdx.x < 32) {
+            const int64_t r = r0 + threadIdx.x;
+            const float f = r < side.rows ? ldexpf(a.scale * kLog2e, -((a.scaled ? a.sc.x_row[r] : 0) + ee)) : 0.f;
+            if (side.num) *(float*)(side.num + rt * side.num_row + threadIdx.x * 4) = f;
+            if (side.live_num) {  // rows that count get the rest once their lse is there
+                float* o = (float*)(side.live_num + rt * side.live_num_row) + threadIdx.x;
+                o[0] = live[threadIdx.x] != 0.f ? f : 0.f, o[32] = INFINITY, o[64] = 0.f, o[96] = __int_as_float(-1);
+            }
+        }
     }
     __syncthreads();
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 31, h = lane >> 5;
-    if (a.nat)
-        for (int s = wave; s < 8; s += 4) {
-            const int ks = c0 / 16 + s;
-            if (ks >= a.ksd) break;
-            typename P::elem o[8][2];
-            const float f = mul[m];
-            for (int j = 0; j < 8; ++j) {
-                const float v = f == 0.f ? 0.f : tile[m][s * 16 + 8 * h + j] * f;
-                to_planes<P, NPL>(v, o[j]);
-            }
-            for (int pl = 0; pl < NPL; ++pl) {
-                typename P::vec w;
-                for (int j = 0; j < 8; ++j) w[j] = o[j][pl];
-                *(typename P::vec*)(a.nat + pl * a.nat_plane + ((int64_t)blockIdx.x * a.ksd + ks) * kBlk + lane * 16) = w;
+    const int64_t row = r0 + m;
+    const bool in = row < side.rows;
+    const float mul_t = pow2i(exp);
+    const float mul = is_x && a.scaled && in ? pow2i(a.sc.x_row[row]) : mul_t;
+    const bool counts = live[m] != 0.f;
+    const T* const src = (const T*)side.src + row * side.ld;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int s = wave + 4 * k, ks = c0 / 16 + s;
+        if (ks >= a.ksd) break;
+        const int c = c0 + 16 * s + 8 * h;
+        T v[8];
+        if (in && side.wide && c + 8 <= a.d) {
+            struct alignas(16) Eight { T v[8]; };
+            const Eight q = *(const Eight*)(src + c);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = q.v[j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = in && c + j < a.d ? src[c + j] : (T)0.f;
+        }
+        if (!is_x && !counts)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = (T)0.f;
+        if (side.turned) {
+            struct alignas(16) Eight { T v[8]; } q;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) q.v[j] = counts ? v[j] : (T)0.f;
+            *(Eight*)&tile[m][16 * s + 8 * h] = q;
+        }
+        typename P::elem o[8][2];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if constexpr (NPL == 2) to_planes<P, NPL>((float)v[j] * mul, o[j]);
+            else o[j][0] = (typename P::elem)v[j];
+        }
+#pragma unroll
+        for (int pl = 0; pl < NPL; ++pl) {
+            typename P::vec w;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j] = o[j][pl];
+            const int64_t at = pl * side.nat_plane + (int64_t)ks * kBlk + lane * 16;
+            if (side.nat) *(typename P::vec*)(side.nat + rt * side.nat_row + at) = w;
+            if (side.live) {
+                const typename P::vec none = {};
+                *(typename P::vec*)(side.live + rt * side.live_row + at) = counts ? w : none;
             }
         }
-    if (a.turned)
-        for (int i = wave; i < 8; i += 4) {  // 4 blocks of 32 columns x 2 steps of 16 rows
-            const int dt = i >> 1, s = i & 1;
-            if (c0 + dt * 32 >= a.d) break;
-            typename P::elem o[8][2];
-            for (int j = 0; j < 8; ++j) {
-                const int r = 16 * s + (j < 4 ? 4 * h + j : 8 + 4 * h + j - 4);
-                const float f = mult[r];
-                const float v = f == 0.f ? 0.f : tile[r][dt * 32 + m] * f;
-                to_planes<P, NPL>(v, o[j]);
-            }
-            for (int pl = 0; pl < NPL; ++pl) {
-                typename P::vec w;
-                for (int j = 0; j < 8; ++j) w[j] = o[j][pl];
-                *(typename P::vec*)(a.turned + pl * a.turned_plane +
-                                    ((int64_t)(c0 / 32 + dt) * a.ksr + (int64_t)blockIdx.x * 2 + s) * kBlk + lane * 16) = w;
-            }
+    }
+    if (!side.turned) return;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int i = wave + 4 * k, dt = i >> 1, s = i & 1;  // 4 blocks of 32 columns x 2 steps of 16 rows
+        if (c0 + dt * 32 >= a.d) break;
+        typename P::elem o[8][2];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int r = 16 * s + (j < 4 ? 4 * h + j : 8 + 4 * h + j - 4);
+            // columns past d were not written by a fragment if they start a new one
+            const T v = c0 + dt * 32 + m < a.d ? tile[r][dt * 32 + m] : (T)0.f;
+            if constexpr (NPL == 2) to_planes<P, NPL>((float)v * mul_t, o[j]);
+            else o[j][0] = (typename P::elem)v;
         }
+#pragma unroll
+        for (int pl = 0; pl < NPL; ++pl) {
+            typename P::vec w;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j] = o[j][pl];
+            *(typename P::vec*)(side.turned + pl * side.turned_plane + (int64_t)(c0 / 32 + dt) * side.turned_d + rt * side.turned_row +
+                                s * kBlk + lane * 16) = w;
+        }
+    }
 }
 
 // ---- the product -----------------------------------------------------------------------------
@@ -291,11 +293,6 @@ struct GemmArgs {
 
 constexpr int kStages = 4;          // of LDS, each a step of 32 over K of both operands
 constexpr int kStage = 32 * kBlk;
-
-// 1 KB from global memory into LDS, 16 bytes per lane, without passing through registers.
-__device__ __forceinline__ void fetch(const char* from, char* to) {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
-}
 
 template <class P, int NPL, int EPI, class T>
 __global__ __launch_bounds__(512) void k_gemm(GemmArgs a) {
@@ -556,9 +553,32 @@ __global__ __launch_bounds__(512) void k_gemm(GemmArgs a) {
 }
 
 // ---- ends ------------------------------------------------------------------------------------
+// The numbers of row t that the gradients of few factors need (see softmax_device.hpp).
+struct RowNumbers {
+    char* first;      // of the first 32 rows, or NULL
+    int64_t step;     // bytes per 32 rows
+    const float* grad;
+    const int32_t* fin;
+};
+
+__device__ __forceinline__ void put_numbers(const RowNumbers& n, int64_t t, int64_t y, int64_t v, const float* offset, float lse) {
+    if (!row_counts(y, v, offset)) return;
+    float w = n.grad ? n.grad[t] : 1.f;
+    if (n.fin) w = ldexpf(w, n.fin[2]);
+    float* o = (float*)(n.first + t / 32 * n.step) + t % 32;
+    o[32] = lse * kLog2e;
+    o[64] = y < v ? w : NAN;
+    o[96] = __int_as_float(y < v ? (int)y : -1);
+}
+
+__global__ __launch_bounds__(256) void k_rows(ccdpp_softmax_t p, const float* lse, RowNumbers n) {
+    const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (t < p.t) put_numbers(n, t, load_target(p.target, p.target_bits, t), p.v, p.offset, lse[t]);
+}
+
 // A wave per row: joins the (max, sum) pairs of its pieces, and takes the target's logit from x and the table.
 template <class T>
-__global__ __launch_bounds__(256) void k_loss(ccdpp_softmax_t p, const float2* part, int64_t pieces, float* loss, float* lse) {
+__global__ __launch_bounds__(256) void k_loss(ccdpp_softmax_t p, const float2* part, int64_t pieces, float* loss, float* lse, RowNumbers num) {
     const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (t >= p.t) return;
     const int lane = threadIdx.x & 63;
@@ -592,22 +612,39 @@ __global__ __launch_bounds__(256) void k_loss(ccdpp_softmax_t p, const float2* p
             out = l - fmaf(dot, p.scale, o);
         }
     }
-    if (lane == 0) loss[t] = out, lse[t] = l;
+    if (lane == 0) {
+        loss[t] = out, lse[t] = l;
+        if (num.first) put_numbers(num, t, y, p.v, p.offset, l);
+    }
 }
 
-// out = factor * sum over splits, in the caller's type and strides.
+// One gradient from the partial sums of its shares, in the caller's type and strides.
+struct FinishSide {
+    const float* part;
+    int splits;
+    int64_t split, rows, ldp;  // ldp: a multiple of 4
+    void* out;
+    int64_t ldo;
+    int which;                 // exponent in fin of the other operand, or -1
+};
+
+// Four columns a thread; dx's blocks first.
 template <class T>
-__global__ __launch_bounds__(256) void k_finish(const float* part, int splits, int64_t split, int64_t rows, int cols, int64_t ldp,
-                                                T* out, int64_t ldo, float scale, const int32_t* fin, int which) {
+__global__ __launch_bounds__(256) void k_finish(FinishSide x, FinishSide e, int64_t blocks_x, int cols, float scale, const int32_t* fin) {
+    const bool is_x = blockIdx.x < blocks_x;
+    const FinishSide& a = is_x ? x : e;
+    const int64_t first = is_x ? blockIdx.x : blockIdx.x - blocks_x, stride = is_x ? blocks_x : gridDim.x - blocks_x;
+    const int quads = (cols + 3) / 4;
     // G's power of two and the other operand's are taken off one after the other: their product may be below any float
-    const float fg = fin ? ldexpf(1.f, -fin[2]) : 1.f, f = fin && which >= 0 ? ldexpf(scale, -fin[which]) : scale;
-    const int64_t n = rows * cols;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-        const int64_t r = i / cols;
-        const int c = (int)(i - r * cols);
-        float v = 0.f;
-        for (int s = 0; s < splits; ++s) v += part[s * split + r * ldp + c];
-        out[r * ldo + c] = (T)(v * fg * f);
+    const float fg = fin ? ldexpf(1.f, -fin[2]) : 1.f, f = fin && a.which >= 0 ? ldexpf(scale, -fin[a.which]) : scale;
+    for (int64_t i = first * 256 + threadIdx.x; i < a.rows * quads; i += stride * 256) {
+        const int64_t r = i / quads;
+        const int c = (int)(i - r * quads) * 4;
+        f32x4 v = {};
+        for (int s = 0; s < a.splits; ++s) v += *(const f32x4*)(a.part + s * a.split + r * a.ldp + c);
+        T* o = (T*)a.out + r * a.ldo + c;
+        for (int j = 0; j < 4; ++j)
+            if (c + j < cols) o[j] = (T)(v[j] * fg * f);
     }
 }
 
@@ -616,13 +653,17 @@ struct Plan {
     int planes = 1;
     bool scaled = false, scale_g = false;
     bool grads = false, forward = false;
+    bool small = false;      // d <= kSmallD: k_small_*
     int64_t tt, vt, dt;      // blocks of 32
     int ksd;                 // steps of 16 over d
     int64_t kst, ksv;        // over rows, over the whole table
     int64_t vc;              // table entries per piece of the gradients (a multiple of 256)
-    int sx, se;              // splits of the two gradients' contractions
+    int64_t dp;              // columns of partial sums
+    int sx, se;              // shares of the two gradients' contractions
+    int sl;                  // shares of the logits (small)
+    int64_t x_tile, xlive_tile, e_tile;  // bundles (small)
     // offsets into the workspace
-    int64_t o_scale, o_xrow, o_fin, o_xf, o_ef, o_o2, o_xt, o_et, o_g, o_gt, o_part, o_dx, o_de, o_lse, bytes;
+    int64_t o_scale, o_xrow, o_fin, o_xf, o_ef, o_xl, o_o2, o_xt, o_et, o_g, o_gt, o_part, o_dx, o_de, bytes;
 };
 
 constexpr int64_t kPieceBytes = int64_t(128) << 20;  // of G
@@ -634,18 +675,9 @@ Plan make_plan(const ccdpp_softmax_t& p, int call) {
     w.planes = p.dtype == CCDPP_F32 ? 2 : 1;
     w.scaled = p.dtype == CCDPP_F32;
     w.scale_g = w.grads && p.dtype != CCDPP_BF16;
+    w.small = p.d <= kSmallD;
     w.tt = (p.t + 31) / 32, w.vt = (p.v + 31) / 32, w.dt = (p.d + 31) / 32;
-    w.ksd = (int)w.dt * 2;
     w.kst = w.tt * 2, w.ksv = w.vt * 2;
-    const int64_t row_bytes = w.tt * 32 * 2 * w.planes;
-    w.vc = std::max<int64_t>(2048, kPieceBytes / std::max<int64_t>(row_bytes, 1) / 256 * 256);
-    w.vc = std::min(w.vc, round_up(p.v, 256));
-    const auto splits = [](int64_t m, int64_t n, int64_t kb) {
-        const int64_t blocks = std::max<int64_t>(1, (m + 7) / 8 * ((n + 7) / 8));
-        return (int)std::max<int64_t>(1, std::min<int64_t>({256 / blocks, kb / 8, 64}));
-    };
-    w.sx = splits(w.tt, w.dt, w.vc / 32);
-    w.se = splits(w.vc / 32, w.dt, w.tt);
     int64_t at = 0;
     const auto take = [&](int64_t n) {
         const int64_t o = at;
@@ -655,6 +687,37 @@ Plan make_plan(const ccdpp_softmax_t& p, int call) {
     w.o_scale = take(3 * kParts * 4);
     w.o_fin = take(64);
     w.o_xrow = take(w.scaled ? p.t * 4 : 0);
+    if (w.small) {
+        // Shares so that about 512 blocks run, two a CU; none is shorter than four tiles.
+        const auto shares = [](int64_t kept, int64_t streamed) {
+            const int64_t blocks = std::max<int64_t>(1, (kept + 3) / 4);
+            return (int)std::max<int64_t>(1, std::min<int64_t>((511 + blocks) / blocks, streamed / 4));
+        };
+        w.ksd = small_steps(p.d);
+        w.dp = w.dt * 32;
+        w.x_tile = (w.planes * w.ksd + 1) * kBlk;
+        w.e_tile = w.xlive_tile = w.x_tile + (w.grads ? w.planes * w.dt * 2 * kBlk : 0);
+        w.sl = shares(w.tt, w.vt), w.sx = shares(w.tt, w.vt), w.se = shares(w.vt, w.tt);
+        w.o_xf = take(w.forward ? w.tt * w.x_tile : 0);
+        w.o_ef = take(w.vt * w.e_tile);
+        w.o_xl = take(w.grads ? w.tt * w.xlive_tile : 0);
+        w.o_part = take(w.forward ? w.sl * p.t * 8 : 0);
+        w.o_dx = take(w.grads ? w.sx * w.tt * 32 * w.dp * 4 : 0);
+        w.o_de = take(w.grads ? w.se * w.vt * 32 * w.dp * 4 : 0);
+        w.bytes = at;
+        return w;
+    }
+    w.ksd = (int)w.dt * 2;
+    w.dp = round_up(p.d, 4);
+    const int64_t row_bytes = w.tt * 32 * 2 * w.planes;
+    w.vc = std::max<int64_t>(2048, kPieceBytes / std::max<int64_t>(row_bytes, 1) / 256 * 256);
+    w.vc = std::min(w.vc, round_up(p.v, 256));
+    const auto splits = [](int64_t m, int64_t n, int64_t kb) {
+        const int64_t blocks = std::max<int64_t>(1, (m + 7) / 8 * ((n + 7) / 8));
+        return (int)std::max<int64_t>(1, std::min<int64_t>({256 / blocks, kb / 8, 64}));
+    };
+    w.sx = splits(w.tt, w.dt, w.vc / 32);
+    w.se = splits(w.vc / 32, w.dt, w.tt);
     w.o_xf = take(w.planes * w.tt * w.ksd * kBlk);
     w.o_ef = take(w.planes * w.vt * w.ksd * kBlk);
     w.o_o2 = take(w.vt * 32 * 4);
@@ -664,10 +727,8 @@ Plan make_plan(const ccdpp_softmax_t& p, int call) {
         w.o_et = take(w.planes * w.dt * w.ksv * kBlk);
         w.o_g = take(w.planes * w.tt * (w.vc / 16) * kBlk);
         w.o_gt = take(w.planes * (w.vc / 32) * w.kst * kBlk);
-        w.o_dx = take(p.v <= w.vc && w.sx == 1 ? 0 : w.sx * p.t * p.d * 4);
-        w.o_de = take(w.se == 1 ? 0 : w.se * w.vc * p.d * 4);
-    } else {
-        w.o_xt = w.o_et = w.o_g = w.o_gt = w.o_dx = w.o_de = 0;
+        w.o_dx = take(p.v <= w.vc && w.sx == 1 ? 0 : w.sx * p.t * w.dp * 4);
+        w.o_de = take(w.se == 1 ? 0 : w.se * w.vc * w.dp * 4);
     }
     w.bytes = at;
     return w;
@@ -679,39 +740,63 @@ Plan make_plan(const ccdpp_softmax_t& p, int call) {
         if (e_ != hipSuccess) return hip_fail(e_, what);              \
     } while (0)
 
+template <class T>
+int finish(const FinishSide& x, const FinishSide& e, int cols, float scale, const int32_t* fin, hipStream_t st) {
+    const int64_t quads = (cols + 3) / 4;
+    const auto blocks = [&](const FinishSide& a) { return a.out ? std::min<int64_t>((a.rows * quads + 255) / 256, 1 << 16) : 0; };
+    const int64_t bx = blocks(x), be = blocks(e);
+    if (bx + be == 0) return CCDPP_OK;
+    k_finish<T><<<(unsigned)(bx + be), 256, 0, st>>>(x, e, bx, cols, scale, fin);
+    OPS_LAUNCH("gradients");
+    return CCDPP_OK;
+}
+
+struct Outs {
+    float *loss, *lse;
+    const float *lse_in, *grad;
+    void* dx;
+    int64_t lddx;
+    void* de;
+    int64_t ldde;
+};
+
 template <int DT>
-int run(const ccdpp_softmax_t& p, int call, float* loss, float* lse, const float* lse_in, const float* grad, void* dx, int64_t lddx,
-        void* de, int64_t ldde, char* ws, hipStream_t st) {
+int run_small(const ccdpp_softmax_t& p, const Plan& w, const Outs& o, const int32_t* fin, char* ws, hipStream_t st) {
     typedef typename Types<DT>::in T;
     typedef typename Types<DT>::op P;
     constexpr int NPL = Types<DT>::planes;
-    const Plan w = make_plan(p, call);
-    Scales sc;
-    sc.e_part = (float*)(ws + w.o_scale), sc.x_part = sc.e_part + kParts, sc.g_part = sc.x_part + kParts;
-    sc.fin = (int32_t*)(ws + w.o_fin), sc.x_row = (int32_t*)(ws + w.o_xrow);
-    const int32_t* fin = w.scaled || w.scale_g ? sc.fin : nullptr;
-    if (w.scaled || w.scale_g) {
-        k_scales<T><<<2 * kParts, 256, 0, st>>>(p, grad, sc, w.scaled, w.grads);
-        OPS_LAUNCH("scales");
-        k_scales_final<<<1, 64, 0, st>>>(sc);
-        OPS_LAUNCH("scales");
+    SmallArgs a = {};
+    a.x = ws + w.o_xf, a.xlive = ws + w.o_xl, a.e = ws + w.o_ef;
+    a.x_tile = w.x_tile, a.xlive_tile = w.xlive_tile, a.e_tile = w.e_tile;
+    a.tt = w.tt, a.vt = w.vt, a.t = p.t, a.v = p.v;
+    a.splits = w.sl, a.splits_x = w.sx, a.splits_e = w.se;
+    a.part = (float2*)(ws + w.o_part);
+    a.dxp = (float*)(ws + w.o_dx), a.dep = (float*)(ws + w.o_de);
+    RowNumbers num = {};
+    if (w.grads) num.first = ws + w.o_xl + NPL * w.ksd * kBlk, num.step = w.xlive_tile, num.grad = o.grad, num.fin = fin;
+    if (w.forward) {
+        const hipError_t e = launch_small_lse<P, NPL>(w.ksd, a, st);
+        if (e != hipSuccess) return hip_fail(e, "logits");
+        k_loss<T><<<(unsigned)((p.t + 3) / 4), 256, 0, st>>>(p, a.part, w.sl, o.loss, o.lse, num);
+        OPS_LAUNCH("loss");
+    } else {
+        k_rows<<<(unsigned)((p.t + 255) / 256), 256, 0, st>>>(p, o.lse_in, num);
+        OPS_LAUNCH("rows");
     }
-    PackArgs pk = {};
-    pk.d = p.d, pk.ksd = w.ksd, pk.target = p.target, pk.target_bits = p.target_bits, pk.v = p.v, pk.offset = p.offset;
-    pk.fin = w.scaled ? sc.fin : nullptr;
-    pk.src = p.x, pk.ld = p.ldx, pk.rows = p.t, pk.ksr = w.kst, pk.which = 1;
-    pk.row_exp = w.scaled ? sc.x_row : nullptr;
-    pk.nat = ws + w.o_xf, pk.nat_plane = w.tt * w.ksd * kBlk;
-    pk.turned = w.grads ? ws + w.o_xt : nullptr, pk.turned_plane = w.dt * w.kst * kBlk;
-    k_pack<DT><<<dim3((unsigned)w.tt, (p.d + 127) / 128), 256, 0, st>>>(pk);
-    OPS_LAUNCH("pack x");
-    pk.src = p.table, pk.ld = p.ldt, pk.rows = p.v, pk.ksr = w.ksv, pk.which = 0, pk.row_exp = nullptr;
-    pk.nat = ws + w.o_ef, pk.nat_plane = w.vt * w.ksd * kBlk;
-    pk.turned = w.grads ? ws + w.o_et : nullptr, pk.turned_plane = w.dt * w.ksv * kBlk;
-    pk.o2 = (float*)(ws + w.o_o2);
-    k_pack<DT><<<dim3((unsigned)w.vt, (p.d + 127) / 128), 256, 0, st>>>(pk);
-    OPS_LAUNCH("pack table");
+    if (!w.grads) return CCDPP_OK;
+    a.blocks_x = o.dx ? (w.tt + 3) / 4 * w.sx : 0, a.blocks_e = o.de ? (w.vt + 3) / 4 * w.se : 0;
+    const hipError_t e = launch_small_grads<P, NPL>(w.ksd, a, st);
+    if (e != hipSuccess) return hip_fail(e, "gradients");
+    const FinishSide x = {a.dxp, w.sx, w.tt * 32 * w.dp, p.t, w.dp, o.dx, o.lddx, w.scaled ? 0 : -1};
+    const FinishSide t = {a.dep, w.se, w.vt * 32 * w.dp, p.v, w.dp, o.de, o.ldde, w.scaled ? 1 : -1};
+    return finish<T>(x, t, p.d, p.scale, fin, st);
+}
 
+template <int DT>
+int run_wide(const ccdpp_softmax_t& p, const Plan& w, const Outs& out, const int32_t* fin, const Scales& sc, char* ws, hipStream_t st) {
+    typedef typename Types<DT>::in T;
+    typedef typename Types<DT>::op P;
+    constexpr int NPL = Types<DT>::planes;
     GemmArgs z = {};
     z.a = ws + w.o_ef, z.b = ws + w.o_xf;
     z.a_plane = w.vt * w.ksd * kBlk, z.b_plane = w.tt * w.ksd * kBlk;
@@ -724,13 +809,14 @@ int run(const ccdpp_softmax_t& p, int call, float* loss, float* lse, const float
         const int64_t blocks = (w.vt + 7) / 8 * ((w.tt + 7) / 8);
         k_gemm<P, NPL, EPI_LSE, T><<<(unsigned)blocks, 512, 0, st>>>(z);
         OPS_LAUNCH("logits");
-        k_loss<T><<<(unsigned)((p.t + 3) / 4), 256, 0, st>>>(p, z.part, (w.vt + 7) / 8, loss, lse);
+        k_loss<T><<<(unsigned)((p.t + 3) / 4), 256, 0, st>>>(p, z.part, (w.vt + 7) / 8, out.loss, out.lse, RowNumbers{});
         OPS_LAUNCH("loss");
     }
     if (!w.grads) return CCDPP_OK;
-    z.lse = w.forward ? lse : lse_in, z.grad = grad;
+    z.lse = w.forward ? out.lse : out.lse_in, z.grad = out.grad;
     z.g = ws + w.o_g, z.gt = ws + w.o_gt;
     z.kst = w.kst;
+    const bool dx_whole = p.v <= w.vc && w.sx == 1;
     for (int64_t v0 = 0; v0 < p.v; v0 += w.vc) {
         const int64_t n = std::min(w.vc, p.v - v0), nt = (n + 31) / 32;
         GemmArgs q = z;
@@ -740,41 +826,84 @@ int run(const ccdpp_softmax_t& p, int call, float* loss, float* lse, const float
         OPS_LAUNCH("G");
         GemmArgs o = {};
         o.n_tiles = w.dt, o.cols = p.d, o.scale = p.scale, o.fin = fin;
-        if (dx) {
+        if (out.dx) {
             o.a = z.g, o.a_plane = q.g_plane, o.a_tile = q.ksv * kBlk, o.m_tiles = w.tt, o.rows = p.t;
             o.b = ws + w.o_et + v0 / 16 * kBlk, o.b_plane = w.dt * w.ksv * kBlk, o.b_tile = w.ksv * kBlk;
-            o.kb = nt, o.splits = w.sx, o.out = (float*)(ws + w.o_dx), o.out_split = p.t * p.d, o.add = v0 > 0;
+            o.kb = nt, o.splits = w.sx, o.out = (float*)(ws + w.o_dx), o.out_split = p.t * w.dp, o.add = v0 > 0;
             o.which = w.scaled ? 0 : -1;
-            o.last = p.v <= w.vc && w.sx == 1 ? dx : nullptr, o.ldo = o.last ? lddx : p.d;
+            o.last = dx_whole ? out.dx : nullptr, o.ldo = o.last ? out.lddx : w.dp;
             k_gemm<P, NPL, EPI_OUT, T><<<dim3((unsigned)((w.tt + 7) / 8 * ((w.dt + 7) / 8)), w.sx), 512, 0, st>>>(o);
             OPS_LAUNCH("dx");
         }
-        if (de) {
+        if (out.de) {
             o.a = z.gt, o.a_plane = q.gt_plane, o.a_tile = w.kst * kBlk, o.m_tiles = nt, o.rows = n;
             o.b = ws + w.o_xt, o.b_plane = w.dt * w.kst * kBlk, o.b_tile = w.kst * kBlk;
-            o.kb = w.tt, o.splits = w.se, o.out = (float*)(ws + w.o_de), o.out_split = w.vc * p.d, o.add = 0;
+            o.kb = w.tt, o.splits = w.se, o.out = (float*)(ws + w.o_de), o.out_split = w.vc * w.dp, o.add = 0;
             o.which = w.scaled ? 1 : -1;
-            o.last = w.se == 1 ? (T*)de + v0 * ldde : nullptr, o.ldo = o.last ? ldde : p.d;
+            T* const de = (T*)out.de + v0 * out.ldde;
+            o.last = w.se == 1 ? de : nullptr, o.ldo = o.last ? out.ldde : w.dp;
             k_gemm<P, NPL, EPI_OUT, T><<<dim3((unsigned)((nt + 7) / 8 * ((w.dt + 7) / 8)), w.se), 512, 0, st>>>(o);
             OPS_LAUNCH("dtable");
-            if (!o.last) {
-                k_finish<T><<<2048, 256, 0, st>>>(o.out, w.se, o.out_split, n, p.d, p.d, (T*)de + v0 * ldde, ldde, p.scale, fin, o.which);
-                OPS_LAUNCH("dtable");
-            }
+            if (!o.last)
+                if (int rc = finish<T>(FinishSide{}, FinishSide{o.out, w.se, o.out_split, n, w.dp, de, out.ldde, o.which}, p.d, p.scale, fin, st)) return rc;
         }
     }
-    if (dx && !(p.v <= w.vc && w.sx == 1)) {
-        k_finish<T><<<2048, 256, 0, st>>>((const float*)(ws + w.o_dx), w.sx, p.t * p.d, p.t, p.d, p.d, (T*)dx, lddx, p.scale, fin, w.scaled ? 0 : -1);
-        OPS_LAUNCH("dx");
-    }
+    if (out.dx && !dx_whole)
+        return finish<T>(FinishSide{(const float*)(ws + w.o_dx), w.sx, p.t * w.dp, p.t, w.dp, out.dx, out.lddx, w.scaled ? 0 : -1}, FinishSide{}, p.d, p.scale, fin, st);
     return CCDPP_OK;
 }
 
+template <int DT>
+int run(const ccdpp_softmax_t& p, int call, const Outs& out, char* ws, hipStream_t st) {
+    typedef typename Types<DT>::in T;
+    constexpr int NPL = Types<DT>::planes;
+    const Plan w = make_plan(p, call);
+    Scales sc;
+    sc.e_part = (float*)(ws + w.o_scale), sc.x_part = sc.e_part + kParts, sc.g_part = sc.x_part + kParts;
+    sc.fin = (int32_t*)(ws + w.o_fin), sc.x_row = (int32_t*)(ws + w.o_xrow);
+    const int32_t* fin = w.scaled || w.scale_g ? sc.fin : nullptr;
+    if (w.scaled) k_scales<true><<<kParts, 1024, 0, st>>>(p, out.grad, sc, w.grads);
+    else if (w.scale_g) k_scales<false><<<kParts, 1024, 0, st>>>(p, out.grad, sc, w.grads);
+    OPS_LAUNCH("scales");
+
+    PackArgs pk = {};
+    pk.sc = sc, pk.scaled = w.scaled, pk.weights = w.scale_g;
+    pk.d = p.d, pk.ksd = w.ksd, pk.target = p.target, pk.target_bits = p.target_bits, pk.v = p.v, pk.scale = p.scale, pk.offset = p.offset;
+    PackSide &x = pk.x, &e = pk.e;
+    x.src = p.x, x.ld = p.ldx, x.rows = p.t, x.tiles = w.tt;
+    e.src = p.table, e.ld = p.ldt, e.rows = p.v, e.tiles = w.vt;
+    x.wide = ((uintptr_t)p.x | (p.ldx * sizeof(T))) % 16 == 0, e.wide = ((uintptr_t)p.table | (p.ldt * sizeof(T))) % 16 == 0;
+    if (w.small) {
+        const int64_t rows = NPL * w.ksd * kBlk, turned = rows + kBlk;
+        if (w.forward) x.nat = ws + w.o_xf, x.num = x.nat + rows;
+        x.nat_row = x.num_row = w.x_tile;
+        e.nat = ws + w.o_ef, e.num = e.nat + rows, e.nat_row = e.num_row = w.e_tile;
+        x.nat_plane = e.nat_plane = w.ksd * kBlk;
+        if (w.grads) {
+            x.live = ws + w.o_xl, x.live_num = x.live + rows, x.live_row = x.live_num_row = w.xlive_tile;
+            x.turned = x.live + turned, e.turned = e.nat + turned;
+            x.turned_row = w.xlive_tile, e.turned_row = w.e_tile;
+            x.turned_d = e.turned_d = 2 * kBlk, x.turned_plane = e.turned_plane = w.dt * 2 * kBlk;
+        }
+    } else {
+        x.nat = ws + w.o_xf, x.nat_plane = w.tt * w.ksd * kBlk;
+        e.nat = ws + w.o_ef, e.nat_plane = w.vt * w.ksd * kBlk, e.o2 = (float*)(ws + w.o_o2);
+        x.nat_row = e.nat_row = w.ksd * kBlk;
+        if (w.grads) {
+            x.turned = ws + w.o_xt, x.turned_plane = w.dt * w.kst * kBlk, x.turned_d = w.kst * kBlk;
+            e.turned = ws + w.o_et, e.turned_plane = w.dt * w.ksv * kBlk, e.turned_d = w.ksv * kBlk;
+            x.turned_row = e.turned_row = 2 * kBlk;
+        }
+    }
+    k_pack<DT><<<dim3((unsigned)(w.tt + w.vt), (p.d + 127) / 128), 256, 0, st>>>(pk);
+    OPS_LAUNCH("pack");
+    return w.small ? run_small<DT>(p, w, out, fin, ws, st) : run_wide<DT>(p, w, out, fin, sc, ws, st);
+}
+
 int check(const ccdpp_softmax_t* p, bool pointers) {
-    constexpr int64_t kMax = (int64_t(1) << 31) - 256;
     if (!p) return fail(CCDPP_EINVAL, "the problem is NULL");
-    if (p->t < 0 || p->t >= kMax) return fail(CCDPP_EINVAL, "t must be in [0, 2^31 - 256)");
-    if (p->v < 1 || p->v >= kMax) return fail(CCDPP_EINVAL, "v must be in [1, 2^31 - 256)");
+    if (p->t < 0 || p->t >= int64_t(1) << 26) return fail(CCDPP_EINVAL, "t must be in [0, 2^26)");
+    if (p->v < 1 || p->v >= int64_t(1) << 28) return fail(CCDPP_EINVAL, "v must be in [1, 2^28)");
     if (p->d < 1 || p->d > 65536) return fail(CCDPP_EINVAL, "d must be in [1, 65536]");
     if (p->dtype < CCDPP_F32 || p->dtype > CCDPP_F16) return fail(CCDPP_EINVAL, "dtype must be CCDPP_F32, CCDPP_BF16 or CCDPP_F16");
     if (p->ldx < p->d || p->ldt < p->d) return fail(CCDPP_EINVAL, "ldx and ldt must be at least d");
@@ -796,19 +925,16 @@ int call(const ccdpp_softmax_t* p, int what, float* loss, float* lse, const floa
     if ((uintptr_t)ws % 256) return fail(CCDPP_EINVAL, "the workspace must be aligned to 256 bytes");
     if (int rc = check_device()) return rc;
     hipStream_t st = (hipStream_t)stream;
-    if (p->t == 0) {
-        if (what != CCDPP_SOFTMAX_LOSS && de) {  // no rows: the table's gradient is zero
-            const int es = p->dtype == CCDPP_F32 ? 4 : 2;
-            if (es == 4) k_finish<float><<<2048, 256, 0, st>>>(nullptr, 0, 0, p->v, p->d, p->d, (float*)de, ldde, 0.f, nullptr, -1);
-            else k_finish<_Float16><<<2048, 256, 0, st>>>(nullptr, 0, 0, p->v, p->d, p->d, (_Float16*)de, ldde, 0.f, nullptr, -1);
-            OPS_LAUNCH("dtable");
-        }
-        return CCDPP_OK;
+    const Outs out = {loss, lse, lse_in, grad, dx, lddx, de, ldde};
+    if (p->t == 0) {  // no rows: the table's gradient is zero
+        const FinishSide none = {nullptr, 0, 0, p->v, 0, what == CCDPP_SOFTMAX_LOSS ? nullptr : de, ldde, -1};
+        return p->dtype == CCDPP_F32 ? finish<float>(FinishSide{}, none, p->d, 0.f, nullptr, st)
+                                     : finish<_Float16>(FinishSide{}, none, p->d, 0.f, nullptr, st);  // all bits 0, as in bfloat16
     }
     switch (p->dtype) {
-        case CCDPP_F32: return run<CCDPP_F32>(*p, what, loss, lse, lse_in, grad, dx, lddx, de, ldde, (char*)ws, st);
-        case CCDPP_BF16: return run<CCDPP_BF16>(*p, what, loss, lse, lse_in, grad, dx, lddx, de, ldde, (char*)ws, st);
-        default: return run<CCDPP_F16>(*p, what, loss, lse, lse_in, grad, dx, lddx, de, ldde, (char*)ws, st);
+        case CCDPP_F32: return run<CCDPP_F32>(*p, what, out, (char*)ws, st);
+        case CCDPP_BF16: return run<CCDPP_BF16>(*p, what, out, (char*)ws, st);
+        default: return run<CCDPP_F16>(*p, what, out, (char*)ws, st);
     }
 }
 

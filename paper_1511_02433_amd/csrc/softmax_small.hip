@@ -1,0 +1,263 @@
+// Softmax loss and gradients where rows have few factors (d <= 128): the products pass G from registers to registers.
+//
+// A block keeps 128 rows of one side (four waves of 32), their fragments in registers, and streams the other side
+// through LDS, 32 rows at a time.  The logits of a 32 x 32 tile come as an accumulator whose lanes hold one kept row and 16
+// streamed ones: sums over the streamed side are sums within a lane, and the terms G of the gradients are, as they
+// stand, the other operand of the product with the turned streamed rows.  Nothing of the size of the logits is
+// written.  The streamed side is cut into shares so that there are blocks for all CUs; shares leave partial sums that
+// k_loss and k_small_finish add in order.
+//
+// Per tile and wave the matrix cores need 32 cycles a product, 3 (d / 16) + 6 (d / 32) of them for 32-bit values, the
+// vector units 16 values of some 5 instructions and an exponential (and the split into two halves): at d = 100 the
+// products bound it, at d = 40 the logits' exponentials do.
+#include "softmax_device.hpp"
+
+namespace ccdops {
+
+int small_steps(int d) {
+    const int ks = (d + 15) / 16;
+    return ks <= 2 ? 2 : ks <= 4 ? ks : ks <= 6 ? 6 : 8;
+}
+
+namespace {
+
+template <class P, int NPL, int KS, bool TURNED>
+struct Stream {
+    static constexpr int DT = (KS + 1) / 2;
+    static constexpr int kRows = NPL * KS;              // block of the rows' numbers
+    static constexpr int kTurned = kRows + 1;           // first block of turned rows
+    static constexpr int kCount = TURNED ? kTurned + NPL * DT * 2 : kTurned;
+    static constexpr int kPer = (kCount + 3) / 4;       // fetches per wave and tile
+    static constexpr int kStages = 3 * kCount <= 80 ? 3 : 2;
+};
+
+// out: [kStages][kCount] KB of LDS.  body(tile, slot) is called for each tile first .. last - 1 with the tile's data in slot.
+template <class S, class F>
+__device__ __forceinline__ void stream(const char* from, int64_t tile_bytes, int64_t first, int64_t last, char* lds, F&& body) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (first >= last) return;
+    // Past the end the last tile is fetched again, and past the last block the last block: counts stay the same.
+    const auto next = [&](int64_t i, int slot) {
+        const char* src = from + min(i, last - 1) * tile_bytes + lane * 16;
+        char* dst = lds + slot * (S::kCount * kBlk);
+#pragma unroll
+        for (int k = 0; k < S::kPer; ++k) {
+            const int c = min(wave + 4 * k, S::kCount - 1);
+            fetch(src + c * kBlk, dst + c * kBlk);
+        }
+    };
+    for (int k = 0; k < S::kStages - 1; ++k) next(first + k, k);
+    int slot = 0;
+    for (int64_t i = first; i < last; ++i) {
+        if constexpr (S::kStages == 3) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(S::kPer) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        const int free_slot = slot == 0 ? S::kStages - 1 : slot - 1;
+        next(i + S::kStages - 1, free_slot);
+        body(i, lds + slot * (S::kCount * kBlk));
+        slot = slot + 1 == S::kStages ? 0 : slot + 1;
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+}
+
+template <class P, int NPL, int KS>
+struct Kept {
+    typename P::vec f[NPL][KS];
+    __device__ __forceinline__ void load(const char* bundle, int lane) {
+#pragma unroll
+        for (int p = 0; p < NPL; ++p)
+#pragma unroll
+            for (int k = 0; k < KS; ++k) f[p][k] = *(const typename P::vec*)(bundle + (p * KS + k) * kBlk + lane * 16);
+    }
+};
+
+// 32 x 32 products of streamed rows (LDS) and kept rows: lane (n, h) gets kept row n, streamed rows 8 q + 4 h + r.
+template <class P, int NPL, int KS>
+__device__ __forceinline__ f32x16 tile_product(const char* slot, const Kept<P, NPL, KS>& kept, int lane) {
+    f32x16 acc = {};
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+        const typename P::vec a = *(const typename P::vec*)(slot + k * kBlk + lane * 16);
+        acc = P::mfma(a, kept.f[0][k], acc);
+        if constexpr (NPL == 2) {
+            acc = P::mfma(a, kept.f[1][k], acc);
+            const typename P::vec b = *(const typename P::vec*)(slot + (KS + k) * kBlk + lane * 16);
+            acc = P::mfma(b, kept.f[0][k], acc);
+        }
+    }
+    return acc;
+}
+
+// The numbers `which` of this lane's 16 streamed rows.
+__device__ __forceinline__ void row_numbers(const char* rows, int which, int h, f32x4* o) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) o[q] = *(const f32x4*)(rows + which * 128 + (8 * q + 4 * h) * 4);
+}
+
+template <class P, int NPL, int KS>
+__global__ __launch_bounds__(256, 2) void k_small_lse(SmallArgs a) {
+    typedef Stream<P, NPL, KS, false> S;
+    __shared__ __align__(16) char lds[S::kStages * S::kCount * kBlk];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 31, h = lane >> 5;
+    const int64_t kept_blocks = (a.tt + 3) / 4;
+    const int64_t kb = blockIdx.x % kept_blocks, split = blockIdx.x / kept_blocks;
+    const int64_t tile = min(kb * 4 + wave, a.tt - 1);
+    const char* const mine = a.x + tile * a.x_tile;
+    Kept<P, NPL, KS> kept;
+    kept.load(mine, lane);
+    const float f = *(const float*)(mine + S::kRows * kBlk + n * 4);
+    float top = -INFINITY, sum = 0.f;
+    stream<S>(a.e, a.e_tile, a.vt * split / a.splits, a.vt * (split + 1) / a.splits, lds, [&](int64_t, const char* slot) {
+        f32x4 o[4];
+        row_numbers(slot + S::kRows * kBlk, 0, h, o);
+        f32x16 z = tile_product<P, NPL, KS>(slot, kept, lane);
+        float m = top;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            z[r] = fmaf(z[r], f, o[r >> 2][r & 3]);
+            m = fmaxf(m, z[r]);
+        }
+        const float ref = m == -INFINITY ? 0.f : m;
+        float s = 0.f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s += exp2_fast(z[r] - ref);
+        sum = fmaf(sum, exp2_fast(top - ref), s);
+        top = m;
+    });
+    const float top2 = __shfl_xor(top, 32), sum2 = __shfl_xor(sum, 32);
+    const float m = fmaxf(top, top2), ref = m == -INFINITY ? 0.f : m;
+    sum = sum * exp2_fast(top - ref) + sum2 * exp2_fast(top2 - ref);
+    const int64_t t = (kb * 4 + wave) * 32 + n;
+    if (h == 0 && t < a.t) a.part[split * a.t + t] = make_float2(m, sum);
+}
+
+// One side's gradients for 128 kept rows: out += turned streamed rows x G.  ITEMS: the kept rows are the table's.
+template <class P, int NPL, int KS, bool ITEMS>
+__device__ __forceinline__ void small_grad(const SmallArgs& a, int64_t block, char* lds) {
+    typedef Stream<P, NPL, KS, true> S;
+    constexpr int DT = S::DT;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 31, h = lane >> 5;
+    const int64_t tiles = ITEMS ? a.vt : a.tt, others = ITEMS ? a.tt : a.vt;
+    const int64_t splits = ITEMS ? a.splits_e : a.splits_x;
+    const int64_t kept_blocks = (tiles + 3) / 4;
+    const int64_t kb = block % kept_blocks, split = block / kept_blocks;
+    const int64_t at = kb * 4 + wave, tile = min(at, tiles - 1);
+    const char* const mine = ITEMS ? a.e + tile * a.e_tile : a.xlive + tile * a.xlive_tile;
+    Kept<P, NPL, KS> kept;
+    kept.load(mine, lane);
+    const float* const own = (const float*)(mine + S::kRows * kBlk) + n;
+    const float first = own[0];  // offset (table) or factor (x)
+    const float own_l2 = ITEMS ? 0.f : own[32], own_w = ITEMS ? 0.f : own[64];
+    const int own_y = ITEMS ? 0 : __float_as_int(own[96]);
+    f32x16 out[DT] = {};
+    stream<S>(ITEMS ? a.xlive : a.e, ITEMS ? a.xlive_tile : a.e_tile, others * split / splits, others * (split + 1) / splits, lds,
+              [&](int64_t i, const char* slot) {
+        const char* const rows = slot + S::kRows * kBlk;
+        const f32x16 z = tile_product<P, NPL, KS>(slot, kept, lane);
+        float g[16];
+        if constexpr (ITEMS) {
+            f32x4 f[4], l2[4], w[4];
+            row_numbers(rows, 0, h, f);
+            row_numbers(rows, 1, h, l2);
+            row_numbers(rows, 2, h, w);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) g[r] = w[r >> 2][r & 3] * exp2_fast(fmaf(z[r], f[r >> 2][r & 3], first) - l2[r >> 2][r & 3]);
+            const int y = ((const int*)rows)[96 + n] - (int)(tile * 32);
+            if (__any(y >= 0 && y < 32)) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (((const int*)rows)[96 + 8 * (r >> 2) + 4 * h + (r & 3)] == (int)(tile * 32) + n) g[r] -= w[r >> 2][r & 3];
+            }
+        } else {
+            f32x4 o[4];
+            row_numbers(rows, 0, h, o);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) g[r] = own_w * exp2_fast(fmaf(z[r], first, o[r >> 2][r & 3]) - own_l2);
+            const int y = own_y - (int)(i * 32);
+            if (__any(y >= 0 && y < 32)) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (y == 8 * (r >> 2) + 4 * h + (r & 3)) g[r] -= own_w;
+            }
+        }
+        typename P::vec pl[NPL][2];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            typename P::elem e[2];
+            to_planes<P, NPL>(g[r], e);
+#pragma unroll
+            for (int p = 0; p < NPL; ++p) pl[p][r >> 3][r & 7] = e[p];
+        }
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const typename P::vec b = *(const typename P::vec*)(slot + (S::kTurned + d * 2 + s) * kBlk + lane * 16);
+                out[d] = P::mfma(b, pl[0][s], out[d]);
+                if constexpr (NPL == 2) {
+                    out[d] = P::mfma(b, pl[1][s], out[d]);
+                    const typename P::vec c = *(const typename P::vec*)(slot + (S::kTurned + (DT + d) * 2 + s) * kBlk + lane * 16);
+                    out[d] = P::mfma(c, pl[0][s], out[d]);
+                }
+            }
+    });
+    if (at >= tiles) return;
+    float* const to = (ITEMS ? a.dep : a.dxp) + ((split * tiles + tile) * 32 + n) * (DT * 32) + 4 * h;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            f32x4 v;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) v[r] = out[d][q * 4 + r];
+            *(f32x4*)(to + d * 32 + q * 8) = v;
+        }
+}
+
+// Blocks for dx first, then blocks for de.
+template <class P, int NPL, int KS>
+__global__ __launch_bounds__(256, 2) void k_small_grads(SmallArgs a) {
+    typedef Stream<P, NPL, KS, true> S;
+    __shared__ __align__(16) char lds[S::kStages * S::kCount * kBlk];
+    if (blockIdx.x < a.blocks_x) small_grad<P, NPL, KS, false>(a, blockIdx.x, lds);
+    else small_grad<P, NPL, KS, true>(a, blockIdx.x - a.blocks_x, lds);
+}
+
+}  // namespace
+
+template <class P, int NPL>
+hipError_t launch_small_lse(int ksd, const SmallArgs& a, hipStream_t st) {
+    const unsigned blocks = (unsigned)((a.tt + 3) / 4 * a.splits);
+    switch (ksd) {
+        case 2: k_small_lse<P, NPL, 2><<<blocks, 256, 0, st>>>(a); break;
+        case 3: k_small_lse<P, NPL, 3><<<blocks, 256, 0, st>>>(a); break;
+        case 4: k_small_lse<P, NPL, 4><<<blocks, 256, 0, st>>>(a); break;
+        case 6: k_small_lse<P, NPL, 6><<<blocks, 256, 0, st>>>(a); break;
+        default: k_small_lse<P, NPL, 8><<<blocks, 256, 0, st>>>(a); break;
+    }
+    return hipGetLastError();
+}
+
+template <class P, int NPL>
+hipError_t launch_small_grads(int ksd, const SmallArgs& a, hipStream_t st) {
+    const unsigned blocks = (unsigned)(a.blocks_x + a.blocks_e);
+    if (!blocks) return hipSuccess;
+    switch (ksd) {
+        case 2: k_small_grads<P, NPL, 2><<<blocks, 256, 0, st>>>(a); break;
+        case 3: k_small_grads<P, NPL, 3><<<blocks, 256, 0, st>>>(a); break;
+        case 4: k_small_grads<P, NPL, 4><<<blocks, 256, 0, st>>>(a); break;
+        case 6: k_small_grads<P, NPL, 6><<<blocks, 256, 0, st>>>(a); break;
+        default: k_small_grads<P, NPL, 8><<<blocks, 256, 0, st>>>(a); break;
+    }
+    return hipGetLastError();
+}
+
+template hipError_t launch_small_lse<BF, 1>(int, const SmallArgs&, hipStream_t);
+template hipError_t launch_small_lse<HF, 1>(int, const SmallArgs&, hipStream_t);
+template hipError_t launch_small_lse<HF, 2>(int, const SmallArgs&, hipStream_t);
+template hipError_t launch_small_grads<BF, 1>(int, const SmallArgs&, hipStream_t);
+template hipError_t launch_small_grads<HF, 1>(int, const SmallArgs&, hipStream_t);
+template hipError_t launch_small_grads<HF, 2>(int, const SmallArgs&, hipStream_t);
+
+}  // namespace ccdops
