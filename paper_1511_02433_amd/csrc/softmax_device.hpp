@@ -46,6 +46,19 @@ __device__ __forceinline__ int scale_exp(float top) {
     return min(126, 14 - e);
 }
 
+// Power of two that brings the table to [1, 2) for the logits.
+__device__ __forceinline__ int unit_exp(float top) {
+    if (!(top > 0.f)) return 0;
+    return max(-126, min(126, 127 - (int)(__float_as_uint(top) >> 23)));
+}
+
+// Power of two for a row of x whose largest |value| (times scale and log2 e) is `top`: that of the table taken back, so
+// that products are logits as they are, or what keeps it below 2^15 (logits beyond 30,000) with a factor left over.
+__device__ __forceinline__ int row_exp(float top, int table) {
+    const int e = (int)(__float_as_uint(top) >> 23) - 127;
+    return max(-126, min(-table, 14 - e));
+}
+
 // Value in planes: hi + lo, 22 bits; lo stays 0 where hi is not finite.
 template <class P, int NPL>
 __device__ __forceinline__ void to_planes(float v, typename P::elem* out) {
@@ -53,6 +66,28 @@ __device__ __forceinline__ void to_planes(float v, typename P::elem* out) {
     if constexpr (NPL == 2) {
         const float hi = (float)out[0];
         out[1] = (typename P::elem)(finite(hi) ? v - hi : 0.f);
+    }
+}
+
+// The terms G of one lane, in planes of operand fragments.  Two planes are cut off toward zero, which pairs of values
+// share an instruction for: 2^-22 of the value is lost on average, 2^-20 at most.
+template <class P, int NPL>
+__device__ __forceinline__ void split_terms(const float* g, typename P::vec (*pl)[2]) {
+    if constexpr (NPL == 2) {
+        typedef __fp16 half2_t __attribute__((ext_vector_type(2)));
+#pragma unroll
+        for (int r = 0; r < 16; r += 2) {
+            const half2_t hi = __builtin_amdgcn_cvt_pkrtz(g[r], g[r + 1]);
+            const half2_t lo = __builtin_amdgcn_cvt_pkrtz(fmaf((float)hi[0], -1.f, g[r]), fmaf((float)hi[1], -1.f, g[r + 1]));
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                pl[0][r >> 3][(r & 7) + k] = (typename P::elem)hi[k];
+                pl[1][r >> 3][(r & 7) + k] = (typename P::elem)lo[k];
+            }
+        }
+    } else {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) pl[0][r >> 3][r & 7] = (typename P::elem)g[r];
     }
 }
 
@@ -78,9 +113,19 @@ __device__ __forceinline__ void fetch(const char* from, char* to) {
 
 // ---- few factors (d <= kSmallD) ------------------------------------------------------------
 // Everything about 32 rows of x or of the table in one piece of memory, in blocks of 1 KB: the operand fragments of the
-// rows [plane][step of 16 over d]; the rows' numbers (32 floats each: factor of the logits, or a table entry's
-// offset in base 2; lse in base 2; weight; target, as int32); the fragments of the turned rows
+// rows [plane][step of 16 over d]; the rows' numbers, 32 floats each; the fragments of the turned rows
 // [plane][32 columns][2 steps of 16 rows].
+enum {
+    kNumFactor = 0,   // x: factor of the accumulated logits (1 for nearly all 32-bit rows)
+    kNumOffset = 0,   // table: offset in base 2, -inf for excluded and missing entries
+    kNumTerm = 1,     // x: log2 |weight| - lse in base 2, G's exponent: G = exp2(logit + term)
+    kNumWeight = 2,   // x: |weight| with G's power of two
+    kNumTarget = 3,   // x: target, as int32
+    kNumLse = 4,      // x: minus lse in base 2; -inf in rows that do not count
+    kNumRaw = 5       // x: weight as it is
+};
+constexpr int kTermExp = 13;  // of dx's terms, which leave the row's weight to the end: at most 2^13 each
+
 constexpr int kSmallD = 128;
 
 struct SmallArgs {
@@ -88,6 +133,7 @@ struct SmallArgs {
     int64_t x_tile, xlive_tile, e_tile; // bytes of one bundle
     int64_t tt, vt;                     // bundles
     int64_t t, v;
+    int offsets;                        // whether the table has offsets
     int splits, splits_x, splits_e;     // shares of the streamed side: logits, dx, de
     int64_t blocks_x;                   // blocks of k_small_grads that compute dx; the others compute de
     int64_t blocks_e;

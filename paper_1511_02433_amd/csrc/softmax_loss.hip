@@ -34,7 +34,7 @@ constexpr int kParts = 256;  // blocks of k_scales, and partial maxima of each q
 
 struct Scales {
     float *e_part, *x_part, *g_part;  // [kParts] largest |table| (excluded items apart), |x| of rows that count, |grad|
-    int32_t* x_row;                   // [t] exponent of each row of x
+    float* x_row;                     // [t] largest |value| of each row of x
     int32_t* fin;                     // [3] exponents: table, x, G
 };
 
@@ -75,7 +75,7 @@ __global__ __launch_bounds__(1024) void k_scales(ccdpp_softmax_t p, const float*
         }
         for (int64_t t = (int64_t)blockIdx.x * 64 + (threadIdx.x >> 4); t < p.t; t += stride) {
             const float m = row_max((const float*)p.x + t * p.ldx, p.d, wx);
-            if ((threadIdx.x & 15) == 0) sc.x_row[t] = scale_exp(m);
+            if ((threadIdx.x & 15) == 0) sc.x_row[t] = m;
             if (row_counts(load_target(p.target, p.target_bits, t), p.v, p.offset)) xm = fmaxf(xm, m);
         }
     }
@@ -114,9 +114,8 @@ struct PackSide {
     int64_t live_row;
     char* turned;                             // its transpose, without the rows that do not count
     int64_t turned_row, turned_d, turned_plane;  // per block of 32 rows, per block of 32 columns, per plane
-    char *num, *live_num;                     // numbers of the rows (see softmax_device.hpp) of the first block of 32
+    char *num, *live_num;                     // numbers of the first 32 rows (see softmax_device.hpp; `num`: the first one only)
     int64_t num_row, live_num_row;
-    float* o2;                                // or the table's offsets in base 2 alone
 };
 struct PackArgs {
     PackSide x, e;
@@ -129,6 +128,7 @@ struct PackArgs {
     int64_t v;
     float scale;
     const float* offset;
+    const float* grad;
 };
 
 // One block: 32 rows x 128 columns, blocks of x first.  A wave takes 16 columns at a time: a lane's 8 values of a
@@ -141,52 +141,61 @@ __global__ __launch_bounds__(256) void k_pack(PackArgs a) {
     constexpr int kPitch = 128 + 16 / sizeof(T);
     __shared__ __align__(16) T tile[32][kPitch];
     __shared__ float live[32], red[4];
+    __shared__ int exps[32];
     const bool is_x = blockIdx.x < a.x.tiles;
     const PackSide& side = is_x ? a.x : a.e;
     const int64_t rt = is_x ? blockIdx.x : blockIdx.x - a.x.tiles, r0 = rt * 32;
     const int c0 = blockIdx.y * 128;
-    int exp = 0;  // of the whole matrix
-    if (a.scaled) exp = scale_exp(parts_max(is_x ? a.sc.x_part : a.sc.e_part, red));
+    int exp = 0, unit = 0;  // powers of two of the turned matrix, and of the table as it is
+    if (a.scaled) {
+        const float em = parts_max(a.sc.e_part, red);
+        unit = unit_exp(em);
+        exp = scale_exp(is_x ? parts_max(a.sc.x_part, red) : em);
+    }
     if (blockIdx.x == 0 && blockIdx.y == 0 && (a.scaled || a.weights)) {
         const float em = a.scaled ? parts_max(a.sc.e_part, red) : 0.f, xm = a.scaled ? parts_max(a.sc.x_part, red) : 0.f;
         const float gm = a.weights ? parts_max(a.sc.g_part, red) : 0.f;
         // G lies within its row's weight, or a few times that where lse is the caller's own: two bits are left for it.
         if (threadIdx.x == 0) a.sc.fin[0] = scale_exp(em), a.sc.fin[1] = scale_exp(xm), a.sc.fin[2] = scale_exp(gm) - 2;
     }
+    // 32-bit rows of x are multiplied with scale and log2 e before they are split.
+    const float before = NPL == 2 ? a.scale * kLog2e : 1.f;
     if (threadIdx.x < 32) {
         const int64_t r = r0 + threadIdx.x;
-        const bool in = r < side.rows;
-        bool counts = in;
-        if (is_x) counts = in && row_counts(load_target(a.target, a.target_bits, r), a.v, a.offset);
-        else counts = in && !(a.offset && a.offset[r] < kExcluded);
-        live[threadIdx.x] = counts ? 1.f : 0.f;
-        if (blockIdx.y == 0) {
-            if (!is_x) {
-                const float o = counts ? (a.offset ? a.offset[r] * kLog2e : 0.f) : -INFINITY;
-                if (side.o2) side.o2[r] = o;
-                if (side.num) *(float*)(side.num + rt * side.num_row + threadIdx.x * 4) = o;
+        bool counts = r < side.rows;
+        if (is_x) {
+            counts = counts && row_counts(load_target(a.target, a.target_bits, r), a.v, a.offset);
+            int e = 0;
+            float f = r < side.rows ? a.scale * kLog2e : 0.f;
+            if (NPL == 2 && r < side.rows) {
+                e = row_exp(a.sc.x_row[r] * fabsf(before), unit);
+                f = ldexpf(1.f, -(e + unit));
             }
-        }
-    }
-    if (is_x && blockIdx.y == 0 && (side.num || side.live_num)) {
-        const int ee = a.scaled ? scale_exp(parts_max(a.sc.e_part, red)) : 0;
-        __syncthreads();
-        if (threadIdx.x < 32) {
-            const int64_t r = r0 + threadIdx.x;
-            const float f = r < side.rows ? ldexpf(a.scale * kLog2e, -((a.scaled ? a.sc.x_row[r] : 0) + ee)) : 0.f;
-            if (side.num) *(float*)(side.num + rt * side.num_row + threadIdx.x * 4) = f;
-            if (side.live_num) {  // rows that count get the rest once their lse is there
-                float* o = (float*)(side.live_num + rt * side.live_num_row) + threadIdx.x;
-                o[0] = live[threadIdx.x] != 0.f ? f : 0.f, o[32] = INFINITY, o[64] = 0.f, o[96] = __int_as_float(-1);
+            exps[threadIdx.x] = e;
+            if (blockIdx.y == 0) {
+                if (side.num) *(float*)(side.num + rt * side.num_row + (kNumFactor * 32 + threadIdx.x) * 4) = f;
+                if (side.live_num) {  // rows that count get the rest once their lse is there
+                    float* o = (float*)(side.live_num + rt * side.live_num_row) + threadIdx.x;
+                    o[kNumFactor * 32] = counts ? f : 0.f;
+                    o[kNumTerm * 32] = o[kNumLse * 32] = -INFINITY;
+                    o[kNumWeight * 32] = o[kNumRaw * 32] = 0.f;
+                    o[kNumTarget * 32] = __int_as_float(-1);
+                }
             }
+        } else {
+            counts = counts && !(a.offset && a.offset[r] < kExcluded);
+            if (blockIdx.y == 0 && side.num)
+                *(float*)(side.num + rt * side.num_row + (kNumOffset * 32 + threadIdx.x) * 4) =
+                    counts ? (a.offset ? a.offset[r] * kLog2e : 0.f) : -INFINITY;
         }
+        // Terms of few factors are exponentials, with no sign: a negative weight's is taken into the turned row.
+        live[threadIdx.x] = !counts ? 0.f : side.live && a.grad && a.grad[r] < 0.f ? -1.f : 1.f;
     }
     __syncthreads();
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 31, h = lane >> 5;
     const int64_t row = r0 + m;
     const bool in = row < side.rows;
-    const float mul_t = pow2i(exp);
-    const float mul = is_x && a.scaled && in ? pow2i(a.sc.x_row[row]) : mul_t;
+    const float mul = pow2i(is_x ? exps[m] : unit), mul_t = pow2i(exp);
     const bool counts = live[m] != 0.f;
     const T* const src = (const T*)side.src + row * side.ld;
 #pragma unroll
@@ -210,13 +219,13 @@ __global__ __launch_bounds__(256) void k_pack(PackArgs a) {
         if (side.turned) {
             struct alignas(16) Eight { T v[8]; } q;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) q.v[j] = counts ? v[j] : (T)0.f;
+            for (int j = 0; j < 8; ++j) q.v[j] = counts ? (live[m] < 0.f ? (T)(-(float)v[j]) : v[j]) : (T)0.f;
             *(Eight*)&tile[m][16 * s + 8 * h] = q;
         }
         typename P::elem o[8][2];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            if constexpr (NPL == 2) to_planes<P, NPL>((float)v[j] * mul, o[j]);
+            if constexpr (NPL == 2) to_planes<P, NPL>((is_x ? (float)v[j] * before : (float)v[j]) * mul, o[j]);
             else o[j][0] = (typename P::elem)v[j];
         }
 #pragma unroll
@@ -272,8 +281,8 @@ struct GemmArgs {
     // logits
     int64_t v0;                  // table entry of row 0 of A
     int64_t t, v;
-    int scaled;                  // 32-bit inputs: x_row, fin[0] hold
-    const int32_t *x_row, *fin;  // exponents; fin is NULL where nothing is scaled
+    const int32_t* fin;          // exponents; NULL where nothing is scaled
+    const float* xf;             // factor of each row's accumulated logits
     float scale;
     const float* offset;
     const float* o2;             // offsets of A's rows in base 2, -inf for excluded and missing ones
@@ -420,11 +429,6 @@ __global__ __launch_bounds__(512) void k_gemm(GemmArgs a) {
         return;
     }
     // Logits in base 2: accumulator times the row's factor, plus offset.
-    const int ee = a.scaled ? a.fin[0] : 0;
-    const auto factor = [&](int64_t t) {
-        const int xe = a.scaled ? a.x_row[min(t, a.t - 1)] : 0;
-        return ldexpf(a.scale * kLog2e, -(xe + ee));
-    };
     const auto offsets = [&](int64_t tile, f32x4* o) {  // of a block of 32 entries, those of this lane's rows
         const float* at = a.o2 + tile * 32 + 4 * h;
 #pragma unroll
@@ -434,7 +438,7 @@ __global__ __launch_bounds__(512) void k_gemm(GemmArgs a) {
         float2(*share)[256] = (float2(*)[256])lds;
         float f[2], top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
 #pragma unroll
-        for (int j = 0; j < 2; ++j) f[j] = factor((bn * 8 + wn * 2 + j) * 32 + n);
+        for (int j = 0; j < 2; ++j) f[j] = a.xf[min((bn * 8 + wn * 2 + j) * 32 + n, a.t - 1)];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int64_t tile = bm * 8 + wm * 4 + i;
@@ -491,7 +495,7 @@ __global__ __launch_bounds__(512) void k_gemm(GemmArgs a) {
             w[j] = 0.f, l2[j] = 0.f, f[j] = 0.f, y[j] = -1, keep[j] = 0;
             if (t < a.t) {
                 const int64_t yt = load_target(a.target, a.target_bits, t);
-                f[j] = factor(t);
+                f[j] = a.xf[t];
                 if (row_counts(yt, a.v, a.offset)) {
                     keep[j] = ~0u;
                     w[j] = a.grad ? a.grad[t] : 1.f;
@@ -522,13 +526,7 @@ __global__ __launch_bounds__(512) void k_gemm(GemmArgs a) {
                         if (at == 8 * (r >> 2) + 4 * h + (r & 3)) g[r] -= w[j];
                 }
                 typename P::vec pl[NPL][2];
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    typename P::elem e2[2];
-                    to_planes<P, NPL>(g[r], e2);
-#pragma unroll
-                    for (int k = 0; k < NPL; ++k) pl[k][r >> 3][r & 7] = e2[k];
-                }
+                split_terms<P, NPL>(g, pl);
 #pragma unroll
                 for (int k = 0; k < NPL; ++k) {
 #pragma unroll
@@ -566,9 +564,12 @@ __device__ __forceinline__ void put_numbers(const RowNumbers& n, int64_t t, int6
     float w = n.grad ? n.grad[t] : 1.f;
     if (n.fin) w = ldexpf(w, n.fin[2]);
     float* o = (float*)(n.first + t / 32 * n.step) + t % 32;
-    o[32] = lse * kLog2e;
-    o[64] = y < v ? w : NAN;
-    o[96] = __int_as_float(y < v ? (int)y : -1);
+    const float l2 = lse * kLog2e;
+    o[kNumLse * 32] = y < v ? -l2 : NAN;
+    o[kNumRaw * 32] = n.grad ? n.grad[t] : 1.f;
+    o[kNumTerm * 32] = y < v ? log2f(fabsf(w)) - l2 : NAN;
+    o[kNumWeight * 32] = fabsf(w);
+    o[kNumTarget * 32] = __int_as_float(y < v ? (int)y : -1);
 }
 
 __global__ __launch_bounds__(256) void k_rows(ccdpp_softmax_t p, const float* lse, RowNumbers n) {
@@ -626,6 +627,7 @@ struct FinishSide {
     void* out;
     int64_t ldo;
     int which;                 // exponent in fin of the other operand, or -1
+    int terms;                 // G's exponent, or -1: fin[2]
 };
 
 // Four columns a thread; dx's blocks first.
@@ -636,7 +638,8 @@ __global__ __launch_bounds__(256) void k_finish(FinishSide x, FinishSide e, int6
     const int64_t first = is_x ? blockIdx.x : blockIdx.x - blocks_x, stride = is_x ? blocks_x : gridDim.x - blocks_x;
     const int quads = (cols + 3) / 4;
     // G's power of two and the other operand's are taken off one after the other: their product may be below any float
-    const float fg = fin ? ldexpf(1.f, -fin[2]) : 1.f, f = fin && a.which >= 0 ? ldexpf(scale, -fin[a.which]) : scale;
+    const float fg = a.terms >= 0 ? ldexpf(1.f, -a.terms) : fin ? ldexpf(1.f, -fin[2]) : 1.f;
+    const float f = fin && a.which >= 0 ? ldexpf(scale, -fin[a.which]) : scale;
     for (int64_t i = first * 256 + threadIdx.x; i < a.rows * quads; i += stride * 256) {
         const int64_t r = i / quads;
         const int c = (int)(i - r * quads) * 4;
@@ -663,7 +666,7 @@ struct Plan {
     int sl;                  // shares of the logits (small)
     int64_t x_tile, xlive_tile, e_tile;  // bundles (small)
     // offsets into the workspace
-    int64_t o_scale, o_xrow, o_fin, o_xf, o_ef, o_xl, o_o2, o_xt, o_et, o_g, o_gt, o_part, o_dx, o_de, bytes;
+    int64_t o_scale, o_xrow, o_fin, o_xf, o_ef, o_xl, o_o2, o_xn, o_xt, o_et, o_g, o_gt, o_part, o_dx, o_de, bytes;
 };
 
 constexpr int64_t kPieceBytes = int64_t(128) << 20;  // of G
@@ -688,16 +691,16 @@ Plan make_plan(const ccdpp_softmax_t& p, int call) {
     w.o_fin = take(64);
     w.o_xrow = take(w.scaled ? p.t * 4 : 0);
     if (w.small) {
-        // Shares so that about 512 blocks run, two a CU; none is shorter than four tiles.
-        const auto shares = [](int64_t kept, int64_t streamed) {
+        // Shares for blocks on all CUs, two to four each; none is shorter than four tiles.
+        const auto shares = [](int64_t kept, int64_t streamed, int64_t want) {
             const int64_t blocks = std::max<int64_t>(1, (kept + 3) / 4);
-            return (int)std::max<int64_t>(1, std::min<int64_t>((511 + blocks) / blocks, streamed / 4));
+            return (int)std::max<int64_t>(1, std::min<int64_t>((want - 1 + blocks) / blocks, streamed / 4));
         };
         w.ksd = small_steps(p.d);
         w.dp = w.dt * 32;
         w.x_tile = (w.planes * w.ksd + 1) * kBlk;
         w.e_tile = w.xlive_tile = w.x_tile + (w.grads ? w.planes * w.dt * 2 * kBlk : 0);
-        w.sl = shares(w.tt, w.vt), w.sx = shares(w.tt, w.vt), w.se = shares(w.vt, w.tt);
+        w.sl = shares(w.tt, w.vt, 1024), w.sx = shares(w.tt, w.vt, 512), w.se = shares(w.vt, w.tt, 512);
         w.o_xf = take(w.forward ? w.tt * w.x_tile : 0);
         w.o_ef = take(w.vt * w.e_tile);
         w.o_xl = take(w.grads ? w.tt * w.xlive_tile : 0);
@@ -721,6 +724,7 @@ Plan make_plan(const ccdpp_softmax_t& p, int call) {
     w.o_xf = take(w.planes * w.tt * w.ksd * kBlk);
     w.o_ef = take(w.planes * w.vt * w.ksd * kBlk);
     w.o_o2 = take(w.vt * 32 * 4);
+    w.o_xn = take(w.tt * 32 * 4);
     w.o_part = take(w.forward ? (w.vt + 7) / 8 * p.t * 8 : 0);
     if (w.grads) {
         w.o_xt = take(w.planes * w.dt * w.kst * kBlk);
@@ -769,6 +773,7 @@ int run_small(const ccdpp_softmax_t& p, const Plan& w, const Outs& o, const int3
     a.x = ws + w.o_xf, a.xlive = ws + w.o_xl, a.e = ws + w.o_ef;
     a.x_tile = w.x_tile, a.xlive_tile = w.xlive_tile, a.e_tile = w.e_tile;
     a.tt = w.tt, a.vt = w.vt, a.t = p.t, a.v = p.v;
+    a.offsets = p.offset != nullptr;
     a.splits = w.sl, a.splits_x = w.sx, a.splits_e = w.se;
     a.part = (float2*)(ws + w.o_part);
     a.dxp = (float*)(ws + w.o_dx), a.dep = (float*)(ws + w.o_de);
@@ -787,13 +792,13 @@ int run_small(const ccdpp_softmax_t& p, const Plan& w, const Outs& o, const int3
     a.blocks_x = o.dx ? (w.tt + 3) / 4 * w.sx : 0, a.blocks_e = o.de ? (w.vt + 3) / 4 * w.se : 0;
     const hipError_t e = launch_small_grads<P, NPL>(w.ksd, a, st);
     if (e != hipSuccess) return hip_fail(e, "gradients");
-    const FinishSide x = {a.dxp, w.sx, w.tt * 32 * w.dp, p.t, w.dp, o.dx, o.lddx, w.scaled ? 0 : -1};
-    const FinishSide t = {a.dep, w.se, w.vt * 32 * w.dp, p.v, w.dp, o.de, o.ldde, w.scaled ? 1 : -1};
+    const FinishSide x = {a.dxp, w.sx, w.tt * 32 * w.dp, p.t, w.dp, o.dx, o.lddx, w.scaled ? 0 : -1, kTermExp};
+    const FinishSide t = {a.dep, w.se, w.vt * 32 * w.dp, p.v, w.dp, o.de, o.ldde, w.scaled ? 1 : -1, -1};
     return finish<T>(x, t, p.d, p.scale, fin, st);
 }
 
 template <int DT>
-int run_wide(const ccdpp_softmax_t& p, const Plan& w, const Outs& out, const int32_t* fin, const Scales& sc, char* ws, hipStream_t st) {
+int run_wide(const ccdpp_softmax_t& p, const Plan& w, const Outs& out, const int32_t* fin, char* ws, hipStream_t st) {
     typedef typename Types<DT>::in T;
     typedef typename Types<DT>::op P;
     constexpr int NPL = Types<DT>::planes;
@@ -802,7 +807,7 @@ int run_wide(const ccdpp_softmax_t& p, const Plan& w, const Outs& out, const int
     z.a_plane = w.vt * w.ksd * kBlk, z.b_plane = w.tt * w.ksd * kBlk;
     z.a_tile = z.b_tile = (int64_t)w.ksd * kBlk;
     z.m_tiles = w.vt, z.n_tiles = w.tt, z.kb = w.ksd / 2, z.splits = 1;
-    z.t = p.t, z.v = p.v, z.scaled = w.scaled, z.x_row = sc.x_row, z.fin = fin, z.o2 = (const float*)(ws + w.o_o2);
+    z.t = p.t, z.v = p.v, z.xf = (const float*)(ws + w.o_xn), z.fin = fin, z.o2 = (const float*)(ws + w.o_o2);
     z.scale = p.scale, z.offset = p.offset, z.target = p.target, z.target_bits = p.target_bits;
     if (w.forward) {
         z.part = (float2*)(ws + w.o_part);
@@ -845,11 +850,11 @@ int run_wide(const ccdpp_softmax_t& p, const Plan& w, const Outs& out, const int
             k_gemm<P, NPL, EPI_OUT, T><<<dim3((unsigned)((nt + 7) / 8 * ((w.dt + 7) / 8)), w.se), 512, 0, st>>>(o);
             OPS_LAUNCH("dtable");
             if (!o.last)
-                if (int rc = finish<T>(FinishSide{}, FinishSide{o.out, w.se, o.out_split, n, w.dp, de, out.ldde, o.which}, p.d, p.scale, fin, st)) return rc;
+                if (int rc = finish<T>(FinishSide{}, FinishSide{o.out, w.se, o.out_split, n, w.dp, de, out.ldde, o.which, -1}, p.d, p.scale, fin, st)) return rc;
         }
     }
     if (out.dx && !dx_whole)
-        return finish<T>(FinishSide{(const float*)(ws + w.o_dx), w.sx, p.t * w.dp, p.t, w.dp, out.dx, out.lddx, w.scaled ? 0 : -1}, FinishSide{}, p.d, p.scale, fin, st);
+        return finish<T>(FinishSide{(const float*)(ws + w.o_dx), w.sx, p.t * w.dp, p.t, w.dp, out.dx, out.lddx, w.scaled ? 0 : -1, -1}, FinishSide{}, p.d, p.scale, fin, st);
     return CCDPP_OK;
 }
 
@@ -860,7 +865,7 @@ int run(const ccdpp_softmax_t& p, int call, const Outs& out, char* ws, hipStream
     const Plan w = make_plan(p, call);
     Scales sc;
     sc.e_part = (float*)(ws + w.o_scale), sc.x_part = sc.e_part + kParts, sc.g_part = sc.x_part + kParts;
-    sc.fin = (int32_t*)(ws + w.o_fin), sc.x_row = (int32_t*)(ws + w.o_xrow);
+    sc.fin = (int32_t*)(ws + w.o_fin), sc.x_row = (float*)(ws + w.o_xrow);
     const int32_t* fin = w.scaled || w.scale_g ? sc.fin : nullptr;
     if (w.scaled) k_scales<true><<<kParts, 1024, 0, st>>>(p, out.grad, sc, w.grads);
     else if (w.scale_g) k_scales<false><<<kParts, 1024, 0, st>>>(p, out.grad, sc, w.grads);
@@ -868,7 +873,7 @@ int run(const ccdpp_softmax_t& p, int call, const Outs& out, char* ws, hipStream
 
     PackArgs pk = {};
     pk.sc = sc, pk.scaled = w.scaled, pk.weights = w.scale_g;
-    pk.d = p.d, pk.ksd = w.ksd, pk.target = p.target, pk.target_bits = p.target_bits, pk.v = p.v, pk.scale = p.scale, pk.offset = p.offset;
+    pk.d = p.d, pk.ksd = w.ksd, pk.target = p.target, pk.target_bits = p.target_bits, pk.v = p.v, pk.scale = p.scale, pk.offset = p.offset, pk.grad = out.grad;
     PackSide &x = pk.x, &e = pk.e;
     x.src = p.x, x.ld = p.ldx, x.rows = p.t, x.tiles = w.tt;
     e.src = p.table, e.ld = p.ldt, e.rows = p.v, e.tiles = w.vt;
@@ -887,7 +892,8 @@ int run(const ccdpp_softmax_t& p, int call, const Outs& out, char* ws, hipStream
         }
     } else {
         x.nat = ws + w.o_xf, x.nat_plane = w.tt * w.ksd * kBlk;
-        e.nat = ws + w.o_ef, e.nat_plane = w.vt * w.ksd * kBlk, e.o2 = (float*)(ws + w.o_o2);
+        e.nat = ws + w.o_ef, e.nat_plane = w.vt * w.ksd * kBlk;
+        x.num = ws + w.o_xn, e.num = ws + w.o_o2, x.num_row = e.num_row = 128;
         x.nat_row = e.nat_row = w.ksd * kBlk;
         if (w.grads) {
             x.turned = ws + w.o_xt, x.turned_plane = w.dt * w.kst * kBlk, x.turned_d = w.kst * kBlk;
@@ -897,7 +903,7 @@ int run(const ccdpp_softmax_t& p, int call, const Outs& out, char* ws, hipStream
     }
     k_pack<DT><<<dim3((unsigned)(w.tt + w.vt), (p.d + 127) / 128), 256, 0, st>>>(pk);
     OPS_LAUNCH("pack");
-    return w.small ? run_small<DT>(p, w, out, fin, ws, st) : run_wide<DT>(p, w, out, fin, sc, ws, st);
+    return w.small ? run_small<DT>(p, w, out, fin, ws, st) : run_wide<DT>(p, w, out, fin, ws, st);
 }
 
 int check(const ccdpp_softmax_t* p, bool pointers) {
@@ -927,7 +933,7 @@ int call(const ccdpp_softmax_t* p, int what, float* loss, float* lse, const floa
     hipStream_t st = (hipStream_t)stream;
     const Outs out = {loss, lse, lse_in, grad, dx, lddx, de, ldde};
     if (p->t == 0) {  // no rows: the table's gradient is zero
-        const FinishSide none = {nullptr, 0, 0, p->v, 0, what == CCDPP_SOFTMAX_LOSS ? nullptr : de, ldde, -1};
+        const FinishSide none = {nullptr, 0, 0, p->v, 0, what == CCDPP_SOFTMAX_LOSS ? nullptr : de, ldde, -1, -1};
         return p->dtype == CCDPP_F32 ? finish<float>(FinishSide{}, none, p->d, 0.f, nullptr, st)
                                      : finish<_Float16>(FinishSide{}, none, p->d, 0.f, nullptr, st);  // all bits 0, as in bfloat16
     }

@@ -72,10 +72,10 @@ struct Kept {
     }
 };
 
-// 32 x 32 products of streamed rows (LDS) and kept rows: lane (n, h) gets kept row n, streamed rows 8 q + 4 h + r.
+// 32 x 32 products of streamed rows (LDS) and kept rows, on top of acc: lane (n, h) gets kept row n, streamed rows
+// 8 q + 4 h + r.
 template <class P, int NPL, int KS>
-__device__ __forceinline__ f32x16 tile_product(const char* slot, const Kept<P, NPL, KS>& kept, int lane) {
-    f32x16 acc = {};
+__device__ __forceinline__ f32x16 tile_product(const char* slot, const Kept<P, NPL, KS>& kept, int lane, f32x16 acc) {
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
         const typename P::vec a = *(const typename P::vec*)(slot + k * kBlk + lane * 16);
@@ -90,13 +90,67 @@ __device__ __forceinline__ f32x16 tile_product(const char* slot, const Kept<P, N
 }
 
 // The numbers `which` of this lane's 16 streamed rows.
-__device__ __forceinline__ void row_numbers(const char* rows, int which, int h, f32x4* o) {
+__device__ __forceinline__ f32x16 row_numbers(const char* rows, int which, int h) {
+    f32x16 o;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) o[q] = *(const f32x4*)(rows + which * 128 + (8 * q + 4 * h) * 4);
+    for (int q = 0; q < 4; ++q) {
+        const f32x4 v = *(const f32x4*)(rows + which * 128 + (8 * q + 4 * h) * 4);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[4 * q + r] = v[r];
+    }
+    return o;
+}
+
+// Sums of exponentials stay relative to `ref`, which the first tile sets; it is only moved when a tile's sum leaves
+// what 32 bits hold well (above 2^40), so that an entry costs its exponential and its addition alone: the logits'
+// accumulator starts at -ref.
+constexpr float kSumLimit = 1099511627776.f;
+
+// UNIT: the accumulated products are the logits (factor 1).
+template <class P, int NPL, int KS, bool UNIT>
+__device__ __forceinline__ void small_lse(const SmallArgs& a, int64_t split, const Kept<P, NPL, KS>& kept, float f, char* lds, float& ref_out,
+                                          float& sum_out) {
+    typedef Stream<P, NPL, KS, false> S;
+    const int lane = threadIdx.x & 63, h = lane >> 5;
+    float ref = 0.f, sum = 0.f;
+    bool set = false;
+    stream<S>(a.e, a.e_tile, a.vt * split / a.splits, a.vt * (split + 1) / a.splits, lds, [&](int64_t i, const char* slot) {
+        const bool offsets = a.offsets || i == a.vt - 1;  // the last tile's missing entries are -inf
+        f32x16 z;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) z[r] = UNIT ? -ref : 0.f;
+        if (UNIT && offsets) z += row_numbers(slot + S::kRows * kBlk, kNumOffset, h);
+        z = tile_product<P, NPL, KS>(slot, kept, lane, z);
+        if constexpr (!UNIT) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) z[r] = fmaf(z[r], f, -ref);
+            if (offsets) z += row_numbers(slot + S::kRows * kBlk, kNumOffset, h);
+        }
+        float s = 0.f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s += exp2_fast(z[r]);
+        if (__any(!set || !(s <= kSumLimit))) {
+            float m = -INFINITY;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) m = fmaxf(m, z[r]);
+            if (set) m = fmaxf(m, 0.f);
+            if (m != -INFINITY) {
+                s = 0.f;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s += exp2_fast(z[r] - m);
+                sum *= exp2_fast(-m);
+                ref += m;
+                set = true;
+            }
+        }
+        sum += s;
+    });
+    ref_out = set ? ref : -INFINITY;
+    sum_out = sum;
 }
 
 template <class P, int NPL, int KS>
-__global__ __launch_bounds__(256, 2) void k_small_lse(SmallArgs a) {
+__global__ __launch_bounds__(256, 4) void k_small_lse(SmallArgs a) {
     typedef Stream<P, NPL, KS, false> S;
     __shared__ __align__(16) char lds[S::kStages * S::kCount * kBlk];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 31, h = lane >> 5;
@@ -106,25 +160,10 @@ __global__ __launch_bounds__(256, 2) void k_small_lse(SmallArgs a) {
     const char* const mine = a.x + tile * a.x_tile;
     Kept<P, NPL, KS> kept;
     kept.load(mine, lane);
-    const float f = *(const float*)(mine + S::kRows * kBlk + n * 4);
-    float top = -INFINITY, sum = 0.f;
-    stream<S>(a.e, a.e_tile, a.vt * split / a.splits, a.vt * (split + 1) / a.splits, lds, [&](int64_t, const char* slot) {
-        f32x4 o[4];
-        row_numbers(slot + S::kRows * kBlk, 0, h, o);
-        f32x16 z = tile_product<P, NPL, KS>(slot, kept, lane);
-        float m = top;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            z[r] = fmaf(z[r], f, o[r >> 2][r & 3]);
-            m = fmaxf(m, z[r]);
-        }
-        const float ref = m == -INFINITY ? 0.f : m;
-        float s = 0.f;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s += exp2_fast(z[r] - ref);
-        sum = fmaf(sum, exp2_fast(top - ref), s);
-        top = m;
-    });
+    const float f = *(const float*)(mine + S::kRows * kBlk + kNumFactor * 128 + n * 4);
+    float top, sum;
+    if (NPL == 2 && __all(f == 1.f)) small_lse<P, NPL, KS, true>(a, split, kept, f, lds, top, sum);
+    else small_lse<P, NPL, KS, false>(a, split, kept, f, lds, top, sum);
     const float top2 = __shfl_xor(top, 32), sum2 = __shfl_xor(sum, 32);
     const float m = fmaxf(top, top2), ref = m == -INFINITY ? 0.f : m;
     sum = sum * exp2_fast(top - ref) + sum2 * exp2_fast(top2 - ref);
@@ -133,62 +172,70 @@ __global__ __launch_bounds__(256, 2) void k_small_lse(SmallArgs a) {
 }
 
 // One side's gradients for 128 kept rows: out += turned streamed rows x G.  ITEMS: the kept rows are the table's.
+// The accumulator of the logits starts at what is added to them, so that a term costs its exponential alone.
 template <class P, int NPL, int KS, bool ITEMS>
-__device__ __forceinline__ void small_grad(const SmallArgs& a, int64_t block, char* lds) {
+__device__ __forceinline__ void small_terms(const SmallArgs& a, int64_t tile, int64_t split, const Kept<P, NPL, KS>& kept, const float* own, char* lds,
+                                            f32x16* out) {
     typedef Stream<P, NPL, KS, true> S;
     constexpr int DT = S::DT;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 31, h = lane >> 5;
-    const int64_t tiles = ITEMS ? a.vt : a.tt, others = ITEMS ? a.tt : a.vt;
-    const int64_t splits = ITEMS ? a.splits_e : a.splits_x;
-    const int64_t kept_blocks = (tiles + 3) / 4;
-    const int64_t kb = block % kept_blocks, split = block / kept_blocks;
-    const int64_t at = kb * 4 + wave, tile = min(at, tiles - 1);
-    const char* const mine = ITEMS ? a.e + tile * a.e_tile : a.xlive + tile * a.xlive_tile;
-    Kept<P, NPL, KS> kept;
-    kept.load(mine, lane);
-    const float* const own = (const float*)(mine + S::kRows * kBlk) + n;
-    const float first = own[0];  // offset (table) or factor (x)
-    const float own_l2 = ITEMS ? 0.f : own[32], own_w = ITEMS ? 0.f : own[64];
-    const int own_y = ITEMS ? 0 : __float_as_int(own[96]);
-    f32x16 out[DT] = {};
+    const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
+    const int64_t others = ITEMS ? a.tt : a.vt, splits = ITEMS ? a.splits_e : a.splits_x;
+    const float factor = own[kNumFactor * 32];                                     // x
+    const float base = ITEMS ? own[kNumOffset * 32] : own[kNumLse * 32] + kTermExp;  // what this row adds to its logits
+    const int own_y = ITEMS ? 0 : __float_as_int(own[kNumTarget * 32]);
+    const bool any_base = !ITEMS || __any(base != 0.f);
+    const bool own_unit = __all(factor == 1.f || factor == 0.f);  // 0: a row that does not count
     stream<S>(ITEMS ? a.xlive : a.e, ITEMS ? a.xlive_tile : a.e_tile, others * split / splits, others * (split + 1) / splits, lds,
               [&](int64_t i, const char* slot) {
         const char* const rows = slot + S::kRows * kBlk;
-        const f32x16 z = tile_product<P, NPL, KS>(slot, kept, lane);
-        float g[16];
-        if constexpr (ITEMS) {
-            f32x4 f[4], l2[4], w[4];
-            row_numbers(rows, 0, h, f);
-            row_numbers(rows, 1, h, l2);
-            row_numbers(rows, 2, h, w);
+        const auto added = [&]() {
+            f32x16 add;
+            if constexpr (ITEMS) {
+                add = row_numbers(rows, kNumTerm, h);
+                if (any_base) add += base;
+            } else {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) g[r] = w[r >> 2][r & 3] * exp2_fast(fmaf(z[r], f[r >> 2][r & 3], first) - l2[r >> 2][r & 3]);
-            const int y = ((const int*)rows)[96 + n] - (int)(tile * 32);
+                for (int r = 0; r < 16; ++r) add[r] = base;
+                if (a.offsets || i == a.vt - 1) add += row_numbers(rows, kNumOffset, h);
+            }
+            return add;
+        };
+        bool unit = NPL == 2 && own_unit;
+        if constexpr (ITEMS && NPL == 2) {
+            const float f = ((const float*)rows)[kNumFactor * 32 + n];
+            unit = __all(f == 1.f || f == 0.f);
+        }
+        f32x16 z = {};
+        if (unit) z = added();
+        z = tile_product<P, NPL, KS>(slot, kept, lane, z);
+        if (!unit) {
+            const f32x16 add = added();
+            const f32x16 f = ITEMS ? row_numbers(rows, kNumFactor, h) : f32x16{};
+#pragma unroll
+            for (int r = 0; r < 16; ++r) z[r] = fmaf(z[r], ITEMS ? f[r] : factor, add[r]);
+        }
+        float g[16];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) g[r] = exp2_fast(z[r]);
+        if constexpr (ITEMS) {
+            const int y = ((const int*)rows)[kNumTarget * 32 + n] - (int)(tile * 32);
             if (__any(y >= 0 && y < 32)) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (((const int*)rows)[96 + 8 * (r >> 2) + 4 * h + (r & 3)] == (int)(tile * 32) + n) g[r] -= w[r >> 2][r & 3];
+                for (int r = 0; r < 16; ++r) {
+                    const int row = 8 * (r >> 2) + 4 * h + (r & 3);
+                    if (((const int*)rows)[kNumTarget * 32 + row] == (int)(tile * 32) + n) g[r] -= ((const float*)rows)[kNumWeight * 32 + row];
+                }
             }
         } else {
-            f32x4 o[4];
-            row_numbers(rows, 0, h, o);
-#pragma unroll
-            for (int r = 0; r < 16; ++r) g[r] = own_w * exp2_fast(fmaf(z[r], first, o[r >> 2][r & 3]) - own_l2);
             const int y = own_y - (int)(i * 32);
             if (__any(y >= 0 && y < 32)) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    if (y == 8 * (r >> 2) + 4 * h + (r & 3)) g[r] -= own_w;
+                    if (y == 8 * (r >> 2) + 4 * h + (r & 3)) g[r] -= (float)(1 << kTermExp);
             }
         }
         typename P::vec pl[NPL][2];
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            typename P::elem e[2];
-            to_planes<P, NPL>(g[r], e);
-#pragma unroll
-            for (int p = 0; p < NPL; ++p) pl[p][r >> 3][r & 7] = e[p];
-        }
+        split_terms<P, NPL>(g, pl);
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -202,7 +249,25 @@ __device__ __forceinline__ void small_grad(const SmallArgs& a, int64_t block, ch
                 }
             }
     });
+}
+
+template <class P, int NPL, int KS, bool ITEMS>
+__device__ __forceinline__ void small_grad(const SmallArgs& a, int64_t block, char* lds) {
+    typedef Stream<P, NPL, KS, true> S;
+    constexpr int DT = S::DT;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 31, h = lane >> 5;
+    const int64_t tiles = ITEMS ? a.vt : a.tt;
+    const int64_t kept_blocks = (tiles + 3) / 4;
+    const int64_t kb = block % kept_blocks, split = block / kept_blocks;
+    const int64_t at = kb * 4 + wave, tile = min(at, tiles - 1);
+    const char* const mine = ITEMS ? a.e + tile * a.e_tile : a.xlive + tile * a.xlive_tile;
+    Kept<P, NPL, KS> kept;
+    kept.load(mine, lane);
+    const float* const own = (const float*)(mine + S::kRows * kBlk) + n;
+    f32x16 out[DT] = {};
+    small_terms<P, NPL, KS, ITEMS>(a, tile, split, kept, own, lds, out);
     if (at >= tiles) return;
+    const float w = ITEMS ? 1.f : own[kNumRaw * 32];
     float* const to = (ITEMS ? a.dep : a.dxp) + ((split * tiles + tile) * 32 + n) * (DT * 32) + 4 * h;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
@@ -210,7 +275,7 @@ __device__ __forceinline__ void small_grad(const SmallArgs& a, int64_t block, ch
         for (int q = 0; q < 4; ++q) {
             f32x4 v;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) v[r] = out[d][q * 4 + r];
+            for (int r = 0; r < 4; ++r) v[r] = out[d][q * 4 + r] * w;
             *(f32x4*)(to + d * 32 + q * 8) = v;
         }
 }
