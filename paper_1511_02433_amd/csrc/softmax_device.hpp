@@ -128,21 +128,34 @@ constexpr int kTermExp = 13;  // of dx's terms, which leave the row's weight to 
 
 constexpr int kSmallD = 128;
 
+// A product of few factors is cut by tiles: kept blocks of 128 rows times streamed tiles of 32, in that order, in shares
+// of `len` tiles, a block each, so that all blocks work equally long.  A share may end in one kept block and go on in the
+// next; every kept block sums the shares that touch it, in order.
+struct Shares {
+    int64_t tiles;   // streamed tiles of each kept block
+    int64_t len;     // tiles of a share
+    int64_t blocks;  // shares
+    __host__ __device__ int64_t first(int64_t kept) const { return kept * tiles / len; }
+    __host__ __device__ int count(int64_t kept) const { return (int)(((kept + 1) * tiles - 1) / len - first(kept) + 1); }
+    __host__ __device__ int64_t most() const { return tiles > 0 ? (tiles + len - 2) / len + 1 : 0; }  // of count()
+};
+
 struct SmallArgs {
     const char *x, *xlive, *e;          // bundles: x without turned rows; x with them, rows that do not count zeroed; the table
     int64_t x_tile, xlive_tile, e_tile; // bytes of one bundle
     int64_t tt, vt;                     // bundles
     int64_t t, v;
     int offsets;                        // whether the table has offsets
-    int splits, splits_x, splits_e;     // shares of the streamed side: logits, dx, de
-    int64_t blocks_x;                   // blocks of k_small_grads that compute dx; the others compute de
-    int64_t blocks_e;
-    float2* part;                       // [split][t]
-    float *dxp, *dep;                   // [split][32 tiles][32 columns of d each]
+    Shares lse, dx, de;                 // dx.blocks or de.blocks 0: not asked for
+    float2* part;                       // [share of the kept block][t]
+    float *dxp, *dep;                   // [share of the kept block][rows, in tiles][d, in blocks of 32]
 };
 
 // ksd: steps of 16 over d that the kernels were built for (small_steps).  Return launch errors.
 int small_steps(int d);
+// Blocks that a CU holds, by registers and LDS.
+constexpr int small_lse_per_cu(int planes, int ks) { return planes * ks > 12 ? 3 : 4; }
+constexpr int small_grads_per_cu(int planes, int ks) { return planes * ks > 8 ? 2 : 3; }
 template <class P, int NPL> hipError_t launch_small_lse(int ksd, const SmallArgs& a, hipStream_t st);
 template <class P, int NPL> hipError_t launch_small_grads(int ksd, const SmallArgs& a, hipStream_t st);
 

@@ -577,14 +577,15 @@ __global__ __launch_bounds__(256) void k_rows(ccdpp_softmax_t p, const float* ls
     if (t < p.t) put_numbers(n, t, load_target(p.target, p.target_bits, t), p.v, p.offset, lse[t]);
 }
 
-// A wave per row: joins the (max, sum) pairs of its pieces, and takes the target's logit from x and the table.
+// A wave per row: joins the (max, sum) pairs of its pieces (0: of its shares), and takes the target's logit from x and the table.
 template <class T>
-__global__ __launch_bounds__(256) void k_loss(ccdpp_softmax_t p, const float2* part, int64_t pieces, float* loss, float* lse, RowNumbers num) {
+__global__ __launch_bounds__(256) void k_loss(ccdpp_softmax_t p, const float2* part, int64_t pieces, Shares shares, float* loss, float* lse, RowNumbers num) {
     const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (t >= p.t) return;
     const int lane = threadIdx.x & 63;
     float m = -INFINITY, s = 0.f;
     bool nan = false;
+    if (!pieces) pieces = shares.count(t / 128);
     for (int64_t i = lane; i < pieces; i += 64) {
         const float2 q = part[i * p.t + t];
         const float top = fmaxf(m, q.x), ref = top == -INFINITY ? 0.f : top;
@@ -622,12 +623,13 @@ __global__ __launch_bounds__(256) void k_loss(ccdpp_softmax_t p, const float2* p
 // One gradient from the partial sums of its shares, in the caller's type and strides.
 struct FinishSide {
     const float* part;
-    int splits;
+    int splits;                // partial sums of every row, unless `shares` counts them
     int64_t split, rows, ldp;  // ldp: a multiple of 4
     void* out;
     int64_t ldo;
     int which;                 // exponent in fin of the other operand, or -1
     int terms;                 // G's exponent, or -1: fin[2]
+    Shares shares;
 };
 
 // Four columns a thread; dx's blocks first.
@@ -643,8 +645,18 @@ __global__ __launch_bounds__(256) void k_finish(FinishSide x, FinishSide e, int6
     for (int64_t i = first * 256 + threadIdx.x; i < a.rows * quads; i += stride * 256) {
         const int64_t r = i / quads;
         const int c = (int)(i - r * quads) * 4;
+        const float* from = a.part + r * a.ldp + c;
         f32x4 v = {};
-        for (int s = 0; s < a.splits; ++s) v += *(const f32x4*)(a.part + s * a.split + r * a.ldp + c);
+        const int splits = a.shares.len ? a.shares.count(r / 128) : a.splits;
+        int s = 0;
+        for (; s + 8 <= splits; s += 8) {  // eight reads in flight
+            f32x4 q[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) q[k] = *(const f32x4*)(from + (s + k) * a.split);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v += q[k];
+        }
+        for (; s < splits; ++s) v += *(const f32x4*)(from + s * a.split);
         T* o = (T*)a.out + r * a.ldo + c;
         for (int j = 0; j < 4; ++j)
             if (c + j < cols) o[j] = (T)(v[j] * fg * f);
@@ -662,8 +674,8 @@ struct Plan {
     int64_t kst, ksv;        // over rows, over the whole table
     int64_t vc;              // table entries per piece of the gradients (a multiple of 256)
     int64_t dp;              // columns of partial sums
-    int sx, se;              // shares of the two gradients' contractions
-    int sl;                  // shares of the logits (small)
+    int sx, se;              // splits of the two gradients' contractions
+    Shares lse, dx, de;      // (small)
     int64_t x_tile, xlive_tile, e_tile;  // bundles (small)
     // offsets into the workspace
     int64_t o_scale, o_xrow, o_fin, o_xf, o_ef, o_xl, o_o2, o_xn, o_xt, o_et, o_g, o_gt, o_part, o_dx, o_de, bytes;
@@ -691,22 +703,27 @@ Plan make_plan(const ccdpp_softmax_t& p, int call) {
     w.o_fin = take(64);
     w.o_xrow = take(w.scaled ? p.t * 4 : 0);
     if (w.small) {
-        // Shares for blocks on all CUs, two to four each; none is shorter than four tiles.
-        const auto shares = [](int64_t kept, int64_t streamed, int64_t want) {
-            const int64_t blocks = std::max<int64_t>(1, (kept + 3) / 4);
-            return (int)std::max<int64_t>(1, std::min<int64_t>((want - 1 + blocks) / blocks, streamed / 4));
+        // As many shares as blocks run at once (a share has four tiles at least).
+        const auto shares = [](int64_t kept_tiles, int64_t tiles, int64_t want) {
+            const int64_t total = (kept_tiles + 3) / 4 * tiles;
+            Shares s = {tiles, std::max<int64_t>((total + want - 1) / want, std::min<int64_t>(tiles, 4)), 0};
+            s.blocks = total ? (total + s.len - 1) / s.len : 0;
+            return s;
         };
         w.ksd = small_steps(p.d);
         w.dp = w.dt * 32;
         w.x_tile = (w.planes * w.ksd + 1) * kBlk;
         w.e_tile = w.xlive_tile = w.x_tile + (w.grads ? w.planes * w.dt * 2 * kBlk : 0);
-        w.sl = shares(w.tt, w.vt, 1024), w.sx = shares(w.tt, w.vt, 512), w.se = shares(w.vt, w.tt, 512);
+        constexpr int kCus = 256;
+        const int half = kCus * small_grads_per_cu(w.planes, w.ksd) / 2;  // dx and de run in one launch
+        w.lse = shares(w.tt, w.vt, kCus * small_lse_per_cu(w.planes, w.ksd));
+        w.dx = shares(w.tt, w.vt, half), w.de = shares(w.vt, w.tt, half);
         w.o_xf = take(w.forward ? w.tt * w.x_tile : 0);
         w.o_ef = take(w.vt * w.e_tile);
         w.o_xl = take(w.grads ? w.tt * w.xlive_tile : 0);
-        w.o_part = take(w.forward ? w.sl * p.t * 8 : 0);
-        w.o_dx = take(w.grads ? w.sx * w.tt * 32 * w.dp * 4 : 0);
-        w.o_de = take(w.grads ? w.se * w.vt * 32 * w.dp * 4 : 0);
+        w.o_part = take(w.forward ? w.lse.most() * p.t * 8 : 0);
+        w.o_dx = take(w.grads ? w.dx.most() * w.tt * 32 * w.dp * 4 : 0);
+        w.o_de = take(w.grads ? w.de.most() * w.vt * 32 * w.dp * 4 : 0);
         w.bytes = at;
         return w;
     }
@@ -774,7 +791,9 @@ int run_small(const ccdpp_softmax_t& p, const Plan& w, const Outs& o, const int3
     a.x_tile = w.x_tile, a.xlive_tile = w.xlive_tile, a.e_tile = w.e_tile;
     a.tt = w.tt, a.vt = w.vt, a.t = p.t, a.v = p.v;
     a.offsets = p.offset != nullptr;
-    a.splits = w.sl, a.splits_x = w.sx, a.splits_e = w.se;
+    a.lse = w.lse, a.dx = w.dx, a.de = w.de;
+    if (!o.dx) a.dx.blocks = 0;
+    if (!o.de) a.de.blocks = 0;
     a.part = (float2*)(ws + w.o_part);
     a.dxp = (float*)(ws + w.o_dx), a.dep = (float*)(ws + w.o_de);
     RowNumbers num = {};
@@ -782,18 +801,17 @@ int run_small(const ccdpp_softmax_t& p, const Plan& w, const Outs& o, const int3
     if (w.forward) {
         const hipError_t e = launch_small_lse<P, NPL>(w.ksd, a, st);
         if (e != hipSuccess) return hip_fail(e, "logits");
-        k_loss<T><<<(unsigned)((p.t + 3) / 4), 256, 0, st>>>(p, a.part, w.sl, o.loss, o.lse, num);
+        k_loss<T><<<(unsigned)((p.t + 3) / 4), 256, 0, st>>>(p, a.part, 0, a.lse, o.loss, o.lse, num);
         OPS_LAUNCH("loss");
     } else {
         k_rows<<<(unsigned)((p.t + 255) / 256), 256, 0, st>>>(p, o.lse_in, num);
         OPS_LAUNCH("rows");
     }
     if (!w.grads) return CCDPP_OK;
-    a.blocks_x = o.dx ? (w.tt + 3) / 4 * w.sx : 0, a.blocks_e = o.de ? (w.vt + 3) / 4 * w.se : 0;
     const hipError_t e = launch_small_grads<P, NPL>(w.ksd, a, st);
     if (e != hipSuccess) return hip_fail(e, "gradients");
-    const FinishSide x = {a.dxp, w.sx, w.tt * 32 * w.dp, p.t, w.dp, o.dx, o.lddx, w.scaled ? 0 : -1, kTermExp};
-    const FinishSide t = {a.dep, w.se, w.vt * 32 * w.dp, p.v, w.dp, o.de, o.ldde, w.scaled ? 1 : -1, -1};
+    const FinishSide x = {a.dxp, 0, w.tt * 32 * w.dp, p.t, w.dp, o.dx, o.lddx, w.scaled ? 0 : -1, kTermExp, w.dx};
+    const FinishSide t = {a.dep, 0, w.vt * 32 * w.dp, p.v, w.dp, o.de, o.ldde, w.scaled ? 1 : -1, -1, w.de};
     return finish<T>(x, t, p.d, p.scale, fin, st);
 }
 
@@ -814,7 +832,7 @@ int run_wide(const ccdpp_softmax_t& p, const Plan& w, const Outs& out, const int
         const int64_t blocks = (w.vt + 7) / 8 * ((w.tt + 7) / 8);
         k_gemm<P, NPL, EPI_LSE, T><<<(unsigned)blocks, 512, 0, st>>>(z);
         OPS_LAUNCH("logits");
-        k_loss<T><<<(unsigned)((p.t + 3) / 4), 256, 0, st>>>(p, z.part, (w.vt + 7) / 8, out.loss, out.lse, RowNumbers{});
+        k_loss<T><<<(unsigned)((p.t + 3) / 4), 256, 0, st>>>(p, z.part, (w.vt + 7) / 8, Shares{}, out.loss, out.lse, RowNumbers{});
         OPS_LAUNCH("loss");
     }
     if (!w.grads) return CCDPP_OK;
@@ -850,11 +868,11 @@ int run_wide(const ccdpp_softmax_t& p, const Plan& w, const Outs& out, const int
             k_gemm<P, NPL, EPI_OUT, T><<<dim3((unsigned)((nt + 7) / 8 * ((w.dt + 7) / 8)), w.se), 512, 0, st>>>(o);
             OPS_LAUNCH("dtable");
             if (!o.last)
-                if (int rc = finish<T>(FinishSide{}, FinishSide{o.out, w.se, o.out_split, n, w.dp, de, out.ldde, o.which, -1}, p.d, p.scale, fin, st)) return rc;
+                if (int rc = finish<T>(FinishSide{}, FinishSide{o.out, w.se, o.out_split, n, w.dp, de, out.ldde, o.which, -1, {}}, p.d, p.scale, fin, st)) return rc;
         }
     }
     if (out.dx && !dx_whole)
-        return finish<T>(FinishSide{(const float*)(ws + w.o_dx), w.sx, p.t * w.dp, p.t, w.dp, out.dx, out.lddx, w.scaled ? 0 : -1, -1}, FinishSide{}, p.d, p.scale, fin, st);
+        return finish<T>(FinishSide{(const float*)(ws + w.o_dx), w.sx, p.t * w.dp, p.t, w.dp, out.dx, out.lddx, w.scaled ? 0 : -1, -1, {}}, FinishSide{}, p.d, p.scale, fin, st);
     return CCDPP_OK;
 }
 
@@ -933,7 +951,7 @@ int call(const ccdpp_softmax_t* p, int what, float* loss, float* lse, const floa
     hipStream_t st = (hipStream_t)stream;
     const Outs out = {loss, lse, lse_in, grad, dx, lddx, de, ldde};
     if (p->t == 0) {  // no rows: the table's gradient is zero
-        const FinishSide none = {nullptr, 0, 0, p->v, 0, what == CCDPP_SOFTMAX_LOSS ? nullptr : de, ldde, -1, -1};
+        const FinishSide none = {nullptr, 0, 0, p->v, 0, what == CCDPP_SOFTMAX_LOSS ? nullptr : de, ldde, -1, -1, {}};
         return p->dtype == CCDPP_F32 ? finish<float>(FinishSide{}, none, p->d, 0.f, nullptr, st)
                                      : finish<_Float16>(FinishSide{}, none, p->d, 0.f, nullptr, st);  // all bits 0, as in bfloat16
     }

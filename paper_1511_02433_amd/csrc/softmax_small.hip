@@ -58,7 +58,20 @@ __device__ __forceinline__ void stream(const char* from, int64_t tile_bytes, int
         body(i, lds + slot * (S::kCount * kBlk));
         slot = slot + 1 == S::kStages ? 0 : slot + 1;
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();  // the next stream may take the slots
+    asm volatile("" ::: "memory");
+}
+
+// Calls body(kept block, first tile, last tile, place among the kept block's shares) for the parts of a share.
+template <class F>
+__device__ __forceinline__ void each_part(const Shares& s, int64_t share, int64_t kept_blocks, F&& body) {
+    const int64_t end = min((share + 1) * s.len, kept_blocks * s.tiles);
+    for (int64_t u = share * s.len; u < end;) {
+        const int64_t kb = u / s.tiles, first = u - kb * s.tiles, n = min(s.tiles - first, end - u);
+        body(kb, first, first + n, share - s.first(kb));
+        u += n;
+    }
 }
 
 template <class P, int NPL, int KS>
@@ -72,20 +85,38 @@ struct Kept {
     }
 };
 
+// Order of a run of N x (READS reads from LDS, PRODUCTS products): the reads AHEAD of the products they are for, the first
+// HAD of them made before.
+template <int N, int READS, int PRODUCTS, int AHEAD, int HAD>
+__device__ __forceinline__ void interleave() {
+    constexpr int A = AHEAD < N ? AHEAD : N;
+    if constexpr (A > HAD) __builtin_amdgcn_sched_group_barrier(0x100, READS * (A - HAD), 0);
+#pragma unroll
+    for (int i = 0; i < N - A; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, PRODUCTS, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, PRODUCTS * A, 0);
+}
+
 // 32 x 32 products of streamed rows (LDS) and kept rows, on top of acc: lane (n, h) gets kept row n, streamed rows
 // 8 q + 4 h + r.
 template <class P, int NPL, int KS>
 __device__ __forceinline__ f32x16 tile_product(const char* slot, const Kept<P, NPL, KS>& kept, int lane, f32x16 acc) {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
         const typename P::vec a = *(const typename P::vec*)(slot + k * kBlk + lane * 16);
         acc = P::mfma(a, kept.f[0][k], acc);
         if constexpr (NPL == 2) {
-            acc = P::mfma(a, kept.f[1][k], acc);
             const typename P::vec b = *(const typename P::vec*)(slot + (KS + k) * kBlk + lane * 16);
+            acc = P::mfma(a, kept.f[1][k], acc);
             acc = P::mfma(b, kept.f[0][k], acc);
         }
     }
+    interleave<KS, NPL, NPL == 2 ? 3 : 1, NPL == 2 ? 2 : 4, 0>();
+    __builtin_amdgcn_sched_barrier(0);
     return acc;
 }
 
@@ -108,13 +139,13 @@ constexpr float kSumLimit = 1099511627776.f;
 
 // UNIT: the accumulated products are the logits (factor 1).
 template <class P, int NPL, int KS, bool UNIT>
-__device__ __forceinline__ void small_lse(const SmallArgs& a, int64_t split, const Kept<P, NPL, KS>& kept, float f, char* lds, float& ref_out,
-                                          float& sum_out) {
+__device__ __forceinline__ void small_lse(const SmallArgs& a, int64_t first, int64_t last, const Kept<P, NPL, KS>& kept, float f, char* lds,
+                                          float& ref_out, float& sum_out) {
     typedef Stream<P, NPL, KS, false> S;
     const int lane = threadIdx.x & 63, h = lane >> 5;
     float ref = 0.f, sum = 0.f;
     bool set = false;
-    stream<S>(a.e, a.e_tile, a.vt * split / a.splits, a.vt * (split + 1) / a.splits, lds, [&](int64_t i, const char* slot) {
+    stream<S>(a.e, a.e_tile, first, last, lds, [&](int64_t i, const char* slot) {
         const bool offsets = a.offsets || i == a.vt - 1;  // the last tile's missing entries are -inf
         f32x16 z;
 #pragma unroll
@@ -150,43 +181,41 @@ __device__ __forceinline__ void small_lse(const SmallArgs& a, int64_t split, con
 }
 
 template <class P, int NPL, int KS>
-__global__ __launch_bounds__(256, 4) void k_small_lse(SmallArgs a) {
+__global__ __launch_bounds__(256, small_lse_per_cu(NPL, KS)) void k_small_lse(SmallArgs a) {
     typedef Stream<P, NPL, KS, false> S;
     __shared__ __align__(16) char lds[S::kStages * S::kCount * kBlk];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 31, h = lane >> 5;
-    const int64_t kept_blocks = (a.tt + 3) / 4;
-    const int64_t kb = blockIdx.x % kept_blocks, split = blockIdx.x / kept_blocks;
-    const int64_t tile = min(kb * 4 + wave, a.tt - 1);
-    const char* const mine = a.x + tile * a.x_tile;
-    Kept<P, NPL, KS> kept;
-    kept.load(mine, lane);
-    const float f = *(const float*)(mine + S::kRows * kBlk + kNumFactor * 128 + n * 4);
-    float top, sum;
-    if (NPL == 2 && __all(f == 1.f)) small_lse<P, NPL, KS, true>(a, split, kept, f, lds, top, sum);
-    else small_lse<P, NPL, KS, false>(a, split, kept, f, lds, top, sum);
-    const float top2 = __shfl_xor(top, 32), sum2 = __shfl_xor(sum, 32);
-    const float m = fmaxf(top, top2), ref = m == -INFINITY ? 0.f : m;
-    sum = sum * exp2_fast(top - ref) + sum2 * exp2_fast(top2 - ref);
-    const int64_t t = (kb * 4 + wave) * 32 + n;
-    if (h == 0 && t < a.t) a.part[split * a.t + t] = make_float2(m, sum);
+    each_part(a.lse, blockIdx.x, (a.tt + 3) / 4, [&](int64_t kb, int64_t first, int64_t last, int64_t place) {
+        const int64_t tile = min(kb * 4 + wave, a.tt - 1);
+        const char* const mine = a.x + tile * a.x_tile;
+        Kept<P, NPL, KS> kept;
+        kept.load(mine, lane);
+        const float f = *(const float*)(mine + S::kRows * kBlk + kNumFactor * 128 + n * 4);
+        float top, sum;
+        if (NPL == 2 && __all(f == 1.f)) small_lse<P, NPL, KS, true>(a, first, last, kept, f, lds, top, sum);
+        else small_lse<P, NPL, KS, false>(a, first, last, kept, f, lds, top, sum);
+        const float top2 = __shfl_xor(top, 32), sum2 = __shfl_xor(sum, 32);
+        const float m = fmaxf(top, top2), ref = m == -INFINITY ? 0.f : m;
+        sum = sum * exp2_fast(top - ref) + sum2 * exp2_fast(top2 - ref);
+        const int64_t t = (kb * 4 + wave) * 32 + n;
+        if (h == 0 && t < a.t) a.part[place * a.t + t] = make_float2(m, sum);
+    });
 }
 
 // One side's gradients for 128 kept rows: out += turned streamed rows x G.  ITEMS: the kept rows are the table's.
 // The accumulator of the logits starts at what is added to them, so that a term costs its exponential alone.
 template <class P, int NPL, int KS, bool ITEMS>
-__device__ __forceinline__ void small_terms(const SmallArgs& a, int64_t tile, int64_t split, const Kept<P, NPL, KS>& kept, const float* own, char* lds,
+__device__ __forceinline__ void small_terms(const SmallArgs& a, int64_t tile, int64_t first, int64_t last, const Kept<P, NPL, KS>& kept, const float* own, char* lds,
                                             f32x16* out) {
     typedef Stream<P, NPL, KS, true> S;
     constexpr int DT = S::DT;
     const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
-    const int64_t others = ITEMS ? a.tt : a.vt, splits = ITEMS ? a.splits_e : a.splits_x;
     const float factor = own[kNumFactor * 32];                                     // x
     const float base = ITEMS ? own[kNumOffset * 32] : own[kNumLse * 32] + kTermExp;  // what this row adds to its logits
     const int own_y = ITEMS ? 0 : __float_as_int(own[kNumTarget * 32]);
     const bool any_base = !ITEMS || __any(base != 0.f);
     const bool own_unit = __all(factor == 1.f || factor == 0.f);  // 0: a row that does not count
-    stream<S>(ITEMS ? a.xlive : a.e, ITEMS ? a.xlive_tile : a.e_tile, others * split / splits, others * (split + 1) / splits, lds,
-              [&](int64_t i, const char* slot) {
+    stream<S>(ITEMS ? a.xlive : a.e, ITEMS ? a.xlive_tile : a.e_tile, first, last, lds, [&](int64_t i, const char* slot) {
         const char* const rows = slot + S::kRows * kBlk;
         const auto added = [&]() {
             f32x16 add;
@@ -214,6 +243,16 @@ __device__ __forceinline__ void small_terms(const SmallArgs& a, int64_t tile, in
 #pragma unroll
             for (int r = 0; r < 16; ++r) z[r] = fmaf(z[r], ITEMS ? f[r] : factor, add[r]);
         }
+        // The first turned fragments arrive while the terms are computed.
+        constexpr int kAhead = NPL == 2 ? 2 : 4;
+        typename P::vec tf[NPL][DT * 2];
+        const auto turned = [&](int i) {
+#pragma unroll
+            for (int p = 0; p < NPL; ++p) tf[p][i] = *(const typename P::vec*)(slot + (S::kTurned + p * DT * 2 + i) * kBlk + lane * 16);
+        };
+#pragma unroll
+        for (int i = 0; i < (kAhead < DT * 2 ? kAhead : DT * 2); ++i) turned(i);
+        asm volatile("" ::: "memory");
         float g[16];
 #pragma unroll
         for (int r = 0; r < 16; ++r) g[r] = exp2_fast(z[r]);
@@ -236,64 +275,66 @@ __device__ __forceinline__ void small_terms(const SmallArgs& a, int64_t tile, in
         }
         typename P::vec pl[NPL][2];
         split_terms<P, NPL>(g, pl);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
+        for (int i = kAhead; i < DT * 2; ++i) turned(i);
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                const typename P::vec b = *(const typename P::vec*)(slot + (S::kTurned + d * 2 + s) * kBlk + lane * 16);
-                out[d] = P::mfma(b, pl[0][s], out[d]);
-                if constexpr (NPL == 2) {
-                    out[d] = P::mfma(b, pl[1][s], out[d]);
-                    const typename P::vec c = *(const typename P::vec*)(slot + (S::kTurned + (DT + d) * 2 + s) * kBlk + lane * 16);
-                    out[d] = P::mfma(c, pl[0][s], out[d]);
-                }
+        for (int i = 0; i < DT * 2; ++i) {
+            f32x16& o = out[i >> 1];
+            o = P::mfma(tf[0][i], pl[0][i & 1], o);
+            if constexpr (NPL == 2) {
+                o = P::mfma(tf[0][i], pl[1][i & 1], o);
+                o = P::mfma(tf[1][i], pl[0][i & 1], o);
             }
+        }
+        interleave<DT * 2, NPL, NPL == 2 ? 3 : 1, kAhead, (kAhead < DT * 2 ? kAhead : DT * 2)>();
+        __builtin_amdgcn_sched_barrier(0);
     });
 }
 
 template <class P, int NPL, int KS, bool ITEMS>
-__device__ __forceinline__ void small_grad(const SmallArgs& a, int64_t block, char* lds) {
+__device__ __forceinline__ void small_grad(const SmallArgs& a, int64_t share, char* lds) {
     typedef Stream<P, NPL, KS, true> S;
     constexpr int DT = S::DT;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 31, h = lane >> 5;
     const int64_t tiles = ITEMS ? a.vt : a.tt;
-    const int64_t kept_blocks = (tiles + 3) / 4;
-    const int64_t kb = block % kept_blocks, split = block / kept_blocks;
-    const int64_t at = kb * 4 + wave, tile = min(at, tiles - 1);
-    const char* const mine = ITEMS ? a.e + tile * a.e_tile : a.xlive + tile * a.xlive_tile;
-    Kept<P, NPL, KS> kept;
-    kept.load(mine, lane);
-    const float* const own = (const float*)(mine + S::kRows * kBlk) + n;
-    f32x16 out[DT] = {};
-    small_terms<P, NPL, KS, ITEMS>(a, tile, split, kept, own, lds, out);
-    if (at >= tiles) return;
-    const float w = ITEMS ? 1.f : own[kNumRaw * 32];
-    float* const to = (ITEMS ? a.dep : a.dxp) + ((split * tiles + tile) * 32 + n) * (DT * 32) + 4 * h;
+    each_part(ITEMS ? a.de : a.dx, share, (tiles + 3) / 4, [&](int64_t kb, int64_t first, int64_t last, int64_t place) {
+        const int64_t at = kb * 4 + wave, tile = min(at, tiles - 1);
+        const char* const mine = ITEMS ? a.e + tile * a.e_tile : a.xlive + tile * a.xlive_tile;
+        Kept<P, NPL, KS> kept;
+        kept.load(mine, lane);
+        const float* const own = (const float*)(mine + S::kRows * kBlk) + n;
+        f32x16 out[DT] = {};
+        small_terms<P, NPL, KS, ITEMS>(a, tile, first, last, kept, own, lds, out);
+        if (at >= tiles) return;
+        const float w = ITEMS ? 1.f : own[kNumRaw * 32];
+        float* const to = (ITEMS ? a.dep : a.dxp) + ((place * tiles + tile) * 32 + n) * (DT * 32) + 4 * h;
 #pragma unroll
-    for (int d = 0; d < DT; ++d)
+        for (int d = 0; d < DT; ++d)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            f32x4 v;
+            for (int q = 0; q < 4; ++q) {
+                f32x4 v;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) v[r] = out[d][q * 4 + r] * w;
-            *(f32x4*)(to + d * 32 + q * 8) = v;
-        }
+                for (int r = 0; r < 4; ++r) v[r] = out[d][q * 4 + r] * w;
+                *(f32x4*)(to + d * 32 + q * 8) = v;
+            }
+    });
 }
 
 // Blocks for dx first, then blocks for de.
 template <class P, int NPL, int KS>
-__global__ __launch_bounds__(256, 2) void k_small_grads(SmallArgs a) {
+__global__ __launch_bounds__(256, small_grads_per_cu(NPL, KS)) void k_small_grads(SmallArgs a) {
     typedef Stream<P, NPL, KS, true> S;
     __shared__ __align__(16) char lds[S::kStages * S::kCount * kBlk];
-    if (blockIdx.x < a.blocks_x) small_grad<P, NPL, KS, false>(a, blockIdx.x, lds);
-    else small_grad<P, NPL, KS, true>(a, blockIdx.x - a.blocks_x, lds);
+    if (blockIdx.x < a.dx.blocks) small_grad<P, NPL, KS, false>(a, blockIdx.x, lds);
+    else small_grad<P, NPL, KS, true>(a, blockIdx.x - a.dx.blocks, lds);
 }
 
 }  // namespace
 
 template <class P, int NPL>
 hipError_t launch_small_lse(int ksd, const SmallArgs& a, hipStream_t st) {
-    const unsigned blocks = (unsigned)((a.tt + 3) / 4 * a.splits);
+    const unsigned blocks = (unsigned)a.lse.blocks;
     switch (ksd) {
         case 2: k_small_lse<P, NPL, 2><<<blocks, 256, 0, st>>>(a); break;
         case 3: k_small_lse<P, NPL, 3><<<blocks, 256, 0, st>>>(a); break;
@@ -306,7 +347,7 @@ hipError_t launch_small_lse(int ksd, const SmallArgs& a, hipStream_t st) {
 
 template <class P, int NPL>
 hipError_t launch_small_grads(int ksd, const SmallArgs& a, hipStream_t st) {
-    const unsigned blocks = (unsigned)(a.blocks_x + a.blocks_e);
+    const unsigned blocks = (unsigned)(a.dx.blocks + a.de.blocks);
     if (!blocks) return hipSuccess;
     switch (ksd) {
         case 2: k_small_grads<P, NPL, 2><<<blocks, 256, 0, st>>>(a); break;
