@@ -715,9 +715,10 @@ Plan make_plan(const ccdpp_softmax_t& p, int call) {
         w.x_tile = (w.planes * w.ksd + 1) * kBlk;
         w.e_tile = w.xlive_tile = w.x_tile + (w.grads ? w.planes * w.dt * 2 * kBlk : 0);
         constexpr int kCus = 256;
-        const int half = kCus * small_grads_per_cu(w.planes, w.ksd) / 2;  // dx and de run in one launch
+        // dx and de run in one launch; a tile of de, whose streamed rows have numbers of their own, takes 5/4 of one of dx
+        const int all = kCus * small_grads_per_cu(w.planes, w.ksd), mine = all * 4 / 9;
         w.lse = shares(w.tt, w.vt, kCus * small_lse_per_cu(w.planes, w.ksd));
-        w.dx = shares(w.tt, w.vt, half), w.de = shares(w.vt, w.tt, half);
+        w.dx = shares(w.tt, w.vt, mine), w.de = shares(w.vt, w.tt, all - mine);
         w.o_xf = take(w.forward ? w.tt * w.x_tile : 0);
         w.o_ef = take(w.vt * w.e_tile);
         w.o_xl = take(w.grads ? w.tt * w.xlive_tile : 0);

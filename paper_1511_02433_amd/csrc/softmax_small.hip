@@ -217,6 +217,7 @@ __device__ __forceinline__ void small_terms(const SmallArgs& a, int64_t tile, in
     const bool own_unit = __all(factor == 1.f || factor == 0.f);  // 0: a row that does not count
     stream<S>(ITEMS ? a.xlive : a.e, ITEMS ? a.xlive_tile : a.e_tile, first, last, lds, [&](int64_t i, const char* slot) {
         const char* const rows = slot + S::kRows * kBlk;
+        const int y = ITEMS ? ((const int*)rows)[kNumTarget * 32 + n] - (int)(tile * 32) : own_y - (int)(i * 32);
         const auto added = [&]() {
             f32x16 add;
             if constexpr (ITEMS) {
@@ -234,8 +235,8 @@ __device__ __forceinline__ void small_terms(const SmallArgs& a, int64_t tile, in
             const float f = ((const float*)rows)[kNumFactor * 32 + n];
             unit = __all(f == 1.f || f == 0.f);
         }
-        f32x16 z = {};
-        if (unit) z = added();
+        f32x16 z = added();
+        if (!unit) z = f32x16{};
         z = tile_product<P, NPL, KS>(slot, kept, lane, z);
         if (!unit) {
             const f32x16 add = added();
@@ -257,20 +258,15 @@ __device__ __forceinline__ void small_terms(const SmallArgs& a, int64_t tile, in
 #pragma unroll
         for (int r = 0; r < 16; ++r) g[r] = exp2_fast(z[r]);
         if constexpr (ITEMS) {
-            const int y = ((const int*)rows)[kNumTarget * 32 + n] - (int)(tile * 32);
-            if (__any(y >= 0 && y < 32)) {
+            if (__any(y >= 0 && y < 32)) {  // popular items: nearly every tile
+                const f32x16 ys = row_numbers(rows, kNumTarget, h), ws = row_numbers(rows, kNumWeight, h);
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int row = 8 * (r >> 2) + 4 * h + (r & 3);
-                    if (((const int*)rows)[kNumTarget * 32 + row] == (int)(tile * 32) + n) g[r] -= ((const float*)rows)[kNumWeight * 32 + row];
-                }
+                for (int r = 0; r < 16; ++r) g[r] -= __float_as_int(ys[r]) == (int)(tile * 32) + n ? ws[r] : 0.f;
             }
         } else {
-            const int y = own_y - (int)(i * 32);
             if (__any(y >= 0 && y < 32)) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (y == 8 * (r >> 2) + 4 * h + (r & 3)) g[r] -= (float)(1 << kTermExp);
+                for (int r = 0; r < 16; ++r) g[r] -= y == 8 * (r >> 2) + 4 * h + (r & 3) ? (float)(1 << kTermExp) : 0.f;
             }
         }
         typename P::vec pl[NPL][2];
