@@ -11,7 +11,8 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB_PATH = os.path.join(PKG, "libccdpp.so")
 SOURCES = ("sweep.hip", "build.hip", "host_copy.hip", "api.hip", "ops_api.hip",
-           "softmax_loss.hip", "softmax_small.hip", "grad_clip.hip")
+           "softmax_loss.hip", "softmax_small.hip",
+           "softmax_few.hip", "grad_clip.hip")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 

@@ -17,6 +17,7 @@ namespace {
 constexpr int kTable = 64;      // tensors per launch
 constexpr int kBlocks = 1024;   // partial sums
 constexpr int64_t kChunk = 8192;
+constexpr int64_t kLittle = 32768;  // values that one block takes in one launch
 
 struct Table {
     const void* in[kTable];
@@ -85,27 +86,36 @@ __device__ __forceinline__ double block_sum(double s, double* red) {
     return all;
 }
 
+template <class F>
+__device__ __forceinline__ void typed(int dtype, F&& body) {
+    if (dtype == CCDPP_F32) body(float());
+    else if (dtype == CCDPP_BF16) body((__bf16)0.f);
+    else body((_Float16)0.f);
+}
+
 __global__ __launch_bounds__(256) void k_squares(Table t, double* parts, int add) {
     __shared__ double red[4];
     double s = 0.0;
     for (int64_t c = blockIdx.x; c < t.chunks; c += gridDim.x) {
         const int i = find(t, c);
         const int64_t lo = (c - t.first[i]) * kChunk, n = min(kChunk, t.size[i] - lo);
-        if (t.dtype[i] == CCDPP_F32) s += chunk_squares<float>(t.in[i], lo, n, t.wide[i]);
-        else if (t.dtype[i] == CCDPP_BF16) s += chunk_squares<__bf16>(t.in[i], lo, n, t.wide[i]);
-        else s += chunk_squares<_Float16>(t.in[i], lo, n, t.wide[i]);
+        typed(t.dtype[i], [&](auto z) { s += chunk_squares<decltype(z)>(t.in[i], lo, n, t.wide[i]); });
     }
     s = block_sum(s, red);
     if (threadIdx.x == 0) parts[blockIdx.x] = add ? parts[blockIdx.x] + s : s;
 }
 
-// norm[0], from partial sums in a fixed order; no tensors: 0.
-__global__ __launch_bounds__(256) void k_norm(const double* parts, int n, float* norm) {
-    __shared__ double red[4];
+// The norm from kBlocks partial sums in a fixed order, by 256 threads.
+__device__ __forceinline__ float norm_of(const double* parts, double* red) {
     double s = 0.0;
-    for (int i = threadIdx.x; i < n; i += 256) s += parts[i];
-    s = block_sum(s, red);
-    if (threadIdx.x == 0) *norm = (float)sqrt(s);
+    for (int i = threadIdx.x; i < kBlocks; i += 256) s += parts[i];
+    return (float)sqrt(block_sum(s, red));
+}
+
+__global__ __launch_bounds__(256) void k_norm(const double* parts, float* norm) {
+    __shared__ double red[4];
+    const float n = norm_of(parts, red);
+    if (threadIdx.x == 0) *norm = n;
 }
 
 // min(1, max_norm / (norm + eps)); NaN for a norm that is NaN, 1 without a limit.
@@ -114,16 +124,33 @@ __device__ __forceinline__ float clip_factor(float norm, float max_norm, float e
     return isinf(max_norm) || norm + eps <= max_norm ? 1.f : max_norm / (norm + eps);
 }
 
-__global__ __launch_bounds__(256) void k_scale(Table t, const float* norm, float max_norm, float eps) {
-    const float c = clip_factor(*norm, max_norm, eps);
-    for (int64_t k = blockIdx.x; k < t.chunks; k += gridDim.x) {
+// Every block adds up the partial sums itself (8 KB from L2), which saves a launch; block 0 leaves the norm.  The
+// chunks that were read last come first: the memory-side cache may still hold them.
+__global__ __launch_bounds__(256) void k_scale(Table t, const double* parts, float* norm, float max_norm, float eps) {
+    __shared__ double red[4];
+    const float nv = norm_of(parts, red);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *norm = nv;
+    const float c = clip_factor(nv, max_norm, eps);
+    for (int64_t k = t.chunks - 1 - blockIdx.x; k >= 0; k -= gridDim.x) {
         const int i = find(t, k);
         if (c == 1.f && t.out[i] == t.in[i]) continue;
         const int64_t lo = (k - t.first[i]) * kChunk, n = min(kChunk, t.size[i] - lo);
-        if (t.dtype[i] == CCDPP_F32) chunk_scale<float>(t.in[i], t.out[i], lo, n, t.wide[i], c);
-        else if (t.dtype[i] == CCDPP_BF16) chunk_scale<__bf16>(t.in[i], t.out[i], lo, n, t.wide[i], c);
-        else chunk_scale<_Float16>(t.in[i], t.out[i], lo, n, t.wide[i], c);
+        typed(t.dtype[i], [&](auto z) { chunk_scale<decltype(z)>(t.in[i], t.out[i], lo, n, t.wide[i], c); });
     }
+}
+
+// Little in all (kLittle values): one block, one launch.
+__global__ __launch_bounds__(1024) void k_little(Table t, int clip, float* norm, float max_norm, float eps) {
+    __shared__ double red[16];
+    double s = 0.0;
+    for (int i = 0; i < t.n; ++i) typed(t.dtype[i], [&](auto z) { s += chunk_squares<decltype(z)>(t.in[i], 0, t.size[i], t.wide[i]); });
+    const float nv = (float)sqrt(block_sum(s, red));
+    if (threadIdx.x == 0) *norm = nv;
+    if (!clip) return;
+    const float c = clip_factor(nv, max_norm, eps);
+    for (int i = 0; i < t.n; ++i)
+        if (c != 1.f || t.out[i] != t.in[i])
+            typed(t.dtype[i], [&](auto z) { chunk_scale<decltype(z)>(t.in[i], t.out[i], 0, t.size[i], t.wide[i], c); });
 }
 
 int run(bool clip, int32_t n, const void* const* in, void* const* out, const int64_t* sizes, const int32_t* dtypes, float max_norm, float eps,
@@ -143,43 +170,45 @@ int run(bool clip, int32_t n, const void* const* in, void* const* out, const int
     if (int rc = check_device()) return rc;
     hipStream_t st = (hipStream_t)stream;
     double* parts = (double*)ws;
-    const auto launch = [&](bool scale) -> int {
-        int filled = 0;
+    Table t;
+    int64_t values = 0;
+    t.n = 0, t.chunks = 0;
+    const auto add = [&](int32_t i) {
+        t.in[t.n] = in[i], t.out[t.n] = clip ? out[i] : nullptr;
+        t.size[t.n] = sizes[i], t.first[t.n] = t.chunks, t.dtype[t.n] = (uint8_t)dtypes[i];
+        t.wide[t.n] = (uintptr_t)in[i] % 16 == 0 && (!clip || (uintptr_t)out[i] % 16 == 0);
+        t.chunks += (sizes[i] + kChunk - 1) / kChunk;
+        ++t.n;
+    };
+    int32_t filled = 0;
+    for (int32_t i = 0; i < n; ++i)
+        if (sizes[i]) ++filled, values += sizes[i];
+    if (filled <= kTable && values <= kLittle) {
+        for (int32_t i = 0; i < n; ++i)
+            if (sizes[i]) add(i);
+        k_little<<<1, 1024, 0, st>>>(t, clip, norm, max_norm, eps);
+        const hipError_t e = hipGetLastError();
+        return e == hipSuccess ? CCDPP_OK : hip_fail(e, "gradient norm");
+    }
+    for (int pass = 0; pass < (clip ? 2 : 1); ++pass) {
         bool first = true;
-        Table t = {};
-        const auto go = [&]() -> int {
-            if (!t.n) return CCDPP_OK;
-            if (scale) {
-                k_scale<<<(unsigned)std::min<int64_t>(4 * kBlocks, t.chunks), 256, 0, st>>>(t, norm, max_norm, eps);
-            } else {
-                const int blocks = first ? kBlocks : (int)std::min<int64_t>(kBlocks, t.chunks);
-                k_squares<<<blocks, 256, 0, st>>>(t, parts, !first);
-                first = false;
-            }
-            const hipError_t e = hipGetLastError();
-            t.n = 0, t.chunks = 0;
-            return e == hipSuccess ? CCDPP_OK : hip_fail(e, "gradient norm");
-        };
         for (int32_t i = 0; i < n; ++i) {
-            if (!sizes[i]) continue;
-            t.in[t.n] = in[i], t.out[t.n] = clip ? out[i] : nullptr;
-            t.size[t.n] = sizes[i], t.first[t.n] = t.chunks, t.dtype[t.n] = (uint8_t)dtypes[i];
-            t.wide[t.n] = (uintptr_t)in[i] % 16 == 0 && (!clip || (uintptr_t)out[i] % 16 == 0);
-            t.chunks += (sizes[i] + kChunk - 1) / kChunk;
-            ++filled;
-            if (++t.n == kTable)
-                if (int rc = go()) return rc;
-        }
-        if (int rc = go()) return rc;
-        if (!scale) {
-            k_norm<<<1, 256, 0, st>>>(parts, filled ? kBlocks : 0, norm);
+            if (sizes[i]) add(i);
+            if (!t.n || (t.n < kTable && i + 1 < n)) continue;
+            if (pass == 0) k_squares<<<first ? kBlocks : (int)std::min<int64_t>(kBlocks, t.chunks), 256, 0, st>>>(t, parts, !first);
+            else k_scale<<<(unsigned)std::min<int64_t>(4 * kBlocks, t.chunks), 256, 0, st>>>(t, parts, norm, max_norm, eps);
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess) return hip_fail(e, "gradient norm");
+            first = false;
+            t.n = 0, t.chunks = 0;
         }
-        return CCDPP_OK;
-    };
-    if (int rc = launch(false)) return rc;
-    return clip ? launch(true) : CCDPP_OK;
+    }
+    if (!clip) {
+        k_norm<<<1, 256, 0, st>>>(parts, norm);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return hip_fail(e, "gradient norm");
+    }
+    return CCDPP_OK;
 }
 
 }  // namespace

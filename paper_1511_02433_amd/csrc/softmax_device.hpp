@@ -159,4 +159,33 @@ constexpr int small_grads_per_cu(int planes, int ks) { return planes * ks > 8 ? 
 template <class P, int NPL> hipError_t launch_small_lse(int ksd, const SmallArgs& a, hipStream_t st);
 template <class P, int NPL> hipError_t launch_small_grads(int ksd, const SmallArgs& a, hipStream_t st);
 
+// ---- few rows (t <= kFewT) -------------------------------------------------------------------
+constexpr int kFewT = 16;
+constexpr int kFewLds = 150 * 1024;  // of x's rows in LDS
+
+struct FewArgs {
+    int t, d, dp;             // dp: columns of partial sums, a multiple of 4
+    int64_t v;
+    const void *x, *table, *target;
+    int64_t ldx, ldt;
+    int target_bits;
+    int wide_x, wide_e, wide_de;  // rows aligned to what a lane reads at a time
+    float scale;
+    const float* offset;
+    float2* part;             // [block][part_row] (max, sum), base 2, or NULL
+    int64_t part_row;
+    float* z;                 // logits in base 2 [t][z_row], or NULL
+    int64_t z_row;
+    const float *lse, *grad;
+    void* de;                 // or NULL
+    int64_t ldde;
+    float* dxp;               // [part][t][dp], or NULL
+    int parts;                // blocks along the table
+    int across;               // threads along a row (a power of two)
+};
+
+int few_across(int d, int columns);
+template <class T> hipError_t launch_few_logits(const FewArgs& a, int blocks, hipStream_t st);
+template <class T> hipError_t launch_few_grads(const FewArgs& a, T* dx, int64_t lddx, hipStream_t st);
+
 }  // namespace ccdops

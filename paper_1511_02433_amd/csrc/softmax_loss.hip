@@ -577,44 +577,67 @@ __global__ __launch_bounds__(256) void k_rows(ccdpp_softmax_t p, const float* ls
     if (t < p.t) put_numbers(n, t, load_target(p.target, p.target_bits, t), p.v, p.offset, lse[t]);
 }
 
-// A wave per row: joins the (max, sum) pairs of its pieces (0: of its shares), and takes the target's logit from x and the table.
-template <class T>
+// Joins the (max, sum) pairs of a row's pieces (0: of its shares), and takes the target's logit from x and the table: a
+// wave a row, or a block of 256 threads where rows are long.
+template <class T, int THREADS>
 __global__ __launch_bounds__(256) void k_loss(ccdpp_softmax_t p, const float2* part, int64_t pieces, Shares shares, float* loss, float* lse, RowNumbers num) {
-    const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    constexpr int kRows = 256 / THREADS;
+    __shared__ float red[4][4];
+    const int64_t t = (int64_t)blockIdx.x * kRows + threadIdx.x / THREADS;
     if (t >= p.t) return;
-    const int lane = threadIdx.x & 63;
+    const int i0 = threadIdx.x % THREADS, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    // the target's products first: their reads are under way while the pieces come
+    const int64_t y = load_target(p.target, p.target_bits, t);
+    const float o = p.offset && y >= 0 && y < p.v ? p.offset[y] : 0.f;
+    float dot = 0.f;
+    if (y >= 0 && y < p.v && !(o < kExcluded)) {
+        const T *x = (const T*)p.x + t * p.ldx, *e = (const T*)p.table + y * p.ldt;
+        constexpr int N = 16 / sizeof(T);
+        int d = 0;
+        if (((uintptr_t)x | (uintptr_t)e) % 16 == 0) {
+            struct alignas(16) Piece { T v[N]; };
+#pragma unroll 4
+            for (d = i0 * N; d + N <= p.d; d += THREADS * N) {
+                const Piece a = *(const Piece*)(x + d), b = *(const Piece*)(e + d);
+#pragma unroll
+                for (int j = 0; j < N; ++j) dot = fmaf((float)a.v[j], (float)b.v[j], dot);
+            }
+            d = p.d / N * N;
+        }
+        for (d += i0; d < p.d; d += THREADS) dot = fmaf((float)x[d], (float)e[d], dot);
+    }
     float m = -INFINITY, s = 0.f;
     bool nan = false;
     if (!pieces) pieces = shares.count(t / 128);
-    for (int64_t i = lane; i < pieces; i += 64) {
+    for (int64_t i = i0; i < pieces; i += THREADS) {
         const float2 q = part[i * p.t + t];
         const float top = fmaxf(m, q.x), ref = top == -INFINITY ? 0.f : top;
         nan |= q.x != q.x || q.y != q.y;
         s = s * exp2_fast(m - ref) + q.y * exp2_fast(q.x - ref);
         m = top;
     }
-    const float top = wave_max(m), ref = top == -INFINITY ? 0.f : top;
+    float top = wave_max(m), ref = top == -INFINITY ? 0.f : top;
     s *= exp2_fast(m - ref);
-    for (int k = 32; k > 0; k >>= 1) s += __shfl_xor(s, k);
-    float l = top == -INFINITY ? -INFINITY : (top + log2f(s)) * kLn2;
-    if (__any(nan)) l = NAN;
-    const int64_t y = load_target(p.target, p.target_bits, t);
-    float out = 0.f;
-    if (y >= p.v) {
-        out = NAN;
-    } else if (y >= 0) {
-        const float o = p.offset ? p.offset[y] : 0.f;
-        if (o < kExcluded) {
-            out = INFINITY;
-        } else {
-            const T *x = (const T*)p.x + t * p.ldx, *e = (const T*)p.table + y * p.ldt;
-            float dot = 0.f;
-            for (int d = lane; d < p.d; d += 64) dot = fmaf((float)x[d], (float)e[d], dot);
-            for (int k = 32; k > 0; k >>= 1) dot += __shfl_xor(dot, k);
-            out = l - fmaf(dot, p.scale, o);
+    for (int k = 32; k > 0; k >>= 1) s += __shfl_xor(s, k), dot += __shfl_xor(dot, k);
+    nan = __any(nan);
+    if constexpr (THREADS == 256) {
+        if (lane == 0) red[wave][0] = top, red[wave][1] = s, red[wave][2] = dot, red[wave][3] = nan ? 1.f : 0.f;
+        __syncthreads();
+        for (int w = 0; w < 4; ++w) top = fmaxf(top, red[w][0]);
+        ref = top == -INFINITY ? 0.f : top;
+        s = 0.f, dot = 0.f;
+        for (int w = 0; w < 4; ++w) {
+            s += red[w][1] * exp2_fast(red[w][0] - ref);
+            dot += red[w][2];
+            nan |= red[w][3] != 0.f;
         }
     }
-    if (lane == 0) {
+    float l = top == -INFINITY ? -INFINITY : (top + log2f(s)) * kLn2;
+    if (nan) l = NAN;
+    float out = 0.f;
+    if (y >= p.v) out = NAN;
+    else if (y >= 0) out = o < kExcluded ? INFINITY : l - fmaf(dot, p.scale, o);
+    if (i0 == 0) {
         loss[t] = out, lse[t] = l;
         if (num.first) put_numbers(num, t, y, p.v, p.offset, l);
     }
@@ -668,7 +691,8 @@ struct Plan {
     int planes = 1;
     bool scaled = false, scale_g = false;
     bool grads = false, forward = false;
-    bool small = false;      // d <= kSmallD: k_small_*
+    bool few = false;        // t <= kFewT: k_few_*
+    bool small = false;      // else d <= kSmallD: k_small_*
     int64_t tt, vt, dt;      // blocks of 32
     int ksd;                 // steps of 16 over d
     int64_t kst, ksv;        // over rows, over the whole table
@@ -678,6 +702,8 @@ struct Plan {
     Shares lse, dx, de;      // (small)
     int64_t x_tile, xlive_tile, e_tile;  // bundles (small)
     // offsets into the workspace
+    int few_rows, few_blocks, few_parts;  // rows of x a launch, blocks of the logits, of the gradients along the table
+    int64_t o_z;
     int64_t o_scale, o_xrow, o_fin, o_xf, o_ef, o_xl, o_o2, o_xn, o_xt, o_et, o_g, o_gt, o_part, o_dx, o_de, bytes;
 };
 
@@ -699,6 +725,26 @@ Plan make_plan(const ccdpp_softmax_t& p, int call) {
         at += round_up(std::max<int64_t>(n, 0), 256);
         return o;
     };
+    w.few = p.t <= kFewT;
+    if (w.few) {
+        const int es = w.planes == 2 ? 4 : 2;
+        const int64_t row = (int64_t)(p.d * es + 63) / 64 * 64 + 16;
+        w.few_rows = (int)std::max<int64_t>(1, std::min<int64_t>(p.t, kFewLds / row));
+        if (row > kFewLds) w.few = false;  // not even one row: the general way
+        // two blocks of eight waves a CU (one where x takes more than half of LDS), a group of 16 table rows each at least
+        w.few_blocks = (int)std::max<int64_t>(1, std::min<int64_t>(w.few_rows * row > 75 * 1024 ? 256 : 512, (p.v + 127) / 128));
+        const int columns = p.t > 8 ? 4 : 16 / es;
+        const int64_t wide = (int64_t)few_across(p.d, columns) * columns, beside = (p.d + wide - 1) / wide;
+        w.few_parts = (int)std::max<int64_t>(1, std::min<int64_t>(1024 / beside, (p.v + 63) / 64));
+    }
+    if (w.few) {
+        w.dp = round_up(p.d, 4);
+        w.o_part = take(w.forward ? w.few_blocks * p.t * 8 : 0);
+        w.o_z = take(w.grads ? p.t * round_up(p.v, 16) * 4 : 0);
+        w.o_dx = take(w.grads ? w.few_parts * p.t * w.dp * 4 : 0);
+        w.bytes = at;
+        return w;
+    }
     w.o_scale = take(3 * kParts * 4);
     w.o_fin = take(64);
     w.o_xrow = take(w.scaled ? p.t * 4 : 0);
@@ -763,6 +809,15 @@ Plan make_plan(const ccdpp_softmax_t& p, int call) {
     } while (0)
 
 template <class T>
+int launch_loss(const ccdpp_softmax_t& p, const float2* part, int64_t pieces, const Shares& shares, float* loss, float* lse, const RowNumbers& num,
+                hipStream_t st) {
+    if (p.d > 256 || p.t <= 256) k_loss<T, 256><<<(unsigned)p.t, 256, 0, st>>>(p, part, pieces, shares, loss, lse, num);
+    else k_loss<T, 64><<<(unsigned)((p.t + 3) / 4), 256, 0, st>>>(p, part, pieces, shares, loss, lse, num);
+    OPS_LAUNCH("loss");
+    return CCDPP_OK;
+}
+
+template <class T>
 int finish(const FinishSide& x, const FinishSide& e, int cols, float scale, const int32_t* fin, hipStream_t st) {
     const int64_t quads = (cols + 3) / 4;
     const auto blocks = [&](const FinishSide& a) { return a.out ? std::min<int64_t>((a.rows * quads + 255) / 256, 1 << 16) : 0; };
@@ -781,6 +836,31 @@ struct Outs {
     void* de;
     int64_t ldde;
 };
+
+template <class T>
+int run_few(const ccdpp_softmax_t& p, const Plan& w, const Outs& o, char* ws, hipStream_t st) {
+    FewArgs a = {};
+    a.d = p.d, a.dp = (int)w.dp, a.v = p.v, a.table = p.table, a.ldt = p.ldt, a.ldx = p.ldx;
+    a.target_bits = p.target_bits, a.scale = p.scale, a.offset = p.offset;
+    a.wide_x = ((uintptr_t)p.x | (p.ldx * sizeof(T))) % 16 == 0, a.wide_e = ((uintptr_t)p.table | (p.ldt * sizeof(T))) % 16 == 0;
+    a.part_row = p.t, a.z_row = round_up(p.v, 16);
+    for (int64_t t0 = 0; t0 < p.t; t0 += w.few_rows) {
+        a.t = (int)std::min<int64_t>(w.few_rows, p.t - t0);
+        a.x = (const T*)p.x + t0 * p.ldx;
+        a.part = w.forward ? (float2*)(ws + w.o_part) + t0 : nullptr;
+        a.z = w.grads ? (float*)(ws + w.o_z) + t0 * a.z_row : nullptr;
+        const hipError_t e = launch_few_logits<T>(a, w.few_blocks, st);
+        if (e != hipSuccess) return hip_fail(e, "logits");
+    }
+    if (w.forward)
+        if (int rc = launch_loss<T>(p, (const float2*)(ws + w.o_part), w.few_blocks, Shares{}, o.loss, o.lse, RowNumbers{}, st)) return rc;
+    if (!w.grads || (!o.dx && !o.de)) return CCDPP_OK;
+    a.t = (int)p.t, a.x = p.x, a.target = p.target, a.z = (float*)(ws + w.o_z), a.part = nullptr;
+    a.lse = w.forward ? o.lse : o.lse_in, a.grad = o.grad;
+    a.de = o.de, a.ldde = o.ldde, a.dxp = o.dx ? (float*)(ws + w.o_dx) : nullptr, a.parts = w.few_parts;
+    const hipError_t e = launch_few_grads<T>(a, (T*)o.dx, o.lddx, st);
+    return e == hipSuccess ? CCDPP_OK : hip_fail(e, "gradients");
+}
 
 template <int DT>
 int run_small(const ccdpp_softmax_t& p, const Plan& w, const Outs& o, const int32_t* fin, char* ws, hipStream_t st) {
@@ -802,8 +882,7 @@ int run_small(const ccdpp_softmax_t& p, const Plan& w, const Outs& o, const int3
     if (w.forward) {
         const hipError_t e = launch_small_lse<P, NPL>(w.ksd, a, st);
         if (e != hipSuccess) return hip_fail(e, "logits");
-        k_loss<T><<<(unsigned)((p.t + 3) / 4), 256, 0, st>>>(p, a.part, 0, a.lse, o.loss, o.lse, num);
-        OPS_LAUNCH("loss");
+        if (int rc = launch_loss<T>(p, a.part, 0, a.lse, o.loss, o.lse, num, st)) return rc;
     } else {
         k_rows<<<(unsigned)((p.t + 255) / 256), 256, 0, st>>>(p, o.lse_in, num);
         OPS_LAUNCH("rows");
@@ -833,8 +912,7 @@ int run_wide(const ccdpp_softmax_t& p, const Plan& w, const Outs& out, const int
         const int64_t blocks = (w.vt + 7) / 8 * ((w.tt + 7) / 8);
         k_gemm<P, NPL, EPI_LSE, T><<<(unsigned)blocks, 512, 0, st>>>(z);
         OPS_LAUNCH("logits");
-        k_loss<T><<<(unsigned)((p.t + 3) / 4), 256, 0, st>>>(p, z.part, (w.vt + 7) / 8, Shares{}, out.loss, out.lse, RowNumbers{});
-        OPS_LAUNCH("loss");
+        if (int rc = launch_loss<T>(p, z.part, (w.vt + 7) / 8, Shares{}, out.loss, out.lse, RowNumbers{}, st)) return rc;
     }
     if (!w.grads) return CCDPP_OK;
     z.lse = w.forward ? out.lse : out.lse_in, z.grad = out.grad;
@@ -882,6 +960,7 @@ int run(const ccdpp_softmax_t& p, int call, const Outs& out, char* ws, hipStream
     typedef typename Types<DT>::in T;
     constexpr int NPL = Types<DT>::planes;
     const Plan w = make_plan(p, call);
+    if (w.few) return run_few<T>(p, w, out, ws, st);
     Scales sc;
     sc.e_part = (float*)(ws + w.o_scale), sc.x_part = sc.e_part + kParts, sc.g_part = sc.x_part + kParts;
     sc.fin = (int32_t*)(ws + w.o_fin), sc.x_row = (float*)(ws + w.o_xrow);

@@ -183,8 +183,6 @@ def softmax_loss_train(x, table, target, *, grad=None, scale=1.0, offset=None, d
 
 def _dense(a):
     """Whether a's values fill one piece of memory, in whatever order of its dimensions."""
-    if a.is_contiguous():
-        return True
     n = 1
     for size, stride in sorted(((s, st) for s, st in zip(a.shape, a.stride()) if s > 1), key=lambda q: q[1]):
         if stride != n:
@@ -196,26 +194,33 @@ def _dense(a):
 def _tensors(tensors, out):
     tensors = list(tensors)
     n = len(tensors)
-    device = None
+    device = tensors[0].device if n and isinstance(tensors[0], torch.Tensor) else None
+    kinds, sizes, flat = [], [], True
     for a in tensors:
-        if not isinstance(a, torch.Tensor) or a.dtype not in _DTYPES:
+        kind = _DTYPES.get(a.dtype) if isinstance(a, torch.Tensor) else None
+        if kind is None:
             raise TypeError("gradients must be float32, bfloat16 or float16 tensors")
-        if not a.is_cuda or (device is not None and a.device != device):
+        if not a.is_cuda or a.device != device:
             raise ValueError("gradients must be in the memory of one device")
-        device = a.device
-        if not _dense(a):
-            raise ValueError("gradients must fill one piece of memory each")
+        if not a.is_contiguous():
+            flat = False
+            if not _dense(a):
+                raise ValueError("gradients must fill one piece of memory each")
+        kinds.append(kind)
+        sizes.append(a.numel())
+    P = ctypes.c_void_p * n
+    ins = outs = P(*[a.data_ptr() for a in tensors])
     if out is not None:
         out = list(out)
         if len(out) != n:
             raise ValueError("out must have one tensor for each gradient")
         for a, o in zip(tensors, out):
-            if o.shape != a.shape or o.dtype != a.dtype or o.device != a.device or (o.stride() != a.stride() and a.numel() > 1):
+            if o.shape != a.shape or o.dtype != a.dtype or o.device != device or not (
+                    o.is_contiguous() if flat else o.stride() == a.stride() or a.numel() < 2):
                 raise ValueError("out must be like the gradients in shape, strides, type and device")
-    P = ctypes.c_void_p * n
-    return (tensors, device or torch.device("cuda", torch.cuda.current_device()), n, P(*[a.data_ptr() for a in tensors]),
-            None if out is None else P(*[o.data_ptr() for o in out]),
-            (ctypes.c_int64 * n)(*[a.numel() for a in tensors]), (ctypes.c_int32 * n)(*[_DTYPES[a.dtype] for a in tensors]))
+        outs = P(*[o.data_ptr() for o in out])
+    return (device or torch.device("cuda", torch.cuda.current_device()), n, ins, outs, (ctypes.c_int64 * n)(*sizes),
+            (ctypes.c_int32 * n)(*kinds))
 
 
 @functools.lru_cache(maxsize=None)
@@ -227,7 +232,7 @@ def _norm_workspace_bytes():
 
 def grad_norm(tensors):
     """The 2-norm of all values of the tensors together: a float32 scalar in device memory."""
-    _, device, n, ptrs, _, sizes, dtypes = _tensors(tensors, None)
+    device, n, ptrs, _, sizes, dtypes = _tensors(tensors, None)
     with _On(device):
         norm = torch.empty((), dtype=torch.float32, device=device)
         ws = torch.empty(_norm_workspace_bytes(), dtype=torch.uint8, device=device)
@@ -239,10 +244,10 @@ def clip_grads(tensors, max_norm, *, eps=1e-6, out=None):
     """Multiplies all tensors with min(1, max_norm / (norm + eps)), in place or into `out`; returns their norm before
     that (a float32 scalar in device memory).  A norm that is NaN makes every value NaN, an infinite one the finite
     values 0."""
-    _, device, n, ptrs, outs, sizes, dtypes = _tensors(tensors, out)
+    device, n, ptrs, outs, sizes, dtypes = _tensors(tensors, out)
     with _On(device):
         norm = torch.empty((), dtype=torch.float32, device=device)
         ws = torch.empty(_norm_workspace_bytes(), dtype=torch.uint8, device=device)
-        _check(_lib().ccdpp_clip_grads(n, ptrs, ptrs if outs is None else outs, sizes, dtypes, max_norm, eps,
+        _check(_lib().ccdpp_clip_grads(n, ptrs, outs, sizes, dtypes, max_norm, eps,
                                        norm.data_ptr(), ws.data_ptr(), ws.numel(), _stream(device)))
     return norm
