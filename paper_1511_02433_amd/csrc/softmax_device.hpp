@@ -1,6 +1,8 @@
 // Device code that the softmax loss's kernels share (gfx950).
 #pragma once
 
+#include <type_traits>
+
 #include "ops_internal.hpp"
 
 namespace ccdops {
@@ -29,11 +31,13 @@ struct HF {
     static __device__ f32x16 mfma(vec a, vec b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 };
 
-// Input type -> operand type and number of planes.
+// Input type -> operand type and number of planes.  `turned`: what many factors' gradients take, half precision, whose 11
+// bits keep the terms G of bfloat16 problems from costing as much as the rounding of the result does; the
+// turned matrices then get a power of two of their own.
 template <int DT> struct Types;
-template <> struct Types<CCDPP_F32> { typedef float in; typedef HF op; static constexpr int planes = 2; };
-template <> struct Types<CCDPP_BF16> { typedef __bf16 in; typedef BF op; static constexpr int planes = 1; };
-template <> struct Types<CCDPP_F16> { typedef _Float16 in; typedef HF op; static constexpr int planes = 1; };
+template <> struct Types<CCDPP_F32> { typedef float in; typedef HF op; typedef HF turned; static constexpr int planes = 2; };
+template <> struct Types<CCDPP_BF16> { typedef __bf16 in; typedef BF op; typedef HF turned; static constexpr int planes = 1; };
+template <> struct Types<CCDPP_F16> { typedef _Float16 in; typedef HF op; typedef HF turned; static constexpr int planes = 1; };
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float pow2i(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }  // -126 <= e <= 127
@@ -69,16 +73,16 @@ __device__ __forceinline__ void to_planes(float v, typename P::elem* out) {
     }
 }
 
-// The terms G of one lane, in planes of operand fragments.  Two planes are cut off toward zero, which pairs of values
-// share an instruction for: 2^-22 of the value is lost on average, 2^-20 at most.
+// The terms G of one lane, in planes of operand fragments.  Two half-precision planes are cut off toward zero, which pairs
+// of values share an instruction for: 2^-22 of the value is lost on average, 2^-20 at most.
 template <class P, int NPL>
 __device__ __forceinline__ void split_terms(const float* g, typename P::vec (*pl)[2]) {
-    if constexpr (NPL == 2) {
+    if constexpr (NPL == 2 && std::is_same<P, HF>::value) {
         typedef __fp16 half2_t __attribute__((ext_vector_type(2)));
 #pragma unroll
         for (int r = 0; r < 16; r += 2) {
             const half2_t hi = __builtin_amdgcn_cvt_pkrtz(g[r], g[r + 1]);
-            const half2_t lo = __builtin_amdgcn_cvt_pkrtz(fmaf((float)hi[0], -1.f, g[r]), fmaf((float)hi[1], -1.f, g[r + 1]));
+            const half2_t lo = __builtin_amdgcn_cvt_pkrtz(g[r] - (float)hi[0], g[r + 1] - (float)hi[1]);
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 pl[0][r >> 3][(r & 7) + k] = (typename P::elem)hi[k];
@@ -87,7 +91,10 @@ __device__ __forceinline__ void split_terms(const float* g, typename P::vec (*pl
         }
     } else {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) pl[0][r >> 3][r & 7] = (typename P::elem)g[r];
+        for (int r = 0; r < 16; ++r) {
+            pl[0][r >> 3][r & 7] = (typename P::elem)g[r];
+            if constexpr (NPL == 2) pl[1][r >> 3][r & 7] = (typename P::elem)(g[r] - (float)pl[0][r >> 3][r & 7]);
+        }
     }
 }
 
@@ -155,7 +162,7 @@ struct SmallArgs {
 int small_steps(int d);
 // Blocks that a CU holds, by registers and LDS.
 constexpr int small_lse_per_cu(int planes, int ks) { return planes * ks > 12 ? 3 : 4; }
-constexpr int small_grads_per_cu(int planes, int ks) { return planes * ks > 8 ? 2 : 3; }
+constexpr int small_grads_per_cu(int planes, int ks) { return ks > 4 || planes * ks > 8 ? 2 : 3; }
 template <class P, int NPL> hipError_t launch_small_lse(int ksd, const SmallArgs& a, hipStream_t st);
 template <class P, int NPL> hipError_t launch_small_grads(int ksd, const SmallArgs& a, hipStream_t st);
 

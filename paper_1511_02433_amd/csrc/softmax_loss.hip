@@ -47,13 +47,16 @@ __device__ __forceinline__ float abs_finite(T v) {
 // Largest finite |value| of a row, by 16 lanes.
 template <class T>
 __device__ __forceinline__ float row_max(const T* row, int d, bool wide) {
+    constexpr int N = 16 / sizeof(T);
+    struct alignas(16) Piece { T v[N]; };
     const int l = threadIdx.x & 15;
     float m = 0.f;
     int c = 0;
     if (wide) {
-        for (; c + 64 <= d; c += 64) {
-            const f32x4 q = *(const f32x4*)(row + c + 4 * l);
-            for (int j = 0; j < 4; ++j) m = fmaxf(m, abs_finite(q[j]));
+        for (; c + 16 * N <= d; c += 16 * N) {
+            const Piece q = *(const Piece*)(row + c + N * l);
+#pragma unroll
+            for (int j = 0; j < N; ++j) m = fmaxf(m, abs_finite(q.v[j]));
         }
     }
     for (c += l; c < d; c += 16) m = fmaxf(m, abs_finite(row[c]));
@@ -61,20 +64,20 @@ __device__ __forceinline__ float row_max(const T* row, int d, bool wide) {
     return m;
 }
 
-// MATS: the table and x (32-bit inputs), 16 lanes a row.  The rows' weights where `grads` is set.
-template <bool MATS>
-__global__ __launch_bounds__(1024) void k_scales(ccdpp_softmax_t p, const float* grad, Scales sc, int grads) {
+// The table and x (where `mats` is set), 16 lanes a row, and the rows' weights (`grads`).
+template <class T>
+__global__ __launch_bounds__(1024) void k_scales(ccdpp_softmax_t p, const float* grad, Scales sc, int mats, int grads) {
     __shared__ float red[16][3];
     float em = 0.f, xm = 0.f, gm = 0.f;
     const int64_t stride = (int64_t)kParts * 64;
-    if constexpr (MATS) {
-        const bool we = ((uintptr_t)p.table | (p.ldt * 4)) % 16 == 0, wx = ((uintptr_t)p.x | (p.ldx * 4)) % 16 == 0;
+    if (mats) {
+        const bool we = ((uintptr_t)p.table | (p.ldt * sizeof(T))) % 16 == 0, wx = ((uintptr_t)p.x | (p.ldx * sizeof(T))) % 16 == 0;
         for (int64_t v = (int64_t)blockIdx.x * 64 + (threadIdx.x >> 4); v < p.v; v += stride) {
             if (p.offset && p.offset[v] < kExcluded) continue;
-            em = fmaxf(em, row_max((const float*)p.table + v * p.ldt, p.d, we));
+            em = fmaxf(em, row_max((const T*)p.table + v * p.ldt, p.d, we));
         }
         for (int64_t t = (int64_t)blockIdx.x * 64 + (threadIdx.x >> 4); t < p.t; t += stride) {
-            const float m = row_max((const float*)p.x + t * p.ldx, p.d, wx);
+            const float m = row_max((const T*)p.x + t * p.ldx, p.d, wx);
             if ((threadIdx.x & 15) == 0) sc.x_row[t] = m;
             if (row_counts(load_target(p.target, p.target_bits, t), p.v, p.offset)) xm = fmaxf(xm, m);
         }
@@ -120,7 +123,7 @@ struct PackSide {
 struct PackArgs {
     PackSide x, e;
     Scales sc;
-    int scaled;    // 32-bit inputs
+    int scaled;    // e_part and x_part hold: the turned matrices (and 32-bit ones as they are) get powers of two
     int weights;   // g_part holds
     int d, ksd;    // ksd: steps of 16 over d
     const void* target;
@@ -133,10 +136,11 @@ struct PackArgs {
 
 // One block: 32 rows x 128 columns, blocks of x first.  A wave takes 16 columns at a time: a lane's 8 values of a
 // fragment are 8 neighbours in memory; the turned ones are picked out of LDS.
-template <int DT>
+template <int DT, bool SMALL>
 __global__ __launch_bounds__(256) void k_pack(PackArgs a) {
     typedef typename Types<DT>::in T;
     typedef typename Types<DT>::op P;
+    typedef typename std::conditional<SMALL, P, typename Types<DT>::turned>::type PT;
     constexpr int NPL = Types<DT>::planes;
     constexpr int kPitch = 128 + 16 / sizeof(T);
     __shared__ __align__(16) T tile[32][kPitch];
@@ -247,22 +251,22 @@ __global__ __launch_bounds__(256) void k_pack(PackArgs a) {
     for (int k = 0; k < 2; ++k) {
         const int i = wave + 4 * k, dt = i >> 1, s = i & 1;  // 4 blocks of 32 columns x 2 steps of 16 rows
         if (c0 + dt * 32 >= a.d) break;
-        typename P::elem o[8][2];
+        typename PT::elem o[8][2];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const int r = 16 * s + (j < 4 ? 4 * h + j : 8 + 4 * h + j - 4);
             // columns past d were not written by a fragment if they start a new one
             const T v = c0 + dt * 32 + m < a.d ? tile[r][dt * 32 + m] : (T)0.f;
-            if constexpr (NPL == 2) to_planes<P, NPL>((float)v * mul_t, o[j]);
-            else o[j][0] = (typename P::elem)v;
+            if constexpr (std::is_same<T, typename PT::elem>::value) o[j][0] = v;
+            else to_planes<PT, NPL>((float)v * mul_t, o[j]);
         }
 #pragma unroll
         for (int pl = 0; pl < NPL; ++pl) {
-            typename P::vec w;
+            typename PT::vec w;
 #pragma unroll
             for (int j = 0; j < 8; ++j) w[j] = o[j][pl];
-            *(typename P::vec*)(side.turned + pl * side.turned_plane + (int64_t)(c0 / 32 + dt) * side.turned_d + rt * side.turned_row +
-                                s * kBlk + lane * 16) = w;
+            *(typename PT::vec*)(side.turned + pl * side.turned_plane + (int64_t)(c0 / 32 + dt) * side.turned_d + rt * side.turned_row +
+                                 s * kBlk + lane * 16) = w;
         }
     }
 }
@@ -303,7 +307,8 @@ struct GemmArgs {
 constexpr int kStages = 4;          // of LDS, each a step of 32 over K of both operands
 constexpr int kStage = 32 * kBlk;
 
-template <class P, int NPL, int EPI, class T>
+// P: operands; PG: terms G.
+template <class P, class PG, int NPL, int EPI, class T>
 __global__ __launch_bounds__(512) void k_gemm(GemmArgs a) {
     constexpr int NSEG = NPL == 2 ? 3 : 1;
     __shared__ __align__(16) char lds[kStages * kStage];
@@ -481,11 +486,11 @@ __global__ __launch_bounds__(512) void k_gemm(GemmArgs a) {
     }
     if constexpr (EPI == EPI_G) {
         // identity in B-operand order for the two steps of 16 entries
-        typename P::vec eye[2];
+        typename PG::vec eye[2];
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
-            for (int k = 0; k < 8; ++k) eye[s][k] = (typename P::elem)(16 * s + (k < 4 ? 4 * h + k : 8 + 4 * h + k - 4) == n ? 1.f : 0.f);
+            for (int k = 0; k < 8; ++k) eye[s][k] = (typename PG::elem)(16 * s + (k < 4 ? 4 * h + k : 8 + 4 * h + k - 4) == n ? 1.f : 0.f);
         float w[2], l2[2], f[2];
         int64_t y[2];        // target, from the piece's first entry
         uint32_t keep[2];    // all ones in rows that count: others are cut off as bits, whatever they hold
@@ -525,25 +530,25 @@ __global__ __launch_bounds__(512) void k_gemm(GemmArgs a) {
                     for (int r = 0; r < 16; ++r)
                         if (at == 8 * (r >> 2) + 4 * h + (r & 3)) g[r] -= w[j];
                 }
-                typename P::vec pl[NPL][2];
-                split_terms<P, NPL>(g, pl);
+                typename PG::vec pl[NPL][2];
+                split_terms<PG, NPL>(g, pl);
 #pragma unroll
                 for (int k = 0; k < NPL; ++k) {
 #pragma unroll
                     for (int s = 0; s < 2; ++s) {
                         u32x4 bits = __builtin_bit_cast(u32x4, pl[k][s]);
                         bits &= keep[j];
-                        pl[k][s] = __builtin_bit_cast(typename P::vec, bits);
+                        pl[k][s] = __builtin_bit_cast(typename PG::vec, bits);
                         *(u32x4*)(a.g + k * a.g_plane + (tt * a.ksv + vt * 2 + s) * kBlk + lane * 16) = bits;
                     }
                     f32x16 tr = {};
-                    tr = P::mfma(pl[k][0], eye[0], tr);
-                    tr = P::mfma(pl[k][1], eye[1], tr);
-                    typename P::vec to[2];
+                    tr = PG::mfma(pl[k][0], eye[0], tr);
+                    tr = PG::mfma(pl[k][1], eye[1], tr);
+                    typename PG::vec to[2];
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) to[r >> 3][r & 7] = (typename P::elem)tr[r];
+                    for (int r = 0; r < 16; ++r) to[r >> 3][r & 7] = (typename PG::elem)tr[r];
 #pragma unroll
-                    for (int s = 0; s < 2; ++s) *(typename P::vec*)(a.gt + k * a.gt_plane + (vt * a.kst + tt * 2 + s) * kBlk + lane * 16) = to[s];
+                    for (int s = 0; s < 2; ++s) *(typename PG::vec*)(a.gt + k * a.gt_plane + (vt * a.kst + tt * 2 + s) * kBlk + lane * 16) = to[s];
                 }
             }
         }
@@ -689,7 +694,8 @@ __global__ __launch_bounds__(256) void k_finish(FinishSide x, FinishSide e, int6
 // ---- host --------------------------------------------------------------------------------------
 struct Plan {
     int planes = 1;
-    bool scaled = false, scale_g = false;
+    bool scaled = false;     // the matrices get powers of two
+    bool scale_g = false;    // so does G
     bool grads = false, forward = false;
     bool few = false;        // t <= kFewT: k_few_*
     bool small = false;      // else d <= kSmallD: k_small_*
@@ -714,9 +720,9 @@ Plan make_plan(const ccdpp_softmax_t& p, int call) {
     w.grads = call != CCDPP_SOFTMAX_LOSS;
     w.forward = call != CCDPP_SOFTMAX_GRAD;
     w.planes = p.dtype == CCDPP_F32 ? 2 : 1;
-    w.scaled = p.dtype == CCDPP_F32;
-    w.scale_g = w.grads && p.dtype != CCDPP_BF16;
     w.small = p.d <= kSmallD;
+    w.scaled = p.dtype == CCDPP_F32 || (p.dtype == CCDPP_BF16 && w.grads && !w.small);
+    w.scale_g = w.grads && (w.scaled || p.dtype == CCDPP_F16);
     w.tt = (p.t + 31) / 32, w.vt = (p.v + 31) / 32, w.dt = (p.d + 31) / 32;
     w.kst = w.tt * 2, w.ksv = w.vt * 2;
     int64_t at = 0;
@@ -899,6 +905,7 @@ template <int DT>
 int run_wide(const ccdpp_softmax_t& p, const Plan& w, const Outs& out, const int32_t* fin, char* ws, hipStream_t st) {
     typedef typename Types<DT>::in T;
     typedef typename Types<DT>::op P;
+    typedef typename Types<DT>::turned PG;
     constexpr int NPL = Types<DT>::planes;
     GemmArgs z = {};
     z.a = ws + w.o_ef, z.b = ws + w.o_xf;
@@ -910,7 +917,7 @@ int run_wide(const ccdpp_softmax_t& p, const Plan& w, const Outs& out, const int
     if (w.forward) {
         z.part = (float2*)(ws + w.o_part);
         const int64_t blocks = (w.vt + 7) / 8 * ((w.tt + 7) / 8);
-        k_gemm<P, NPL, EPI_LSE, T><<<(unsigned)blocks, 512, 0, st>>>(z);
+        k_gemm<P, PG, NPL, EPI_LSE, T><<<(unsigned)blocks, 512, 0, st>>>(z);
         OPS_LAUNCH("logits");
         if (int rc = launch_loss<T>(p, z.part, (w.vt + 7) / 8, Shares{}, out.loss, out.lse, RowNumbers{}, st)) return rc;
     }
@@ -924,7 +931,7 @@ int run_wide(const ccdpp_softmax_t& p, const Plan& w, const Outs& out, const int
         GemmArgs q = z;
         q.v0 = v0, q.a = z.a + v0 / 32 * z.a_tile, q.o2 = z.o2 + v0, q.m_tiles = nt;
         q.ksv = nt * 2, q.g_plane = w.tt * q.ksv * kBlk, q.gt_plane = nt * w.kst * kBlk;
-        k_gemm<P, NPL, EPI_G, T><<<(unsigned)((nt + 7) / 8 * ((w.tt + 7) / 8)), 512, 0, st>>>(q);
+        k_gemm<P, PG, NPL, EPI_G, T><<<(unsigned)((nt + 7) / 8 * ((w.tt + 7) / 8)), 512, 0, st>>>(q);
         OPS_LAUNCH("G");
         GemmArgs o = {};
         o.n_tiles = w.dt, o.cols = p.d, o.scale = p.scale, o.fin = fin;
@@ -934,7 +941,7 @@ int run_wide(const ccdpp_softmax_t& p, const Plan& w, const Outs& out, const int
             o.kb = nt, o.splits = w.sx, o.out = (float*)(ws + w.o_dx), o.out_split = p.t * w.dp, o.add = v0 > 0;
             o.which = w.scaled ? 0 : -1;
             o.last = dx_whole ? out.dx : nullptr, o.ldo = o.last ? out.lddx : w.dp;
-            k_gemm<P, NPL, EPI_OUT, T><<<dim3((unsigned)((w.tt + 7) / 8 * ((w.dt + 7) / 8)), w.sx), 512, 0, st>>>(o);
+            k_gemm<PG, PG, NPL, EPI_OUT, T><<<dim3((unsigned)((w.tt + 7) / 8 * ((w.dt + 7) / 8)), w.sx), 512, 0, st>>>(o);
             OPS_LAUNCH("dx");
         }
         if (out.de) {
@@ -944,7 +951,7 @@ int run_wide(const ccdpp_softmax_t& p, const Plan& w, const Outs& out, const int
             o.which = w.scaled ? 1 : -1;
             T* const de = (T*)out.de + v0 * out.ldde;
             o.last = w.se == 1 ? de : nullptr, o.ldo = o.last ? out.ldde : w.dp;
-            k_gemm<P, NPL, EPI_OUT, T><<<dim3((unsigned)((nt + 7) / 8 * ((w.dt + 7) / 8)), w.se), 512, 0, st>>>(o);
+            k_gemm<PG, PG, NPL, EPI_OUT, T><<<dim3((unsigned)((nt + 7) / 8 * ((w.dt + 7) / 8)), w.se), 512, 0, st>>>(o);
             OPS_LAUNCH("dtable");
             if (!o.last)
                 if (int rc = finish<T>(FinishSide{}, FinishSide{o.out, w.se, o.out_split, n, w.dp, de, out.ldde, o.which, -1, {}}, p.d, p.scale, fin, st)) return rc;
@@ -965,9 +972,10 @@ int run(const ccdpp_softmax_t& p, int call, const Outs& out, char* ws, hipStream
     sc.e_part = (float*)(ws + w.o_scale), sc.x_part = sc.e_part + kParts, sc.g_part = sc.x_part + kParts;
     sc.fin = (int32_t*)(ws + w.o_fin), sc.x_row = (float*)(ws + w.o_xrow);
     const int32_t* fin = w.scaled || w.scale_g ? sc.fin : nullptr;
-    if (w.scaled) k_scales<true><<<kParts, 1024, 0, st>>>(p, out.grad, sc, w.grads);
-    else if (w.scale_g) k_scales<false><<<kParts, 1024, 0, st>>>(p, out.grad, sc, w.grads);
-    OPS_LAUNCH("scales");
+    if (w.scaled || w.scale_g) {
+        k_scales<T><<<kParts, 1024, 0, st>>>(p, out.grad, sc, w.scaled, w.grads);
+        OPS_LAUNCH("scales");
+    }
 
     PackArgs pk = {};
     pk.sc = sc, pk.scaled = w.scaled, pk.weights = w.scale_g;
@@ -999,7 +1007,9 @@ int run(const ccdpp_softmax_t& p, int call, const Outs& out, char* ws, hipStream
             x.turned_row = e.turned_row = 2 * kBlk;
         }
     }
-    k_pack<DT><<<dim3((unsigned)(w.tt + w.vt), (p.d + 127) / 128), 256, 0, st>>>(pk);
+    const dim3 grid((unsigned)(w.tt + w.vt), (p.d + 127) / 128);
+    if (w.small) k_pack<DT, true><<<grid, 256, 0, st>>>(pk);
+    else k_pack<DT, false><<<grid, 256, 0, st>>>(pk);
     OPS_LAUNCH("pack");
     return w.small ? run_small<DT>(p, w, out, fin, ws, st) : run_wide<DT>(p, w, out, fin, ws, st);
 }

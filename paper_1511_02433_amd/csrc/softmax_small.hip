@@ -269,8 +269,10 @@ __device__ __forceinline__ void small_terms(const SmallArgs& a, int64_t tile, in
                 for (int r = 0; r < 16; ++r) g[r] -= y == 8 * (r >> 2) + 4 * h + (r & 3) ? (float)(1 << kTermExp) : 0.f;
             }
         }
-        typename P::vec pl[NPL][2];
-        split_terms<P, NPL>(g, pl);
+        // Two planes of G for 16-bit types too: the products are not what bounds these, and one plane's rounding would
+        // cost as much as that of the result.
+        typename P::vec pl[2][2];
+        split_terms<P, 2>(g, pl);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = kAhead; i < DT * 2; ++i) turned(i);
@@ -278,12 +280,10 @@ __device__ __forceinline__ void small_terms(const SmallArgs& a, int64_t tile, in
         for (int i = 0; i < DT * 2; ++i) {
             f32x16& o = out[i >> 1];
             o = P::mfma(tf[0][i], pl[0][i & 1], o);
-            if constexpr (NPL == 2) {
-                o = P::mfma(tf[0][i], pl[1][i & 1], o);
-                o = P::mfma(tf[1][i], pl[0][i & 1], o);
-            }
+            o = P::mfma(tf[0][i], pl[1][i & 1], o);
+            if constexpr (NPL == 2) o = P::mfma(tf[1][i], pl[0][i & 1], o);
         }
-        interleave<DT * 2, NPL, NPL == 2 ? 3 : 1, kAhead, (kAhead < DT * 2 ? kAhead : DT * 2)>();
+        interleave<DT * 2, NPL, NPL + 1, kAhead, (kAhead < DT * 2 ? kAhead : DT * 2)>();
         __builtin_amdgcn_sched_barrier(0);
     });
 }
