@@ -272,7 +272,7 @@ __global__ __launch_bounds__(256) void k_pack(PackArgs a) {
 }
 
 // ---- the product -----------------------------------------------------------------------------
-// C (M x N) = A (M x K) B (N x K)^T from fragments: 256 x 256 of C per block, 8 waves of 128 x 64 each.
+// C (M x N) = A (M x K) B (N x K)^T from fragments: 256 x 256 of C per block.
 enum { EPI_LSE = 0, EPI_G = 1, EPI_OUT = 2 };
 
 struct GemmArgs {
@@ -298,8 +298,9 @@ struct GemmArgs {
     int64_t g_plane, gt_plane;
     int64_t ksv, kst;
     // other products
-    float* out;                  // [split][M][ldo]
+    float* out;                  // [split][N][ldo]: of a gradient's rows; M are its columns
     void* last;                  // or the result itself
+    int wide;                    // its rows are aligned to four values
     int64_t out_split, rows, cols, ldo;
     int add, which;              // which: the exponent in fin of the other operand, or -1
 };
@@ -308,129 +309,185 @@ constexpr int kStages = 4;          // of LDS, each a step of 32 over K of both 
 constexpr int kStage = 32 * kBlk;
 
 // P: operands; PG: terms G.
+constexpr int kNf = 2;                  // blocks of 32 columns of a wave
+constexpr int kWaveCols = 8 / kNf;      // waves beside each other
+constexpr int kWaves = 2 * kWaveCols, kGemmThreads = 64 * kWaves;
+constexpr int kEach = 8 / kWaves;       // blocks of 32 rows of each operand that a wave fetches
+
 template <class P, class PG, int NPL, int EPI, class T>
-__global__ __launch_bounds__(512) void k_gemm(GemmArgs a) {
+__global__ __launch_bounds__(kGemmThreads) void k_gemm(GemmArgs a) {
     constexpr int NSEG = NPL == 2 ? 3 : 1;
     __shared__ __align__(16) char lds[kStages * kStage];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wm = wave >> 2, wn = wave & 3;
+    const int wm = wave / kWaveCols, wn = wave % kWaveCols;
     const int split = blockIdx.y;
     // Blocks b, b + 8, .. share an XCD and its L2: each gets a contiguous run of tiles, eight rows of tiles at a time.
+    // (Places are the same for all lanes, which the compiler does not see through the divisions.)
     const int64_t mb = (a.m_tiles + 7) / 8, nb = (a.n_tiles + 7) / 8;
-    int64_t bm, bn;
+    int bm, bn;
     {
         const int64_t all = mb * nb, x = blockIdx.x & 7, per = all >> 3, more = all & 7;
         const int64_t id = x * per + min(x, more) + (blockIdx.x >> 3);
         const int64_t band = id / (8 * nb), first = band * 8, height = min((int64_t)8, mb - first);
         const int64_t in = id - band * 8 * nb;
-        bm = first + in % height, bn = in / height;
+        bm = __builtin_amdgcn_readfirstlane((int)(first + in % height));
+        bn = __builtin_amdgcn_readfirstlane((int)(in / height));
     }
-    const int64_t k0 = a.kb * split / a.splits, k1 = a.kb * (split + 1) / a.splits;
-    f32x16 acc[4][2];
+    const int k0 = __builtin_amdgcn_readfirstlane((int)(a.kb * split / a.splits));
+    const int steps = __builtin_amdgcn_readfirstlane((int)(a.kb * (split + 1) / a.splits)) - k0, total = steps * NSEG;
+    f32x16 acc[4][kNf];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int j = 0; j < kNf; ++j)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
 
-    // A wave brings one block of 32 rows of either operand, 2 KB a stage each.
-    const int64_t steps = k1 - k0, total = steps * NSEG;
+    // A wave brings kEach blocks of 32 rows of either operand, 2 KB a stage each.
     if (total > 0) {
-        const char* const a0 = a.a + min(bm * 8 + wave, a.m_tiles - 1) * a.a_tile + k0 * 2 * kBlk + lane * 16;
-        const char* const b0 = a.b + min(bn * 8 + wave, a.n_tiles - 1) * a.b_tile + k0 * 2 * kBlk + lane * 16;
-        const char *pa = a0, *pb = b0;
-        int64_t left = steps;
-        int seg = 0;
-        char* const to = lds + wave * 2 * kBlk;
+        const char *a0[kEach], *b0[kEach];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            a0[i] = a.a + min((int64_t)bm * 8 + wave * kEach + i, a.m_tiles - 1) * a.a_tile + (int64_t)k0 * 2 * kBlk;
+            b0[i] = a.b + min((int64_t)bn * 8 + wave * kEach + i, a.n_tiles - 1) * a.b_tile + (int64_t)k0 * 2 * kBlk;
+        }
+        char* const to = lds + wave * kEach * 2 * kBlk;
+        const uint32_t mine = lane * 16;
         int slot = 0;
+        int k_next = 0;
         // Past the last step the last one is fetched again, so that the count of loads in flight stays the same.
         const auto next = [&]() {
-            char* const s = to + slot * kStage;
-            fetch(pa, s);
-            fetch(pa + kBlk, s + kBlk);
-            fetch(pb, s + 16 * kBlk);
-            fetch(pb + kBlk, s + 17 * kBlk);
-            slot = (slot + 1) & (kStages - 1);
-            if (--left > 0) {
-                pa += 2 * kBlk, pb += 2 * kBlk;
-            } else if (seg < NSEG - 1) {
-                ++seg;
-                pa = a0 + (seg == 2 ? a.a_plane : 0), pb = b0 + (seg == 1 ? a.b_plane : 0);
-                left = steps;
-            } else {
-                left = 1;
+            int64_t at_a = (int64_t)k_next * 2 * kBlk, at_b = at_a;
+            if constexpr (NSEG == 3) {
+                const int64_t run = (int64_t)steps * 2 * kBlk, second = k_next >= steps ? run : 0, third = k_next >= 2 * steps ? run : 0;
+                at_a += (third ? a.a_plane : 0) - second - third;
+                at_b += (second && !third ? a.b_plane : 0) - second - third;
             }
+            k_next += k_next + 1 < total ? 1 : 0;
+            char* const s = to + slot * kStage;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const char *pa = a0[i] + at_a, *pb = b0[i] + at_b;
+                fetch(pa + mine, s + i * 2 * kBlk);
+                fetch(pa + kBlk + mine, s + (i * 2 + 1) * kBlk);
+                fetch(pb + mine, s + (16 + i * 2) * kBlk);
+                fetch(pb + kBlk + mine, s + (16 + i * 2 + 1) * kBlk);
+            }
+            slot = (slot + 1) & (kStages - 1);
         };
-        typename P::vec fa[2][4], fb[2][2];
+        typename P::vec fa[2][4], fb[2][kNf];
         const char* const ra = lds + wm * 8 * kBlk + lane * 16;
-        const char* const rb = lds + (16 + wn * 4) * kBlk + lane * 16;
+        const char* const rb = lds + (16 + wn * kNf * 2) * kBlk + lane * 16;
         const auto read = [&](int s, int at, int buf) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) fa[buf][i] = *(const typename P::vec*)(ra + at * kStage + (2 * i + s) * kBlk);
 #pragma unroll
-            for (int j = 0; j < 2; ++j) fb[buf][j] = *(const typename P::vec*)(rb + at * kStage + (2 * j + s) * kBlk);
+            for (int j = 0; j < kNf; ++j) fb[buf][j] = *(const typename P::vec*)(rb + at * kStage + (2 * j + s) * kBlk);
         };
-        // Eight products; the reads (and fetches) issued with them go in between, one after each.
+        // The reads (and fetches) issued with a run of products go in between, one after each.
         const auto multiply = [&](int buf, bool fetched) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int j = 0; j < 2; ++j) acc[i][j] = P::mfma(fa[buf][i], fb[buf][j], acc[i][j]);
+                for (int j = 0; j < kNf; ++j) acc[i][j] = P::mfma(fa[buf][i], fb[buf][j], acc[i][j]);
+            constexpr int kProducts = 4 * kNf, kReads = 4 + kNf, kFetches = 4 * kEach;
 #pragma unroll
-            for (int i = 0; i < 6; ++i) {
+            for (int i = 0; i < kProducts; ++i) {
                 __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-                if (fetched && i < 4) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+                if (i < kReads) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                else if (fetched && i < kReads + kFetches) __builtin_amdgcn_sched_group_barrier(0x020, (kFetches + kProducts - kReads - 1) / (kProducts - kReads), 0);
             }
-            __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
             __builtin_amdgcn_sched_barrier(0);
             asm volatile("" ::: "memory");
         };
         next(), next(), next(), next();
-        asm volatile("s_waitcnt vmcnt(12)" ::: "memory");
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(12 * kEach) : "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         read(0, 0, 0);
         int at = 0;
-        for (int64_t k = total; k > 0; --k) {
+        for (int k = total; k > 0; --k) {
             read(1, at, 1);
             multiply(0, false);
             // Everybody is done with this stage and has the next one: fetch into this one, read on in the next.
-            asm volatile("s_waitcnt vmcnt(8) lgkmcnt(0)" ::: "memory");
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(8 * kEach) : "memory");
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
-            next();
             at = (at + 1) & (kStages - 1);
             read(0, at, 0);
+            next();
             multiply(1, true);
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
     const int n = lane & 31, h = lane >> 5;
     if constexpr (EPI == EPI_OUT) {
+        // The product is the gradient turned: a lane has four neighbouring columns of a row at a time.
         // Last piece and only share: the caller's type.  Else 32 bits, added to what earlier pieces left.
         const float fg = a.fin ? ldexpf(1.f, -a.fin[2]) : 1.f, f = a.fin && a.which >= 0 ? ldexpf(a.scale, -a.fin[a.which]) : a.scale;
-        float* const part = a.out + split * a.out_split;
+        struct alignas(4 * sizeof(T)) Four { T v[4]; };
+        if (a.last && !a.wide) {
+            // Rows that are not aligned: 32 rows of the wave's 128 columns at a time through LDS (quads of columns swapped
+            // about by the row, so that neither side meets a bank twice), and out 64 neighbours at a time.
+            __syncthreads();
+            float* const mine = (float*)(lds + wave * (32 * 128 * 4));
+            const int64_t col0 = ((int64_t)bm * 8 + wm * 4) * 32;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+            for (int j = 0; j < kNf; ++j) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int64_t col = (bn * 8 + wn * 2 + j) * 32 + n;
-                const int64_t row0 = (bm * 8 + wm * 4 + i) * 32 + 4 * h;
-                if (col >= a.cols) continue;
+                for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int64_t row = row0 + 8 * (r >> 2) + (r & 3);
-                    if (row >= a.rows) continue;
-                    if (a.last) {
-                        ((T*)a.last)[row * a.ldo + col] = (T)(acc[i][j][r] * fg * f);
+                    for (int q = 0; q < 4; ++q) {
+                        f32x4 v;
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) v[r] = acc[i][j][4 * q + r] * fg * f;
+                        *(f32x4*)(mine + n * 128 + ((i * 8 + 2 * q + h) ^ n) * 4) = v;
+                    }
+                __builtin_amdgcn_wave_barrier();
+                const int64_t row0 = ((int64_t)bn * 8 + wn * kNf + j) * 32;
+                const int rows = (int)min((int64_t)32, a.rows - row0);
+#pragma unroll 4
+                for (int r = 0; r < rows; ++r)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const int c = lane + 64 * k;
+                        if (col0 + c < a.cols) ((T*)a.last)[(row0 + r) * a.ldo + col0 + c] = (T)mine[r * 128 + ((c >> 2) ^ r) * 4 + (c & 3)];
+                    }
+                __builtin_amdgcn_wave_barrier();
+            }
+            return;
+        }
+#pragma unroll
+        for (int j = 0; j < kNf; ++j) {
+            const int64_t row = ((int64_t)bn * 8 + wn * kNf + j) * 32 + n;
+            if (row >= a.rows) continue;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int64_t col = ((int64_t)bm * 8 + wm * 4 + i) * 32 + 8 * q + 4 * h;
+                    if (col >= a.cols) continue;
+                    f32x4 v;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) v[r] = acc[i][j][4 * q + r];
+                    if (!a.last) {  // columns of partial sums are a multiple of four
+                        f32x4* const o = (f32x4*)(a.out + split * a.out_split + row * a.ldo + col);
+                        *o = a.add ? *o + v : v;
+                        continue;
+                    }
+                    Four t;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) t.v[r] = (T)(v[r] * fg * f);
+                    T* const o = (T*)a.last + row * a.ldo + col;
+                    if (a.wide && col + 4 <= a.cols) {
+                        *(Four*)o = t;
                     } else {
-                        float* o = part + row * a.ldo + col;
-                        *o = a.add ? *o + acc[i][j][r] : acc[i][j][r];
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (col + r < a.cols) o[r] = t.v[r];
                     }
                 }
-            }
+        }
         return;
     }
     // Logits in base 2: accumulator times the row's factor, plus offset.
@@ -441,12 +498,12 @@ __global__ __launch_bounds__(512) void k_gemm(GemmArgs a) {
     };
     if constexpr (EPI == EPI_LSE) {
         float2(*share)[256] = (float2(*)[256])lds;
-        float f[2], top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
+        float f[kNf], top[kNf], sum[kNf];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) f[j] = a.xf[min((bn * 8 + wn * 2 + j) * 32 + n, a.t - 1)];
+        for (int j = 0; j < kNf; ++j) top[j] = -INFINITY, sum[j] = 0.f, f[j] = a.xf[min(((int64_t)bn * 8 + wn * kNf + j) * 32 + n, a.t - 1)];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int64_t tile = bm * 8 + wm * 4 + i;
+            const int64_t tile = (int64_t)bm * 8 + wm * 4 + i;
             f32x4 o[4];
             if (tile < a.m_tiles) {
                 offsets(tile, o);
@@ -455,7 +512,7 @@ __global__ __launch_bounds__(512) void k_gemm(GemmArgs a) {
                 for (int q = 0; q < 4; ++q) o[q] = -INFINITY;
             }
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+            for (int j = 0; j < kNf; ++j)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     acc[i][j][r] = fmaf(acc[i][j][r], f[j], o[r >> 2][r & 3]);
@@ -464,7 +521,7 @@ __global__ __launch_bounds__(512) void k_gemm(GemmArgs a) {
         }
         __syncthreads();  // LDS is free
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
+        for (int j = 0; j < kNf; ++j) {
             top[j] = fmaxf(top[j], __shfl_xor(top[j], 32));
             const float ref = top[j] == -INFINITY ? 0.f : top[j];
 #pragma unroll
@@ -472,12 +529,12 @@ __global__ __launch_bounds__(512) void k_gemm(GemmArgs a) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) sum[j] += exp2_fast(acc[i][j][r] - ref);
             sum[j] += __shfl_xor(sum[j], 32);
-            if (h == 0) share[wm][(wn * 2 + j) * 32 + n] = make_float2(top[j], sum[j]);
+            if (h == 0) share[wm][(wn * kNf + j) * 32 + n] = make_float2(top[j], sum[j]);
         }
         __syncthreads();
-        if (threadIdx.x < 256) {
-            const int64_t t = bn * 256 + threadIdx.x;
-            const float2 p = share[0][threadIdx.x], q = share[1][threadIdx.x];
+        for (int i = threadIdx.x; i < 256; i += kGemmThreads) {
+            const int64_t t = (int64_t)bn * 256 + i;
+            const float2 p = share[0][i], q = share[1][i];
             const float m = fmaxf(p.x, q.x);
             const float mr = m == -INFINITY ? 0.f : m;
             if (t < a.t) a.part[bm * a.t + t] = make_float2(m, p.y * exp2_fast(p.x - mr) + q.y * exp2_fast(q.x - mr));
@@ -491,12 +548,12 @@ __global__ __launch_bounds__(512) void k_gemm(GemmArgs a) {
         for (int s = 0; s < 2; ++s)
 #pragma unroll
             for (int k = 0; k < 8; ++k) eye[s][k] = (typename PG::elem)(16 * s + (k < 4 ? 4 * h + k : 8 + 4 * h + k - 4) == n ? 1.f : 0.f);
-        float w[2], l2[2], f[2];
-        int64_t y[2];        // target, from the piece's first entry
-        uint32_t keep[2];    // all ones in rows that count: others are cut off as bits, whatever they hold
+        float w[kNf], l2[kNf], f[kNf];
+        int64_t y[kNf];        // target, from the piece's first entry
+        uint32_t keep[kNf];    // all ones in rows that count: others are cut off as bits, whatever they hold
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int64_t t = (bn * 8 + wn * 2 + j) * 32 + n;
+        for (int j = 0; j < kNf; ++j) {
+            const int64_t t = ((int64_t)bn * 8 + wn * kNf + j) * 32 + n;
             w[j] = 0.f, l2[j] = 0.f, f[j] = 0.f, y[j] = -1, keep[j] = 0;
             if (t < a.t) {
                 const int64_t yt = load_target(a.target, a.target_bits, t);
@@ -513,13 +570,13 @@ __global__ __launch_bounds__(512) void k_gemm(GemmArgs a) {
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int64_t vt = bm * 8 + wm * 4 + i;
+            const int64_t vt = (int64_t)bm * 8 + wm * 4 + i;
             if (vt >= a.m_tiles) continue;
             f32x4 o[4];
             offsets(vt, o);
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int64_t tt = bn * 8 + wn * 2 + j;
+            for (int j = 0; j < kNf; ++j) {
+                const int64_t tt = (int64_t)bn * 8 + wn * kNf + j;
                 if (tt >= a.n_tiles) continue;
                 float g[16];
 #pragma unroll
@@ -713,7 +770,7 @@ struct Plan {
     int64_t o_scale, o_xrow, o_fin, o_xf, o_ef, o_xl, o_o2, o_xn, o_xt, o_et, o_g, o_gt, o_part, o_dx, o_de, bytes;
 };
 
-constexpr int64_t kPieceBytes = int64_t(128) << 20;  // of G
+constexpr int64_t kPieceBytes = int64_t(512) << 20;  // of G (8192 x 131072 x 4096: 1.5% over 128 MiB)
 
 Plan make_plan(const ccdpp_softmax_t& p, int call) {
     Plan w;
@@ -917,7 +974,7 @@ int run_wide(const ccdpp_softmax_t& p, const Plan& w, const Outs& out, const int
     if (w.forward) {
         z.part = (float2*)(ws + w.o_part);
         const int64_t blocks = (w.vt + 7) / 8 * ((w.tt + 7) / 8);
-        k_gemm<P, PG, NPL, EPI_LSE, T><<<(unsigned)blocks, 512, 0, st>>>(z);
+        k_gemm<P, PG, NPL, EPI_LSE, T><<<(unsigned)blocks, kGemmThreads, 0, st>>>(z);
         OPS_LAUNCH("logits");
         if (int rc = launch_loss<T>(p, z.part, (w.vt + 7) / 8, Shares{}, out.loss, out.lse, RowNumbers{}, st)) return rc;
     }
@@ -931,27 +988,28 @@ int run_wide(const ccdpp_softmax_t& p, const Plan& w, const Outs& out, const int
         GemmArgs q = z;
         q.v0 = v0, q.a = z.a + v0 / 32 * z.a_tile, q.o2 = z.o2 + v0, q.m_tiles = nt;
         q.ksv = nt * 2, q.g_plane = w.tt * q.ksv * kBlk, q.gt_plane = nt * w.kst * kBlk;
-        k_gemm<P, PG, NPL, EPI_G, T><<<(unsigned)((nt + 7) / 8 * ((w.tt + 7) / 8)), 512, 0, st>>>(q);
+        k_gemm<P, PG, NPL, EPI_G, T><<<(unsigned)((nt + 7) / 8 * ((w.tt + 7) / 8)), kGemmThreads, 0, st>>>(q);
         OPS_LAUNCH("G");
         GemmArgs o = {};
-        o.n_tiles = w.dt, o.cols = p.d, o.scale = p.scale, o.fin = fin;
+        o.m_tiles = w.dt, o.cols = p.d, o.scale = p.scale, o.fin = fin;
+        const auto wide = [](const void* at, int64_t ld) { return ((uintptr_t)at | (uintptr_t)(ld * sizeof(T))) % (4 * sizeof(T)) == 0; };
         if (out.dx) {
-            o.a = z.g, o.a_plane = q.g_plane, o.a_tile = q.ksv * kBlk, o.m_tiles = w.tt, o.rows = p.t;
-            o.b = ws + w.o_et + v0 / 16 * kBlk, o.b_plane = w.dt * w.ksv * kBlk, o.b_tile = w.ksv * kBlk;
+            o.a = ws + w.o_et + v0 / 16 * kBlk, o.a_plane = w.dt * w.ksv * kBlk, o.a_tile = w.ksv * kBlk;
+            o.b = z.g, o.b_plane = q.g_plane, o.b_tile = q.ksv * kBlk, o.n_tiles = w.tt, o.rows = p.t;
             o.kb = nt, o.splits = w.sx, o.out = (float*)(ws + w.o_dx), o.out_split = p.t * w.dp, o.add = v0 > 0;
             o.which = w.scaled ? 0 : -1;
-            o.last = dx_whole ? out.dx : nullptr, o.ldo = o.last ? out.lddx : w.dp;
-            k_gemm<PG, PG, NPL, EPI_OUT, T><<<dim3((unsigned)((w.tt + 7) / 8 * ((w.dt + 7) / 8)), w.sx), 512, 0, st>>>(o);
+            o.last = dx_whole ? out.dx : nullptr, o.ldo = o.last ? out.lddx : w.dp, o.wide = wide(out.dx, out.lddx);
+            k_gemm<PG, PG, NPL, EPI_OUT, T><<<dim3((unsigned)((w.tt + 7) / 8 * ((w.dt + 7) / 8)), w.sx), kGemmThreads, 0, st>>>(o);
             OPS_LAUNCH("dx");
         }
         if (out.de) {
-            o.a = z.gt, o.a_plane = q.gt_plane, o.a_tile = w.kst * kBlk, o.m_tiles = nt, o.rows = n;
-            o.b = ws + w.o_xt, o.b_plane = w.dt * w.kst * kBlk, o.b_tile = w.kst * kBlk;
+            o.a = ws + w.o_xt, o.a_plane = w.dt * w.kst * kBlk, o.a_tile = w.kst * kBlk;
+            o.b = z.gt, o.b_plane = q.gt_plane, o.b_tile = w.kst * kBlk, o.n_tiles = nt, o.rows = n;
             o.kb = w.tt, o.splits = w.se, o.out = (float*)(ws + w.o_de), o.out_split = w.vc * w.dp, o.add = 0;
             o.which = w.scaled ? 1 : -1;
             T* const de = (T*)out.de + v0 * out.ldde;
-            o.last = w.se == 1 ? de : nullptr, o.ldo = o.last ? out.ldde : w.dp;
-            k_gemm<PG, PG, NPL, EPI_OUT, T><<<dim3((unsigned)((nt + 7) / 8 * ((w.dt + 7) / 8)), w.se), 512, 0, st>>>(o);
+            o.last = w.se == 1 ? de : nullptr, o.ldo = o.last ? out.ldde : w.dp, o.wide = wide(de, out.ldde);
+            k_gemm<PG, PG, NPL, EPI_OUT, T><<<dim3((unsigned)((nt + 7) / 8 * ((w.dt + 7) / 8)), w.se), kGemmThreads, 0, st>>>(o);
             OPS_LAUNCH("dtable");
             if (!o.last)
                 if (int rc = finish<T>(FinishSide{}, FinishSide{o.out, w.se, o.out_split, n, w.dp, de, out.ldde, o.which, -1, {}}, p.d, p.scale, fin, st)) return rc;
