@@ -305,7 +305,7 @@ struct GemmArgs {
     int add, which;              // which: the exponent in fin of the other operand, or -1
 };
 
-constexpr int kStages = 4;          // of LDS, each a step of 32 over K of both operands
+constexpr int kStages = 4;          // of LDS
 constexpr int kStage = 32 * kBlk;
 
 // P: operands; PG: terms G.
@@ -316,7 +316,6 @@ constexpr int kEach = 8 / kWaves;       // blocks of 32 rows of each operand tha
 
 template <class P, class PG, int NPL, int EPI, class T>
 __global__ __launch_bounds__(kGemmThreads) void k_gemm(GemmArgs a) {
-    constexpr int NSEG = NPL == 2 ? 3 : 1;
     __shared__ __align__(16) char lds[kStages * kStage];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / kWaveCols, wn = wave % kWaveCols;
@@ -334,7 +333,7 @@ __global__ __launch_bounds__(kGemmThreads) void k_gemm(GemmArgs a) {
         bn = __builtin_amdgcn_readfirstlane((int)(in / height));
     }
     const int k0 = __builtin_amdgcn_readfirstlane((int)(a.kb * split / a.splits));
-    const int steps = __builtin_amdgcn_readfirstlane((int)(a.kb * (split + 1) / a.splits)) - k0, total = steps * NSEG;
+    const int steps = __builtin_amdgcn_readfirstlane((int)(a.kb * (split + 1) / a.splits)) - k0;
     f32x16 acc[4][kNf];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -343,82 +342,109 @@ __global__ __launch_bounds__(kGemmThreads) void k_gemm(GemmArgs a) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
 
-    // A wave brings kEach blocks of 32 rows of either operand, 2 KB a stage each.
-    if (total > 0) {
+    // A stage of LDS is 32 KB.  One plane: 32 columns of K, two steps of 16.  Two planes: 16 columns, hi and lo.  A wave
+    // brings kEach blocks of 32 rows of either operand.
+    if (steps > 0) {
         const char *a0[kEach], *b0[kEach];
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             a0[i] = a.a + min((int64_t)bm * 8 + wave * kEach + i, a.m_tiles - 1) * a.a_tile + (int64_t)k0 * 2 * kBlk;
             b0[i] = a.b + min((int64_t)bn * 8 + wave * kEach + i, a.n_tiles - 1) * a.b_tile + (int64_t)k0 * 2 * kBlk;
         }
+        const int total = NPL == 2 ? 2 * steps : steps;  // stages
+        constexpr int kStep = NPL == 2 ? kBlk : 2 * kBlk;
+        const int64_t beside_a = NPL == 2 ? a.a_plane : kBlk, beside_b = NPL == 2 ? a.b_plane : kBlk;
         char* const to = lds + wave * kEach * 2 * kBlk;
         const uint32_t mine = lane * 16;
-        int slot = 0;
-        int k_next = 0;
-        // Past the last step the last one is fetched again, so that the count of loads in flight stays the same.
+        int slot = 0, k_next = 0;
+        // Past the last stage the last one is fetched again, so that the count of loads in flight stays the same.
         const auto next = [&]() {
-            int64_t at_a = (int64_t)k_next * 2 * kBlk, at_b = at_a;
-            if constexpr (NSEG == 3) {
-                const int64_t run = (int64_t)steps * 2 * kBlk, second = k_next >= steps ? run : 0, third = k_next >= 2 * steps ? run : 0;
-                at_a += (third ? a.a_plane : 0) - second - third;
-                at_b += (second && !third ? a.b_plane : 0) - second - third;
-            }
-            k_next += k_next + 1 < total ? 1 : 0;
+            const int64_t at_k = (int64_t)k_next * kStep;
+            k_next = __builtin_amdgcn_readfirstlane(min(k_next + 1, total - 1));
             char* const s = to + slot * kStage;
 #pragma unroll
             for (int i = 0; i < kEach; ++i) {
-                const char *pa = a0[i] + at_a, *pb = b0[i] + at_b;
+                const char *pa = a0[i] + at_k, *pb = b0[i] + at_k;
                 fetch(pa + mine, s + i * 2 * kBlk);
-                fetch(pa + kBlk + mine, s + (i * 2 + 1) * kBlk);
+                fetch(pa + beside_a + mine, s + (i * 2 + 1) * kBlk);
                 fetch(pb + mine, s + (16 + i * 2) * kBlk);
-                fetch(pb + kBlk + mine, s + (16 + i * 2 + 1) * kBlk);
+                fetch(pb + beside_b + mine, s + (16 + i * 2 + 1) * kBlk);
             }
             slot = (slot + 1) & (kStages - 1);
         };
-        typename P::vec fa[2][4], fb[2][kNf];
         const char* const ra = lds + wm * 8 * kBlk + lane * 16;
         const char* const rb = lds + (16 + wn * kNf * 2) * kBlk + lane * 16;
-        const auto read = [&](int s, int at, int buf) {
+        // What a stage holds for this wave, the half `s` of it (step or plane).
+        const auto read = [&](int s, int at, typename P::vec* fa, typename P::vec* fb) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) fa[buf][i] = *(const typename P::vec*)(ra + at * kStage + (2 * i + s) * kBlk);
+            for (int i = 0; i < 4; ++i) fa[i] = *(const typename P::vec*)(ra + at * kStage + (2 * i + s) * kBlk);
 #pragma unroll
-            for (int j = 0; j < kNf; ++j) fb[buf][j] = *(const typename P::vec*)(rb + at * kStage + (2 * j + s) * kBlk);
+            for (int j = 0; j < kNf; ++j) fb[j] = *(const typename P::vec*)(rb + at * kStage + (2 * j + s) * kBlk);
         };
-        // The reads (and fetches) issued with a run of products go in between, one after each.
-        const auto multiply = [&](int buf, bool fetched) {
+        const auto multiply = [&](const typename P::vec* fa, const typename P::vec* fb) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int j = 0; j < kNf; ++j) acc[i][j] = P::mfma(fa[buf][i], fb[buf][j], acc[i][j]);
-            constexpr int kProducts = 4 * kNf, kReads = 4 + kNf, kFetches = 4 * kEach;
+                for (int j = 0; j < kNf; ++j) acc[i][j] = P::mfma(fa[i], fb[j], acc[i][j]);
+        };
+        // The order of a run of `products`: a read from LDS after each of the first ones, then the fetches.
+        const auto order = [](auto products, auto reads, auto fetches) {
+            constexpr int p = decltype(products)::value, r = decltype(reads)::value, f = decltype(fetches)::value;
 #pragma unroll
-            for (int i = 0; i < kProducts; ++i) {
+            for (int i = 0; i < p; ++i) {
                 __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                if (i < kReads) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-                else if (fetched && i < kReads + kFetches) __builtin_amdgcn_sched_group_barrier(0x020, (kFetches + kProducts - kReads - 1) / (kProducts - kReads), 0);
+                if (i < r) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                else if (f && i < r + f) __builtin_amdgcn_sched_group_barrier(0x020, (f + p - r - 1) / (p - r), 0);
             }
             __builtin_amdgcn_sched_barrier(0);
             asm volatile("" ::: "memory");
         };
+        // Everybody has read this stage into registers and brought what the next one holds.
+        const auto meet = [&]() {
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(8 * kEach) : "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+        };
+        constexpr std::integral_constant<int, 4 * kNf> kRun = {};
+        constexpr std::integral_constant<int, 4 + kNf> kReads = {};
+        constexpr std::integral_constant<int, 4 * kEach> kFetches = {};
+        constexpr std::integral_constant<int, 0> kNone = {};
         next(), next(), next(), next();
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"(12 * kEach) : "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        read(0, 0, 0);
         int at = 0;
-        for (int k = total; k > 0; --k) {
-            read(1, at, 1);
-            multiply(0, false);
-            // Everybody is done with this stage and has the next one: fetch into this one, read on in the next.
-            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(8 * kEach) : "memory");
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-            at = (at + 1) & (kStages - 1);
-            read(0, at, 0);
-            next();
-            multiply(1, true);
+        typename P::vec fa[4][4], fb[4][kNf];
+        if constexpr (NPL == 1) {
+            read(0, at, fa[0], fb[0]);
+            for (int k = total; k > 0; --k) {
+                read(1, at, fa[1], fb[1]);
+                multiply(fa[0], fb[0]);
+                order(kRun, kReads, kNone);
+                meet();
+                at = (at + 1) & (kStages - 1);
+                read(0, at, fa[0], fb[0]);
+                next();
+                multiply(fa[1], fb[1]);
+                order(kRun, kReads, kFetches);
+            }
+        } else {
+            // hi hi + hi lo + lo hi; a stage's operands come while the one before is multiplied
+            constexpr std::integral_constant<int, 3 * kRun> kRun3 = {};
+            constexpr std::integral_constant<int, 2 * kReads> kReads2 = {};
+            read(0, at, fa[0], fb[0]), read(1, at, fa[1], fb[1]);
+            for (int k = total; k > 0; k -= 2)
+#pragma unroll
+                for (int u = 0; u < 4; u += 2) {
+                    meet();
+                    at = (at + 1) & (kStages - 1);
+                    read(0, at, fa[2 - u], fb[2 - u]), read(1, at, fa[3 - u], fb[3 - u]);
+                    next();
+                    multiply(fa[u], fb[u]), multiply(fa[u], fb[u + 1]), multiply(fa[u + 1], fb[u]);
+                    order(kRun3, kReads2, kFetches);
+                }
         }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     }
     const int n = lane & 31, h = lane >> 5;
     if constexpr (EPI == EPI_OUT) {
