@@ -25,45 +25,34 @@ struct Table {
     int64_t size[kTable];
     int64_t first[kTable];   // first chunk of each tensor
     uint8_t dtype[kTable];
-    uint8_t wide[kTable];    // both pointers aligned to 16 bytes
     int n;
     int64_t chunks;
 };
 
-template <class T> struct alignas(16) Vec { T v[16 / sizeof(T)]; };
-
 template <class T>
-__device__ __forceinline__ double chunk_squares(const void* base, int64_t lo, int64_t n, bool wide) {
+__device__ __forceinline__ double chunk_squares(const void* base, int64_t lo, int64_t n) {
     const T* g = (const T*)base + lo;
     constexpr int W = 16 / sizeof(T);
     double s = 0.0;
-    int64_t i = 0;
-    if (wide) {
-        for (int64_t k = threadIdx.x; k < n / W; k += blockDim.x) {
-            const Vec<T> q = ((const Vec<T>*)g)[k];
-            for (int j = 0; j < W; ++j) s += (double)(float)q.v[j] * (double)(float)q.v[j];
-        }
-        i = n / W * W;
+    for (int64_t k = threadIdx.x; k < n / W; k += blockDim.x) {
+        const Run<T, W> q = ((const Run<T, W>*)g)[k];
+        for (int j = 0; j < W; ++j) s += (double)(float)q.v[j] * (double)(float)q.v[j];
     }
-    for (i += threadIdx.x; i < n; i += blockDim.x) s += (double)(float)g[i] * (double)(float)g[i];
+    for (int64_t i = n / W * W + threadIdx.x; i < n; i += blockDim.x) s += (double)(float)g[i] * (double)(float)g[i];
     return s;
 }
 
 template <class T>
-__device__ __forceinline__ void chunk_scale(const void* base, void* out, int64_t lo, int64_t n, bool wide, float c) {
+__device__ __forceinline__ void chunk_scale(const void* base, void* out, int64_t lo, int64_t n, float c) {
     const T* g = (const T*)base + lo;
     T* o = (T*)out + lo;
     constexpr int W = 16 / sizeof(T);
-    int64_t i = 0;
-    if (wide) {
-        for (int64_t k = threadIdx.x; k < n / W; k += blockDim.x) {
-            Vec<T> q = ((const Vec<T>*)g)[k];
-            for (int j = 0; j < W; ++j) q.v[j] = (T)((float)q.v[j] * c);
-            ((Vec<T>*)o)[k] = q;
-        }
-        i = n / W * W;
+    for (int64_t k = threadIdx.x; k < n / W; k += blockDim.x) {
+        Run<T, W> q = ((const Run<T, W>*)g)[k];
+        for (int j = 0; j < W; ++j) q.v[j] = (T)((float)q.v[j] * c);
+        ((Run<T, W>*)o)[k] = q;
     }
-    for (i += threadIdx.x; i < n; i += blockDim.x) o[i] = (T)((float)g[i] * c);
+    for (int64_t i = n / W * W + threadIdx.x; i < n; i += blockDim.x) o[i] = (T)((float)g[i] * c);
 }
 
 // The tensor that a chunk belongs to.
@@ -99,7 +88,7 @@ __global__ __launch_bounds__(256) void k_squares(Table t, double* parts, int add
     for (int64_t c = blockIdx.x; c < t.chunks; c += gridDim.x) {
         const int i = find(t, c);
         const int64_t lo = (c - t.first[i]) * kChunk, n = min(kChunk, t.size[i] - lo);
-        typed(t.dtype[i], [&](auto z) { s += chunk_squares<decltype(z)>(t.in[i], lo, n, t.wide[i]); });
+        typed(t.dtype[i], [&](auto z) { s += chunk_squares<decltype(z)>(t.in[i], lo, n); });
     }
     s = block_sum(s, red);
     if (threadIdx.x == 0) parts[blockIdx.x] = add ? parts[blockIdx.x] + s : s;
@@ -135,7 +124,7 @@ __global__ __launch_bounds__(256) void k_scale(Table t, const double* parts, flo
         const int i = find(t, k);
         if (c == 1.f && t.out[i] == t.in[i]) continue;
         const int64_t lo = (k - t.first[i]) * kChunk, n = min(kChunk, t.size[i] - lo);
-        typed(t.dtype[i], [&](auto z) { chunk_scale<decltype(z)>(t.in[i], t.out[i], lo, n, t.wide[i], c); });
+        typed(t.dtype[i], [&](auto z) { chunk_scale<decltype(z)>(t.in[i], t.out[i], lo, n, c); });
     }
 }
 
@@ -143,14 +132,14 @@ __global__ __launch_bounds__(256) void k_scale(Table t, const double* parts, flo
 __global__ __launch_bounds__(1024) void k_little(Table t, int clip, float* norm, float max_norm, float eps) {
     __shared__ double red[16];
     double s = 0.0;
-    for (int i = 0; i < t.n; ++i) typed(t.dtype[i], [&](auto z) { s += chunk_squares<decltype(z)>(t.in[i], 0, t.size[i], t.wide[i]); });
+    for (int i = 0; i < t.n; ++i) typed(t.dtype[i], [&](auto z) { s += chunk_squares<decltype(z)>(t.in[i], 0, t.size[i]); });
     const float nv = (float)sqrt(block_sum(s, red));
     if (threadIdx.x == 0) *norm = nv;
     if (!clip) return;
     const float c = clip_factor(nv, max_norm, eps);
     for (int i = 0; i < t.n; ++i)
         if (c != 1.f || t.out[i] != t.in[i])
-            typed(t.dtype[i], [&](auto z) { chunk_scale<decltype(z)>(t.in[i], t.out[i], 0, t.size[i], t.wide[i], c); });
+            typed(t.dtype[i], [&](auto z) { chunk_scale<decltype(z)>(t.in[i], t.out[i], 0, t.size[i], c); });
 }
 
 int run(bool clip, int32_t n, const void* const* in, void* const* out, const int64_t* sizes, const int32_t* dtypes, float max_norm, float eps,
@@ -176,7 +165,6 @@ int run(bool clip, int32_t n, const void* const* in, void* const* out, const int
     const auto add = [&](int32_t i) {
         t.in[t.n] = in[i], t.out[t.n] = clip ? out[i] : nullptr;
         t.size[t.n] = sizes[i], t.first[t.n] = t.chunks, t.dtype[t.n] = (uint8_t)dtypes[i];
-        t.wide[t.n] = (uintptr_t)in[i] % 16 == 0 && (!clip || (uintptr_t)out[i] % 16 == 0);
         t.chunks += (sizes[i] + kChunk - 1) / kChunk;
         ++t.n;
     };

@@ -176,7 +176,6 @@ struct FewArgs {
     const void *x, *table, *target;
     int64_t ldx, ldt;
     int target_bits;
-    int wide_x, wide_e, wide_de;  // rows aligned to what a lane reads at a time
     float scale;
     const float* offset;
     float2* part;             // [block][part_row] (max, sum), base 2, or NULL

@@ -41,9 +41,9 @@ template <> struct Few<_Float16> {
 
 // 16 bytes of a row from column c on; columns past d are 0.
 template <class T>
-__device__ __forceinline__ u32x4 piece(const T* row, int c, int d, bool wide) {
+__device__ __forceinline__ u32x4 piece(const T* row, int c, int d) {
     constexpr int N = 16 / sizeof(T);
-    if (wide && c + N <= d) return *(const u32x4*)(row + c);
+    if (c + N <= d) return __builtin_bit_cast(u32x4, *(const Run<T, N>*)(row + c));
     struct alignas(16) { T v[N]; } q;
 #pragma unroll
     for (int j = 0; j < N; ++j) q.v[j] = c + j < d ? row[c + j] : (T)0.f;
@@ -55,10 +55,10 @@ __global__ __launch_bounds__(kWaves * 64) void k_few_logits(FewArgs a) {
     constexpr int N = 16 / sizeof(T);
     extern __shared__ __align__(16) char lds[];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, q = lane >> 4;
-    const int steps = (a.d + 4 * N - 1) / (4 * N), whole = a.wide_e ? a.d / (4 * N) : 0, pitch = steps * 64 + 16;
+    const int steps = (a.d + 4 * N - 1) / (4 * N), whole = a.d / (4 * N), pitch = steps * 64 + 16;
     for (int i = threadIdx.x; i < a.t * steps * 4; i += kWaves * 64) {
         const int t = i / (steps * 4), c = i - t * steps * 4;
-        *(u32x4*)(lds + t * pitch + c * 16) = piece((const T*)a.x + t * a.ldx, c * N, a.d, a.wide_x);
+        *(u32x4*)(lds + t * pitch + c * 16) = piece((const T*)a.x + t * a.ldx, c * N, a.d);
     }
     __syncthreads();
     const char* const mine = lds + min(m, a.t - 1) * pitch + q * 16;
@@ -72,11 +72,11 @@ __global__ __launch_bounds__(kWaves * 64) void k_few_logits(FewArgs a) {
         for (; s + 8 <= whole; s += 8) {  // eight reads in flight
             u32x4 e[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) e[k] = *(const u32x4*)(row + ((s + k) * 4 + q) * N);
+            for (int k = 0; k < 8; ++k) e[k] = __builtin_bit_cast(u32x4, *(const Run<T, N>*)(row + ((s + k) * 4 + q) * N));
 #pragma unroll
             for (int k = 0; k < 8; ++k) z = Few<T>::step(e[k], *(const u32x4*)(mine + (s + k) * 64), z);
         }
-        for (; s < steps; ++s) z = Few<T>::step(piece(row, (s * 4 + q) * N, a.d, a.wide_e), *(const u32x4*)(mine + s * 64), z);
+        for (; s < steps; ++s) z = Few<T>::step(piece(row, (s * 4 + q) * N, a.d), *(const u32x4*)(mine + s * 64), z);
         // lane (m, q): row m of x, table rows 4 q + i
         const int64_t v0 = g * 16 + 4 * q;
         float ref = top;
@@ -141,9 +141,8 @@ __global__ __launch_bounds__(256) void k_few_grads(FewArgs a) {
             x[t][j] = counts && a.de && c + j < a.d ? (float)((const T*)a.x)[t * a.ldx + c + j] : 0.f;
         }
     }
-    // 16 (or 8) bytes at a time where all of a row's columns allow it
-    struct alignas(C * sizeof(T)) Piece { T v[C]; };
-    const bool wide = a.wide_e && c + C <= a.d, wide_out = a.wide_de && c + C <= a.d;
+    typedef Run<T, C> Piece;
+    const bool whole = c + C <= a.d;
     for (int64_t b = r0; b < r1; b += kBatch) {
         const int n = (int)min((int64_t)kBatch, r1 - b);
         __syncthreads();
@@ -169,7 +168,7 @@ __global__ __launch_bounds__(256) void k_few_grads(FewArgs a) {
             for (int u = 0; u < U; ++u) {
                 const int64_t v = b + min(r + u * down, n - 1);
                 const T* const row = (const T*)a.table + v * a.ldt + c;
-                if (wide) {
+                if (whole) {
                     e[u] = *(const Piece*)row;
                 } else {
 #pragma unroll
@@ -198,7 +197,7 @@ __global__ __launch_bounds__(256) void k_few_grads(FewArgs a) {
                 Piece o;
 #pragma unroll
                 for (int j = 0; j < C; ++j) o.v[j] = (T)de[j];
-                if (wide_out) {
+                if (whole) {
                     *(Piece*)to = o;
                 } else {
 #pragma unroll
@@ -257,8 +256,6 @@ void grads(const FewArgs& a, hipStream_t st) {
     FewArgs b = a;
     b.across = few_across(a.d, C);
     const dim3 grid((a.d + b.across * C - 1) / (b.across * C), a.parts);
-    const auto aligned = [](const void* p, int64_t ld) { return ((uintptr_t)p | (uintptr_t)(ld * sizeof(T))) % (C * sizeof(T)) == 0; };
-    b.wide_e = aligned(a.table, a.ldt), b.wide_de = aligned(a.de, a.ldde);
     k_few_grads<T, TT, C><<<grid, 256, 0, st>>>(b);
 }
 

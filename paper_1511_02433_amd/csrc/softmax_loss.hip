@@ -44,41 +44,44 @@ __device__ __forceinline__ float abs_finite(T v) {
     return finite(a) ? a : 0.f;
 }
 
-// Largest finite |value| of a row, by 16 lanes.
+// Largest finite |value| of `n` values from `lane` of `lanes` threads, eight reads in flight.
 template <class T>
-__device__ __forceinline__ float row_max(const T* row, int d, bool wide) {
-    constexpr int N = 16 / sizeof(T);
-    struct alignas(16) Piece { T v[N]; };
-    const int l = threadIdx.x & 15;
+__device__ __forceinline__ float run_max(const T* at, int64_t n, int64_t lane, int64_t lanes) {
+    constexpr int N = 16 / sizeof(T), U = 4;
     float m = 0.f;
-    int c = 0;
-    if (wide) {
-        for (; c + 16 * N <= d; c += 16 * N) {
-            const Piece q = *(const Piece*)(row + c + N * l);
+    const int64_t whole = n / N;
+    for (int64_t i = lane; i < whole; i += lanes * U) {
+        Run<T, N> q[U];
 #pragma unroll
-            for (int j = 0; j < N; ++j) m = fmaxf(m, abs_finite(q.v[j]));
-        }
+        for (int u = 0; u < U; ++u) q[u] = *(const Run<T, N>*)(at + min(i + u * lanes, whole - 1) * N);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int j = 0; j < N; ++j) m = fmaxf(m, abs_finite(q[u].v[j]));
     }
-    for (c += l; c < d; c += 16) m = fmaxf(m, abs_finite(row[c]));
-    for (int k = 8; k > 0; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
+    for (int64_t i = whole * N + lane; i < n; i += lanes) m = fmaxf(m, abs_finite(at[i]));
     return m;
 }
 
-// The table and x (where `mats` is set), 16 lanes a row, and the rows' weights (`grads`).
+// The table and x (where `mats` is set), 16 lanes a row or 64 where it is long (the table in one run where no items are
+// excluded and rows follow one another), and the rows' weights (`grads`).
 template <class T>
 __global__ __launch_bounds__(1024) void k_scales(ccdpp_softmax_t p, const float* grad, Scales sc, int mats, int grads) {
     __shared__ float red[16][3];
     float em = 0.f, xm = 0.f, gm = 0.f;
-    const int64_t stride = (int64_t)kParts * 64;
     if (mats) {
-        const bool we = ((uintptr_t)p.table | (p.ldt * sizeof(T))) % 16 == 0, wx = ((uintptr_t)p.x | (p.ldx * sizeof(T))) % 16 == 0;
-        for (int64_t v = (int64_t)blockIdx.x * 64 + (threadIdx.x >> 4); v < p.v; v += stride) {
-            if (p.offset && p.offset[v] < kExcluded) continue;
-            em = fmaxf(em, row_max((const T*)p.table + v * p.ldt, p.d, we));
+        const int lanes = p.d > 256 ? 64 : 16, l = threadIdx.x & (lanes - 1), per = 1024 / lanes;
+        const int64_t first = (int64_t)blockIdx.x * per + threadIdx.x / lanes, stride = (int64_t)kParts * per;
+        if (!p.offset && p.ldt == p.d) {
+            em = run_max((const T*)p.table, p.v * p.d, (int64_t)blockIdx.x * 1024 + threadIdx.x, (int64_t)kParts * 1024);
+        } else {
+            for (int64_t v = first; v < p.v; v += stride)
+                if (!p.offset || !(p.offset[v] < kExcluded)) em = fmaxf(em, run_max((const T*)p.table + v * p.ldt, p.d, l, lanes));
         }
-        for (int64_t t = (int64_t)blockIdx.x * 64 + (threadIdx.x >> 4); t < p.t; t += stride) {
-            const float m = row_max((const T*)p.x + t * p.ldx, p.d, wx);
-            if ((threadIdx.x & 15) == 0) sc.x_row[t] = m;
+        for (int64_t t = first; t < p.t; t += stride) {
+            float m = run_max((const T*)p.x + t * p.ldx, p.d, l, lanes);
+            for (int k = lanes / 2; k > 0; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
+            if (l == 0) sc.x_row[t] = m;
             if (row_counts(load_target(p.target, p.target_bits, t), p.v, p.offset)) xm = fmaxf(xm, m);
         }
     }
@@ -110,7 +113,6 @@ __device__ __forceinline__ float parts_max(const float* part, float* red) {
 struct PackSide {
     const void* src;
     int64_t ld, rows, tiles;                  // tiles: blocks of 32 rows
-    int wide;                                 // rows aligned to 16 bytes
     char* nat;                                // the matrix as it is
     int64_t nat_row, nat_plane;               // bytes per block of 32 rows, per plane
     char* live;                               // the same with rows that do not count zeroed (x)
@@ -208,9 +210,8 @@ __global__ __launch_bounds__(256) void k_pack(PackArgs a) {
         if (ks >= a.ksd) break;
         const int c = c0 + 16 * s + 8 * h;
         T v[8];
-        if (in && side.wide && c + 8 <= a.d) {
-            struct alignas(16) Eight { T v[8]; };
-            const Eight q = *(const Eight*)(src + c);
+        if (in && c + 8 <= a.d) {
+            const Run<T, 8> q = *(const Run<T, 8>*)(src + c);
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = q.v[j];
         } else {
@@ -451,9 +452,9 @@ __global__ __launch_bounds__(kGemmThreads) void k_gemm(GemmArgs a) {
         // The product is the gradient turned: a lane has four neighbouring columns of a row at a time.
         // Last piece and only share: the caller's type.  Else 32 bits, added to what earlier pieces left.
         const float fg = a.fin ? ldexpf(1.f, -a.fin[2]) : 1.f, f = a.fin && a.which >= 0 ? ldexpf(a.scale, -a.fin[a.which]) : a.scale;
-        struct alignas(4 * sizeof(T)) Four { T v[4]; };
         if (a.last && !a.wide) {
-            // Rows that are not aligned: 32 rows of the wave's 128 columns at a time through LDS (quads of columns swapped
+            // Rows that are not aligned to four values (stores across them take longer: 50,021 x 777 in half
+            // precision 161 us against 142): 32 rows of the wave's 128 columns at a time through LDS (quads of columns swapped
             // about by the row, so that neither side meets a bank twice), and out 64 neighbours at a time.
             __syncthreads();
             float* const mine = (float*)(lds + wave * (32 * 128 * 4));
@@ -501,12 +502,12 @@ __global__ __launch_bounds__(kGemmThreads) void k_gemm(GemmArgs a) {
                         *o = a.add ? *o + v : v;
                         continue;
                     }
-                    Four t;
+                    Run<T, 4> t;
 #pragma unroll
                     for (int r = 0; r < 4; ++r) t.v[r] = (T)(v[r] * fg * f);
                     T* const o = (T*)a.last + row * a.ldo + col;
-                    if (a.wide && col + 4 <= a.cols) {
-                        *(Four*)o = t;
+                    if (col + 4 <= a.cols) {
+                        *(Run<T, 4>*)o = t;
                     } else {
 #pragma unroll
                         for (int r = 0; r < 4; ++r)
@@ -681,18 +682,13 @@ __global__ __launch_bounds__(256) void k_loss(ccdpp_softmax_t p, const float2* p
     if (y >= 0 && y < p.v && !(o < kExcluded)) {
         const T *x = (const T*)p.x + t * p.ldx, *e = (const T*)p.table + y * p.ldt;
         constexpr int N = 16 / sizeof(T);
-        int d = 0;
-        if (((uintptr_t)x | (uintptr_t)e) % 16 == 0) {
-            struct alignas(16) Piece { T v[N]; };
 #pragma unroll 4
-            for (d = i0 * N; d + N <= p.d; d += THREADS * N) {
-                const Piece a = *(const Piece*)(x + d), b = *(const Piece*)(e + d);
+        for (int d = i0 * N; d + N <= p.d; d += THREADS * N) {
+            const Run<T, N> a = *(const Run<T, N>*)(x + d), b = *(const Run<T, N>*)(e + d);
 #pragma unroll
-                for (int j = 0; j < N; ++j) dot = fmaf((float)a.v[j], (float)b.v[j], dot);
-            }
-            d = p.d / N * N;
+            for (int j = 0; j < N; ++j) dot = fmaf((float)a.v[j], (float)b.v[j], dot);
         }
-        for (d += i0; d < p.d; d += THREADS) dot = fmaf((float)x[d], (float)e[d], dot);
+        for (int d = p.d / N * N + i0; d < p.d; d += THREADS) dot = fmaf((float)x[d], (float)e[d], dot);
     }
     float m = -INFINITY, s = 0.f;
     bool nan = false;
@@ -769,8 +765,16 @@ __global__ __launch_bounds__(256) void k_finish(FinishSide x, FinishSide e, int6
         }
         for (; s < splits; ++s) v += *(const f32x4*)(from + s * a.split);
         T* o = (T*)a.out + r * a.ldo + c;
-        for (int j = 0; j < 4; ++j)
-            if (c + j < cols) o[j] = (T)(v[j] * fg * f);
+        Run<T, 4> t;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) t.v[j] = (T)(v[j] * fg * f);
+        if (c + 4 <= cols) {
+            *(Run<T, 4>*)o = t;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (c + j < cols) o[j] = t.v[j];
+        }
     }
 }
 
@@ -931,7 +935,6 @@ int run_few(const ccdpp_softmax_t& p, const Plan& w, const Outs& o, char* ws, hi
     FewArgs a = {};
     a.d = p.d, a.dp = (int)w.dp, a.v = p.v, a.table = p.table, a.ldt = p.ldt, a.ldx = p.ldx;
     a.target_bits = p.target_bits, a.scale = p.scale, a.offset = p.offset;
-    a.wide_x = ((uintptr_t)p.x | (p.ldx * sizeof(T))) % 16 == 0, a.wide_e = ((uintptr_t)p.table | (p.ldt * sizeof(T))) % 16 == 0;
     a.part_row = p.t, a.z_row = round_up(p.v, 16);
     for (int64_t t0 = 0; t0 < p.t; t0 += w.few_rows) {
         a.t = (int)std::min<int64_t>(w.few_rows, p.t - t0);
@@ -1067,7 +1070,6 @@ int run(const ccdpp_softmax_t& p, int call, const Outs& out, char* ws, hipStream
     PackSide &x = pk.x, &e = pk.e;
     x.src = p.x, x.ld = p.ldx, x.rows = p.t, x.tiles = w.tt;
     e.src = p.table, e.ld = p.ldt, e.rows = p.v, e.tiles = w.vt;
-    x.wide = ((uintptr_t)p.x | (p.ldx * sizeof(T))) % 16 == 0, e.wide = ((uintptr_t)p.table | (p.ldt * sizeof(T))) % 16 == 0;
     if (w.small) {
         const int64_t rows = NPL * w.ksd * kBlk, turned = rows + kBlk;
         if (w.forward) x.nat = ws + w.o_xf, x.num = x.nat + rows;
