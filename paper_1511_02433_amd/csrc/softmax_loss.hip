@@ -295,7 +295,7 @@ struct GemmArgs {
     const void* target;
     int target_bits;
     const float *lse, *grad;
-    char *g, *gt;                // G [plane][t/32][ksv], G^T [plane][v/32][kst] fragments
+    char *g, *gt;                // G [plane][t/32][ksv], G^T [plane][v/32][kst] fragments, or NULL
     int64_t g_plane, gt_plane;
     int64_t ksv, kst;
     // other products
@@ -308,6 +308,72 @@ struct GemmArgs {
 
 constexpr int kStages = 4;          // of LDS
 constexpr int kStage = 32 * kBlk;
+
+// What a row's terms G = w (2^(logit - l2) - [target]) take.
+struct TermRow {
+    float w = 0.f, l2 = 0.f, f = 0.f;
+    int64_t y = -1;      // target, from the first table entry of the piece
+    uint32_t keep = 0;   // all ones in rows that count: others are cut off as bits, whatever they hold
+    __device__ __forceinline__ void load(const GemmArgs& a, int64_t t) {
+        if (t >= a.t) return;
+        const int64_t yt = load_target(a.target, a.target_bits, t);
+        f = a.xf[t];
+        if (!row_counts(yt, a.v, a.offset)) return;
+        keep = ~0u;
+        w = a.grad ? a.grad[t] : 1.f;
+        if (a.fin) w = ldexpf(w, a.fin[2]);
+        if (yt >= a.v) w = NAN;
+        l2 = a.lse[t] * kLog2e;
+        y = yt - a.v0;
+    }
+};
+
+// Writes 32 x 32 terms as operand fragments, of G and (by a product with the identity) of G^T.
+template <class PG, int NPL>
+struct TermBlocks {
+    typename PG::vec eye[2];  // the identity in B-operand order for the two steps of 16 entries
+    __device__ __forceinline__ explicit TermBlocks(int lane) {
+        const int n = lane & 31, h = lane >> 5;
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) eye[s][k] = (typename PG::elem)(16 * s + (k < 4 ? 4 * h + k : 8 + 4 * h + k - 4) == n ? 1.f : 0.f);
+    }
+    // z: logits in base 2, lane (n, h): row n, entries 8 q + 4 h + r.
+    __device__ __forceinline__ void put(const GemmArgs& a, int64_t vt, int64_t tt, int lane, const f32x16& z, const TermRow& row) const {
+        const int h = lane >> 5;
+        float g[16];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) g[r] = row.w * exp2_fast(z[r] - row.l2);
+        const int64_t at = row.y - vt * 32;
+        if (__any(at >= 0 && at < 32)) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (at == 8 * (r >> 2) + 4 * h + (r & 3)) g[r] -= row.w;
+        }
+        typename PG::vec pl[NPL][2];
+        split_terms<PG, NPL>(g, pl);
+#pragma unroll
+        for (int k = 0; k < NPL; ++k) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                u32x4 bits = __builtin_bit_cast(u32x4, pl[k][s]);
+                bits &= row.keep;
+                pl[k][s] = __builtin_bit_cast(typename PG::vec, bits);
+                if (a.g) *(u32x4*)(a.g + k * a.g_plane + (tt * a.ksv + vt * 2 + s) * kBlk + lane * 16) = bits;
+            }
+            if (!a.gt) continue;
+            f32x16 tr = {};
+            tr = PG::mfma(pl[k][0], eye[0], tr);
+            tr = PG::mfma(pl[k][1], eye[1], tr);
+            typename PG::vec to[2];
+#pragma unroll
+            for (int r = 0; r < 16; ++r) to[r >> 3][r & 7] = (typename PG::elem)tr[r];
+#pragma unroll
+            for (int s = 0; s < 2; ++s) *(typename PG::vec*)(a.gt + k * a.gt_plane + (vt * a.kst + tt * 2 + s) * kBlk + lane * 16) = to[s];
+        }
+    }
+};
 
 // P: operands; PG: terms G.
 constexpr int kNf = 2;                  // blocks of 32 columns of a wave
@@ -569,32 +635,10 @@ __global__ __launch_bounds__(kGemmThreads) void k_gemm(GemmArgs a) {
         return;
     }
     if constexpr (EPI == EPI_G) {
-        // identity in B-operand order for the two steps of 16 entries
-        typename PG::vec eye[2];
+        const TermBlocks<PG, NPL> terms(lane);
+        TermRow row[kNf];
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-            for (int k = 0; k < 8; ++k) eye[s][k] = (typename PG::elem)(16 * s + (k < 4 ? 4 * h + k : 8 + 4 * h + k - 4) == n ? 1.f : 0.f);
-        float w[kNf], l2[kNf], f[kNf];
-        int64_t y[kNf];        // target, from the piece's first entry
-        uint32_t keep[kNf];    // all ones in rows that count: others are cut off as bits, whatever they hold
-#pragma unroll
-        for (int j = 0; j < kNf; ++j) {
-            const int64_t t = ((int64_t)bn * 8 + wn * kNf + j) * 32 + n;
-            w[j] = 0.f, l2[j] = 0.f, f[j] = 0.f, y[j] = -1, keep[j] = 0;
-            if (t < a.t) {
-                const int64_t yt = load_target(a.target, a.target_bits, t);
-                f[j] = a.xf[t];
-                if (row_counts(yt, a.v, a.offset)) {
-                    keep[j] = ~0u;
-                    w[j] = a.grad ? a.grad[t] : 1.f;
-                    if (a.fin) w[j] = ldexpf(w[j], a.fin[2]);
-                    if (yt >= a.v) w[j] = NAN;
-                    l2[j] = a.lse[t] * kLog2e;
-                    y[j] = yt - a.v0;
-                }
-            }
-        }
+        for (int j = 0; j < kNf; ++j) row[j].load(a, ((int64_t)bn * 8 + wn * kNf + j) * 32 + n);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int64_t vt = (int64_t)bm * 8 + wm * 4 + i;
@@ -605,38 +649,82 @@ __global__ __launch_bounds__(kGemmThreads) void k_gemm(GemmArgs a) {
             for (int j = 0; j < kNf; ++j) {
                 const int64_t tt = (int64_t)bn * 8 + wn * kNf + j;
                 if (tt >= a.n_tiles) continue;
-                float g[16];
+                f32x16 z;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) g[r] = w[j] * exp2_fast(fmaf(acc[i][j][r], f[j], o[r >> 2][r & 3]) - l2[j]);
-                const int64_t at = y[j] - vt * 32;
-                if (__any(at >= 0 && at < 32)) {
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (at == 8 * (r >> 2) + 4 * h + (r & 3)) g[r] -= w[j];
-                }
-                typename PG::vec pl[NPL][2];
-                split_terms<PG, NPL>(g, pl);
-#pragma unroll
-                for (int k = 0; k < NPL; ++k) {
-#pragma unroll
-                    for (int s = 0; s < 2; ++s) {
-                        u32x4 bits = __builtin_bit_cast(u32x4, pl[k][s]);
-                        bits &= keep[j];
-                        pl[k][s] = __builtin_bit_cast(typename PG::vec, bits);
-                        *(u32x4*)(a.g + k * a.g_plane + (tt * a.ksv + vt * 2 + s) * kBlk + lane * 16) = bits;
-                    }
-                    f32x16 tr = {};
-                    tr = PG::mfma(pl[k][0], eye[0], tr);
-                    tr = PG::mfma(pl[k][1], eye[1], tr);
-                    typename PG::vec to[2];
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) to[r >> 3][r & 7] = (typename PG::elem)tr[r];
-#pragma unroll
-                    for (int s = 0; s < 2; ++s) *(typename PG::vec*)(a.gt + k * a.gt_plane + (vt * a.kst + tt * 2 + s) * kBlk + lane * 16) = to[s];
-                }
+                for (int r = 0; r < 16; ++r) z[r] = fmaf(acc[i][j][r], row[j].f, o[r >> 2][r & 3]);
+                terms.put(a, vt, tt, lane, z, row[j]);
             }
         }
     }
+}
+
+// ---- logits of small products ----------------------------------------------------------------
+// Where blocks of 256 x 256 logits are fewer than CUs, their contraction is cut as well: the shares' partial logits
+// (64 MB at most in all) are joined here, and stay for the gradients' terms.
+struct JoinArgs {
+    float* z;            // [share][t][pitch]; the first one receives the logits in base 2
+    int shares;
+    int64_t share, pitch, t;
+    const float *xf, *o2;
+    float2* part;        // [blocks of 1024 entries][t], or NULL
+};
+
+__global__ __launch_bounds__(256) void k_join(JoinArgs a) {
+    __shared__ float red[4][2];
+    const int64_t t = blockIdx.y, v = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    float top = -INFINITY, sum = 0.f;
+    f32x4 z = {};
+    if (v < a.pitch) {
+        float* const at = a.z + t * a.pitch + v;
+        int s = 0;
+        for (; s + 8 <= a.shares; s += 8) {  // eight reads in flight
+            f32x4 q[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) q[k] = *(const f32x4*)(at + (s + k) * a.share);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) z += q[k];
+        }
+        for (; s < a.shares; ++s) z += *(const f32x4*)(at + s * a.share);
+        const f32x4 o = *(const f32x4*)(a.o2 + v);
+        const float f = a.xf[t];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) z[r] = fmaf(z[r], f, o[r]), top = fmaxf(top, z[r]);
+        *(f32x4*)at = z;
+    }
+    if (!a.part) return;
+    top = wave_max(top);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (lane == 0) red[wave][0] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(red[0][0], red[1][0]), fmaxf(red[2][0], red[3][0]));
+    const float ref = top == -INFINITY ? 0.f : top;
+    if (v < a.pitch)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sum += exp2_fast(z[r] - ref);
+    for (int k = 32; k > 0; k >>= 1) sum += __shfl_xor(sum, k);
+    if (lane == 0) red[wave][1] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) a.part[blockIdx.x * a.t + t] = make_float2(top, red[0][1] + red[1][1] + red[2][1] + red[3][1]);
+}
+
+// The terms of 32 x 32 logits a wave.
+template <class PG, int NPL>
+__global__ __launch_bounds__(256) void k_terms(GemmArgs a, const float* z, int64_t pitch) {
+    const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
+    const int64_t vt = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), tt = blockIdx.y;
+    if (vt >= a.m_tiles) return;
+    const TermBlocks<PG, NPL> terms(lane);
+    TermRow row;
+    row.load(a, tt * 32 + n);
+    const float* const from = z + min(tt * 32 + n, a.t - 1) * pitch + vt * 32 + 4 * h;
+    f32x16 q;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const f32x4 four = *(const f32x4*)(from + 8 * k);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) q[4 * k + r] = four[r];
+    }
+    terms.put(a, vt, tt, lane, q, row);
 }
 
 // ---- ends ------------------------------------------------------------------------------------
@@ -792,11 +880,12 @@ struct Plan {
     int64_t vc;              // table entries per piece of the gradients (a multiple of 256)
     int64_t dp;              // columns of partial sums
     int sx, se;              // splits of the two gradients' contractions
+    int sz;                  // shares of the logits' contraction; 1: logits are not kept
     Shares lse, dx, de;      // (small)
     int64_t x_tile, xlive_tile, e_tile;  // bundles (small)
     // offsets into the workspace
     int few_rows, few_blocks, few_parts;  // rows of x a launch, blocks of the logits, of the gradients along the table
-    int64_t o_z;
+    int64_t o_z;             // kept logits
     int64_t o_scale, o_xrow, o_fin, o_xf, o_ef, o_xl, o_o2, o_xn, o_xt, o_et, o_g, o_gt, o_part, o_dx, o_de, bytes;
 };
 
@@ -878,6 +967,19 @@ Plan make_plan(const ccdpp_softmax_t& p, int call) {
     };
     w.sx = splits(w.tt, w.dt, w.vc / 32);
     w.se = splits(w.vc / 32, w.dt, w.tt);
+    // With half of the CUs or more without a block of logits the contraction may be cut too.  A step of 32 takes a block
+    // half a microsecond (three times that with two planes), in the logits and again in the terms unless they are
+    // kept; the kept ones cost a launch, and are written and read at 3 TB/s.  (27 x 2,372 x 3,274 floats, loss and gradients: 396
+    // us whole, 98 in 25 shares; 1,796 x 3,893 x 687 in half precision, the loss: 32 whole, 51 in two.)
+    const int64_t tiles = (w.vt + 7) / 8 * ((w.tt + 7) / 8);
+    w.sz = 1;
+    if (tiles <= 128) {
+        const double steps = w.ksd / 2 * (w.planes == 2 ? 1.5 : 0.5), kept = 8e-6 / 3 * (double)p.t * (double)p.v;
+        double best = 1.5 * steps;  // (the same for every call, so that their results agree)
+        for (int n = 2; n <= 256 / tiles && n <= w.ksd / 4; ++n)
+            if (steps / n + 5 + n * kept < best) best = steps / n + 5 + n * kept, w.sz = n;
+    }
+    w.o_z = take(w.sz > 1 ? w.sz * p.t * w.vt * 32 * 4 : 0);
     w.o_xf = take(w.planes * w.tt * w.ksd * kBlk);
     w.o_ef = take(w.planes * w.vt * w.ksd * kBlk);
     w.o_o2 = take(w.vt * 32 * 4);
@@ -1000,16 +1102,27 @@ int run_wide(const ccdpp_softmax_t& p, const Plan& w, const Outs& out, const int
     z.m_tiles = w.vt, z.n_tiles = w.tt, z.kb = w.ksd / 2, z.splits = 1;
     z.t = p.t, z.v = p.v, z.xf = (const float*)(ws + w.o_xn), z.fin = fin, z.o2 = (const float*)(ws + w.o_o2);
     z.scale = p.scale, z.offset = p.offset, z.target = p.target, z.target_bits = p.target_bits;
-    if (w.forward) {
-        z.part = (float2*)(ws + w.o_part);
-        const int64_t blocks = (w.vt + 7) / 8 * ((w.tt + 7) / 8);
-        k_gemm<P, PG, NPL, EPI_LSE, T><<<(unsigned)blocks, kGemmThreads, 0, st>>>(z);
+    float* const kept = (float*)(ws + w.o_z);
+    const int64_t pitch = w.vt * 32, chunks = (pitch + 1023) / 1024;
+    const unsigned blocks = (unsigned)((w.vt + 7) / 8 * ((w.tt + 7) / 8));
+    if (w.sz > 1) {
+        GemmArgs q = z;
+        q.out = kept, q.out_split = p.t * pitch, q.ldo = q.cols = pitch, q.rows = p.t, q.splits = w.sz;
+        k_gemm<P, PG, NPL, EPI_OUT, T><<<dim3(blocks, w.sz), kGemmThreads, 0, st>>>(q);
         OPS_LAUNCH("logits");
-        if (int rc = launch_loss<T>(p, z.part, (w.vt + 7) / 8, Shares{}, out.loss, out.lse, RowNumbers{}, st)) return rc;
+        const JoinArgs j = {kept, w.sz, q.out_split, pitch, p.t, z.xf, z.o2, w.forward ? (float2*)(ws + w.o_part) : nullptr};
+        k_join<<<dim3((unsigned)chunks, (unsigned)p.t), 256, 0, st>>>(j);
+        OPS_LAUNCH("logits");
+    } else if (w.forward) {
+        z.part = (float2*)(ws + w.o_part);
+        k_gemm<P, PG, NPL, EPI_LSE, T><<<blocks, kGemmThreads, 0, st>>>(z);
+        OPS_LAUNCH("logits");
     }
+    if (w.forward)
+        if (int rc = launch_loss<T>(p, (const float2*)(ws + w.o_part), w.sz > 1 ? chunks : (w.vt + 7) / 8, Shares{}, out.loss, out.lse, RowNumbers{}, st)) return rc;
     if (!w.grads) return CCDPP_OK;
     z.lse = w.forward ? out.lse : out.lse_in, z.grad = out.grad;
-    z.g = ws + w.o_g, z.gt = ws + w.o_gt;
+    z.g = out.dx ? ws + w.o_g : nullptr, z.gt = out.de ? ws + w.o_gt : nullptr;
     z.kst = w.kst;
     const bool dx_whole = p.v <= w.vc && w.sx == 1;
     for (int64_t v0 = 0; v0 < p.v; v0 += w.vc) {
@@ -1017,7 +1130,8 @@ int run_wide(const ccdpp_softmax_t& p, const Plan& w, const Outs& out, const int
         GemmArgs q = z;
         q.v0 = v0, q.a = z.a + v0 / 32 * z.a_tile, q.o2 = z.o2 + v0, q.m_tiles = nt;
         q.ksv = nt * 2, q.g_plane = w.tt * q.ksv * kBlk, q.gt_plane = nt * w.kst * kBlk;
-        k_gemm<P, PG, NPL, EPI_G, T><<<(unsigned)((nt + 7) / 8 * ((w.tt + 7) / 8)), kGemmThreads, 0, st>>>(q);
+        if (w.sz > 1) k_terms<PG, NPL><<<dim3((unsigned)((nt + 3) / 4), (unsigned)w.tt), 256, 0, st>>>(q, kept + v0, pitch);
+        else k_gemm<P, PG, NPL, EPI_G, T><<<(unsigned)((nt + 7) / 8 * ((w.tt + 7) / 8)), kGemmThreads, 0, st>>>(q);
         OPS_LAUNCH("G");
         GemmArgs o = {};
         o.m_tiles = w.dt, o.cols = p.d, o.scale = p.scale, o.fin = fin;
