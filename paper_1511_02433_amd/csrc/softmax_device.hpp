@@ -166,9 +166,9 @@ constexpr int small_grads_per_cu(int planes, int ks) { return ks > 4 || planes *
 template <class P, int NPL> hipError_t launch_small_lse(int ksd, const SmallArgs& a, hipStream_t st);
 template <class P, int NPL> hipError_t launch_small_grads(int ksd, const SmallArgs& a, hipStream_t st);
 
-// ---- few rows (t <= kFewT) -------------------------------------------------------------------
-constexpr int kFewT = 16;
-constexpr int kFewLds = 150 * 1024;  // of x's rows in LDS
+// ---- few rows --------------------------------------------------------------------------------
+constexpr int kDirectT = 128;  // rows whose logits are computed from the table as it lies
+constexpr int kFewT = 16;      // rows whose gradients are, too
 
 struct FewArgs {
     int t, d, dp;             // dp: columns of partial sums, a multiple of 4
@@ -178,20 +178,29 @@ struct FewArgs {
     int target_bits;
     float scale;
     const float* offset;
-    float2* part;             // [block][part_row] (max, sum), base 2, or NULL
-    int64_t part_row;
+    int share, chunk;         // see FewShape
+    float2* part;             // [block][t] (max, sum), base 2, or NULL
     float* z;                 // logits in base 2 [t][z_row], or NULL
-    int64_t z_row;
+    int64_t z_row;            // a multiple of 32
     const float *lse, *grad;
     void* de;                 // or NULL
     int64_t ldde;
     float* dxp;               // [part][t][dp], or NULL
     int parts;                // blocks along the table
-    int across;               // threads along a row (a power of two)
+    int across;               // waves along a row
 };
 
+struct FewShape {
+    int share;    // waves that share the columns of 16 table rows
+    int rows;     // groups of 16 table rows of a wave
+    int chunk;    // steps of 64 bytes of x's rows in LDS at a time
+    int blocks;
+    int64_t lds;
+};
+
+FewShape few_shape(int64_t t, int64_t v, int d, int bytes);
 int few_across(int d, int columns);
-template <class T> hipError_t launch_few_logits(const FewArgs& a, int blocks, hipStream_t st);
+template <class T> hipError_t launch_few_logits(const FewArgs& a, const FewShape& s, hipStream_t st);
 template <class T> hipError_t launch_few_grads(const FewArgs& a, T* dx, int64_t lddx, hipStream_t st);
 
 }  // namespace ccdops

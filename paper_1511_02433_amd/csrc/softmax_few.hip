@@ -1,15 +1,17 @@
-// Softmax loss and gradients of few rows (t <= 16): a request, a handful of tokens (gfx950).
+// Softmax loss of few rows (t <= 128) and gradients of very few (t <= 16): a request, a handful of tokens, a small
+// evaluation (gfx950).
 //
 // Bound by reading the table, once for the logits and, for gradients, once more, and by writing its gradient: nothing is
-// packed or turned.  The logits of so few rows are smaller than the table, so gradients keep them in the workspace.
+// packed or turned.  The logits of so few rows are kept for the gradients.
 //
-// k_few_logits: a wave takes 16 table rows against 16 rows of x (those that exist, from LDS).  Each lane reads 16 bytes of
-// its table row at a time, 64 bytes a row and step, straight into the operand of a 16 x 16 product: of 16-bit values
-// 32 columns a step, of 32-bit ones 16 columns in four v_mfma_f32_16x16x4_f32, with exact products.  Any order of the
-// columns will do as long as x has the same.
+// k_direct_logits: a wave takes 16 table rows (or twice that) against all rows of x.  Each lane reads 16 bytes of its table
+// row at a time, 64 bytes a row and step, straight into the operand of 16 x 16 products: of 16-bit values 32 columns a
+// step, of 32-bit ones 16 columns in four v_mfma_f32_16x16x4_f32, with exact products.  Any order of the columns will do
+// as long as x, which comes from LDS, has the same.  Where table rows are few, waves share their columns.
 //
-// k_few_grads: a thread owns a few columns; it reads them row by row of the table, adds to its columns of dx and writes
-// those of dtable, 2 t operations for each value read and written.
+// k_few_grads: 16 table rows and 16 rows of x at a time in v_mfma_f32_16x16x4_f32, whatever the type: the table's values
+// are the operand of dx as they are read, x's are kept in registers for dtable, and the terms G stay in 32 bits.  A row's
+// values go to and from 16 lanes by 16 bytes.
 #include <algorithm>
 
 #include "softmax_device.hpp"
@@ -50,106 +52,185 @@ __device__ __forceinline__ u32x4 piece(const T* row, int c, int d) {
     return __builtin_bit_cast(u32x4, q);
 }
 
-template <class T>
-__global__ __launch_bounds__(kWaves * 64) void k_few_logits(FewArgs a) {
-    constexpr int N = 16 / sizeof(T);
+// TG: 16 rows of x each; R: 16 table rows each that a wave takes at a time.
+template <class T, int TG, int R>
+__global__ __launch_bounds__(kWaves * 64) void k_direct_logits(FewArgs a) {
+    constexpr int N = 16 / sizeof(T), U = R * TG > 8 ? 2 : 4;
     extern __shared__ __align__(16) char lds[];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, q = lane >> 4;
-    const int steps = (a.d + 4 * N - 1) / (4 * N), whole = a.d / (4 * N), pitch = steps * 64 + 16;
-    for (int i = threadIdx.x; i < a.t * steps * 4; i += kWaves * 64) {
-        const int t = i / (steps * 4), c = i - t * steps * 4;
-        *(u32x4*)(lds + t * pitch + c * 16) = piece((const T*)a.x + t * a.ldx, c * N, a.d);
-    }
-    __syncthreads();
-    const char* const mine = lds + min(m, a.t - 1) * pitch + q * 16;
+    const int steps = (a.d + 4 * N - 1) / (4 * N), pitch = a.chunk * 64 + 16;
+    const int part = wave & (a.share - 1), mine = wave / a.share, per = kWaves / a.share;  // `share` waves share their columns
+    const char* x[TG];
+#pragma unroll
+    for (int g = 0; g < TG; ++g) x[g] = lds + min(g * 16 + m, a.t - 1) * pitch + q * 16;
     const float f = a.scale * kLog2e;
-    float top = -INFINITY, sum = 0.f;
-    const int64_t groups = (a.v + 15) / 16;
-    for (int64_t g = (int64_t)blockIdx.x * kWaves + wave; g < groups; g += (int64_t)gridDim.x * kWaves) {
-        const T* const row = (const T*)a.table + min(g * 16 + m, a.v - 1) * a.ldt;
-        f32x4 z = {};
-        int s = 0;
-        for (; s + 8 <= whole; s += 8) {  // eight reads in flight
-            u32x4 e[8];
+    float top[TG], sum[TG];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) e[k] = __builtin_bit_cast(u32x4, *(const Run<T, N>*)(row + ((s + k) * 4 + q) * N));
+    for (int g = 0; g < TG; ++g) top[g] = -INFINITY, sum[g] = 0.f;
+    const int64_t groups = (a.v + 31) / 32 * 2, blocks = (groups + per * R - 1) / (per * R);
+    bool staged = false;
+    for (int64_t b = blockIdx.x; b < blocks; b += gridDim.x) {
+        const int64_t g0 = (b * per + mine) * R;
+        const T* row[R];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) z = Few<T>::step(e[k], *(const u32x4*)(mine + (s + k) * 64), z);
+        for (int r = 0; r < R; ++r) row[r] = (const T*)a.table + min((g0 + r) * 16 + m, a.v - 1) * a.ldt;
+        f32x4 z[R][TG] = {};
+        for (int c0 = 0; c0 < steps; c0 += a.chunk) {
+            const int n = min(a.chunk, steps - c0);
+            if (!staged || a.chunk < steps) {
+                __syncthreads();
+                const int all = a.t * n * 4;
+                for (int i = threadIdx.x; i < all; i += kWaves * 64 * 4) {  // four reads in flight
+                    u32x4 p[4];
+                    int to[4];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        const int k = min(i + u * kWaves * 64, all - 1), t = k / (n * 4), c = k - t * n * 4;
+                        to[u] = t * pitch + c * 16;
+                        p[u] = piece((const T*)a.x + t * a.ldx, (c0 * 4 + c) * N, a.d);
+                    }
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) *(u32x4*)(lds + to[u]) = p[u];
+                }
+                __syncthreads();
+                staged = true;
+            }
+            const int first = n * part / a.share, last = n * (part + 1) / a.share;
+            const int whole = min(last, a.d / (4 * N) - c0);
+            int s = first;
+            for (; s + U <= whole; s += U) {
+                u32x4 e[U][R];
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int r = 0; r < R; ++r) e[u][r] = __builtin_bit_cast(u32x4, *(const Run<T, N>*)(row[r] + ((c0 + s + u) * 4 + q) * N));
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int g = 0; g < TG; ++g) {
+                        const u32x4 k = *(const u32x4*)(x[g] + (s + u) * 64);
+#pragma unroll
+                        for (int r = 0; r < R; ++r) z[r][g] = Few<T>::step(e[u][r], k, z[r][g]);
+                    }
+            }
+            for (; s < last; ++s)
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const u32x4 e = piece(row[r], ((c0 + s) * 4 + q) * N, a.d);
+#pragma unroll
+                    for (int g = 0; g < TG; ++g) z[r][g] = Few<T>::step(e, *(const u32x4*)(x[g] + s * 64), z[r][g]);
+                }
         }
-        for (; s < steps; ++s) z = Few<T>::step(piece(row, (s * 4 + q) * N, a.d), *(const u32x4*)(mine + s * 64), z);
+        if (a.share > 1) {  // the sharing waves' sums, in order, behind the rows of x
+            f32x4* const shared = (f32x4*)(lds + a.t * pitch);
+            __syncthreads();
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int g = 0; g < TG; ++g) shared[(wave * R * TG + r * TG + g) * 64 + lane] = z[r][g];
+            __syncthreads();
+            if (part == 0)
+                for (int w = 1; w < a.share; ++w)
+#pragma unroll
+                    for (int r = 0; r < R; ++r)
+#pragma unroll
+                        for (int g = 0; g < TG; ++g) z[r][g] += shared[((wave + w) * R * TG + r * TG + g) * 64 + lane];
+        }
+        if (part != 0) continue;
         // lane (m, q): row m of x, table rows 4 q + i
-        const int64_t v0 = g * 16 + 4 * q;
-        float ref = top;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float o = v0 + i >= a.v ? -INFINITY : a.offset ? a.offset[v0 + i] : 0.f;
-            z[i] = o < kExcluded ? -INFINITY : fmaf(z[i], f, o * kLog2e);
-            ref = fmaxf(ref, z[i]);
+        for (int r = 0; r < R; ++r) {
+            const int64_t v0 = (g0 + r) * 16 + 4 * q;
+            if (g0 + r >= groups) continue;
+            float o[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                o[i] = v0 + i >= a.v ? -INFINITY : a.offset ? a.offset[v0 + i] : 0.f;
+                if (o[i] < kExcluded) o[i] = -INFINITY;
+            }
+#pragma unroll
+            for (int g = 0; g < TG; ++g) {
+                float ref = top[g];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    z[r][g][i] = o[i] == -INFINITY ? -INFINITY : fmaf(z[r][g][i], f, o[i] * kLog2e);
+                    ref = fmaxf(ref, z[r][g][i]);
+                }
+                if (a.z && g * 16 + m < a.t) *(f32x4*)(a.z + (g * 16 + m) * a.z_row + v0) = z[r][g];
+                const float base = ref == -INFINITY ? 0.f : ref;
+                sum[g] *= exp2_fast(top[g] - base);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum[g] += exp2_fast(z[r][g][i] - base);
+                top[g] = ref;
+            }
         }
-        if (a.z && m < a.t) *(f32x4*)(a.z + m * a.z_row + v0) = z;
-        const float r = ref == -INFINITY ? 0.f : ref;
-        sum *= exp2_fast(top - r);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sum += exp2_fast(z[i] - r);
-        top = ref;
     }
     if (!a.part) return;
-#pragma unroll
-    for (int k = 16; k < 64; k <<= 1) {
-        const float top2 = __shfl_xor(top, k), sum2 = __shfl_xor(sum, k);
-        const float ref = fmaxf(top, top2), r = ref == -INFINITY ? 0.f : ref;
-        sum = sum * exp2_fast(top - r) + sum2 * exp2_fast(top2 - r);
-        top = ref;
-    }
     __syncthreads();
     float2* const share = (float2*)lds;
-    if (q == 0) share[wave * 16 + m] = make_float2(top, sum);
-    __syncthreads();
-    if (threadIdx.x < a.t) {
-        for (int w = 0; w < kWaves; ++w) {
-            const float2 p = share[w * 16 + threadIdx.x];
-            if (w == 0) {
-                top = p.x, sum = p.y;
-                continue;
-            }
-            const float ref = fmaxf(top, p.x), r = ref == -INFINITY ? 0.f : ref;
-            sum = sum * exp2_fast(top - r) + p.y * exp2_fast(p.x - r);
-            top = ref;
+#pragma unroll
+    for (int g = 0; g < TG; ++g) {
+#pragma unroll
+        for (int k = 16; k < 64; k <<= 1) {
+            const float top2 = __shfl_xor(top[g], k), sum2 = __shfl_xor(sum[g], k);
+            const float ref = fmaxf(top[g], top2), r = ref == -INFINITY ? 0.f : ref;
+            sum[g] = sum[g] * exp2_fast(top[g] - r) + sum2 * exp2_fast(top2 - r);
+            top[g] = ref;
         }
-        a.part[blockIdx.x * a.part_row + threadIdx.x] = make_float2(top, sum);
+        if (q == 0) share[wave * TG * 16 + g * 16 + m] = make_float2(top[g], sum[g]);
+    }
+    __syncthreads();
+    for (int t = threadIdx.x; t < a.t; t += kWaves * 64) {
+        float2 p = share[t];
+        for (int w = 1; w < kWaves; ++w) {
+            const float2 o = share[w * TG * 16 + t];
+            const float ref = fmaxf(p.x, o.x), r = ref == -INFINITY ? 0.f : ref;
+            p = make_float2(ref, p.y * exp2_fast(p.x - r) + o.y * exp2_fast(o.x - r));
+        }
+        a.part[blockIdx.x * (int64_t)a.t + t] = p;
     }
 }
 
-// TT: rows that registers are kept for; C: columns of a thread.
 constexpr int kBatch = 128;  // table rows whose terms are in LDS at a time
 
-template <class T, int TT, int C>
-__global__ __launch_bounds__(256) void k_few_grads(FewArgs a) {
-    __shared__ float terms[kBatch][TT];
-    __shared__ float keep[kBatch];
-    __shared__ __align__(16) float red[256 * C];
-    const int across = a.across, tx = threadIdx.x & (across - 1), ty = threadIdx.x / across, down = 256 / across;
-    const int c = (blockIdx.x * across + tx) * C;
-    const int64_t r0 = a.v * blockIdx.y / gridDim.y, r1 = a.v * (blockIdx.y + 1) / gridDim.y;
-    float x[TT][C], dx[TT][C];
-#pragma unroll
-    for (int t = 0; t < TT; ++t) {
-        const bool counts = t < a.t && row_counts(load_target(a.target, a.target_bits, t), a.v, a.offset);
-#pragma unroll
-        for (int j = 0; j < C; ++j) {
-            dx[t][j] = 0.f;
-            x[t][j] = counts && a.de && c + j < a.d ? (float)((const T*)a.x)[t * a.ldx + c + j] : 0.f;
-        }
-    }
+template <class T>
+__global__ __launch_bounds__(256, 2) void k_few_grads(FewArgs a) {
+    constexpr int C = 16 / sizeof(T);  // columns of a lane: 16 C of them are beside each other
     typedef Run<T, C> Piece;
+    __shared__ float terms[kBatch][17];
+    __shared__ float keep[kBatch];
+    __shared__ __align__(16) float red[4][16 * 16 * C];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, q = lane >> 4;
+    const int across = a.across, wx = wave & (across - 1), wy = wave / across, down = 4 / across;
+    const int c = (blockIdx.x * across + wx) * 16 * C + n * C;
     const bool whole = c + C <= a.d;
+    const int64_t r0 = a.v * blockIdx.y / gridDim.y, r1 = a.v * (blockIdx.y + 1) / gridDim.y;
+    // x as the operand of dtable: rows 4 j + q, zero where they do not count
+    float x[4][C];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int t = 4 * j + q;
+        const bool counts = a.de && t < a.t && row_counts(load_target(a.target, a.target_bits, t), a.v, a.offset);
+#pragma unroll
+        for (int i = 0; i < C; ++i) x[j][i] = counts && c + i < a.d ? (float)((const T*)a.x)[t * a.ldx + c + i] : 0.f;
+    }
+    f32x4 dx[C] = {};
+    const auto read = [&](int64_t row, Piece& e) {
+        const T* const at = (const T*)a.table + row * a.ldt + c;
+        if (whole) {
+            e = *(const Piece*)at;
+        } else {
+#pragma unroll
+            for (int i = 0; i < C; ++i) e.v[i] = c + i < a.d ? at[i] : (T)0.f;
+        }
+    };
     for (int64_t b = r0; b < r1; b += kBatch) {
-        const int n = (int)min((int64_t)kBatch, r1 - b);
+        const int rows = (int)min((int64_t)kBatch, r1 - b);
         __syncthreads();
-        for (int i = threadIdx.x; i < TT * kBatch; i += 256) {
+        for (int i = threadIdx.x; i < 16 * kBatch; i += 256) {
             const int t = i / kBatch, r = i % kBatch;
             float g = 0.f;
-            if (t < a.t && r < n) {
+            if (t < a.t && r < rows) {
                 const int64_t y = load_target(a.target, a.target_bits, t);
                 if (row_counts(y, a.v, a.offset)) {
                     const float w = y < a.v ? (a.grad ? a.grad[t] : 1.f) * a.scale : NAN;
@@ -158,76 +239,65 @@ __global__ __launch_bounds__(256) void k_few_grads(FewArgs a) {
                 }
             }
             terms[r][t] = g;
-            if (t == 0) keep[r] = r < n && a.offset && a.offset[b + r] < kExcluded ? 0.f : 1.f;
+            if (t == 0) keep[r] = r < rows && !(a.offset && a.offset[b + r] < kExcluded) ? 1.f : 0.f;
         }
         __syncthreads();
-        constexpr int U = 4;  // rows in flight
-        for (int r = ty; r < n; r += down * U) {
-            Piece e[U];
+        const int tiles = (rows + 15) / 16;
+        Piece next[4];
+        if (wy < tiles)
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int64_t v = b + min(r + u * down, n - 1);
-                const T* const row = (const T*)a.table + v * a.ldt + c;
-                if (whole) {
-                    e[u] = *(const Piece*)row;
-                } else {
+            for (int j = 0; j < 4; ++j) read(b + min(wy * 16 + 4 * j + q, rows - 1), next[j]);
+        for (int i = wy; i < tiles; i += down) {
+            Piece e[4];
 #pragma unroll
-                    for (int j = 0; j < C; ++j) e[u].v[j] = c + j < a.d ? row[j] : (T)0.f;
+            for (int j = 0; j < 4; ++j) e[j] = next[j];
+            if (i + down < tiles)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) read(b + min((i + down) * 16 + 4 * j + q, rows - 1), next[j]);
+            f32x4 de[C] = {};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int row = i * 16 + 4 * j + q;
+                const bool k = keep[row] != 0.f;
+                const float gx = terms[row][n], ge = terms[i * 16 + n][4 * j + q];
+#pragma unroll
+                for (int l = 0; l < C; ++l) {
+                    dx[l] = __builtin_amdgcn_mfma_f32_16x16x4f32(gx, k ? (float)e[j].v[l] : 0.f, dx[l], 0, 0, 0);
+                    de[l] = __builtin_amdgcn_mfma_f32_16x16x4f32(ge, x[j][l], de[l], 0, 0, 0);
                 }
             }
+            if (!a.de) continue;
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int at = r + u * down;
-                if (at >= n) break;
-                const bool k = keep[at] != 0.f;
-                float de[C];
-#pragma unroll
-                for (int j = 0; j < C; ++j) de[j] = 0.f;
-#pragma unroll
-                for (int t = 0; t < TT; ++t) {
-                    const float g = terms[at][t];
-#pragma unroll
-                    for (int j = 0; j < C; ++j) {
-                        dx[t][j] = fmaf(g, k ? (float)e[u].v[j] : 0.f, dx[t][j]);
-                        de[j] = fmaf(g, x[t][j], de[j]);
-                    }
-                }
-                if (!a.de) continue;
-                T* const to = (T*)a.de + (b + at) * a.ldde + c;
+            for (int r = 0; r < 4; ++r) {
+                const int row = i * 16 + 4 * q + r;
+                if (row >= rows) continue;
+                T* const to = (T*)a.de + (b + row) * a.ldde + c;
                 Piece o;
 #pragma unroll
-                for (int j = 0; j < C; ++j) o.v[j] = (T)de[j];
+                for (int l = 0; l < C; ++l) o.v[l] = (T)de[l][r];
                 if (whole) {
                     *(Piece*)to = o;
                 } else {
 #pragma unroll
-                    for (int j = 0; j < C; ++j)
-                        if (c + j < a.d) to[j] = o.v[j];
+                    for (int l = 0; l < C; ++l)
+                        if (c + l < a.d) to[l] = o.v[l];
                 }
             }
         }
     }
     if (!a.dxp) return;
-    // Rows that went down different threads are added in order; a block leaves one partial sum.
-    for (int t = 0; t < TT; ++t) {
-        if (t >= a.t) break;
-        __syncthreads();
+    // Waves that took different rows are added in order; a block leaves one partial sum.
 #pragma unroll
-        for (int j = 0; j < C; ++j) {
-            float v = 0.f;
+    for (int l = 0; l < C; ++l)
 #pragma unroll
-            for (int k = 0; k < TT; ++k)
-                if (k == t) v = dx[k][j];
-            red[(ty * across + tx) * C + j] = v;
-        }
-        __syncthreads();
-        for (int i = threadIdx.x; i < across * C; i += 256) {
-            const int col = blockIdx.x * across * C + i;
-            if (col >= a.dp) continue;
-            float s = 0.f;
-            for (int k = 0; k < down; ++k) s += red[k * across * C + i];
-            a.dxp[((int64_t)blockIdx.y * a.t + t) * a.dp + col] = s;
-        }
+        for (int r = 0; r < 4; ++r) red[wave][(4 * q + r) * 16 * C + n * C + l] = dx[l][r];
+    __syncthreads();
+    for (int i = threadIdx.x; i < a.t * across * 16 * C; i += 256) {
+        const int t = i / (across * 16 * C), k = i - t * across * 16 * C, w = k / (16 * C), col = blockIdx.x * across * 16 * C + k;
+        if (col >= a.dp) continue;
+        float s = 0.f;
+        for (int y = 0; y < down; ++y) s += red[y * across + w][t * 16 * C + (k - w * 16 * C)];
+        a.dxp[((int64_t)blockIdx.y * a.t + t) * a.dp + col] = s;
     }
 }
 
@@ -249,53 +319,67 @@ __global__ __launch_bounds__(256) void k_few_finish(FewArgs a, int parts, T* dx,
         if (quad * 4 + j < a.d) dx[t * lddx + quad * 4 + j] = (T)s[j];
 }
 
-template <class T, int TT>
-void grads(const FewArgs& a, hipStream_t st) {
-    // 16 bytes a thread, four columns where registers are short
-    constexpr int C = TT > 8 ? 4 : 16 / sizeof(T);
-    FewArgs b = a;
-    b.across = few_across(a.d, C);
-    const dim3 grid((a.d + b.across * C - 1) / (b.across * C), a.parts);
-    k_few_grads<T, TT, C><<<grid, 256, 0, st>>>(b);
+template <class T, int TG, int R>
+hipError_t logits(const FewArgs& a, int blocks, size_t lds, hipStream_t st) {
+    if (lds > 64 * 1024) {
+        const hipError_t e = hipFuncSetAttribute((const void*)k_direct_logits<T, TG, R>, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+        if (e != hipSuccess) return e;
+    }
+    k_direct_logits<T, TG, R><<<blocks, kWaves * 64, lds, st>>>(a);
+    return hipGetLastError();
 }
 
 }  // namespace
 
-int few_across(int d, int columns) {
-    int n = 8;
-    while (n < 256 && n * columns < d) n *= 2;
-    return n;
+FewShape few_shape(int64_t t, int64_t v, int d, int bytes) {
+    FewShape s;
+    const int64_t groups = (v + 31) / 32 * 2, steps = ((int64_t)d * bytes + 63) / 64;
+    // Waves for all CUs, eight each: where groups of 16 table rows are fewer, up to eight waves share one, four steps each,
+    // as long as a block still has as many table rows as rows of x, which it brings to LDS.
+    s.share = 1;
+    while (s.share < kWaves && groups * s.share < 2048 && steps >= 8 * s.share && kWaves / (2 * s.share) * 16 >= t) s.share *= 2;
+    s.rows = t > 16 && s.share == 1 && groups >= 8192 ? 2 : 1;
+    // x in LDS, all of it or by columns, so that two blocks fit a CU
+    const int64_t room = 78 * 1024 - (s.share > 1 ? kWaves * ((t + 15) / 16) * 1024 : 0);
+    s.chunk = (int)std::max<int64_t>(1, std::min<int64_t>(steps, (room / t - 16) / 64));
+    const int64_t per = (int64_t)(kWaves / s.share) * s.rows;
+    s.blocks = (int)std::min<int64_t>(512, (groups + per - 1) / per);
+    const int tg = t <= 16 ? 1 : t <= 32 ? 2 : t <= 64 ? 4 : 8;
+    s.lds = std::max<int64_t>(t * (s.chunk * 64 + 16) + (s.share > 1 ? kWaves * s.rows * tg * 1024 : 0), kWaves * tg * 16 * 8);
+    return s;
 }
 
 template <class T>
-hipError_t launch_few_logits(const FewArgs& a, int blocks, hipStream_t st) {
-    constexpr int N = 16 / sizeof(T);
-    const int steps = (a.d + 4 * N - 1) / (4 * N);
-    const size_t lds = std::max<size_t>((size_t)a.t * (steps * 64 + 16), kWaves * 16 * sizeof(float2));
-    if (lds > 64 * 1024) {
-        const hipError_t e = hipFuncSetAttribute((const void*)k_few_logits<T>, hipFuncAttributeMaxDynamicSharedMemorySize, kFewLds);
-        if (e != hipSuccess) return e;
-    }
-    k_few_logits<T><<<blocks, kWaves * 64, lds, st>>>(a);
-    return hipGetLastError();
+hipError_t launch_few_logits(const FewArgs& a, const FewShape& s, hipStream_t st) {
+    FewArgs b = a;
+    b.share = s.share, b.chunk = s.chunk;
+    if (a.t <= 16) return logits<T, 1, 1>(b, s.blocks, s.lds, st);
+    if (a.t <= 32) return s.rows == 2 ? logits<T, 2, 2>(b, s.blocks, s.lds, st) : logits<T, 2, 1>(b, s.blocks, s.lds, st);
+    if (a.t <= 64) return s.rows == 2 ? logits<T, 4, 2>(b, s.blocks, s.lds, st) : logits<T, 4, 1>(b, s.blocks, s.lds, st);
+    return s.rows == 2 ? logits<T, 8, 2>(b, s.blocks, s.lds, st) : logits<T, 8, 1>(b, s.blocks, s.lds, st);
 }
 
 template <class T>
 hipError_t launch_few_grads(const FewArgs& a, T* dx, int64_t lddx, hipStream_t st) {
-    if (a.t <= 1) grads<T, 1>(a, st);
-    else if (a.t <= 2) grads<T, 2>(a, st);
-    else if (a.t <= 4) grads<T, 4>(a, st);
-    else if (a.t <= 8) grads<T, 8>(a, st);
-    else grads<T, 16>(a, st);
-    hipError_t e = hipGetLastError();
+    constexpr int C = 16 / sizeof(T);
+    FewArgs b = a;
+    b.across = few_across(a.d, C);
+    k_few_grads<T><<<dim3((a.d + b.across * 16 * C - 1) / (b.across * 16 * C), a.parts), 256, 0, st>>>(b);
+    const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !dx) return e;
     k_few_finish<T><<<a.t * ((a.dp / 4 + 15) / 16), 256, 0, st>>>(a, a.parts, dx, lddx);
     return hipGetLastError();
 }
 
-template hipError_t launch_few_logits<float>(const FewArgs&, int, hipStream_t);
-template hipError_t launch_few_logits<__bf16>(const FewArgs&, int, hipStream_t);
-template hipError_t launch_few_logits<_Float16>(const FewArgs&, int, hipStream_t);
+int few_across(int d, int columns) {
+    int n = 1;
+    while (n < 4 && n * 16 * columns < d) n *= 2;
+    return n;
+}
+
+template hipError_t launch_few_logits<float>(const FewArgs&, const FewShape&, hipStream_t);
+template hipError_t launch_few_logits<__bf16>(const FewArgs&, const FewShape&, hipStream_t);
+template hipError_t launch_few_logits<_Float16>(const FewArgs&, const FewShape&, hipStream_t);
 template hipError_t launch_few_grads<float>(const FewArgs&, float*, int64_t, hipStream_t);
 template hipError_t launch_few_grads<__bf16>(const FewArgs&, __bf16*, int64_t, hipStream_t);
 template hipError_t launch_few_grads<_Float16>(const FewArgs&, _Float16*, int64_t, hipStream_t);

@@ -884,7 +884,9 @@ struct Plan {
     Shares lse, dx, de;      // (small)
     int64_t x_tile, xlive_tile, e_tile;  // bundles (small)
     // offsets into the workspace
-    int few_rows, few_blocks, few_parts;  // rows of x a launch, blocks of the logits, of the gradients along the table
+    bool direct = false;     // t <= kDirectT: the logits by k_direct_logits
+    FewShape shape = {};
+    int few_parts = 0;       // blocks of the gradients along the table
     int64_t o_z;             // kept logits
     int64_t o_scale, o_xrow, o_fin, o_xf, o_ef, o_xl, o_o2, o_xn, o_xt, o_et, o_g, o_gt, o_part, o_dx, o_de, bytes;
 };
@@ -907,22 +909,18 @@ Plan make_plan(const ccdpp_softmax_t& p, int call) {
         at += round_up(std::max<int64_t>(n, 0), 256);
         return o;
     };
+    const int es = w.planes == 2 ? 4 : 2;
     w.few = p.t <= kFewT;
-    if (w.few) {
-        const int es = w.planes == 2 ? 4 : 2;
-        const int64_t row = (int64_t)(p.d * es + 63) / 64 * 64 + 16;
-        w.few_rows = (int)std::max<int64_t>(1, std::min<int64_t>(p.t, kFewLds / row));
-        if (row > kFewLds) w.few = false;  // not even one row: the general way
-        // two blocks of eight waves a CU (one where x takes more than half of LDS), a group of 16 table rows each at least
-        w.few_blocks = (int)std::max<int64_t>(1, std::min<int64_t>(w.few_rows * row > 75 * 1024 ? 256 : 512, (p.v + 127) / 128));
-        const int columns = p.t > 8 ? 4 : 16 / es;
-        const int64_t wide = (int64_t)few_across(p.d, columns) * columns, beside = (p.d + wide - 1) / wide;
-        w.few_parts = (int)std::max<int64_t>(1, std::min<int64_t>(1024 / beside, (p.v + 63) / 64));
+    w.direct = w.few || (p.t <= kDirectT && !w.small);
+    if (w.direct) {
+        w.shape = few_shape(std::max<int64_t>(p.t, 1), p.v, p.d, es);
+        w.o_part = take(w.forward ? w.shape.blocks * p.t * 8 : 0);
+        w.o_z = take(w.grads ? p.t * w.vt * 32 * 4 : 0);
     }
     if (w.few) {
+        const int64_t wide = (int64_t)few_across(p.d, 16 / es) * 16 * (16 / es), beside = (p.d + wide - 1) / wide;
+        w.few_parts = (int)std::max<int64_t>(1, std::min<int64_t>(1024 / beside, (p.v + 63) / 64));
         w.dp = round_up(p.d, 4);
-        w.o_part = take(w.forward ? w.few_blocks * p.t * 8 : 0);
-        w.o_z = take(w.grads ? p.t * round_up(p.v, 16) * 4 : 0);
         w.o_dx = take(w.grads ? w.few_parts * p.t * w.dp * 4 : 0);
         w.bytes = at;
         return w;
@@ -973,18 +971,20 @@ Plan make_plan(const ccdpp_softmax_t& p, int call) {
     // us whole, 98 in 25 shares; 1,796 x 3,893 x 687 in half precision, the loss: 32 whole, 51 in two.)
     const int64_t tiles = (w.vt + 7) / 8 * ((w.tt + 7) / 8);
     w.sz = 1;
-    if (tiles <= 128) {
+    if (tiles <= 128 && !w.direct) {
         const double steps = w.ksd / 2 * (w.planes == 2 ? 1.5 : 0.5), kept = 8e-6 / 3 * (double)p.t * (double)p.v;
         double best = 1.5 * steps;  // (the same for every call, so that their results agree)
         for (int n = 2; n <= 256 / tiles && n <= w.ksd / 4; ++n)
             if (steps / n + 5 + n * kept < best) best = steps / n + 5 + n * kept, w.sz = n;
     }
-    w.o_z = take(w.sz > 1 ? w.sz * p.t * w.vt * 32 * 4 : 0);
-    w.o_xf = take(w.planes * w.tt * w.ksd * kBlk);
-    w.o_ef = take(w.planes * w.vt * w.ksd * kBlk);
+    if (!w.direct) {
+        w.o_z = take(w.sz > 1 ? w.sz * p.t * w.vt * 32 * 4 : 0);
+        w.o_xf = take(w.planes * w.tt * w.ksd * kBlk);
+        w.o_ef = take(w.planes * w.vt * w.ksd * kBlk);
+    }
     w.o_o2 = take(w.vt * 32 * 4);
     w.o_xn = take(w.tt * 32 * 4);
-    w.o_part = take(w.forward ? (w.vt + 7) / 8 * p.t * 8 : 0);
+    if (!w.direct) w.o_part = take(w.forward ? (w.vt + 7) / 8 * p.t * 8 : 0);
     if (w.grads) {
         w.o_xt = take(w.planes * w.dt * w.kst * kBlk);
         w.o_et = take(w.planes * w.dt * w.ksv * kBlk);
@@ -1032,27 +1032,22 @@ struct Outs {
     int64_t ldde;
 };
 
+// The logits of few rows, their loss, and what gradients of very few need.
 template <class T>
-int run_few(const ccdpp_softmax_t& p, const Plan& w, const Outs& o, char* ws, hipStream_t st) {
+int run_direct(const ccdpp_softmax_t& p, const Plan& w, const Outs& o, char* ws, hipStream_t st) {
     FewArgs a = {};
-    a.d = p.d, a.dp = (int)w.dp, a.v = p.v, a.table = p.table, a.ldt = p.ldt, a.ldx = p.ldx;
-    a.target_bits = p.target_bits, a.scale = p.scale, a.offset = p.offset;
-    a.part_row = p.t, a.z_row = round_up(p.v, 16);
-    for (int64_t t0 = 0; t0 < p.t; t0 += w.few_rows) {
-        a.t = (int)std::min<int64_t>(w.few_rows, p.t - t0);
-        a.x = (const T*)p.x + t0 * p.ldx;
-        a.part = w.forward ? (float2*)(ws + w.o_part) + t0 : nullptr;
-        a.z = w.grads ? (float*)(ws + w.o_z) + t0 * a.z_row : nullptr;
-        const hipError_t e = launch_few_logits<T>(a, w.few_blocks, st);
-        if (e != hipSuccess) return hip_fail(e, "logits");
-    }
+    a.t = (int)p.t, a.d = p.d, a.dp = (int)w.dp, a.v = p.v, a.x = p.x, a.table = p.table, a.ldt = p.ldt, a.ldx = p.ldx;
+    a.target = p.target, a.target_bits = p.target_bits, a.scale = p.scale, a.offset = p.offset;
+    a.part = w.forward ? (float2*)(ws + w.o_part) : nullptr;
+    a.z = w.grads ? (float*)(ws + w.o_z) : nullptr, a.z_row = w.vt * 32;
+    hipError_t e = launch_few_logits<T>(a, w.shape, st);
+    if (e != hipSuccess) return hip_fail(e, "logits");
     if (w.forward)
-        if (int rc = launch_loss<T>(p, (const float2*)(ws + w.o_part), w.few_blocks, Shares{}, o.loss, o.lse, RowNumbers{}, st)) return rc;
-    if (!w.grads || (!o.dx && !o.de)) return CCDPP_OK;
-    a.t = (int)p.t, a.x = p.x, a.target = p.target, a.z = (float*)(ws + w.o_z), a.part = nullptr;
+        if (int rc = launch_loss<T>(p, a.part, w.shape.blocks, Shares{}, o.loss, o.lse, RowNumbers{}, st)) return rc;
+    if (!w.few || !w.grads || (!o.dx && !o.de)) return CCDPP_OK;
     a.lse = w.forward ? o.lse : o.lse_in, a.grad = o.grad;
     a.de = o.de, a.ldde = o.ldde, a.dxp = o.dx ? (float*)(ws + w.o_dx) : nullptr, a.parts = w.few_parts;
-    const hipError_t e = launch_few_grads<T>(a, (T*)o.dx, o.lddx, st);
+    e = launch_few_grads<T>(a, (T*)o.dx, o.lddx, st);
     return e == hipSuccess ? CCDPP_OK : hip_fail(e, "gradients");
 }
 
@@ -1105,7 +1100,9 @@ int run_wide(const ccdpp_softmax_t& p, const Plan& w, const Outs& out, const int
     float* const kept = (float*)(ws + w.o_z);
     const int64_t pitch = w.vt * 32, chunks = (pitch + 1023) / 1024;
     const unsigned blocks = (unsigned)((w.vt + 7) / 8 * ((w.tt + 7) / 8));
-    if (w.sz > 1) {
+    if (w.direct) {
+        // done
+    } else if (w.sz > 1) {
         GemmArgs q = z;
         q.out = kept, q.out_split = p.t * pitch, q.ldo = q.cols = pitch, q.rows = p.t, q.splits = w.sz;
         k_gemm<P, PG, NPL, EPI_OUT, T><<<dim3(blocks, w.sz), kGemmThreads, 0, st>>>(q);
@@ -1118,7 +1115,7 @@ int run_wide(const ccdpp_softmax_t& p, const Plan& w, const Outs& out, const int
         k_gemm<P, PG, NPL, EPI_LSE, T><<<blocks, kGemmThreads, 0, st>>>(z);
         OPS_LAUNCH("logits");
     }
-    if (w.forward)
+    if (w.forward && !w.direct)
         if (int rc = launch_loss<T>(p, (const float2*)(ws + w.o_part), w.sz > 1 ? chunks : (w.vt + 7) / 8, Shares{}, out.loss, out.lse, RowNumbers{}, st)) return rc;
     if (!w.grads) return CCDPP_OK;
     z.lse = w.forward ? out.lse : out.lse_in, z.grad = out.grad;
@@ -1130,7 +1127,7 @@ int run_wide(const ccdpp_softmax_t& p, const Plan& w, const Outs& out, const int
         GemmArgs q = z;
         q.v0 = v0, q.a = z.a + v0 / 32 * z.a_tile, q.o2 = z.o2 + v0, q.m_tiles = nt;
         q.ksv = nt * 2, q.g_plane = w.tt * q.ksv * kBlk, q.gt_plane = nt * w.kst * kBlk;
-        if (w.sz > 1) k_terms<PG, NPL><<<dim3((unsigned)((nt + 3) / 4), (unsigned)w.tt), 256, 0, st>>>(q, kept + v0, pitch);
+        if (w.sz > 1 || w.direct) k_terms<PG, NPL><<<dim3((unsigned)((nt + 3) / 4), (unsigned)w.tt), 256, 0, st>>>(q, kept + v0, pitch);
         else k_gemm<P, PG, NPL, EPI_G, T><<<(unsigned)((nt + 7) / 8 * ((w.tt + 7) / 8)), kGemmThreads, 0, st>>>(q);
         OPS_LAUNCH("G");
         GemmArgs o = {};
@@ -1168,7 +1165,10 @@ int run(const ccdpp_softmax_t& p, int call, const Outs& out, char* ws, hipStream
     typedef typename Types<DT>::in T;
     constexpr int NPL = Types<DT>::planes;
     const Plan w = make_plan(p, call);
-    if (w.few) return run_few<T>(p, w, out, ws, st);
+    if (w.direct) {
+        const int rc = run_direct<T>(p, w, out, ws, st);
+        if (rc != CCDPP_OK || w.few || !w.grads) return rc;
+    }
     Scales sc;
     sc.e_part = (float*)(ws + w.o_scale), sc.x_part = sc.e_part + kParts, sc.g_part = sc.x_part + kParts;
     sc.fin = (int32_t*)(ws + w.o_fin), sc.x_row = (float*)(ws + w.o_xrow);
@@ -1197,8 +1197,9 @@ int run(const ccdpp_softmax_t& p, int call, const Outs& out, char* ws, hipStream
             x.turned_d = e.turned_d = 2 * kBlk, x.turned_plane = e.turned_plane = w.dt * 2 * kBlk;
         }
     } else {
-        x.nat = ws + w.o_xf, x.nat_plane = w.tt * w.ksd * kBlk;
-        e.nat = ws + w.o_ef, e.nat_plane = w.vt * w.ksd * kBlk;
+        if (!w.direct) x.nat = ws + w.o_xf, e.nat = ws + w.o_ef;
+        x.nat_plane = w.tt * w.ksd * kBlk;
+        e.nat_plane = w.vt * w.ksd * kBlk;
         x.num = ws + w.o_xn, e.num = ws + w.o_o2, x.num_row = e.num_row = 128;
         x.nat_row = e.nat_row = w.ksd * kBlk;
         if (w.grads) {
