@@ -18,6 +18,7 @@ constexpr int kTable = 64;      // tensors per launch
 constexpr int kBlocks = 1024;   // partial sums
 constexpr int64_t kChunk = 8192;
 constexpr int64_t kLittle = 32768;  // values that one block takes in one launch
+constexpr int64_t kLittleChunk = 512;
 
 struct Table {
     const void* in[kTable];
@@ -30,29 +31,29 @@ struct Table {
 };
 
 template <class T>
-__device__ __forceinline__ double chunk_squares(const void* base, int64_t lo, int64_t n) {
+__device__ __forceinline__ double chunk_squares(const void* base, int64_t lo, int64_t n, int lane, int lanes) {
     const T* g = (const T*)base + lo;
     constexpr int W = 16 / sizeof(T);
     double s = 0.0;
-    for (int64_t k = threadIdx.x; k < n / W; k += blockDim.x) {
-        const Run<T, W> q = ((const Run<T, W>*)g)[k];
+    for (int64_t k = lane; k < n / W; k += lanes) {
+        const Run<T, W> q = load_run<W>(g + k * W);
         for (int j = 0; j < W; ++j) s += (double)(float)q.v[j] * (double)(float)q.v[j];
     }
-    for (int64_t i = n / W * W + threadIdx.x; i < n; i += blockDim.x) s += (double)(float)g[i] * (double)(float)g[i];
+    for (int64_t i = n / W * W + lane; i < n; i += lanes) s += (double)(float)g[i] * (double)(float)g[i];
     return s;
 }
 
 template <class T>
-__device__ __forceinline__ void chunk_scale(const void* base, void* out, int64_t lo, int64_t n, float c) {
+__device__ __forceinline__ void chunk_scale(const void* base, void* out, int64_t lo, int64_t n, float c, int lane, int lanes) {
     const T* g = (const T*)base + lo;
     T* o = (T*)out + lo;
     constexpr int W = 16 / sizeof(T);
-    for (int64_t k = threadIdx.x; k < n / W; k += blockDim.x) {
-        Run<T, W> q = ((const Run<T, W>*)g)[k];
+    for (int64_t k = lane; k < n / W; k += lanes) {
+        Run<T, W> q = load_run<W>(g + k * W);
         for (int j = 0; j < W; ++j) q.v[j] = (T)((float)q.v[j] * c);
-        ((Run<T, W>*)o)[k] = q;
+        store_run<W>(o + k * W, q);
     }
-    for (int64_t i = n / W * W + threadIdx.x; i < n; i += blockDim.x) o[i] = (T)((float)g[i] * c);
+    for (int64_t i = n / W * W + lane; i < n; i += lanes) o[i] = (T)((float)g[i] * c);
 }
 
 // The tensor that a chunk belongs to.
@@ -88,7 +89,7 @@ __global__ __launch_bounds__(256) void k_squares(Table t, double* parts, int add
     for (int64_t c = blockIdx.x; c < t.chunks; c += gridDim.x) {
         const int i = find(t, c);
         const int64_t lo = (c - t.first[i]) * kChunk, n = min(kChunk, t.size[i] - lo);
-        typed(t.dtype[i], [&](auto z) { s += chunk_squares<decltype(z)>(t.in[i], lo, n); });
+        typed(t.dtype[i], [&](auto z) { s += chunk_squares<decltype(z)>(t.in[i], lo, n, threadIdx.x, 256); });
     }
     s = block_sum(s, red);
     if (threadIdx.x == 0) parts[blockIdx.x] = add ? parts[blockIdx.x] + s : s;
@@ -124,22 +125,30 @@ __global__ __launch_bounds__(256) void k_scale(Table t, const double* parts, flo
         const int i = find(t, k);
         if (c == 1.f && t.out[i] == t.in[i]) continue;
         const int64_t lo = (k - t.first[i]) * kChunk, n = min(kChunk, t.size[i] - lo);
-        typed(t.dtype[i], [&](auto z) { chunk_scale<decltype(z)>(t.in[i], t.out[i], lo, n, c); });
+        typed(t.dtype[i], [&](auto z) { chunk_scale<decltype(z)>(t.in[i], t.out[i], lo, n, c, threadIdx.x, 256); });
     }
 }
 
-// Little in all (kLittle values): one block, one launch.
+// Little in all (kLittle values): one block, one launch; a wave takes a chunk of kLittleChunk values.
 __global__ __launch_bounds__(1024) void k_little(Table t, int clip, float* norm, float max_norm, float eps) {
     __shared__ double red[16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const auto each = [&](auto&& body) {
+        for (int k = wave; k < (int)t.chunks; k += 16) {
+            const int i = find(t, k);
+            const int64_t lo = (k - t.first[i]) * kLittleChunk, n = min(kLittleChunk, t.size[i] - lo);
+            typed(t.dtype[i], [&](auto z) { body(z, i, lo, n); });
+        }
+    };
     double s = 0.0;
-    for (int i = 0; i < t.n; ++i) typed(t.dtype[i], [&](auto z) { s += chunk_squares<decltype(z)>(t.in[i], 0, t.size[i]); });
+    each([&](auto z, int i, int64_t lo, int64_t n) { s += chunk_squares<decltype(z)>(t.in[i], lo, n, lane, 64); });
     const float nv = (float)sqrt(block_sum(s, red));
     if (threadIdx.x == 0) *norm = nv;
     if (!clip) return;
     const float c = clip_factor(nv, max_norm, eps);
-    for (int i = 0; i < t.n; ++i)
-        if (c != 1.f || t.out[i] != t.in[i])
-            typed(t.dtype[i], [&](auto z) { chunk_scale<decltype(z)>(t.in[i], t.out[i], 0, t.size[i], c); });
+    each([&](auto z, int i, int64_t lo, int64_t n) {
+        if (c != 1.f || t.out[i] != t.in[i]) chunk_scale<decltype(z)>(t.in[i], t.out[i], lo, n, c, lane, 64);
+    });
 }
 
 int run(bool clip, int32_t n, const void* const* in, void* const* out, const int64_t* sizes, const int32_t* dtypes, float max_norm, float eps,
@@ -162,16 +171,18 @@ int run(bool clip, int32_t n, const void* const* in, void* const* out, const int
     Table t;
     int64_t values = 0;
     t.n = 0, t.chunks = 0;
+    int64_t chunk = kChunk;
     const auto add = [&](int32_t i) {
         t.in[t.n] = in[i], t.out[t.n] = clip ? out[i] : nullptr;
         t.size[t.n] = sizes[i], t.first[t.n] = t.chunks, t.dtype[t.n] = (uint8_t)dtypes[i];
-        t.chunks += (sizes[i] + kChunk - 1) / kChunk;
+        t.chunks += (sizes[i] + chunk - 1) / chunk;
         ++t.n;
     };
     int32_t filled = 0;
     for (int32_t i = 0; i < n; ++i)
         if (sizes[i]) ++filled, values += sizes[i];
     if (filled <= kTable && values <= kLittle) {
+        chunk = kLittleChunk;
         for (int32_t i = 0; i < n; ++i)
             if (sizes[i]) add(i);
         k_little<<<1, 1024, 0, st>>>(t, clip, norm, max_norm, eps);

@@ -9,9 +9,9 @@
 // step, of 32-bit ones 16 columns in four v_mfma_f32_16x16x4_f32, with exact products.  Any order of the columns will do
 // as long as x, which comes from LDS, has the same.  Where table rows are few, waves share their columns.
 //
-// k_few_grads: 16 table rows and 16 rows of x at a time in v_mfma_f32_16x16x4_f32, whatever the type: the table's values
-// are the operand of dx as they are read, x's are kept in registers for dtable, and the terms G stay in 32 bits.  A row's
-// values go to and from 16 lanes by 16 bytes.
+// k_few_grads: 16 table rows and 16 rows of x at a time (v_mfma_f32_16x16x4_f32, or 16x16x16 for 16-bit types): the
+// table's values are the operand of dx as they are read, x's are kept in registers for dtable, and the terms G stay in 32
+// bits, or two 16-bit planes.  A row's values go to and from 16 lanes by 16 bytes.
 #include <algorithm>
 
 #include "softmax_device.hpp"
@@ -43,14 +43,11 @@ template <> struct Few<_Float16> {
 
 // 16 bytes of a row from column c on; columns past d are 0.
 template <class T>
-__device__ __forceinline__ u32x4 piece(const T* row, int c, int d) {
-    constexpr int N = 16 / sizeof(T);
-    if (c + N <= d) return __builtin_bit_cast(u32x4, *(const Run<T, N>*)(row + c));
-    struct alignas(16) { T v[N]; } q;
-#pragma unroll
-    for (int j = 0; j < N; ++j) q.v[j] = c + j < d ? row[c + j] : (T)0.f;
-    return __builtin_bit_cast(u32x4, q);
+__device__ __forceinline__ u32x4 piece(const T* row, int c, int d, int64_t room) {
+    return __builtin_bit_cast(u32x4, load_tail<16 / sizeof(T)>(row, c, d, room));
 }
+
+constexpr int kBatch = 128;  // table rows whose terms are in LDS at a time
 
 // TG: 16 rows of x each; R: 16 table rows each that a wave takes at a time.
 template <class T, int TG, int R>
@@ -72,8 +69,12 @@ __global__ __launch_bounds__(kWaves * 64) void k_direct_logits(FewArgs a) {
     for (int64_t b = blockIdx.x; b < blocks; b += gridDim.x) {
         const int64_t g0 = (b * per + mine) * R;
         const T* row[R];
+        int64_t room[R];
 #pragma unroll
-        for (int r = 0; r < R; ++r) row[r] = (const T*)a.table + min((g0 + r) * 16 + m, a.v - 1) * a.ldt;
+        for (int r = 0; r < R; ++r) {
+            const int64_t v = min((g0 + r) * 16 + m, a.v - 1);
+            row[r] = (const T*)a.table + v * a.ldt, room[r] = (a.v - 1 - v) * a.ldt + a.d;
+        }
         f32x4 z[R][TG] = {};
         for (int c0 = 0; c0 < steps; c0 += a.chunk) {
             const int n = min(a.chunk, steps - c0);
@@ -87,7 +88,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_direct_logits(FewArgs a) {
                     for (int u = 0; u < 4; ++u) {
                         const int k = min(i + u * kWaves * 64, all - 1), t = k / (n * 4), c = k - t * n * 4;
                         to[u] = t * pitch + c * 16;
-                        p[u] = piece((const T*)a.x + t * a.ldx, (c0 * 4 + c) * N, a.d);
+                        p[u] = piece((const T*)a.x + t * a.ldx, (c0 * 4 + c) * N, a.d, (a.t - 1 - t) * a.ldx + a.d);
                     }
 #pragma unroll
                     for (int u = 0; u < 4; ++u) *(u32x4*)(lds + to[u]) = p[u];
@@ -103,7 +104,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_direct_logits(FewArgs a) {
 #pragma unroll
                 for (int u = 0; u < U; ++u)
 #pragma unroll
-                    for (int r = 0; r < R; ++r) e[u][r] = __builtin_bit_cast(u32x4, *(const Run<T, N>*)(row[r] + ((c0 + s + u) * 4 + q) * N));
+                    for (int r = 0; r < R; ++r) e[u][r] = __builtin_bit_cast(u32x4, load_run<N>(row[r] + ((c0 + s + u) * 4 + q) * N));
 #pragma unroll
                 for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -116,7 +117,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_direct_logits(FewArgs a) {
             for (; s < last; ++s)
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
-                    const u32x4 e = piece(row[r], ((c0 + s) * 4 + q) * N, a.d);
+                    const u32x4 e = piece(row[r], ((c0 + s) * 4 + q) * N, a.d, room[r]);
 #pragma unroll
                     for (int g = 0; g < TG; ++g) z[r][g] = Few<T>::step(e, *(const u32x4*)(x[g] + s * 64), z[r][g]);
                 }
@@ -191,58 +192,97 @@ __global__ __launch_bounds__(kWaves * 64) void k_direct_logits(FewArgs a) {
     }
 }
 
-constexpr int kBatch = 128;  // table rows whose terms are in LDS at a time
+// What the terms of up to 16 rows take, in LDS.
+struct FewRows {
+    float w[16], l2[16];  // weight (times scale), lse in base 2; 0 and +inf in rows that do not count
+    int y[16];            // target, or -1
+};
+
+// By the whole block; returns the largest finite |weight|.
+__device__ __forceinline__ float few_rows(const FewArgs& a, FewRows& rows) {
+    const int t = threadIdx.x & 15;
+    float w = 0.f, l2 = INFINITY;
+    int y = -1;
+    if (t < a.t) {
+        const int64_t yt = load_target(a.target, a.target_bits, t);
+        if (row_counts(yt, a.v, a.offset)) {
+            w = yt < a.v ? (a.grad ? a.grad[t] : 1.f) * a.scale : NAN;
+            l2 = a.lse[t] * kLog2e;
+            y = yt < a.v ? (int)yt : -1;
+        }
+    }
+    if (threadIdx.x < 16) rows.w[t] = w, rows.l2[t] = l2, rows.y[t] = y;
+    return wave_max(finite(w) ? fabsf(w) : 0.f);
+}
+
+// The terms of table rows b .. b + n - 1 (128 at most) by 256 threads: a thread has one table row and every other row of x,
+// its logits' reads all in flight.  put(table row, row of x, term); keep(table row, whether the item counts).
+template <class F, class K>
+__device__ __forceinline__ void few_terms(const FewArgs& a, const FewRows& rows, int64_t b, int n, float up, float up2, F&& put, K&& keep) {
+    const int r = threadIdx.x & (kBatch - 1), t0 = threadIdx.x / kBatch;
+    const int64_t v = b + min(r, n - 1);
+    float z[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) z[k] = a.z[min(t0 + 2 * k, a.t - 1) * a.z_row + v];
+    if (t0 == 0) keep(r, r < n && !(a.offset && a.offset[v] < kExcluded));
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const int t = t0 + 2 * k;
+        const float w = rows.w[t] * up * up2;
+        float g = w * (exp2_fast(z[k] - rows.l2[t]) - (rows.y[t] == v ? 1.f : 0.f));
+        if (r >= n || rows.l2[t] == INFINITY) g = 0.f;
+        put(r, t, g);
+    }
+}
+
+// Waves that took different rows are added in order; a block leaves one partial sum of dx.
+template <int C>
+__device__ __forceinline__ void add_waves(const FewArgs& a, const float (*red)[16 * 16 * C]) {
+    const int across = a.across, down = 4 / across;
+    __syncthreads();
+    for (int i = threadIdx.x; i < a.t * across * 16 * C; i += 256) {
+        const int t = i / (across * 16 * C), k = i - t * across * 16 * C, w = k / (16 * C), col = blockIdx.x * across * 16 * C + k;
+        if (col >= a.dp) continue;
+        float s = 0.f;
+        for (int y = 0; y < down; ++y) s += red[y * across + w][t * 16 * C + (k - w * 16 * C)];
+        a.dxp[((int64_t)blockIdx.y * a.t + t) * a.dp + col] = s;
+    }
+}
 
 template <class T>
-__global__ __launch_bounds__(256, 2) void k_few_grads(FewArgs a) {
+__global__ __launch_bounds__(256, 3) void k_few_grads(FewArgs a) {
     constexpr int C = 16 / sizeof(T);  // columns of a lane: 16 C of them are beside each other
     typedef Run<T, C> Piece;
+    __shared__ FewRows info;
     __shared__ float terms[kBatch][17];
     __shared__ float keep[kBatch];
     __shared__ __align__(16) float red[4][16 * 16 * C];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, q = lane >> 4;
     const int across = a.across, wx = wave & (across - 1), wy = wave / across, down = 4 / across;
     const int c = (blockIdx.x * across + wx) * 16 * C + n * C;
-    const bool whole = c + C <= a.d;
+    const bool idle = c - n * C >= a.d;  // the wave's columns are past the row
     const int64_t r0 = a.v * blockIdx.y / gridDim.y, r1 = a.v * (blockIdx.y + 1) / gridDim.y;
     // x as the operand of dtable: rows 4 j + q, zero where they do not count
     float x[4][C];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const int t = 4 * j + q;
-        const bool counts = a.de && t < a.t && row_counts(load_target(a.target, a.target_bits, t), a.v, a.offset);
+        Piece row = {};
+        if (a.de && t < a.t && row_counts(load_target(a.target, a.target_bits, t), a.v, a.offset))
+            row = load_tail<C>((const T*)a.x + t * a.ldx, c, a.d, (a.t - 1 - t) * a.ldx + a.d);
 #pragma unroll
-        for (int i = 0; i < C; ++i) x[j][i] = counts && c + i < a.d ? (float)((const T*)a.x)[t * a.ldx + c + i] : 0.f;
+        for (int i = 0; i < C; ++i) x[j][i] = (float)row.v[i];
     }
+    few_rows(a, info);
     f32x4 dx[C] = {};
-    const auto read = [&](int64_t row, Piece& e) {
-        const T* const at = (const T*)a.table + row * a.ldt + c;
-        if (whole) {
-            e = *(const Piece*)at;
-        } else {
-#pragma unroll
-            for (int i = 0; i < C; ++i) e.v[i] = c + i < a.d ? at[i] : (T)0.f;
-        }
-    };
+    const auto read = [&](int64_t row, Piece& e) { e = load_tail<C>((const T*)a.table + row * a.ldt, c, a.d, (a.v - 1 - row) * a.ldt + a.d); };
     for (int64_t b = r0; b < r1; b += kBatch) {
         const int rows = (int)min((int64_t)kBatch, r1 - b);
         __syncthreads();
-        for (int i = threadIdx.x; i < 16 * kBatch; i += 256) {
-            const int t = i / kBatch, r = i % kBatch;
-            float g = 0.f;
-            if (t < a.t && r < rows) {
-                const int64_t y = load_target(a.target, a.target_bits, t);
-                if (row_counts(y, a.v, a.offset)) {
-                    const float w = y < a.v ? (a.grad ? a.grad[t] : 1.f) * a.scale : NAN;
-                    const float p = exp2_fast(a.z[t * a.z_row + b + r] - a.lse[t] * kLog2e);
-                    g = w * (p - (y == b + r ? 1.f : 0.f));
-                }
-            }
-            terms[r][t] = g;
-            if (t == 0) keep[r] = r < rows && !(a.offset && a.offset[b + r] < kExcluded) ? 1.f : 0.f;
-        }
+        few_terms(a, info, b, rows, 1.f, 1.f, [&](int r, int t, float g) { terms[r][t] = g; },
+                  [&](int r, bool counts) { keep[r] = counts ? 1.f : 0.f; });
         __syncthreads();
-        const int tiles = (rows + 15) / 16;
+        const int tiles = idle ? 0 : (rows + 15) / 16;
         Piece next[4];
         if (wy < tiles)
 #pragma unroll
@@ -271,34 +311,128 @@ __global__ __launch_bounds__(256, 2) void k_few_grads(FewArgs a) {
             for (int r = 0; r < 4; ++r) {
                 const int row = i * 16 + 4 * q + r;
                 if (row >= rows) continue;
-                T* const to = (T*)a.de + (b + row) * a.ldde + c;
                 Piece o;
 #pragma unroll
                 for (int l = 0; l < C; ++l) o.v[l] = (T)de[l][r];
-                if (whole) {
-                    *(Piece*)to = o;
-                } else {
-#pragma unroll
-                    for (int l = 0; l < C; ++l)
-                        if (c + l < a.d) to[l] = o.v[l];
-                }
+                store_tail<C>((T*)a.de + (b + row) * a.ldde, c, a.d, o);
             }
         }
     }
     if (!a.dxp) return;
-    // Waves that took different rows are added in order; a block leaves one partial sum.
 #pragma unroll
     for (int l = 0; l < C; ++l)
 #pragma unroll
         for (int r = 0; r < 4; ++r) red[wave][(4 * q + r) * 16 * C + n * C + l] = dx[l][r];
-    __syncthreads();
-    for (int i = threadIdx.x; i < a.t * across * 16 * C; i += 256) {
-        const int t = i / (across * 16 * C), k = i - t * across * 16 * C, w = k / (16 * C), col = blockIdx.x * across * 16 * C + k;
-        if (col >= a.dp) continue;
-        float s = 0.f;
-        for (int y = 0; y < down; ++y) s += red[y * across + w][t * 16 * C + (k - w * 16 * C)];
-        a.dxp[((int64_t)blockIdx.y * a.t + t) * a.dp + col] = s;
+    add_waves<C>(a, red);
+}
+
+// 16-bit types: the same with v_mfma_f32_16x16x16 on the values as they are; the terms, by a power of two below 2^13, are
+// the sum of two 16-bit planes.
+template <class T> struct Half;
+template <> struct Half<_Float16> {
+    typedef _Float16 vec __attribute__((ext_vector_type(4)));
+    static __device__ __forceinline__ f32x4 mfma(vec a, vec b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x16f16(a, b, c, 0, 0, 0); }
+};
+template <> struct Half<__bf16> {
+    typedef __bf16 vec __attribute__((ext_vector_type(4)));
+    typedef short bits __attribute__((ext_vector_type(4)));
+    static __device__ __forceinline__ f32x4 mfma(vec a, vec b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(bits, a), __builtin_bit_cast(bits, b), c, 0, 0, 0);
     }
+};
+
+template <class T>
+__global__ __launch_bounds__(256, 3) void k_few_grads16(FewArgs a) {
+    constexpr int C = 8;
+    typedef Run<T, C> Piece;
+    typedef typename Half<T>::vec V;
+    __shared__ __align__(16) T by_row[2][kBatch][20];      // [plane][table row][row of x], pitch against bank conflicts
+    __shared__ __align__(16) T by_x[2][16][kBatch + 8];    // [plane][row of x][table row]
+    __shared__ FewRows info;
+    __shared__ uint16_t keep[kBatch];
+    __shared__ __align__(16) float red[4][16 * 16 * C];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, q = lane >> 4;
+    const int across = a.across, wx = wave & (across - 1), wy = wave / across, down = 4 / across;
+    const int c = (blockIdx.x * across + wx) * 16 * C + n * C;
+    const bool idle = c - n * C >= a.d;  // the wave's columns are past the row
+    const int64_t r0 = a.v * blockIdx.y / gridDim.y, r1 = a.v * (blockIdx.y + 1) / gridDim.y;
+    const float most = few_rows(a, info);
+    const int e2 = scale_exp(most) - 2;
+    const float up = ldexpf(1.f, e2 / 2), up2 = ldexpf(1.f, e2 - e2 / 2), back = ldexpf(1.f, -(e2 / 2)), back2 = ldexpf(1.f, -(e2 - e2 / 2));
+    V x[C];  // the operand of dtable: rows 4 q + i, zero where they do not count
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int t = 4 * q + i;
+        Piece row = {};
+        if (a.de && t < a.t && row_counts(load_target(a.target, a.target_bits, t), a.v, a.offset))
+            row = load_tail<C>((const T*)a.x + t * a.ldx, c, a.d, (a.t - 1 - t) * a.ldx + a.d);
+#pragma unroll
+        for (int l = 0; l < C; ++l) x[l][i] = row.v[l];
+    }
+    f32x4 dx[C] = {};
+    const auto read = [&](int64_t row, Piece& e) { e = load_tail<C>((const T*)a.table + row * a.ldt, c, a.d, (a.v - 1 - row) * a.ldt + a.d); };
+    for (int64_t b = r0; b < r1; b += kBatch) {
+        const int rows = (int)min((int64_t)kBatch, r1 - b);
+        const int tiles = idle ? 0 : (rows + 15) / 16;
+        Piece next[4];
+        if (wy < tiles)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) read(b + min(wy * 16 + 4 * q + j, rows - 1), next[j]);
+        __syncthreads();
+        few_terms(a, info, b, rows, up, up2,
+                  [&](int r, int t, float g) {
+                      const T hi = (T)g, lo = finite((float)hi) ? (T)(g - (float)hi) : (T)0.f;
+                      by_row[0][r][t] = hi, by_row[1][r][t] = lo;
+                      by_x[0][t][r] = hi, by_x[1][t][r] = lo;
+                  },
+                  [&](int r, bool counts) { keep[r] = counts ? 0xffff : 0; });
+        __syncthreads();
+        for (int i = wy; i < tiles; i += down) {
+            Piece e[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) e[j] = next[j];
+            if (i + down < tiles)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) read(b + min((i + down) * 16 + 4 * q + j, rows - 1), next[j]);
+            uint16_t k[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) k[j] = keep[i * 16 + 4 * q + j];
+            V gx[2], ge[2];
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                gx[p] = *(const V*)&by_x[p][n][i * 16 + 4 * q];
+                ge[p] = *(const V*)&by_row[p][i * 16 + n][4 * q];
+            }
+            f32x4 de[C] = {};
+#pragma unroll
+            for (int l = 0; l < C; ++l) {
+                V v;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = __builtin_bit_cast(T, (uint16_t)(__builtin_bit_cast(uint16_t, e[j].v[l]) & k[j]));
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    dx[l] = Half<T>::mfma(gx[p], v, dx[l]);
+                    de[l] = Half<T>::mfma(ge[p], x[l], de[l]);
+                }
+            }
+            if (!a.de) continue;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int row = i * 16 + 4 * q + r;
+                if (row >= rows) continue;
+                Piece o;
+#pragma unroll
+                for (int l = 0; l < C; ++l) o.v[l] = (T)(de[l][r] * back * back2);
+                store_tail<C>((T*)a.de + (b + row) * a.ldde, c, a.d, o);
+            }
+        }
+    }
+    if (!a.dxp) return;
+#pragma unroll
+    for (int l = 0; l < C; ++l)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) red[wave][(4 * q + r) * 16 * C + n * C + l] = dx[l][r] * back * back2;
+    add_waves<C>(a, red);
 }
 
 // dx from the blocks' partial sums: 16 quads of columns x 16 shares of the partial sums a block, joined in order.
@@ -364,7 +498,9 @@ hipError_t launch_few_grads(const FewArgs& a, T* dx, int64_t lddx, hipStream_t s
     constexpr int C = 16 / sizeof(T);
     FewArgs b = a;
     b.across = few_across(a.d, C);
-    k_few_grads<T><<<dim3((a.d + b.across * 16 * C - 1) / (b.across * 16 * C), a.parts), 256, 0, st>>>(b);
+    const dim3 grid((a.d + b.across * 16 * C - 1) / (b.across * 16 * C), a.parts);
+    if constexpr (sizeof(T) == 4) k_few_grads<T><<<grid, 256, 0, st>>>(b);
+    else k_few_grads16<T><<<grid, 256, 0, st>>>(b);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !dx) return e;
     k_few_finish<T><<<a.t * ((a.dp / 4 + 15) / 16), 256, 0, st>>>(a, a.parts, dx, lddx);

@@ -53,7 +53,7 @@ __device__ __forceinline__ float run_max(const T* at, int64_t n, int64_t lane, i
     for (int64_t i = lane; i < whole; i += lanes * U) {
         Run<T, N> q[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) q[u] = *(const Run<T, N>*)(at + min(i + u * lanes, whole - 1) * N);
+        for (int u = 0; u < U; ++u) q[u] = load_run<N>(at + min(i + u * lanes, whole - 1) * N);
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -209,23 +209,17 @@ __global__ __launch_bounds__(256) void k_pack(PackArgs a) {
         const int s = wave + 4 * k, ks = c0 / 16 + s;
         if (ks >= a.ksd) break;
         const int c = c0 + 16 * s + 8 * h;
-        T v[8];
-        if (in && c + 8 <= a.d) {
-            const Run<T, 8> q = *(const Run<T, 8>*)(src + c);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = q.v[j];
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = in && c + j < a.d ? src[c + j] : (T)0.f;
-        }
+        Run<T, 8> q = {};
+        if (in) q = load_tail<8>(src, c, a.d, (side.rows - 1 - row) * side.ld + a.d);
+        T* const v = q.v;
         if (!is_x && !counts)
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = (T)0.f;
         if (side.turned) {
-            struct alignas(16) Eight { T v[8]; } q;
+            struct alignas(16) Eight { T v[8]; } to;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) q.v[j] = counts ? (live[m] < 0.f ? (T)(-(float)v[j]) : v[j]) : (T)0.f;
-            *(Eight*)&tile[m][16 * s + 8 * h] = q;
+            for (int j = 0; j < 8; ++j) to.v[j] = counts ? (live[m] < 0.f ? (T)(-(float)v[j]) : v[j]) : (T)0.f;
+            *(Eight*)&tile[m][16 * s + 8 * h] = to;
         }
         typename P::elem o[8][2];
 #pragma unroll
@@ -573,7 +567,7 @@ __global__ __launch_bounds__(kGemmThreads) void k_gemm(GemmArgs a) {
                     for (int r = 0; r < 4; ++r) t.v[r] = (T)(v[r] * fg * f);
                     T* const o = (T*)a.last + row * a.ldo + col;
                     if (col + 4 <= a.cols) {
-                        *(Run<T, 4>*)o = t;
+                        store_run<4>(o, t);
                     } else {
 #pragma unroll
                         for (int r = 0; r < 4; ++r)
@@ -772,7 +766,7 @@ __global__ __launch_bounds__(256) void k_loss(ccdpp_softmax_t p, const float2* p
         constexpr int N = 16 / sizeof(T);
 #pragma unroll 4
         for (int d = i0 * N; d + N <= p.d; d += THREADS * N) {
-            const Run<T, N> a = *(const Run<T, N>*)(x + d), b = *(const Run<T, N>*)(e + d);
+            const Run<T, N> a = load_run<N>(x + d), b = load_run<N>(e + d);
 #pragma unroll
             for (int j = 0; j < N; ++j) dot = fmaf((float)a.v[j], (float)b.v[j], dot);
         }
@@ -857,7 +851,7 @@ __global__ __launch_bounds__(256) void k_finish(FinishSide x, FinishSide e, int6
 #pragma unroll
         for (int j = 0; j < 4; ++j) t.v[j] = (T)(v[j] * fg * f);
         if (c + 4 <= cols) {
-            *(Run<T, 4>*)o = t;
+            store_run<4>(o, t);
         } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
@@ -919,7 +913,7 @@ Plan make_plan(const ccdpp_softmax_t& p, int call) {
     }
     if (w.few) {
         const int64_t wide = (int64_t)few_across(p.d, 16 / es) * 16 * (16 / es), beside = (p.d + wide - 1) / wide;
-        w.few_parts = (int)std::max<int64_t>(1, std::min<int64_t>(1024 / beside, (p.v + 63) / 64));
+        w.few_parts = (int)std::max<int64_t>(1, std::min<int64_t>((es == 4 ? 1024 : 768) / beside, (p.v + 63) / 64));  // as many blocks as run at once
         w.dp = round_up(p.d, 4);
         w.o_dx = take(w.grads ? w.few_parts * p.t * w.dp * 4 : 0);
         w.bytes = at;

@@ -57,82 +57,93 @@ def _check(rc):
 
 
 class _On:
-    """Makes the tensors' device current while a call runs, where it is not."""
+    """Makes a device current while a call runs, where it is not."""
+    __slots__ = ("guard",)
 
-    def __init__(self, device):
-        self._guard = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+    def __init__(self, index):
+        self.guard = None if index == torch.cuda.current_device() else torch.cuda.device(index)
 
     def __enter__(self):
-        if self._guard:
-            self._guard.__enter__()
+        if self.guard:
+            self.guard.__enter__()
 
     def __exit__(self, *exc):
-        if self._guard:
-            self._guard.__exit__(*exc)
+        if self.guard:
+            self.guard.__exit__(*exc)
 
 
 def _matrix(a, name):
+    """The row stride of a matrix of device memory."""
     if not isinstance(a, torch.Tensor) or a.dim() != 2:
         raise TypeError(f"{name} must be a matrix (a two-dimensional tensor)")
-    if not a.is_cuda:
+    if a.get_device() < 0:
         raise ValueError(f"{name} must be in device memory")
     if a.dtype not in _DTYPES:
         raise TypeError(f"{name} must be float32, bfloat16 or float16, not {a.dtype}")
     rows, d = a.shape
-    if d > 1 and a.stride(1) != 1:
+    ld, step = a.stride()
+    if step != 1 and d > 1:
         raise ValueError(f"{name}'s rows must be contiguous")
-    return a.stride(0) if rows > 1 else max(d, 1)
+    return ld if rows > 1 else max(d, 1)
 
 
-def _vector(a, name, n, dtypes, device):
+def _vector(a, name, n, dtypes, index):
     if not isinstance(a, torch.Tensor) or a.dtype not in dtypes:
         raise TypeError(f"{name} must be a tensor of {' or '.join(str(t)[6:] for t in dtypes)}")
-    if a.shape != (n,) or not a.is_contiguous():
+    if a.dim() != 1 or a.numel() != n or not a.is_contiguous():
         raise ValueError(f"{name} must be contiguous, with {n} values")
-    if a.device != device:
-        raise ValueError(f"{name} must be on {device}")
+    if a.get_device() != index:
+        raise ValueError(f"{name} must be on device {index}")
     return a.data_ptr()
+
+
+_INTS, _FLOATS = (torch.int64, torch.int32), (torch.float32,)
 
 
 def _problem(x, table, target, scale, offset):
     ldx, ldt = _matrix(x, "x"), _matrix(table, "table")
-    if x.dtype != table.dtype or x.device != table.device:
+    index, dtype = x.get_device(), x.dtype
+    if dtype != table.dtype or index != table.get_device():
         raise ValueError("x and table must have the same type and device")
-    if x.shape[1] != table.shape[1]:
-        raise ValueError(f"x has {x.shape[1]} columns and table {table.shape[1]}")
-    y = _vector(target, "target", x.shape[0], (torch.int64, torch.int32), x.device)
-    o = None if offset is None else _vector(offset, "offset", table.shape[0], (torch.float32,), x.device)
-    return Softmax(x.shape[0], table.shape[0], x.shape[1], _DTYPES[x.dtype], x.data_ptr(), ldx, table.data_ptr(), ldt,
-                   y, 64 if target.dtype == torch.int64 else 32, scale, o)
+    (t, d), (v, e) = x.shape, table.shape
+    if d != e:
+        raise ValueError(f"x has {d} columns and table {e}")
+    y = _vector(target, "target", t, _INTS, index)
+    o = None if offset is None else _vector(offset, "offset", v, _FLOATS, index)
+    return Softmax(t, v, d, _DTYPES[dtype], x.data_ptr(), ldx, table.data_ptr(), ldt, y,
+                   64 if target.dtype == torch.int64 else 32, scale, o), index
 
 
 def _workspace(p, call, device):
     n = ctypes.c_int64()
     _check(_lib().ccdpp_softmax_workspace(ctypes.byref(p), call, ctypes.byref(n)))
-    return torch.empty(n.value, dtype=torch.uint8, device=device)
+    return torch.empty(n.value, dtype=torch.uint8, device=device), n
 
 
-def _stream(device):
-    return torch.cuda.current_stream(device).cuda_stream
+# PyTorch's current stream of a device, as the handle alone (1.9 us with the stream object).
+_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
 def _out(a, like, name):
-    if a is None:
-        return torch.empty(like.shape, dtype=like.dtype, device=like.device)
-    if _matrix(a, name) < 0 or a.shape != like.shape or a.dtype != like.dtype or a.device != like.device:
+    if _matrix(a, name) < 0 or a.shape != like.shape or a.dtype != like.dtype or a.get_device() != like.get_device():
         raise ValueError(f"{name} must have the shape, type and device of what it is the gradient of")
     return a
 
 
 def _gradient_buffers(x, table, dx, dtable, need):
     """(dx, its pointer, its row stride, dtable, ...) for the gradients that are asked for."""
-    for n in need:
-        if n not in ("x", "table"):
-            raise ValueError(f"need is made of 'x' and 'table', not {n!r}")
+    if not set(need) <= {"x", "table"}:
+        raise ValueError(f"need is made of 'x' and 'table', not {need!r}")
     got = []
     for name, like, a in (("x", x, dx), ("table", table, dtable)):
-        a = _out(a, like, "d" + name) if name in need else None
-        got += [a, None if a is None else a.data_ptr(), 0 if a is None else _matrix(a, "d" + name)]
+        if name not in need:
+            got += [None, None, 0]
+        elif a is None:
+            a = torch.empty(like.shape, dtype=like.dtype, device=like.device)
+            got += [a, a.data_ptr(), max(like.shape[1], 1)]
+        else:
+            a = _out(a, like, "d" + name)
+            got += [a, a.data_ptr(), _matrix(a, "d" + name)]
     return got
 
 
@@ -141,13 +152,13 @@ def softmax_loss(x, table, target, *, scale=1.0, offset=None):
     target's logit.  x: t x d, table: v x d (float32, bfloat16 or float16; rows may lie apart), target: int32 or int64.
     A negative target marks an ignored row (loss 0); one past the table makes the row's loss NaN.  offset: float32 per
     item or None; -inf (or anything below -1e38) excludes an item, and a target that is excluded has loss +inf."""
-    p = _problem(x, table, target, scale, offset)
-    with _On(x.device):
-        loss = torch.empty(p.t, dtype=torch.float32, device=x.device)
-        lse = torch.empty_like(loss)
-        ws = _workspace(p, LOSS, x.device)
-        _check(_lib().ccdpp_softmax_loss(ctypes.byref(p), loss.data_ptr(), lse.data_ptr(), ws.data_ptr(), ws.numel(),
-                                         _stream(x.device)))
+    p, index = _problem(x, table, target, scale, offset)
+    device = x.device
+    with _On(index):
+        loss = torch.empty(p.t, dtype=torch.float32, device=device)
+        lse = torch.empty(p.t, dtype=torch.float32, device=device)
+        ws, n = _workspace(p, LOSS, device)
+        _check(_lib().ccdpp_softmax_loss(ctypes.byref(p), loss.data_ptr(), lse.data_ptr(), ws.data_ptr(), n, _stream(index)))
     return loss, lse
 
 
@@ -155,29 +166,29 @@ def softmax_loss_grad(x, table, target, lse, *, grad=None, scale=1.0, offset=Non
     """(dx, dtable): gradients of sum_i grad[i] loss[i], from the lse of softmax_loss.  grad: float32 per row, or None
     for ones.  dx and dtable may be given to write to.  A gradient that is not in `need` is not computed (None).
     Ignored rows, rows whose target is excluded and excluded items take no part, whatever they hold."""
-    p = _problem(x, table, target, scale, offset)
-    l = _vector(lse, "lse", p.t, (torch.float32,), x.device)
-    g = None if grad is None else _vector(grad, "grad", p.t, (torch.float32,), x.device)
-    with _On(x.device):
+    p, index = _problem(x, table, target, scale, offset)
+    l = _vector(lse, "lse", p.t, _FLOATS, index)
+    g = None if grad is None else _vector(grad, "grad", p.t, _FLOATS, index)
+    with _On(index):
         dx, pdx, lddx, dtable, pde, ldde = _gradient_buffers(x, table, dx, dtable, need)
-        ws = _workspace(p, GRAD, x.device)
-        _check(_lib().ccdpp_softmax_loss_grad(ctypes.byref(p), l, g, pdx, lddx, pde, ldde, ws.data_ptr(), ws.numel(),
-                                              _stream(x.device)))
+        ws, n = _workspace(p, GRAD, x.device)
+        _check(_lib().ccdpp_softmax_loss_grad(ctypes.byref(p), l, g, pdx, lddx, pde, ldde, ws.data_ptr(), n, _stream(index)))
     return dx, dtable
 
 
 def softmax_loss_train(x, table, target, *, grad=None, scale=1.0, offset=None, dx=None, dtable=None, need=("x", "table")):
     """(loss, lse, dx, dtable): softmax_loss and softmax_loss_grad in one call, for rows whose weights `grad` are known
     beforehand (1 / the number of rows that count, for a mean)."""
-    p = _problem(x, table, target, scale, offset)
-    g = None if grad is None else _vector(grad, "grad", p.t, (torch.float32,), x.device)
-    with _On(x.device):
-        loss = torch.empty(p.t, dtype=torch.float32, device=x.device)
-        lse = torch.empty_like(loss)
+    p, index = _problem(x, table, target, scale, offset)
+    g = None if grad is None else _vector(grad, "grad", p.t, _FLOATS, index)
+    device = x.device
+    with _On(index):
+        loss = torch.empty(p.t, dtype=torch.float32, device=device)
+        lse = torch.empty(p.t, dtype=torch.float32, device=device)
         dx, pdx, lddx, dtable, pde, ldde = _gradient_buffers(x, table, dx, dtable, need)
-        ws = _workspace(p, TRAIN, x.device)
+        ws, n = _workspace(p, TRAIN, device)
         _check(_lib().ccdpp_softmax_loss_train(ctypes.byref(p), loss.data_ptr(), lse.data_ptr(), g, pdx, lddx, pde, ldde,
-                                               ws.data_ptr(), ws.numel(), _stream(x.device)))
+                                               ws.data_ptr(), n, _stream(index)))
     return loss, lse, dx, dtable
 
 
@@ -191,35 +202,39 @@ def _dense(a):
     return True
 
 
+def _each(method, tensors):
+    return list(map(method, tensors))
+
+
 def _tensors(tensors, out):
+    """(device index, n, and the library's tables of) the gradients and what they are clipped into."""
     tensors = list(tensors)
     n = len(tensors)
-    device = tensors[0].device if n and isinstance(tensors[0], torch.Tensor) else None
-    kinds, sizes, flat = [], [], True
-    for a in tensors:
-        kind = _DTYPES.get(a.dtype) if isinstance(a, torch.Tensor) else None
-        if kind is None:
-            raise TypeError("gradients must be float32, bfloat16 or float16 tensors")
-        if not a.is_cuda or a.device != device:
-            raise ValueError("gradients must be in the memory of one device")
-        if not a.is_contiguous():
-            flat = False
-            if not _dense(a):
-                raise ValueError("gradients must fill one piece of memory each")
-        kinds.append(kind)
-        sizes.append(a.numel())
+    T = torch.Tensor
+    where = set(_each(T.get_device, tensors))  # (a TypeError for what is no tensor)
+    dtypes = [a.dtype for a in tensors]
+    kinds = [_DTYPES.get(t) for t in dtypes]
+    if None in kinds:
+        raise TypeError("gradients must be float32, bfloat16 or float16 tensors")
+    if len(where) > 1 or -1 in where:
+        raise ValueError("gradients must be in the memory of one device")
+    flat = all(map(T.is_contiguous, tensors))
+    if not flat and not all(map(_dense, tensors)):
+        raise ValueError("gradients must fill one piece of memory each")
+    sizes = _each(T.numel, tensors)
     P = ctypes.c_void_p * n
-    ins = outs = P(*[a.data_ptr() for a in tensors])
+    ins = outs = P(*_each(T.data_ptr, tensors))
     if out is not None:
         out = list(out)
         if len(out) != n:
             raise ValueError("out must have one tensor for each gradient")
-        for a, o in zip(tensors, out):
-            if o.shape != a.shape or o.dtype != a.dtype or o.device != device or not (
-                    o.is_contiguous() if flat else o.stride() == a.stride() or a.numel() < 2):
-                raise ValueError("out must be like the gradients in shape, strides, type and device")
-        outs = P(*[o.data_ptr() for o in out])
-    return (device or torch.device("cuda", torch.cuda.current_device()), n, ins, outs, (ctypes.c_int64 * n)(*sizes),
+        if (not set(_each(T.get_device, out)) <= where or [o.dtype for o in out] != dtypes or _each(T.numel, out) != sizes
+                or _each(T.dim, out) != _each(T.dim, tensors)
+                or not (all(map(T.is_contiguous, out)) if flat else all(
+                    o.shape == a.shape and (o.stride() == a.stride() or a.numel() < 2) for a, o in zip(tensors, out)))):
+            raise ValueError("out must be like the gradients in shape, strides, type and device")
+        outs = P(*_each(T.data_ptr, out))
+    return (where.pop() if where else torch.cuda.current_device(), n, ins, outs, (ctypes.c_int64 * n)(*sizes),
             (ctypes.c_int32 * n)(*kinds))
 
 
@@ -232,11 +247,12 @@ def _norm_workspace_bytes():
 
 def grad_norm(tensors):
     """The 2-norm of all values of the tensors together: a float32 scalar in device memory."""
-    device, n, ptrs, _, sizes, dtypes = _tensors(tensors, None)
-    with _On(device):
+    index, n, ptrs, _, sizes, dtypes = _tensors(tensors, None)
+    with _On(index):
+        device = torch.device("cuda", index)
         norm = torch.empty((), dtype=torch.float32, device=device)
         ws = torch.empty(_norm_workspace_bytes(), dtype=torch.uint8, device=device)
-        _check(_lib().ccdpp_grad_norm(n, ptrs, sizes, dtypes, norm.data_ptr(), ws.data_ptr(), ws.numel(), _stream(device)))
+        _check(_lib().ccdpp_grad_norm(n, ptrs, sizes, dtypes, norm.data_ptr(), ws.data_ptr(), ws.numel(), _stream(index)))
     return norm
 
 
@@ -244,10 +260,11 @@ def clip_grads(tensors, max_norm, *, eps=1e-6, out=None):
     """Multiplies all tensors with min(1, max_norm / (norm + eps)), in place or into `out`; returns their norm before
     that (a float32 scalar in device memory).  A norm that is NaN makes every value NaN, an infinite one the finite
     values 0."""
-    device, n, ptrs, outs, sizes, dtypes = _tensors(tensors, out)
-    with _On(device):
+    index, n, ptrs, outs, sizes, dtypes = _tensors(tensors, out)
+    with _On(index):
+        device = torch.device("cuda", index)
         norm = torch.empty((), dtype=torch.float32, device=device)
         ws = torch.empty(_norm_workspace_bytes(), dtype=torch.uint8, device=device)
-        _check(_lib().ccdpp_clip_grads(n, ptrs, outs, sizes, dtypes, max_norm, eps,
-                                       norm.data_ptr(), ws.data_ptr(), ws.numel(), _stream(device)))
+        _check(_lib().ccdpp_clip_grads(n, ptrs, outs, sizes, dtypes, max_norm, eps, norm.data_ptr(), ws.data_ptr(), ws.numel(),
+                                       _stream(index)))
     return norm
