@@ -52,7 +52,7 @@ constexpr int kBatch = 128;  // table rows whose terms are in LDS at a time
 // TG: 16 rows of x each; R: 16 table rows each that a wave takes at a time.
 template <class T, int TG, int R>
 __global__ __launch_bounds__(kWaves * 64) void k_direct_logits(FewArgs a) {
-    constexpr int N = 16 / sizeof(T), U = R * TG > 8 ? 2 : 4;
+    constexpr int N = 16 / sizeof(T), U = R * TG > 8 ? 2 : R * TG > 1 ? 4 : 8;
     extern __shared__ __align__(16) char lds[];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, q = lane >> 4;
     const int steps = (a.d + 4 * N - 1) / (4 * N), pitch = a.chunk * 64 + 16;
