@@ -17,15 +17,16 @@ namespace {
 constexpr int kTable = 64;      // tensors per launch
 constexpr int kBlocks = 1024;   // partial sums
 constexpr int64_t kChunk = 8192;
-constexpr int64_t kLittle = 32768;  // values that one block takes in one launch
-constexpr int64_t kLittleChunk = 512;
+// What one block takes in one launch: kMine chunks of kLittleChunk bytes for each of its waves.
+constexpr int kMine = 6;
+constexpr int64_t kLittleChunk = 2048;
 
 struct Table {
     const void* in[kTable];
     void* out[kTable];
     int64_t size[kTable];
     int64_t first[kTable];   // first chunk of each tensor
-    uint8_t dtype[kTable];
+    int32_t dtype[kTable];
     int n;
     int64_t chunks;
 };
@@ -129,27 +130,82 @@ __global__ __launch_bounds__(256) void k_scale(Table t, const double* parts, flo
     }
 }
 
-// Little in all (kLittle values): one block, one launch; a wave takes a chunk of kLittleChunk values.
+// Little in all: one block, one launch.  Its time is that of the round trips to memory, so there is one: a wave reads
+// all its chunks at once, two runs of 16 bytes a lane, and a thread one of the values that tensors have over (eight
+// threads a tensor); all are kept for the clipping.  A choice between accesses would wait for them, so that of the types
+// comes after them.
 __global__ __launch_bounds__(1024) void k_little(Table t, int clip, float* norm, float max_norm, float eps) {
+    typedef Loose<2>::four loose;
     __shared__ double red[16];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int first = lane < t.n ? (int)t.first[lane] : INT32_MAX;
+    const int mine = min((int)threadIdx.x >> 3, kTable - 1);
+    int type = t.dtype[mine];
+    int64_t size = t.size[mine], from = (int64_t)t.in[mine];
+    asm volatile("" : "+v"(first), "+v"(type), "+v"(size), "+v"(from));  // are there before the reads below, which are not to be waited for
+    words4 run[kMine][2] = {};
+    // body(tensor, first byte, bytes of the chunk, its runs)
     const auto each = [&](auto&& body) {
-        for (int k = wave; k < (int)t.chunks; k += 16) {
-            const int i = find(t, k);
-            const int64_t lo = (k - t.first[i]) * kLittleChunk, n = min(kLittleChunk, t.size[i] - lo);
-            typed(t.dtype[i], [&](auto z) { body(z, i, lo, n); });
+#pragma unroll
+        for (int k = 0; k < kMine; ++k) {
+            const int chunk = wave + 16 * k;
+            if (chunk < t.chunks) {
+                const int i = __popcll(__ballot(first <= chunk)) - 1;
+                const int64_t lo = (chunk - t.first[i]) * kLittleChunk, all = t.size[i] << (t.dtype[i] == CCDPP_F32 ? 2 : 1);
+                body(i, lo, (int)min(kLittleChunk, all - lo), run[k]);
+            }
         }
     };
-    double s = 0.0;
-    each([&](auto z, int i, int64_t lo, int64_t n) { s += chunk_squares<decltype(z)>(t.in[i], lo, n, lane, 64); });
+    each([&](int i, int64_t lo, int n, words4* q) {
+        const char* const g = (const char*)t.in[i] + lo;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+            if (j * 1024 + lane * 16 + 16 <= n) q[j] = *(const loose*)(g + j * 1024 + lane * 16);
+    });
+    const int per = type == CCDPP_F32 ? 4 : 8;
+    const int64_t at = size / per * per + (threadIdx.x & 7);
+    const bool has = (int)threadIdx.x >> 3 < t.n && at < size;
+    float over = 0.f;
+    if (has) typed(type, [&](auto z) { over = (float)((const decltype(z)*)from)[at]; });
+    double s = (double)over * (double)over;
+    each([&](int i, int64_t, int, words4* q) {
+        typed(t.dtype[i], [&](auto z) {
+            typedef decltype(z) T;
+            constexpr int W = 16 / sizeof(T);
+#pragma unroll
+            for (int j = 0; j < 2 * W; ++j) {
+                const float v = (float)__builtin_bit_cast(Run<T, W>, q[j / W]).v[j % W];
+                s += (double)v * (double)v;
+            }
+        });
+    });
     const float nv = (float)sqrt(block_sum(s, red));
     if (threadIdx.x == 0) *norm = nv;
     if (!clip) return;
     const float c = clip_factor(nv, max_norm, eps);
-    each([&](auto z, int i, int64_t lo, int64_t n) {
-        if (c != 1.f || t.out[i] != t.in[i]) chunk_scale<decltype(z)>(t.in[i], t.out[i], lo, n, c, lane, 64);
+    const auto as_it_is = [&](int i) { return c == 1.f && t.out[i] == t.in[i]; };
+    each([&](int i, int64_t lo, int n, words4* q) {
+        if (as_it_is(i)) return;
+        char* const o = (char*)t.out[i] + lo;
+        typed(t.dtype[i], [&](auto z) {
+            typedef decltype(z) T;
+            constexpr int W = 16 / sizeof(T);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                Run<T, W> r = __builtin_bit_cast(Run<T, W>, q[j]);
+#pragma unroll
+                for (int w = 0; w < W; ++w) r.v[w] = (T)((float)r.v[w] * c);
+                if (j * 1024 + lane * 16 + 16 <= n) store_run<W>((T*)(o + j * 1024 + lane * 16), r);
+            }
+        });
     });
+    if (has && !as_it_is(mine)) typed(type, [&](auto z) { ((decltype(z)*)t.out[mine])[at] = (decltype(z))(over * c); });
 }
+
+int64_t size_of(int32_t dtype) { return dtype == CCDPP_F32 ? 4 : 2; }
+
+// Chunks of whole runs of 16 bytes.
+int64_t little_chunks(int64_t size, int32_t dtype) { return (size * size_of(dtype) / 16 * 16 + kLittleChunk - 1) / kLittleChunk; }
 
 int run(bool clip, int32_t n, const void* const* in, void* const* out, const int64_t* sizes, const int32_t* dtypes, float max_norm, float eps,
         float* norm, void* ws, int64_t ws_bytes, void* stream) {
@@ -161,7 +217,7 @@ int run(bool clip, int32_t n, const void* const* in, void* const* out, const int
         if (sizes[i] < 0) return fail(CCDPP_EINVAL, "a tensor's size is negative");
         if (dtypes[i] < CCDPP_F32 || dtypes[i] > CCDPP_F16) return fail(CCDPP_EINVAL, "dtypes must be CCDPP_F32, CCDPP_BF16 or CCDPP_F16");
         if (sizes[i] > 0 && (!in[i] || (clip && !out[i]))) return fail(CCDPP_EINVAL, "a tensor is NULL");
-        const uintptr_t es = dtypes[i] == CCDPP_F32 ? 4 : 2;
+        const uintptr_t es = size_of(dtypes[i]);
         if (sizes[i] > 0 && ((uintptr_t)in[i] % es || (clip && (uintptr_t)out[i] % es))) return fail(CCDPP_EINVAL, "a tensor is not aligned to its type");
     }
     if (!ws || (uintptr_t)ws % 256 || ws_bytes < kBlocks * 8) return fail(CCDPP_EINVAL, "the workspace is too small or not aligned to 256 bytes");
@@ -169,20 +225,19 @@ int run(bool clip, int32_t n, const void* const* in, void* const* out, const int
     hipStream_t st = (hipStream_t)stream;
     double* parts = (double*)ws;
     Table t;
-    int64_t values = 0;
     t.n = 0, t.chunks = 0;
-    int64_t chunk = kChunk;
+    bool little = false;
     const auto add = [&](int32_t i) {
         t.in[t.n] = in[i], t.out[t.n] = clip ? out[i] : nullptr;
-        t.size[t.n] = sizes[i], t.first[t.n] = t.chunks, t.dtype[t.n] = (uint8_t)dtypes[i];
-        t.chunks += (sizes[i] + chunk - 1) / chunk;
+        t.size[t.n] = sizes[i], t.first[t.n] = t.chunks, t.dtype[t.n] = dtypes[i];
+        t.chunks += little ? little_chunks(sizes[i], dtypes[i]) : (sizes[i] + kChunk - 1) / kChunk;
         ++t.n;
     };
-    int32_t filled = 0;
+    int64_t filled = 0, pieces = 0;
     for (int32_t i = 0; i < n; ++i)
-        if (sizes[i]) ++filled, values += sizes[i];
-    if (filled <= kTable && values <= kLittle) {
-        chunk = kLittleChunk;
+        if (sizes[i]) ++filled, pieces += little_chunks(sizes[i], dtypes[i]);
+    if (filled <= kTable && pieces <= 16 * kMine) {
+        little = true;
         for (int32_t i = 0; i < n; ++i)
             if (sizes[i]) add(i);
         k_little<<<1, 1024, 0, st>>>(t, clip, norm, max_norm, eps);

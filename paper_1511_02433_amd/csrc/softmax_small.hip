@@ -15,8 +15,7 @@
 namespace ccdops {
 
 int small_steps(int d) {
-    const int ks = (d + 15) / 16;
-    return ks <= 2 ? 2 : ks <= 4 ? ks : ks <= 6 ? 6 : 8;
+    return (d + 15) / 16;
 }
 
 namespace {
@@ -332,10 +331,13 @@ template <class P, int NPL>
 hipError_t launch_small_lse(int ksd, const SmallArgs& a, hipStream_t st) {
     const unsigned blocks = (unsigned)a.lse.blocks;
     switch (ksd) {
+        case 1: k_small_lse<P, NPL, 1><<<blocks, 256, 0, st>>>(a); break;
         case 2: k_small_lse<P, NPL, 2><<<blocks, 256, 0, st>>>(a); break;
         case 3: k_small_lse<P, NPL, 3><<<blocks, 256, 0, st>>>(a); break;
         case 4: k_small_lse<P, NPL, 4><<<blocks, 256, 0, st>>>(a); break;
+        case 5: k_small_lse<P, NPL, 5><<<blocks, 256, 0, st>>>(a); break;
         case 6: k_small_lse<P, NPL, 6><<<blocks, 256, 0, st>>>(a); break;
+        case 7: k_small_lse<P, NPL, 7><<<blocks, 256, 0, st>>>(a); break;
         default: k_small_lse<P, NPL, 8><<<blocks, 256, 0, st>>>(a); break;
     }
     return hipGetLastError();
@@ -346,10 +348,13 @@ hipError_t launch_small_grads(int ksd, const SmallArgs& a, hipStream_t st) {
     const unsigned blocks = (unsigned)(a.dx.blocks + a.de.blocks);
     if (!blocks) return hipSuccess;
     switch (ksd) {
+        case 1: k_small_grads<P, NPL, 1><<<blocks, 256, 0, st>>>(a); break;
         case 2: k_small_grads<P, NPL, 2><<<blocks, 256, 0, st>>>(a); break;
         case 3: k_small_grads<P, NPL, 3><<<blocks, 256, 0, st>>>(a); break;
         case 4: k_small_grads<P, NPL, 4><<<blocks, 256, 0, st>>>(a); break;
+        case 5: k_small_grads<P, NPL, 5><<<blocks, 256, 0, st>>>(a); break;
         case 6: k_small_grads<P, NPL, 6><<<blocks, 256, 0, st>>>(a); break;
+        case 7: k_small_grads<P, NPL, 7><<<blocks, 256, 0, st>>>(a); break;
         default: k_small_grads<P, NPL, 8><<<blocks, 256, 0, st>>>(a); break;
     }
     return hipGetLastError();
