@@ -4,10 +4,10 @@
  * ccdpp.h learns factors W (users) and H (items) from squared error.  The calls
  * here train and judge such factors, or any rows against any table, as a choice
  * among all items: the softmax cross entropy of rows x_t over a whole table
- * e_v with its gradients, without holding the t x v logits (those of up to 128
- * rows are kept between the passes over the table, and up to 64 MiB of partial
- * ones of small problems), and the global norm of many gradient tensors with their
- * clipping.
+ * e_v with its gradients, without holding the t x v logits (a training pass
+ * over many columns keeps up to 1 GiB of them for its gradients, and all calls
+ * those of up to 128 rows, or up to 64 MiB of partial ones of small problems),
+ * and the global norm of many gradient tensors with their clipping.
  *
  * Conventions for every call:
  *  - Array arguments are DEVICE memory on the current HIP device, owned by the

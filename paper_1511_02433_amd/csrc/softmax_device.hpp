@@ -16,7 +16,6 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kExcluded = -1e38f;  // offsets below this exclude an item
-constexpr int kParts = 256;          // partial maxima of k_scales per quantity
 constexpr int kBlk = 1024;           // bytes of one operand fragment
 
 // The 16-bit type that the matrix instructions read.

@@ -1,4 +1,4 @@
-// Softmax cross entropy of rows against a whole table, and its gradients, without keeping the logits (gfx950).
+// Softmax cross entropy of rows against a whole table, and its gradients, without keeping all logits (gfx950).
 //
 //   z_tv = s x_t.e_v + o_v     lse_t = log sum_v exp z_tv     loss_t = lse_t - z_{t,y_t}
 //   G_tv = g_t (exp(z_tv - lse_t) - [v = y_t])     dx = s G E     de = s G^T X
@@ -286,6 +286,8 @@ struct GemmArgs {
     const float* offset;
     const float* o2;             // offsets of A's rows in base 2, -inf for excluded and missing ones
     float2* part;                // [blocks of 256 table entries][t] (max, sum), base 2
+    float* kept;                 // logits of the first kept_tiles blocks of 32 entries [t/32][block][32 x 32, as in an accumulator]
+    int64_t kept_tiles;
     const void* target;
     int target_bits;
     const float *lse, *grad;
@@ -605,6 +607,20 @@ __global__ __launch_bounds__(kGemmThreads) void k_gemm(GemmArgs a) {
                     acc[i][j][r] = fmaf(acc[i][j][r], f[j], o[r >> 2][r & 3]);
                     top[j] = fmaxf(top[j], acc[i][j][r]);
                 }
+            if (tile >= a.kept_tiles) continue;
+#pragma unroll
+            for (int j = 0; j < kNf; ++j) {
+                const int64_t tt = (int64_t)bn * 8 + wn * kNf + j;
+                if (tt >= a.n_tiles) continue;
+                f32x4* const to = (f32x4*)(a.kept + (tt * a.kept_tiles + tile) * 1024) + lane;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    f32x4 four;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) four[r] = acc[i][j][4 * q + r];
+                    to[q * 64] = four;
+                }
+            }
         }
         __syncthreads();  // LDS is free
 #pragma unroll
@@ -701,23 +717,25 @@ __global__ __launch_bounds__(256) void k_join(JoinArgs a) {
     if (threadIdx.x == 0) a.part[blockIdx.x * a.t + t] = make_float2(top, red[0][1] + red[1][1] + red[2][1] + red[3][1]);
 }
 
-// The terms of 32 x 32 logits a wave.
+// The terms of 32 x 32 logits a wave: from rows (pitch), or from what k_gemm kept (pitch 0; v0 is the piece's first entry).
 template <class PG, int NPL>
 __global__ __launch_bounds__(256) void k_terms(GemmArgs a, const float* z, int64_t pitch) {
     const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
-    const int64_t vt = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), tt = blockIdx.y;
+    const uint32_t across = (uint32_t)((a.m_tiles + 3) / 4);
+    const int64_t vt = (int64_t)(blockIdx.x % across) * 4 + (threadIdx.x >> 6), tt = blockIdx.x / across;
     if (vt >= a.m_tiles) return;
-    const TermBlocks<PG, NPL> terms(lane);
-    TermRow row;
-    row.load(a, tt * 32 + n);
-    const float* const from = z + min(tt * 32 + n, a.t - 1) * pitch + vt * 32 + 4 * h;
+    const float* const from = pitch ? z + min(tt * 32 + n, a.t - 1) * pitch + vt * 32 + 4 * h : a.kept + (tt * a.kept_tiles + a.v0 / 32 + vt) * 1024 + lane * 4;
+    const int step = pitch ? 8 : 256;
     f32x16 q;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        const f32x4 four = *(const f32x4*)(from + 8 * k);
+        const f32x4 four = *(const f32x4*)(from + step * k);
 #pragma unroll
         for (int r = 0; r < 4; ++r) q[4 * k + r] = four[r];
     }
+    const TermBlocks<PG, NPL> terms(lane);
+    TermRow row;
+    row.load(a, tt * 32 + n);
     terms.put(a, vt, tt, lane, q, row);
 }
 
@@ -874,7 +892,8 @@ struct Plan {
     int64_t vc;              // table entries per piece of the gradients (a multiple of 256)
     int64_t dp;              // columns of partial sums
     int sx, se;              // splits of the two gradients' contractions
-    int sz;                  // shares of the logits' contraction; 1: logits are not kept
+    int sz;                  // shares of the logits' contraction; above 1 all logits are kept, in rows
+    int64_t kept = 0;        // table entries whose logits are kept for the gradients, in blocks (0, whole pieces or all)
     Shares lse, dx, de;      // (small)
     int64_t x_tile, xlive_tile, e_tile;  // bundles (small)
     // offsets into the workspace
@@ -886,6 +905,14 @@ struct Plan {
 };
 
 constexpr int64_t kPieceBytes = int64_t(512) << 20;  // of G (8192 x 131072 x 4096: 1.5% over 128 MiB)
+
+
+// A training pass may keep logits between its two halves, in kKeptBytes at most, whatever t and v are.  Written and read
+// they cost 8 bytes an entry, computed again a product over the factors: the first is less from some 384 columns on in 32
+// bits and 1,024 in 16 (2,000 x 32,003 rows, computed again or kept: 256 floats 529 and 549 us, 512 floats 789 and 729, 1,024
+// floats 1,401 and 1,207; 512 halves 390 and 424, 1,024 halves 603 and 577, 4,096 halves 2,020 and 1,679).
+constexpr int64_t kKeptBytes = int64_t(1) << 30;
+constexpr int keep_from(int planes) { return planes == 2 ? 384 : 1024; }
 
 Plan make_plan(const ccdpp_softmax_t& p, int call) {
     Plan w;
@@ -972,7 +999,11 @@ Plan make_plan(const ccdpp_softmax_t& p, int call) {
             if (steps / n + 5 + n * kept < best) best = steps / n + 5 + n * kept, w.sz = n;
     }
     if (!w.direct) {
-        w.o_z = take(w.sz > 1 ? w.sz * p.t * w.vt * 32 * 4 : 0);
+        if (w.sz == 1 && w.forward && w.grads && p.d >= keep_from(w.planes)) {
+            const int64_t fit = kKeptBytes / (w.tt * 32 * 4);
+            w.kept = fit >= w.vt * 32 ? w.vt * 32 : fit / w.vc * w.vc;
+        }
+        w.o_z = take(w.sz > 1 ? w.sz * p.t * w.vt * 32 * 4 : w.kept * w.tt * 32 * 4);
         w.o_xf = take(w.planes * w.tt * w.ksd * kBlk);
         w.o_ef = take(w.planes * w.vt * w.ksd * kBlk);
     }
@@ -1106,6 +1137,7 @@ int run_wide(const ccdpp_softmax_t& p, const Plan& w, const Outs& out, const int
         OPS_LAUNCH("logits");
     } else if (w.forward) {
         z.part = (float2*)(ws + w.o_part);
+        z.kept = kept, z.kept_tiles = w.kept / 32;
         k_gemm<P, PG, NPL, EPI_LSE, T><<<blocks, kGemmThreads, 0, st>>>(z);
         OPS_LAUNCH("logits");
     }
@@ -1121,7 +1153,9 @@ int run_wide(const ccdpp_softmax_t& p, const Plan& w, const Outs& out, const int
         GemmArgs q = z;
         q.v0 = v0, q.a = z.a + v0 / 32 * z.a_tile, q.o2 = z.o2 + v0, q.m_tiles = nt;
         q.ksv = nt * 2, q.g_plane = w.tt * q.ksv * kBlk, q.gt_plane = nt * w.kst * kBlk;
-        if (w.sz > 1 || w.direct) k_terms<PG, NPL><<<dim3((unsigned)((nt + 3) / 4), (unsigned)w.tt), 256, 0, st>>>(q, kept + v0, pitch);
+        const unsigned tiles = (unsigned)((nt + 3) / 4 * w.tt);
+        if (w.sz > 1 || w.direct) k_terms<PG, NPL><<<tiles, 256, 0, st>>>(q, kept + v0, pitch);
+        else if (v0 < w.kept) k_terms<PG, NPL><<<tiles, 256, 0, st>>>(q, nullptr, 0);
         else k_gemm<P, PG, NPL, EPI_G, T><<<(unsigned)((nt + 7) / 8 * ((w.tt + 7) / 8)), kGemmThreads, 0, st>>>(q);
         OPS_LAUNCH("G");
         GemmArgs o = {};

@@ -248,3 +248,28 @@ def test_graphs_of_other_ways_replay(t, v, d, dtype):
         assert all(torch.equal(a, b) for a, b in zip(got, want)), k
         assert bool(torch.isfinite(norm))
         _ = (x.float() @ x.float().t()).sum().item()
+
+
+@pytest.mark.parametrize("t,v,d,dtype", [(300, 40_001, 400, "f32"), (33, 290_000, 390, "f16"), (1500, 9_999, 1030, "bf16"), (1500, 9_999, 1030, "f16"),
+                                         (8300, 33_100, 388, "f32")])
+def test_logits_kept_for_the_gradients(t, v, d, dtype):
+    """All of them, or those of the first pieces (8,300 rows of 32 bits: 16,128 entries a piece, two pieces).  They are the
+    logits that a call of its own computes again, so the gradients are the same, bit for bit."""
+    x, e, y, g = make(t, v, d, dtype, seed=d)
+    offset = torch.zeros(v, device="cuda")
+    offset[::7] = -0.5
+    offset[1::1001] = float("-inf")
+    y[t // 2] = -1
+    y[3] = 1  # excluded
+    loss, lse, dx, de = ops().softmax_loss_train(x, e, y, grad=g, offset=offset)
+    l2, s2 = ops().softmax_loss(x, e, y, offset=offset)
+    dx2, de2 = ops().softmax_loss_grad(x, e, y, lse, grad=g, offset=offset)
+    assert torch.equal(loss, l2) and torch.equal(lse, s2) and torch.equal(dx, dx2) and torch.equal(de, de2)
+    only = ops().softmax_loss_train(x, e, y, grad=g, offset=offset, need=("table",))
+    assert only[2] is None and torch.equal(only[3], de)
+    without = (y >= 0) & torch.isinf(offset[y.clamp(min=0)])  # rows whose target is excluded: the plain form ignores them
+    assert bool(without[3]) and bool(torch.isposinf(loss[without]).all())
+    assert float(dx[without].abs().max()) == 0 and float(de[1::1001].abs().max()) == 0
+    keep = torch.where(without, torch.full_like(y, -1), y)
+    loss = torch.where(without, torch.zeros_like(loss), loss)
+    check((loss, lse, dx, de), plain(x, e, keep, g, offset=offset), dtype)
