@@ -143,7 +143,13 @@ struct Shares {
     int64_t blocks;  // shares
     __host__ __device__ int64_t first(int64_t kept) const { return kept * tiles / len; }
     __host__ __device__ int count(int64_t kept) const { return (int)(((kept + 1) * tiles - 1) / len - first(kept) + 1); }
+    __host__ __device__ bool whole() const { return len > 0 && tiles > 0 && len % tiles == 0; }  // a share per kept block
     __host__ __device__ int64_t most() const { return tiles > 0 ? (tiles + len - 2) / len + 1 : 0; }  // of count()
+};
+
+struct SmallOut {
+    void* to;     // a gradient
+    int64_t ld;
 };
 
 struct SmallArgs {
@@ -155,6 +161,10 @@ struct SmallArgs {
     Shares lse, dx, de;                 // dx.blocks or de.blocks 0: not asked for
     float2* part;                       // [share of the kept block][t]
     float *dxp, *dep;                   // [share of the kept block][rows, in tiles][d, in blocks of 32]
+    SmallOut dx_out, de_out;            // of kept blocks that have one share
+    int d, scaled;                      // scaled: fin holds exponents of x and the table
+    const int32_t* fin;                 // or NULL
+    float scale;
 };
 
 // ksd: steps of 16 over d that the kernels were built for (small_steps).  Return launch errors.

@@ -855,6 +855,7 @@ __global__ __launch_bounds__(256) void k_finish(FinishSide x, FinishSide e, int6
         const float* from = a.part + r * a.ldp + c;
         f32x4 v = {};
         const int splits = a.shares.len ? a.shares.count(r / 128) : a.splits;
+        if (a.shares.len && splits == 1) continue;  // is there
         int s = 0;
         for (; s + 8 <= splits; s += 8) {  // eight reads in flight
             f32x4 q[8];
@@ -954,6 +955,7 @@ Plan make_plan(const ccdpp_softmax_t& p, int call) {
         const auto shares = [](int64_t kept_tiles, int64_t tiles, int64_t want) {
             const int64_t total = (kept_tiles + 3) / 4 * tiles;
             Shares s = {tiles, std::max<int64_t>((total + want - 1) / want, std::min<int64_t>(tiles, 4)), 0};
+            if (s.len >= 8 * tiles) s.len = round_up(s.len, tiles);  // whole blocks: no partial sums, for an eighth more at most
             s.blocks = total ? (total + s.len - 1) / s.len : 0;
             return s;
         };
@@ -1040,7 +1042,7 @@ int launch_loss(const ccdpp_softmax_t& p, const float2* part, int64_t pieces, co
 template <class T>
 int finish(const FinishSide& x, const FinishSide& e, int cols, float scale, const int32_t* fin, hipStream_t st) {
     const int64_t quads = (cols + 3) / 4;
-    const auto blocks = [&](const FinishSide& a) { return a.out ? std::min<int64_t>((a.rows * quads + 255) / 256, 1 << 16) : 0; };
+    const auto blocks = [&](const FinishSide& a) { return a.out && !a.shares.whole() ? std::min<int64_t>((a.rows * quads + 255) / 256, 1 << 16) : 0; };
     const int64_t bx = blocks(x), be = blocks(e);
     if (bx + be == 0) return CCDPP_OK;
     k_finish<T><<<(unsigned)(bx + be), 256, 0, st>>>(x, e, bx, cols, scale, fin);
@@ -1091,6 +1093,8 @@ int run_small(const ccdpp_softmax_t& p, const Plan& w, const Outs& o, const int3
     if (!o.de) a.de.blocks = 0;
     a.part = (float2*)(ws + w.o_part);
     a.dxp = (float*)(ws + w.o_dx), a.dep = (float*)(ws + w.o_de);
+    a.dx_out = {o.dx, o.lddx}, a.de_out = {o.de, o.ldde};
+    a.d = p.d, a.scaled = w.scaled, a.fin = fin, a.scale = p.scale;
     RowNumbers num = {};
     if (w.grads) num.first = ws + w.o_xl + NPL * w.ksd * kBlk, num.step = w.xlive_tile, num.grad = o.grad, num.fin = fin;
     if (w.forward) {

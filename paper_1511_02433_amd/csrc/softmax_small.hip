@@ -5,7 +5,7 @@
 // streamed ones: sums over the streamed side are sums within a lane, and the terms G of the gradients are, as they
 // stand, the other operand of the product with the turned streamed rows.  Nothing of the size of the logits is
 // written.  The streamed side is cut into shares so that there are blocks for all CUs; shares leave partial sums that
-// k_loss and k_small_finish add in order.
+// k_loss and k_finish add in order; a kept block whose streamed side is in one share is written as a result.
 //
 // Per tile and wave the matrix cores need 32 cycles a product, 3 (d / 16) + 6 (d / 32) of them for 32-bit values, the
 // vector units 16 values of some 5 instructions and an exponential (and the split into two halves): at d = 100 the
@@ -287,6 +287,10 @@ __device__ __forceinline__ void small_terms(const SmallArgs& a, int64_t tile, in
     });
 }
 
+// What the sums are multiplied with, one after the other: G's power of two is taken off, and the other operand's.
+__device__ __forceinline__ float small_terms_factor(const SmallArgs& a, bool items) { return items ? (a.fin ? ldexpf(1.f, -a.fin[2]) : 1.f) : ldexpf(1.f, -kTermExp); }
+__device__ __forceinline__ float small_factor(const SmallArgs& a, bool items) { return a.scaled ? ldexpf(a.scale, -a.fin[items ? 1 : 0]) : a.scale; }
+
 template <class P, int NPL, int KS, bool ITEMS>
 __device__ __forceinline__ void small_grad(const SmallArgs& a, int64_t share, char* lds) {
     typedef Stream<P, NPL, KS, true> S;
@@ -303,6 +307,25 @@ __device__ __forceinline__ void small_grad(const SmallArgs& a, int64_t share, ch
         small_terms<P, NPL, KS, ITEMS>(a, tile, first, last, kept, own, lds, out);
         if (at >= tiles) return;
         const float w = ITEMS ? 1.f : own[kNumRaw * 32];
+        const SmallOut& o = ITEMS ? a.de_out : a.dx_out;
+        if (first == 0 && last == (ITEMS ? a.de : a.dx).tiles) {  // nothing to add: the result itself
+            typedef typename std::conditional<NPL == 2, float, typename P::elem>::type T;
+            const int64_t row = tile * 32 + n;
+            if (row >= (ITEMS ? a.v : a.t)) return;
+            const float fg = small_terms_factor(a, ITEMS), f = small_factor(a, ITEMS);
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    Run<T, 4> v;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) v.v[r] = (T)(out[d][q * 4 + r] * w * fg * f);
+                    T* const at = (T*)o.to + row * o.ld + 4 * h;
+                    if (d < DT - 1) store_run<4>(at + d * 32 + q * 8, v);  // columns that there are
+                    else store_tail<4>(at, d * 32 + q * 8, a.d - 4 * h, v);
+                }
+            return;
+        }
         float* const to = (ITEMS ? a.dep : a.dxp) + ((place * tiles + tile) * 32 + n) * (DT * 32) + 4 * h;
 #pragma unroll
         for (int d = 0; d < DT; ++d)
