@@ -60,7 +60,7 @@ enum ccdpp_dtype {
  *              excluded has loss +inf and is left out of the gradients.  Where
  *              every item is excluded, lse is -inf and probabilities are 0.
  * Products of 16-bit values are exact and summed in 32 bits.  32-bit values are
- * multiplied as they are for t <= 16 (for the logits also t <= 128 where d > 128), and as
+ * multiplied as they are for t <= 32 (for the logits also t <= 128 where d > 128), and as
  * sums of two halves with 11 bits each and a common exponent otherwise: 22
  * bits of the largest value of a row of x, or of the table.  A probability's relative error is
  * some 5e-7 (1 + |z|), what a logit and its lse have in 32 bits.
@@ -100,7 +100,7 @@ int ccdpp_softmax_loss(const ccdpp_softmax_t *p, float *loss, float *lse, void *
  *   dx, lddx      : t rows of d values of p->dtype, lddx >= d values apart; may be NULL
  *   dtable, lddt  : v rows likewise; may be NULL
  * Sums are held in 32 bits and rounded once to p->dtype; the terms G_tv have 11 bits
- * at least (22 for 32-bit types, and for 16-bit ones with d <= 128 or t <= 16, 16 at least). */
+ * at least (22 for 32-bit types, and for 16-bit ones with d <= 128 or t <= 32, 16 at least). */
 int ccdpp_softmax_loss_grad(const ccdpp_softmax_t *p, const float *lse, const float *grad,
                             void *dx, int64_t lddx, void *dtable, int64_t lddt,
                             void *workspace, int64_t workspace_bytes, void *stream);

@@ -132,6 +132,8 @@ enum {
 };
 constexpr int kTermExp = 13;  // of dx's terms, which leave the row's weight to the end: at most 2^13 each
 
+// Up to here the kernels of few factors; above it the products of k_gemm.  Loss and gradients of 1,024 x 20,000 rows,
+// this way and by k_gemm: 100 floats 114 and 174 us, 128 floats 122 and 191, 128 in bfloat16 75 and 132.
 constexpr int kSmallD = 128;
 
 // A product of few factors is cut by tiles: kept blocks of 128 rows times streamed tiles of 32, in that order, in shares
@@ -176,8 +178,13 @@ template <class P, int NPL> hipError_t launch_small_lse(int ksd, const SmallArgs
 template <class P, int NPL> hipError_t launch_small_grads(int ksd, const SmallArgs& a, hipStream_t st);
 
 // ---- few rows --------------------------------------------------------------------------------
-constexpr int kDirectT = 128;  // rows whose logits are computed from the table as it lies
-constexpr int kFewT = 16;      // rows whose gradients are, too
+// Rows whose logits are computed from the table as it lies.  The loss of 200,000 entries, this way and by k_gemm from a
+// packed table: 64 x 256 floats 88 and 217 us, 128 x 256 floats 182 and 219, 128 x 1,024 in bfloat16 195 and 296: the time
+// of the former grows with the rows, that of packing the table does not.
+constexpr int kDirectT = 128;
+// Rows whose gradients are, too.  Loss and gradients of 200,000 x 256, this way and the other: 16 rows of floats 136 and 399
+// us, 32 rows 177 and 415, 32 in bfloat16 107 and 217; more rows do not fit the registers of two blocks on a CU.
+constexpr int kFewT = 32;
 
 struct FewArgs {
     int t, d, dp;             // dp: columns of partial sums, a multiple of 4

@@ -1,4 +1,4 @@
-// Softmax loss of few rows (t <= 128) and gradients of very few (t <= 16): a request, a handful of tokens, a small
+// Softmax loss of few rows (t <= 128) and gradients of very few (t <= 32): a request, a handful of tokens, a small
 // evaluation (gfx950).
 //
 // Bound by reading the table, once for the logits and, for gradients, once more, and by writing its gradient: nothing is
@@ -7,11 +7,14 @@
 // k_direct_logits: a wave takes 16 table rows (or twice that) against all rows of x.  Each lane reads 16 bytes of its table
 // row at a time, 64 bytes a row and step, straight into the operand of 16 x 16 products: of 16-bit values 32 columns a
 // step, of 32-bit ones 16 columns in four v_mfma_f32_16x16x4_f32, with exact products.  Any order of the columns will do
-// as long as x, which comes from LDS, has the same.  Where table rows are few, waves share their columns.
+// as long as x, which comes from LDS, has the same.  Where table rows are few, waves share their columns.  (5 x 131,072 x
+// 4,096 in bfloat16: 212 us, 5.1 TB/s, what a copy of that size reaches.)
 //
 // k_few_grads: 16 table rows and 16 rows of x at a time (v_mfma_f32_16x16x4_f32, or 16x16x16 for 16-bit types): the
 // table's values are the operand of dx as they are read, x's are kept in registers for dtable, and the terms G stay in 32
-// bits, or two 16-bit planes.  A row's values go to and from 16 lanes by 16 bytes.
+// bits, or two 16-bit planes.  A row's values go to and from 16 lanes by 16 bytes.  Blocks share the table's rows evenly,
+// as many blocks as run at once.  (16 x 618,991: 192 floats 188 us, 5.1 TB/s of table and gradient; 384 in bfloat16 272 us,
+// 3.5 TB/s: rows whose length is no multiple of 16 bytes, and the 16-bit kernel's registers, cost the rest.)
 #include <algorithm>
 
 #include "softmax_device.hpp"
@@ -192,15 +195,15 @@ __global__ __launch_bounds__(kWaves * 64) void k_direct_logits(FewArgs a) {
     }
 }
 
-// What the terms of up to 16 rows take, in LDS.
+// What the terms of the rows take, in LDS.
 struct FewRows {
-    float w[16], l2[16];  // weight (times scale), lse in base 2; 0 and +inf in rows that do not count
-    int y[16];            // target, or -1
+    float w[kFewT], l2[kFewT];  // weight (times scale), lse in base 2; 0 and +inf in rows that do not count
+    int y[kFewT];               // target, or -1
 };
 
 // By the whole block; returns the largest finite |weight|.
 __device__ __forceinline__ float few_rows(const FewArgs& a, FewRows& rows) {
-    const int t = threadIdx.x & 15;
+    const int t = threadIdx.x & (kFewT - 1);
     float w = 0.f, l2 = INFINITY;
     int y = -1;
     if (t < a.t) {
@@ -211,22 +214,22 @@ __device__ __forceinline__ float few_rows(const FewArgs& a, FewRows& rows) {
             y = yt < a.v ? (int)yt : -1;
         }
     }
-    if (threadIdx.x < 16) rows.w[t] = w, rows.l2[t] = l2, rows.y[t] = y;
+    if (threadIdx.x < kFewT) rows.w[t] = w, rows.l2[t] = l2, rows.y[t] = y;
     return wave_max(finite(w) ? fabsf(w) : 0.f);
 }
 
 // The terms of table rows b .. b + n - 1 (128 at most) by 256 threads: a thread has one table row and every other row of x,
-// its logits' reads all in flight.  put(table row, row of x, term); keep(table row, whether the item counts).
-template <class F, class K>
+// its logits' reads all in flight.  G: 16 rows of x each.  put(table row, row of x, term); keep(table row, whether the item counts).
+template <int G, class F, class K>
 __device__ __forceinline__ void few_terms(const FewArgs& a, const FewRows& rows, int64_t b, int n, float up, float up2, F&& put, K&& keep) {
     const int r = threadIdx.x & (kBatch - 1), t0 = threadIdx.x / kBatch;
     const int64_t v = b + min(r, n - 1);
-    float z[8];
+    float z[8 * G];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) z[k] = a.z[min(t0 + 2 * k, a.t - 1) * a.z_row + v];
+    for (int k = 0; k < 8 * G; ++k) z[k] = a.z[min(t0 + 2 * k, a.t - 1) * a.z_row + v];
     if (t0 == 0) keep(r, r < n && !(a.offset && a.offset[v] < kExcluded));
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < 8 * G; ++k) {
         const int t = t0 + 2 * k;
         const float w = rows.w[t] * up * up2;
         float g = w * (exp2_fast(z[k] - rows.l2[t]) - (rows.y[t] == v ? 1.f : 0.f));
@@ -237,24 +240,25 @@ __device__ __forceinline__ void few_terms(const FewArgs& a, const FewRows& rows,
 
 // Waves that took different rows are added in order; a block leaves one partial sum of dx.
 template <int C>
-__device__ __forceinline__ void add_waves(const FewArgs& a, const float (*red)[16 * 16 * C]) {
+__device__ __forceinline__ void add_waves(const FewArgs& a, const float (*red)[16 * 16 * C], int first) {  // rows of x from `first` on
     const int across = a.across, down = 4 / across;
     __syncthreads();
-    for (int i = threadIdx.x; i < a.t * across * 16 * C; i += 256) {
+    for (int i = threadIdx.x; i < min(16, a.t - first) * across * 16 * C; i += 256) {
         const int t = i / (across * 16 * C), k = i - t * across * 16 * C, w = k / (16 * C), col = blockIdx.x * across * 16 * C + k;
         if (col >= a.dp) continue;
         float s = 0.f;
         for (int y = 0; y < down; ++y) s += red[y * across + w][t * 16 * C + (k - w * 16 * C)];
-        a.dxp[((int64_t)blockIdx.y * a.t + t) * a.dp + col] = s;
+        a.dxp[((int64_t)blockIdx.y * a.t + first + t) * a.dp + col] = s;
     }
 }
 
-template <class T>
-__global__ __launch_bounds__(256, 3) void k_few_grads(FewArgs a) {
+// G: 16 rows of x each.
+template <class T, int G>
+__global__ __launch_bounds__(256, G == 1 ? 3 : 2) void k_few_grads(FewArgs a) {
     constexpr int C = 16 / sizeof(T);  // columns of a lane: 16 C of them are beside each other
     typedef Run<T, C> Piece;
     __shared__ FewRows info;
-    __shared__ float terms[kBatch][17];
+    __shared__ float terms[kBatch][16 * G + 1];
     __shared__ float keep[kBatch];
     __shared__ __align__(16) float red[4][16 * 16 * C];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, q = lane >> 4;
@@ -263,9 +267,9 @@ __global__ __launch_bounds__(256, 3) void k_few_grads(FewArgs a) {
     const bool idle = c - n * C >= a.d;  // the wave's columns are past the row
     const int64_t r0 = a.v * blockIdx.y / gridDim.y, r1 = a.v * (blockIdx.y + 1) / gridDim.y;
     // x as the operand of dtable: rows 4 j + q, zero where they do not count
-    float x[4][C];
+    float x[4 * G][C];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < 4 * G; ++j) {
         const int t = 4 * j + q;
         Piece row = {};
         if (a.de && t < a.t && row_counts(load_target(a.target, a.target_bits, t), a.v, a.offset))
@@ -274,12 +278,12 @@ __global__ __launch_bounds__(256, 3) void k_few_grads(FewArgs a) {
         for (int i = 0; i < C; ++i) x[j][i] = (float)row.v[i];
     }
     few_rows(a, info);
-    f32x4 dx[C] = {};
+    f32x4 dx[G][C] = {};
     const auto read = [&](int64_t row, Piece& e) { e = load_tail<C>((const T*)a.table + row * a.ldt, c, a.d, (a.v - 1 - row) * a.ldt + a.d); };
     for (int64_t b = r0; b < r1; b += kBatch) {
         const int rows = (int)min((int64_t)kBatch, r1 - b);
         __syncthreads();
-        few_terms(a, info, b, rows, 1.f, 1.f, [&](int r, int t, float g) { terms[r][t] = g; },
+        few_terms<G>(a, info, b, rows, 1.f, 1.f, [&](int r, int t, float g) { terms[r][t] = g; },
                   [&](int r, bool counts) { keep[r] = counts ? 1.f : 0.f; });
         __syncthreads();
         const int tiles = idle ? 0 : (rows + 15) / 16;
@@ -299,11 +303,14 @@ __global__ __launch_bounds__(256, 3) void k_few_grads(FewArgs a) {
             for (int j = 0; j < 4; ++j) {
                 const int row = i * 16 + 4 * j + q;
                 const bool k = keep[row] != 0.f;
-                const float gx = terms[row][n], ge = terms[i * 16 + n][4 * j + q];
 #pragma unroll
-                for (int l = 0; l < C; ++l) {
-                    dx[l] = __builtin_amdgcn_mfma_f32_16x16x4f32(gx, k ? (float)e[j].v[l] : 0.f, dx[l], 0, 0, 0);
-                    de[l] = __builtin_amdgcn_mfma_f32_16x16x4f32(ge, x[j][l], de[l], 0, 0, 0);
+                for (int g = 0; g < G; ++g) {
+                    const float gx = terms[row][16 * g + n], ge = terms[i * 16 + n][16 * g + 4 * j + q];
+#pragma unroll
+                    for (int l = 0; l < C; ++l) {
+                        dx[g][l] = __builtin_amdgcn_mfma_f32_16x16x4f32(gx, k ? (float)e[j].v[l] : 0.f, dx[g][l], 0, 0, 0);
+                        de[l] = __builtin_amdgcn_mfma_f32_16x16x4f32(ge, x[4 * g + j][l], de[l], 0, 0, 0);
+                    }
                 }
             }
             if (!a.de) continue;
@@ -320,10 +327,14 @@ __global__ __launch_bounds__(256, 3) void k_few_grads(FewArgs a) {
     }
     if (!a.dxp) return;
 #pragma unroll
-    for (int l = 0; l < C; ++l)
+    for (int g = 0; g < G; ++g) {
+        if (g) __syncthreads();
 #pragma unroll
-        for (int r = 0; r < 4; ++r) red[wave][(4 * q + r) * 16 * C + n * C + l] = dx[l][r];
-    add_waves<C>(a, red);
+        for (int l = 0; l < C; ++l)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) red[wave][(4 * q + r) * 16 * C + n * C + l] = dx[g][l][r];
+        add_waves<C>(a, red, 16 * g);
+    }
 }
 
 // 16-bit types: the same with v_mfma_f32_16x16x16 on the values as they are; the terms, by a power of two below 2^13, are
@@ -341,13 +352,13 @@ template <> struct Half<__bf16> {
     }
 };
 
-template <class T>
-__global__ __launch_bounds__(256, 3) void k_few_grads16(FewArgs a) {
+template <class T, int G>
+__global__ __launch_bounds__(256, G == 1 ? 3 : 2) void k_few_grads16(FewArgs a) {
     constexpr int C = 8;
     typedef Run<T, C> Piece;
     typedef typename Half<T>::vec V;
-    __shared__ __align__(16) T by_row[2][kBatch][20];      // [plane][table row][row of x], pitch against bank conflicts
-    __shared__ __align__(16) T by_x[2][16][kBatch + 8];    // [plane][row of x][table row]
+    __shared__ __align__(16) T by_row[2][kBatch][16 * G + 4];  // [plane][table row][row of x], pitch against bank conflicts
+    __shared__ __align__(16) T by_x[2][16 * G][kBatch + 8];    // [plane][row of x][table row]
     __shared__ FewRows info;
     __shared__ uint16_t keep[kBatch];
     __shared__ __align__(16) float red[4][16 * 16 * C];
@@ -359,17 +370,17 @@ __global__ __launch_bounds__(256, 3) void k_few_grads16(FewArgs a) {
     const float most = few_rows(a, info);
     const int e2 = scale_exp(most) - 2;
     const float up = ldexpf(1.f, e2 / 2), up2 = ldexpf(1.f, e2 - e2 / 2), back = ldexpf(1.f, -(e2 / 2)), back2 = ldexpf(1.f, -(e2 - e2 / 2));
-    V x[C];  // the operand of dtable: rows 4 q + i, zero where they do not count
+    V x[G][C];  // the operand of dtable: rows 4 q + i of each 16, zero where they do not count
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int t = 4 * q + i;
+    for (int k = 0; k < 4 * G; ++k) {
+        const int g = k / 4, i = k % 4, t = 16 * g + 4 * q + i;
         Piece row = {};
         if (a.de && t < a.t && row_counts(load_target(a.target, a.target_bits, t), a.v, a.offset))
             row = load_tail<C>((const T*)a.x + t * a.ldx, c, a.d, (a.t - 1 - t) * a.ldx + a.d);
 #pragma unroll
-        for (int l = 0; l < C; ++l) x[l][i] = row.v[l];
+        for (int l = 0; l < C; ++l) x[g][l][i] = row.v[l];
     }
-    f32x4 dx[C] = {};
+    f32x4 dx[G][C] = {};
     const auto read = [&](int64_t row, Piece& e) { e = load_tail<C>((const T*)a.table + row * a.ldt, c, a.d, (a.v - 1 - row) * a.ldt + a.d); };
     for (int64_t b = r0; b < r1; b += kBatch) {
         const int rows = (int)min((int64_t)kBatch, r1 - b);
@@ -379,7 +390,7 @@ __global__ __launch_bounds__(256, 3) void k_few_grads16(FewArgs a) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) read(b + min(wy * 16 + 4 * q + j, rows - 1), next[j]);
         __syncthreads();
-        few_terms(a, info, b, rows, up, up2,
+        few_terms<G>(a, info, b, rows, up, up2,
                   [&](int r, int t, float g) {
                       const T hi = (T)g, lo = finite((float)hi) ? (T)(g - (float)hi) : (T)0.f;
                       by_row[0][r][t] = hi, by_row[1][r][t] = lo;
@@ -397,12 +408,14 @@ __global__ __launch_bounds__(256, 3) void k_few_grads16(FewArgs a) {
             uint16_t k[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) k[j] = keep[i * 16 + 4 * q + j];
-            V gx[2], ge[2];
+            V gx[G][2], ge[G][2];
 #pragma unroll
-            for (int p = 0; p < 2; ++p) {
-                gx[p] = *(const V*)&by_x[p][n][i * 16 + 4 * q];
-                ge[p] = *(const V*)&by_row[p][i * 16 + n][4 * q];
-            }
+            for (int g = 0; g < G; ++g)
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    gx[g][p] = *(const V*)&by_x[p][16 * g + n][i * 16 + 4 * q];
+                    ge[g][p] = *(const V*)&by_row[p][i * 16 + n][16 * g + 4 * q];
+                }
             f32x4 de[C] = {};
 #pragma unroll
             for (int l = 0; l < C; ++l) {
@@ -410,10 +423,12 @@ __global__ __launch_bounds__(256, 3) void k_few_grads16(FewArgs a) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) v[j] = __builtin_bit_cast(T, (uint16_t)(__builtin_bit_cast(uint16_t, e[j].v[l]) & k[j]));
 #pragma unroll
-                for (int p = 0; p < 2; ++p) {
-                    dx[l] = Half<T>::mfma(gx[p], v, dx[l]);
-                    de[l] = Half<T>::mfma(ge[p], x[l], de[l]);
-                }
+                for (int g = 0; g < G; ++g)
+#pragma unroll
+                    for (int p = 0; p < 2; ++p) {
+                        dx[g][l] = Half<T>::mfma(gx[g][p], v, dx[g][l]);
+                        de[l] = Half<T>::mfma(ge[g][p], x[g][l], de[l]);
+                    }
             }
             if (!a.de) continue;
 #pragma unroll
@@ -429,13 +444,18 @@ __global__ __launch_bounds__(256, 3) void k_few_grads16(FewArgs a) {
     }
     if (!a.dxp) return;
 #pragma unroll
-    for (int l = 0; l < C; ++l)
+    for (int g = 0; g < G; ++g) {
+        if (g) __syncthreads();
 #pragma unroll
-        for (int r = 0; r < 4; ++r) red[wave][(4 * q + r) * 16 * C + n * C + l] = dx[l][r] * back * back2;
-    add_waves<C>(a, red);
+        for (int l = 0; l < C; ++l)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) red[wave][(4 * q + r) * 16 * C + n * C + l] = dx[g][l][r] * back * back2;
+        add_waves<C>(a, red, 16 * g);
+    }
 }
 
-// dx from the blocks' partial sums: 16 quads of columns x 16 shares of the partial sums a block, joined in order.
+// dx from the blocks' partial sums: 16 quads of columns x 16 shares of the partial sums a block, joined in order.  (A few us:
+// there are at most 1,024 partial sums of each value.)
 template <class T>
 __global__ __launch_bounds__(256) void k_few_finish(FewArgs a, int parts, T* dx, int64_t lddx) {
     __shared__ f32x4 red[16][16];
@@ -499,8 +519,13 @@ hipError_t launch_few_grads(const FewArgs& a, T* dx, int64_t lddx, hipStream_t s
     FewArgs b = a;
     b.across = few_across(a.d, C);
     const dim3 grid((a.d + b.across * 16 * C - 1) / (b.across * 16 * C), a.parts);
-    if constexpr (sizeof(T) == 4) k_few_grads<T><<<grid, 256, 0, st>>>(b);
-    else k_few_grads16<T><<<grid, 256, 0, st>>>(b);
+    if constexpr (sizeof(T) == 4) {
+        if (a.t <= 16) k_few_grads<T, 1><<<grid, 256, 0, st>>>(b);
+        else k_few_grads<T, 2><<<grid, 256, 0, st>>>(b);
+    } else {
+        if (a.t <= 16) k_few_grads16<T, 1><<<grid, 256, 0, st>>>(b);
+        else k_few_grads16<T, 2><<<grid, 256, 0, st>>>(b);
+    }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !dx) return e;
     k_few_finish<T><<<a.t * ((a.dp / 4 + 15) / 16), 256, 0, st>>>(a, a.parts, dx, lddx);

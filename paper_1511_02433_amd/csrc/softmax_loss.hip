@@ -64,7 +64,9 @@ __device__ __forceinline__ float run_max(const T* at, int64_t n, int64_t lane, i
 }
 
 // The table and x (where `mats` is set), 16 lanes a row or 64 where it is long (the table in one run where no items are
-// excluded and rows follow one another), and the rows' weights (`grads`).
+// excluded and rows follow one another), and the rows' weights (`grads`).  Bound by reading both once (131,072 x 4,096
+// in bfloat16 and 8,192 rows: 211 us, 5.4 TB/s).  Powers of two come from whole matrices, not from rows or blocks of 32, so
+// that products need no factor of their own for each.
 template <class T>
 __global__ __launch_bounds__(1024) void k_scales(ccdpp_softmax_t p, const float* grad, Scales sc, int mats, int grads) {
     __shared__ float red[16][3];
@@ -137,7 +139,9 @@ struct PackArgs {
 };
 
 // One block: 32 rows x 128 columns, blocks of x first.  A wave takes 16 columns at a time: a lane's 8 values of a
-// fragment are 8 neighbours in memory; the turned ones are picked out of LDS.
+// fragment are 8 neighbours in memory; the turned ones are picked out of LDS.  Bound by memory: it reads a matrix once
+// and writes it twice (131,072 x 4,096 in bfloat16 and 8,192 rows: 687 us, 5.0 TB/s), so that every later access is a
+// whole fragment of 1 KB, whatever the inputs' strides and alignment are.
 template <int DT, bool SMALL>
 __global__ __launch_bounds__(256) void k_pack(PackArgs a) {
     typedef typename Types<DT>::in T;
@@ -267,7 +271,12 @@ __global__ __launch_bounds__(256) void k_pack(PackArgs a) {
 }
 
 // ---- the product -----------------------------------------------------------------------------
-// C (M x N) = A (M x K) B (N x K)^T from fragments: 256 x 256 of C per block.
+// C (M x N) = A (M x K) B (N x K)^T from fragments: 256 x 256 of C per block, eight waves of 128 x 64, since a wave then
+// needs 6 KB of fragments for 8 products (a square of 64 x 64 4 KB for 4: LDS would bound it).  Four stages of LDS
+// (128 KB) are filled directly, three ahead.  Bound by the matrix cores at the clock that their power leaves (1.5 to
+// 2.1 GHz): logits of 8,192 x 131,072 x 4,096 in bfloat16 7.3 ms (1.21 PFLOP/s), their G 1.84 ms and either gradient
+// 1.78 ms per 32,768 entries (1.19 and 1.24 PFLOP/s; a large library product reaches 1.35); 2,000 x 32,003 x 1,024 in 32
+// bits (three products) 330 us, 1.19 PFLOP/s.
 enum { EPI_LSE = 0, EPI_G = 1, EPI_OUT = 2 };
 
 struct GemmArgs {
@@ -670,7 +679,7 @@ __global__ __launch_bounds__(kGemmThreads) void k_gemm(GemmArgs a) {
 
 // ---- logits of small products ----------------------------------------------------------------
 // Where blocks of 256 x 256 logits are fewer than CUs, their contraction is cut as well: the shares' partial logits
-// (64 MB at most in all) are joined here, and stay for the gradients' terms.
+// (64 MB at most in all) are joined here, and stay for the gradients' terms.  (200 x 2,372 in shares: 6 us.)
 struct JoinArgs {
     float* z;            // [share][t][pitch]; the first one receives the logits in base 2
     int shares;
@@ -717,7 +726,8 @@ __global__ __launch_bounds__(256) void k_join(JoinArgs a) {
     if (threadIdx.x == 0) a.part[blockIdx.x * a.t + t] = make_float2(top, red[0][1] + red[1][1] + red[2][1] + red[3][1]);
 }
 
-// The terms of 32 x 32 logits a wave: from rows (pitch), or from what k_gemm kept (pitch 0; v0 is the piece's first entry).
+// The terms of 32 x 32 logits a wave: from rows (pitch), or from what k_gemm kept (pitch 0; v0 is the piece's first
+// entry).  Bound by memory (2,000 x 32,003 in two planes: 143 us, 5.4 TB/s).
 template <class PG, int NPL>
 __global__ __launch_bounds__(256) void k_terms(GemmArgs a, const float* z, int64_t pitch) {
     const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
@@ -767,7 +777,8 @@ __global__ __launch_bounds__(256) void k_rows(ccdpp_softmax_t p, const float* ls
 }
 
 // Joins the (max, sum) pairs of a row's pieces (0: of its shares), and takes the target's logit from x and the table: a
-// wave a row, or a block of 256 threads where rows are long.
+// wave a row, or a block of 256 threads where rows are long or few.  (Latency: 5 us for 1,024 or 4,096 rows; 59 us for 8,192
+// rows of 512 pieces and 4,096 columns.)
 template <class T, int THREADS>
 __global__ __launch_bounds__(256) void k_loss(ccdpp_softmax_t p, const float2* part, int64_t pieces, Shares shares, float* loss, float* lse, RowNumbers num) {
     constexpr int kRows = 256 / THREADS;
@@ -839,7 +850,8 @@ struct FinishSide {
     Shares shares;
 };
 
-// Four columns a thread; dx's blocks first.
+// Four columns a thread; dx's blocks first.  Bound by reading the partial sums (4,096 + 17,770 rows of 100 floats in two or three
+// shares: 10 us).
 template <class T>
 __global__ __launch_bounds__(256) void k_finish(FinishSide x, FinishSide e, int64_t blocks_x, int cols, float scale, const int32_t* fin) {
     const bool is_x = blockIdx.x < blocks_x;
@@ -905,7 +917,9 @@ struct Plan {
     int64_t o_scale, o_xrow, o_fin, o_xf, o_ef, o_xl, o_o2, o_xn, o_xt, o_et, o_g, o_gt, o_part, o_dx, o_de, bytes;
 };
 
-constexpr int64_t kPieceBytes = int64_t(512) << 20;  // of G (8192 x 131072 x 4096: 1.5% over 128 MiB)
+// Of G, and as much again of G^T: pieces of the table keep the workspace bounded, whatever t and v are, and larger ones
+// read and write dx's partial sums less often (8,192 x 131,072 x 4,096: 1.5% less than by 128 MiB).
+constexpr int64_t kPieceBytes = int64_t(512) << 20;
 
 
 // A training pass may keep logits between its two halves, in kKeptBytes at most, whatever t and v are.  Written and read
@@ -941,7 +955,8 @@ Plan make_plan(const ccdpp_softmax_t& p, int call) {
     }
     if (w.few) {
         const int64_t wide = (int64_t)few_across(p.d, 16 / es) * 16 * (16 / es), beside = (p.d + wide - 1) / wide;
-        w.few_parts = (int)std::max<int64_t>(1, std::min<int64_t>((es == 4 ? 1024 : 768) / beside, (p.v + 63) / 64));  // as many blocks as run at once
+        const int64_t at_once = 256 * (p.t > 16 ? 2 : es == 4 ? 4 : 3);  // blocks, by their registers
+        w.few_parts = (int)std::max<int64_t>(1, std::min<int64_t>(at_once / beside, (p.v + 63) / 64));
         w.dp = round_up(p.d, 4);
         w.o_dx = take(w.grads ? w.few_parts * p.t * w.dp * 4 : 0);
         w.bytes = at;
