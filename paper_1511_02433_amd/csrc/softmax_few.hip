@@ -485,6 +485,12 @@ hipError_t logits(const FewArgs& a, int blocks, size_t lds, hipStream_t st) {
 
 }  // namespace
 
+// Groups of 16 rows of x that the kernels are built for.
+static int few_groups(int64_t t) {
+    const int n = (int)((t + 15) / 16);
+    return n == 7 ? 8 : n;
+}
+
 FewShape few_shape(int64_t t, int64_t v, int d, int bytes) {
     FewShape s;
     const int64_t groups = (v + 31) / 32 * 2, steps = ((int64_t)d * bytes + 63) / 64;
@@ -498,7 +504,7 @@ FewShape few_shape(int64_t t, int64_t v, int d, int bytes) {
     s.chunk = (int)std::max<int64_t>(1, std::min<int64_t>(steps, (room / t - 16) / 64));
     const int64_t per = (int64_t)(kWaves / s.share) * s.rows;
     s.blocks = (int)std::min<int64_t>(512, (groups + per - 1) / per);
-    const int tg = t <= 16 ? 1 : t <= 32 ? 2 : t <= 64 ? 4 : 8;
+    const int tg = few_groups(t);
     s.lds = std::max<int64_t>(t * (s.chunk * 64 + 16) + (s.share > 1 ? kWaves * s.rows * tg * 1024 : 0), kWaves * tg * 16 * 8);
     return s;
 }
@@ -507,10 +513,16 @@ template <class T>
 hipError_t launch_few_logits(const FewArgs& a, const FewShape& s, hipStream_t st) {
     FewArgs b = a;
     b.share = s.share, b.chunk = s.chunk;
-    if (a.t <= 16) return logits<T, 1, 1>(b, s.blocks, s.lds, st);
-    if (a.t <= 32) return s.rows == 2 ? logits<T, 2, 2>(b, s.blocks, s.lds, st) : logits<T, 2, 1>(b, s.blocks, s.lds, st);
-    if (a.t <= 64) return s.rows == 2 ? logits<T, 4, 2>(b, s.blocks, s.lds, st) : logits<T, 4, 1>(b, s.blocks, s.lds, st);
-    return s.rows == 2 ? logits<T, 8, 2>(b, s.blocks, s.lds, st) : logits<T, 8, 1>(b, s.blocks, s.lds, st);
+    const bool two = s.rows == 2;
+    switch (few_groups(a.t)) {
+        case 1: return logits<T, 1, 1>(b, s.blocks, s.lds, st);
+        case 2: return two ? logits<T, 2, 2>(b, s.blocks, s.lds, st) : logits<T, 2, 1>(b, s.blocks, s.lds, st);
+        case 3: return two ? logits<T, 3, 2>(b, s.blocks, s.lds, st) : logits<T, 3, 1>(b, s.blocks, s.lds, st);
+        case 4: return two ? logits<T, 4, 2>(b, s.blocks, s.lds, st) : logits<T, 4, 1>(b, s.blocks, s.lds, st);
+        case 5: return two ? logits<T, 5, 2>(b, s.blocks, s.lds, st) : logits<T, 5, 1>(b, s.blocks, s.lds, st);
+        case 6: return two ? logits<T, 6, 2>(b, s.blocks, s.lds, st) : logits<T, 6, 1>(b, s.blocks, s.lds, st);
+        default: return two ? logits<T, 8, 2>(b, s.blocks, s.lds, st) : logits<T, 8, 1>(b, s.blocks, s.lds, st);
+    }
 }
 
 template <class T>
