@@ -128,3 +128,33 @@ def test_refusals():
     for kw in (dict(max_norm=-1.0), dict(max_norm=math.nan), dict(max_norm=1.0, eps=-1.0)):
         with pytest.raises(CCDPPError):
             o.clip_grads([a], **kw)
+
+
+@pytest.mark.parametrize("dtypes", [["f32"], ["bf16"], ["f16"], ["f32", "bf16", "f16"]])
+@pytest.mark.parametrize("sizes", [[i % 11 for i in range(64)], [i % 11 + 1 for i in range(64)], [i % 11 + 1 for i in range(65)], [49_152], [49_153],
+                                   [98_304], [98_305], [48_001, 7, 0, 9, 515], [513, 1023, 1025, 2047, 2049, 4, 3], [700] * 64])
+def test_what_one_block_takes(sizes, dtypes):
+    """Around the tensors, chunks and runs of one block, from odd addresses, into odd addresses."""
+    kinds = [DT[dtypes[i % len(dtypes)]] for i in range(len(sizes))]
+    gen = torch.Generator().manual_seed(len(sizes))
+    inside = [torch.randn(n + 9, generator=gen).to(k).cuda() for n, k in zip(sizes, kinds)]
+    ts = [a[i % 4: i % 4 + n] for i, (a, n) in enumerate(zip(inside, sizes))]
+    want = exact_norm(ts)
+    limit = want / 2
+    around = [torch.full_like(a, 7.0) for a in inside]
+    out = [a[(i + 1) % 3: (i + 1) % 3 + n] for i, (a, n) in enumerate(zip(around, sizes))]
+    norm = ops().clip_grads(ts, limit, out=out)
+    assert abs(float(norm) - want) <= 2e-7 * want and torch.equal(norm, ops().grad_norm(ts))
+    c = limit / (want + 1e-6)
+    for i, (a, o, n, room) in enumerate(zip(ts, out, sizes, around)):
+        w = a.double() * c
+        slack = 2.0 ** -25 if a.dtype == torch.float16 else 0.0
+        assert bool(((o.double() - w).abs() <= TOL[a.dtype] * w.abs() + slack).all())
+        first = (i + 1) % 3
+        assert bool((room[:first] == 7).all()) and bool((room[first + n:] == 7).all())
+    kept = [a.clone() for a in inside]
+    ops().clip_grads(ts, limit)  # in place
+    for i, (a, b, n, o) in enumerate(zip(inside, kept, sizes, out)):
+        first = i % 4
+        assert torch.equal(a[first: first + n], o)
+        assert torch.equal(a[:first], b[:first]) and torch.equal(a[first + n:], b[first + n:])

@@ -273,3 +273,38 @@ def test_logits_kept_for_the_gradients(t, v, d, dtype):
     keep = torch.where(without, torch.full_like(y, -1), y)
     loss = torch.where(without, torch.zeros_like(loss), loss)
     check((loss, lse, dx, de), plain(x, e, keep, g, offset=offset), dtype)
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("t,v,d", [(17, 700, 33), (25, 701, 333), (32, 1999, 130), (31, 5, 9)])
+def test_two_groups_of_few_rows(t, v, d, dtype):
+    """Rows in both groups of 16 that are ignored, excluded or hold NaN, weights of either sign, int32 targets, rows apart."""
+    x, e, y, g = make(t, v, d, dtype, seed=t)
+    y[y == 1] = 0
+    offset = torch.zeros(v, device="cuda")
+    offset[::3] = -1.25
+    offset[1] = float("-inf")
+    g[::2] *= -1
+    g[5] = 0
+    y[2], y[t - 1] = -1, 1
+    wide = torch.full((t, d + 3), float("nan"), device="cuda", dtype=DT[dtype])
+    wide[:, 2:d + 2] = x
+    x1 = wide[:, 2:d + 2]
+    x1[2] = float("nan")
+    e1 = e.clone()
+    e1[1] = float("inf")
+    loss, lse, dx, de = ops().softmax_loss_train(x1, e1, y.int(), grad=g, offset=offset)
+    assert float(loss[2]) == 0 and float(loss[t - 1]) == float("inf")
+    assert float(dx[2].abs().max()) == 0 and float(dx[t - 1].abs().max()) == 0 and float(de[1].abs().max()) == 0
+    l2, s2 = ops().softmax_loss(x1, e1, y, offset=offset)
+    dx2, de2 = ops().softmax_loss_grad(x1, e1, y, lse, grad=g, offset=offset)
+    assert torch.equal(loss, l2) and torch.equal(dx, dx2) and torch.equal(de, de2)
+    ex, ee = x.clone(), e.clone()
+    ex[2], ee[1] = 0, 0
+    keep = y.clone()
+    keep[t - 1] = -1
+    want = plain(ex, ee, keep, g, offset=offset)
+    loss, lse = loss.clone(), lse.clone()
+    loss[t - 1] = 0
+    lse[2] = want[1][2]
+    check((loss, lse, dx, de), want, dtype)
