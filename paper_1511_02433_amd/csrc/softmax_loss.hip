@@ -101,13 +101,24 @@ __global__ __launch_bounds__(1024) void k_scales(ccdpp_softmax_t p, const float*
     }
 }
 
-// Largest of kParts partial maxima, by 256 threads.
-__device__ __forceinline__ float parts_max(const float* part, float* red) {
-    const float m = wave_max(part[threadIdx.x]);
+// Largest of kParts partial maxima of each quantity that is asked for (0 for the others), by 256 threads, with one round
+// trip to memory.
+struct Tops {
+    float e, x, g;
+};
+__device__ __forceinline__ Tops parts_max(const Scales& sc, bool want_e, bool want_x, bool want_g, float (*red)[3]) {
+    const int i = threadIdx.x, wave = i >> 6;
+    Tops top = {want_e ? sc.e_part[i] : 0.f, want_x ? sc.x_part[i] : 0.f, want_g ? sc.g_part[i] : 0.f};
+    if (want_e) top.e = wave_max(top.e);
+    if (want_x) top.x = wave_max(top.x);
+    if (want_g) top.g = wave_max(top.g);
+    if ((i & 63) == 0) red[wave][0] = top.e, red[wave][1] = top.x, red[wave][2] = top.g;
     __syncthreads();
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
-    __syncthreads();
-    return fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    const auto of = [&](int k) { return fmaxf(fmaxf(red[0][k], red[1][k]), fmaxf(red[2][k], red[3][k])); };
+    if (want_e) top.e = of(0);
+    if (want_x) top.x = of(1);
+    if (want_g) top.g = of(2);
+    return top;
 }
 
 // ---- operands in fragment order ----------------------------------------------------------
@@ -140,7 +151,7 @@ struct PackArgs {
 
 // One block: 32 rows x 128 columns, blocks of x first.  A wave takes 16 columns at a time: a lane's 8 values of a
 // fragment are 8 neighbours in memory; the turned ones are picked out of LDS.  Bound by memory: it reads a matrix once
-// and writes it twice (131,072 x 4,096 in bfloat16 and 8,192 rows: 687 us, 5.0 TB/s), so that every later access is a
+// and writes it twice (131,072 x 4,096 in bfloat16 and 8,192 rows: 709 us, 4.9 TB/s), so that every later access is a
 // whole fragment of 1 KB, whatever the inputs' strides and alignment are.
 template <int DT, bool SMALL>
 __global__ __launch_bounds__(256) void k_pack(PackArgs a) {
@@ -150,35 +161,51 @@ __global__ __launch_bounds__(256) void k_pack(PackArgs a) {
     constexpr int NPL = Types<DT>::planes;
     constexpr int kPitch = 128 + 16 / sizeof(T);
     __shared__ __align__(16) T tile[32][kPitch];
-    __shared__ float live[32], red[4];
+    __shared__ float live[32], red[4][3];
     __shared__ int exps[32];
     const bool is_x = blockIdx.x < a.x.tiles;
     const PackSide& side = is_x ? a.x : a.e;
     const int64_t rt = is_x ? blockIdx.x : blockIdx.x - a.x.tiles, r0 = rt * 32;
     const int c0 = blockIdx.y * 128;
-    int exp = 0, unit = 0;  // powers of two of the turned matrix, and of the table as it is
-    if (a.scaled) {
-        const float em = parts_max(a.sc.e_part, red);
-        unit = unit_exp(em);
-        exp = scale_exp(is_x ? parts_max(a.sc.x_part, red) : em);
+    // All that is read, before the first wait.
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 31, h = lane >> 5;
+    const int64_t row = r0 + m;
+    const bool in = row < side.rows;
+    const T* const src = (const T*)side.src + row * side.ld;
+    Run<T, 8> held[2] = {};
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int s = wave + 4 * k;
+        if (in && c0 / 16 + s < a.ksd) held[k] = load_tail<8>(src, c0 + 16 * s + 8 * h, a.d, (side.rows - 1 - row) * side.ld + a.d);
     }
-    if (blockIdx.x == 0 && blockIdx.y == 0 && (a.scaled || a.weights)) {
-        const float em = a.scaled ? parts_max(a.sc.e_part, red) : 0.f, xm = a.scaled ? parts_max(a.sc.x_part, red) : 0.f;
-        const float gm = a.weights ? parts_max(a.sc.g_part, red) : 0.f;
+    const int64_t r = r0 + threadIdx.x;  // of the first 32 threads
+    bool row_in = threadIdx.x < 32 && r < side.rows, row_live = row_in, negative = false;
+    float row_top = 0.f, row_offset = 0.f;
+    if (row_in && is_x) {
+        if (NPL == 2) row_top = a.sc.x_row[r];
+        if (side.live && a.grad) negative = a.grad[r] < 0.f;
+        row_live = row_counts(load_target(a.target, a.target_bits, r), a.v, a.offset);
+    } else if (row_in && a.offset) {
+        row_offset = a.offset[r];
+        row_live = !(row_offset < kExcluded);
+    }
+    int exp = 0, unit = 0;  // powers of two of the turned matrix, and of the table as it is
+    const bool leaves = blockIdx.x == 0 && blockIdx.y == 0;  // the exponents
+    if (a.scaled || (leaves && a.weights)) {
+        const Tops top = parts_max(a.sc, a.scaled, a.scaled && (is_x || leaves), leaves && a.weights, red);
+        unit = a.scaled ? unit_exp(top.e) : 0;
+        exp = a.scaled ? scale_exp(is_x ? top.x : top.e) : 0;
         // G lies within its row's weight, or a few times that where lse is the caller's own: two bits are left for it.
-        if (threadIdx.x == 0) a.sc.fin[0] = scale_exp(em), a.sc.fin[1] = scale_exp(xm), a.sc.fin[2] = scale_exp(gm) - 2;
+        if (leaves && threadIdx.x == 0) a.sc.fin[0] = scale_exp(top.e), a.sc.fin[1] = scale_exp(top.x), a.sc.fin[2] = scale_exp(top.g) - 2;
     }
     // 32-bit rows of x are multiplied with scale and log2 e before they are split.
     const float before = NPL == 2 ? a.scale * kLog2e : 1.f;
     if (threadIdx.x < 32) {
-        const int64_t r = r0 + threadIdx.x;
-        bool counts = r < side.rows;
         if (is_x) {
-            counts = counts && row_counts(load_target(a.target, a.target_bits, r), a.v, a.offset);
             int e = 0;
-            float f = r < side.rows ? a.scale * kLog2e : 0.f;
-            if (NPL == 2 && r < side.rows) {
-                e = row_exp(a.sc.x_row[r] * fabsf(before), unit);
+            float f = row_in ? a.scale * kLog2e : 0.f;
+            if (NPL == 2 && row_in) {
+                e = row_exp(row_top * fabsf(before), unit);
                 f = ldexpf(1.f, -(e + unit));
             }
             exps[threadIdx.x] = e;
@@ -186,36 +213,26 @@ __global__ __launch_bounds__(256) void k_pack(PackArgs a) {
                 if (side.num) *(float*)(side.num + rt * side.num_row + (kNumFactor * 32 + threadIdx.x) * 4) = f;
                 if (side.live_num) {  // rows that count get the rest once their lse is there
                     float* o = (float*)(side.live_num + rt * side.live_num_row) + threadIdx.x;
-                    o[kNumFactor * 32] = counts ? f : 0.f;
+                    o[kNumFactor * 32] = row_live ? f : 0.f;
                     o[kNumTerm * 32] = o[kNumLse * 32] = -INFINITY;
                     o[kNumWeight * 32] = o[kNumRaw * 32] = 0.f;
                     o[kNumTarget * 32] = __int_as_float(-1);
                 }
             }
-        } else {
-            counts = counts && !(a.offset && a.offset[r] < kExcluded);
-            if (blockIdx.y == 0 && side.num)
-                *(float*)(side.num + rt * side.num_row + (kNumOffset * 32 + threadIdx.x) * 4) =
-                    counts ? (a.offset ? a.offset[r] * kLog2e : 0.f) : -INFINITY;
+        } else if (blockIdx.y == 0 && side.num) {
+            *(float*)(side.num + rt * side.num_row + (kNumOffset * 32 + threadIdx.x) * 4) = row_live ? row_offset * kLog2e : -INFINITY;
         }
         // Terms of few factors are exponentials, with no sign: a negative weight's is taken into the turned row.
-        live[threadIdx.x] = !counts ? 0.f : side.live && a.grad && a.grad[r] < 0.f ? -1.f : 1.f;
+        live[threadIdx.x] = !row_live ? 0.f : negative ? -1.f : 1.f;
     }
     __syncthreads();
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 31, h = lane >> 5;
-    const int64_t row = r0 + m;
-    const bool in = row < side.rows;
     const float mul = pow2i(is_x ? exps[m] : unit), mul_t = pow2i(exp);
     const bool counts = live[m] != 0.f;
-    const T* const src = (const T*)side.src + row * side.ld;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
         const int s = wave + 4 * k, ks = c0 / 16 + s;
         if (ks >= a.ksd) break;
-        const int c = c0 + 16 * s + 8 * h;
-        Run<T, 8> q = {};
-        if (in) q = load_tail<8>(src, c, a.d, (side.rows - 1 - row) * side.ld + a.d);
-        T* const v = q.v;
+        T* const v = held[k].v;
         if (!is_x && !counts)
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = (T)0.f;
