@@ -134,9 +134,10 @@ __device__ __forceinline__ f32x16 row_numbers(const char* rows, int which, int h
     return o;
 }
 
-// Sums of exponentials stay relative to `ref`, which the first tile sets; it is only moved when a tile's sum leaves
-// what 32 bits hold well (above 2^40), so that an entry costs its exponential and its addition alone: the logits'
-// accumulator starts at -ref.
+// Sums of exponentials stay relative to `ref`, which the first tile with a finite logit sets; it is only moved when a tile's
+// sum leaves what 32 bits hold well (above 2^40), so that an entry costs its exponential and its addition alone: the
+// logits' accumulator starts at -ref.  Where the reference has to move, the tile's products are made again from 0: the
+// first reference may be a finite mask's (-1e9), and what was added to that has lost its last digits.
 constexpr float kSumLimit = 1099511627776.f;
 
 // UNIT: the accumulated products are the logits (factor 1).
@@ -149,30 +150,35 @@ __device__ __forceinline__ void small_lse(const SmallArgs& a, int64_t first, int
     bool set = false;
     stream<S>(a.e, a.e_tile, first, last, lds, [&](int64_t i, const char* slot) {
         const bool offsets = a.offsets || i == a.vt - 1;  // the last tile's missing entries are -inf
-        f32x16 z;
+        const auto logits = [&](float from) {
+            f32x16 z;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) z[r] = UNIT ? -ref : 0.f;
-        if (UNIT && offsets) z += row_numbers(slot + S::kRows * kBlk, kNumOffset, h);
-        z = tile_product<P, NPL, KS>(slot, kept, lane, z);
-        if constexpr (!UNIT) {
+            for (int r = 0; r < 16; ++r) z[r] = UNIT ? from : 0.f;
+            if (UNIT && offsets) z += row_numbers(slot + S::kRows * kBlk, kNumOffset, h);
+            z = tile_product<P, NPL, KS>(slot, kept, lane, z);
+            if constexpr (!UNIT) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) z[r] = fmaf(z[r], f, -ref);
-            if (offsets) z += row_numbers(slot + S::kRows * kBlk, kNumOffset, h);
-        }
+                for (int r = 0; r < 16; ++r) z[r] = fmaf(z[r], f, from);
+                if (offsets) z += row_numbers(slot + S::kRows * kBlk, kNumOffset, h);
+            }
+            return z;
+        };
+        f32x16 z = logits(-ref);
         float s = 0.f;
 #pragma unroll
         for (int r = 0; r < 16; ++r) s += exp2_fast(z[r]);
-        if (__any(!set || !(s <= kSumLimit))) {
-            float m = -INFINITY;
+        const bool moves = !set || s > kSumLimit;
+        if (__any(moves)) {
+            if (__any(set && moves)) z = logits(0.f);  // (relative to 0 as they are in lanes that have no reference yet)
+            float m = set ? ref : -INFINITY;
 #pragma unroll
             for (int r = 0; r < 16; ++r) m = fmaxf(m, z[r]);
-            if (set) m = fmaxf(m, 0.f);
-            if (m != -INFINITY) {
+            if (moves && m != -INFINITY) {
                 s = 0.f;
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s += exp2_fast(z[r] - m);
-                sum *= exp2_fast(-m);
-                ref += m;
+                if (set) sum *= exp2_fast(ref - m);  // (0 before: the factor would be infinite for low logits)
+                ref = m;
                 set = true;
             }
         }

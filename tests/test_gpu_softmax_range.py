@@ -1,0 +1,89 @@
+"""The softmax loss far from where its numbers are easy: logits that are all low, finite masks, values and weights of very
+different sizes, items and rows that hardly count.  Compared with plain float64 torch on the GPU, row by row and item by item.
+
+Tolerances.  A logit and a log-sum-exp z have 32 bits: 5e-7 (1 + |z|) each, Z the largest |z| of what is not masked, so a loss
+is within 1e-6 (1 + Z) and a probability within that relative to itself."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+def ops():
+    from paper_1511_02433_amd import ops as o
+    return o
+
+
+def make(t, v, d, dtype, seed=0, spread=2.0):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.randn(t, d, generator=gen, device="cuda").to(DT[dtype])
+    e = (torch.randn(v, d, generator=gen, device="cuda") * (spread / math.sqrt(d))).to(DT[dtype])
+    y = torch.randint(0, v, (t,), generator=gen, device="cuda")
+    return x, e, y
+
+
+def logits(x, e, scale=1.0, offset=None):
+    z = scale * torch.mm(x.double(), e.double().t())
+    return z if offset is None else z + offset.double()
+
+
+def check_loss(x, e, y, loss, lse, offset=None, masked=None):
+    z = logits(x, e, 1.0, offset)
+    want = torch.logsumexp(z, dim=1)
+    rows = torch.arange(len(y), device="cuda")
+    size = z if masked is None else z[:, ~masked]
+    tol = 1e-6 * (1 + float(size.abs().max()))
+    assert float((lse.double() - want).abs().max()) <= tol
+    assert float((loss.double() - (want - z[rows, y])).abs().max()) <= tol
+    return z, want
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("t", [32, 33, 200])
+@pytest.mark.parametrize("d", [8, 40, 128, 136])
+@pytest.mark.parametrize("shift", [-85.0, -100.0, -1000.0, 500.0])
+def test_a_shift_of_all_logits(t, d, shift, dtype):
+    x, e, y = make(t, 1000, d, dtype, seed=d)
+    offset = torch.full((1000,), shift, device="cuda")
+    loss, lse, dx, de = ops().softmax_loss_train(x, e, y, offset=offset)
+    z, want = check_loss(x, e, y, loss, lse, offset)
+    g = torch.exp(z - want[:, None])
+    g[torch.arange(t, device="cuda"), y] -= 1
+    tol = {"f32": 2e-5, "bf16": 1e-2, "f16": 2e-3}[dtype] + 1e-6 * (1 + abs(shift))
+    for a, b in ((dx, torch.mm(g, e.double())), (de, torch.mm(g.t().contiguous(), x.double()))):
+        assert float((a.double() - b).norm()) <= tol * float(b.norm())
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("t", [32, 33, 200])
+@pytest.mark.parametrize("d", [8, 40, 128, 136])
+@pytest.mark.parametrize("mask", [-300.0, -1e4, -65504.0, -1e6, -1e9])
+@pytest.mark.parametrize("first,last", [(0, 32), (0, 64), (128, 160), (480, 640)])
+def test_finite_masks(t, d, mask, first, last, dtype):
+    """Masks over whole tiles of 32 items, where a share of the table begins among them."""
+    x, e, y = make(t, 1000, d, dtype, seed=d)
+    offset = torch.zeros(1000, device="cuda")
+    offset[first:last] = mask
+    masked = offset < 0
+    y = torch.where(masked[y], torch.full_like(y, 700), y)
+    loss, lse = ops().softmax_loss(x, e, y, offset=offset)
+    check_loss(x, e, y, loss, lse, offset, masked)
+    l2, s2, dx, de = ops().softmax_loss_train(x, e, y, offset=offset)
+    assert torch.equal(loss, l2) and torch.equal(lse, s2)
+    assert bool(torch.isfinite(dx).all()) and float(de[masked].float().abs().max()) == 0.0
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("t,d", [(40, 40), (300, 100)])
+def test_a_distance_softmax(t, d, dtype):
+    """offset = -|e|^2 / 2: every logit of rows near none of the items is low."""
+    x, e, y = make(t, 3000, d, dtype, seed=t, spread=30.0)
+    x = (x.float() * 0.1).to(DT[dtype])
+    offset = -0.5 * e.float().square().sum(1)
+    loss, lse = ops().softmax_loss(x, e, y, offset=offset)
+    check_loss(x, e, y, loss, lse, offset)
