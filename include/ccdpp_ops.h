@@ -61,9 +61,12 @@ enum ccdpp_dtype {
  *              every item is excluded, lse is -inf and probabilities are 0.
  * Products of 16-bit values are exact and summed in 32 bits.  32-bit values are
  * multiplied as they are for t <= 32 (for the logits also t <= 128 where d > 128), and as
- * sums of two halves with 11 bits each and a common exponent otherwise: 22
- * bits of the largest value of a row of x, or of the table.  A probability's relative error is
- * some 5e-7 (1 + |z|), what a logit and its lse have in 32 bits.
+ * sums of two halves with 11 bits each otherwise: 22 bits of every value down to 2^-17 of
+ * the largest of its row (of x or of the table), and 2^-39 of that largest below it.  (With
+ * d <= 128 and scaled rows of x whose norm times the table's largest value is at most
+ * some 20, values are held to 2^-25 or better of the table's largest and its inverse, which is 5e-7 of a logit.)
+ * A logit's and a probability's relative error are some 5e-7 (1 + |z|), what a logit and
+ * its lse have in 32 bits.
  */
 typedef struct ccdpp_softmax {
     int64_t t, v;

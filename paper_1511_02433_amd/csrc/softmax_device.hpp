@@ -55,12 +55,11 @@ __device__ __forceinline__ int unit_exp(float top) {
     return max(-126, min(126, 127 - (int)(__float_as_uint(top) >> 23)));
 }
 
-// Power of two for a row of x whose largest |value| (times scale and log2 e) is `top`: that of the table taken back, so
-// that products are logits as they are, or what keeps it below 2^15 (logits beyond 30,000) with a factor left over.
-__device__ __forceinline__ int row_exp(float top, int table) {
-    const int e = (int)(__float_as_uint(top) >> 23) - 127;
-    return max(-126, min(-table, 14 - e));
-}
+// Two half-precision planes hold a value to 22 bits of itself, or to 2^-25.  With the whole table under one power of two
+// (unit_exp) and x under its inverse the products are logits as they are, and what the table's values lack of 22 bits
+// costs a logit some 2^-26 |x'|, x' being the row of x as it is multiplied.  Up to this |x'| that is 5e-7; beyond it a
+// large value of the table could cost other items their digits, and every row of either side gets a power of two of its own.
+constexpr float kUnitNorm = 32.f;
 
 // Value in planes: hi + lo, 22 bits; lo stays 0 where hi is not finite.
 template <class P, int NPL>
@@ -107,9 +106,16 @@ __device__ __forceinline__ bool row_counts(int64_t y, int64_t v, const float* of
     return !(y < v && offset && offset[y] < kExcluded);
 }
 
+// Largest value of a wave, by moves between lanes that do not go through LDS: within rows of 16 lanes, then from row to row.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float max_from(float m) {
+    const int i = __builtin_bit_cast(int, m);
+    return fmaxf(m, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(i, i, CTRL, ROWS, 0xf, false)));
+}
 __device__ __forceinline__ float wave_max(float m) {
-    for (int k = 32; k > 0; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
-    return m;
+    m = max_from<0x111, 0xf>(m), m = max_from<0x112, 0xf>(m), m = max_from<0x114, 0xf>(m), m = max_from<0x118, 0xf>(m);  // row_shr
+    m = max_from<0x142, 0xa>(m), m = max_from<0x143, 0xc>(m);  // row_bcast:15, row_bcast:31
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, m), 63));
 }
 
 // 1 KB from global memory into LDS, 16 bytes per lane, without passing through registers.
@@ -122,8 +128,9 @@ __device__ __forceinline__ void fetch(const char* from, char* to) {
 // rows [plane][step of 16 over d]; the rows' numbers, 32 floats each; the fragments of the turned rows
 // [plane][32 columns][2 steps of 16 rows].
 enum {
-    kNumFactor = 0,   // x: factor of the accumulated logits (1 for nearly all 32-bit rows)
+    kNumFactor = 0,   // x: factor of the accumulated logits; of 32-bit rows an exponent, as int32 (0 unless rows have their own)
     kNumOffset = 0,   // table: offset in base 2, -inf for excluded and missing entries
+    kNumExp = 1,      // table: the same exponent
     kNumTerm = 1,     // x: log2 |weight| - lse in base 2, G's exponent: G = exp2(logit + term)
     kNumWeight = 2,   // x: |weight| with G's power of two
     kNumTarget = 3,   // x: target, as int32

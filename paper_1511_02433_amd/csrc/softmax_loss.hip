@@ -28,14 +28,15 @@ namespace ccdops {
 namespace {
 
 // ---- scales of 32-bit inputs ----------------------------------------------------------
-// Exponents of the powers of two that x's rows (their own, for the logits; one for all rows that count, for de), the
-// table and the rows' weights are multiplied with.  Only finite values count.
+// Exponents of the powers of two that x's rows and the table's (their own, for the logits; one for all that count, for the
+// gradients) and the rows' weights are multiplied with.  Only finite values count.
 constexpr int kParts = 256;  // blocks of k_scales, and partial maxima of each quantity
 
 struct Scales {
     float *e_part, *x_part, *g_part;  // [kParts] largest |table| (excluded items apart), |x| of rows that count, |grad|
-    float* x_row;                     // [t] largest |value| of each row of x
-    int32_t* fin;                     // [3] exponents: table, x, G
+    float* n_part;                    // [kParts] largest 2-norm of a row of x (few factors)
+    float *x_row, *e_row;             // [t], [v] largest |value| of each row; e_row: NULL where it is not asked for
+    int32_t* fin;                     // [4] exponents: table, x, G; whether rows have their own (few factors)
 };
 
 template <class T>
@@ -63,26 +64,45 @@ __device__ __forceinline__ float run_max(const T* at, int64_t n, int64_t lane, i
     return m;
 }
 
-// The table and x (where `mats` is set), 16 lanes a row or 64 where it is long (the table in one run where no items are
-// excluded and rows follow one another), and the rows' weights (`grads`).  Bound by reading both once (131,072 x 4,096
-// in bfloat16 and 8,192 rows: 211 us, 5.4 TB/s).  Powers of two come from whole matrices, not from rows or blocks of 32, so
-// that products need no factor of their own for each.
+// Largest value over the lanes (16 or 64) that share a row.
+__device__ __forceinline__ float lanes_max(float m, int lanes) {
+    for (int k = lanes / 2; k > 0; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
+    return m;
+}
+
+// The table and x (where `mats` is set), 16 lanes a row or 64 where it is long (the table in one run where its rows are not
+// asked for, no items are excluded and rows follow one another), and the rows' weights (`grads`).  Bound by reading both
+// once (131,072 x 4,096 in bfloat16 and 8,192 rows: 211 us, 5.4 TB/s).  The logits of wide 32-bit rows take a power of two
+// from each row; what is contracted over rows (the turned matrices) one from the whole matrix.
 template <class T>
-__global__ __launch_bounds__(1024) void k_scales(ccdpp_softmax_t p, const float* grad, Scales sc, int mats, int grads) {
-    __shared__ float red[16][3];
-    float em = 0.f, xm = 0.f, gm = 0.f;
+__global__ __launch_bounds__(1024) void k_scales(ccdpp_softmax_t p, const float* grad, Scales sc, int mats, int norms, int grads) {
+    __shared__ float red[16][4];
+    float em = 0.f, xm = 0.f, gm = 0.f, nm = 0.f;
     if (mats) {
-        const int lanes = p.d > 256 ? 64 : 16, l = threadIdx.x & (lanes - 1), per = 1024 / lanes;
+        const int lanes = p.d > (sc.e_row ? 1024 : 256) ? 64 : 16, l = threadIdx.x & (lanes - 1), per = 1024 / lanes;
         const int64_t first = (int64_t)blockIdx.x * per + threadIdx.x / lanes, stride = (int64_t)kParts * per;
-        if (!p.offset && p.ldt == p.d) {
+        if (!sc.e_row && !p.offset && p.ldt == p.d) {
             em = run_max((const T*)p.table, p.v * p.d, (int64_t)blockIdx.x * 1024 + threadIdx.x, (int64_t)kParts * 1024);
         } else {
-            for (int64_t v = first; v < p.v; v += stride)
-                if (!p.offset || !(p.offset[v] < kExcluded)) em = fmaxf(em, run_max((const T*)p.table + v * p.ldt, p.d, l, lanes));
+            for (int64_t v = first; v < p.v; v += stride) {
+                float m = 0.f;
+                if (!p.offset || !(p.offset[v] < kExcluded)) m = run_max((const T*)p.table + v * p.ldt, p.d, l, lanes);
+                em = fmaxf(em, m);
+                if (sc.e_row) {
+                    m = lanes_max(m, lanes);
+                    if (l == 0) sc.e_row[v] = m;
+                }
+            }
         }
         for (int64_t t = first; t < p.t; t += stride) {
-            float m = run_max((const T*)p.x + t * p.ldx, p.d, l, lanes);
-            for (int k = lanes / 2; k > 0; k >>= 1) m = fmaxf(m, __shfl_xor(m, k));
+            const T* const row = (const T*)p.x + t * p.ldx;
+            const float m = lanes_max(run_max(row, p.d, l, lanes), lanes);
+            if (norms) {
+                double s = 0.0;
+                for (int i = l; i < p.d; i += lanes) s += (double)abs_finite(row[i]) * (double)abs_finite(row[i]);
+                for (int k = lanes / 2; k > 0; k >>= 1) s += __shfl_xor(s, k);
+                nm = fmaxf(nm, (float)sqrt(s));
+            }
             if (l == 0) sc.x_row[t] = m;
             if (row_counts(load_target(p.target, p.target_bits, t), p.v, p.offset)) xm = fmaxf(xm, m);
         }
@@ -90,34 +110,35 @@ __global__ __launch_bounds__(1024) void k_scales(ccdpp_softmax_t p, const float*
     if (grads)
         for (int64_t t = (int64_t)blockIdx.x * 1024 + threadIdx.x; t < p.t; t += (int64_t)kParts * 1024)
             if (row_counts(load_target(p.target, p.target_bits, t), p.v, p.offset)) gm = fmaxf(gm, grad ? abs_finite(grad[t]) : 1.f);
-    em = wave_max(em), xm = wave_max(xm), gm = wave_max(gm);
+    em = wave_max(em), xm = wave_max(xm), gm = wave_max(gm), nm = wave_max(nm);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    if (lane == 0) red[wave][0] = em, red[wave][1] = xm, red[wave][2] = gm;
+    if (lane == 0) red[wave][0] = em, red[wave][1] = xm, red[wave][2] = gm, red[wave][3] = nm;
     __syncthreads();
-    if (wave == 0) {
-        em = lane < 16 ? red[lane][0] : 0.f, xm = lane < 16 ? red[lane][1] : 0.f, gm = lane < 16 ? red[lane][2] : 0.f;
-        em = wave_max(em), xm = wave_max(xm), gm = wave_max(gm);
-        if (lane == 0) sc.e_part[blockIdx.x] = em, sc.x_part[blockIdx.x] = xm, sc.g_part[blockIdx.x] = gm;
+    if (wave < 4) {  // a wave each
+        const float m = wave_max(lane < 16 ? red[lane][wave] : 0.f);
+        if (lane == 0) (wave == 0 ? sc.e_part : wave == 1 ? sc.x_part : wave == 2 ? sc.g_part : sc.n_part)[blockIdx.x] = m;
     }
 }
 
 // Largest of kParts partial maxima of each quantity that is asked for (0 for the others), by 256 threads, with one round
 // trip to memory.
 struct Tops {
-    float e, x, g;
+    float e, x, g, n;
 };
-__device__ __forceinline__ Tops parts_max(const Scales& sc, bool want_e, bool want_x, bool want_g, float (*red)[3]) {
+__device__ __forceinline__ Tops parts_max(const Scales& sc, bool want_e, bool want_x, bool want_g, bool want_n, float (*red)[4]) {
     const int i = threadIdx.x, wave = i >> 6;
-    Tops top = {want_e ? sc.e_part[i] : 0.f, want_x ? sc.x_part[i] : 0.f, want_g ? sc.g_part[i] : 0.f};
+    Tops top = {want_e ? sc.e_part[i] : 0.f, want_x ? sc.x_part[i] : 0.f, want_g ? sc.g_part[i] : 0.f, want_n ? sc.n_part[i] : 0.f};
     if (want_e) top.e = wave_max(top.e);
     if (want_x) top.x = wave_max(top.x);
     if (want_g) top.g = wave_max(top.g);
-    if ((i & 63) == 0) red[wave][0] = top.e, red[wave][1] = top.x, red[wave][2] = top.g;
+    if (want_n) top.n = wave_max(top.n);
+    if ((i & 63) == 0) red[wave][0] = top.e, red[wave][1] = top.x, red[wave][2] = top.g, red[wave][3] = top.n;
     __syncthreads();
     const auto of = [&](int k) { return fmaxf(fmaxf(red[0][k], red[1][k]), fmaxf(red[2][k], red[3][k])); };
     if (want_e) top.e = of(0);
     if (want_x) top.x = of(1);
     if (want_g) top.g = of(2);
+    if (want_n) top.n = of(3);
     return top;
 }
 
@@ -134,6 +155,7 @@ struct PackSide {
     int64_t turned_row, turned_d, turned_plane;  // per block of 32 rows, per block of 32 columns, per plane
     char *num, *live_num;                     // numbers of the first 32 rows (see softmax_device.hpp; `num`: the first one only)
     int64_t num_row, live_num_row;
+    char* exps;                               // the table's kNumExp, num_row apart (32-bit values)
 };
 struct PackArgs {
     PackSide x, e;
@@ -161,7 +183,7 @@ __global__ __launch_bounds__(256) void k_pack(PackArgs a) {
     constexpr int NPL = Types<DT>::planes;
     constexpr int kPitch = 128 + 16 / sizeof(T);
     __shared__ __align__(16) T tile[32][kPitch];
-    __shared__ float live[32], red[4][3];
+    __shared__ float live[32], red[4][4], tops[4][32];
     __shared__ int exps[32];
     const bool is_x = blockIdx.x < a.x.tiles;
     const PackSide& side = is_x ? a.x : a.e;
@@ -181,33 +203,46 @@ __global__ __launch_bounds__(256) void k_pack(PackArgs a) {
     const int64_t r = r0 + threadIdx.x;  // of the first 32 threads
     bool row_in = threadIdx.x < 32 && r < side.rows, row_live = row_in, negative = false;
     float row_top = 0.f, row_offset = 0.f;
+    if (NPL == 2 && row_in && (is_x || a.sc.e_row)) row_top = (is_x ? a.sc.x_row : a.sc.e_row)[r];
     if (row_in && is_x) {
-        if (NPL == 2) row_top = a.sc.x_row[r];
         if (side.live && a.grad) negative = a.grad[r] < 0.f;
         row_live = row_counts(load_target(a.target, a.target_bits, r), a.v, a.offset);
     } else if (row_in && a.offset) {
         row_offset = a.offset[r];
         row_live = !(row_offset < kExcluded);
     }
+    // 32-bit rows of x are multiplied with scale and log2 e before they are split.
+    const float before = NPL == 2 ? a.scale * kLog2e : 1.f;
     int exp = 0, unit = 0;  // powers of two of the turned matrix, and of the table as it is
+    bool own = !SMALL;      // rows have their own (32-bit values)
     const bool leaves = blockIdx.x == 0 && blockIdx.y == 0;  // the exponents
     if (a.scaled || (leaves && a.weights)) {
-        const Tops top = parts_max(a.sc, a.scaled, a.scaled && (is_x || leaves), leaves && a.weights, red);
-        unit = a.scaled ? unit_exp(top.e) : 0;
+        const Tops top = parts_max(a.sc, a.scaled, a.scaled && (is_x || leaves), leaves && a.weights, SMALL && NPL == 2, red);
+        if constexpr (SMALL && NPL == 2) {
+            unit = unit_exp(top.e);
+            own = !(top.n * fabsf(before) * pow2i(-unit) <= kUnitNorm);
+            if (leaves && threadIdx.x == 0) a.sc.fin[3] = own;
+            if (own && !is_x) {  // (all columns are here)
+                float most = 0.f;
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) most = fmaxf(most, abs_finite(held[k].v[j]));
+                most = fmaxf(most, __shfl_xor(most, 32));
+                if (h == 0) tops[wave][m] = most;
+                __syncthreads();
+                if (threadIdx.x < 32) row_top = fmaxf(fmaxf(tops[0][threadIdx.x], tops[1][threadIdx.x]), fmaxf(tops[2][threadIdx.x], tops[3][threadIdx.x]));
+            }
+        }
         exp = a.scaled ? scale_exp(is_x ? top.x : top.e) : 0;
         // G lies within its row's weight, or a few times that where lse is the caller's own: two bits are left for it.
         if (leaves && threadIdx.x == 0) a.sc.fin[0] = scale_exp(top.e), a.sc.fin[1] = scale_exp(top.x), a.sc.fin[2] = scale_exp(top.g) - 2;
     }
-    // 32-bit rows of x are multiplied with scale and log2 e before they are split.
-    const float before = NPL == 2 ? a.scale * kLog2e : 1.f;
     if (threadIdx.x < 32) {
         if (is_x) {
-            int e = 0;
+            const int e = own ? scale_exp(row_top * fabsf(before)) : -unit;
             float f = row_in ? a.scale * kLog2e : 0.f;
-            if (NPL == 2 && row_in) {
-                e = row_exp(row_top * fabsf(before), unit);
-                f = ldexpf(1.f, -(e + unit));
-            }
+            if (NPL == 2) f = __int_as_float(own ? -e : 0);
             exps[threadIdx.x] = e;
             if (blockIdx.y == 0) {
                 if (side.num) *(float*)(side.num + rt * side.num_row + (kNumFactor * 32 + threadIdx.x) * 4) = f;
@@ -219,14 +254,17 @@ __global__ __launch_bounds__(256) void k_pack(PackArgs a) {
                     o[kNumTarget * 32] = __int_as_float(-1);
                 }
             }
-        } else if (blockIdx.y == 0 && side.num) {
-            *(float*)(side.num + rt * side.num_row + (kNumOffset * 32 + threadIdx.x) * 4) = row_live ? row_offset * kLog2e : -INFINITY;
+        } else {
+            const int e = own ? scale_exp(row_top) : unit;
+            exps[threadIdx.x] = e;
+            if (blockIdx.y == 0 && side.num) *(float*)(side.num + rt * side.num_row + (kNumOffset * 32 + threadIdx.x) * 4) = row_live ? row_offset * kLog2e : -INFINITY;
+            if (NPL == 2 && own && blockIdx.y == 0 && side.exps) *(int*)(side.exps + rt * side.num_row + threadIdx.x * 4) = -e;
         }
         // Terms of few factors are exponentials, with no sign: a negative weight's is taken into the turned row.
         live[threadIdx.x] = !row_live ? 0.f : negative ? -1.f : 1.f;
     }
     __syncthreads();
-    const float mul = pow2i(is_x ? exps[m] : unit), mul_t = pow2i(exp);
+    const float mul = NPL == 2 ? pow2i(exps[m]) : 1.f, mul_t = pow2i(exp);
     const bool counts = live[m] != 0.f;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
@@ -307,7 +345,8 @@ struct GemmArgs {
     int64_t v0;                  // table entry of row 0 of A
     int64_t t, v;
     const int32_t* fin;          // exponents; NULL where nothing is scaled
-    const float* xf;             // factor of each row's accumulated logits
+    const float* xf;             // factor of each row's accumulated logits (32-bit values: an exponent)
+    const int* ek;               // exponents of A's rows (32-bit values)
     float scale;
     const float* offset;
     const float* o2;             // offsets of A's rows in base 2, -inf for excluded and missing ones
@@ -605,7 +644,16 @@ __global__ __launch_bounds__(kGemmThreads) void k_gemm(GemmArgs a) {
         }
         return;
     }
-    // Logits in base 2: accumulator times the row's factor, plus offset.
+    // Logits in base 2: accumulator times the row's factor, plus offset; of 32-bit values both rows' powers of two are taken off.
+    typedef int i32x4 __attribute__((ext_vector_type(4)));
+    const auto logit = [](float acc, float f, int k, float o) {
+        if constexpr (NPL == 2) return __builtin_amdgcn_ldexpf(acc, __float_as_int(f) + k) + o;
+        else return fmaf(acc, f, o);
+    };
+    const auto exponents = [&](int64_t tile, i32x4* k) {  // of a block of 32 entries, like their offsets
+#pragma unroll
+        for (int q = 0; q < 4; ++q) k[q] = NPL == 2 ? *(const i32x4*)(a.ek + tile * 32 + 4 * h + 8 * q) : i32x4{};
+    };
     const auto offsets = [&](int64_t tile, f32x4* o) {  // of a block of 32 entries, those of this lane's rows
         const float* at = a.o2 + tile * 32 + 4 * h;
 #pragma unroll
@@ -620,8 +668,10 @@ __global__ __launch_bounds__(kGemmThreads) void k_gemm(GemmArgs a) {
         for (int i = 0; i < 4; ++i) {
             const int64_t tile = (int64_t)bm * 8 + wm * 4 + i;
             f32x4 o[4];
+            i32x4 k[4] = {};
             if (tile < a.m_tiles) {
                 offsets(tile, o);
+                exponents(tile, k);
             } else {
 #pragma unroll
                 for (int q = 0; q < 4; ++q) o[q] = -INFINITY;
@@ -630,7 +680,7 @@ __global__ __launch_bounds__(kGemmThreads) void k_gemm(GemmArgs a) {
             for (int j = 0; j < kNf; ++j)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    acc[i][j][r] = fmaf(acc[i][j][r], f[j], o[r >> 2][r & 3]);
+                    acc[i][j][r] = logit(acc[i][j][r], f[j], k[r >> 2][r & 3], o[r >> 2][r & 3]);
                     top[j] = fmaxf(top[j], acc[i][j][r]);
                 }
             if (tile >= a.kept_tiles) continue;
@@ -680,14 +730,16 @@ __global__ __launch_bounds__(kGemmThreads) void k_gemm(GemmArgs a) {
             const int64_t vt = (int64_t)bm * 8 + wm * 4 + i;
             if (vt >= a.m_tiles) continue;
             f32x4 o[4];
+            i32x4 k[4];
             offsets(vt, o);
+            exponents(vt, k);
 #pragma unroll
             for (int j = 0; j < kNf; ++j) {
                 const int64_t tt = (int64_t)bn * 8 + wn * kNf + j;
                 if (tt >= a.n_tiles) continue;
                 f32x16 z;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) z[r] = fmaf(acc[i][j][r], row[j].f, o[r >> 2][r & 3]);
+                for (int r = 0; r < 16; ++r) z[r] = logit(acc[i][j][r], row[j].f, k[r >> 2][r & 3], o[r >> 2][r & 3]);
                 terms.put(a, vt, tt, lane, z, row[j]);
             }
         }
@@ -702,6 +754,7 @@ struct JoinArgs {
     int shares;
     int64_t share, pitch, t;
     const float *xf, *o2;
+    const int* ek;       // (32-bit values: xf and ek are exponents) or NULL
     float2* part;        // [blocks of 1024 entries][t], or NULL
 };
 
@@ -724,7 +777,10 @@ __global__ __launch_bounds__(256) void k_join(JoinArgs a) {
         const f32x4 o = *(const f32x4*)(a.o2 + v);
         const float f = a.xf[t];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) z[r] = fmaf(z[r], f, o[r]), top = fmaxf(top, z[r]);
+        for (int r = 0; r < 4; ++r) {
+            z[r] = a.ek ? __builtin_amdgcn_ldexpf(z[r], __float_as_int(f) + a.ek[v + r]) + o[r] : fmaf(z[r], f, o[r]);
+            top = fmaxf(top, z[r]);
+        }
         *(f32x4*)at = z;
     }
     if (!a.part) return;
@@ -931,7 +987,7 @@ struct Plan {
     FewShape shape = {};
     int few_parts = 0;       // blocks of the gradients along the table
     int64_t o_z;             // kept logits
-    int64_t o_scale, o_xrow, o_fin, o_xf, o_ef, o_xl, o_o2, o_xn, o_xt, o_et, o_g, o_gt, o_part, o_dx, o_de, bytes;
+    int64_t o_scale, o_xrow, o_erow, o_ek, o_fin, o_xf, o_ef, o_xl, o_o2, o_xn, o_xt, o_et, o_g, o_gt, o_part, o_dx, o_de, bytes;
 };
 
 // Of G, and as much again of G^T: pieces of the table keep the workspace bounded, whatever t and v are, and larger ones
@@ -979,7 +1035,7 @@ Plan make_plan(const ccdpp_softmax_t& p, int call) {
         w.bytes = at;
         return w;
     }
-    w.o_scale = take(3 * kParts * 4);
+    w.o_scale = take(4 * kParts * 4);
     w.o_fin = take(64);
     w.o_xrow = take(w.scaled ? p.t * 4 : 0);
     if (w.small) {
@@ -1009,6 +1065,8 @@ Plan make_plan(const ccdpp_softmax_t& p, int call) {
         w.bytes = at;
         return w;
     }
+    w.o_erow = take(w.planes == 2 && !w.direct ? p.v * 4 : 0);
+    w.o_ek = take(w.planes == 2 ? w.vt * 32 * 4 : 0);
     w.ksd = (int)w.dt * 2;
     w.dp = round_up(p.d, 4);
     const int64_t row_bytes = w.tt * 32 * 2 * w.planes;
@@ -1156,7 +1214,7 @@ int run_wide(const ccdpp_softmax_t& p, const Plan& w, const Outs& out, const int
     z.a_plane = w.vt * w.ksd * kBlk, z.b_plane = w.tt * w.ksd * kBlk;
     z.a_tile = z.b_tile = (int64_t)w.ksd * kBlk;
     z.m_tiles = w.vt, z.n_tiles = w.tt, z.kb = w.ksd / 2, z.splits = 1;
-    z.t = p.t, z.v = p.v, z.xf = (const float*)(ws + w.o_xn), z.fin = fin, z.o2 = (const float*)(ws + w.o_o2);
+    z.t = p.t, z.v = p.v, z.xf = (const float*)(ws + w.o_xn), z.fin = fin, z.o2 = (const float*)(ws + w.o_o2), z.ek = (const int*)(ws + w.o_ek);
     z.scale = p.scale, z.offset = p.offset, z.target = p.target, z.target_bits = p.target_bits;
     float* const kept = (float*)(ws + w.o_z);
     const int64_t pitch = w.vt * 32, chunks = (pitch + 1023) / 1024;
@@ -1168,7 +1226,7 @@ int run_wide(const ccdpp_softmax_t& p, const Plan& w, const Outs& out, const int
         q.out = kept, q.out_split = p.t * pitch, q.ldo = q.cols = pitch, q.rows = p.t, q.splits = w.sz;
         k_gemm<P, PG, NPL, EPI_OUT, T><<<dim3(blocks, w.sz), kGemmThreads, 0, st>>>(q);
         OPS_LAUNCH("logits");
-        const JoinArgs j = {kept, w.sz, q.out_split, pitch, p.t, z.xf, z.o2, w.forward ? (float2*)(ws + w.o_part) : nullptr};
+        const JoinArgs j = {kept, w.sz, q.out_split, pitch, p.t, z.xf, z.o2, NPL == 2 ? z.ek : nullptr, w.forward ? (float2*)(ws + w.o_part) : nullptr};
         k_join<<<dim3((unsigned)chunks, (unsigned)p.t), 256, 0, st>>>(j);
         OPS_LAUNCH("logits");
     } else if (w.forward) {
@@ -1187,7 +1245,7 @@ int run_wide(const ccdpp_softmax_t& p, const Plan& w, const Outs& out, const int
     for (int64_t v0 = 0; v0 < p.v; v0 += w.vc) {
         const int64_t n = std::min(w.vc, p.v - v0), nt = (n + 31) / 32;
         GemmArgs q = z;
-        q.v0 = v0, q.a = z.a + v0 / 32 * z.a_tile, q.o2 = z.o2 + v0, q.m_tiles = nt;
+        q.v0 = v0, q.a = z.a + v0 / 32 * z.a_tile, q.o2 = z.o2 + v0, q.ek = z.ek + v0, q.m_tiles = nt;
         q.ksv = nt * 2, q.g_plane = w.tt * q.ksv * kBlk, q.gt_plane = nt * w.kst * kBlk;
         const unsigned tiles = (unsigned)((nt + 3) / 4 * w.tt);
         if (w.sz > 1 || w.direct) k_terms<PG, NPL><<<tiles, 256, 0, st>>>(q, kept + v0, pitch);
@@ -1235,10 +1293,12 @@ int run(const ccdpp_softmax_t& p, int call, const Outs& out, char* ws, hipStream
     }
     Scales sc;
     sc.e_part = (float*)(ws + w.o_scale), sc.x_part = sc.e_part + kParts, sc.g_part = sc.x_part + kParts;
+    sc.n_part = sc.g_part + kParts;
     sc.fin = (int32_t*)(ws + w.o_fin), sc.x_row = (float*)(ws + w.o_xrow);
+    sc.e_row = NPL == 2 && !w.small && !w.direct ? (float*)(ws + w.o_erow) : nullptr;
     const int32_t* fin = w.scaled || w.scale_g ? sc.fin : nullptr;
     if (w.scaled || w.scale_g) {
-        k_scales<T><<<kParts, 1024, 0, st>>>(p, out.grad, sc, w.scaled, w.grads);
+        k_scales<T><<<kParts, 1024, 0, st>>>(p, out.grad, sc, w.scaled, NPL == 2 && w.small, w.grads);
         OPS_LAUNCH("scales");
     }
 
@@ -1252,7 +1312,7 @@ int run(const ccdpp_softmax_t& p, int call, const Outs& out, char* ws, hipStream
         const int64_t rows = NPL * w.ksd * kBlk, turned = rows + kBlk;
         if (w.forward) x.nat = ws + w.o_xf, x.num = x.nat + rows;
         x.nat_row = x.num_row = w.x_tile;
-        e.nat = ws + w.o_ef, e.num = e.nat + rows, e.nat_row = e.num_row = w.e_tile;
+        e.nat = ws + w.o_ef, e.num = e.nat + rows, e.exps = e.num + kNumExp * 128, e.nat_row = e.num_row = w.e_tile;
         x.nat_plane = e.nat_plane = w.ksd * kBlk;
         if (w.grads) {
             x.live = ws + w.o_xl, x.live_num = x.live + rows, x.live_row = x.live_num_row = w.xlive_tile;
@@ -1264,7 +1324,7 @@ int run(const ccdpp_softmax_t& p, int call, const Outs& out, char* ws, hipStream
         if (!w.direct) x.nat = ws + w.o_xf, e.nat = ws + w.o_ef;
         x.nat_plane = w.tt * w.ksd * kBlk;
         e.nat_plane = w.vt * w.ksd * kBlk;
-        x.num = ws + w.o_xn, e.num = ws + w.o_o2, x.num_row = e.num_row = 128;
+        x.num = ws + w.o_xn, e.num = ws + w.o_o2, e.exps = ws + w.o_ek, x.num_row = e.num_row = 128;
         x.nat_row = e.nat_row = w.ksd * kBlk;
         if (w.grads) {
             x.turned = ws + w.o_xt, x.turned_plane = w.dt * w.kst * kBlk, x.turned_d = w.kst * kBlk;

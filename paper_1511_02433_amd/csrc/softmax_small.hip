@@ -140,7 +140,14 @@ __device__ __forceinline__ f32x16 row_numbers(const char* rows, int which, int h
 // first reference may be a finite mask's (-1e9), and what was added to that has lost its last digits.
 constexpr float kSumLimit = 1099511627776.f;
 
-// UNIT: the accumulated products are the logits (factor 1).
+// Logits from accumulated products of kept and streamed rows: `f` is x's number, `k` the table's exponent (32-bit values).
+template <int NPL>
+__device__ __forceinline__ float small_logit(float acc, float f, int k, float add) {
+    if constexpr (NPL == 2) return __builtin_amdgcn_ldexpf(acc, __float_as_int(f) + k) + add;
+    else return fmaf(acc, f, add);
+}
+
+// UNIT: the accumulated products are the logits (32-bit values whose rows have no powers of two of their own).
 template <class P, int NPL, int KS, bool UNIT>
 __device__ __forceinline__ void small_lse(const SmallArgs& a, int64_t first, int64_t last, const Kept<P, NPL, KS>& kept, float f, char* lds,
                                           float& ref_out, float& sum_out) {
@@ -157,8 +164,9 @@ __device__ __forceinline__ void small_lse(const SmallArgs& a, int64_t first, int
             if (UNIT && offsets) z += row_numbers(slot + S::kRows * kBlk, kNumOffset, h);
             z = tile_product<P, NPL, KS>(slot, kept, lane, z);
             if constexpr (!UNIT) {
+                const f32x16 k = NPL == 2 ? row_numbers(slot + S::kRows * kBlk, kNumExp, h) : f32x16{};
 #pragma unroll
-                for (int r = 0; r < 16; ++r) z[r] = fmaf(z[r], f, from);
+                for (int r = 0; r < 16; ++r) z[r] = small_logit<NPL>(z[r], f, __float_as_int(k[r]), from);
                 if (offsets) z += row_numbers(slot + S::kRows * kBlk, kNumOffset, h);
             }
             return z;
@@ -200,7 +208,7 @@ __global__ __launch_bounds__(256, small_lse_per_cu(NPL, KS)) void k_small_lse(Sm
         kept.load(mine, lane);
         const float f = *(const float*)(mine + S::kRows * kBlk + kNumFactor * 128 + n * 4);
         float top, sum;
-        if (NPL == 2 && __all(f == 1.f)) small_lse<P, NPL, KS, true>(a, first, last, kept, f, lds, top, sum);
+        if (NPL == 2 && !a.fin[3]) small_lse<P, NPL, KS, true>(a, first, last, kept, f, lds, top, sum);
         else small_lse<P, NPL, KS, false>(a, first, last, kept, f, lds, top, sum);
         const float top2 = __shfl_xor(top, 32), sum2 = __shfl_xor(sum, 32);
         const float m = fmaxf(top, top2), ref = m == -INFINITY ? 0.f : m;
@@ -222,7 +230,8 @@ __device__ __forceinline__ void small_terms(const SmallArgs& a, int64_t tile, in
     const float base = ITEMS ? own[kNumOffset * 32] : own[kNumLse * 32] + kTermExp;  // what this row adds to its logits
     const int own_y = ITEMS ? 0 : __float_as_int(own[kNumTarget * 32]);
     const bool any_base = !ITEMS || __any(base != 0.f);
-    const bool own_unit = __all(factor == 1.f || factor == 0.f);  // 0: a row that does not count
+    const int own_exp = ITEMS && NPL == 2 ? __float_as_int(own[kNumExp * 32]) : 0;
+    const bool unit = NPL == 2 && !a.fin[3];
     stream<S>(ITEMS ? a.xlive : a.e, ITEMS ? a.xlive_tile : a.e_tile, first, last, lds, [&](int64_t i, const char* slot) {
         const char* const rows = slot + S::kRows * kBlk;
         const int y = ITEMS ? ((const int*)rows)[kNumTarget * 32 + n] - (int)(tile * 32) : own_y - (int)(i * 32);
@@ -238,19 +247,14 @@ __device__ __forceinline__ void small_terms(const SmallArgs& a, int64_t tile, in
             }
             return add;
         };
-        bool unit = NPL == 2 && own_unit;
-        if constexpr (ITEMS && NPL == 2) {
-            const float f = ((const float*)rows)[kNumFactor * 32 + n];
-            unit = __all(f == 1.f || f == 0.f);
-        }
         f32x16 z = added();
         if (!unit) z = f32x16{};
         z = tile_product<P, NPL, KS>(slot, kept, lane, z);
         if (!unit) {
             const f32x16 add = added();
-            const f32x16 f = ITEMS ? row_numbers(rows, kNumFactor, h) : f32x16{};
+            const f32x16 f = ITEMS ? row_numbers(rows, kNumFactor, h) : NPL == 2 ? row_numbers(rows, kNumExp, h) : f32x16{};
 #pragma unroll
-            for (int r = 0; r < 16; ++r) z[r] = fmaf(z[r], ITEMS ? f[r] : factor, add[r]);
+            for (int r = 0; r < 16; ++r) z[r] = small_logit<NPL>(z[r], ITEMS ? f[r] : factor, ITEMS ? own_exp : __float_as_int(f[r]), add[r]);
         }
         // The first turned fragments arrive while the terms are computed.
         constexpr int kAhead = NPL == 2 ? 2 : 4;

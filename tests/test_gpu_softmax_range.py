@@ -87,3 +87,57 @@ def test_a_distance_softmax(t, d, dtype):
     offset = -0.5 * e.float().square().sum(1)
     loss, lse = ops().softmax_loss(x, e, y, offset=offset)
     check_loss(x, e, y, loss, lse, offset)
+
+
+SIZES32 = [(32, 1000, 40), (33, 1000, 40), (200, 1000, 128), (100, 700, 200), (200, 1000, 512), (400, 20_000, 160)]
+
+
+def grads64(x, e, y, z, lse, g, scale=1.0):
+    """(G, dx, dtable) in 64 bits."""
+    p = torch.exp(z - lse[:, None])
+    p[torch.arange(len(y), device="cuda"), y] -= 1
+    p = p * (g.double() * scale)[:, None]
+    return p, torch.mm(p, e.double()), torch.mm(p.t().contiguous(), x.double())
+
+
+@pytest.mark.parametrize("t,v,d", SIZES32)
+@pytest.mark.parametrize("size", [30.0, 1e3, 1e4])
+@pytest.mark.parametrize("where", ["an item", "a column of the table", "a whole item", "a row of x"])
+def test_one_large_value_costs_the_others_nothing(t, v, d, size, where):
+    """32-bit values; the other side holds zeros where the large ones are, so that no logit is large.  The planes hold 22 bits
+    of each value down to 2^-17 of its row's largest (1e4 is 2^13 here), so the tolerance is that of plain inputs."""
+    x, e, y = make(t, v, d, "f32", seed=d)
+    if where == "a row of x":
+        e[:, 3] = 0
+        x[5, 3] = size
+    else:
+        x[:, 3] = 0
+        if where == "an item":
+            e[v // 2, 3] = size
+        elif where == "a column of the table":
+            e[:, 3] *= size
+        else:
+            x[:, ::2] = 0
+            e[v // 2, ::2] *= size
+    loss, lse, dx, de = ops().softmax_loss_train(x, e, y)
+    z, want = check_loss(x, e, y, loss, lse)
+    g, wx, we = grads64(x, e, y, z, want, torch.ones(t, device="cuda"))
+    cols = [c for c in range(d) if c != 3] if where != "a whole item" else list(range(1, d, 2))
+    # 2e-5 as for plain inputs, of the terms' sum where they cancel
+    assert float((dx.double() - wx)[:, cols].norm()) <= 2e-5 * float(wx[:, cols].norm())
+    assert float((de.double() - we)[:, cols].norm()) <= 2e-5 * float(we[:, cols].norm())
+
+
+@pytest.mark.parametrize("t,v,d", SIZES32)
+def test_items_and_rows_of_very_different_sizes(t, v, d):
+    """Items and rows over eight powers of ten, their products still within 32 bits' reach: the small ones' logits are as near
+    to their own size as the large ones'."""
+    x, e, y = make(t, v, d, "f32", seed=d + 1)
+    e *= torch.logspace(-8, 0, v, device="cuda")[torch.randperm(v, device="cuda", generator=torch.Generator("cuda").manual_seed(3))][:, None]
+    x *= torch.logspace(-4, 0, t, device="cuda")[:, None]
+    loss, lse = ops().softmax_loss(x, e, y)
+    check_loss(x, e, y, loss, lse)
+    big = x * 1e6
+    small = e * 1e-6
+    loss, lse = ops().softmax_loss(big, small, y)
+    check_loss(big, small, y, loss, lse)
