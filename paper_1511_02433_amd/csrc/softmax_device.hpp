@@ -71,16 +71,17 @@ __device__ __forceinline__ void to_planes(float v, typename P::elem* out) {
     }
 }
 
-// The terms G of one lane, in planes of operand fragments.  Two half-precision planes are cut off toward zero, which pairs
-// of values share an instruction for: 2^-22 of the value is lost on average, 2^-20 at most.
+// The terms G of one lane, in planes of operand fragments, rounded to nearest (pairs of half-precision values share an
+// instruction): 22 bits of each term in two planes down to 2^-3, 2^-25 below it.
 template <class P, int NPL>
 __device__ __forceinline__ void split_terms(const float* g, typename P::vec (*pl)[2]) {
     if constexpr (NPL == 2 && std::is_same<P, HF>::value) {
-        typedef __fp16 half2_t __attribute__((ext_vector_type(2)));
+        typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
+        typedef float float2_t __attribute__((ext_vector_type(2)));
 #pragma unroll
         for (int r = 0; r < 16; r += 2) {
-            const half2_t hi = __builtin_amdgcn_cvt_pkrtz(g[r], g[r + 1]);
-            const half2_t lo = __builtin_amdgcn_cvt_pkrtz(g[r] - (float)hi[0], g[r + 1] - (float)hi[1]);
+            const half2_t hi = __builtin_convertvector((float2_t){g[r], g[r + 1]}, half2_t);
+            const half2_t lo = __builtin_convertvector((float2_t){g[r] - (float)hi[0], g[r + 1] - (float)hi[1]}, half2_t);
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 pl[0][r >> 3][(r & 7) + k] = (typename P::elem)hi[k];
@@ -116,6 +117,13 @@ __device__ __forceinline__ float wave_max(float m) {
     m = max_from<0x111, 0xf>(m), m = max_from<0x112, 0xf>(m), m = max_from<0x114, 0xf>(m), m = max_from<0x118, 0xf>(m);  // row_shr
     m = max_from<0x142, 0xa>(m), m = max_from<0x143, 0xc>(m);  // row_bcast:15, row_bcast:31
     return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, m), 63));
+}
+
+// The larger of a lane's value and that of the lane 32 places away.
+__device__ __forceinline__ float halves_max(float m) {
+    const uint32_t i = __float_as_uint(m);
+    const auto both = __builtin_amdgcn_permlane32_swap(i, i, false, false);
+    return fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
 }
 
 // 1 KB from global memory into LDS, 16 bytes per lane, without passing through registers.

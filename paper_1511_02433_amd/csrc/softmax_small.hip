@@ -218,18 +218,27 @@ __global__ __launch_bounds__(256, small_lse_per_cu(NPL, KS)) void k_small_lse(Sm
     });
 }
 
-// One side's gradients for 128 kept rows: out += turned streamed rows x G.  ITEMS: the kept rows are the table's.
+// Half-precision terms of an item whose largest one so far, in their common scale (at most 2^13), is below kTermLow or
+// above kTermHigh get a power of two of their own that brings it to 2^kTermStart: an item that is unlikely for every row,
+// or whose rows weigh little, keeps its digits (relative to its own largest term, two planes hold 2^-24 or better).
+constexpr float kTermLow = 0.5f, kTermHigh = 32768.f, kTermLeast = 7.9e-31f;  // (2^-100)
+constexpr int kTermStart = 7;
+
+// One side's gradients for 128 kept rows: out += turned streamed rows x G.  ITEMS: the kept rows are the table's; returns the
+// power of two that this lane's sums are yet to be multiplied with.
 // The accumulator of the logits starts at what is added to them, so that a term costs its exponential alone.
 template <class P, int NPL, int KS, bool ITEMS>
-__device__ __forceinline__ void small_terms(const SmallArgs& a, int64_t tile, int64_t first, int64_t last, const Kept<P, NPL, KS>& kept, const float* own, char* lds,
+__device__ __forceinline__ int small_terms(const SmallArgs& a, int64_t tile, int64_t first, int64_t last, const Kept<P, NPL, KS>& kept, const float* own, char* lds,
                                             f32x16* out) {
     typedef Stream<P, NPL, KS, true> S;
     constexpr int DT = S::DT;
     const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
     const float factor = own[kNumFactor * 32];                                     // x
-    const float base = ITEMS ? own[kNumOffset * 32] : own[kNumLse * 32] + kTermExp;  // what this row adds to its logits
+    float base = ITEMS ? own[kNumOffset * 32] : own[kNumLse * 32] + kTermExp;  // what this row adds to its logits
     const int own_y = ITEMS ? 0 : __float_as_int(own[kNumTarget * 32]);
-    const bool any_base = !ITEMS || __any(base != 0.f);
+    constexpr bool MOVES = ITEMS && std::is_same<P, HF>::value;
+    int ref = 0;       // MOVES: terms are taken times 2^-ref
+    float most = 0.f;  // and the largest one so far
     const int own_exp = ITEMS && NPL == 2 ? __float_as_int(own[kNumExp * 32]) : 0;
     const bool unit = NPL == 2 && !a.fin[3];
     stream<S>(ITEMS ? a.xlive : a.e, ITEMS ? a.xlive_tile : a.e_tile, first, last, lds, [&](int64_t i, const char* slot) {
@@ -239,7 +248,7 @@ __device__ __forceinline__ void small_terms(const SmallArgs& a, int64_t tile, in
             f32x16 add;
             if constexpr (ITEMS) {
                 add = row_numbers(rows, kNumTerm, h);
-                if (any_base) add += base;
+                if (__any(base != 0.f)) add += base;
             } else {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) add[r] = base;
@@ -272,13 +281,33 @@ __device__ __forceinline__ void small_terms(const SmallArgs& a, int64_t tile, in
         if constexpr (ITEMS) {
             if (__any(y >= 0 && y < 32)) {  // popular items: nearly every tile
                 const f32x16 ys = row_numbers(rows, kNumTarget, h), ws = row_numbers(rows, kNumWeight, h);
+                const float up = MOVES ? pow2i(-ref) : 1.f;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) g[r] -= __float_as_int(ys[r]) == (int)(tile * 32) + n ? ws[r] : 0.f;
+                for (int r = 0; r < 16; ++r) g[r] = fmaf(__float_as_int(ys[r]) == (int)(tile * 32) + n ? ws[r] : 0.f, -up, g[r]);
             }
         } else {
             if (__any(y >= 0 && y < 32)) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) g[r] -= y == 8 * (r >> 2) + 4 * h + (r & 3) ? (float)(1 << kTermExp) : 0.f;
+            }
+        }
+        if constexpr (MOVES) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) most = fmaxf(most, fabsf(g[r]));
+            // (none, and terms below 2^-113 of the largest weight, stay as they are)
+            const auto moves = [&]() { return most > kTermHigh || (most < kTermLow && most > kTermLeast); };
+            if (__any(moves())) {
+                most = halves_max(most);
+                const bool mine = moves() && finite(most);
+                const int up = mine ? kTermStart - ((int)(__float_as_uint(most) >> 23) - 127) : 0;
+                if (__any(mine)) {
+                    const float f = pow2i(up);
+                    ref -= up, base += (float)up, most *= f;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) g[r] *= f;
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) out[d] *= f;
+                }
             }
         }
         // Two planes of G for 16-bit types too: the products are not what bounds these, and one plane's rounding would
@@ -298,6 +327,7 @@ __device__ __forceinline__ void small_terms(const SmallArgs& a, int64_t tile, in
         interleave<DT * 2, NPL, NPL + 1, kAhead, (kAhead < DT * 2 ? kAhead : DT * 2)>();
         __builtin_amdgcn_sched_barrier(0);
     });
+    return ref;
 }
 
 // What the sums are multiplied with, one after the other: G's power of two is taken off, and the other operand's.
@@ -317,9 +347,9 @@ __device__ __forceinline__ void small_grad(const SmallArgs& a, int64_t share, ch
         kept.load(mine, lane);
         const float* const own = (const float*)(mine + S::kRows * kBlk) + n;
         f32x16 out[DT] = {};
-        small_terms<P, NPL, KS, ITEMS>(a, tile, first, last, kept, own, lds, out);
+        const int ref = small_terms<P, NPL, KS, ITEMS>(a, tile, first, last, kept, own, lds, out);
         if (at >= tiles) return;
-        const float w = ITEMS ? 1.f : own[kNumRaw * 32];
+        const float w = ITEMS ? pow2i(ref) : own[kNumRaw * 32];
         const SmallOut& o = ITEMS ? a.de_out : a.dx_out;
         if (first == 0 && last == (ITEMS ? a.de : a.dx).tiles) {  // nothing to add: the result itself
             typedef typename std::conditional<NPL == 2, float, typename P::elem>::type T;

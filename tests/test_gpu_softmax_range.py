@@ -141,3 +141,63 @@ def test_items_and_rows_of_very_different_sizes(t, v, d):
     small = e * 1e-6
     loss, lse = ops().softmax_loss(big, small, y)
     check_loss(big, small, y, loss, lse)
+
+
+def check_rows(got, want, terms, dtype, z):
+    """Each row of a gradient against its own size.  got_v = sum_t G_tv x_t: every term has the probability's relative error,
+    1e-6 (1 + z), and that of its representation, 2^-20 (two planes) or 2^-11 (one); what is compared with is the 2-norm of
+    `terms`, sum_t |G_tv| |x_t|, as terms may cancel.  The result is rounded once, by 2^-24, 2^-8 or 2^-11 of
+    itself (half precision: 2^-25 at least)."""
+    tol = {"f32": 2.0 ** -20, "bf16": 2.0 ** -11, "f16": 2.0 ** -11}[dtype] + 1e-6 * (1 + z)
+    once = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}[dtype]
+    floor = 2.0 ** -25 * math.sqrt(got.shape[1]) if dtype == "f16" else 1e-38
+    off = (got.double() - want).norm(dim=1) - (tol * terms.norm(dim=1) + once * want.norm(dim=1) + floor)
+    assert float(off.max()) <= 0.0, (int(off.argmax()), float(((got.double() - want).norm(dim=1) / terms.norm(dim=1)).nan_to_num().max()))
+
+
+# rows, items, factors: few rows; few factors
+ROWS = [(8, 600, 40), (20, 600, 200), (33, 600, 40), (300, 600, 128), (500, 5000, 17)]
+
+
+def rare_items(t, v, d, dtype, offsets, seed):
+    x, e, y = make(t, v, d, dtype, seed=seed)
+    offset = torch.zeros(v, device="cuda")
+    which = torch.arange(3, v, 11, device="cuda")
+    offset[which] = torch.tensor(offsets, device="cuda")[torch.arange(len(which), device="cuda") % len(offsets)]
+    y = torch.where(offset[y] < 0, (y + 1) % v, y)
+    assert not bool((offset[y] < 0).any())
+    return x, e, y, offset
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("t,v,d", ROWS)
+def test_items_that_are_unlikely_for_every_row(t, v, d, dtype):
+    """An item's gradient is as near to its own size as a popular one's: rare tokens are learned from it and nothing else."""
+    offsets = [-4.0, -8.0, -14.0] if dtype == "f16" else [-4.0, -8.0, -12.0, -16.0, -20.0, -30.0, -60.0]
+    x, e, y, offset = rare_items(t, v, d, dtype, offsets, seed=t)
+    g = torch.full((t,), 2000.0 if dtype == "f16" else 1.0, device="cuda")
+    loss, lse, dx, de = ops().softmax_loss_train(x, e, y, grad=g, offset=offset)
+    z, want = check_loss(x, e, y, loss, lse, offset)
+    p, wx, we = grads64(x, e, y, z, want, g)
+    size = float(z.abs().max())
+    check_rows(de, we, torch.mm(p.abs().t().contiguous(), x.double().abs()), dtype, size)
+    check_rows(dx, wx, torch.mm(p.abs(), e.double().abs()), dtype, size)
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("t,v,d", ROWS)
+@pytest.mark.parametrize("negative", [False, True])
+def test_weights_of_very_different_sizes(t, v, d, dtype, negative):
+    """Seven powers of ten (half precision: six): every row's dx by its own weight, every item's gradient by its rows'."""
+    x, e, y, offset = rare_items(t, v, d, dtype, [-3.0, -10.0], seed=t + 1)
+    gen = torch.Generator(device="cuda").manual_seed(t)
+    g = 10.0 ** (torch.rand(t, generator=gen, device="cuda") * (6 if dtype == "f16" else 7) - (3 if dtype == "f16" else 7))
+    if negative:
+        g[::3] *= -1
+        g[1] = 0
+    loss, lse, dx, de = ops().softmax_loss_train(x, e, y, grad=g, offset=offset)
+    z, want = check_loss(x, e, y, loss, lse, offset)
+    p, wx, we = grads64(x, e, y, z, want, g)
+    size = float(z.abs().max())
+    check_rows(dx, wx, torch.mm(p.abs(), e.double().abs()), dtype, size)
+    check_rows(de, we, torch.mm(p.abs().t().contiguous(), x.double().abs()), dtype, size)
