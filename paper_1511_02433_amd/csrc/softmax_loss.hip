@@ -359,20 +359,38 @@ struct GemmArgs {
     char *g, *gt;                // G [plane][t/32][ksv], G^T [plane][v/32][kst] fragments, or NULL
     int64_t g_plane, gt_plane;
     int64_t ksv, kst;
+    uint8_t* lev;                // powers of two of G^T's items, of 64 rows each: [v/32][t/64][32]
+    int* item_e;                 // those of all rows, [v/32][32]
     // other products
     float* out;                  // [split][N][ldo]: of a gradient's rows; M are its columns
     void* last;                  // or the result itself
     int wide;                    // its rows are aligned to four values
     int64_t out_split, rows, cols, ldo;
     int add, which;              // which: the exponent in fin of the other operand, or -1
+    int own;                     // whether the rows' terms have powers of two of their own: kRowsOwn (from grad), kItemsOwn (item_e)
 };
+enum { kNoneOwn = 0, kRowsOwn = 1, kItemsOwn = 2 };
 
 constexpr int kStages = 4;          // of LDS
 constexpr int kStage = 32 * kBlk;
 
+// Terms are held in half precision (one plane or two), largest weight at 2^12 .. 2^13, and what they are multiplied with has
+// a power of two of its own for all its rows.  So that neither a row that weighs little nor an item that is unlikely for every
+// row loses its digits to the others: terms of a row whose weight is below kLight of that scale are taken times 2^light_exp
+// (in G, for dx); and those of an item whose largest one is below kItemLow among 64 rows times a power of its own (in G^T,
+// for dtable: k_levels brings an item's groups of 64 rows to one power).  Both come off the gradients' rows.  Above these
+// limits a term's last place, 2^-24, is 2^-18 of its item's largest term or better.
+constexpr float kLight = 16.f, kItemLow = 0.015625f;
+constexpr int kNoTerms = 255;   // in lev: no terms in these rows
+__device__ __forceinline__ int light_exp(float w) {  // w: weight in G's scale
+    const float a = fabsf(w);
+    return a < kLight && a > 0.f ? min(12 + 127 - (int)(__float_as_uint(a) >> 23), 120) : 0;
+}
+
 // What a row's terms G = w (2^(logit - l2) - [target]) take.
 struct TermRow {
     float w = 0.f, l2 = 0.f, f = 0.f;
+    int light = 0;       // w has this power of two of its own
     int64_t y = -1;      // target, from the first table entry of the piece
     uint32_t keep = 0;   // all ones in rows that count: others are cut off as bits, whatever they hold
     __device__ __forceinline__ void load(const GemmArgs& a, int64_t t) {
@@ -382,7 +400,9 @@ struct TermRow {
         if (!row_counts(yt, a.v, a.offset)) return;
         keep = ~0u;
         w = a.grad ? a.grad[t] : 1.f;
-        if (a.fin) w = ldexpf(w, a.fin[2]);
+        w = ldexpf(w, a.fin[2]);
+        light = light_exp(w);
+        w = ldexpf(w, light);
         if (yt >= a.v) w = NAN;
         l2 = a.lse[t] * kLog2e;
         y = yt - a.v0;
@@ -400,8 +420,9 @@ struct TermBlocks {
 #pragma unroll
             for (int k = 0; k < 8; ++k) eye[s][k] = (typename PG::elem)(16 * s + (k < 4 ? 4 * h + k : 8 + 4 * h + k - 4) == n ? 1.f : 0.f);
     }
-    // z: logits in base 2, lane (n, h): row n, entries 8 q + 4 h + r.
-    __device__ __forceinline__ void put(const GemmArgs& a, int64_t vt, int64_t tt, int lane, const f32x16& z, const TermRow& row) const {
+    // z: logits in base 2, lane (n, h): row n, entries 8 q + 4 h + r.  Returns the largest term of the lane's item n among
+    // its 16 rows of G^T (0 where that is not asked for).
+    __device__ __forceinline__ float put(const GemmArgs& a, int64_t vt, int64_t tt, int lane, const f32x16& z, const TermRow& row) const {
         const int h = lane >> 5;
         float g[16];
 #pragma unroll
@@ -412,16 +433,80 @@ struct TermBlocks {
             for (int r = 0; r < 16; ++r)
                 if (at == 8 * (r >> 2) + 4 * h + (r & 3)) g[r] -= row.w;
         }
+        return write(a, vt, tt, lane, g, row.keep, a.g);
+    }
+
+    // The terms of 64 rows (two tiles; the second one may not be there), and their items' power of two.
+    __device__ __forceinline__ void put_pair(const GemmArgs& a, int64_t vt, int64_t tt, int lane, const f32x16& z0, const f32x16& z1, bool two,
+                                             const TermRow& row0, const TermRow& row1) const {
+        float top = put(a, vt, tt, lane, z0, row0);
+        if (two) top = fmaxf(top, put(a, vt, tt + 1, lane, z1, row1));
+        if (!a.gt) return;
+        top = halves_max(top);
+        int own = 0;
+        if (__any((row0.light | row1.light) != 0) || __any(top < kItemLow && a.o2[vt * 32 + (lane & 31)] != -INFINITY))
+            own = put_again(a, vt, tt, lane, z0, z1, two, row0, row1);
+        if (lane < 32) {
+            if (a.lev) a.lev[(vt * ((a.n_tiles + 1) / 2) + tt / 2) * 32 + lane] = (uint8_t)own;
+            else a.item_e[vt * 32 + lane] = own == kNoTerms ? 0 : own;
+        }
+    }
+
+    // G^T once more, each item's terms by the power of two that brings its largest one above 1; returns that of item `lane`.
+    __device__ int put_again(const GemmArgs& a, int64_t vt, int64_t tt, int lane, const f32x16& z0, const f32x16& z1, bool two, const TermRow& row0,
+                             const TermRow& row1) const {
+        const int h = lane >> 5;
+        const float w0 = row0.keep ? log2f(fabsf(row0.w)) - (float)row0.light : -INFINITY;
+        const float w1 = row1.keep && two ? log2f(fabsf(row1.w)) - (float)row1.light : -INFINITY;
+        const int64_t y0 = row0.y - vt * 32, y1 = row1.y - vt * 32;
+        int own[16], mine = 0;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int item = 8 * (r >> 2) + 4 * h + (r & 3);
+            float c = w0 == -INFINITY ? -INFINITY : fmaxf(z0[r] - row0.l2 + w0, y0 == item ? w0 : -INFINITY);
+            if (w1 != -INFINITY) c = fmaxf(c, fmaxf(z1[r] - row1.l2 + w1, y1 == item ? w1 : -INFINITY));
+            // the largest among the 32 lanes of either half
+            c = max_from<0x111, 0xf>(c), c = max_from<0x112, 0xf>(c), c = max_from<0x114, 0xf>(c), c = max_from<0x118, 0xf>(c);
+            c = max_from<0x142, 0xa>(c);
+            const int i = __builtin_bit_cast(int, c);
+            const float low = __builtin_bit_cast(float, __builtin_amdgcn_readlane(i, 31)), high = __builtin_bit_cast(float, __builtin_amdgcn_readlane(i, 63));
+            const auto power = [](float top) {  // multiples of 8, so that neighbouring groups of rows mostly agree
+                if (top == -INFINITY) return kNoTerms;
+                return top < -6.f ? (int)fminf(8.f * ceilf((4.f - top) * 0.125f), 112.f) : 0;
+            };
+            const int p0 = power(low), p1 = power(high);
+            own[r] = h ? p1 : p0;
+            const int first = 8 * (r >> 2) + (r & 3);
+            if (lane == first) mine = p0;
+            if (lane == first + 4) mine = p1;
+        }
+        const auto tile = [&](int64_t tt, const f32x16& z, const TermRow& row, int64_t y) {
+            float g[16];
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int up = (own[r] == kNoTerms ? 0 : own[r]) - row.light;
+                g[r] = row.w * exp2_fast(z[r] - row.l2 + (float)up);
+                if (y == 8 * (r >> 2) + 4 * h + (r & 3)) g[r] -= __builtin_amdgcn_ldexpf(row.w, up);
+            }
+            write(a, vt, tt, lane, g, row.keep, nullptr);
+        };
+        tile(tt, z0, row0, y0);
+        if (two) tile(tt + 1, z1, row1, y1);
+        return mine;
+    }
+
+    __device__ __forceinline__ float write(const GemmArgs& a, int64_t vt, int64_t tt, int lane, const float* g, uint32_t keep, char* to_g) const {
         typename PG::vec pl[NPL][2];
+        float top = 0.f;
         split_terms<PG, NPL>(g, pl);
 #pragma unroll
         for (int k = 0; k < NPL; ++k) {
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 u32x4 bits = __builtin_bit_cast(u32x4, pl[k][s]);
-                bits &= row.keep;
+                bits &= keep;
                 pl[k][s] = __builtin_bit_cast(typename PG::vec, bits);
-                if (a.g) *(u32x4*)(a.g + k * a.g_plane + (tt * a.ksv + vt * 2 + s) * kBlk + lane * 16) = bits;
+                if (to_g) *(u32x4*)(to_g + k * a.g_plane + (tt * a.ksv + vt * 2 + s) * kBlk + lane * 16) = bits;
             }
             if (!a.gt) continue;
             f32x16 tr = {};
@@ -430,9 +515,13 @@ struct TermBlocks {
             typename PG::vec to[2];
 #pragma unroll
             for (int r = 0; r < 16; ++r) to[r >> 3][r & 7] = (typename PG::elem)tr[r];
+            if (k == 0)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) top = fmaxf(top, fabsf(tr[r]));
 #pragma unroll
             for (int s = 0; s < 2; ++s) *(typename PG::vec*)(a.gt + k * a.gt_plane + (vt * a.kst + tt * 2 + s) * kBlk + lane * 16) = to[s];
         }
+        return top;
     }
 };
 
@@ -578,7 +667,13 @@ __global__ __launch_bounds__(kGemmThreads) void k_gemm(GemmArgs a) {
     if constexpr (EPI == EPI_OUT) {
         // The product is the gradient turned: a lane has four neighbouring columns of a row at a time.
         // Last piece and only share: the caller's type.  Else 32 bits, added to what earlier pieces left.
-        const float fg = a.fin ? ldexpf(1.f, -a.fin[2]) : 1.f, f = a.fin && a.which >= 0 ? ldexpf(a.scale, -a.fin[a.which]) : a.scale;
+        // The terms' powers of two and the other operand's are taken off one after the other.
+        const int eg = a.fin ? a.fin[2] : 0;
+        const float f = a.fin && a.which >= 0 ? ldexpf(a.scale, -a.fin[a.which]) : a.scale;
+        const auto row_exp = [&](int64_t row) {
+            if (a.own == kItemsOwn) return a.item_e[row];
+            return a.own == kRowsOwn && a.grad ? light_exp(ldexpf(a.grad[row], eg)) : 0;
+        };
         if (a.last && !a.wide) {
             // Rows that are not aligned to four values (stores across them take longer: 50,021 x 777 in half
             // precision 161 us against 142): 32 rows of the wave's 128 columns at a time through LDS (quads of columns swapped
@@ -588,17 +683,18 @@ __global__ __launch_bounds__(kGemmThreads) void k_gemm(GemmArgs a) {
             const int64_t col0 = ((int64_t)bm * 8 + wm * 4) * 32;
 #pragma unroll
             for (int j = 0; j < kNf; ++j) {
+                const int64_t row0 = ((int64_t)bn * 8 + wn * kNf + j) * 32;
+                const int e = eg + row_exp(min(row0 + n, a.rows - 1));
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         f32x4 v;
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) v[r] = acc[i][j][4 * q + r] * fg * f;
+                        for (int r = 0; r < 4; ++r) v[r] = __builtin_amdgcn_ldexpf(acc[i][j][4 * q + r], -e) * f;
                         *(f32x4*)(mine + n * 128 + ((i * 8 + 2 * q + h) ^ n) * 4) = v;
                     }
                 __builtin_amdgcn_wave_barrier();
-                const int64_t row0 = ((int64_t)bn * 8 + wn * kNf + j) * 32;
                 const int rows = (int)min((int64_t)32, a.rows - row0);
 #pragma unroll 4
                 for (int r = 0; r < rows; ++r)
@@ -615,6 +711,7 @@ __global__ __launch_bounds__(kGemmThreads) void k_gemm(GemmArgs a) {
         for (int j = 0; j < kNf; ++j) {
             const int64_t row = ((int64_t)bn * 8 + wn * kNf + j) * 32 + n;
             if (row >= a.rows) continue;
+            const int e = row_exp(row) + (a.last ? eg : 0);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -623,7 +720,7 @@ __global__ __launch_bounds__(kGemmThreads) void k_gemm(GemmArgs a) {
                     if (col >= a.cols) continue;
                     f32x4 v;
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) v[r] = acc[i][j][4 * q + r];
+                    for (int r = 0; r < 4; ++r) v[r] = __builtin_amdgcn_ldexpf(acc[i][j][4 * q + r], -e);
                     if (!a.last) {  // columns of partial sums are a multiple of four
                         f32x4* const o = (f32x4*)(a.out + split * a.out_split + row * a.ldo + col);
                         *o = a.add ? *o + v : v;
@@ -631,7 +728,7 @@ __global__ __launch_bounds__(kGemmThreads) void k_gemm(GemmArgs a) {
                     }
                     Run<T, 4> t;
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) t.v[r] = (T)(v[r] * fg * f);
+                    for (int r = 0; r < 4; ++r) t.v[r] = (T)(v[r] * f);
                     T* const o = (T*)a.last + row * a.ldo + col;
                     if (col + 4 <= a.cols) {
                         store_run<4>(o, t);
@@ -721,27 +818,52 @@ __global__ __launch_bounds__(kGemmThreads) void k_gemm(GemmArgs a) {
         return;
     }
     if constexpr (EPI == EPI_G) {
+        __syncthreads();  // LDS is free
         const TermBlocks<PG, NPL> terms(lane);
         TermRow row[kNf];
 #pragma unroll
         for (int j = 0; j < kNf; ++j) row[j].load(a, ((int64_t)bn * 8 + wn * kNf + j) * 32 + n);
+        const int64_t tt = (int64_t)bn * 8 + wn * kNf;  // (even)
+        if (tt >= a.n_tiles) return;
+        // Logits go through LDS, half of the wave's at a time, and the terms' code is there once: unrolled, what rare groups
+        // take would not fit the registers.
+        f32x4* const mine = (f32x4*)(lds + wave * (16 * kBlk)) + lane;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int64_t vt = (int64_t)bm * 8 + wm * 4 + i;
-            if (vt >= a.m_tiles) continue;
-            f32x4 o[4];
-            i32x4 k[4];
-            offsets(vt, o);
-            exponents(vt, k);
+        for (int i0 = 0; i0 < 4; i0 += 2) {
 #pragma unroll
-            for (int j = 0; j < kNf; ++j) {
-                const int64_t tt = (int64_t)bn * 8 + wn * kNf + j;
-                if (tt >= a.n_tiles) continue;
-                f32x16 z;
+            for (int i = i0; i < i0 + 2; ++i) {
+                const int64_t vt = min((int64_t)bm * 8 + wm * 4 + i, a.m_tiles - 1);
+                f32x4 o[4];
+                i32x4 k[4];
+                offsets(vt, o);
+                exponents(vt, k);
 #pragma unroll
-                for (int r = 0; r < 16; ++r) z[r] = logit(acc[i][j][r], row[j].f, k[r >> 2][r & 3], o[r >> 2][r & 3]);
-                terms.put(a, vt, tt, lane, z, row[j]);
+                for (int j = 0; j < kNf; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        f32x4 four;
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) four[r] = logit(acc[i][j][4 * q + r], row[j].f, k[q][r], o[q][r]);
+                        mine[(((i - i0) * kNf + j) * 4 + q) * 64] = four;
+                    }
             }
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+            for (int i = i0; i < i0 + 2; ++i) {
+                const int64_t vt = (int64_t)bm * 8 + wm * 4 + i;
+                if (vt >= a.m_tiles) break;
+                f32x16 z[kNf];
+#pragma unroll
+                for (int j = 0; j < kNf; ++j)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const f32x4 four = mine[(((i - i0) * kNf + j) * 4 + q) * 64];
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) z[j][4 * q + r] = four[r];
+                    }
+                terms.put_pair(a, vt, tt, lane, z[0], z[1], tt + 1 < a.n_tiles, row[0], row[1]);
+            }
+            __builtin_amdgcn_wave_barrier();
         }
     }
 }
@@ -799,27 +921,63 @@ __global__ __launch_bounds__(256) void k_join(JoinArgs a) {
     if (threadIdx.x == 0) a.part[blockIdx.x * a.t + t] = make_float2(top, red[0][1] + red[1][1] + red[2][1] + red[3][1]);
 }
 
-// The terms of 32 x 32 logits a wave: from rows (pitch), or from what k_gemm kept (pitch 0; v0 is the piece's first
+// The terms of 64 rows x 32 entries a wave: from rows (pitch), or from what k_gemm kept (pitch 0; v0 is the piece's first
 // entry).  Bound by memory (2,000 x 32,003 in two planes: 143 us, 5.4 TB/s).
 template <class PG, int NPL>
 __global__ __launch_bounds__(256) void k_terms(GemmArgs a, const float* z, int64_t pitch) {
     const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
     const uint32_t across = (uint32_t)((a.m_tiles + 3) / 4);
-    const int64_t vt = (int64_t)(blockIdx.x % across) * 4 + (threadIdx.x >> 6), tt = blockIdx.x / across;
+    const int64_t vt = (int64_t)(blockIdx.x % across) * 4 + (threadIdx.x >> 6), tt = blockIdx.x / across * 2;
     if (vt >= a.m_tiles) return;
-    const float* const from = pitch ? z + min(tt * 32 + n, a.t - 1) * pitch + vt * 32 + 4 * h : a.kept + (tt * a.kept_tiles + a.v0 / 32 + vt) * 1024 + lane * 4;
+    const bool two = tt + 1 < a.n_tiles;
     const int step = pitch ? 8 : 256;
-    f32x16 q;
+    f32x16 q[2];
+    TermRow row[2];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const f32x4 four = *(const f32x4*)(from + step * k);
+    for (int j = 0; j < 2; ++j) {
+        const int64_t at = two ? tt + j : tt;
+        const float* const from = pitch ? z + min(at * 32 + n, a.t - 1) * pitch + vt * 32 + 4 * h : a.kept + (at * a.kept_tiles + a.v0 / 32 + vt) * 1024 + lane * 4;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) q[4 * k + r] = four[r];
+        for (int k = 0; k < 4; ++k) {
+            const f32x4 four = *(const f32x4*)(from + step * k);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) q[j][4 * k + r] = four[r];
+        }
     }
+    row[0].load(a, tt * 32 + n);
+    if (two) row[1].load(a, tt * 32 + 32 + n);
     const TermBlocks<PG, NPL> terms(lane);
-    TermRow row;
-    row.load(a, tt * 32 + n);
-    terms.put(a, vt, tt, lane, q, row);
+    terms.put_pair(a, vt, tt, lane, q[0], q[1], two, row[0], row[1]);
+}
+
+// One power of two for each item over all groups of 64 rows, the lowest of theirs: fragments of G^T that have another one are
+// brought to it (most have none of their own, and nothing is moved).  A block per 32 items.
+template <int NPL>
+__global__ __launch_bounds__(256) void k_levels(GemmArgs a) {
+    __shared__ int low[8][32];
+    const int item = threadIdx.x & 31, part = threadIdx.x >> 5, groups = (int)((a.n_tiles + 1) / 2);
+    const uint8_t* const lev = a.lev + (int64_t)blockIdx.x * groups * 32;
+    int least = kNoTerms;
+    for (int g = part; g < groups; g += 8) least = min(least, (int)lev[g * 32 + item]);
+    low[part][item] = least;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 8; ++k) least = min(least, low[k][item]);
+    if (part == 0) a.item_e[(int64_t)blockIdx.x * 32 + item] = least == kNoTerms ? 0 : least;
+    const int lane = threadIdx.x & 63;
+    for (int g = threadIdx.x >> 6; g < groups; g += 4) {
+        const int own = lev[g * 32 + item], down = own == kNoTerms ? 0 : own - least;
+        if (!__any(down != 0)) continue;
+        for (int tt = 2 * g; tt < min(2 * g + 2, (int)a.n_tiles); ++tt)
+#pragma unroll
+            for (int i = 0; i < 2 * NPL; ++i) {
+                f16x8* const at = (f16x8*)(a.gt + (i >> 1) * a.gt_plane + (blockIdx.x * a.kst + tt * 2 + (i & 1)) * kBlk + lane * 16);
+                f16x8 v = *at;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] = (_Float16)__builtin_amdgcn_ldexpf((float)v[k], -down);
+                *at = v;
+            }
+    }
 }
 
 // ---- ends ------------------------------------------------------------------------------------
@@ -987,6 +1145,7 @@ struct Plan {
     FewShape shape = {};
     int few_parts = 0;       // blocks of the gradients along the table
     int64_t o_z;             // kept logits
+    int64_t o_lev, o_item;
     int64_t o_scale, o_xrow, o_erow, o_ek, o_fin, o_xf, o_ef, o_xl, o_o2, o_xn, o_xt, o_et, o_g, o_gt, o_part, o_dx, o_de, bytes;
 };
 
@@ -1107,6 +1266,8 @@ Plan make_plan(const ccdpp_softmax_t& p, int call) {
         w.o_et = take(w.planes * w.dt * w.ksv * kBlk);
         w.o_g = take(w.planes * w.tt * (w.vc / 16) * kBlk);
         w.o_gt = take(w.planes * (w.vc / 32) * w.kst * kBlk);
+        w.o_lev = take(w.tt > 2 ? (w.tt + 1) / 2 * w.vc : 0);
+        w.o_item = take(w.vc * 4);
         w.o_dx = take(p.v <= w.vc && w.sx == 1 ? 0 : w.sx * p.t * w.dp * 4);
         w.o_de = take(w.se == 1 ? 0 : w.se * w.vc * w.dp * 4);
     }
@@ -1241,25 +1402,30 @@ int run_wide(const ccdpp_softmax_t& p, const Plan& w, const Outs& out, const int
     z.lse = w.forward ? out.lse : out.lse_in, z.grad = out.grad;
     z.g = out.dx ? ws + w.o_g : nullptr, z.gt = out.de ? ws + w.o_gt : nullptr;
     z.kst = w.kst;
+    z.lev = w.tt > 2 ? (uint8_t*)(ws + w.o_lev) : nullptr, z.item_e = (int*)(ws + w.o_item);
     const bool dx_whole = p.v <= w.vc && w.sx == 1;
     for (int64_t v0 = 0; v0 < p.v; v0 += w.vc) {
         const int64_t n = std::min(w.vc, p.v - v0), nt = (n + 31) / 32;
         GemmArgs q = z;
         q.v0 = v0, q.a = z.a + v0 / 32 * z.a_tile, q.o2 = z.o2 + v0, q.ek = z.ek + v0, q.m_tiles = nt;
         q.ksv = nt * 2, q.g_plane = w.tt * q.ksv * kBlk, q.gt_plane = nt * w.kst * kBlk;
-        const unsigned tiles = (unsigned)((nt + 3) / 4 * w.tt);
+        const unsigned tiles = (unsigned)((nt + 3) / 4 * ((w.tt + 1) / 2));
         if (w.sz > 1 || w.direct) k_terms<PG, NPL><<<tiles, 256, 0, st>>>(q, kept + v0, pitch);
         else if (v0 < w.kept) k_terms<PG, NPL><<<tiles, 256, 0, st>>>(q, nullptr, 0);
         else k_gemm<P, PG, NPL, EPI_G, T><<<(unsigned)((nt + 7) / 8 * ((w.tt + 7) / 8)), kGemmThreads, 0, st>>>(q);
         OPS_LAUNCH("G");
+        if (out.de && z.lev) {
+            k_levels<NPL><<<(unsigned)nt, 256, 0, st>>>(q);
+            OPS_LAUNCH("G");
+        }
         GemmArgs o = {};
-        o.m_tiles = w.dt, o.cols = p.d, o.scale = p.scale, o.fin = fin;
+        o.m_tiles = w.dt, o.cols = p.d, o.scale = p.scale, o.fin = fin, o.grad = out.grad, o.item_e = z.item_e;
         const auto wide = [](const void* at, int64_t ld) { return ((uintptr_t)at | (uintptr_t)(ld * sizeof(T))) % (4 * sizeof(T)) == 0; };
         if (out.dx) {
             o.a = ws + w.o_et + v0 / 16 * kBlk, o.a_plane = w.dt * w.ksv * kBlk, o.a_tile = w.ksv * kBlk;
             o.b = z.g, o.b_plane = q.g_plane, o.b_tile = q.ksv * kBlk, o.n_tiles = w.tt, o.rows = p.t;
             o.kb = nt, o.splits = w.sx, o.out = (float*)(ws + w.o_dx), o.out_split = p.t * w.dp, o.add = v0 > 0;
-            o.which = w.scaled ? 0 : -1;
+            o.which = w.scaled ? 0 : -1, o.own = kRowsOwn;
             o.last = dx_whole ? out.dx : nullptr, o.ldo = o.last ? out.lddx : w.dp, o.wide = wide(out.dx, out.lddx);
             k_gemm<PG, PG, NPL, EPI_OUT, T><<<dim3((unsigned)((w.tt + 7) / 8 * ((w.dt + 7) / 8)), w.sx), kGemmThreads, 0, st>>>(o);
             OPS_LAUNCH("dx");
@@ -1268,7 +1434,7 @@ int run_wide(const ccdpp_softmax_t& p, const Plan& w, const Outs& out, const int
             o.a = ws + w.o_xt, o.a_plane = w.dt * w.kst * kBlk, o.a_tile = w.kst * kBlk;
             o.b = z.gt, o.b_plane = q.gt_plane, o.b_tile = w.kst * kBlk, o.n_tiles = nt, o.rows = n;
             o.kb = w.tt, o.splits = w.se, o.out = (float*)(ws + w.o_de), o.out_split = w.vc * w.dp, o.add = 0;
-            o.which = w.scaled ? 1 : -1;
+            o.which = w.scaled ? 1 : -1, o.own = kItemsOwn;
             T* const de = (T*)out.de + v0 * out.ldde;
             o.last = w.se == 1 ? de : nullptr, o.ldo = o.last ? out.ldde : w.dp, o.wide = wide(de, out.ldde);
             k_gemm<PG, PG, NPL, EPI_OUT, T><<<dim3((unsigned)((nt + 7) / 8 * ((w.dt + 7) / 8)), w.se), kGemmThreads, 0, st>>>(o);

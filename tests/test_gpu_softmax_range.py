@@ -155,8 +155,10 @@ def check_rows(got, want, terms, dtype, z):
     assert float(off.max()) <= 0.0, (int(off.argmax()), float(((got.double() - want).norm(dim=1) / terms.norm(dim=1)).nan_to_num().max()))
 
 
-# rows, items, factors: few rows; few factors
-ROWS = [(8, 600, 40), (20, 600, 200), (33, 600, 40), (300, 600, 128), (500, 5000, 17)]
+# rows, items, factors: few rows; few factors; logits from the table as it lies; contractions that are cut; products in tiles,
+# logits kept or not; more rows than one group of terms
+ROWS = [(8, 600, 40), (20, 600, 200), (33, 600, 40), (300, 600, 128), (500, 5000, 17), (40, 600, 200), (100, 600, 136), (200, 600, 200),
+        (300, 20_000, 160), (300, 15_000, 400), (2100, 3000, 136)]
 
 
 def rare_items(t, v, d, dtype, offsets, seed):
