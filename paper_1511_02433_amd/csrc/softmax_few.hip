@@ -199,9 +199,17 @@ __global__ __launch_bounds__(kWaves * 64) void k_direct_logits(FewArgs a) {
 struct FewRows {
     float w[kFewT], l2[kFewT];  // weight (times scale), lse in base 2; 0 and +inf in rows that do not count
     int y[kFewT];               // target, or -1
+    int e[kFewT];               // OWN: the weight is taken times this power of two, which brings it to 2^12 .. 2^13
 };
 
+// Power of two that brings a term to 2^12 .. 2^13.
+__device__ __forceinline__ int term_exp(float top) {
+    const float a = fabsf(top);
+    return a > 0.f && finite(a) ? min(126, 12 + 127 - (int)(__float_as_uint(a) >> 23)) : 0;
+}
+
 // By the whole block; returns the largest finite |weight|.
+template <bool OWN>
 __device__ __forceinline__ float few_rows(const FewArgs& a, FewRows& rows) {
     const int t = threadIdx.x & (kFewT - 1);
     float w = 0.f, l2 = INFINITY;
@@ -214,12 +222,15 @@ __device__ __forceinline__ float few_rows(const FewArgs& a, FewRows& rows) {
             y = yt < a.v ? (int)yt : -1;
         }
     }
-    if (threadIdx.x < kFewT) rows.w[t] = w, rows.l2[t] = l2, rows.y[t] = y;
+    if (threadIdx.x < kFewT) {
+        const int e = OWN ? term_exp(w) : 0;
+        rows.w[t] = OWN ? ldexpf(w, e) : w, rows.l2[t] = l2, rows.y[t] = y, rows.e[t] = e;
+    }
     return wave_max(finite(w) ? fabsf(w) : 0.f);
 }
 
 // The terms of table rows b .. b + n - 1 (128 at most) by 256 threads: a thread has one table row and every other row of x,
-// its logits' reads all in flight.  G: 16 rows of x each.  put(table row, row of x, term); keep(table row, whether the item counts).
+// its logits' reads all in flight.  G: 16 rows of x each.  put(table row, row of x, its number among this thread's, term); keep(table row, whether the item counts).
 template <int G, class F, class K>
 __device__ __forceinline__ void few_terms(const FewArgs& a, const FewRows& rows, int64_t b, int n, float up, float up2, F&& put, K&& keep) {
     const int r = threadIdx.x & (kBatch - 1), t0 = threadIdx.x / kBatch;
@@ -234,7 +245,7 @@ __device__ __forceinline__ void few_terms(const FewArgs& a, const FewRows& rows,
         const float w = rows.w[t] * up * up2;
         float g = w * (exp2_fast(z[k] - rows.l2[t]) - (rows.y[t] == v ? 1.f : 0.f));
         if (r >= n || rows.l2[t] == INFINITY) g = 0.f;
-        put(r, t, g);
+        put(r, t, k, g);
     }
 }
 
@@ -277,13 +288,13 @@ __global__ __launch_bounds__(256, G == 1 ? 3 : 2) void k_few_grads(FewArgs a) {
 #pragma unroll
         for (int i = 0; i < C; ++i) x[j][i] = (float)row.v[i];
     }
-    few_rows(a, info);
+    few_rows<false>(a, info);
     f32x4 dx[G][C] = {};
     const auto read = [&](int64_t row, Piece& e) { e = load_tail<C>((const T*)a.table + row * a.ldt, c, a.d, (a.v - 1 - row) * a.ldt + a.d); };
     for (int64_t b = r0; b < r1; b += kBatch) {
         const int rows = (int)min((int64_t)kBatch, r1 - b);
         __syncthreads();
-        few_terms<G>(a, info, b, rows, 1.f, 1.f, [&](int r, int t, float g) { terms[r][t] = g; },
+        few_terms<G>(a, info, b, rows, 1.f, 1.f, [&](int r, int t, int, float g) { terms[r][t] = g; },
                   [&](int r, bool counts) { keep[r] = counts ? 1.f : 0.f; });
         __syncthreads();
         const int tiles = idle ? 0 : (rows + 15) / 16;
@@ -337,8 +348,9 @@ __global__ __launch_bounds__(256, G == 1 ? 3 : 2) void k_few_grads(FewArgs a) {
     }
 }
 
-// 16-bit types: the same with v_mfma_f32_16x16x16 on the values as they are; the terms, by a power of two below 2^13, are
-// the sum of two 16-bit planes.
+// 16-bit types: the same with v_mfma_f32_16x16x16 on the values as they are; the terms are the sum of two 16-bit planes.  In
+// bfloat16 all have a power of two of the largest weight; half precision, whose range ends at 2^-24, has one for each row
+// of x (for dx) and, for dtable, one for each table row, so that light rows and unlikely items keep their digits.
 template <class T> struct Half;
 template <> struct Half<_Float16> {
     typedef _Float16 vec __attribute__((ext_vector_type(4)));
@@ -362,13 +374,17 @@ __global__ __launch_bounds__(256, G == 1 ? 3 : 2) void k_few_grads16(FewArgs a) 
     __shared__ FewRows info;
     __shared__ uint16_t keep[kBatch];
     __shared__ __align__(16) float red[4][16 * 16 * C];
+    constexpr bool OWN = std::is_same<T, _Float16>::value;
+    // in `red`, which is not used before the end: a third block on a CU has no room for more
+    float(*const tops)[kBatch] = (float(*)[kBatch])red[0];
+    int* const item_e = (int*)red[1];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, q = lane >> 4;
     const int across = a.across, wx = wave & (across - 1), wy = wave / across, down = 4 / across;
     const int c = (blockIdx.x * across + wx) * 16 * C + n * C;
     const bool idle = c - n * C >= a.d;  // the wave's columns are past the row
     const int64_t r0 = a.v * blockIdx.y / gridDim.y, r1 = a.v * (blockIdx.y + 1) / gridDim.y;
-    const float most = few_rows(a, info);
-    const int e2 = scale_exp(most) - 2;
+    const float most = few_rows<OWN>(a, info);
+    const int e2 = OWN ? 0 : scale_exp(most) - 2;
     const float up = ldexpf(1.f, e2 / 2), up2 = ldexpf(1.f, e2 - e2 / 2), back = ldexpf(1.f, -(e2 / 2)), back2 = ldexpf(1.f, -(e2 - e2 / 2));
     V x[G][C];  // the operand of dtable: rows 4 q + i of each 16, zero where they do not count
 #pragma unroll
@@ -390,13 +406,28 @@ __global__ __launch_bounds__(256, G == 1 ? 3 : 2) void k_few_grads16(FewArgs a) 
 #pragma unroll
             for (int j = 0; j < 4; ++j) read(b + min(wy * 16 + 4 * q + j, rows - 1), next[j]);
         __syncthreads();
+        float own[8 * G], top = 0.f;  // OWN: the terms as they are
         few_terms<G>(a, info, b, rows, up, up2,
-                  [&](int r, int t, float g) {
+                  [&](int r, int t, int k, float g) {
                       const T hi = (T)g, lo = finite((float)hi) ? (T)(g - (float)hi) : (T)0.f;
-                      by_row[0][r][t] = hi, by_row[1][r][t] = lo;
                       by_x[0][t][r] = hi, by_x[1][t][r] = lo;
+                      if constexpr (OWN) own[k] = __builtin_amdgcn_ldexpf(g, -info.e[t]), top = fmaxf(top, fabsf(own[k]));
+                      else by_row[0][r][t] = hi, by_row[1][r][t] = lo;
                   },
                   [&](int r, bool counts) { keep[r] = counts ? 0xffff : 0; });
+        if constexpr (OWN) {
+            const int r = threadIdx.x & (kBatch - 1), t0 = threadIdx.x / kBatch;
+            tops[t0][r] = top;
+            __syncthreads();
+            const int e = term_exp(fmaxf(tops[0][r], tops[1][r]));
+            if (t0 == 0) item_e[r] = e;
+#pragma unroll
+            for (int k = 0; k < 8 * G; ++k) {
+                const float g = __builtin_amdgcn_ldexpf(own[k], e);
+                const T hi = (T)g, lo = finite((float)hi) ? (T)(g - (float)hi) : (T)0.f;
+                by_row[0][r][t0 + 2 * k] = hi, by_row[1][r][t0 + 2 * k] = lo;
+            }
+        }
         __syncthreads();
         for (int i = wy; i < tiles; i += down) {
             Piece e[4];
@@ -437,7 +468,7 @@ __global__ __launch_bounds__(256, G == 1 ? 3 : 2) void k_few_grads16(FewArgs a) 
                 if (row >= rows) continue;
                 Piece o;
 #pragma unroll
-                for (int l = 0; l < C; ++l) o.v[l] = (T)(de[l][r] * back * back2);
+                for (int l = 0; l < C; ++l) o.v[l] = (T)(OWN ? __builtin_amdgcn_ldexpf(de[l][r], -item_e[row]) : de[l][r] * back * back2);
                 store_tail<C>((T*)a.de + (b + row) * a.ldde, c, a.d, o);
             }
         }
@@ -445,11 +476,12 @@ __global__ __launch_bounds__(256, G == 1 ? 3 : 2) void k_few_grads16(FewArgs a) 
     if (!a.dxp) return;
 #pragma unroll
     for (int g = 0; g < G; ++g) {
-        if (g) __syncthreads();
+        if (g || OWN) __syncthreads();
 #pragma unroll
         for (int l = 0; l < C; ++l)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) red[wave][(4 * q + r) * 16 * C + n * C + l] = dx[g][l][r] * back * back2;
+            for (int r = 0; r < 4; ++r)
+                red[wave][(4 * q + r) * 16 * C + n * C + l] = OWN ? __builtin_amdgcn_ldexpf(dx[g][l][r], -info.e[16 * g + 4 * q + r]) : dx[g][l][r] * back * back2;
         add_waves<C>(a, red, 16 * g);
     }
 }

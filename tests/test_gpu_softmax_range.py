@@ -203,3 +203,23 @@ def test_weights_of_very_different_sizes(t, v, d, dtype, negative):
     size = float(z.abs().max())
     check_rows(dx, wx, torch.mm(p.abs(), e.double().abs()), dtype, size)
     check_rows(de, we, torch.mm(p.abs().t().contiguous(), x.double().abs()), dtype, size)
+
+
+@pytest.mark.parametrize("t,v,d", [(8, 20_000, 40), (20, 20_000, 100), (31, 3000, 72), (40, 20_000, 40), (100, 20_000, 136), (300, 20_000, 136)])
+def test_half_precision_weights_up_to_the_types_range(t, v, d):
+    """From 10^-3 to 3 10^4: the largest gradients are near half precision's end, the smallest still far above its beginning."""
+    x, e, y = make(t, v, d, "f32", seed=t)
+    x, e = (x * 0.25).half(), (e * 4).half()
+    gen = torch.Generator(device="cuda").manual_seed(t)
+    g = 10.0 ** (torch.rand(t, generator=gen, device="cuda") * 7.5 - 3)
+    g[0], g[1] = 3e4, 1e-3
+    y[0] = 7
+    y[1:] = torch.where(y[1:] == 7, torch.full_like(y[1:], 8), y[1:])
+    loss, lse, dx, de = ops().softmax_loss_train(x, e, y, grad=g)
+    z, want = check_loss(x, e, y, loss, lse)
+    p, wx, we = grads64(x, e, y, z, want, g)
+    size = float(z.abs().max())
+    for got, w, terms in ((dx, wx, torch.mm(p.abs(), e.double().abs())), (de, we, torch.mm(p.abs().t().contiguous(), x.double().abs()))):
+        fits = w.abs().amax(dim=1) < 6e4
+        assert int(fits.sum()) >= len(fits) - 2
+        check_rows(got[fits], w[fits], terms[fits], "f16", size)
