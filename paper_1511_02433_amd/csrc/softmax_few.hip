@@ -197,10 +197,12 @@ __global__ __launch_bounds__(kWaves * 64) void k_direct_logits(FewArgs a) {
 
 // What the terms of the rows take, in LDS.
 struct FewRows {
-    float w[kFewT], l2[kFewT];  // weight (times scale), lse in base 2; 0 and +inf in rows that do not count
-    int y[kFewT];               // target, or -1
+    float w[kFewT], l2[kFewT];  // weight (times scale), lse in base 2
+    int y[kFewT];               // target; -1: past the table; kOut: the row does not count
     int e[kFewT];               // OWN: the weight is taken times this power of two, which brings it to 2^12 .. 2^13
 };
+
+constexpr int kOut = -2;
 
 // Power of two that brings a term to 2^12 .. 2^13.
 __device__ __forceinline__ int term_exp(float top) {
@@ -212,8 +214,8 @@ __device__ __forceinline__ int term_exp(float top) {
 template <bool OWN>
 __device__ __forceinline__ float few_rows(const FewArgs& a, FewRows& rows) {
     const int t = threadIdx.x & (kFewT - 1);
-    float w = 0.f, l2 = INFINITY;
-    int y = -1;
+    float w = 0.f, l2 = 0.f;
+    int y = kOut;
     if (t < a.t) {
         const int64_t yt = load_target(a.target, a.target_bits, t);
         if (row_counts(yt, a.v, a.offset)) {
@@ -244,7 +246,7 @@ __device__ __forceinline__ void few_terms(const FewArgs& a, const FewRows& rows,
         const int t = t0 + 2 * k;
         const float w = rows.w[t] * up * up2;
         float g = w * (exp2_fast(z[k] - rows.l2[t]) - (rows.y[t] == v ? 1.f : 0.f));
-        if (r >= n || rows.l2[t] == INFINITY) g = 0.f;
+        if (r >= n || rows.y[t] == kOut) g = 0.f;
         put(r, t, k, g);
     }
 }

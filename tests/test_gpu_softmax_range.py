@@ -223,3 +223,22 @@ def test_half_precision_weights_up_to_the_types_range(t, v, d):
         fits = w.abs().amax(dim=1) < 6e4
         assert int(fits.sum()) >= len(fits) - 2
         check_rows(got[fits], w[fits], terms[fits], "f16", size)
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("t,v,d", [(1, 300, 40), (20, 300, 40), (32, 300, 200), (33, 300, 40), (40, 300, 200), (150, 300, 200)])
+def test_an_infinite_lse_leaves_the_targets_part(t, v, d, dtype):
+    """From the definition: every probability is 0, and G is -1 at the target, whatever the number of rows: dx is the target's
+    item, 16-bit values as they are, 32-bit ones with 22 bits."""
+    x, e, y = make(t, v, d, dtype, seed=t)
+    lse = torch.logsumexp(logits(x, e), dim=1).float()
+    lse[0] = math.inf
+    y[-1] = 3 if t == 1 else -1
+    dx, de = ops().softmax_loss_grad(x, e, y, lse)
+    assert float((dx[0] + e[y[0]]).abs().max()) <= (2.0 ** -21 if dtype == "f32" else 0.0) * float(e[y[0]].abs().max())
+    assert t == 1 or float(dx[-1].float().abs().max()) == 0.0
+    p = torch.exp(logits(x, e) - lse.double()[:, None])
+    p[torch.arange(t, device="cuda"), y.clamp(min=0)] -= 1
+    p[y < 0] = 0
+    want = torch.mm(p.t().contiguous(), x.double())
+    assert float((de.double() - want).norm()) <= {"f32": 2e-5, "bf16": 1e-2, "f16": 2e-3}[dtype] * float(want.norm())
