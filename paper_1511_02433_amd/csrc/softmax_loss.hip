@@ -1014,58 +1014,59 @@ template <class T, int THREADS>
 __global__ __launch_bounds__(256) void k_loss(ccdpp_softmax_t p, const float2* part, int64_t pieces, Shares shares, float* loss, float* lse, RowNumbers num) {
     constexpr int kRows = 256 / THREADS;
     __shared__ float red[4][4];
-    const int64_t t = (int64_t)blockIdx.x * kRows + threadIdx.x / THREADS;
-    if (t >= p.t) return;
     const int i0 = threadIdx.x % THREADS, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    // the target's products first: their reads are under way while the pieces come
-    const int64_t y = load_target(p.target, p.target_bits, t);
-    const float o = p.offset && y >= 0 && y < p.v ? p.offset[y] : 0.f;
-    float dot = 0.f;
-    if (y >= 0 && y < p.v && !(o < kExcluded)) {
-        const T *x = (const T*)p.x + t * p.ldx, *e = (const T*)p.table + y * p.ldt;
-        constexpr int N = 16 / sizeof(T);
+    for (int64_t t = (int64_t)blockIdx.x * kRows + threadIdx.x / THREADS; t < p.t; t += (int64_t)gridDim.x * kRows) {
+        // the target's products first: their reads are under way while the pieces come
+        const int64_t y = load_target(p.target, p.target_bits, t);
+        const float o = p.offset && y >= 0 && y < p.v ? p.offset[y] : 0.f;
+        float dot = 0.f;
+        if (y >= 0 && y < p.v && !(o < kExcluded)) {
+            const T *x = (const T*)p.x + t * p.ldx, *e = (const T*)p.table + y * p.ldt;
+            constexpr int N = 16 / sizeof(T);
 #pragma unroll 4
-        for (int d = i0 * N; d + N <= p.d; d += THREADS * N) {
-            const Run<T, N> a = load_run<N>(x + d), b = load_run<N>(e + d);
+            for (int d = i0 * N; d + N <= p.d; d += THREADS * N) {
+                const Run<T, N> a = load_run<N>(x + d), b = load_run<N>(e + d);
 #pragma unroll
-            for (int j = 0; j < N; ++j) dot = fmaf((float)a.v[j], (float)b.v[j], dot);
+                for (int j = 0; j < N; ++j) dot = fmaf((float)a.v[j], (float)b.v[j], dot);
+            }
+            for (int d = p.d / N * N + i0; d < p.d; d += THREADS) dot = fmaf((float)x[d], (float)e[d], dot);
         }
-        for (int d = p.d / N * N + i0; d < p.d; d += THREADS) dot = fmaf((float)x[d], (float)e[d], dot);
-    }
-    float m = -INFINITY, s = 0.f;
-    bool nan = false;
-    if (!pieces) pieces = shares.count(t / 128);
-    for (int64_t i = i0; i < pieces; i += THREADS) {
-        const float2 q = part[i * p.t + t];
-        const float top = fmaxf(m, q.x), ref = top == -INFINITY ? 0.f : top;
-        nan |= q.x != q.x || q.y != q.y;
-        s = s * exp2_fast(m - ref) + q.y * exp2_fast(q.x - ref);
-        m = top;
-    }
-    float top = wave_max(m), ref = top == -INFINITY ? 0.f : top;
-    s *= exp2_fast(m - ref);
-    for (int k = 32; k > 0; k >>= 1) s += __shfl_xor(s, k), dot += __shfl_xor(dot, k);
-    nan = __any(nan);
-    if constexpr (THREADS == 256) {
-        if (lane == 0) red[wave][0] = top, red[wave][1] = s, red[wave][2] = dot, red[wave][3] = nan ? 1.f : 0.f;
-        __syncthreads();
-        for (int w = 0; w < 4; ++w) top = fmaxf(top, red[w][0]);
-        ref = top == -INFINITY ? 0.f : top;
-        s = 0.f, dot = 0.f;
-        for (int w = 0; w < 4; ++w) {
-            s += red[w][1] * exp2_fast(red[w][0] - ref);
-            dot += red[w][2];
-            nan |= red[w][3] != 0.f;
+        float m = -INFINITY, s = 0.f;
+        bool nan = false;
+        const int64_t n = pieces ? pieces : shares.count(t / 128);
+        for (int64_t i = i0; i < n; i += THREADS) {
+            const float2 q = part[i * p.t + t];
+            const float top = fmaxf(m, q.x), ref = top == -INFINITY ? 0.f : top;
+            nan |= q.x != q.x || q.y != q.y;
+            s = s * exp2_fast(m - ref) + q.y * exp2_fast(q.x - ref);
+            m = top;
         }
-    }
-    float l = top == -INFINITY ? -INFINITY : (top + log2f(s)) * kLn2;
-    if (nan) l = NAN;
-    float out = 0.f;
-    if (y >= p.v) out = NAN;
-    else if (y >= 0) out = o < kExcluded ? INFINITY : l - fmaf(dot, p.scale, o);
-    if (i0 == 0) {
-        loss[t] = out, lse[t] = l;
-        if (num.first) put_numbers(num, t, y, p.v, p.offset, l);
+        float top = wave_max(m), ref = top == -INFINITY ? 0.f : top;
+        s *= exp2_fast(m - ref);
+        for (int k = 32; k > 0; k >>= 1) s += __shfl_xor(s, k), dot += __shfl_xor(dot, k);
+        nan = __any(nan);
+        if constexpr (THREADS == 256) {
+            if (lane == 0) red[wave][0] = top, red[wave][1] = s, red[wave][2] = dot, red[wave][3] = nan ? 1.f : 0.f;
+            __syncthreads();
+            for (int w = 0; w < 4; ++w) top = fmaxf(top, red[w][0]);
+            ref = top == -INFINITY ? 0.f : top;
+            s = 0.f, dot = 0.f;
+            for (int w = 0; w < 4; ++w) {
+                s += red[w][1] * exp2_fast(red[w][0] - ref);
+                dot += red[w][2];
+                nan |= red[w][3] != 0.f;
+            }
+        }
+        float l = top == -INFINITY ? -INFINITY : (top + log2f(s)) * kLn2;
+        if (nan) l = NAN;
+        float out = 0.f;
+        if (y >= p.v) out = NAN;
+        else if (y >= 0) out = o < kExcluded ? INFINITY : l - fmaf(dot, p.scale, o);
+        if (i0 == 0) {
+            loss[t] = out, lse[t] = l;
+            if (num.first) put_numbers(num, t, y, p.v, p.offset, l);
+        }
+        if (THREADS == 256 && t + gridDim.x < p.t) __syncthreads();  // `red` is free again
     }
 }
 
@@ -1284,8 +1285,9 @@ Plan make_plan(const ccdpp_softmax_t& p, int call) {
 template <class T>
 int launch_loss(const ccdpp_softmax_t& p, const float2* part, int64_t pieces, const Shares& shares, float* loss, float* lse, const RowNumbers& num,
                 hipStream_t st) {
-    if (p.d > 256 || p.t <= 256) k_loss<T, 256><<<(unsigned)p.t, 256, 0, st>>>(p, part, pieces, shares, loss, lse, num);
-    else k_loss<T, 64><<<(unsigned)((p.t + 3) / 4), 256, 0, st>>>(p, part, pieces, shares, loss, lse, num);
+    constexpr int64_t kMost = 1 << 22;  // blocks (a launch holds 2^32 threads at most)
+    if (p.d > 256 || p.t <= 256) k_loss<T, 256><<<(unsigned)std::min(p.t, kMost), 256, 0, st>>>(p, part, pieces, shares, loss, lse, num);
+    else k_loss<T, 64><<<(unsigned)std::min((p.t + 3) / 4, kMost), 256, 0, st>>>(p, part, pieces, shares, loss, lse, num);
     OPS_LAUNCH("loss");
     return CCDPP_OK;
 }
