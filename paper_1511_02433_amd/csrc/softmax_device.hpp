@@ -161,7 +161,7 @@ struct Shares {
     __host__ __device__ int64_t first(int64_t kept) const { return kept * tiles / len; }
     __host__ __device__ int count(int64_t kept) const { return (int)(((kept + 1) * tiles - 1) / len - first(kept) + 1); }
     __host__ __device__ bool whole() const { return len > 0 && tiles > 0 && len % tiles == 0; }  // a share per kept block
-    __host__ __device__ int64_t most() const { return tiles > 0 ? (tiles + len - 2) / len + 1 : 0; }  // of count()
+    __host__ __device__ int64_t most() const { return whole() ? 1 : tiles > 0 ? (tiles + len - 2) / len + 1 : 0; }  // of count()
 };
 
 struct SmallOut {

@@ -1134,7 +1134,8 @@ struct Plan {
     int64_t tt, vt, dt;      // blocks of 32
     int ksd;                 // steps of 16 over d
     int64_t kst, ksv;        // over rows, over the whole table
-    int64_t vc;              // table entries per piece of the gradients (a multiple of 256)
+    int64_t vc, tc;          // table entries and rows per piece of the gradients (multiples of 256)
+    int64_t tz;              // rows per launch of the logits (a multiple of 256)
     int64_t dp;              // columns of partial sums
     int sx, se;              // splits of the two gradients' contractions
     int sz;                  // shares of the logits' contraction; above 1 all logits are kept, in rows
@@ -1150,9 +1151,13 @@ struct Plan {
     int64_t o_scale, o_xrow, o_erow, o_ek, o_fin, o_xf, o_ef, o_xl, o_o2, o_xn, o_xt, o_et, o_g, o_gt, o_part, o_dx, o_de, bytes;
 };
 
-// Of G, and as much again of G^T: pieces of the table keep the workspace bounded, whatever t and v are, and larger ones
-// read and write dx's partial sums less often (8,192 x 131,072 x 4,096: 1.5% less than by 128 MiB).
+// Of G, and as much again of G^T: pieces of the table, and of the rows where they are many, keep the workspace bounded,
+// whatever t and v are; larger ones read and write dx's partial sums less often (8,192 x 131,072 x 4,096: 1.5% less than by
+// 128 MiB).
 constexpr int64_t kPieceBytes = int64_t(512) << 20;
+constexpr int64_t kLeastEntries = 2048;  // of a piece
+// The logits' (max, sum) pairs of a launch: at most this, or those of 256 rows.
+constexpr int64_t kPairBytes = int64_t(256) << 20;
 
 
 // A training pass may keep logits between its two halves, in kKeptBytes at most, whatever t and v are.  Written and read
@@ -1220,8 +1225,8 @@ Plan make_plan(const ccdpp_softmax_t& p, int call) {
         w.o_ef = take(w.vt * w.e_tile);
         w.o_xl = take(w.grads ? w.tt * w.xlive_tile : 0);
         w.o_part = take(w.forward ? w.lse.most() * p.t * 8 : 0);
-        w.o_dx = take(w.grads ? w.dx.most() * w.tt * 32 * w.dp * 4 : 0);
-        w.o_de = take(w.grads ? w.de.most() * w.vt * 32 * w.dp * 4 : 0);
+        w.o_dx = take(w.grads && !w.dx.whole() ? w.dx.most() * w.tt * 32 * w.dp * 4 : 0);
+        w.o_de = take(w.grads && !w.de.whole() ? w.de.most() * w.vt * 32 * w.dp * 4 : 0);
         w.bytes = at;
         return w;
     }
@@ -1229,15 +1234,17 @@ Plan make_plan(const ccdpp_softmax_t& p, int call) {
     w.o_ek = take(w.planes == 2 ? w.vt * 32 * 4 : 0);
     w.ksd = (int)w.dt * 2;
     w.dp = round_up(p.d, 4);
-    const int64_t row_bytes = w.tt * 32 * 2 * w.planes;
-    w.vc = std::max<int64_t>(2048, kPieceBytes / std::max<int64_t>(row_bytes, 1) / 256 * 256);
+    w.tc = std::min(round_up(std::max<int64_t>(p.t, 1), 256), kPieceBytes / (kLeastEntries * 2 * w.planes));
+    const int64_t pt = std::min(w.tc / 32, std::max<int64_t>(w.tt, 1));  // blocks of 32 rows of a piece
+    w.vc = std::max(kLeastEntries, kPieceBytes / (pt * 32 * 2 * w.planes) / 256 * 256);
     w.vc = std::min(w.vc, round_up(p.v, 256));
+    w.tz = std::min(round_up(std::max<int64_t>(p.t, 1), 256), std::max<int64_t>(256, kPairBytes / ((w.vt + 7) / 8 * 8) / 256 * 256));
     const auto splits = [](int64_t m, int64_t n, int64_t kb) {
         const int64_t blocks = std::max<int64_t>(1, (m + 7) / 8 * ((n + 7) / 8));
         return (int)std::max<int64_t>(1, std::min<int64_t>({256 / blocks, kb / 8, 64}));
     };
-    w.sx = splits(w.tt, w.dt, w.vc / 32);
-    w.se = splits(w.vc / 32, w.dt, w.tt);
+    w.sx = splits(pt, w.dt, w.vc / 32);
+    w.se = splits(w.vc / 32, w.dt, pt);
     // With half of the CUs or more without a block of logits the contraction may be cut too.  A step of 32 takes a block
     // half a microsecond (three times that with two planes), in the logits and again in the terms unless they are
     // kept; the kept ones cost a launch, and are written and read at 3 TB/s.  (27 x 2,372 x 3,274 floats, loss and gradients: 396
@@ -1261,16 +1268,16 @@ Plan make_plan(const ccdpp_softmax_t& p, int call) {
     }
     w.o_o2 = take(w.vt * 32 * 4);
     w.o_xn = take(w.tt * 32 * 4);
-    if (!w.direct) w.o_part = take(w.forward ? (w.vt + 7) / 8 * p.t * 8 : 0);
+    if (!w.direct) w.o_part = take(w.forward ? (w.vt + 7) / 8 * std::min(w.tz, p.t) * 8 : 0);
     if (w.grads) {
         w.o_xt = take(w.planes * w.dt * w.kst * kBlk);
         w.o_et = take(w.planes * w.dt * w.ksv * kBlk);
-        w.o_g = take(w.planes * w.tt * (w.vc / 16) * kBlk);
-        w.o_gt = take(w.planes * (w.vc / 32) * w.kst * kBlk);
-        w.o_lev = take(w.tt > 2 ? (w.tt + 1) / 2 * w.vc : 0);
+        w.o_g = take(w.planes * pt * (w.vc / 16) * kBlk);
+        w.o_gt = take(w.planes * (w.vc / 32) * pt * 2 * kBlk);
+        w.o_lev = take(pt > 2 ? (pt + 1) / 2 * w.vc : 0);
         w.o_item = take(w.vc * 4);
         w.o_dx = take(p.v <= w.vc && w.sx == 1 ? 0 : w.sx * p.t * w.dp * 4);
-        w.o_de = take(w.se == 1 ? 0 : w.se * w.vc * w.dp * 4);
+        w.o_de = take(w.se == 1 && p.t <= w.tc ? 0 : w.se * w.vc * w.dp * 4);
     }
     w.bytes = at;
     return w;
@@ -1366,6 +1373,25 @@ int run_small(const ccdpp_softmax_t& p, const Plan& w, const Outs& o, const int3
     return finish<T>(x, t, p.d, p.scale, fin, st);
 }
 
+// Rows t0 .. of a problem.
+ccdpp_softmax_t rows_of(const ccdpp_softmax_t& p, int64_t t0, int64_t n, int64_t value_bytes) {
+    ccdpp_softmax_t q = p;
+    q.t = n;
+    q.x = (const char*)p.x + t0 * p.ldx * value_bytes;
+    q.target = (const char*)p.target + t0 * (p.target_bits / 8);
+    return q;
+}
+
+// The operands of rows t0 .. t0 + n - 1, and what comes of them, in place of all rows'.
+void take_rows(GemmArgs& q, const Plan& w, int64_t t0, int64_t n) {
+    q.b += t0 / 32 * q.b_tile, q.n_tiles = (n + 31) / 32, q.t = n;
+    q.xf += t0;
+    q.target = (const char*)q.target + t0 * (q.target_bits / 8);
+    if (q.kept) q.kept += t0 / 32 * (w.kept / 32) * 1024;
+    if (q.lse) q.lse += t0;
+    if (q.grad) q.grad += t0;
+}
+
 template <int DT>
 int run_wide(const ccdpp_softmax_t& p, const Plan& w, const Outs& out, const int32_t* fin, char* ws, hipStream_t st) {
     typedef typename Types<DT>::in T;
@@ -1379,70 +1405,85 @@ int run_wide(const ccdpp_softmax_t& p, const Plan& w, const Outs& out, const int
     z.m_tiles = w.vt, z.n_tiles = w.tt, z.kb = w.ksd / 2, z.splits = 1;
     z.t = p.t, z.v = p.v, z.xf = (const float*)(ws + w.o_xn), z.fin = fin, z.o2 = (const float*)(ws + w.o_o2), z.ek = (const int*)(ws + w.o_ek);
     z.scale = p.scale, z.offset = p.offset, z.target = p.target, z.target_bits = p.target_bits;
-    float* const kept = (float*)(ws + w.o_z);
+    z.kept = (float*)(ws + w.o_z), z.kept_tiles = w.kept / 32;
+    float2* const part = (float2*)(ws + w.o_part);
     const int64_t pitch = w.vt * 32, chunks = (pitch + 1023) / 1024;
-    const unsigned blocks = (unsigned)((w.vt + 7) / 8 * ((w.tt + 7) / 8));
+    const auto blocks = [](int64_t m, int64_t n) { return (unsigned)((m + 7) / 8 * ((n + 7) / 8)); };
     if (w.direct) {
         // done
     } else if (w.sz > 1) {
         GemmArgs q = z;
-        q.out = kept, q.out_split = p.t * pitch, q.ldo = q.cols = pitch, q.rows = p.t, q.splits = w.sz;
-        k_gemm<P, PG, NPL, EPI_OUT, T><<<dim3(blocks, w.sz), kGemmThreads, 0, st>>>(q);
+        q.out = z.kept, q.out_split = p.t * pitch, q.ldo = q.cols = pitch, q.rows = p.t, q.splits = w.sz;
+        k_gemm<P, PG, NPL, EPI_OUT, T><<<dim3(blocks(w.vt, w.tt), w.sz), kGemmThreads, 0, st>>>(q);
         OPS_LAUNCH("logits");
-        const JoinArgs j = {kept, w.sz, q.out_split, pitch, p.t, z.xf, z.o2, NPL == 2 ? z.ek : nullptr, w.forward ? (float2*)(ws + w.o_part) : nullptr};
+        const JoinArgs j = {z.kept, w.sz, q.out_split, pitch, p.t, z.xf, z.o2, NPL == 2 ? z.ek : nullptr, w.forward ? part : nullptr};
         k_join<<<dim3((unsigned)chunks, (unsigned)p.t), 256, 0, st>>>(j);
         OPS_LAUNCH("logits");
+        if (w.forward)
+            if (int rc = launch_loss<T>(p, part, chunks, Shares{}, out.loss, out.lse, RowNumbers{}, st)) return rc;
     } else if (w.forward) {
-        z.part = (float2*)(ws + w.o_part);
-        z.kept = kept, z.kept_tiles = w.kept / 32;
-        k_gemm<P, PG, NPL, EPI_LSE, T><<<blocks, kGemmThreads, 0, st>>>(z);
-        OPS_LAUNCH("logits");
+        for (int64_t t0 = 0; t0 < p.t; t0 += w.tz) {
+            const int64_t n = std::min(w.tz, p.t - t0);
+            GemmArgs q = z;
+            take_rows(q, w, t0, n);
+            q.part = part;
+            k_gemm<P, PG, NPL, EPI_LSE, T><<<blocks(w.vt, q.n_tiles), kGemmThreads, 0, st>>>(q);
+            OPS_LAUNCH("logits");
+            if (int rc = launch_loss<T>(rows_of(p, t0, n, sizeof(T)), part, (w.vt + 7) / 8, Shares{}, out.loss + t0, out.lse + t0, RowNumbers{}, st)) return rc;
+        }
     }
-    if (w.forward && !w.direct)
-        if (int rc = launch_loss<T>(p, (const float2*)(ws + w.o_part), w.sz > 1 ? chunks : (w.vt + 7) / 8, Shares{}, out.loss, out.lse, RowNumbers{}, st)) return rc;
     if (!w.grads) return CCDPP_OK;
     z.lse = w.forward ? out.lse : out.lse_in, z.grad = out.grad;
     z.g = out.dx ? ws + w.o_g : nullptr, z.gt = out.de ? ws + w.o_gt : nullptr;
-    z.kst = w.kst;
-    z.lev = w.tt > 2 ? (uint8_t*)(ws + w.o_lev) : nullptr, z.item_e = (int*)(ws + w.o_item);
-    const bool dx_whole = p.v <= w.vc && w.sx == 1;
+    z.item_e = (int*)(ws + w.o_item);
+    const bool dx_whole = p.v <= w.vc && w.sx == 1, de_whole = p.t <= w.tc && w.se == 1;
     for (int64_t v0 = 0; v0 < p.v; v0 += w.vc) {
         const int64_t n = std::min(w.vc, p.v - v0), nt = (n + 31) / 32;
-        GemmArgs q = z;
-        q.v0 = v0, q.a = z.a + v0 / 32 * z.a_tile, q.o2 = z.o2 + v0, q.ek = z.ek + v0, q.m_tiles = nt;
-        q.ksv = nt * 2, q.g_plane = w.tt * q.ksv * kBlk, q.gt_plane = nt * w.kst * kBlk;
-        const unsigned tiles = (unsigned)((nt + 3) / 4 * ((w.tt + 1) / 2));
-        if (w.sz > 1 || w.direct) k_terms<PG, NPL><<<tiles, 256, 0, st>>>(q, kept + v0, pitch);
-        else if (v0 < w.kept) k_terms<PG, NPL><<<tiles, 256, 0, st>>>(q, nullptr, 0);
-        else k_gemm<P, PG, NPL, EPI_G, T><<<(unsigned)((nt + 7) / 8 * ((w.tt + 7) / 8)), kGemmThreads, 0, st>>>(q);
-        OPS_LAUNCH("G");
-        if (out.de && z.lev) {
-            k_levels<NPL><<<(unsigned)nt, 256, 0, st>>>(q);
-            OPS_LAUNCH("G");
-        }
         GemmArgs o = {};
-        o.m_tiles = w.dt, o.cols = p.d, o.scale = p.scale, o.fin = fin, o.grad = out.grad, o.item_e = z.item_e;
+        o.m_tiles = w.dt, o.cols = p.d, o.scale = p.scale, o.fin = fin, o.item_e = z.item_e;
         const auto wide = [](const void* at, int64_t ld) { return ((uintptr_t)at | (uintptr_t)(ld * sizeof(T))) % (4 * sizeof(T)) == 0; };
-        if (out.dx) {
-            o.a = ws + w.o_et + v0 / 16 * kBlk, o.a_plane = w.dt * w.ksv * kBlk, o.a_tile = w.ksv * kBlk;
-            o.b = z.g, o.b_plane = q.g_plane, o.b_tile = q.ksv * kBlk, o.n_tiles = w.tt, o.rows = p.t;
-            o.kb = nt, o.splits = w.sx, o.out = (float*)(ws + w.o_dx), o.out_split = p.t * w.dp, o.add = v0 > 0;
-            o.which = w.scaled ? 0 : -1, o.own = kRowsOwn;
-            o.last = dx_whole ? out.dx : nullptr, o.ldo = o.last ? out.lddx : w.dp, o.wide = wide(out.dx, out.lddx);
-            k_gemm<PG, PG, NPL, EPI_OUT, T><<<dim3((unsigned)((w.tt + 7) / 8 * ((w.dt + 7) / 8)), w.sx), kGemmThreads, 0, st>>>(o);
-            OPS_LAUNCH("dx");
+        T* const de = out.de ? (T*)out.de + v0 * out.ldde : nullptr;
+        for (int64_t t0 = 0; t0 < p.t; t0 += w.tc) {
+            const int64_t tn = std::min(w.tc, p.t - t0);
+            GemmArgs q = z;
+            take_rows(q, w, t0, tn);
+            q.v0 = v0, q.a = z.a + v0 / 32 * z.a_tile, q.o2 = z.o2 + v0, q.ek = z.ek + v0, q.m_tiles = nt;
+            q.ksv = nt * 2, q.kst = q.n_tiles * 2;
+            q.g_plane = q.n_tiles * q.ksv * kBlk, q.gt_plane = nt * q.kst * kBlk;
+            q.lev = q.n_tiles > 2 ? (uint8_t*)(ws + w.o_lev) : nullptr;
+            const unsigned tiles = (unsigned)((nt + 3) / 4 * ((q.n_tiles + 1) / 2));
+            if (w.sz > 1 || w.direct) k_terms<PG, NPL><<<tiles, 256, 0, st>>>(q, z.kept + v0, pitch);
+            else if (v0 < w.kept) k_terms<PG, NPL><<<tiles, 256, 0, st>>>(q, nullptr, 0);
+            else k_gemm<P, PG, NPL, EPI_G, T><<<blocks(nt, q.n_tiles), kGemmThreads, 0, st>>>(q);
+            OPS_LAUNCH("G");
+            if (out.de && q.lev) {
+                k_levels<NPL><<<(unsigned)nt, 256, 0, st>>>(q);
+                OPS_LAUNCH("G");
+            }
+            o.grad = q.grad;
+            if (out.dx) {
+                T* const dx = (T*)out.dx + t0 * out.lddx;
+                o.a = ws + w.o_et + v0 / 16 * kBlk, o.a_plane = w.dt * w.ksv * kBlk, o.a_tile = w.ksv * kBlk;
+                o.b = q.g, o.b_plane = q.g_plane, o.b_tile = q.ksv * kBlk, o.n_tiles = q.n_tiles, o.rows = tn;
+                o.kb = nt, o.splits = w.sx, o.out = (float*)(ws + w.o_dx) + t0 * w.dp, o.out_split = p.t * w.dp, o.add = v0 > 0;
+                o.which = w.scaled ? 0 : -1, o.own = kRowsOwn;
+                o.last = dx_whole ? dx : nullptr, o.ldo = o.last ? out.lddx : w.dp, o.wide = wide(dx, out.lddx);
+                k_gemm<PG, PG, NPL, EPI_OUT, T><<<dim3(blocks(w.dt, q.n_tiles), w.sx), kGemmThreads, 0, st>>>(o);
+                OPS_LAUNCH("dx");
+            }
+            if (out.de) {
+                o.a = ws + w.o_xt + t0 / 16 * kBlk, o.a_plane = w.dt * w.kst * kBlk, o.a_tile = w.kst * kBlk;
+                o.b = q.gt, o.b_plane = q.gt_plane, o.b_tile = q.kst * kBlk, o.n_tiles = nt, o.rows = n;
+                o.kb = q.n_tiles, o.splits = w.se, o.out = (float*)(ws + w.o_de), o.out_split = w.vc * w.dp, o.add = t0 > 0;
+                o.which = w.scaled ? 1 : -1, o.own = kItemsOwn;
+                o.last = de_whole ? de : nullptr, o.ldo = o.last ? out.ldde : w.dp, o.wide = wide(de, out.ldde);
+                k_gemm<PG, PG, NPL, EPI_OUT, T><<<dim3(blocks(w.dt, nt), w.se), kGemmThreads, 0, st>>>(o);
+                OPS_LAUNCH("dtable");
+            }
         }
-        if (out.de) {
-            o.a = ws + w.o_xt, o.a_plane = w.dt * w.kst * kBlk, o.a_tile = w.kst * kBlk;
-            o.b = z.gt, o.b_plane = q.gt_plane, o.b_tile = w.kst * kBlk, o.n_tiles = nt, o.rows = n;
-            o.kb = w.tt, o.splits = w.se, o.out = (float*)(ws + w.o_de), o.out_split = w.vc * w.dp, o.add = 0;
-            o.which = w.scaled ? 1 : -1, o.own = kItemsOwn;
-            T* const de = (T*)out.de + v0 * out.ldde;
-            o.last = w.se == 1 ? de : nullptr, o.ldo = o.last ? out.ldde : w.dp, o.wide = wide(de, out.ldde);
-            k_gemm<PG, PG, NPL, EPI_OUT, T><<<dim3((unsigned)((nt + 7) / 8 * ((w.dt + 7) / 8)), w.se), kGemmThreads, 0, st>>>(o);
-            OPS_LAUNCH("dtable");
-            if (!o.last)
-                if (int rc = finish<T>(FinishSide{}, FinishSide{o.out, w.se, o.out_split, n, w.dp, de, out.ldde, o.which, -1, {}}, p.d, p.scale, fin, st)) return rc;
+        if (out.de && !de_whole) {
+            const FinishSide e = {(const float*)(ws + w.o_de), w.se, w.vc * w.dp, n, w.dp, de, out.ldde, w.scaled ? 1 : -1, -1, {}};
+            if (int rc = finish<T>(FinishSide{}, e, p.d, p.scale, fin, st)) return rc;
         }
     }
     if (out.dx && !dx_whole)
