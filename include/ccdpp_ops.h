@@ -12,7 +12,7 @@
  * Conventions for every call:
  *  - Array arguments are DEVICE memory on the current HIP device, owned by the
  *    caller (tables of pointers and sizes, and the structures, are host memory
- *    and read during the call).  Outputs must not overlap inputs or the
+ *    and read during the call), aligned to its type.  Outputs must not overlap inputs or the
  *    workspace unless a call says so.
  *  - Calls enqueue their work on `stream` (a hipStream_t; NULL: the null
  *    stream) and return; nothing waits for the device, nothing is allocated,
@@ -88,8 +88,8 @@ enum ccdpp_softmax_call {
     CCDPP_SOFTMAX_TRAIN = 2   /* ccdpp_softmax_loss_train */
 };
 
-/* Bytes of workspace of `call` (enum ccdpp_softmax_call) on this problem; reads
- * the sizes, dtype and strides of p and whether its pointers are aligned. */
+/* Bytes of workspace of `call` (enum ccdpp_softmax_call) on this problem: of its
+ * sizes and dtype; no pointer of p is read. */
 int ccdpp_softmax_workspace(const ccdpp_softmax_t *p, int32_t call, int64_t *bytes);
 
 /* loss[i] = lse[i] - z[i, target_i] and lse[i] = log sum_v exp z_iv, float[t] each. */

@@ -1548,6 +1548,8 @@ int run(const ccdpp_softmax_t& p, int call, const Outs& out, char* ws, hipStream
     return w.small ? run_small<DT>(p, w, out, fin, ws, st) : run_wide<DT>(p, w, out, fin, ws, st);
 }
 
+uintptr_t value_bytes(const ccdpp_softmax_t& p) { return p.dtype == CCDPP_F32 ? 4 : 2; }
+
 int check(const ccdpp_softmax_t* p, bool pointers) {
     if (!p) return fail(CCDPP_EINVAL, "the problem is NULL");
     if (p->t < 0 || p->t >= int64_t(1) << 26) return fail(CCDPP_EINVAL, "t must be in [0, 2^26)");
@@ -1558,7 +1560,11 @@ int check(const ccdpp_softmax_t* p, bool pointers) {
     if ((double)p->t * (double)p->v >= 549755813888.0) return fail(CCDPP_EINVAL, "t * v must be below 2^39: take fewer rows at a time");
     if (p->target_bits != 32 && p->target_bits != 64) return fail(CCDPP_EINVAL, "target_bits must be 32 or 64");
     if (!std::isfinite(p->scale)) return fail(CCDPP_EINVAL, "scale must be finite");
-    if (pointers && (!p->table || (p->t > 0 && (!p->x || !p->target)))) return fail(CCDPP_EINVAL, "x, table and target must be non-NULL");
+    if (!pointers) return CCDPP_OK;
+    if (!p->table || (p->t > 0 && (!p->x || !p->target))) return fail(CCDPP_EINVAL, "x, table and target must be non-NULL");
+    const uintptr_t value = value_bytes(*p);
+    if ((uintptr_t)p->table % value || (uintptr_t)p->x % value || (uintptr_t)p->target % (p->target_bits / 8) || (uintptr_t)p->offset % 4)
+        return fail(CCDPP_EINVAL, "x, table, target and offset must be aligned to their types");
     return CCDPP_OK;
 }
 
@@ -1568,6 +1574,8 @@ int call(const ccdpp_softmax_t* p, int what, float* loss, float* lse, const floa
     if (what != CCDPP_SOFTMAX_GRAD && p->t > 0 && (!loss || !lse)) return fail(CCDPP_EINVAL, "loss and lse must be non-NULL");
     if (what == CCDPP_SOFTMAX_GRAD && p->t > 0 && !lse_in) return fail(CCDPP_EINVAL, "lse must be non-NULL");
     if (what != CCDPP_SOFTMAX_LOSS && ((dx && lddx < p->d) || (de && ldde < p->d))) return fail(CCDPP_EINVAL, "lddx and lddt must be at least d");
+    if ((((uintptr_t)loss | (uintptr_t)lse | (uintptr_t)lse_in | (uintptr_t)grad) % 4) || (((uintptr_t)dx | (uintptr_t)de) % value_bytes(*p)))
+        return fail(CCDPP_EINVAL, "loss, lse, grad, dx and dtable must be aligned to their types");
     const Plan w = make_plan(*p, what);
     if (ws_bytes < w.bytes || (!ws && w.bytes > 0)) return fail(CCDPP_EINVAL, "the workspace is too small");
     if ((uintptr_t)ws % 256) return fail(CCDPP_EINVAL, "the workspace must be aligned to 256 bytes");

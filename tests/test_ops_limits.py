@@ -1,4 +1,5 @@
-"""What the operators' workspaces hold, from the sizes alone (no GPU): bounded whatever the numbers of rows and items are."""
+"""What the operators' workspaces hold, from the sizes alone (no GPU): bounded whatever the numbers of rows and items are; and which
+pointers the calls refuse."""
 import ctypes
 
 import pytest
@@ -60,3 +61,28 @@ def test_few_factors(t, v, d, dtype):
     packed = 1024 * (tt * (2 * plain + turned) + vt * (plain + turned))
     of_table = 768 * 2 * 128 * 32 * blocks * 4  # (at most two kept blocks of 128 a share)
     assert workspace(t, v, d, dtype, ops.TRAIN) <= packed + 8 * 8 * t + 4 * t + of_table + MIB
+
+
+@pytest.mark.parametrize("dtype, value", [(0, 4), (1, 2), (2, 2)])
+def test_pointers_that_are_not_aligned_to_their_type_are_refused(dtype, value):
+    """By the calls, on the host; the workspace's size needs no pointer."""
+    L, B, E = _lib_or_skip(), ctypes.byref, C.CCDPP_EINVAL
+    fields = dict(t=4, v=10, d=8, dtype=dtype, x=256, ldx=8, table=256, ldt=8, target=256, target_bits=64, scale=1.0, offset=None)
+
+    def problem(**kw):
+        return ops.Softmax(*[{**fields, **kw}[n] for n, _ in ops.Softmax._fields_])
+
+    for kw in (dict(x=256 + value // 2), dict(table=256 + value // 2), dict(target=260), dict(target=258, target_bits=32), dict(offset=258)):
+        p, n = problem(**kw), ctypes.c_int64()
+        assert L.ccdpp_softmax_workspace(B(p), ops.TRAIN, B(n)) == 0
+        for rc in (L.ccdpp_softmax_loss(B(p), 256, 256, 256, 1 << 40, None), L.ccdpp_softmax_loss_grad(B(p), 256, None, 256, 8, 256, 8, 256, 1 << 40, None),
+                   L.ccdpp_softmax_loss_train(B(p), 256, 256, None, 256, 8, 256, 8, 256, 1 << 40, None)):
+            assert rc == E and "aligned to their types" in L.ccdpp_ops_last_error().decode(), kw
+    p = problem()
+    off = 256 + value // 2
+    for args in ((258, 256, None, 256, 256), (256, 258, None, 256, 256), (256, 256, 258, 256, 256), (256, 256, None, off, 256), (256, 256, None, 256, off)):
+        loss, lse, grad, dx, de = args
+        assert L.ccdpp_softmax_loss_train(B(p), loss, lse, grad, dx, 8, de, 8, 256, 1 << 40, None) == E, args
+        assert "aligned to their types" in L.ccdpp_ops_last_error().decode()
+    assert L.ccdpp_softmax_loss_grad(B(p), 258, None, 256, 8, 256, 8, 256, 1 << 40, None) == E
+    assert "aligned to their types" in L.ccdpp_ops_last_error().decode()
