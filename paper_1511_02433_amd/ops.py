@@ -51,6 +51,10 @@ def _lib():
     return L
 
 
+# Tells autograd that tensors of the caller's have other values now, as torch's own operators in place do.
+_written = torch.autograd.graph.increment_version
+
+
 def _check(rc):
     if rc < 0:
         raise _c.CCDPPError(rc, _lib().ccdpp_ops_last_error().decode())
@@ -169,10 +173,13 @@ def softmax_loss_grad(x, table, target, lse, *, grad=None, scale=1.0, offset=Non
     p, index = _problem(x, table, target, scale, offset)
     l = _vector(lse, "lse", p.t, _FLOATS, index)
     g = None if grad is None else _vector(grad, "grad", p.t, _FLOATS, index)
+    given = [a for a in (dx, dtable) if a is not None]
     with _On(index):
         dx, pdx, lddx, dtable, pde, ldde = _gradient_buffers(x, table, dx, dtable, need)
         ws, n = _workspace(p, GRAD, x.device)
         _check(_lib().ccdpp_softmax_loss_grad(ctypes.byref(p), l, g, pdx, lddx, pde, ldde, ws.data_ptr(), n, _stream(index)))
+    if given:
+        _written(given)
     return dx, dtable
 
 
@@ -182,6 +189,7 @@ def softmax_loss_train(x, table, target, *, grad=None, scale=1.0, offset=None, d
     p, index = _problem(x, table, target, scale, offset)
     g = None if grad is None else _vector(grad, "grad", p.t, _FLOATS, index)
     device = x.device
+    given = [a for a in (dx, dtable) if a is not None]
     with _On(index):
         loss = torch.empty(p.t, dtype=torch.float32, device=device)
         lse = torch.empty(p.t, dtype=torch.float32, device=device)
@@ -189,6 +197,8 @@ def softmax_loss_train(x, table, target, *, grad=None, scale=1.0, offset=None, d
         ws, n = _workspace(p, TRAIN, device)
         _check(_lib().ccdpp_softmax_loss_train(ctypes.byref(p), loss.data_ptr(), lse.data_ptr(), g, pdx, lddx, pde, ldde,
                                                ws.data_ptr(), n, _stream(index)))
+    if given:
+        _written(given)
     return loss, lse, dx, dtable
 
 
@@ -207,8 +217,7 @@ def _each(method, tensors):
 
 
 def _tensors(tensors, out):
-    """(device index, n, and the library's tables of) the gradients and what they are clipped into."""
-    tensors = list(tensors)
+    """(device index, n, the library's tables of) the gradients and what they are clipped into; `tensors` is a list."""
     n = len(tensors)
     T = torch.Tensor
     where = set(_each(T.get_device, tensors))  # (a TypeError for what is no tensor)
@@ -225,7 +234,6 @@ def _tensors(tensors, out):
     P = ctypes.c_void_p * n
     ins = outs = P(*_each(T.data_ptr, tensors))
     if out is not None:
-        out = list(out)
         if len(out) != n:
             raise ValueError("out must have one tensor for each gradient")
         if (not set(_each(T.get_device, out)) <= where or [o.dtype for o in out] != dtypes or _each(T.numel, out) != sizes
@@ -247,7 +255,7 @@ def _norm_workspace_bytes():
 
 def grad_norm(tensors):
     """The 2-norm of all values of the tensors together: a float32 scalar in device memory."""
-    index, n, ptrs, _, sizes, dtypes = _tensors(tensors, None)
+    index, n, ptrs, _, sizes, dtypes = _tensors(list(tensors), None)
     with _On(index):
         device = torch.device("cuda", index)
         norm = torch.empty((), dtype=torch.float32, device=device)
@@ -260,6 +268,7 @@ def clip_grads(tensors, max_norm, *, eps=1e-6, out=None):
     """Multiplies all tensors with min(1, max_norm / (norm + eps)), in place or into `out`; returns their norm before
     that (a float32 scalar in device memory).  A norm that is NaN makes every value NaN, an infinite one the finite
     values 0."""
+    tensors, out = list(tensors), None if out is None else list(out)
     index, n, ptrs, outs, sizes, dtypes = _tensors(tensors, out)
     with _On(index):
         device = torch.device("cuda", index)
@@ -267,4 +276,5 @@ def clip_grads(tensors, max_norm, *, eps=1e-6, out=None):
         ws = torch.empty(_norm_workspace_bytes(), dtype=torch.uint8, device=device)
         _check(_lib().ccdpp_clip_grads(n, ptrs, outs, sizes, dtypes, max_norm, eps, norm.data_ptr(), ws.data_ptr(), ws.numel(),
                                        _stream(index)))
+    _written(tensors if out is None else out)
     return norm
