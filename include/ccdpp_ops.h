@@ -96,14 +96,18 @@ int ccdpp_softmax_workspace(const ccdpp_softmax_t *p, int32_t call, int64_t *byt
 int ccdpp_softmax_loss(const ccdpp_softmax_t *p, float *loss, float *lse, void *workspace,
                        int64_t workspace_bytes, void *stream);
 
-/* Gradients of sum_t grad_t loss_t, from the lse of ccdpp_softmax_loss:
+/* Gradients of sum_t grad_t loss_t, from the lse of ccdpp_softmax_loss on the same problem (a
+ * lower one gives terms beyond their weight, which overflow to infinities and NaN from 8 times on):
  *   dx_t = scale sum_v G_tv e_v,  dtable_v = scale sum_t G_tv x_t,
  *   G_tv = grad_t (exp(z_tv - lse_t) - [v = target_t]).
  *   grad          : float[t], or NULL for ones
  *   dx, lddx      : t rows of d values of p->dtype, lddx >= d values apart; may be NULL
  *   dtable, lddt  : v rows likewise; may be NULL
- * Sums are held in 32 bits and rounded once to p->dtype; the terms G_tv have 11 bits
- * at least (22 for 32-bit types, and for 16-bit ones with d <= 128 or t <= 32, 16 at least). */
+ * Sums are held in 32 bits and rounded once to p->dtype.  The terms G_tv are rounded to 11 bits
+ * for 16-bit types with d > 128 and t > 32, to 16 at least for other 16-bit ones, and to 22 for 32-bit
+ * types (t <= 32: as they are), but none by more than 2^-29 of its row's weight for dx and 2^-19 of its
+ * item's largest term for dtable: light rows and unlikely items keep their digits.  32-bit x and
+ * tables have 22 bits of each value down to 2^-17 of the largest of all, 2^-39 of that below it. */
 int ccdpp_softmax_loss_grad(const ccdpp_softmax_t *p, const float *lse, const float *grad,
                             void *dx, int64_t lddx, void *dtable, int64_t lddt,
                             void *workspace, int64_t workspace_bytes, void *stream);
@@ -128,7 +132,8 @@ int ccdpp_grad_norm(int32_t n, const void *const *tensors, const int64_t *sizes,
  *   out      : host array of n device pointers; out[i] == tensors[i] clips in place (no
  *              other overlap).  In place, tensors are not written where c is 1.
  *   max_norm : >= 0 (may be infinite); eps : >= 0
- * A norm that is NaN makes every output NaN; one that is infinite makes c = 0. */
+ * A norm that is NaN makes every output NaN; one that is infinite makes c = 0 (1 where max_norm is, too).
+ * Tensors that share memory with one another are not clipped twice but undefined. */
 int ccdpp_clip_grads(int32_t n, const void *const *tensors, void *const *out, const int64_t *sizes,
                      const int32_t *dtypes, float max_norm, float eps, float *norm, void *workspace,
                      int64_t workspace_bytes, void *stream);

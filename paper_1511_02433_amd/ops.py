@@ -155,7 +155,8 @@ def softmax_loss(x, table, target, *, scale=1.0, offset=None):
     """(loss, lse), float32 per row: lse[i] = log sum_v exp(scale x_i.table_v + offset_v), loss[i] = lse[i] - the
     target's logit.  x: t x d, table: v x d (float32, bfloat16 or float16; rows may lie apart), target: int32 or int64.
     A negative target marks an ignored row (loss 0); one past the table makes the row's loss NaN.  offset: float32 per
-    item or None; -inf (or anything below -1e38) excludes an item, and a target that is excluded has loss +inf."""
+    item or None; -inf (or anything below -1e38) excludes an item, and a target that is excluded has loss +inf.  No graph is
+    recorded, whatever x and table require: softmax_loss_grad and softmax_loss_train give the gradients."""
     p, index = _problem(x, table, target, scale, offset)
     device = x.device
     with _On(index):
@@ -267,7 +268,8 @@ def grad_norm(tensors):
 def clip_grads(tensors, max_norm, *, eps=1e-6, out=None):
     """Multiplies all tensors with min(1, max_norm / (norm + eps)), in place or into `out`; returns their norm before
     that (a float32 scalar in device memory).  A norm that is NaN makes every value NaN, an infinite one the finite
-    values 0."""
+    values 0 (unless max_norm is infinite, too).  A tensor is there once: one that shares memory with another would be
+    read by one block while another clips it."""
     tensors, out = list(tensors), None if out is None else list(out)
     index, n, ptrs, outs, sizes, dtypes = _tensors(tensors, out)
     with _On(index):
