@@ -9,7 +9,7 @@
 // v_mfma_f32_32x32x16 operand in lane order (lane l: row l % 32, columns 8 (l / 32) .. + 7), 1 KB in one piece.  k_pack
 // brings x and the table into that order once per call, zero-padded, both as they are and turned (for the
 // contraction over their rows), whatever their strides, alignment and type.  32-bit values become two half-precision
-// planes, hi + lo, under a common power of two; a product of such matrices is the three products hi hi + hi lo +
+// planes, hi + lo, under powers of two (each row's own for the logits, the matrix's for the gradients); a product of such matrices is the three products hi hi + hi lo +
 // lo hi, summed in the same accumulator (lo lo is below 2^-22 of the result).
 //
 // The accumulator of the logits holds, per lane, one row t and 16 table entries v = 8 q + 4 h + r (h = lane / 32): those
@@ -331,7 +331,7 @@ __global__ __launch_bounds__(256) void k_pack(PackArgs a) {
 // (128 KB) are filled directly, three ahead.  Bound by the matrix cores at the clock that their power leaves (1.5 to
 // 2.1 GHz): logits of 8,192 x 131,072 x 4,096 in bfloat16 7.3 ms (1.21 PFLOP/s), their G 1.84 ms and either gradient
 // 1.78 ms per 32,768 entries (1.19 and 1.24 PFLOP/s; a large library product reaches 1.35); 2,000 x 32,003 x 1,024 in 32
-// bits (three products) 330 us, 1.19 PFLOP/s.
+// bits (three products) 358 us, 1.10 PFLOP/s.
 enum { EPI_LSE = 0, EPI_G = 1, EPI_OUT = 2 };
 
 struct GemmArgs {
@@ -922,7 +922,7 @@ __global__ __launch_bounds__(256) void k_join(JoinArgs a) {
 }
 
 // The terms of 64 rows x 32 entries a wave: from rows (pitch), or from what k_gemm kept (pitch 0; v0 is the piece's first
-// entry).  Bound by memory (2,000 x 32,003 in two planes: 143 us, 5.4 TB/s).
+// entry).  Bound by memory (2,000 x 32,003 in two planes: 145 us, 5.3 TB/s).
 template <class PG, int NPL>
 __global__ __launch_bounds__(256) void k_terms(GemmArgs a, const float* z, int64_t pitch) {
     const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
@@ -951,7 +951,7 @@ __global__ __launch_bounds__(256) void k_terms(GemmArgs a, const float* z, int64
 }
 
 // One power of two for each item over all groups of 64 rows, the lowest of theirs: fragments of G^T that have another one are
-// brought to it (most have none of their own, and nothing is moved).  A block per 32 items.
+// brought to it (most have none of their own, and nothing is moved: 1,003 x 50,021 then take 5 us).  A block per 32 items.
 template <int NPL>
 __global__ __launch_bounds__(256) void k_levels(GemmArgs a) {
     __shared__ int low[8][32];

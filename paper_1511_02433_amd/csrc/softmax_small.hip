@@ -9,10 +9,10 @@
 //
 // Per tile and wave the matrix cores need 32 cycles a product, 3 (d / 16) + 6 (d / 32) of them for 32-bit values, the
 // vector units 16 values of some 5 instructions and an exponential (and the split into two halves): at d = 100 the
-// products bound it, at d = 40 the logits' exponentials do.  Measured, in 32 bits: the logits of 1,500 x 624,961 x 40 306 us
-// (3.1 10^12 exponentials a second, 0.9 PFLOP/s of products), of 4,096 x 17,770 x 100 59 us; both gradients of the latter 225 us (1.2
-// PFLOP/s of products executed, in 2 blocks a CU), of 1,024 x 10,681 x 40 25 us.  A matrix instruction and the vector
-// instructions of the terms take turns at issuing, so neither reaches its rate alone.
+// products bound it, at d = 40 the logits' exponentials do.  Measured, in 32 bits: the logits of 1,500 x 624,961 x 40 302 us
+// (3.1 10^12 exponentials a second, 0.9 PFLOP/s of products), of 4,096 x 17,770 x 100 56 us; both gradients of the latter 225 us (1.2
+// PFLOP/s of products executed, in 2 blocks a CU), of 1,024 x 10,681 x 40 25 us.  Within a wave a tile's exponentials follow its
+// products; the matrix cores are busy 58% of the time, and the CU's other waves fill the rest in part.
 #include "softmax_device.hpp"
 
 namespace ccdops {
