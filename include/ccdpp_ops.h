@@ -63,8 +63,7 @@ enum ccdpp_dtype {
  * multiplied as they are for t <= 32 (for the logits also t <= 128 where d > 128), and as
  * sums of two halves with 11 bits each otherwise: 22 bits of every value down to 2^-17 of
  * the largest of its row (of x or of the table), and 2^-39 of that largest below it.  (With
- * d <= 128 and scaled rows of x whose norm times the table's largest value is at most
- * some 20, values are held to 2^-25 or better of the table's largest and its inverse, which is 5e-7 of a logit.)
+ * d <= 128, of the table's largest, or to what is some 5e-7 of a logit, where x is small enough for that.)
  * A logit's and a probability's relative error are some 5e-7 (1 + |z|), what a logit and
  * its lse have in 32 bits.
  */

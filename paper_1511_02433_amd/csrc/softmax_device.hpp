@@ -49,17 +49,20 @@ __device__ __forceinline__ int scale_exp(float top) {
     return min(126, 14 - e);
 }
 
-// Power of two that brings the table to [1, 2) for the logits.
+// Power of two that brings the table to [4, 8) for the logits.
 __device__ __forceinline__ int unit_exp(float top) {
     if (!(top > 0.f)) return 0;
-    return max(-126, min(126, 127 - (int)(__float_as_uint(top) >> 23)));
+    return max(-126, min(126, 129 - (int)(__float_as_uint(top) >> 23)));
 }
 
 // Two half-precision planes hold a value to 22 bits of itself, or to 2^-25.  With the whole table under one power of two
-// (unit_exp) and x under its inverse the products are logits as they are, and what the table's values lack of 22 bits
-// costs a logit some 2^-26 |x'|, x' being the row of x as it is multiplied.  Up to this |x'| that is 5e-7; beyond it a
-// large value of the table could cost other items their digits, and every row of either side gets a power of two of its own.
-constexpr float kUnitNorm = 32.f;
+// (unit_exp) and x under its inverse the products are logits as they are, and what the table's and x's values lack of 22 bits
+// costs a logit some 2^-26 |x'| and 2^-26 |e'|, x' and e' being the rows as they are multiplied.  Up to kUnitNorm that is
+// 5e-7 each (|e'| is 12 for 40 factors and 22 for 128, if the largest is five deviations).  Beyond it a large value of the table could cost other items their digits: rows of x get powers of two of their own, so that the table's
+// can be 2^14 higher (a factor for each row of x), which is as good up to kFactorNorm, and from there on the table's rows have
+// their own, too.  (1,500 x 624,961 x 40 floats, the three ways: 330, 384 and 429 us.)
+constexpr float kUnitNorm = 32.f, kFactorNorm = 32.f * 16384.f;
+enum { kUnit = 0, kFactor = 1, kOwn = 2 };
 
 // Value in planes: hi + lo, 22 bits; lo stays 0 where hi is not finite.
 template <class P, int NPL>
@@ -136,9 +139,9 @@ __device__ __forceinline__ void fetch(const char* from, char* to) {
 // rows [plane][step of 16 over d]; the rows' numbers, 32 floats each; the fragments of the turned rows
 // [plane][32 columns][2 steps of 16 rows].
 enum {
-    kNumFactor = 0,   // x: factor of the accumulated logits; of 32-bit rows an exponent, as int32 (0 unless rows have their own)
+    kNumFactor = 0,   // x: factor of the accumulated logits, or (kOwn) an exponent, as int32
     kNumOffset = 0,   // table: offset in base 2, -inf for excluded and missing entries
-    kNumExp = 1,      // table: the same exponent
+    kNumExp = 1,      // table: (kOwn) the exponent of its row
     kNumTerm = 1,     // x: log2 |weight| - lse in base 2, G's exponent: G = exp2(logit + term)
     kNumWeight = 2,   // x: |weight| with G's power of two
     kNumTarget = 3,   // x: target, as int32

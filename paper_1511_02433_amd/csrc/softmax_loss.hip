@@ -36,7 +36,7 @@ struct Scales {
     float *e_part, *x_part, *g_part;  // [kParts] largest |table| (excluded items apart), |x| of rows that count, |grad|
     float* n_part;                    // [kParts] largest 2-norm of a row of x (few factors)
     float *x_row, *e_row;             // [t], [v] largest |value| of each row; e_row: NULL where it is not asked for
-    int32_t* fin;                     // [4] exponents: table, x, G; whether rows have their own (few factors)
+    int32_t* fin;                     // [4] exponents: table, x, G; kUnit, kFactor or kOwn (few factors)
 };
 
 template <class T>
@@ -214,15 +214,17 @@ __global__ __launch_bounds__(256) void k_pack(PackArgs a) {
     // 32-bit rows of x are multiplied with scale and log2 e before they are split.
     const float before = NPL == 2 ? a.scale * kLog2e : 1.f;
     int exp = 0, unit = 0;  // powers of two of the turned matrix, and of the table as it is
-    bool own = !SMALL;      // rows have their own (32-bit values)
+    int way = kOwn;         // of 32-bit rows
     const bool leaves = blockIdx.x == 0 && blockIdx.y == 0;  // the exponents
     if (a.scaled || (leaves && a.weights)) {
         const Tops top = parts_max(a.sc, a.scaled, a.scaled && (is_x || leaves), leaves && a.weights, SMALL && NPL == 2, red);
         if constexpr (SMALL && NPL == 2) {
             unit = unit_exp(top.e);
-            own = !(top.n * fabsf(before) * pow2i(-unit) <= kUnitNorm);
-            if (leaves && threadIdx.x == 0) a.sc.fin[3] = own;
-            if (own && !is_x) {  // (all columns are here)
+            const float norm = top.n * fabsf(before) * pow2i(-unit);
+            way = norm <= kUnitNorm ? kUnit : norm <= kFactorNorm ? kFactor : kOwn;
+            if (way == kFactor) unit = scale_exp(top.e);
+            if (leaves && threadIdx.x == 0) a.sc.fin[3] = way;
+            if (way == kOwn && !is_x) {  // (all columns are here)
                 float most = 0.f;
 #pragma unroll
                 for (int k = 0; k < 2; ++k)
@@ -240,9 +242,9 @@ __global__ __launch_bounds__(256) void k_pack(PackArgs a) {
     }
     if (threadIdx.x < 32) {
         if (is_x) {
-            const int e = own ? scale_exp(row_top * fabsf(before)) : -unit;
+            const int e = way == kUnit ? -unit : scale_exp(row_top * fabsf(before));
             float f = row_in ? a.scale * kLog2e : 0.f;
-            if (NPL == 2) f = __int_as_float(own ? -e : 0);
+            if (NPL == 2) f = way == kOwn ? __int_as_float(-e) : way == kFactor ? ldexpf(1.f, -(e + unit)) : 1.f;
             exps[threadIdx.x] = e;
             if (blockIdx.y == 0) {
                 if (side.num) *(float*)(side.num + rt * side.num_row + (kNumFactor * 32 + threadIdx.x) * 4) = f;
@@ -255,10 +257,10 @@ __global__ __launch_bounds__(256) void k_pack(PackArgs a) {
                 }
             }
         } else {
-            const int e = own ? scale_exp(row_top) : unit;
+            const int e = way == kOwn ? scale_exp(row_top) : unit;
             exps[threadIdx.x] = e;
             if (blockIdx.y == 0 && side.num) *(float*)(side.num + rt * side.num_row + (kNumOffset * 32 + threadIdx.x) * 4) = row_live ? row_offset * kLog2e : -INFINITY;
-            if (NPL == 2 && own && blockIdx.y == 0 && side.exps) *(int*)(side.exps + rt * side.num_row + threadIdx.x * 4) = -e;
+            if (NPL == 2 && way == kOwn && blockIdx.y == 0 && side.exps) *(int*)(side.exps + rt * side.num_row + threadIdx.x * 4) = -e;
         }
         // Terms of few factors are exponentials, with no sign: a negative weight's is taken into the turned row.
         live[threadIdx.x] = !row_live ? 0.f : negative ? -1.f : 1.f;

@@ -140,15 +140,11 @@ __device__ __forceinline__ f32x16 row_numbers(const char* rows, int which, int h
 // first reference may be a finite mask's (-1e9), and what was added to that has lost its last digits.
 constexpr float kSumLimit = 1099511627776.f;
 
-// Logits from accumulated products of kept and streamed rows: `f` is x's number, `k` the table's exponent (32-bit values).
-template <int NPL>
-__device__ __forceinline__ float small_logit(float acc, float f, int k, float add) {
-    if constexpr (NPL == 2) return __builtin_amdgcn_ldexpf(acc, __float_as_int(f) + k) + add;
-    else return fmaf(acc, f, add);
-}
+// Logits from accumulated products of kept and streamed rows: `f` is x's number, `k` the table's exponent (kOwn).
+__device__ __forceinline__ float own_logit(float acc, float f, int k, float add) { return __builtin_amdgcn_ldexpf(acc, __float_as_int(f) + k) + add; }
 
-// UNIT: the accumulated products are the logits (32-bit values whose rows have no powers of two of their own).
-template <class P, int NPL, int KS, bool UNIT>
+// WAY: the accumulated products are the logits (kUnit), have a factor for each row of x (kFactor), or exponents (kOwn).
+template <class P, int NPL, int KS, int WAY>
 __device__ __forceinline__ void small_lse(const SmallArgs& a, int64_t first, int64_t last, const Kept<P, NPL, KS>& kept, float f, char* lds,
                                           float& ref_out, float& sum_out) {
     typedef Stream<P, NPL, KS, false> S;
@@ -160,13 +156,13 @@ __device__ __forceinline__ void small_lse(const SmallArgs& a, int64_t first, int
         const auto logits = [&](float from) {
             f32x16 z;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) z[r] = UNIT ? from : 0.f;
-            if (UNIT && offsets) z += row_numbers(slot + S::kRows * kBlk, kNumOffset, h);
+            for (int r = 0; r < 16; ++r) z[r] = WAY == kUnit ? from : 0.f;
+            if (WAY == kUnit && offsets) z += row_numbers(slot + S::kRows * kBlk, kNumOffset, h);
             z = tile_product<P, NPL, KS>(slot, kept, lane, z);
-            if constexpr (!UNIT) {
-                const f32x16 k = NPL == 2 ? row_numbers(slot + S::kRows * kBlk, kNumExp, h) : f32x16{};
+            if constexpr (WAY != kUnit) {
+                const f32x16 k = WAY == kOwn ? row_numbers(slot + S::kRows * kBlk, kNumExp, h) : f32x16{};
 #pragma unroll
-                for (int r = 0; r < 16; ++r) z[r] = small_logit<NPL>(z[r], f, __float_as_int(k[r]), from);
+                for (int r = 0; r < 16; ++r) z[r] = WAY == kOwn ? own_logit(z[r], f, __float_as_int(k[r]), from) : fmaf(z[r], f, from);
                 if (offsets) z += row_numbers(slot + S::kRows * kBlk, kNumOffset, h);
             }
             return z;
@@ -208,8 +204,10 @@ __global__ __launch_bounds__(256, small_lse_per_cu(NPL, KS)) void k_small_lse(Sm
         kept.load(mine, lane);
         const float f = *(const float*)(mine + S::kRows * kBlk + kNumFactor * 128 + n * 4);
         float top, sum;
-        if (NPL == 2 && !a.fin[3]) small_lse<P, NPL, KS, true>(a, first, last, kept, f, lds, top, sum);
-        else small_lse<P, NPL, KS, false>(a, first, last, kept, f, lds, top, sum);
+        const int way = NPL == 2 ? a.fin[3] : kFactor;
+        if (NPL == 2 && way == kUnit) small_lse<P, NPL, KS, kUnit>(a, first, last, kept, f, lds, top, sum);
+        else if (NPL == 2 && way == kOwn) small_lse<P, NPL, KS, kOwn>(a, first, last, kept, f, lds, top, sum);
+        else small_lse<P, NPL, KS, kFactor>(a, first, last, kept, f, lds, top, sum);
         const float top2 = __shfl_xor(top, 32), sum2 = __shfl_xor(sum, 32);
         const float m = fmaxf(top, top2), ref = m == -INFINITY ? 0.f : m;
         sum = sum * exp2_fast(top - ref) + sum2 * exp2_fast(top2 - ref);
@@ -239,8 +237,8 @@ __device__ __forceinline__ int small_terms(const SmallArgs& a, int64_t tile, int
     constexpr bool MOVES = ITEMS && std::is_same<P, HF>::value;
     int ref = 0;       // MOVES: terms are taken times 2^-ref
     float most = 0.f;  // and the largest one so far
-    const int own_exp = ITEMS && NPL == 2 ? __float_as_int(own[kNumExp * 32]) : 0;
-    const bool unit = NPL == 2 && !a.fin[3];
+    const int way = NPL == 2 ? a.fin[3] : kFactor;
+    const bool unit = way == kUnit;
     stream<S>(ITEMS ? a.xlive : a.e, ITEMS ? a.xlive_tile : a.e_tile, first, last, lds, [&](int64_t i, const char* slot) {
         const char* const rows = slot + S::kRows * kBlk;
         const int y = ITEMS ? ((const int*)rows)[kNumTarget * 32 + n] - (int)(tile * 32) : own_y - (int)(i * 32);
@@ -261,9 +259,16 @@ __device__ __forceinline__ int small_terms(const SmallArgs& a, int64_t tile, int
         z = tile_product<P, NPL, KS>(slot, kept, lane, z);
         if (!unit) {
             const f32x16 add = added();
-            const f32x16 f = ITEMS ? row_numbers(rows, kNumFactor, h) : NPL == 2 ? row_numbers(rows, kNumExp, h) : f32x16{};
+            if (NPL == 2 && way == kOwn) {
+                const f32x16 k = row_numbers(rows, ITEMS ? kNumFactor : kNumExp, h);
+                const float mine = ITEMS ? own[kNumExp * 32] : factor;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) z[r] = small_logit<NPL>(z[r], ITEMS ? f[r] : factor, ITEMS ? own_exp : __float_as_int(f[r]), add[r]);
+                for (int r = 0; r < 16; ++r) z[r] = own_logit(z[r], mine, __float_as_int(k[r]), add[r]);
+            } else {
+                const f32x16 f = ITEMS ? row_numbers(rows, kNumFactor, h) : f32x16{};
+#pragma unroll
+                for (int r = 0; r < 16; ++r) z[r] = fmaf(z[r], ITEMS ? f[r] : factor, add[r]);
+            }
         }
         // The first turned fragments arrive while the terms are computed.
         constexpr int kAhead = NPL == 2 ? 2 : 4;
