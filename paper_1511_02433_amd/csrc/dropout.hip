@@ -1,0 +1,91 @@
+// Dropout whose mask is drawn again wherever it is needed (gfx950).
+//
+//   y_ij = [residual_ij +] x_ij [r_ij >= p 2^32] / (1 - p)
+//
+// r is a word of Philox4x32 with 7 rounds, the fewest that pass the tests of its authors: four columns share a counter.
+#include <cmath>
+
+#include "ccdpp_seq.h"
+#include "ops_internal.hpp"
+
+namespace ccdops {
+namespace {
+
+struct Drop {
+    int64_t n, d, ldx, ldr, ldy, first_row;
+    const void *x, *residual;
+    void* y;
+    uint64_t seed;
+    const uint64_t* seed_at;
+    uint32_t least;   // words from here on are kept
+    int none;         // 1: nothing is kept
+    float scale;
+};
+
+struct Words { uint32_t w[4]; };
+
+// The keys of the rounds are the caller's, so that they are computed once.
+__device__ __forceinline__ Words philox(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t k0, uint32_t k1) {
+    uint32_t c3 = 0;
+#pragma unroll
+    for (int r = 0; r < 7; ++r) {
+        const uint64_t p = (uint64_t)c0 * 0xD2511F53u, q = (uint64_t)c2 * 0xCD9E8D57u;
+        c0 = (uint32_t)(q >> 32) ^ c1 ^ k0, c1 = (uint32_t)q;
+        c2 = (uint32_t)(p >> 32) ^ c3 ^ k1, c3 = (uint32_t)p;
+        k0 += 0x9E3779B9u, k1 += 0xBB67AE85u;
+    }
+    return {{c0, c1, c2, c3}};
+}
+
+// A thread takes four columns of a row.
+template <class T>
+__global__ __launch_bounds__(256) void k_drop(Drop a) {
+    const uint64_t seed = a.seed_at ? *a.seed_at : a.seed;
+    const int64_t fours = (a.d + 3) / 4, all = a.n * fours;
+    for (int64_t i = blockIdx.x * (int64_t)blockDim.x + threadIdx.x; i < all; i += (int64_t)gridDim.x * blockDim.x) {
+        const int64_t row = i / fours, q = i - row * fours;
+        const uint64_t at = (uint64_t)(a.first_row + row);
+        const Words w = philox((uint32_t)q, (uint32_t)at, (uint32_t)(at >> 32), (uint32_t)seed, (uint32_t)(seed >> 32));
+        for (int j = 0; j < 4; ++j) {
+            const int64_t c = 4 * q + j;
+            if (c >= a.d) break;
+            float v = !a.none && w.w[j] >= a.least ? (float)((const T*)a.x)[row * a.ldx + c] * a.scale : 0.f;
+            if (a.residual) v = (float)((const T*)a.residual)[row * a.ldr + c] + v;
+            ((T*)a.y)[row * a.ldy + c] = (T)v;
+        }
+    }
+}
+
+template <class F>
+void typed(int dtype, F&& body) {
+    if (dtype == CCDPP_F32) body(float());
+    else if (dtype == CCDPP_BF16) body((__bf16)0.f);
+    else body((_Float16)0.f);
+}
+
+}  // namespace
+}  // namespace ccdops
+
+extern "C" int ccdpp_dropout(int64_t n, int64_t d, int32_t dtype, const void* x, int64_t ldx, const void* residual, int64_t ldr, void* y,
+                             int64_t ldy, double p, uint64_t seed, const uint64_t* seed_at, int64_t first_row, void* stream) {
+    using namespace ccdops;
+    if (n < 0 || n >= (int64_t)1 << 31 || d < 1 || d >= (int64_t)1 << 31) return fail(CCDPP_EINVAL, "n must be in [0, 2^31) and d in [1, 2^31)");
+    if (dtype < CCDPP_F32 || dtype > CCDPP_F16) return fail(CCDPP_EINVAL, "dtype must be CCDPP_F32, CCDPP_BF16 or CCDPP_F16");
+    if (!(p >= 0.0 && p <= 1.0)) return fail(CCDPP_EINVAL, "p must be in [0, 1]");
+    if (first_row < 0 || first_row > INT64_MAX - n) return fail(CCDPP_EINVAL, "first_row must be >= 0, and no row beyond 2^63");
+    if (ldx < d || ldy < d || (residual && ldr < d)) return fail(CCDPP_EINVAL, "row strides must be at least d");
+    if (n > 0 && (!x || !y)) return fail(CCDPP_EINVAL, "x and y must be non-NULL");
+    const uintptr_t es = dtype == CCDPP_F32 ? 4 : 2;
+    if ((uintptr_t)x % es || (uintptr_t)y % es || (uintptr_t)residual % es || (uintptr_t)seed_at % 8)
+        return fail(CCDPP_EINVAL, "pointers must be aligned to their types");
+    if ((y == x && ldy != ldx) || (residual && y == residual && ldy != ldr)) return fail(CCDPP_EINVAL, "y in place must have the same row stride");
+    if (int rc = check_device()) return rc;
+    if (n == 0) return CCDPP_OK;
+    const double least = std::rint(p * 4294967296.0);
+    Drop a = {n, d, ldx, ldr, ldy, first_row, x, residual, y, seed, seed_at, 0, least >= 4294967296.0, 0.f};
+    if (!a.none) a.least = (uint32_t)least, a.scale = (float)(1.0 / (1.0 - p));
+    const int64_t blocks = (n * ((d + 3) / 4) + 255) / 256;
+    typed(dtype, [&](auto z) { k_drop<decltype(z)><<<(unsigned)(blocks < 8192 ? blocks : 8192), 256, 0, (hipStream_t)stream>>>(a); });
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? CCDPP_OK : hip_fail(e, "dropout");
+}
