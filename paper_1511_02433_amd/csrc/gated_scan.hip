@@ -2,13 +2,17 @@
 //
 //   h_t = a_t h_(t-1) + u_t;   GIVEN: a = gate, u = x;   SIGMOID: a = 1 / (1 + e^-gate), u = (1 - a) x
 //   l_t = dy_t + a_(t+1) l_(t+1);   dx_t = l_t (times 1 - a_t),  dgate_t = l_t h_(t-1)  (or l_t (h_(t-1) - x_t) a_t (1 - a_t))
+#include <algorithm>
+#include <type_traits>
+
 #include "ccdpp_seq.h"
 #include "ops_internal.hpp"
 
 namespace ccdops {
 namespace {
 
-constexpr int kKeep = 16;  // rows for each state that is kept
+constexpr int kRows = 16;      // of a chunk; one state of a chunk is kept
+constexpr int kThreads = 256;  // of a block
 
 // Both a and 1 - a to some 2^-22 of themselves, for gates of either sign: e = exp(-|gate|), with what the product by log2 e
 // rounds off put back.
@@ -30,6 +34,39 @@ __device__ __forceinline__ Terms terms_of(float x, float gate) {
     return {g.a, g.rest * x, g.rest};
 }
 
+// N values at an address that is aligned to their type alone, in one access.
+template <int N, class T>
+__device__ __forceinline__ Run<T, N> load_few(const T* at) {
+    constexpr int B = N * sizeof(T);
+    if constexpr (N == 1) return {{*at}};
+    else if constexpr (B == 4) {
+        typedef uint32_t loose __attribute__((aligned(2), may_alias));
+        return __builtin_bit_cast(Run<T, N>, (uint32_t)*(const loose*)at);
+    } else return load_run<N>(at);
+}
+template <int N, class T>
+__device__ __forceinline__ void store_few(T* at, Run<T, N> r) {
+    constexpr int B = N * sizeof(T);
+    if constexpr (N == 1) *at = r.v[0];
+    else if constexpr (B == 4) {
+        typedef uint32_t loose __attribute__((aligned(2), may_alias));
+        *(loose*)at = __builtin_bit_cast(uint32_t, r);
+    } else store_run<N>(at, r);
+}
+
+// Where a share of rows begins.  q >= 0: within sequence q, which has rows prev to next - 1; else where a sequence begins, or in no
+// sequence at all.
+struct Share {
+    int64_t begin, prev, next;
+    int64_t q;
+};
+// kRows rows of a chunk: the sequence of the first one (-1 or s: none), and a bit for each row that begins a sequence (or the rows
+// behind all), bit kRows for the row after the chunk.
+struct Chunk {
+    int32_t q;
+    uint32_t begins;
+};
+
 struct Scan {
     int64_t n, s, ldx, ldg, ldy, lddx, lddg;
     int d, bits;
@@ -37,6 +74,15 @@ struct Scan {
     const float *initial, *dlast, *kept;
     void *y, *dx, *dgate;  // y: the states, or dy
     float *last, *keep, *dinitial;
+    // How the work is shared out.
+    int strips, lanes, groups, shares;  // a block has `groups` groups of `lanes` lanes
+    int64_t rows;                       // of a share, before it is moved to where a sequence begins
+    int64_t chunks;
+    Share* share;      // shares + 1
+    Chunk* chunk;      // chunks
+    int32_t* of_row;   // the sequence that begins at a row, for such rows alone
+    float* carry;      // A and H of each share and column
+    int sums, tables, marks;  // blocks of each kind in the first launch
 };
 
 __device__ __forceinline__ int64_t start_of(const Scan& a, int64_t q) {
@@ -44,55 +90,510 @@ __device__ __forceinline__ int64_t start_of(const Scan& a, int64_t q) {
     return min(max(v, (int64_t)0), a.n);
 }
 
-// Rows that belong to no sequence get zeros; a block takes rows in turn.
+// The first of the s + 1 starts that is at least `row`, by a wave: 64 probes at a time.
+__device__ int64_t find_start(const Scan& a, int64_t row) {
+    int64_t lo = 0, hi = a.s + 1;
+    while (lo < hi) {
+        const int64_t step = (hi - lo + 63) / 64, at = lo + (threadIdx.x & 63) * step;
+        const int below = __popcll(__ballot(at < hi && start_of(a, min(at, a.s)) < row));
+        const int64_t from = lo;
+        if (below) lo = from + (below - 1) * step + 1;
+        if (below < 64) hi = min(hi, from + below * step);
+    }
+    return lo;
+}
+
+// Share p begins at row p * rows, or where a sequence does if that is no more than a quarter of a share away: what goes on from one
+// share to the next costs a second pass over its rows.
+__device__ Share share_of(const Scan& a, int64_t p) {
+    if (p <= 0) return {0, 0, 0, -1};
+    if (p >= a.shares) return {a.n, 0, 0, -1};
+    const int64_t row = p * a.rows, j = find_start(a, row), near = a.rows / 4;
+    const int64_t next = j <= a.s ? start_of(a, j) : a.n, prev = j > 0 ? start_of(a, j - 1) : 0;
+    if (next >= row && next - row <= near) return {next, 0, 0, -1};
+    if (j > 0 && prev <= row && row - prev <= near) return {prev, 0, 0, -1};
+    if (j == 0 || j > a.s || prev > row || next < row) return {row, 0, 0, -1};
+    return {row, prev, next, j - 1};
+}
+
+// What a chain of rows does to the state before it: A state + H; where a sequence begins in it the state behind it is H, whatever
+// was before (A is kReset then, a bit pattern that no product has: products have no signalling NaN).
+constexpr uint32_t kReset = 0x7F800001u;
+
+// A thread's place: `lanes` lanes side by side take the columns of a strip, W each, and `groups` of them a chunk each, one after
+// another.  The last lanes of a row take its last W columns, if need be with another lane, which gets the same.
+template <int W>
+struct Place {
+    int lane, group, col;
+    bool works;
+    __device__ Place(const Scan& a, int strip) {
+        group = threadIdx.x / a.lanes, lane = threadIdx.x - group * a.lanes;
+        works = group < a.groups;
+        col = min((strip * a.lanes + lane) * W, a.d - W);
+    }
+};
+
+template <int W>
+struct Exchange {
+    float A[2][W][kThreads], H[2][W][kThreads];
+};
+
+// Joins the chains of a block's groups: c goes in as the state before all of them and out as that behind all; returns the state
+// before this group.  One barrier a step; steps alternate between two buffers.
+template <int W>
+__device__ __forceinline__ void join(const Scan& a, Exchange<W>& e, const Place<W>& at, int step, const float (&A)[W], const float (&H)[W], bool reset, float (&c)[W],
+                                     float (&mine)[W]) {
+    const int b = step & 1;
+#pragma unroll
+    for (int w = 0; w < W; ++w) e.A[b][w][threadIdx.x] = reset ? __uint_as_float(kReset) : A[w], e.H[b][w][threadIdx.x] = H[w];
+    __syncthreads();
+    for (int g = 0; g < a.groups; ++g) {
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            const float p = e.A[b][w][g * a.lanes + at.lane], q = e.H[b][w][g * a.lanes + at.lane];
+            if (g == at.group) mine[w] = c[w];
+            c[w] = __float_as_uint(p) == kReset ? q : fmaf(p, c[w], q);
+        }
+    }
+}
+
+// The address of the next row from that of this one: sixteen multiples of every stride at once would not stay in registers.
 template <class T>
-__global__ __launch_bounds__(256) void k_outside(Scan a, void* y, int64_t ldy) {
-    const int64_t lo = a.s ? start_of(a, 0) : a.n, hi = a.s ? start_of(a, a.s) : a.n;
-    for (int64_t r = blockIdx.x; r < a.n; r += gridDim.x) {
-        if (r >= lo && r < hi) continue;
-        for (int c = threadIdx.x; c < a.d; c += 256) ((T*)y)[r * ldy + c] = (T)0.f;
-    }
+__device__ __forceinline__ void next(T*& at, int64_t ld) {
+    at += ld;
+    asm("" : "+v"(at));
 }
 
-// A thread for each sequence and column.
-template <class T, bool SIGMOID>
-__global__ __launch_bounds__(64) void k_scan(Scan a) {
-    const int64_t q = blockIdx.x;
-    const int64_t lo = start_of(a, q), hi = start_of(a, q + 1);
-    for (int c = threadIdx.x; c < a.d; c += 64) {
-        float h = a.initial ? a.initial[q * a.d + c] : 0.f;
-        for (int64_t t = lo; t < hi; ++t) {
-            if (a.keep && t % kKeep == 0) a.keep[t / kKeep * a.d + c] = h;
-            const Terms m = terms_of<SIGMOID>((float)((const T*)a.x)[t * a.ldx + c], (float)((const T*)a.gate)[t * a.ldg + c]);
-            h = fmaf(m.a, h, m.u);
-            ((T*)a.y)[t * a.ldy + c] = (T)h;
-        }
-        if (a.last) a.last[q * a.d + c] = h;
-    }
-}
-
-template <class T, bool SIGMOID>
-__global__ __launch_bounds__(64) void k_scan_grad(Scan a) {
-    const int64_t q = blockIdx.x;
-    const int64_t lo = start_of(a, q), hi = start_of(a, q + 1);
-    for (int c = threadIdx.x; c < a.d; c += 64) {
-        float m = a.dlast ? a.dlast[q * a.d + c] : 0.f;
-        for (int64_t t = hi - 1; t >= lo; --t) {
-            // The state before row t, from what was kept last.
-            const int64_t from = max(t / kKeep * kKeep, lo);
-            float h = from == lo ? (a.initial ? a.initial[q * a.d + c] : 0.f) : a.kept[t / kKeep * a.d + c];
-            for (int64_t i = from; i < t; ++i) {
-                const Terms w = terms_of<SIGMOID>((float)((const T*)a.x)[i * a.ldx + c], (float)((const T*)a.gate)[i * a.ldg + c]);
-                h = fmaf(w.a, h, w.u);
+template <class T, int W>
+struct Rows {
+    Run<T, W> v[kRows];
+    // Those of a chunk; rows from n on are not read.
+    __device__ __forceinline__ void load(const void* base, int64_t ld, int64_t row, int64_t n, int col) {
+        const T* at = (const T*)base + row * ld + col;
+        if (row + kRows <= n) {
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) v[i] = load_few<W>(at), next(at, ld);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) {
+                if (row + i < n) v[i] = load_few<W>(at);
+                next(at, ld);
             }
-            const float x = (float)((const T*)a.x)[t * a.ldx + c];
-            const Terms w = terms_of<SIGMOID>(x, (float)((const T*)a.gate)[t * a.ldg + c]);
-            const float l = (float)((const T*)a.y)[t * a.ldy + c] + m;
-            ((T*)a.dx)[t * a.lddx + c] = (T)(SIGMOID ? w.rest * l : l);
-            ((T*)a.dgate)[t * a.lddg + c] = (T)(SIGMOID ? l * (h - x) * (w.a * w.rest) : l * h);
-            m = w.a * l;
         }
-        if (a.dinitial) a.dinitial[q * a.d + c] = m;
+    }
+};
+
+// A row of the s x d states of sequences; NULL for what is no sequence.
+template <class P>
+__device__ __forceinline__ P* states_of(const Scan& a, P* base, int64_t q, int col) {
+    return base && (uint64_t)q < (uint64_t)a.s ? base + q * a.d + col : nullptr;
+}
+
+// The rows of a chunk within [lo, hi), as bits.
+__device__ __forceinline__ uint32_t rows_within(int64_t row, int64_t lo, int64_t hi) {
+    const int from = (int)min(max(lo - row, (int64_t)0), (int64_t)kRows), to = (int)min(max(hi - row, (int64_t)0), (int64_t)kRows);
+    return to > from ? ((1u << to) - 1) & ~((1u << from) - 1) : 0u;
+}
+
+constexpr uint32_t kAll = (1u << kRows) - 1;
+
+// The first launch: what the rows of a sequence that goes on behind a share do to the state before them (for the gradients: of one that
+// began before it), for every share and strip; the shares; the chunks; and the states of sequences without rows.
+template <class T, int W, bool SIGMOID, bool GRAD>
+__global__ __launch_bounds__(kThreads) void k_scan_first(Scan a) {
+    __shared__ Exchange<W> e;
+    __shared__ Share two[2];
+    const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    int block = blockIdx.x;
+    if (block < a.sums) {
+        const int strip = block % a.strips, p = block / a.strips + (GRAD ? 1 : 0);
+        if (wave < 2) {
+            const Share s = share_of(a, p + wave);
+            if ((threadIdx.x & 63) == 0) two[wave] = s;
+        }
+        __syncthreads();
+        const Share at_begin = two[0], at_end = two[1];
+        const Share& edge = GRAD ? at_begin : at_end;
+        if (edge.q < 0) return;
+        const int64_t lo = GRAD ? at_begin.begin : max(at_begin.begin, edge.prev), hi = GRAD ? min(at_end.begin, edge.next) : at_end.begin;
+        const Place<W> at(a, strip);
+        const int64_t c0 = lo / kRows, c1 = (hi + kRows - 1) / kRows;
+        float A[W], C[W];  // of all rows so far
+#pragma unroll
+        for (int w = 0; w < W; ++w) A[w] = 1.f, C[w] = 0.f;
+        Rows<T, W> x, gate;  // x: dy for the gradients
+        const auto chunk_of = [&](int64_t step) { return GRAD ? c1 - 1 - step * a.groups - at.group : c0 + step * a.groups + at.group; };
+        const auto load = [&](int64_t step) {
+            const int64_t c = chunk_of(step);
+            if (!at.works || c < c0 || c >= c1) return;
+            gate.load(a.gate, a.ldg, c * kRows, a.n, at.col);
+            if (GRAD) x.load(a.y, a.ldy, c * kRows, a.n, at.col);
+            else x.load(a.x, a.ldx, c * kRows, a.n, at.col);
+        };
+        float first[W];  // the state before a sequence's first row, or behind its last one
+        const bool ends = GRAD ? edge.next <= at_end.begin : edge.prev >= at_begin.begin;
+        const float* from = GRAD ? a.dlast : a.initial;
+#pragma unroll
+        for (int w = 0; w < W; ++w) first[w] = ends && from ? from[edge.q * a.d + at.col + w] : 0.f;
+        load(0);
+        const int64_t steps = (c1 - c0 + a.groups - 1) / a.groups;
+        for (int64_t step = 0; step < steps; ++step) {
+            const int64_t c = chunk_of(step);
+            const uint32_t in = at.works && c >= c0 && c < c1 ? rows_within(c * kRows, lo, hi) : 0u;
+            float d[kRows][W], u[kRows][W];
+#pragma unroll
+            for (int i = 0; i < kRows; ++i)
+#pragma unroll
+                for (int w = 0; w < W; ++w) {
+                    const Terms m = terms_of<SIGMOID && !GRAD>((float)x.v[i].v[w], (float)gate.v[i].v[w]);
+                    d[i][w] = GRAD && SIGMOID ? sigmoid_of((float)gate.v[i].v[w]).a : m.a, u[i][w] = m.u;
+                }
+            if (in != kAll) {
+#pragma unroll
+                for (int i = 0; i < kRows; ++i)
+#pragma unroll
+                    for (int w = 0; w < W; ++w)
+                        if (!(in >> i & 1)) d[i][w] = 1.f, u[i][w] = 0.f;
+            }
+            load(step + 1);
+            float pa[W], ph[W], mine[W];
+            // (The state that comes in at lo, or at hi - 1, is put into that row: nothing comes before it.)
+            const int64_t mark = in ? (GRAD ? hi - 1 : lo) - c * kRows : -1;
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                pa[w] = 1.f, ph[w] = 0.f;
+#pragma unroll
+                for (int k = 0; k < kRows; ++k) {
+                    const int i = GRAD ? kRows - 1 - k : k;
+                    if (i == mark) ph[w] = first[w];
+                    pa[w] *= d[i][w];
+                    ph[w] = GRAD ? d[i][w] * (u[i][w] + ph[w]) : fmaf(d[i][w], ph[w], u[i][w]);
+                }
+            }
+            float all[W];
+#pragma unroll
+            for (int w = 0; w < W; ++w) all[w] = 1.f;
+            join<W>(a, e, at, (int)step, pa, ph, false, C, mine);
+            for (int g = 0; g < a.groups; ++g)
+#pragma unroll
+                for (int w = 0; w < W; ++w) all[w] *= e.A[step & 1][w][g * a.lanes + at.lane];
+#pragma unroll
+            for (int w = 0; w < W; ++w) A[w] *= all[w];
+        }
+        if (at.group == 0) {
+            float* out = a.carry + ((int64_t)p * a.d + at.col) * 2;
+#pragma unroll
+            for (int w = 0; w < W; ++w) out[2 * w] = A[w], out[2 * w + 1] = C[w];
+        }
+        return;
+    }
+    block -= a.sums;
+    if (block < a.tables) {
+        const int64_t c = block * (int64_t)blockDim.x + threadIdx.x;
+        if (c >= a.chunks) return;
+        // The first start from `row` on.
+        const auto find = [&](int64_t row, int64_t lo) {
+            int64_t hi = a.s + 1;
+            while (lo < hi) {
+                const int64_t mid = (lo + hi) / 2;
+                if (start_of(a, mid) < row) lo = mid + 1;
+                else hi = mid;
+            }
+            return lo;
+        };
+        const int64_t row = c * kRows;
+        int64_t j = find(row, 0), r = -1;
+        Chunk k = {(int32_t)(j - 1), 0u};
+        while (j <= a.s) {
+            const int64_t begin = start_of(a, j);
+            if (begin < row || begin > row + kRows || begin <= r) break;
+            r = begin;
+            const bool more = j < a.s && start_of(a, j + 1) == r;  // sequences without rows begin there, too
+            j = more ? find(r + 1, j + 1) : j + 1;
+            k.begins |= 1u << (r - row);
+            if (r == row) k.q = (int32_t)(j - 1);
+            if (r < row + kRows && r < a.n) a.of_row[r] = (int32_t)(j - 1);
+        }
+        a.chunk[c] = k;
+        return;
+    }
+    block -= a.tables;
+    if (block < a.marks) {
+        const int p = block * waves + wave;
+        if (p > a.shares) return;
+        const Share s = share_of(a, p);
+        if ((threadIdx.x & 63) == 0) a.share[p] = s;
+        return;
+    }
+    block -= a.marks;
+    float* const out = GRAD ? a.dinitial : a.last;
+    const float* const from = GRAD ? a.dlast : a.initial;
+    const int64_t q0 = ((int64_t)block * waves + wave) * 64, mine = q0 + (threadIdx.x & 63);
+    uint64_t none = __ballot(mine < a.s && start_of(a, min(mine, a.s)) >= start_of(a, min(mine + 1, a.s)));
+    while (none) {
+        const int64_t q = q0 + __ffsll((unsigned long long)none) - 1;
+        none &= none - 1;
+        for (int c = threadIdx.x & 63; c < a.d; c += 64) out[q * a.d + c] = from ? from[q * a.d + c] : 0.f;
+    }
+}
+
+// The state that comes into a share from those before it (for the gradients: after it): the groups take a part of the shares each, and
+// join what they have.
+template <int W, bool GRAD>
+__device__ void carry_in(const Scan& a, Exchange<W>& e, const Place<W>& at, int p, const Share& edge, float (&c)[W]) {
+#pragma unroll
+    for (int w = 0; w < W; ++w) c[w] = 0.f;
+    if (edge.q < 0) return;
+    // The share in which the sequence begins (ends); there, nothing comes in.
+    int far = (int)min(max((GRAD ? edge.next - 1 : edge.prev) / a.rows, (int64_t)0), (int64_t)a.shares - 1);
+    if (GRAD) {
+        far = max(far - 1, p + 1);
+        while (far + 1 < a.shares && a.share[far + 1].begin < edge.next) ++far;
+    } else {
+        far = min(far + 1, p - 1);
+        while (far > 0 && a.share[far].begin > edge.prev) --far;
+    }
+    const int count = GRAD ? far - p : p - far, per = (count + a.groups - 1) / a.groups;
+    const int from = min(at.group * per, count), to = min(from + per, count);
+    float A[W], H[W], mine[W];
+#pragma unroll
+    for (int w = 0; w < W; ++w) A[w] = 1.f, H[w] = 0.f;
+    if (at.works) {
+#pragma unroll 4
+        for (int i = from; i < to; ++i) {
+            const float* k = a.carry + ((int64_t)(GRAD ? far - i : far + i) * a.d + at.col) * 2;
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                const float f = k[2 * w], g = k[2 * w + 1];
+                if (i == 0) H[w] = g;
+                else H[w] = fmaf(f, H[w], g), A[w] *= f;
+            }
+        }
+    }
+    join<W>(a, e, at, 0, A, H, at.works && from == 0 && to > 0, c, mine);
+    __syncthreads();
+}
+
+template <class T, int W, bool SIGMOID>
+__global__ __launch_bounds__(kThreads) void k_scan(Scan a) {
+    __shared__ Exchange<W> e;
+    const int strip = blockIdx.x % a.strips, p = blockIdx.x / a.strips;
+    const Place<W> at(a, strip);
+    const Share share = a.share[p];
+    const int64_t begin = share.begin, end = a.share[p + 1].begin;
+    const int64_t lo = a.s ? max(start_of(a, 0), begin) : end, hi = a.s ? min(start_of(a, a.s), end) : end;  // rows of sequences
+    const int64_t c0 = begin / kRows, c1 = (end + kRows - 1) / kRows, steps = (c1 - c0 + a.groups - 1) / a.groups;
+    Rows<T, W> x, gate;
+    Chunk k;
+    const auto load = [&](int64_t step) {
+        const int64_t c = c0 + step * a.groups + at.group;
+        if (!at.works || c >= c1) return;
+        k = a.chunk[c];
+        x.load(a.x, a.ldx, c * kRows, a.n, at.col);
+        gate.load(a.gate, a.ldg, c * kRows, a.n, at.col);
+    };
+    load(0);
+    float carry[W];
+    carry_in<W, false>(a, e, at, p, share, carry);
+    for (int64_t step = 0; step < steps; ++step) {
+        const int64_t c = c0 + step * a.groups + at.group, row = c * kRows;
+        const bool here = at.works && c < c1;
+        const uint32_t mine = here ? rows_within(row, begin, end) : 0u, in = here ? rows_within(row, lo, hi) : 0u;
+        const uint32_t firsts = here ? k.begins & mine : 0u, lasts = here ? k.begins >> 1 & in : 0u;
+        const bool plain = in == kAll && !(firsts | lasts);
+        int64_t q = k.q;
+        float d[kRows][W], u[kRows][W];
+#pragma unroll
+        for (int i = 0; i < kRows; ++i)
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                const Terms m = terms_of<SIGMOID>((float)x.v[i].v[w], (float)gate.v[i].v[w]);
+                d[i][w] = m.a, u[i][w] = m.u;
+            }
+        load(step + 1);
+        float A[W], H[W], h[W];
+#pragma unroll
+        for (int w = 0; w < W; ++w) A[w] = 1.f, H[w] = 0.f;
+        if (plain) {
+#pragma unroll
+            for (int i = 0; i < kRows; ++i)
+#pragma unroll
+                for (int w = 0; w < W; ++w) A[w] *= d[i][w], H[w] = fmaf(d[i][w], H[w], u[i][w]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) {
+                const bool inside = in >> i & 1, first = firsts >> i & 1;
+                const float* from = nullptr;
+                if (first && inside && a.initial) from = states_of(a, a.initial, a.of_row[row + i], at.col);
+#pragma unroll
+                for (int w = 0; w < W; ++w) {
+                    if (!inside) d[i][w] = 1.f, u[i][w] = 0.f;
+                    if (from) u[i][w] = fmaf(d[i][w], from[w], u[i][w]);
+                    A[w] *= d[i][w], H[w] = first ? u[i][w] : fmaf(d[i][w], H[w], u[i][w]);
+                }
+            }
+        }
+        join<W>(a, e, at, (int)step, A, H, firsts != 0, carry, h);
+        if (a.keep && (mine & 1)) {
+            Run<float, W> r;
+#pragma unroll
+            for (int w = 0; w < W; ++w) r.v[w] = h[w];
+            store_few<W>(a.keep + c * a.d + at.col, r);
+        }
+        T* y = (T*)a.y + row * a.ldy + at.col;
+        if (plain) {
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) {
+                Run<T, W> r;
+#pragma unroll
+                for (int w = 0; w < W; ++w) h[w] = fmaf(d[i][w], h[w], u[i][w]), r.v[w] = (T)h[w];
+                store_few<W>(y, r);
+                next(y, a.ldy);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) {
+                const bool inside = in >> i & 1, first = firsts >> i & 1;
+                if (first && inside) q = a.of_row[row + i];
+                Run<T, W> r;
+#pragma unroll
+                for (int w = 0; w < W; ++w) {
+                    h[w] = first ? u[i][w] : fmaf(d[i][w], h[w], u[i][w]);
+                    r.v[w] = inside ? (T)h[w] : (T)0.f;
+                }
+                if (mine >> i & 1) store_few<W>(y, r);
+                next(y, a.ldy);
+                if (float* const to = lasts >> i & 1 ? states_of(a, a.last, q, at.col) : nullptr)
+#pragma unroll
+                    for (int w = 0; w < W; ++w) to[w] = h[w];
+            }
+        }
+    }
+}
+
+template <class T, int W, bool SIGMOID>
+__global__ __launch_bounds__(kThreads) void k_scan_grad(Scan a) {
+    __shared__ Exchange<W> e;
+    const int strip = blockIdx.x % a.strips, p = blockIdx.x / a.strips;
+    const Place<W> at(a, strip);
+    const Share share = a.share[p + 1];
+    const int64_t begin = a.share[p].begin, end = share.begin;
+    const int64_t lo = a.s ? max(start_of(a, 0), begin) : end, hi = a.s ? min(start_of(a, a.s), end) : end;
+    const int64_t c0 = begin / kRows, c1 = (end + kRows - 1) / kRows, steps = (c1 - c0 + a.groups - 1) / a.groups;
+    Rows<T, W> x, gate, dy;
+    Run<float, W> h0;
+    Chunk k;
+    const auto load = [&](int64_t step) {
+        const int64_t c = c1 - 1 - step * a.groups - at.group;
+        if (!at.works || c < c0) return;
+        k = a.chunk[c];
+        h0 = load_few<W>(a.kept + c * a.d + at.col);
+        x.load(a.x, a.ldx, c * kRows, a.n, at.col);
+        gate.load(a.gate, a.ldg, c * kRows, a.n, at.col);
+        dy.load(a.y, a.ldy, c * kRows, a.n, at.col);
+    };
+    load(0);
+    float carry[W];
+    carry_in<W, true>(a, e, at, p, share, carry);
+    for (int64_t step = 0; step < steps; ++step) {
+        const int64_t c = c1 - 1 - step * a.groups - at.group, row = c * kRows;
+        const bool here = at.works && c >= c0;
+        const uint32_t mine = here ? rows_within(row, begin, end) : 0u, in = here ? rows_within(row, lo, hi) : 0u;
+        const uint32_t firsts = here ? k.begins & in : 0u, lasts = here ? k.begins >> 1 & in : 0u;
+        const bool plain = in == kAll && !(firsts | lasts);
+        const int64_t q0 = k.q;
+        // a and 1 - a, what l is multiplied by for dgate, and dy.
+        float d[kRows][W], rest[kRows][W], f[kRows][W], g[kRows][W];
+        float h[W];
+#pragma unroll
+        for (int w = 0; w < W; ++w) h[w] = h0.v[w];
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            const float* from = nullptr;
+            const bool first = !plain && (firsts >> i & 1);
+            if (first && a.initial) from = states_of(a, a.initial, a.of_row[row + i], at.col);
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                const float v = (float)x.v[i].v[w];
+                const Terms m = terms_of<SIGMOID>(v, (float)gate.v[i].v[w]);
+                d[i][w] = m.a, rest[i][w] = m.rest, g[i][w] = (float)dy.v[i].v[w];
+                if (first) h[w] = from ? from[w] : 0.f;
+                f[i][w] = SIGMOID ? (h[w] - v) * (m.a * m.rest) : h[w];
+                const bool inside = plain || (in >> i & 1);
+                h[w] = inside ? fmaf(m.a, h[w], m.u) : h[w];
+                if (!inside) d[i][w] = 1.f, g[i][w] = 0.f;
+            }
+        }
+        load(step + 1);
+        float A[W], H[W], m[W];
+#pragma unroll
+        for (int w = 0; w < W; ++w) A[w] = 1.f, H[w] = 0.f;
+        // The sequence of a row with a last one in its chunk.
+        const auto sequence_at = [&](int i) {
+            const uint32_t before = firsts & ((2u << i) - 1);
+            return before ? (int64_t)a.of_row[row + 31 - __builtin_clz(before)] : q0;
+        };
+        if (plain) {
+#pragma unroll
+            for (int i = kRows - 1; i >= 0; --i)
+#pragma unroll
+                for (int w = 0; w < W; ++w) A[w] *= d[i][w], H[w] = d[i][w] * (g[i][w] + H[w]);
+        } else {
+#pragma unroll
+            for (int i = kRows - 1; i >= 0; --i) {
+                const bool inside = in >> i & 1;
+                if (lasts >> i & 1) {
+                    const float* from = states_of(a, a.dlast, sequence_at(i), at.col);
+#pragma unroll
+                    for (int w = 0; w < W; ++w) H[w] = from ? from[w] : 0.f;
+                }
+#pragma unroll
+                for (int w = 0; w < W; ++w) A[w] *= d[i][w], H[w] = inside ? d[i][w] * (g[i][w] + H[w]) : H[w];
+            }
+        }
+        join<W>(a, e, at, (int)step, A, H, lasts != 0, carry, m);
+        T* dx = (T*)a.dx + (row + kRows - 1) * a.lddx + at.col;
+        T* dg = (T*)a.dgate + (row + kRows - 1) * a.lddg + at.col;
+        if (plain) {
+#pragma unroll
+            for (int i = kRows - 1; i >= 0; --i) {
+                Run<T, W> r, t;
+#pragma unroll
+                for (int w = 0; w < W; ++w) {
+                    const float l = g[i][w] + m[w];
+                    r.v[w] = (T)(SIGMOID ? rest[i][w] * l : l), t.v[w] = (T)(l * f[i][w]);
+                    m[w] = d[i][w] * l;
+                }
+                store_few<W>(dx, r);
+                store_few<W>(dg, t);
+                next(dx, -a.lddx), next(dg, -a.lddg);
+            }
+        } else {
+#pragma unroll
+            for (int i = kRows - 1; i >= 0; --i) {
+                const bool inside = in >> i & 1;
+                if (lasts >> i & 1) {
+                    const float* from = states_of(a, a.dlast, sequence_at(i), at.col);
+#pragma unroll
+                    for (int w = 0; w < W; ++w) m[w] = from ? from[w] : 0.f;
+                }
+                Run<T, W> r, t;
+#pragma unroll
+                for (int w = 0; w < W; ++w) {
+                    const float l = g[i][w] + m[w];
+                    r.v[w] = inside ? (T)(SIGMOID ? rest[i][w] * l : l) : (T)0.f, t.v[w] = inside ? (T)(l * f[i][w]) : (T)0.f;
+                    m[w] = inside ? d[i][w] * l : m[w];
+                }
+                if (mine >> i & 1) {
+                    store_few<W>(dx, r);
+                    store_few<W>(dg, t);
+                }
+                next(dx, -a.lddx), next(dg, -a.lddg);
+                if (float* const to = (firsts >> i & 1) && a.dinitial ? states_of(a, a.dinitial, a.of_row[row + i], at.col) : nullptr)
+#pragma unroll
+                    for (int w = 0; w < W; ++w) to[w] = m[w];
+            }
+        }
     }
 }
 
@@ -142,7 +643,67 @@ int check_pointers(const ccdpp_scan_t* p, const void* kept, const void* ws, int6
     return CCDPP_OK;
 }
 
-int64_t workspace(const ccdpp_scan_t*, int32_t) { return 256; }
+// How a call's work is shared out, and where its temporaries lie in the workspace (from 0 on).
+struct Layout {
+    int width, strips, lanes, groups, shares;
+    int64_t rows, chunks;
+    int64_t share, chunk, of_row, carry, bytes;
+};
+
+Layout layout(const ccdpp_scan_t* p) {
+    Layout l;
+    l.width = p->d >= 2 ? 2 : 1;
+    const int lanes = (p->d + l.width - 1) / l.width;
+    l.strips = (lanes + 63) / 64;
+    l.lanes = (lanes + l.strips - 1) / l.strips;
+    l.groups = std::min(kThreads / l.lanes, 64);
+    l.chunks = (p->n + kRows - 1) / kRows;
+    const int64_t most = std::max<int64_t>(1, 1024 / l.strips), least = std::max<int64_t>(1, 512 / l.strips);
+    int64_t shares = std::min(std::max(p->s, least), most);
+    shares = std::max<int64_t>(1, std::min(shares, l.chunks / l.groups));
+    l.rows = round_up((std::max<int64_t>(p->n, 1) + shares - 1) / shares, kRows);
+    l.shares = (int)((std::max<int64_t>(p->n, 1) + l.rows - 1) / l.rows);
+    l.share = 0;
+    l.chunk = round_up(l.share + (l.shares + 1) * (int64_t)sizeof(Share), 256);
+    l.of_row = round_up(l.chunk + l.chunks * (int64_t)sizeof(Chunk), 256);
+    l.carry = round_up(l.of_row + p->n * 4, 256);
+    l.bytes = round_up(l.carry + (int64_t)l.shares * p->d * 8, 256);
+    return l;
+}
+
+int64_t workspace(const ccdpp_scan_t* p, int32_t) { return layout(p).bytes; }
+
+void set(Scan& a, const ccdpp_scan_t* p, const Layout& l, void* ws) {
+    a.n = p->n, a.s = p->s, a.ldx = p->ldx, a.ldg = p->ldg, a.d = p->d, a.bits = p->starts_bits;
+    a.x = p->x, a.gate = p->gate, a.starts = p->starts, a.initial = p->initial;
+    a.strips = l.strips, a.lanes = l.lanes, a.groups = l.groups, a.shares = l.shares, a.rows = l.rows, a.chunks = l.chunks;
+    a.share = (Share*)((char*)ws + l.share), a.chunk = (Chunk*)((char*)ws + l.chunk), a.of_row = (int32_t*)((char*)ws + l.of_row);
+    a.carry = (float*)((char*)ws + l.carry);
+    a.sums = l.strips * (l.shares - 1);
+    a.tables = (int)((l.chunks + kThreads - 1) / kThreads);
+    a.marks = (l.shares + 1 + kThreads / 64 - 1) / (kThreads / 64);
+}
+
+template <bool GRAD>
+int launch(const ccdpp_scan_t* p, const Layout& l, const Scan& a, bool ends, hipStream_t st) {
+    const int64_t nones = ends ? (p->s + kThreads - 1) / kThreads : 0;
+    const int64_t first = (int64_t)a.sums + a.tables + a.marks + nones;
+    typed(p->dtype, p->mode, [&](auto z, auto sigmoid) {
+        typedef decltype(z) T;
+        constexpr bool S = decltype(sigmoid)::value;
+        const auto both = [&](auto w) {
+            constexpr int W = decltype(w)::value;
+            k_scan_first<T, W, S, GRAD><<<(unsigned)first, kThreads, 0, st>>>(a);
+            if (p->n == 0) return;
+            if constexpr (GRAD) k_scan_grad<T, W, S><<<(unsigned)(l.strips * l.shares), kThreads, 0, st>>>(a);
+            else k_scan<T, W, S><<<(unsigned)(l.strips * l.shares), kThreads, 0, st>>>(a);
+        };
+        if (l.width == 2) both(std::integral_constant<int, 2>());
+        else both(std::integral_constant<int, 1>());
+    });
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? CCDPP_OK : hip_fail(e, GRAD ? "gated scan gradients" : "gated scan");
+}
 
 }  // namespace
 }  // namespace ccdops
@@ -162,7 +723,7 @@ int ccdpp_scan_kept(const ccdpp_scan_t* p, int64_t* bytes) {
     using namespace ccdops;
     if (!bytes) return fail(CCDPP_EINVAL, "bytes is NULL");
     if (int rc = check(p)) return rc;
-    *bytes = (p->n + kKeep - 1) / kKeep * p->d * 4;
+    *bytes = (p->n + kRows - 1) / kRows * p->d * 4;
     return CCDPP_OK;
 }
 
@@ -174,17 +735,11 @@ int ccdpp_gated_scan(const ccdpp_scan_t* p, void* y, int64_t ldy, float* last, v
     if (ldy < p->d) return fail(CCDPP_EINVAL, "ldy must be at least d");
     if (misaligned(y, p->dtype == CCDPP_F32 ? 4 : 2) || misaligned(last, 4)) return fail(CCDPP_EINVAL, "pointers must be aligned to their types");
     if (int rc = check_device()) return rc;
+    const Layout l = layout(p);
     Scan a = {};
-    a.n = p->n, a.s = p->s, a.ldx = p->ldx, a.ldg = p->ldg, a.ldy = ldy, a.d = p->d, a.bits = p->starts_bits;
-    a.x = p->x, a.gate = p->gate, a.starts = p->starts, a.initial = p->initial, a.y = y, a.last = last, a.keep = (float*)kept;
-    hipStream_t st = (hipStream_t)stream;
-    typed(p->dtype, p->mode, [&](auto z, auto sigmoid) {
-        typedef decltype(z) T;
-        if (a.n) k_outside<T><<<1024, 256, 0, st>>>(a, y, ldy);
-        if (a.s) k_scan<T, decltype(sigmoid)::value><<<(unsigned)a.s, 64, 0, st>>>(a);
-    });
-    const hipError_t e = hipGetLastError();
-    return e == hipSuccess ? CCDPP_OK : hip_fail(e, "gated scan");
+    set(a, p, l, ws);
+    a.y = y, a.ldy = ldy, a.last = last, a.keep = (float*)kept;
+    return launch<false>(p, l, a, last != nullptr, (hipStream_t)stream);
 }
 
 int ccdpp_gated_scan_grad(const ccdpp_scan_t* p, const void* dy, int64_t lddy, const float* dlast, const void* kept, void* dx, int64_t lddx, void* dgate,
@@ -198,19 +753,12 @@ int ccdpp_gated_scan_grad(const ccdpp_scan_t* p, const void* dy, int64_t lddy, c
     if (misaligned(dy, es) || misaligned(dx, es) || misaligned(dgate, es) || misaligned(dlast, 4) || misaligned(dinitial, 4))
         return fail(CCDPP_EINVAL, "pointers must be aligned to their types");
     if (int rc = check_device()) return rc;
+    const Layout l = layout(p);
     Scan a = {};
-    a.n = p->n, a.s = p->s, a.ldx = p->ldx, a.ldg = p->ldg, a.ldy = lddy, a.lddx = lddx, a.lddg = lddg, a.d = p->d, a.bits = p->starts_bits;
-    a.x = p->x, a.gate = p->gate, a.starts = p->starts, a.initial = p->initial, a.dlast = dlast, a.kept = (const float*)kept;
-    a.y = const_cast<void*>(dy), a.dx = dx, a.dgate = dgate, a.dinitial = dinitial;
-    hipStream_t st = (hipStream_t)stream;
-    typed(p->dtype, p->mode, [&](auto z, auto sigmoid) {
-        typedef decltype(z) T;
-        if (a.n) k_outside<T><<<1024, 256, 0, st>>>(a, dx, lddx);
-        if (a.n) k_outside<T><<<1024, 256, 0, st>>>(a, dgate, lddg);
-        if (a.s) k_scan_grad<T, decltype(sigmoid)::value><<<(unsigned)a.s, 64, 0, st>>>(a);
-    });
-    const hipError_t e = hipGetLastError();
-    return e == hipSuccess ? CCDPP_OK : hip_fail(e, "gated scan gradients");
+    set(a, p, l, ws);
+    a.y = const_cast<void*>(dy), a.ldy = lddy, a.dlast = dlast, a.kept = (const float*)kept;
+    a.dx = dx, a.lddx = lddx, a.dgate = dgate, a.lddg = lddg, a.dinitial = dinitial;
+    return launch<true>(p, l, a, dinitial != nullptr, (hipStream_t)stream);
 }
 
 int ccdpp_gated_scan_step(int64_t n, int32_t d, int32_t dtype, int32_t mode, const void* x, int64_t ldx, const void* gate, int64_t ldg, float* state,
