@@ -34,25 +34,59 @@ __device__ __forceinline__ Terms terms_of(float x, float gate) {
     return {g.a, g.rest * x, g.rest};
 }
 
-// N values at an address that is aligned to their type alone, in one access.
-template <int N, class T>
-__device__ __forceinline__ Run<T, N> load_few(const T* at) {
-    constexpr int B = N * sizeof(T);
-    if constexpr (N == 1) return {{*at}};
-    else if constexpr (B == 4) {
-        typedef uint32_t loose __attribute__((aligned(2), may_alias));
-        return __builtin_bit_cast(Run<T, N>, (uint32_t)*(const loose*)at);
-    } else return load_run<N>(at);
-}
-template <int N, class T>
-__device__ __forceinline__ void store_few(T* at, Run<T, N> r) {
-    constexpr int B = N * sizeof(T);
-    if constexpr (N == 1) *at = r.v[0];
-    else if constexpr (B == 4) {
-        typedef uint32_t loose __attribute__((aligned(2), may_alias));
-        *(loose*)at = __builtin_bit_cast(uint32_t, r);
-    } else store_run<N>(at, r);
-}
+// W values of a row as they lie in memory, in one access that is aligned to their type alone.  Two of 16 bits stay one word until
+// they are used: of an array of them the compiler makes a register each.
+template <class T, int W>
+struct Few {
+    static_assert(W == 1 || sizeof(T) == 4, "");
+    Run<T, W> r;
+    __device__ __forceinline__ void load(const T* at) {
+        if constexpr (W == 1) r.v[0] = *at;
+        else r = load_run<W>(at);
+    }
+    __device__ __forceinline__ void store(T* at) const {
+        if constexpr (W == 1) *at = r.v[0];
+        else store_run<W>(at, r);
+    }
+    __device__ __forceinline__ float get(int w) const { return (float)r.v[w]; }
+    // The same, but unknown to the compiler: what it computes of it here is not computed before a branch for both its sides.
+    __device__ __forceinline__ Few again() const {
+        Few f = *this;
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int w = 0; w < W; ++w) asm("" : "+v"(f.r.v[w]));
+        } else {
+            uint32_t word = __builtin_bit_cast(uint16_t, f.r.v[0]);
+            asm("" : "+v"(word));
+            f.r.v[0] = __builtin_bit_cast(T, (uint16_t)word);
+        }
+        return f;
+    }
+    __device__ __forceinline__ void set(const float (&v)[W]) {
+#pragma unroll
+        for (int w = 0; w < W; ++w) r.v[w] = (T)v[w];
+    }
+};
+template <class T>
+struct Pair {
+    typedef T two __attribute__((ext_vector_type(2)));
+    typedef uint32_t loose __attribute__((aligned(2), may_alias));
+    uint32_t word;
+    __device__ __forceinline__ void load(const T* at) { word = *(const loose*)at; }
+    __device__ __forceinline__ void store(T* at) const { *(loose*)at = word; }
+    __device__ __forceinline__ float get(int w) const {
+        if constexpr (std::is_same<T, __bf16>::value) return __uint_as_float(w ? word & 0xFFFF0000u : word << 16);
+        else return (float)__builtin_bit_cast(two, word)[w];
+    }
+    __device__ __forceinline__ Pair again() const {
+        Pair f = *this;
+        asm("" : "+v"(f.word));
+        return f;
+    }
+    __device__ __forceinline__ void set(const float (&v)[2]) { word = __builtin_bit_cast(uint32_t, (two){(T)v[0], (T)v[1]}); }
+};
+template <> struct Few<__bf16, 2> : Pair<__bf16> {};
+template <> struct Few<_Float16, 2> : Pair<_Float16> {};
 
 // Where a share of rows begins.  q >= 0: within sequence q, which has rows prev to next - 1; else where a sequence begins, or in no
 // sequence at all.
@@ -166,17 +200,17 @@ __device__ __forceinline__ void next(T*& at, int64_t ld) {
 
 template <class T, int W>
 struct Rows {
-    Run<T, W> v[kRows];
+    Few<T, W> v[kRows];
     // Those of a chunk; rows from n on are not read.
     __device__ __forceinline__ void load(const void* base, int64_t ld, int64_t row, int64_t n, int col) {
         const T* at = (const T*)base + row * ld + col;
         if (row + kRows <= n) {
 #pragma unroll
-            for (int i = 0; i < kRows; ++i) v[i] = load_few<W>(at), next(at, ld);
+            for (int i = 0; i < kRows; ++i) v[i].load(at), next(at, ld);
         } else {
 #pragma unroll
             for (int i = 0; i < kRows; ++i) {
-                if (row + i < n) v[i] = load_few<W>(at);
+                if (row + i < n) v[i].load(at);
                 next(at, ld);
             }
         }
@@ -245,8 +279,8 @@ __global__ __launch_bounds__(kThreads) void k_scan_first(Scan a) {
             for (int i = 0; i < kRows; ++i)
 #pragma unroll
                 for (int w = 0; w < W; ++w) {
-                    const Terms m = terms_of<SIGMOID && !GRAD>((float)x.v[i].v[w], (float)gate.v[i].v[w]);
-                    d[i][w] = GRAD && SIGMOID ? sigmoid_of((float)gate.v[i].v[w]).a : m.a, u[i][w] = m.u;
+                    const Terms m = terms_of<SIGMOID && !GRAD>(x.v[i].get(w), gate.v[i].get(w));
+                    d[i][w] = GRAD && SIGMOID ? sigmoid_of(gate.v[i].get(w)).a : m.a, u[i][w] = m.u;
                 }
             if (in != kAll) {
 #pragma unroll
@@ -407,7 +441,7 @@ __global__ __launch_bounds__(kThreads) void k_scan(Scan a) {
         for (int i = 0; i < kRows; ++i)
 #pragma unroll
             for (int w = 0; w < W; ++w) {
-                const Terms m = terms_of<SIGMOID>((float)x.v[i].v[w], (float)gate.v[i].v[w]);
+                const Terms m = terms_of<SIGMOID>(x.v[i].get(w), gate.v[i].get(w));
                 d[i][w] = m.a, u[i][w] = m.u;
             }
         load(step + 1);
@@ -435,19 +469,19 @@ __global__ __launch_bounds__(kThreads) void k_scan(Scan a) {
         }
         join<W>(a, e, at, (int)step, A, H, firsts != 0, carry, h);
         if (a.keep && (mine & 1)) {
-            Run<float, W> r;
-#pragma unroll
-            for (int w = 0; w < W; ++w) r.v[w] = h[w];
-            store_few<W>(a.keep + c * a.d + at.col, r);
+            Few<float, W> r;
+            r.set(h);
+            r.store(a.keep + c * a.d + at.col);
         }
         T* y = (T*)a.y + row * a.ldy + at.col;
         if (plain) {
 #pragma unroll
             for (int i = 0; i < kRows; ++i) {
-                Run<T, W> r;
 #pragma unroll
-                for (int w = 0; w < W; ++w) h[w] = fmaf(d[i][w], h[w], u[i][w]), r.v[w] = (T)h[w];
-                store_few<W>(y, r);
+                for (int w = 0; w < W; ++w) h[w] = fmaf(d[i][w], h[w], u[i][w]);
+                Few<T, W> r;
+                r.set(h);
+                r.store(y);
                 next(y, a.ldy);
             }
         } else {
@@ -455,13 +489,15 @@ __global__ __launch_bounds__(kThreads) void k_scan(Scan a) {
             for (int i = 0; i < kRows; ++i) {
                 const bool inside = in >> i & 1, first = firsts >> i & 1;
                 if (first && inside) q = a.of_row[row + i];
-                Run<T, W> r;
+                float out[W];
 #pragma unroll
                 for (int w = 0; w < W; ++w) {
                     h[w] = first ? u[i][w] : fmaf(d[i][w], h[w], u[i][w]);
-                    r.v[w] = inside ? (T)h[w] : (T)0.f;
+                    out[w] = inside ? h[w] : 0.f;
                 }
-                if (mine >> i & 1) store_few<W>(y, r);
+                Few<T, W> r;
+                r.set(out);
+                if (mine >> i & 1) r.store(y);
                 next(y, a.ldy);
                 if (float* const to = lasts >> i & 1 ? states_of(a, a.last, q, at.col) : nullptr)
 #pragma unroll
@@ -481,13 +517,13 @@ __global__ __launch_bounds__(kThreads) void k_scan_grad(Scan a) {
     const int64_t lo = a.s ? max(start_of(a, 0), begin) : end, hi = a.s ? min(start_of(a, a.s), end) : end;
     const int64_t c0 = begin / kRows, c1 = (end + kRows - 1) / kRows, steps = (c1 - c0 + a.groups - 1) / a.groups;
     Rows<T, W> x, gate, dy;
-    Run<float, W> h0;
+    Few<float, W> h0;
     Chunk k;
     const auto load = [&](int64_t step) {
         const int64_t c = c1 - 1 - step * a.groups - at.group;
         if (!at.works || c < c0) return;
         k = a.chunk[c];
-        h0 = load_few<W>(a.kept + c * a.d + at.col);
+        h0.load(a.kept + c * a.d + at.col);
         x.load(a.x, a.ldx, c * kRows, a.n, at.col);
         gate.load(a.gate, a.ldg, c * kRows, a.n, at.col);
         dy.load(a.y, a.ldy, c * kRows, a.n, at.col);
@@ -502,32 +538,35 @@ __global__ __launch_bounds__(kThreads) void k_scan_grad(Scan a) {
         const uint32_t firsts = here ? k.begins & in : 0u, lasts = here ? k.begins >> 1 & in : 0u;
         const bool plain = in == kAll && !(firsts | lasts);
         const int64_t q0 = k.q;
-        // a and 1 - a, what l is multiplied by for dgate, and dy.
-        float d[kRows][W], rest[kRows][W], f[kRows][W], g[kRows][W];
-        float h[W];
-#pragma unroll
-        for (int w = 0; w < W; ++w) h[w] = h0.v[w];
-#pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            const float* from = nullptr;
-            const bool first = !plain && (firsts >> i & 1);
-            if (first && a.initial) from = states_of(a, a.initial, a.of_row[row + i], at.col);
-#pragma unroll
-            for (int w = 0; w < W; ++w) {
-                const float v = (float)x.v[i].v[w];
-                const Terms m = terms_of<SIGMOID>(v, (float)gate.v[i].v[w]);
-                d[i][w] = m.a, rest[i][w] = m.rest, g[i][w] = (float)dy.v[i].v[w];
-                if (first) h[w] = from ? from[w] : 0.f;
-                f[i][w] = SIGMOID ? (h[w] - v) * (m.a * m.rest) : h[w];
-                const bool inside = plain || (in >> i & 1);
-                h[w] = inside ? fmaf(m.a, h[w], m.u) : h[w];
-                if (!inside) d[i][w] = 1.f, g[i][w] = 0.f;
+        // Kept in registers from the pass down the rows for the two up: what l is multiplied by for dgate, dy as it is, and the gate: as it
+        // is, or the lesser of a and 1 - a, negative where that is 1 - a (the other one is 1 less its absolute value to half a step).
+        float f[kRows][W], lesser[kRows][W];
+        const Rows<T, W> g = dy, given = gate;
+        const auto a_of = [&](int i, int w, const auto& gate) {
+            if (!SIGMOID) return gate.get(w);
+            const float v = lesser[i][w];
+            return __float_as_uint(v) >> 31 ? 1.f + v : v;
+        };
+        const auto rest_of = [&](int i, int w) {
+            const float v = lesser[i][w];
+            return __float_as_uint(v) >> 31 ? -v : 1.f - v;
+        };
+        // One row down: its f, and the state behind it.
+        const auto down = [&](int i, int w, const auto& x, const auto& gate, float& h) {
+            const float v = x.get(w), z = gate.get(w);
+            if constexpr (SIGMOID) {
+                const Gate m = sigmoid_of(z);
+                lesser[i][w] = z >= 0.f ? -m.rest : m.a;
+                f[i][w] = (h - v) * (m.a * m.rest);
+                h = fmaf(m.a, h, m.rest * v);
+            } else {
+                f[i][w] = h;
+                h = fmaf(z, h, v);
             }
-        }
-        load(step + 1);
-        float A[W], H[W], m[W];
+        };
+        float h[W], A[W], H[W], m[W];
 #pragma unroll
-        for (int w = 0; w < W; ++w) A[w] = 1.f, H[w] = 0.f;
+        for (int w = 0; w < W; ++w) h[w] = h0.get(w), A[w] = 1.f, H[w] = 0.f;
         // The sequence of a row with a last one in its chunk.
         const auto sequence_at = [&](int i) {
             const uint32_t before = firsts & ((2u << i) - 1);
@@ -535,59 +574,105 @@ __global__ __launch_bounds__(kThreads) void k_scan_grad(Scan a) {
         };
         if (plain) {
 #pragma unroll
+            for (int i = 0; i < kRows; ++i) {
+#pragma unroll
+                for (int w = 0; w < W; ++w) down(i, w, x.v[i], gate.v[i], h[w]);
+                if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) {
+                if (firsts >> i & 1) {
+                    const float* from = a.initial ? states_of(a, a.initial, a.of_row[row + i], at.col) : nullptr;
+#pragma unroll
+                    for (int w = 0; w < W; ++w) h[w] = from ? from[w] : 0.f;
+                }
+                const auto xi = x.v[i].again(), zi = gate.v[i].again();
+#pragma unroll
+                for (int w = 0; w < W; ++w) {
+                    float to = h[w];
+                    down(i, w, xi, zi, to);
+                    h[w] = in >> i & 1 ? to : h[w];
+                }
+            }
+        }
+        // (Unknown to the compiler again: it would keep both factors of every value from one pass to the next.)
+        const auto forget = [&] {
+            if constexpr (SIGMOID)
+#pragma unroll
+                for (int i = 0; i < kRows; ++i)
+#pragma unroll
+                    for (int w = 0; w < W; ++w) asm("" : "+v"(lesser[i][w]));
+        };
+        forget();
+        load(step + 1);
+        if (plain) {
+#pragma unroll
             for (int i = kRows - 1; i >= 0; --i)
 #pragma unroll
-                for (int w = 0; w < W; ++w) A[w] *= d[i][w], H[w] = d[i][w] * (g[i][w] + H[w]);
+                for (int w = 0; w < W; ++w) {
+                    const float d = a_of(i, w, given.v[i]);
+                    A[w] *= d, H[w] = d * (g.v[i].get(w) + H[w]);
+                    if (i % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+                }
         } else {
 #pragma unroll
             for (int i = kRows - 1; i >= 0; --i) {
-                const bool inside = in >> i & 1;
                 if (lasts >> i & 1) {
                     const float* from = states_of(a, a.dlast, sequence_at(i), at.col);
 #pragma unroll
                     for (int w = 0; w < W; ++w) H[w] = from ? from[w] : 0.f;
                 }
+                const auto gi = g.v[i].again(), zi = given.v[i].again();
 #pragma unroll
-                for (int w = 0; w < W; ++w) A[w] *= d[i][w], H[w] = inside ? d[i][w] * (g[i][w] + H[w]) : H[w];
+                for (int w = 0; w < W; ++w) {
+                    const float d = a_of(i, w, zi);
+                    if (in >> i & 1) A[w] *= d, H[w] = d * (gi.get(w) + H[w]);
+                }
             }
         }
+        forget();
         join<W>(a, e, at, (int)step, A, H, lasts != 0, carry, m);
         T* dx = (T*)a.dx + (row + kRows - 1) * a.lddx + at.col;
         T* dg = (T*)a.dgate + (row + kRows - 1) * a.lddg + at.col;
+        // One row up: its gradients, and what goes on to the row before it.
+        const auto up = [&](int i, int w, const auto& g, const auto& gate, float& m, float& to_x, float& to_gate) {
+            const float l = g.get(w) + m;
+            to_x = SIGMOID ? rest_of(i, w) * l : l, to_gate = l * f[i][w];
+            m = a_of(i, w, gate) * l;
+        };
         if (plain) {
 #pragma unroll
             for (int i = kRows - 1; i >= 0; --i) {
-                Run<T, W> r, t;
+                float to_x[W], to_gate[W];
 #pragma unroll
-                for (int w = 0; w < W; ++w) {
-                    const float l = g[i][w] + m[w];
-                    r.v[w] = (T)(SIGMOID ? rest[i][w] * l : l), t.v[w] = (T)(l * f[i][w]);
-                    m[w] = d[i][w] * l;
-                }
-                store_few<W>(dx, r);
-                store_few<W>(dg, t);
+                for (int w = 0; w < W; ++w) up(i, w, g.v[i], given.v[i], m[w], to_x[w], to_gate[w]);
+                Few<T, W> r, t;
+                r.set(to_x), t.set(to_gate);
+                r.store(dx), t.store(dg);
                 next(dx, -a.lddx), next(dg, -a.lddg);
+                if (i % 4 == 0) __builtin_amdgcn_sched_barrier(0);
             }
         } else {
 #pragma unroll
             for (int i = kRows - 1; i >= 0; --i) {
-                const bool inside = in >> i & 1;
                 if (lasts >> i & 1) {
                     const float* from = states_of(a, a.dlast, sequence_at(i), at.col);
 #pragma unroll
                     for (int w = 0; w < W; ++w) m[w] = from ? from[w] : 0.f;
                 }
-                Run<T, W> r, t;
+                float to_x[W], to_gate[W];
+                const auto gi = g.v[i].again(), zi = given.v[i].again();
 #pragma unroll
                 for (int w = 0; w < W; ++w) {
-                    const float l = g[i][w] + m[w];
-                    r.v[w] = inside ? (T)(SIGMOID ? rest[i][w] * l : l) : (T)0.f, t.v[w] = inside ? (T)(l * f[i][w]) : (T)0.f;
-                    m[w] = inside ? d[i][w] * l : m[w];
+                    float to = m[w];
+                    up(i, w, gi, zi, to, to_x[w], to_gate[w]);
+                    if (in >> i & 1) m[w] = to;
+                    else to_x[w] = to_gate[w] = 0.f;
                 }
-                if (mine >> i & 1) {
-                    store_few<W>(dx, r);
-                    store_few<W>(dg, t);
-                }
+                Few<T, W> r, t;
+                r.set(to_x), t.set(to_gate);
+                if (mine >> i & 1) r.store(dx), t.store(dg);
                 next(dx, -a.lddx), next(dg, -a.lddg);
                 if (float* const to = (firsts >> i & 1) && a.dinitial ? states_of(a, a.dinitial, a.of_row[row + i], at.col) : nullptr)
 #pragma unroll
