@@ -109,8 +109,8 @@ int ccdpp_gated_scan_step(int64_t n, int32_t d, int32_t dtype, int32_t mode, con
  *   done   : one byte per beam, or NULL for zeros.  A beam with one other than 0 is at its end:
  *            its logits are not read, and it goes on as itself, with the item `end` and its score
  *   end    : the item that ends a beam, or -1
- * NaN counts as the greatest; all continuations of a beam with a NaN, or with +inf, among its z have
- * the score NaN.
+ * Among z, NaN counts as +inf; all continuations of a beam that has one of them have the score NaN, and
+ * NaN counts as the greatest score.
  */
 typedef struct ccdpp_beam {
     int64_t groups, v;

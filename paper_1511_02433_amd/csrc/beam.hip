@@ -2,6 +2,7 @@
 //
 // Beam b continued by item i has the score  s_b + z_bi - L_b,  L_b = log sum_j exp z_bj.  Within a beam the order is that of z, which is
 // exact in 32 bits: a row leaves its k greatest keys (z, then the lowest item).  Between beams scores are compared in 64 bits.
+#include <algorithm>
 #include <cmath>
 
 #include "ccdpp_seq.h"
@@ -10,124 +11,276 @@
 namespace ccdops {
 namespace {
 
-constexpr int kMost = 64;  // beams of a group, and continuations
+constexpr int kMost = 64;             // beams of a group, and continuations
+constexpr int64_t kGrid = 1 << 20;    // blocks of a launch
 
-// Descending order as a whole number: NaN first, -0 as 0.  The key of -inf is kNone.
-constexpr uint32_t kNone = 0x007FFFFFu;
+constexpr int kEach = 32;             // logits of a lane in a chunk
+constexpr int kChunk = 64 * kEach;    // of a wave
+constexpr int kWaves = 4;             // of a block
+constexpr float kLog2e = 1.44269504f;
+
+// Ascending order of values as whole numbers: NaN last.
 __device__ __forceinline__ uint32_t order_of(float z) {
-    if (z != z) return 0xFFFFFFFFu;
-    const uint32_t u = __float_as_uint(z + 0.f);
+    const uint32_t u = __float_as_uint(z);
     return u >> 31 ? ~u : u | 0x80000000u;
 }
-__device__ __forceinline__ float value_of(uint32_t o) {
-    if (o == 0xFFFFFFFFu) return NAN;
-    return __uint_as_float(o >> 31 ? o & 0x7FFFFFFFu : ~o);
-}
+__device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float(o >> 31 ? o & 0x7FFFFFFFu : ~o); }
 __device__ __forceinline__ uint64_t order_of(double z) {
     if (z != z) return ~0ull;
     const uint64_t u = (uint64_t)__double_as_longlong(z + 0.0);
     return u >> 63 ? ~u : u | 1ull << 63;
 }
 
+// The greatest value of a wave, for all its lanes: lanes of a row of 16 from each other, then the rows' last ones.
+template <int CTRL, int ROWS, class V>
+__device__ __forceinline__ V from_lane(V v) {
+    const int x = __builtin_bit_cast(int, v);
+    return __builtin_bit_cast(V, __builtin_amdgcn_update_dpp(x, x, CTRL, ROWS, 0xF, false));
+}
+template <class V>
+__device__ __forceinline__ V greater(V a, V b) { return a > b ? a : b; }
+__device__ __forceinline__ float greater(float a, float b) { return fmaxf(a, b); }
+template <class V>
+__device__ __forceinline__ V wave_max(V v) {
+    v = greater(v, from_lane<0x111, 0xF>(v));
+    v = greater(v, from_lane<0x112, 0xF>(v));
+    v = greater(v, from_lane<0x114, 0xF>(v));
+    v = greater(v, from_lane<0x118, 0xF>(v));
+    v = greater(v, from_lane<0x142, 0xA>(v));
+    v = greater(v, from_lane<0x143, 0xC>(v));
+    return __builtin_bit_cast(V, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+}
+__device__ __forceinline__ uint64_t wave_max(uint64_t v) {
+    const uint32_t hi = wave_max((uint32_t)(v >> 32)), lo = wave_max((uint32_t)(v >> 32) == hi ? (uint32_t)v : 0u);
+    return (uint64_t)hi << 32 | lo;
+}
+template <class V>
+__device__ __forceinline__ V lane_of(V v, int lane) { return __builtin_bit_cast(V, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane)); }
+__device__ __forceinline__ uint64_t lane_of(uint64_t v, int lane) { return (uint64_t)lane_of((uint32_t)(v >> 32), lane) << 32 | lane_of((uint32_t)v, lane); }
+
+// The greatest keys of a wave in descending order, one a lane; 0: none.  A key is a value's order and then the lowest item, so no two are equal.
+struct Best {
+    uint64_t key;
+    __device__ __forceinline__ void insert(uint64_t k) {
+        const int at = __popcll(__ballot(key > k)), lane = threadIdx.x & 63;
+        const uint32_t hi = from_lane<0x138, 0xF>((uint32_t)(key >> 32)), lo = from_lane<0x138, 0xF>((uint32_t)key);  // of the lane before
+        key = lane < at ? key : lane == at ? k : (uint64_t)hi << 32 | lo;
+    }
+};
+
 struct Beam {
     int64_t groups, v, ld, end;
-    int beams, k;
+    int beams, k, shares;
+    int64_t each;      // chunks of a share of a row
     const void* logits;
     const float *score, *offset;
     const uint8_t* done;
     float* out_score;
     int64_t *parent, *item;
     uint8_t* out_done;
-    double* sums;     // L of each row
-    uint64_t* keys;   // k of each row, descending; 0: none
+    double* sums;      // of exponentials over a share, relative to
+    float* tops;       // its greatest logit
+    uint64_t* keys;    // k of each share, descending; 0: none
 };
 
-template <class T>
-__device__ __forceinline__ float logit(const Beam& a, int64_t row, int64_t i) {
-    const float z = (float)((const T*)a.logits)[row * a.ld + i];
-    if (!a.offset) return z;
-    const float o = a.offset[i];
-    return o < -1e38f ? -INFINITY : z + o;
-}
-
-template <class V, class F>
-__device__ __forceinline__ V block_join(V v, V* red, F&& f) {
-    for (int k = 32; k > 0; k >>= 1) v = f(v, __shfl_xor(v, k));
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = red[0];
-    for (int w = 1; w < (int)blockDim.x / 64; ++w) v = f(v, red[w]);
-    return v;
-}
-
-// One block a row, which it reads k + 2 times.
-template <class T>
-__global__ __launch_bounds__(256) void k_beam_rows(Beam a) {
-    __shared__ uint64_t red[4];
-    const int64_t row = blockIdx.x;
-    const float s = a.score[row];
-    if (s == -INFINITY || (a.done && a.done[row])) return;
-    uint32_t top = 0;
-    for (int64_t i = threadIdx.x; i < a.v; i += 256) top = max(top, order_of(logit<T>(a, row, i)));
-    top = (uint32_t)block_join((uint64_t)top, red, [](uint64_t p, uint64_t q) { return p > q ? p : q; });
-    const float m = value_of(top);
-    double sum = 0.0;
-    for (int64_t i = threadIdx.x; i < a.v; i += 256) {
-        const float z = logit<T>(a, row, i);
-        sum += z == -INFINITY ? 0.0 : exp((double)z - m);
+// A chunk's logits as they are in memory, and their offsets: lane l has V side by side at l V, and again every 64 V.
+template <class T, bool OFFSET>
+struct Chunk {
+    static constexpr int V = 16 / sizeof(T), J = kEach / V;
+    Run<T, V> raw[J];
+    Run<float, 4> off[OFFSET ? kEach / 4 : 1];
+    __device__ __forceinline__ void load(const T* row, const float* offset, int64_t first, int64_t v) {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const int64_t i = first + j * 64 * V + lane * V;
+            if (first + kChunk <= v || i + V <= v) {
+                raw[j] = load_run<V>(row + i);
+                if constexpr (OFFSET)
+#pragma unroll
+                    for (int q = 0; q < V / 4; ++q) off[j * V / 4 + q] = load_run<4>(offset + i + 4 * q);
+            } else {
+#pragma unroll
+                for (int w = 0; w < V; ++w) {
+                    raw[j].v[w] = i + w < v ? row[i + w] : (T)-INFINITY;
+                    if constexpr (OFFSET) off[(j * V + w) / 4].v[w % 4] = i + w < v ? offset[i + w] : 0.f;
+                }
+            }
+        }
     }
-    sum = block_join(sum, (double*)red, [](double p, double q) { return p + q; });
-    if (threadIdx.x == 0) a.sums[row] = top == kNone ? -INFINITY : m + log(sum);
-    uint64_t last = ~0ull;
-    for (int j = 0; j < a.k; ++j) {
-        uint64_t best = 0;
-        for (int64_t i = threadIdx.x; i < a.v; i += 256) {
-            const uint32_t o = order_of(logit<T>(a, row, i));
-            const uint64_t key = (uint64_t)o << 32 | (uint32_t)~(uint32_t)i;
-            if (o != kNone && key < last && key > best) best = key;
+    // The logit with its offset; -inf where it takes no part, +inf for NaN.
+    __device__ __forceinline__ float get(int e) const {
+        float z = (float)raw[e / V].v[e % V];
+        if constexpr (OFFSET) {
+            const float o = off[e / 4].v[e % 4];
+            z = o < -1e38f ? -INFINITY : z + o;
         }
-        last = block_join(best, red, [](uint64_t p, uint64_t q) { return p > q ? p : q; });
-        if (threadIdx.x == 0) a.keys[row * a.k + j] = last;
+        return z != z ? INFINITY : z + 0.f;
+    }
+};
+
+// One block for each share of a row.  Its waves take chunks in turn; a chunk is read once: its exponentials are added up relative to the
+// lane's greatest logit so far (in 32 bits within a chunk, in 64 over them), then what is greater than the wave's k-th best so far is taken
+// out, the greatest first, at most k times.  With values in any order that is some k (1 + log(chunks)) times in all.
+template <class T, bool OFFSET>
+__global__ __launch_bounds__(64 * kWaves) void k_beam_rows(Beam a) {
+    typedef Chunk<T, OFFSET> C;
+    __shared__ uint64_t lists[kWaves][kMost];
+    __shared__ double sums[kWaves];
+    __shared__ float tops[kWaves];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t items = a.groups * a.beams * a.shares;
+    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const int64_t row = item / a.shares;
+        if (a.score[row] == -INFINITY || (a.done && a.done[row])) continue;
+        const int64_t begin = (item - row * a.shares) * a.each, end = min(begin + a.each, (a.v + kChunk - 1) / kChunk);
+        const T* const base = (const T*)a.logits + row * a.ld;
+        Best best = {0};
+        float top = -INFINITY, least = -INFINITY;  // of the lane; the k-th best of the wave
+        double sum = 0.0;
+        C next;
+        if (begin + wave < end) next.load(base, a.offset, (begin + wave) * kChunk, a.v);
+        for (int64_t c = begin + wave; c < end; c += kWaves) {
+            float z[kEach];
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) z[e] = next.get(e);
+            if (c + kWaves < end) next.load(base, a.offset, (c + kWaves) * kChunk, a.v);
+            const auto greatest = [&] {
+                float m = z[0];
+#pragma unroll
+                for (int e = 1; e < kEach; ++e) m = fmaxf(m, z[e]);
+                return m;
+            };
+            float m = greatest();
+            const float was = top;
+            top = fmaxf(top, m);
+            const float ref = top == -INFINITY ? 0.f : top;
+            float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) part[e & 3] += __builtin_amdgcn_exp2f((z[e] - ref) * kLog2e);
+            sum = sum * (was == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((was - ref) * kLog2e)) + (double)((part[0] + part[1]) + (part[2] + part[3]));
+            while (__ballot(m > least)) {
+                const float most = wave_max(m);
+                // The lowest item that has it, and out with it.
+                int at = 0;
+                bool found = false;
+#pragma unroll
+                for (int j = 0; j < C::J; ++j) {
+                    if (found) continue;
+                    uint64_t any = 0;
+#pragma unroll
+                    for (int w = 0; w < C::V; ++w) any |= __ballot(z[j * C::V + w] == most);
+                    if (any) {
+                        found = true;
+                        const int owner = __ffsll((unsigned long long)any) - 1;
+                        int which = 0;
+#pragma unroll
+                        for (int w = C::V - 1; w >= 0; --w)
+                            if (__ballot(z[j * C::V + w] == most) >> owner & 1) which = w;
+#pragma unroll
+                        for (int w = 0; w < C::V; ++w) z[j * C::V + w] = lane == owner && w == which ? -INFINITY : z[j * C::V + w];
+                        at = j * 64 * C::V + owner * C::V + which;
+                    }
+                }
+                m = greatest();
+                best.insert((uint64_t)order_of(most) << 32 | (uint32_t)~(uint32_t)(c * kChunk + at));
+                const uint64_t last = lane_of(best.key, a.k - 1);
+                least = last ? value_of((uint32_t)(last >> 32)) : -INFINITY;
+            }
+        }
+        const float all = wave_max(top);
+        if (top != all) sum *= top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((top - all) * kLog2e);
+        for (int k = 32; k > 0; k >>= 1) sum += __shfl_xor(sum, k);
+        __syncthreads();
+        lists[wave][lane] = best.key;
+        if (lane == 0) sums[wave] = sum, tops[wave] = all;
+        __syncthreads();
+        if (wave == 0) {
+            for (int w = 1; w < kWaves; ++w)
+                for (int j = 0; j < a.k; ++j) {
+                    const uint64_t k = lists[w][j];
+                    if (k <= lane_of(best.key, a.k - 1)) break;
+                    best.insert(k);
+                }
+            if (lane < a.k) a.keys[item * a.k + lane] = best.key;
+            if (lane == 0) {
+                float t = tops[0];
+                for (int w = 1; w < kWaves; ++w) t = fmaxf(t, tops[w]);
+                double s = 0.0;
+                for (int w = 0; w < kWaves; ++w)
+                    if (tops[w] != -INFINITY) s += sums[w] * (double)__builtin_amdgcn_exp2f((tops[w] - t) * kLog2e);
+                a.sums[item] = s, a.tops[item] = t;
+            }
+        }
     }
 }
 
-// One wave a group: lane b goes down the list of beam b.
-__global__ __launch_bounds__(64) void k_beam_join(Beam a) {
-    const int64_t g = blockIdx.x;
-    const int b = threadIdx.x;
-    const int64_t row = g * a.beams + b;
-    float s = -INFINITY;
-    bool done = false;
-    if (b < a.beams) s = a.score[row], done = a.done && a.done[row];
-    const bool live = s != -INFINITY;
-    const double sum = live && !done ? a.sums[row] : 0.0;
-    int at = 0;
-    for (int j = 0; j < a.k; ++j) {
-        double value = -INFINITY;
-        int64_t item = -1;
-        if (live && done && at == 0) value = s, item = a.end;
-        if (live && !done && at < a.k) {
-            const uint64_t key = a.keys[row * a.k + at];
-            if (key) value = s + ((double)value_of((uint32_t)(key >> 32)) - sum), item = (uint32_t)~(uint32_t)key;
+// One block a group: a wave joins the shares of a row, then the first wave goes down the beams' lists, lane b that of beam b.
+__global__ __launch_bounds__(1024) void k_beam_join(Beam a) {
+    __shared__ uint64_t lists[kMost][kMost];
+    __shared__ double logs[kMost];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+    for (int64_t g = blockIdx.x; g < a.groups; g += gridDim.x) {
+        for (int b = wave; b < a.beams; b += waves) {
+            const int64_t row = g * a.beams + b;
+            if (a.score[row] == -INFINITY || (a.done && a.done[row])) continue;
+            const int64_t first = row * a.shares;
+            Best best = {lane < a.k ? a.keys[first * a.k + lane] : 0};
+            constexpr int kAtOnce = 8;  // lists that are read together
+            for (int s = 1; s < a.shares; s += kAtOnce) {
+                uint64_t other[kAtOnce];
+#pragma unroll
+                for (int u = 0; u < kAtOnce; ++u) other[u] = lane < a.k && s + u < a.shares ? a.keys[(first + s + u) * a.k + lane] : 0;
+#pragma unroll
+                for (int u = 0; u < kAtOnce; ++u)
+                    for (int j = 0; j < a.k; ++j) {
+                        const uint64_t k = lane_of(other[u], j);
+                        if (k <= lane_of(best.key, a.k - 1)) break;
+                        best.insert(k);
+                    }
+            }
+            float top = -INFINITY;
+            for (int s = lane; s < a.shares; s += 64) top = fmaxf(top, a.tops[first + s]);
+            top = wave_max(top);
+            double sum = 0.0;
+            for (int s = lane; s < a.shares; s += 64)
+                if (a.tops[first + s] != -INFINITY) sum += a.sums[first + s] * exp((double)a.tops[first + s] - top);
+            for (int k = 32; k > 0; k >>= 1) sum += __shfl_xor(sum, k);
+            if (lane < a.k) lists[b][lane] = best.key;
+            if (lane == 0) logs[b] = top == INFINITY ? (double)NAN : top + log(sum);
         }
-        const uint64_t mine = order_of(value);
-        uint64_t best = mine;
-        for (int k = 32; k > 0; k >>= 1) {
-            const uint64_t o = __shfl_xor(best, k);
-            best = o > best ? o : best;
+        __syncthreads();
+        if (wave == 0) {
+            const int b = lane;
+            const int64_t row = g * a.beams + b;
+            float s = -INFINITY;
+            bool done = false;
+            if (b < a.beams) s = a.score[row], done = a.done && a.done[row];
+            const bool live = s != -INFINITY;
+            const double sum = live && !done ? logs[b] : 0.0;
+            int at = 0;
+            for (int j = 0; j < a.k; ++j) {
+                double value = -INFINITY;
+                int64_t item = -1;
+                if (live && done && at == 0) value = s, item = a.end;
+                if (live && !done && at < a.k) {
+                    const uint64_t key = lists[b][at];
+                    if (key) value = s + ((double)value_of((uint32_t)(key >> 32)) - sum), item = (uint32_t)~(uint32_t)key;
+                }
+                const uint64_t mine = order_of(value), most = wave_max(mine);
+                const bool none = most == order_of((double)-INFINITY);
+                const int winner = __ffsll((unsigned long long)__ballot(mine == most)) - 1;
+                if (b == winner) {
+                    const int64_t out = g * a.k + j;
+                    a.out_score[out] = none ? -INFINITY : (float)value;
+                    a.parent[out] = none ? -1 : b;
+                    a.item[out] = none ? -1 : item;
+                    if (a.out_done) a.out_done[out] = none || item == a.end;
+                    ++at;
+                }
+            }
         }
-        const bool none = best == order_of((double)-INFINITY);
-        const uint64_t who = __ballot(mine == best);
-        const int winner = __ffsll((unsigned long long)who) - 1;
-        if (b == winner) {
-            const int64_t out = g * a.k + j;
-            a.out_score[out] = none ? -INFINITY : (float)value;
-            a.parent[out] = none ? -1 : b;
-            a.item[out] = none ? -1 : item;
-            if (a.out_done) a.out_done[out] = none || item == a.end;
-            ++at;
-        }
+        __syncthreads();
     }
 }
 
@@ -138,16 +291,19 @@ struct Moves {
     char* out[kTable];
     int64_t stride[kTable], bytes[kTable];
     const int64_t* parent;
+    int64_t rows;  // groups * k
     int beams, k, n;
 };
 
 __global__ __launch_bounds__(256) void k_reorder(Moves m) {
-    const int64_t at = blockIdx.x, g = at / m.k, parent = m.parent[at];
-    const bool there = parent >= 0 && parent < m.beams;
-    for (int t = 0; t < m.n; ++t) {
-        const char* from = m.in[t] + (g * m.beams + (there ? parent : 0)) * m.stride[t];
-        char* to = m.out[t] + at * m.bytes[t];
-        for (int64_t i = threadIdx.x; i < m.bytes[t]; i += 256) to[i] = there ? from[i] : (char)0;
+    for (int64_t at = blockIdx.x; at < m.rows; at += gridDim.x) {
+        const int64_t g = at / m.k, parent = m.parent[at];
+        const bool there = parent >= 0 && parent < m.beams;
+        for (int t = 0; t < m.n; ++t) {
+            const char* from = m.in[t] + (g * m.beams + (there ? parent : 0)) * m.stride[t];
+            char* to = m.out[t] + at * m.bytes[t];
+            for (int64_t i = threadIdx.x; i < m.bytes[t]; i += 256) to[i] = there ? from[i] : (char)0;
+        }
     }
 }
 
@@ -164,7 +320,25 @@ int check(const ccdpp_beam_t* p) {
     return CCDPP_OK;
 }
 
-int64_t workspace(const ccdpp_beam_t* p) { return round_up(p->groups * p->beams * 8 * (1 + (int64_t)p->k), 256) + 256; }
+// How a row is shared out among blocks, and where the shares' results lie in the workspace (from 0 on).
+struct Layout {
+    int64_t shares, each, sums, tops, keys, bytes;
+};
+
+Layout layout(const ccdpp_beam_t* p) {
+    Layout l;
+    const int64_t rows = p->groups * p->beams, chunks = (p->v + kChunk - 1) / kChunk;
+    const int64_t wanted = std::max<int64_t>(1, std::min<int64_t>(2048 / std::max<int64_t>(rows, 1), 256));
+    l.each = std::max<int64_t>(round_up((chunks + wanted - 1) / wanted, kWaves), kWaves);
+    l.shares = (chunks + l.each - 1) / l.each;
+    l.sums = 0;
+    l.tops = round_up(rows * l.shares * 8, 256);
+    l.keys = l.tops + round_up(rows * l.shares * 4, 256);
+    l.bytes = l.keys + round_up(rows * l.shares * p->k * 8, 256) + 256;
+    return l;
+}
+
+int64_t workspace(const ccdpp_beam_t* p) { return layout(p).bytes; }
 
 }  // namespace
 }  // namespace ccdops
@@ -191,13 +365,23 @@ int ccdpp_beam_select(const ccdpp_beam_t* p, float* out_score, int64_t* parent, 
     if (!ws || (uintptr_t)ws % 256 || ws_bytes < workspace(p)) return fail(CCDPP_EINVAL, "the workspace is too small or not aligned to 256 bytes");
     if (int rc = check_device()) return rc;
     if (rows == 0) return CCDPP_OK;
-    Beam a = {p->groups, p->v, p->ld, p->end, p->beams, p->k, p->logits, p->score, p->offset, p->done, out_score, parent, item, out_done,
-              (double*)ws, (uint64_t*)ws + rows};
+    const Layout l = layout(p);
+    Beam a = {};
+    a.groups = p->groups, a.v = p->v, a.ld = p->ld, a.end = p->end, a.beams = p->beams, a.k = p->k, a.shares = (int)l.shares, a.each = l.each;
+    a.logits = p->logits, a.score = p->score, a.offset = p->offset, a.done = p->done;
+    a.out_score = out_score, a.parent = parent, a.item = item, a.out_done = out_done;
+    a.sums = (double*)((char*)ws + l.sums), a.tops = (float*)((char*)ws + l.tops), a.keys = (uint64_t*)((char*)ws + l.keys);
     hipStream_t st = (hipStream_t)stream;
-    if (p->dtype == CCDPP_F32) k_beam_rows<float><<<(unsigned)rows, 256, 0, st>>>(a);
-    else if (p->dtype == CCDPP_BF16) k_beam_rows<__bf16><<<(unsigned)rows, 256, 0, st>>>(a);
-    else k_beam_rows<_Float16><<<(unsigned)rows, 256, 0, st>>>(a);
-    k_beam_join<<<(unsigned)p->groups, 64, 0, st>>>(a);
+    const unsigned blocks = (unsigned)std::min<int64_t>(rows * l.shares, kGrid);
+    const auto rows_of = [&](auto z) {
+        typedef decltype(z) T;
+        if (p->offset) k_beam_rows<T, true><<<blocks, 64 * kWaves, 0, st>>>(a);
+        else k_beam_rows<T, false><<<blocks, 64 * kWaves, 0, st>>>(a);
+    };
+    if (p->dtype == CCDPP_F32) rows_of(float());
+    else if (p->dtype == CCDPP_BF16) rows_of((__bf16)0.f);
+    else rows_of((_Float16)0.f);
+    k_beam_join<<<(unsigned)std::min<int64_t>(p->groups, kGrid), 64 * std::min(p->beams, 16), 0, st>>>(a);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? CCDPP_OK : hip_fail(e, "beam selection");
 }
@@ -216,11 +400,11 @@ int ccdpp_beam_reorder(int64_t groups, int32_t beams, int32_t k, const int64_t* 
     if (int rc = check_device()) return rc;
     if (groups == 0) return CCDPP_OK;
     Moves m;
-    m.parent = parent, m.beams = beams, m.k = k, m.n = 0;
+    m.parent = parent, m.rows = groups * k, m.beams = beams, m.k = k, m.n = 0;
     for (int32_t i = 0; i < n; ++i) {
         if (row_bytes[i]) m.in[m.n] = (const char*)in[i], m.out[m.n] = (char*)out[i], m.stride[m.n] = in_stride[i], m.bytes[m.n] = row_bytes[i], ++m.n;
         if (!m.n || (m.n < kTable && i + 1 < n)) continue;
-        k_reorder<<<(unsigned)(groups * k), 256, 0, (hipStream_t)stream>>>(m);
+        k_reorder<<<(unsigned)std::min<int64_t>(m.rows, kGrid), 256, 0, (hipStream_t)stream>>>(m);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return hip_fail(e, "beam reordering");
         m.n = 0;

@@ -22,7 +22,7 @@ def seq():
 
 
 def oracle(logits, score, k, offset=None, done=None, end=None):
-    """Continuations as (score, beam, item), on the host: NaN first, then by score, beam, z, item."""
+    """Continuations as (score, beam, item), on the host: by score (NaN first), beam, z (NaN as infinity), item."""
     g, b = score.shape
     z = logits.float()
     if offset is not None:
@@ -43,9 +43,6 @@ def oracle(logits, score, k, offset=None, done=None, end=None):
             total = math.nan if bad else float(torch.logsumexp(row, 0))
             key = torch.where(torch.isnan(row), torch.tensor(math.inf, dtype=torch.float64), row)
             order = torch.sort(key, descending=True, stable=True).indices
-            if bool(torch.isnan(row).any()):  # NaN before infinity
-                nan = torch.isnan(row[order])
-                order = torch.cat([order[nan], order[~nan]])
             for r, item in enumerate(order[:k].tolist()):
                 if float(row[item]) != -math.inf:
                     found.append((s + (float(row[item]) - total), j, r, item))
