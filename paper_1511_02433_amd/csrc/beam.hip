@@ -119,15 +119,57 @@ struct Chunk {
     }
 };
 
+// What a wave has found: keys in no order, of which the k greatest count.  A value is put there if it is above `own`, the k-th greatest of
+// those there or less (later items do not go before equal ones that are there), and not below what another wave of the block knows.
+constexpr int kFound = 192, kAdded = 128;
+struct Found {
+    uint64_t* keys;
+    int n;
+    float own;
+    static __device__ __forceinline__ void agree() {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+    // Leaves the k greatest, in descending order: a key's place is the number of greater ones.
+    __device__ __forceinline__ void prune(int k) {
+        const int lane = threadIdx.x & 63;
+        agree();
+        uint64_t mine[kFound / 64];
+        int place[kFound / 64];
+#pragma unroll
+        for (int u = 0; u < kFound / 64; ++u) mine[u] = lane + 64 * u < n ? keys[lane + 64 * u] : 0, place[u] = 0;
+#pragma unroll
+        for (int v = 0; v < kFound / 64; ++v) {
+            const int last = min(n - 64 * v, 64);
+            for (int i = 0; i < last; ++i) {
+                const uint64_t other = lane_of(mine[v], i);
+#pragma unroll
+                for (int u = 0; u < kFound / 64; ++u)
+                    if (64 * u < n) place[u] += other > mine[u];
+            }
+        }
+        agree();
+#pragma unroll
+        for (int u = 0; u < kFound / 64; ++u)
+            if (lane + 64 * u < n && place[u] < k) keys[place[u]] = mine[u];
+        agree();
+        if (n >= k) own = fmaxf(own, value_of(__builtin_amdgcn_readfirstlane((uint32_t)(keys[k - 1] >> 32))));
+        n = min(n, k);
+    }
+};
+
 // One block for each share of a row.  Its waves take chunks in turn; a chunk is read once: its exponentials are added up relative to the
-// lane's greatest logit so far (in 32 bits within a chunk, in 64 over them), then what is greater than the wave's k-th best so far is taken
-// out, the greatest first, at most k times.  With values in any order that is some k (1 + log(chunks)) times in all.
+// lane's greatest logit so far (in 32 bits within a chunk, in 64 over them), then what may be among the k best is put aside.  Of a wave's
+// first chunk that is what is not below the k-th greatest of its lanes' greatest values; with values in any order little is found after that.
+// Where more than kAdded values pass (many equal or ascending ones), the k greatest of the chunk are taken out one by one.
 template <class T, bool OFFSET>
 __global__ __launch_bounds__(64 * kWaves) void k_beam_rows(Beam a) {
     typedef Chunk<T, OFFSET> C;
-    __shared__ uint64_t lists[kWaves][kMost];
+    __shared__ uint64_t keys[kWaves][kFound];
     __shared__ double sums[kWaves];
     __shared__ float tops[kWaves];
+    __shared__ int counts[kWaves];
+    __shared__ uint32_t known;  // the order of a value that k of the block's are not below
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t items = a.groups * a.beams * a.shares;
     for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
@@ -135,16 +177,20 @@ __global__ __launch_bounds__(64 * kWaves) void k_beam_rows(Beam a) {
         if (a.score[row] == -INFINITY || (a.done && a.done[row])) continue;
         const int64_t begin = (item - row * a.shares) * a.each, end = min(begin + a.each, (a.v + kChunk - 1) / kChunk);
         const T* const base = (const T*)a.logits + row * a.ld;
-        Best best = {0};
-        float top = -INFINITY, least = -INFINITY;  // of the lane; the k-th best of the wave
-        double sum = 0.0;
         C next;
         if (begin + wave < end) next.load(base, a.offset, (begin + wave) * kChunk, a.v);
+        __syncthreads();
+        if (threadIdx.x == 0) known = 0;
+        __syncthreads();
+        Found found = {keys[wave], 0, -INFINITY};
+        float top = -INFINITY;  // of the lane
+        double sum = 0.0;
         for (int64_t c = begin + wave; c < end; c += kWaves) {
             float z[kEach];
 #pragma unroll
             for (int e = 0; e < kEach; ++e) z[e] = next.get(e);
             if (c + kWaves < end) next.load(base, a.offset, (c + kWaves) * kChunk, a.v);
+            const uint32_t all_know = *(volatile uint32_t*)&known;
             const auto greatest = [&] {
                 float m = z[0];
 #pragma unroll
@@ -159,50 +205,97 @@ __global__ __launch_bounds__(64 * kWaves) void k_beam_rows(Beam a) {
 #pragma unroll
             for (int e = 0; e < kEach; ++e) part[e & 3] += __builtin_amdgcn_exp2f((z[e] - ref) * kLog2e);
             sum = sum * (was == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((was - ref) * kLog2e)) + (double)((part[0] + part[1]) + (part[2] + part[3]));
-            while (__ballot(m > least)) {
-                const float most = wave_max(m);
-                // The lowest item that has it, and out with it.
-                int at = 0;
-                bool found = false;
+            // At least `bound`: above own, and not below what others know.
+            const auto bound_of = [&] { return value_of(max(order_of(found.own) + 1, all_know)); };
+            float bound = bound_of();
+            uint64_t lanes = __ballot(m >= bound);
+            if (!lanes) continue;
+            const auto key_of = [&](float v, int at) { return (uint64_t)order_of(v) << 32 | (uint32_t)~(uint32_t)(c * kChunk + at); };
+            float raised = -INFINITY;
+            if (__popcll(lanes) > a.k) {  // the k-th greatest of the lanes' greatest
+                int above = 0;
 #pragma unroll
-                for (int j = 0; j < C::J; ++j) {
-                    if (found) continue;
-                    uint64_t any = 0;
-#pragma unroll
-                    for (int w = 0; w < C::V; ++w) any |= __ballot(z[j * C::V + w] == most);
-                    if (any) {
-                        found = true;
-                        const int owner = __ffsll((unsigned long long)any) - 1;
-                        int which = 0;
-#pragma unroll
-                        for (int w = C::V - 1; w >= 0; --w)
-                            if (__ballot(z[j * C::V + w] == most) >> owner & 1) which = w;
-#pragma unroll
-                        for (int w = 0; w < C::V; ++w) z[j * C::V + w] = lane == owner && w == which ? -INFINITY : z[j * C::V + w];
-                        at = j * 64 * C::V + owner * C::V + which;
-                    }
-                }
-                m = greatest();
-                best.insert((uint64_t)order_of(most) << 32 | (uint32_t)~(uint32_t)(c * kChunk + at));
-                const uint64_t last = lane_of(best.key, a.k - 1);
-                least = last ? value_of((uint32_t)(last >> 32)) : -INFINITY;
+                for (int l = 0; l < 64; ++l) above += lane_of(m, l) > m;
+                raised = -wave_max(above < a.k ? -m : -INFINITY);
+                bound = fmaxf(bound, raised);
             }
+            int passing = __popcll(__ballot(m >= bound)) * kEach;  // at most
+            if (passing > kAdded) {
+                passing = 0;
+#pragma unroll
+                for (int e = 0; e < kEach; ++e) passing += __popcll(__ballot(z[e] >= bound));
+            }
+            if (found.n + min(passing, kAdded) > kFound) found.prune(a.k);
+            if (passing <= kAdded) {
+                asm("" : "+v"(bound));  // (compared again: 32 masks would not stay in scalar registers)
+#pragma unroll
+                for (int e = 0; e < kEach; ++e) {
+                    const bool pass = z[e] >= bound;
+                    const uint64_t those = __ballot(pass);
+                    if (!those) continue;
+                    const int at = found.n + __builtin_amdgcn_mbcnt_hi((uint32_t)(those >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)those, 0));
+                    if (pass) found.keys[at] = key_of(z[e], (e / C::V) * 64 * C::V + lane * C::V + e % C::V);
+                    found.n += __popcll(those);
+                }
+            } else {
+                bound = bound_of();
+                raised = -INFINITY;
+                for (int i = 0; i < a.k && __ballot(m >= bound); ++i) {
+                    const float most = wave_max(m);
+                    // The lowest item that has it, and out with it.
+                    int at = 0;
+                    bool there = false;
+#pragma unroll
+                    for (int j = 0; j < C::J; ++j) {
+                        if (there) continue;
+                        uint64_t any = 0;
+#pragma unroll
+                        for (int w = 0; w < C::V; ++w) any |= __ballot(z[j * C::V + w] == most);
+                        if (any) {
+                            there = true;
+                            const int owner = __ffsll((unsigned long long)any) - 1;
+                            int which = 0;
+#pragma unroll
+                            for (int w = C::V - 1; w >= 0; --w)
+                                if (__ballot(z[j * C::V + w] == most) >> owner & 1) which = w;
+#pragma unroll
+                            for (int w = 0; w < C::V; ++w) z[j * C::V + w] = lane == owner && w == which ? -INFINITY : z[j * C::V + w];
+                            at = j * 64 * C::V + owner * C::V + which;
+                        }
+                    }
+                    m = greatest();
+                    if (lane == 0) found.keys[found.n] = key_of(most, at);
+                    ++found.n;
+                    if (i + 1 == a.k) raised = most;
+                }
+            }
+            const float before = found.own;
+            found.own = fmaxf(before, raised);
+            if (found.n >= 2 * a.k) found.prune(a.k);
+            if (found.own > before && lane == 0) atomicMax(&known, order_of(found.own));
         }
+        found.prune(a.k);
         const float all = wave_max(top);
         if (top != all) sum *= top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((top - all) * kLog2e);
         for (int k = 32; k > 0; k >>= 1) sum += __shfl_xor(sum, k);
+        if (lane == 0) sums[wave] = sum, tops[wave] = all, counts[wave] = found.n;
         __syncthreads();
-        lists[wave][lane] = best.key;
-        if (lane == 0) sums[wave] = sum, tops[wave] = all;
-        __syncthreads();
+        // Places among all waves' keys.
+        const uint64_t mine = lane < found.n ? keys[wave][lane] : 0;
+        int place = lane, total = 0;
+        uint64_t theirs[kWaves];
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) theirs[w] = keys[w][lane];
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const int n = __builtin_amdgcn_readfirstlane(counts[w]);
+            total += n;
+            if (w == wave) continue;
+            for (int i = 0; i < n; ++i) place += lane_of(theirs[w], i) > mine;
+        }
+        if (lane < found.n && place < a.k) a.keys[item * a.k + place] = mine;
         if (wave == 0) {
-            for (int w = 1; w < kWaves; ++w)
-                for (int j = 0; j < a.k; ++j) {
-                    const uint64_t k = lists[w][j];
-                    if (k <= lane_of(best.key, a.k - 1)) break;
-                    best.insert(k);
-                }
-            if (lane < a.k) a.keys[item * a.k + lane] = best.key;
+            if (lane >= total && lane < a.k) a.keys[item * a.k + lane] = 0;
             if (lane == 0) {
                 float t = tops[0];
                 for (int w = 1; w < kWaves; ++w) t = fmaxf(t, tops[w]);
@@ -225,12 +318,20 @@ __global__ __launch_bounds__(1024) void k_beam_join(Beam a) {
             const int64_t row = g * a.beams + b;
             if (a.score[row] == -INFINITY || (a.done && a.done[row])) continue;
             const int64_t first = row * a.shares;
-            Best best = {lane < a.k ? a.keys[first * a.k + lane] : 0};
-            constexpr int kAtOnce = 8;  // lists that are read together
-            for (int s = 1; s < a.shares; s += kAtOnce) {
-                uint64_t other[kAtOnce];
+            // What most rows need is asked for at once: the first lists, tops and sums.
+            constexpr int kAtOnce = 8;
+            uint64_t other[kAtOnce];
+            const auto ask = [&](int s) {
 #pragma unroll
                 for (int u = 0; u < kAtOnce; ++u) other[u] = lane < a.k && s + u < a.shares ? a.keys[(first + s + u) * a.k + lane] : 0;
+            };
+            float my_top = -INFINITY;
+            double my_sum = 0.0;
+            if (lane < a.shares) my_top = a.tops[first + lane], my_sum = a.sums[first + lane];
+            ask(0);
+            Best best = {other[0]};
+            other[0] = 0;
+            for (int s = 0;;) {
 #pragma unroll
                 for (int u = 0; u < kAtOnce; ++u)
                     for (int j = 0; j < a.k; ++j) {
@@ -238,13 +339,18 @@ __global__ __launch_bounds__(1024) void k_beam_join(Beam a) {
                         if (k <= lane_of(best.key, a.k - 1)) break;
                         best.insert(k);
                     }
+                s += kAtOnce;
+                if (s >= a.shares) break;
+                ask(s);
             }
-            float top = -INFINITY;
-            for (int s = lane; s < a.shares; s += 64) top = fmaxf(top, a.tops[first + s]);
-            top = wave_max(top);
-            double sum = 0.0;
-            for (int s = lane; s < a.shares; s += 64)
-                if (a.tops[first + s] != -INFINITY) sum += a.sums[first + s] * exp((double)a.tops[first + s] - top);
+            for (int s = lane + 64; s < a.shares; s += 64) {
+                const float t = a.tops[first + s], more = fmaxf(my_top, t);
+                if (t == -INFINITY) continue;
+                my_sum = my_sum * (my_top == -INFINITY ? 0.0 : exp((double)my_top - more)) + a.sums[first + s] * exp((double)t - more);
+                my_top = more;
+            }
+            const float top = wave_max(my_top);
+            double sum = my_top == -INFINITY ? 0.0 : my_sum * exp((double)my_top - top);
             for (int k = 32; k > 0; k >>= 1) sum += __shfl_xor(sum, k);
             if (lane < a.k) lists[b][lane] = best.key;
             if (lane == 0) logs[b] = top == INFINITY ? (double)NAN : top + log(sum);
@@ -291,18 +397,30 @@ struct Moves {
     char* out[kTable];
     int64_t stride[kTable], bytes[kTable];
     const int64_t* parent;
-    int64_t rows;  // groups * k
+    int64_t rows, pieces;  // groups * k; pieces of a row of all tensors
     int beams, k, n;
 };
 
+// Rows of out are cut into pieces of kPiece bytes, one for each block of 256 threads at a time: a run of 16 bytes for each, and the
+// bytes that a row has over one by one.
+constexpr int64_t kPiece = 4096;
 __global__ __launch_bounds__(256) void k_reorder(Moves m) {
-    for (int64_t at = blockIdx.x; at < m.rows; at += gridDim.x) {
+    const int64_t items = m.rows * m.pieces;
+    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const int64_t at = item / m.pieces;
         const int64_t g = at / m.k, parent = m.parent[at];
         const bool there = parent >= 0 && parent < m.beams;
-        for (int t = 0; t < m.n; ++t) {
-            const char* from = m.in[t] + (g * m.beams + (there ? parent : 0)) * m.stride[t];
-            char* to = m.out[t] + at * m.bytes[t];
-            for (int64_t i = threadIdx.x; i < m.bytes[t]; i += 256) to[i] = there ? from[i] : (char)0;
+        int64_t piece = item - at * m.pieces;
+        int t = 0;
+        while (piece >= (m.bytes[t] + kPiece - 1) / kPiece) piece -= (m.bytes[t] + kPiece - 1) / kPiece, ++t;
+        const int64_t lo = piece * kPiece + 16 * threadIdx.x;
+        const uint8_t* from = (const uint8_t*)m.in[t] + (g * m.beams + (there ? parent : 0)) * m.stride[t];
+        uint8_t* to = (uint8_t*)m.out[t] + at * m.bytes[t];
+        typedef words4 loose __attribute__((aligned(1), may_alias));
+        if (lo + 16 <= m.bytes[t]) {
+            *(loose*)(to + lo) = there ? *(const loose*)(from + lo) : (words4){0, 0, 0, 0};
+        } else {
+            for (int64_t i = lo; i < m.bytes[t]; ++i) to[i] = there ? from[i] : (uint8_t)0;
         }
     }
 }
@@ -328,7 +446,7 @@ struct Layout {
 Layout layout(const ccdpp_beam_t* p) {
     Layout l;
     const int64_t rows = p->groups * p->beams, chunks = (p->v + kChunk - 1) / kChunk;
-    const int64_t wanted = std::max<int64_t>(1, std::min<int64_t>(2048 / std::max<int64_t>(rows, 1), 256));
+    const int64_t wanted = std::max<int64_t>(1, std::min<int64_t>(512 / std::max<int64_t>(rows, 1), 256));
     l.each = std::max<int64_t>(round_up((chunks + wanted - 1) / wanted, kWaves), kWaves);
     l.shares = (chunks + l.each - 1) / l.each;
     l.sums = 0;
@@ -400,14 +518,14 @@ int ccdpp_beam_reorder(int64_t groups, int32_t beams, int32_t k, const int64_t* 
     if (int rc = check_device()) return rc;
     if (groups == 0) return CCDPP_OK;
     Moves m;
-    m.parent = parent, m.rows = groups * k, m.beams = beams, m.k = k, m.n = 0;
+    m.parent = parent, m.rows = groups * k, m.beams = beams, m.k = k, m.n = 0, m.pieces = 0;
     for (int32_t i = 0; i < n; ++i) {
-        if (row_bytes[i]) m.in[m.n] = (const char*)in[i], m.out[m.n] = (char*)out[i], m.stride[m.n] = in_stride[i], m.bytes[m.n] = row_bytes[i], ++m.n;
+        if (row_bytes[i]) m.in[m.n] = (const char*)in[i], m.out[m.n] = (char*)out[i], m.stride[m.n] = in_stride[i], m.bytes[m.n] = row_bytes[i], m.pieces += (row_bytes[i] + kPiece - 1) / kPiece, ++m.n;
         if (!m.n || (m.n < kTable && i + 1 < n)) continue;
-        k_reorder<<<(unsigned)std::min<int64_t>(m.rows, kGrid), 256, 0, (hipStream_t)stream>>>(m);
+        k_reorder<<<(unsigned)std::min<int64_t>(m.rows * m.pieces, kGrid), 256, 0, (hipStream_t)stream>>>(m);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return hip_fail(e, "beam reordering");
-        m.n = 0;
+        m.n = 0, m.pieces = 0;
     }
     return CCDPP_OK;
 }
