@@ -3,10 +3,11 @@
 //   y_ij = [residual_ij +] x_ij [r_ij >= p 2^32] / (1 - p)
 //
 // r is a word of Philox4x32 with 7 rounds, the fewest that pass the tests of its authors: four columns share a counter.
+#include <algorithm>
 #include <cmath>
 
 #include "ccdpp_seq.h"
-#include "ops_internal.hpp"
+#include "seq_device.hpp"
 
 namespace ccdops {
 namespace {
@@ -20,11 +21,11 @@ struct Drop {
     uint32_t least;   // words from here on are kept
     int none;         // 1: nothing is kept
     float scale;
+    int64_t groups, step;  // of columns; rows that are at work at once
 };
 
 struct Words { uint32_t w[4]; };
 
-// The keys of the rounds are the caller's, so that they are computed once.
 __device__ __forceinline__ Words philox(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t k0, uint32_t k1) {
     uint32_t c3 = 0;
 #pragma unroll
@@ -37,21 +38,40 @@ __device__ __forceinline__ Words philox(uint32_t c0, uint32_t c1, uint32_t c2, u
     return {{c0, c1, c2, c3}};
 }
 
-// A thread takes four columns of a row.
-template <class T>
+// A thread keeps its kColumns columns and goes down the rows, `step` at a time, so the words' first round and half of their second are
+// computed once for the rows that share the upper half of their number.
+constexpr int kColumns = 8;
+constexpr int64_t kThreads = 1 << 19;  // of a launch: eight blocks of 256 for each CU
+
+template <class T, bool RESIDUAL>
 __global__ __launch_bounds__(256) void k_drop(Drop a) {
     const uint64_t seed = a.seed_at ? *a.seed_at : a.seed;
-    const int64_t fours = (a.d + 3) / 4, all = a.n * fours;
-    for (int64_t i = blockIdx.x * (int64_t)blockDim.x + threadIdx.x; i < all; i += (int64_t)gridDim.x * blockDim.x) {
-        const int64_t row = i / fours, q = i - row * fours;
-        const uint64_t at = (uint64_t)(a.first_row + row);
-        const Words w = philox((uint32_t)q, (uint32_t)at, (uint32_t)(at >> 32), (uint32_t)seed, (uint32_t)(seed >> 32));
-        for (int j = 0; j < 4; ++j) {
-            const int64_t c = 4 * q + j;
-            if (c >= a.d) break;
-            float v = !a.none && w.w[j] >= a.least ? (float)((const T*)a.x)[row * a.ldx + c] * a.scale : 0.f;
-            if (a.residual) v = (float)((const T*)a.residual)[row * a.ldr + c] + v;
-            ((T*)a.y)[row * a.ldy + c] = (T)v;
+    const uint32_t k0 = (uint32_t)seed, k1 = (uint32_t)(seed >> 32);
+    const int64_t thread = blockIdx.x * (int64_t)blockDim.x + threadIdx.x;
+    int64_t row = thread / a.groups;
+    if (row >= a.step) return;
+    const int64_t c = (thread - row * a.groups) * kColumns;
+    const bool whole = c + kColumns <= a.d;
+    while (row < a.n) {
+        const uint64_t first = (uint64_t)(a.first_row + row);
+        const uint32_t high = (uint32_t)(first >> 32);
+        const int64_t same = (int64_t)(0x100000000ull - (uint32_t)first);  // rows from here on with this upper half
+        const int64_t end = min(a.n, row + same);
+        for (; row < end; row += a.step) {
+            Values<T, kColumns> x, res, y;
+            x.load((const T*)a.x + row * a.ldx, c, a.d, whole);
+            if constexpr (RESIDUAL) res.load((const T*)a.residual + row * a.ldr, c, a.d, whole);
+            const uint32_t low = (uint32_t)(a.first_row + row);
+#pragma unroll
+            for (int q = 0; q < kColumns / 4; ++q) {
+                const Words w = philox((uint32_t)(c / 4) + q, low, high, k0, k1);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float v = !a.none && w.w[j] >= a.least ? x.get(4 * q + j) * a.scale : 0.f;
+                    y.set(4 * q + j, RESIDUAL ? res.get(4 * q + j) + v : v);
+                }
+            }
+            y.store((T*)a.y + row * a.ldy, c, a.d, whole);
         }
     }
 }
@@ -82,10 +102,16 @@ extern "C" int ccdpp_dropout(int64_t n, int64_t d, int32_t dtype, const void* x,
     if (int rc = check_device()) return rc;
     if (n == 0) return CCDPP_OK;
     const double least = std::rint(p * 4294967296.0);
-    Drop a = {n, d, ldx, ldr, ldy, first_row, x, residual, y, seed, seed_at, 0, least >= 4294967296.0, 0.f};
+    Drop a = {n, d, ldx, ldr, ldy, first_row, x, residual, y, seed, seed_at, 0, least >= 4294967296.0, 0.f, 0, 0};
     if (!a.none) a.least = (uint32_t)least, a.scale = (float)(1.0 / (1.0 - p));
-    const int64_t blocks = (n * ((d + 3) / 4) + 255) / 256;
-    typed(dtype, [&](auto z) { k_drop<decltype(z)><<<(unsigned)(blocks < 8192 ? blocks : 8192), 256, 0, (hipStream_t)stream>>>(a); });
+    a.groups = (d + kColumns - 1) / kColumns;
+    a.step = std::min<int64_t>(n, std::max<int64_t>(1, kThreads / a.groups));
+    const unsigned blocks = (unsigned)((a.groups * a.step + 255) / 256);
+    typed(dtype, [&](auto z) {
+        typedef decltype(z) T;
+        if (residual) k_drop<T, true><<<blocks, 256, 0, (hipStream_t)stream>>>(a);
+        else k_drop<T, false><<<blocks, 256, 0, (hipStream_t)stream>>>(a);
+    });
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? CCDPP_OK : hip_fail(e, "dropout");
 }

@@ -6,7 +6,7 @@
 #include <type_traits>
 
 #include "ccdpp_seq.h"
-#include "ops_internal.hpp"
+#include "seq_device.hpp"
 
 namespace ccdops {
 namespace {
@@ -682,15 +682,25 @@ __global__ __launch_bounds__(kThreads) void k_scan_grad(Scan a) {
     }
 }
 
+// A thread takes eight columns of a row.
+constexpr int kStepColumns = 8;
 template <class T, bool SIGMOID>
 __global__ __launch_bounds__(256) void k_step(int64_t n, int d, const T* x, int64_t ldx, const T* gate, int64_t ldg, float* state, int64_t lds, T* y,
                                               int64_t ldy) {
-    for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < n * d; i += (int64_t)gridDim.x * 256) {
-        const int64_t r = i / d, c = i - r * d;
-        const Terms w = terms_of<SIGMOID>((float)x[r * ldx + c], (float)gate[r * ldg + c]);
-        const float h = fmaf(w.a, state[r * lds + c], w.u);
-        state[r * lds + c] = h;
-        y[r * ldy + c] = (T)h;
+    const int64_t groups = (d + kStepColumns - 1) / kStepColumns;
+    for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < n * groups; i += (int64_t)gridDim.x * 256) {
+        const int64_t r = i / groups, c = (i - r * groups) * kStepColumns;
+        const bool whole = c + kStepColumns <= d;
+        Values<T, kStepColumns> u, z, out;
+        Values<float, kStepColumns> h;
+        u.load(x + r * ldx, c, d, whole), z.load(gate + r * ldg, c, d, whole), h.load(state + r * lds, c, d, whole);
+#pragma unroll
+        for (int j = 0; j < kStepColumns; ++j) {
+            const Terms w = terms_of<SIGMOID>(u.get(j), z.get(j));
+            const float v = fmaf(w.a, h.get(j), w.u);
+            h.set(j, v), out.set(j, v);
+        }
+        h.store(state + r * lds, c, d, whole), out.store(y + r * ldy, c, d, whole);
     }
 }
 
@@ -857,7 +867,7 @@ int ccdpp_gated_scan_step(int64_t n, int32_t d, int32_t dtype, int32_t mode, con
     if (misaligned(x, es) || misaligned(gate, es) || misaligned(y, es) || misaligned(state, 4)) return fail(CCDPP_EINVAL, "pointers must be aligned to their types");
     if (int rc = check_device()) return rc;
     if (n == 0) return CCDPP_OK;
-    const int64_t blocks = (n * d + 255) / 256;
+    const int64_t blocks = (n * ((d + kStepColumns - 1) / kStepColumns) + 255) / 256;
     typed(dtype, mode, [&](auto z, auto sigmoid) {
         typedef decltype(z) T;
         k_step<T, decltype(sigmoid)::value><<<(unsigned)(blocks < 8192 ? blocks : 8192), 256, 0, (hipStream_t)stream>>>(n, d, (const T*)x, ldx, (const T*)gate, ldg,
