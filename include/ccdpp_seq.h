@@ -73,7 +73,7 @@ int ccdpp_scan_kept(const ccdpp_scan_t *p, int64_t *bytes);
  * has none).
  *   y, ldy : n rows of d values of dtype, ldy >= d values apart
  *   last   : float, s rows of d, or NULL
- *   kept   : ccdpp_scan_kept bytes, aligned to 16, or NULL: one state in 16 rows */
+ *   kept   : ccdpp_scan_kept bytes, aligned to 16, or NULL: one state in 8 rows */
 int ccdpp_gated_scan(const ccdpp_scan_t *p, void *y, int64_t ldy, float *last, void *kept,
                      void *workspace, int64_t workspace_bytes, void *stream);
 

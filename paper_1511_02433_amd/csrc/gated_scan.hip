@@ -11,19 +11,20 @@
 namespace ccdops {
 namespace {
 
-constexpr int kRows = 16;      // of a chunk; one state of a chunk is kept
-constexpr int kThreads = 256;  // of a block
+constexpr int kRows = 8;       // of a chunk; one state of a chunk is kept
+constexpr int kThreads = 512;  // of a block
 
-// Both a and 1 - a to some 2^-22 of themselves, for gates of either sign: e = exp(-|gate|), with what the product by log2 e
-// rounds off put back.
+// Both a and 1 - a to some 2^-21 of themselves, for gates of either sign: e = exp(-|gate|), with what the product by log2 e rounded off put
+// back.  (e is 0 to 32 bits where -104 takes the place of less, and a product of infinities would be NaN; a gate that is NaN stays it.)
 struct Gate { float a, rest; };
 __device__ __forceinline__ Gate sigmoid_of(float gate) {
-    const float z = -fabsf(gate), p = z * 1.44269504f;
-    const float off = fmaf(z, 1.44269504f, -p) + z * 1.92596299e-8f;  // z log2 e - p
+    const float z = __builtin_elementwise_maximum(-fabsf(gate), -104.f), p = z * 1.44269504f;
+    const float off = fmaf(-p, -1.90465430e-9f, fmaf(-p, 0.693147182f, z));  // z - p ln 2
     float e = __builtin_amdgcn_exp2f(p);
-    e = p > -200.f ? fmaf(e, off * 0.693147181f, e) : e;
+    e = fmaf(e, off, e);
     const float big = __builtin_amdgcn_rcpf(1.f + e), small = e * big;
-    return gate >= 0.f ? Gate{big, small} : gate < 0.f ? Gate{small, big} : Gate{gate, gate};
+    const bool up = gate >= 0.f;
+    return {up ? big : small, up ? small : big};
 }
 
 struct Terms { float a, u, rest; };
@@ -95,7 +96,7 @@ struct Share {
     int64_t q;
 };
 // kRows rows of a chunk: the sequence of the first one (-1 or s: none), and a bit for each row that begins a sequence (or the rows
-// behind all), bit kRows for the row after the chunk.
+// behind all), bit kRows for the row after the chunk.  kSkips: sequences without rows begin in it, too; of_row says which begin there.
 struct Chunk {
     int32_t q;
     uint32_t begins;
@@ -110,7 +111,7 @@ struct Scan {
     float *last, *keep, *dinitial;
     // How the work is shared out.
     int strips, lanes, groups, shares;  // a block has `groups` groups of `lanes` lanes
-    int64_t rows;                       // of a share, before it is moved to where a sequence begins
+    int64_t rows, near;                 // of a share, before it is moved to where a sequence begins, and how far it is moved at most
     int64_t chunks;
     Share* share;      // shares + 1
     Chunk* chunk;      // chunks
@@ -137,21 +138,22 @@ __device__ int64_t find_start(const Scan& a, int64_t row) {
     return lo;
 }
 
-// Share p begins at row p * rows, or where a sequence does if that is no more than a quarter of a share away: what goes on from one
+// Share p begins at row p * rows, or where a sequence does if that is near: what goes on from one
 // share to the next costs a second pass over its rows.
 __device__ Share share_of(const Scan& a, int64_t p) {
     if (p <= 0) return {0, 0, 0, -1};
     if (p >= a.shares) return {a.n, 0, 0, -1};
-    const int64_t row = p * a.rows, j = find_start(a, row), near = a.rows / 4;
+    const int64_t row = p * a.rows, j = find_start(a, row);
     const int64_t next = j <= a.s ? start_of(a, j) : a.n, prev = j > 0 ? start_of(a, j - 1) : 0;
-    if (next >= row && next - row <= near) return {next, 0, 0, -1};
-    if (j > 0 && prev <= row && row - prev <= near) return {prev, 0, 0, -1};
+    if (next >= row && next - row <= a.near) return {next, 0, 0, -1};
+    if (j > 0 && prev <= row && row - prev <= a.near) return {prev, 0, 0, -1};
     if (j == 0 || j > a.s || prev > row || next < row) return {row, 0, 0, -1};
     return {row, prev, next, j - 1};
 }
 
 // What a chain of rows does to the state before it: A state + H; where a sequence begins in it the state behind it is H, whatever
 // was before (A is kReset then, a bit pattern that no product has: products have no signalling NaN).
+constexpr uint32_t kSkips = 1u << 31;
 constexpr uint32_t kReset = 0x7F800001u;
 
 // A thread's place: `lanes` lanes side by side take the columns of a strip, W each, and `groups` of them a chunk each, one after
@@ -169,7 +171,10 @@ struct Place {
 
 template <int W>
 struct Exchange {
-    float A[2][W][kThreads], H[2][W][kThreads];
+    struct alignas(8 * W) Link {
+        float A[W], H[W];
+    };
+    Link of[2][kThreads];
 };
 
 // Joins the chains of a block's groups: c goes in as the state before all of them and out as that behind all; returns the state
@@ -177,16 +182,20 @@ struct Exchange {
 template <int W>
 __device__ __forceinline__ void join(const Scan& a, Exchange<W>& e, const Place<W>& at, int step, const float (&A)[W], const float (&H)[W], bool reset, float (&c)[W],
                                      float (&mine)[W]) {
-    const int b = step & 1;
+    typename Exchange<W>::Link* const of = e.of[step & 1];
+    typename Exchange<W>::Link own;
 #pragma unroll
-    for (int w = 0; w < W; ++w) e.A[b][w][threadIdx.x] = reset ? __uint_as_float(kReset) : A[w], e.H[b][w][threadIdx.x] = H[w];
+    for (int w = 0; w < W; ++w) own.A[w] = reset ? __uint_as_float(kReset) : A[w], own.H[w] = H[w];
+    of[threadIdx.x] = own;
     __syncthreads();
+#pragma unroll 4
     for (int g = 0; g < a.groups; ++g) {
+        const typename Exchange<W>::Link one = of[g * a.lanes + at.lane];
+        const bool begins = __float_as_uint(one.A[0]) == kReset, before = g == at.group;
 #pragma unroll
         for (int w = 0; w < W; ++w) {
-            const float p = e.A[b][w][g * a.lanes + at.lane], q = e.H[b][w][g * a.lanes + at.lane];
-            if (g == at.group) mine[w] = c[w];
-            c[w] = __float_as_uint(p) == kReset ? q : fmaf(p, c[w], q);
+            mine[w] = before ? c[w] : mine[w];
+            c[w] = begins ? one.H[w] : fmaf(one.A[w], c[w], one.H[w]);
         }
     }
 }
@@ -216,6 +225,13 @@ struct Rows {
         }
     }
 };
+
+// The sequence of row i of a chunk.
+__device__ __forceinline__ int64_t sequence_of(const Scan& a, Chunk k, int64_t row, int i) {
+    const uint32_t up_to = k.begins & ((2u << i) - 1) & ~1u;
+    if (!(k.begins & kSkips) || !up_to) return k.q + __popc(up_to);
+    return a.of_row[row + 31 - __builtin_clz(up_to)];
+}
 
 // A row of the s x d states of sequences; NULL for what is no sequence.
 template <class P>
@@ -310,7 +326,7 @@ __global__ __launch_bounds__(kThreads) void k_scan_first(Scan a) {
             join<W>(a, e, at, (int)step, pa, ph, false, C, mine);
             for (int g = 0; g < a.groups; ++g)
 #pragma unroll
-                for (int w = 0; w < W; ++w) all[w] *= e.A[step & 1][w][g * a.lanes + at.lane];
+                for (int w = 0; w < W; ++w) all[w] *= e.of[step & 1][g * a.lanes + at.lane].A[w];
 #pragma unroll
             for (int w = 0; w < W; ++w) A[w] *= all[w];
         }
@@ -338,6 +354,7 @@ __global__ __launch_bounds__(kThreads) void k_scan_first(Scan a) {
         const int64_t row = c * kRows;
         int64_t j = find(row, 0), r = -1;
         Chunk k = {(int32_t)(j - 1), 0u};
+        int64_t q = j - 1;  // the last sequence so far
         while (j <= a.s) {
             const int64_t begin = start_of(a, j);
             if (begin < row || begin > row + kRows || begin <= r) break;
@@ -345,7 +362,8 @@ __global__ __launch_bounds__(kThreads) void k_scan_first(Scan a) {
             const bool more = j < a.s && start_of(a, j + 1) == r;  // sequences without rows begin there, too
             j = more ? find(r + 1, j + 1) : j + 1;
             k.begins |= 1u << (r - row);
-            if (r == row) k.q = (int32_t)(j - 1);
+            if (r == row) k.q = (int32_t)(j - 1), q = j - 1;
+            else if (j - 1 != ++q) k.begins |= kSkips, q = j - 1;
             if (r < row + kRows && r < a.n) a.of_row[r] = (int32_t)(j - 1);
         }
         a.chunk[c] = k;
@@ -379,21 +397,18 @@ __device__ void carry_in(const Scan& a, Exchange<W>& e, const Place<W>& at, int 
     for (int w = 0; w < W; ++w) c[w] = 0.f;
     if (edge.q < 0) return;
     // The share in which the sequence begins (ends); there, nothing comes in.
-    int far = (int)min(max((GRAD ? edge.next - 1 : edge.prev) / a.rows, (int64_t)0), (int64_t)a.shares - 1);
-    if (GRAD) {
-        far = max(far - 1, p + 1);
-        while (far + 1 < a.shares && a.share[far + 1].begin < edge.next) ++far;
-    } else {
-        far = min(far + 1, p - 1);
-        while (far > 0 && a.share[far].begin > edge.prev) --far;
-    }
+    // (Share i begins at i * rows or where the sequence does if that is near, as share_of has it.)
+    const int64_t i = (GRAD ? edge.next - 1 : edge.prev) / a.rows;
+    int far;
+    if (GRAD) far = (int)min(max(edge.next - i * a.rows <= a.near ? i - 1 : i, (int64_t)p + 1), (int64_t)a.shares - 1);
+    else far = (int)min(max((i + 1) * a.rows - edge.prev <= a.near ? i + 1 : i, (int64_t)0), (int64_t)p - 1);
     const int count = GRAD ? far - p : p - far, per = (count + a.groups - 1) / a.groups;
     const int from = min(at.group * per, count), to = min(from + per, count);
     float A[W], H[W], mine[W];
 #pragma unroll
     for (int w = 0; w < W; ++w) A[w] = 1.f, H[w] = 0.f;
     if (at.works) {
-#pragma unroll 4
+#pragma unroll 8
         for (int i = from; i < to; ++i) {
             const float* k = a.carry + ((int64_t)(GRAD ? far - i : far + i) * a.d + at.col) * 2;
 #pragma unroll
@@ -435,7 +450,7 @@ __global__ __launch_bounds__(kThreads) void k_scan(Scan a) {
         const uint32_t mine = here ? rows_within(row, begin, end) : 0u, in = here ? rows_within(row, lo, hi) : 0u;
         const uint32_t firsts = here ? k.begins & mine : 0u, lasts = here ? k.begins >> 1 & in : 0u;
         const bool plain = in == kAll && !(firsts | lasts);
-        int64_t q = k.q;
+        const Chunk now = k;
         float d[kRows][W], u[kRows][W];
 #pragma unroll
         for (int i = 0; i < kRows; ++i)
@@ -458,7 +473,7 @@ __global__ __launch_bounds__(kThreads) void k_scan(Scan a) {
             for (int i = 0; i < kRows; ++i) {
                 const bool inside = in >> i & 1, first = firsts >> i & 1;
                 const float* from = nullptr;
-                if (first && inside && a.initial) from = states_of(a, a.initial, a.of_row[row + i], at.col);
+                if (first && inside && a.initial) from = states_of(a, a.initial, sequence_of(a, now, row, i), at.col);
 #pragma unroll
                 for (int w = 0; w < W; ++w) {
                     if (!inside) d[i][w] = 1.f, u[i][w] = 0.f;
@@ -488,7 +503,6 @@ __global__ __launch_bounds__(kThreads) void k_scan(Scan a) {
 #pragma unroll
             for (int i = 0; i < kRows; ++i) {
                 const bool inside = in >> i & 1, first = firsts >> i & 1;
-                if (first && inside) q = a.of_row[row + i];
                 float out[W];
 #pragma unroll
                 for (int w = 0; w < W; ++w) {
@@ -499,7 +513,7 @@ __global__ __launch_bounds__(kThreads) void k_scan(Scan a) {
                 r.set(out);
                 if (mine >> i & 1) r.store(y);
                 next(y, a.ldy);
-                if (float* const to = lasts >> i & 1 ? states_of(a, a.last, q, at.col) : nullptr)
+                if (float* const to = (lasts >> i & 1) && a.last ? states_of(a, a.last, sequence_of(a, now, row, i), at.col) : nullptr)
 #pragma unroll
                     for (int w = 0; w < W; ++w) to[w] = h[w];
             }
@@ -537,53 +551,32 @@ __global__ __launch_bounds__(kThreads) void k_scan_grad(Scan a) {
         const uint32_t mine = here ? rows_within(row, begin, end) : 0u, in = here ? rows_within(row, lo, hi) : 0u;
         const uint32_t firsts = here ? k.begins & in : 0u, lasts = here ? k.begins >> 1 & in : 0u;
         const bool plain = in == kAll && !(firsts | lasts);
-        const int64_t q0 = k.q;
-        // Kept in registers from the pass down the rows for the two up: what l is multiplied by for dgate, dy as it is, and the gate: as it
-        // is, or the lesser of a and 1 - a, negative where that is 1 - a (the other one is 1 less its absolute value to half a step).
-        float f[kRows][W], lesser[kRows][W];
-        const Rows<T, W> g = dy, given = gate;
-        const auto a_of = [&](int i, int w, const auto& gate) {
-            if (!SIGMOID) return gate.get(w);
-            const float v = lesser[i][w];
-            return __float_as_uint(v) >> 31 ? 1.f + v : v;
-        };
-        const auto rest_of = [&](int i, int w) {
-            const float v = lesser[i][w];
-            return __float_as_uint(v) >> 31 ? -v : 1.f - v;
-        };
+        const Chunk now = k;
+        // Kept in registers from the pass down the rows for the two up: a, 1 - a, what l is multiplied by for dgate, and dy as it is.
+        float d[kRows][W], rest[kRows][W], f[kRows][W];
+        const Rows<T, W> g = dy;
         // One row down: its f, and the state behind it.
         const auto down = [&](int i, int w, const auto& x, const auto& gate, float& h) {
             const float v = x.get(w), z = gate.get(w);
-            if constexpr (SIGMOID) {
-                const Gate m = sigmoid_of(z);
-                lesser[i][w] = z >= 0.f ? -m.rest : m.a;
-                f[i][w] = (h - v) * (m.a * m.rest);
-                h = fmaf(m.a, h, m.rest * v);
-            } else {
-                f[i][w] = h;
-                h = fmaf(z, h, v);
-            }
+            const Terms m = terms_of<SIGMOID>(v, z);
+            d[i][w] = m.a, rest[i][w] = m.rest;
+            f[i][w] = SIGMOID ? (h - v) * (m.a * m.rest) : h;
+            h = fmaf(m.a, h, m.u);
         };
         float h[W], A[W], H[W], m[W];
 #pragma unroll
         for (int w = 0; w < W; ++w) h[w] = h0.get(w), A[w] = 1.f, H[w] = 0.f;
-        // The sequence of a row with a last one in its chunk.
-        const auto sequence_at = [&](int i) {
-            const uint32_t before = firsts & ((2u << i) - 1);
-            return before ? (int64_t)a.of_row[row + 31 - __builtin_clz(before)] : q0;
-        };
         if (plain) {
 #pragma unroll
             for (int i = 0; i < kRows; ++i) {
 #pragma unroll
                 for (int w = 0; w < W; ++w) down(i, w, x.v[i], gate.v[i], h[w]);
-                if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
             }
         } else {
 #pragma unroll
             for (int i = 0; i < kRows; ++i) {
                 if (firsts >> i & 1) {
-                    const float* from = a.initial ? states_of(a, a.initial, a.of_row[row + i], at.col) : nullptr;
+                    const float* from = a.initial ? states_of(a, a.initial, sequence_of(a, now, row, i), at.col) : nullptr;
 #pragma unroll
                     for (int w = 0; w < W; ++w) h[w] = from ? from[w] : 0.f;
                 }
@@ -596,77 +589,62 @@ __global__ __launch_bounds__(kThreads) void k_scan_grad(Scan a) {
                 }
             }
         }
-        // (Unknown to the compiler again: it would keep both factors of every value from one pass to the next.)
-        const auto forget = [&] {
-            if constexpr (SIGMOID)
-#pragma unroll
-                for (int i = 0; i < kRows; ++i)
-#pragma unroll
-                    for (int w = 0; w < W; ++w) asm("" : "+v"(lesser[i][w]));
-        };
-        forget();
         load(step + 1);
         if (plain) {
 #pragma unroll
             for (int i = kRows - 1; i >= 0; --i)
 #pragma unroll
                 for (int w = 0; w < W; ++w) {
-                    const float d = a_of(i, w, given.v[i]);
-                    A[w] *= d, H[w] = d * (g.v[i].get(w) + H[w]);
-                    if (i % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+                    A[w] *= d[i][w], H[w] = d[i][w] * (g.v[i].get(w) + H[w]);
                 }
         } else {
 #pragma unroll
             for (int i = kRows - 1; i >= 0; --i) {
                 if (lasts >> i & 1) {
-                    const float* from = states_of(a, a.dlast, sequence_at(i), at.col);
+                    const float* from = states_of(a, a.dlast, a.dlast ? sequence_of(a, now, row, i) : 0, at.col);
 #pragma unroll
                     for (int w = 0; w < W; ++w) H[w] = from ? from[w] : 0.f;
                 }
-                const auto gi = g.v[i].again(), zi = given.v[i].again();
+                const auto gi = g.v[i].again();
 #pragma unroll
-                for (int w = 0; w < W; ++w) {
-                    const float d = a_of(i, w, zi);
-                    if (in >> i & 1) A[w] *= d, H[w] = d * (gi.get(w) + H[w]);
-                }
+                for (int w = 0; w < W; ++w)
+                    if (in >> i & 1) A[w] *= d[i][w], H[w] = d[i][w] * (gi.get(w) + H[w]);
             }
         }
-        forget();
         join<W>(a, e, at, (int)step, A, H, lasts != 0, carry, m);
         T* dx = (T*)a.dx + (row + kRows - 1) * a.lddx + at.col;
         T* dg = (T*)a.dgate + (row + kRows - 1) * a.lddg + at.col;
         // One row up: its gradients, and what goes on to the row before it.
-        const auto up = [&](int i, int w, const auto& g, const auto& gate, float& m, float& to_x, float& to_gate) {
+        const auto up = [&](int i, int w, const auto& g, float& m, float& to_x, float& to_gate) {
             const float l = g.get(w) + m;
-            to_x = SIGMOID ? rest_of(i, w) * l : l, to_gate = l * f[i][w];
-            m = a_of(i, w, gate) * l;
+            to_x = SIGMOID ? rest[i][w] * l : l, to_gate = l * f[i][w];
+            m = d[i][w] * l;
         };
         if (plain) {
 #pragma unroll
             for (int i = kRows - 1; i >= 0; --i) {
                 float to_x[W], to_gate[W];
 #pragma unroll
-                for (int w = 0; w < W; ++w) up(i, w, g.v[i], given.v[i], m[w], to_x[w], to_gate[w]);
+                for (int w = 0; w < W; ++w) up(i, w, g.v[i], m[w], to_x[w], to_gate[w]);
                 Few<T, W> r, t;
                 r.set(to_x), t.set(to_gate);
                 r.store(dx), t.store(dg);
                 next(dx, -a.lddx), next(dg, -a.lddg);
-                if (i % 4 == 0) __builtin_amdgcn_sched_barrier(0);
             }
         } else {
 #pragma unroll
             for (int i = kRows - 1; i >= 0; --i) {
                 if (lasts >> i & 1) {
-                    const float* from = states_of(a, a.dlast, sequence_at(i), at.col);
+                    const float* from = states_of(a, a.dlast, a.dlast ? sequence_of(a, now, row, i) : 0, at.col);
 #pragma unroll
                     for (int w = 0; w < W; ++w) m[w] = from ? from[w] : 0.f;
                 }
                 float to_x[W], to_gate[W];
-                const auto gi = g.v[i].again(), zi = given.v[i].again();
+                const auto gi = g.v[i].again();
 #pragma unroll
                 for (int w = 0; w < W; ++w) {
                     float to = m[w];
-                    up(i, w, gi, zi, to, to_x[w], to_gate[w]);
+                    up(i, w, gi, to, to_x[w], to_gate[w]);
                     if (in >> i & 1) m[w] = to;
                     else to_x[w] = to_gate[w] = 0.f;
                 }
@@ -674,7 +652,7 @@ __global__ __launch_bounds__(kThreads) void k_scan_grad(Scan a) {
                 r.set(to_x), t.set(to_gate);
                 if (mine >> i & 1) r.store(dx), t.store(dg);
                 next(dx, -a.lddx), next(dg, -a.lddg);
-                if (float* const to = (firsts >> i & 1) && a.dinitial ? states_of(a, a.dinitial, a.of_row[row + i], at.col) : nullptr)
+                if (float* const to = (firsts >> i & 1) && a.dinitial ? states_of(a, a.dinitial, sequence_of(a, now, row, i), at.col) : nullptr)
 #pragma unroll
                     for (int w = 0; w < W; ++w) to[w] = m[w];
             }
@@ -745,17 +723,23 @@ struct Layout {
     int64_t share, chunk, of_row, carry, bytes;
 };
 
+constexpr int64_t kLeastBlocks = 256, kMostBlocks = 512;
+
 Layout layout(const ccdpp_scan_t* p) {
     Layout l;
     l.width = p->d >= 2 ? 2 : 1;
     const int lanes = (p->d + l.width - 1) / l.width;
-    l.strips = (lanes + 63) / 64;
-    l.lanes = (lanes + l.strips - 1) / l.strips;
-    l.groups = std::min(kThreads / l.lanes, 64);
     l.chunks = (p->n + kRows - 1) / kRows;
-    const int64_t most = std::max<int64_t>(1, 1024 / l.strips), least = std::max<int64_t>(1, 512 / l.strips);
-    int64_t shares = std::min(std::max(p->s, least), most);
-    shares = std::max<int64_t>(1, std::min(shares, l.chunks / l.groups));
+    int64_t shares = 1;
+    for (int widest = 64;; widest /= 2) {
+        l.strips = (lanes + widest - 1) / widest;
+        l.lanes = (lanes + l.strips - 1) / l.strips;
+        l.groups = std::min(kThreads / l.lanes, 64);
+        const int64_t most = std::max<int64_t>(1, kMostBlocks / l.strips), least = std::max<int64_t>(1, kLeastBlocks / l.strips);
+        shares = std::min(std::max(p->s, least), most);
+        shares = std::max<int64_t>(1, std::min(shares, l.chunks / l.groups));
+        if (l.strips * shares >= kMostBlocks || widest * l.width * (p->dtype == CCDPP_F32 ? 4 : 2) <= 256) break;
+    }
     l.rows = round_up((std::max<int64_t>(p->n, 1) + shares - 1) / shares, kRows);
     l.shares = (int)((std::max<int64_t>(p->n, 1) + l.rows - 1) / l.rows);
     l.share = 0;
@@ -771,7 +755,7 @@ int64_t workspace(const ccdpp_scan_t* p, int32_t) { return layout(p).bytes; }
 void set(Scan& a, const ccdpp_scan_t* p, const Layout& l, void* ws) {
     a.n = p->n, a.s = p->s, a.ldx = p->ldx, a.ldg = p->ldg, a.d = p->d, a.bits = p->starts_bits;
     a.x = p->x, a.gate = p->gate, a.starts = p->starts, a.initial = p->initial;
-    a.strips = l.strips, a.lanes = l.lanes, a.groups = l.groups, a.shares = l.shares, a.rows = l.rows, a.chunks = l.chunks;
+    a.strips = l.strips, a.lanes = l.lanes, a.groups = l.groups, a.shares = l.shares, a.rows = l.rows, a.near = l.rows * 3 / 8, a.chunks = l.chunks;
     a.share = (Share*)((char*)ws + l.share), a.chunk = (Chunk*)((char*)ws + l.chunk), a.of_row = (int32_t*)((char*)ws + l.of_row);
     a.carry = (float*)((char*)ws + l.carry);
     a.sums = l.strips * (l.shares - 1);

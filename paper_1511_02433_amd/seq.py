@@ -103,6 +103,12 @@ def _sequences(x, gate, starts, initial, mode):
                 gate.data_ptr(), ldg, at, first), index
 
 
+def _kept_rows(p):
+    n = ctypes.c_int64()
+    _check(_lib().ccdpp_scan_kept(ctypes.byref(p), ctypes.byref(n)))
+    return n.value // (4 * p.d)
+
+
 def _scan_workspace(p, call, device):
     n = ctypes.c_int64()
     _check(_lib().ccdpp_scan_workspace(ctypes.byref(p), call, ctypes.byref(n)))
@@ -123,7 +129,7 @@ def gated_scan(x, gate, *, starts, initial=None, mode="sigmoid", keep=False, y=N
         last = torch.empty((p.s, p.d), dtype=torch.float32, device=device)
         kept, at = None, None
         if keep:
-            kept = torch.empty(((p.n + 15) // 16, p.d), dtype=torch.float32, device=device)
+            kept = torch.empty(_kept_rows(p), p.d, dtype=torch.float32, device=device)
             at = kept.data_ptr()
         ws, n = _scan_workspace(p, FORWARD, device)
         _check(_lib().ccdpp_gated_scan(ctypes.byref(p), y.data_ptr(), ldy, last.data_ptr(), at, ws.data_ptr(), n, _stream(index)))
@@ -137,7 +143,7 @@ def gated_scan_grad(x, gate, dy, kept, *, starts, initial=None, mode="sigmoid", 
     float32, s x d, or None for zeros; dinitial is None where initial is.  dx and dgate may be given to write to."""
     p, index = _sequences(x, gate, starts, initial, mode)
     lddy = _alike(dy, "dy", x)
-    k = _states(kept, "kept", (p.n + 15) // 16, p.d, index)
+    k = _states(kept, "kept", _kept_rows(p), p.d, index)
     dl = None if dlast is None else _states(dlast, "dlast", p.s, p.d, index)
     given = [a for a in (dx, dgate) if a is not None]
     with _On(index):

@@ -96,7 +96,7 @@ def test_kept_states_and_workspaces_are_small():
     for rows, s, d in ((0, 0, 1), (1, 1, 1), (17, 3, 65536), (1_000_209, 6041, 40), (32_768, 16, 4096), (65_537, 1, 100), ((1 << 31) - 1, (1 << 31) - 1, 8)):
         for dtype in (0, 1, 2):
             p = scan(n=rows, s=s, d=d, ldx=d, ldg=d, dtype=dtype)
-            assert L.ccdpp_scan_kept(B(p), B(n)) == 0 and n.value == (rows + 15) // 16 * 4 * d
+            assert L.ccdpp_scan_kept(B(p), B(n)) == 0 and n.value == (rows + 7) // 8 * 4 * d
             for call in (0, 1):
                 # a few numbers a row, and the states of the shares of rows
                 assert L.ccdpp_scan_workspace(B(p), call, B(n)) == 0 and 0 <= n.value <= 8 * rows + 64 * d * 4096 + (1 << 20)
