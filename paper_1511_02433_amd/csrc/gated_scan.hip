@@ -13,6 +13,7 @@ namespace {
 
 constexpr int kRows = 8;       // of a chunk; one state of a chunk is kept
 constexpr int kThreads = 512;  // of a block
+constexpr int kLanes = 64;     // of a group, at most
 
 // Both a and 1 - a to some 2^-21 of themselves, for gates of either sign: e = exp(-|gate|), with what the product by log2 e rounded off put
 // back.  (e is 0 to 32 bits where -104 takes the place of less, and a product of infinities would be NaN; a gate that is NaN stays it.)
@@ -175,13 +176,42 @@ struct Exchange {
         float A[W], H[W];
     };
     Link of[2][kThreads];
+    float behind[2][kLanes][W];  // the state behind the last group's rows
 };
 
-// Joins the chains of a block's groups: c goes in as the state before all of them and out as that behind all; returns the state
-// before this group.  One barrier a step; steps alternate between two buffers.
+// The state before this group's rows, from the chains of the groups before it and the state before all: `first` at the first step,
+// then what the last group left (leave).  One barrier a step; steps alternate between two buffers.
 template <int W>
-__device__ __forceinline__ void join(const Scan& a, Exchange<W>& e, const Place<W>& at, int step, const float (&A)[W], const float (&H)[W], bool reset, float (&c)[W],
-                                     float (&mine)[W]) {
+__device__ __forceinline__ void join(Exchange<W>& e, const Scan& a, const Place<W>& at, int step, const float (&A)[W], const float (&H)[W], bool reset,
+                                     const float (&first)[W], float (&c)[W]) {
+    typename Exchange<W>::Link* const of = e.of[step & 1];
+    typename Exchange<W>::Link own;
+#pragma unroll
+    for (int w = 0; w < W; ++w) own.A[w] = reset ? __uint_as_float(kReset) : A[w], own.H[w] = H[w];
+    of[threadIdx.x] = own;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < W; ++w) c[w] = step ? e.behind[step & 1][at.lane][w] : first[w];
+    const int before = at.works ? at.group : 0;
+#pragma unroll 4
+    for (int g = 0; g < before; ++g) {
+        const typename Exchange<W>::Link one = of[g * a.lanes + at.lane];
+        const bool begins = __float_as_uint(one.A[0]) == kReset;
+#pragma unroll
+        for (int w = 0; w < W; ++w) c[w] = begins ? one.H[w] : fmaf(one.A[w], c[w], one.H[w]);
+    }
+}
+template <int W>
+__device__ __forceinline__ void leave(Exchange<W>& e, const Scan& a, const Place<W>& at, int step, const float (&h)[W]) {
+    if (at.group == a.groups - 1)
+#pragma unroll
+        for (int w = 0; w < W; ++w) e.behind[(step + 1) & 1][at.lane][w] = h[w];
+}
+
+// The same over all groups: c goes in as the state before them and out as that behind.
+template <int W>
+__device__ __forceinline__ void join_all(const Scan& a, Exchange<W>& e, const Place<W>& at, int step, const float (&A)[W], const float (&H)[W], bool reset,
+                                         float (&c)[W]) {
     typename Exchange<W>::Link* const of = e.of[step & 1];
     typename Exchange<W>::Link own;
 #pragma unroll
@@ -191,12 +221,9 @@ __device__ __forceinline__ void join(const Scan& a, Exchange<W>& e, const Place<
 #pragma unroll 4
     for (int g = 0; g < a.groups; ++g) {
         const typename Exchange<W>::Link one = of[g * a.lanes + at.lane];
-        const bool begins = __float_as_uint(one.A[0]) == kReset, before = g == at.group;
+        const bool begins = __float_as_uint(one.A[0]) == kReset;
 #pragma unroll
-        for (int w = 0; w < W; ++w) {
-            mine[w] = before ? c[w] : mine[w];
-            c[w] = begins ? one.H[w] : fmaf(one.A[w], c[w], one.H[w]);
-        }
+        for (int w = 0; w < W; ++w) c[w] = begins ? one.H[w] : fmaf(one.A[w], c[w], one.H[w]);
     }
 }
 
@@ -306,7 +333,7 @@ __global__ __launch_bounds__(kThreads) void k_scan_first(Scan a) {
                         if (!(in >> i & 1)) d[i][w] = 1.f, u[i][w] = 0.f;
             }
             load(step + 1);
-            float pa[W], ph[W], mine[W];
+            float pa[W], ph[W];
             // (The state that comes in at lo, or at hi - 1, is put into that row: nothing comes before it.)
             const int64_t mark = in ? (GRAD ? hi - 1 : lo) - c * kRows : -1;
 #pragma unroll
@@ -323,7 +350,7 @@ __global__ __launch_bounds__(kThreads) void k_scan_first(Scan a) {
             float all[W];
 #pragma unroll
             for (int w = 0; w < W; ++w) all[w] = 1.f;
-            join<W>(a, e, at, (int)step, pa, ph, false, C, mine);
+            join_all<W>(a, e, at, (int)step, pa, ph, false, C);
             for (int g = 0; g < a.groups; ++g)
 #pragma unroll
                 for (int w = 0; w < W; ++w) all[w] *= e.of[step & 1][g * a.lanes + at.lane].A[w];
@@ -404,22 +431,31 @@ __device__ void carry_in(const Scan& a, Exchange<W>& e, const Place<W>& at, int 
     else far = (int)min(max((i + 1) * a.rows - edge.prev <= a.near ? i + 1 : i, (int64_t)0), (int64_t)p - 1);
     const int count = GRAD ? far - p : p - far, per = (count + a.groups - 1) / a.groups;
     const int from = min(at.group * per, count), to = min(from + per, count);
-    float A[W], H[W], mine[W];
+    float A[W], H[W];
 #pragma unroll
     for (int w = 0; w < W; ++w) A[w] = 1.f, H[w] = 0.f;
     if (at.works) {
-#pragma unroll 8
-        for (int i = from; i < to; ++i) {
-            const float* k = a.carry + ((int64_t)(GRAD ? far - i : far + i) * a.d + at.col) * 2;
+        constexpr int kAtOnce = 16;  // that are read together
+        for (int i0 = from; i0 < to; i0 += kAtOnce) {
+            float f[kAtOnce][W], g[kAtOnce][W];
 #pragma unroll
-            for (int w = 0; w < W; ++w) {
-                const float f = k[2 * w], g = k[2 * w + 1];
-                if (i == 0) H[w] = g;
-                else H[w] = fmaf(f, H[w], g), A[w] *= f;
+            for (int u = 0; u < kAtOnce; ++u) {
+                const int i = min(i0 + u, to - 1);
+                const float* k = a.carry + ((int64_t)(GRAD ? far - i : far + i) * a.d + at.col) * 2;
+#pragma unroll
+                for (int w = 0; w < W; ++w) f[u][w] = k[2 * w], g[u][w] = k[2 * w + 1];
             }
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u)
+#pragma unroll
+                for (int w = 0; w < W; ++w) {
+                    if (i0 + u >= to) continue;
+                    if (i0 + u == 0) H[w] = g[u][w];
+                    else H[w] = fmaf(f[u][w], H[w], g[u][w]), A[w] *= f[u][w];
+                }
         }
     }
-    join<W>(a, e, at, 0, A, H, at.works && from == 0 && to > 0, c, mine);
+    join_all<W>(a, e, at, 0, A, H, at.works && from == 0 && to > 0, c);
     __syncthreads();
 }
 
@@ -482,7 +518,7 @@ __global__ __launch_bounds__(kThreads) void k_scan(Scan a) {
                 }
             }
         }
-        join<W>(a, e, at, (int)step, A, H, firsts != 0, carry, h);
+        join<W>(e, a, at, (int)step, A, H, firsts != 0, carry, h);
         if (a.keep && (mine & 1)) {
             Few<float, W> r;
             r.set(h);
@@ -518,6 +554,7 @@ __global__ __launch_bounds__(kThreads) void k_scan(Scan a) {
                     for (int w = 0; w < W; ++w) to[w] = h[w];
             }
         }
+        leave<W>(e, a, at, (int)step, h);
     }
 }
 
@@ -611,7 +648,7 @@ __global__ __launch_bounds__(kThreads) void k_scan_grad(Scan a) {
                     if (in >> i & 1) A[w] *= d[i][w], H[w] = d[i][w] * (gi.get(w) + H[w]);
             }
         }
-        join<W>(a, e, at, (int)step, A, H, lasts != 0, carry, m);
+        join<W>(e, a, at, (int)step, A, H, lasts != 0, carry, m);
         T* dx = (T*)a.dx + (row + kRows - 1) * a.lddx + at.col;
         T* dg = (T*)a.dgate + (row + kRows - 1) * a.lddg + at.col;
         // One row up: its gradients, and what goes on to the row before it.
@@ -657,6 +694,7 @@ __global__ __launch_bounds__(kThreads) void k_scan_grad(Scan a) {
                     for (int w = 0; w < W; ++w) to[w] = m[w];
             }
         }
+        leave<W>(e, a, at, (int)step, m);
     }
 }
 
@@ -723,7 +761,7 @@ struct Layout {
     int64_t share, chunk, of_row, carry, bytes;
 };
 
-constexpr int64_t kLeastBlocks = 256, kMostBlocks = 512;
+constexpr int64_t kLeastBlocks = 512, kMostBlocks = 512;
 
 Layout layout(const ccdpp_scan_t* p) {
     Layout l;
@@ -731,7 +769,7 @@ Layout layout(const ccdpp_scan_t* p) {
     const int lanes = (p->d + l.width - 1) / l.width;
     l.chunks = (p->n + kRows - 1) / kRows;
     int64_t shares = 1;
-    for (int widest = 64;; widest /= 2) {
+    for (int widest = kLanes;; widest /= 2) {
         l.strips = (lanes + widest - 1) / widest;
         l.lanes = (lanes + l.strips - 1) / l.strips;
         l.groups = std::min(kThreads / l.lanes, 64);
