@@ -108,14 +108,12 @@ struct Chunk {
             }
         }
     }
-    // The logit with its offset; -inf where it takes no part, +inf for NaN.
+    // The logit with its offset; -inf where it takes no part.
     __device__ __forceinline__ float get(int e) const {
-        float z = (float)raw[e / V].v[e % V];
-        if constexpr (OFFSET) {
-            const float o = off[e / 4].v[e % 4];
-            z = o < -1e38f ? -INFINITY : z + o;
-        }
-        return z != z ? INFINITY : z + 0.f;
+        const float z = (float)raw[e / V].v[e % V];
+        if constexpr (!OFFSET) return z;
+        const float o = off[e / 4].v[e % 4];
+        return o < -1e38f ? -INFINITY : z + o;
     }
 };
 
@@ -191,10 +189,16 @@ __global__ __launch_bounds__(64 * kWaves) void k_beam_rows(Beam a) {
             for (int e = 0; e < kEach; ++e) z[e] = next.get(e);
             if (c + kWaves < end) next.load(base, a.offset, (c + kWaves) * kChunk, a.v);
             const uint32_t all_know = *(volatile uint32_t*)&known;
+            float run[C::J];  // the greatest of a run
             const auto greatest = [&] {
-                float m = z[0];
+                float m = -INFINITY;
 #pragma unroll
-                for (int e = 1; e < kEach; ++e) m = fmaxf(m, z[e]);
+                for (int j = 0; j < C::J; ++j) {
+                    run[j] = z[j * C::V];
+#pragma unroll
+                    for (int w = 1; w < C::V; ++w) run[j] = fmaxf(run[j], z[j * C::V + w]);
+                    m = fmaxf(m, run[j]);
+                }
                 return m;
             };
             float m = greatest();
@@ -204,13 +208,20 @@ __global__ __launch_bounds__(64 * kWaves) void k_beam_rows(Beam a) {
             float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int e = 0; e < kEach; ++e) part[e & 3] += __builtin_amdgcn_exp2f((z[e] - ref) * kLog2e);
-            sum = sum * (was == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((was - ref) * kLog2e)) + (double)((part[0] + part[1]) + (part[2] + part[3]));
+            const float parts = (part[0] + part[1]) + (part[2] + part[3]);
+            if (__ballot(parts != parts)) {  // NaN (or infinity less infinity): NaN counts as infinity
+#pragma unroll
+                for (int e = 0; e < kEach; ++e) z[e] = z[e] != z[e] ? INFINITY : z[e];
+                m = greatest();
+                top = fmaxf(top, m);
+            }
+            sum = sum * (was == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((was - ref) * kLog2e)) + (double)parts;
             // At least `bound`: above own, and not below what others know.
-            const auto bound_of = [&] { return value_of(max(order_of(found.own) + 1, all_know)); };
+            const auto bound_of = [&] { return value_of(max(order_of(found.own + 0.f) + 1, all_know)); };
             float bound = bound_of();
             uint64_t lanes = __ballot(m >= bound);
             if (!lanes) continue;
-            const auto key_of = [&](float v, int at) { return (uint64_t)order_of(v) << 32 | (uint32_t)~(uint32_t)(c * kChunk + at); };
+            const auto key_of = [&](float v, int at) { return (uint64_t)order_of(v + 0.f) << 32 | (uint32_t)~(uint32_t)(c * kChunk + at); };  // (-0 is 0)
             float raised = -INFINITY;
             if (__popcll(lanes) > a.k) {  // the k-th greatest of the lanes' greatest
                 int above = 0;
@@ -229,13 +240,18 @@ __global__ __launch_bounds__(64 * kWaves) void k_beam_rows(Beam a) {
             if (passing <= kAdded) {
                 asm("" : "+v"(bound));  // (compared again: 32 masks would not stay in scalar registers)
 #pragma unroll
-                for (int e = 0; e < kEach; ++e) {
-                    const bool pass = z[e] >= bound;
-                    const uint64_t those = __ballot(pass);
-                    if (!those) continue;
-                    const int at = found.n + __builtin_amdgcn_mbcnt_hi((uint32_t)(those >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)those, 0));
-                    if (pass) found.keys[at] = key_of(z[e], (e / C::V) * 64 * C::V + lane * C::V + e % C::V);
-                    found.n += __popcll(those);
+                for (int j = 0; j < C::J; ++j) {
+                    if (!__ballot(run[j] >= bound)) continue;
+#pragma unroll
+                    for (int w = 0; w < C::V; ++w) {
+                        const int e = j * C::V + w;
+                        const bool pass = z[e] >= bound;
+                        const uint64_t those = __ballot(pass);
+                        if (!those) continue;
+                        const int at = found.n + __builtin_amdgcn_mbcnt_hi((uint32_t)(those >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)those, 0));
+                        if (pass) found.keys[at] = key_of(z[e], j * 64 * C::V + lane * C::V + w);
+                        found.n += __popcll(those);
+                    }
                 }
             } else {
                 bound = bound_of();
@@ -272,7 +288,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_beam_rows(Beam a) {
             const float before = found.own;
             found.own = fmaxf(before, raised);
             if (found.n >= 2 * a.k) found.prune(a.k);
-            if (found.own > before && lane == 0) atomicMax(&known, order_of(found.own));
+            if (found.own > before && lane == 0) atomicMax(&known, order_of(found.own + 0.f));
         }
         found.prune(a.k);
         const float all = wave_max(top);
@@ -314,11 +330,13 @@ __global__ __launch_bounds__(1024) void k_beam_join(Beam a) {
     __shared__ double logs[kMost];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     for (int64_t g = blockIdx.x; g < a.groups; g += gridDim.x) {
+        float my_score = -INFINITY;  // of beam `lane`
+        bool my_done = false;
+        if (lane < a.beams) my_score = a.score[g * a.beams + lane], my_done = a.done && a.done[g * a.beams + lane];
         for (int b = wave; b < a.beams; b += waves) {
             const int64_t row = g * a.beams + b;
-            if (a.score[row] == -INFINITY || (a.done && a.done[row])) continue;
             const int64_t first = row * a.shares;
-            // What most rows need is asked for at once: the first lists, tops and sums.
+            // What most rows need is asked for at once: the first lists, tops and sums.  (Where the beam is none or done they hold nothing.)
             constexpr int kAtOnce = 8;
             uint64_t other[kAtOnce];
             const auto ask = [&](int s) {
@@ -329,6 +347,7 @@ __global__ __launch_bounds__(1024) void k_beam_join(Beam a) {
             double my_sum = 0.0;
             if (lane < a.shares) my_top = a.tops[first + lane], my_sum = a.sums[first + lane];
             ask(0);
+            if (lane_of(my_score, b) == -INFINITY || __ballot(my_done) >> b & 1) continue;
             Best best = {other[0]};
             other[0] = 0;
             for (int s = 0;;) {
@@ -350,18 +369,19 @@ __global__ __launch_bounds__(1024) void k_beam_join(Beam a) {
                 my_top = more;
             }
             const float top = wave_max(my_top);
-            double sum = my_top == -INFINITY ? 0.0 : my_sum * exp((double)my_top - top);
-            for (int k = 32; k > 0; k >>= 1) sum += __shfl_xor(sum, k);
+            double sum = my_sum;
+            if (a.shares > 1) {
+                sum = my_top == -INFINITY ? 0.0 : my_sum * exp((double)my_top - top);
+                for (int k = 32; k > 0; k >>= 1) sum += __shfl_xor(sum, k);
+            }
             if (lane < a.k) lists[b][lane] = best.key;
             if (lane == 0) logs[b] = top == INFINITY ? (double)NAN : top + log(sum);
         }
         __syncthreads();
         if (wave == 0) {
             const int b = lane;
-            const int64_t row = g * a.beams + b;
-            float s = -INFINITY;
-            bool done = false;
-            if (b < a.beams) s = a.score[row], done = a.done && a.done[row];
+            const float s = my_score;
+            const bool done = my_done;
             const bool live = s != -INFINITY;
             const double sum = live && !done ? logs[b] : 0.0;
             int at = 0;

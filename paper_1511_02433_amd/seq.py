@@ -103,16 +103,25 @@ def _sequences(x, gate, starts, initial, mode):
                 gate.data_ptr(), ldg, at, first), index
 
 
+# Sizes of workspaces go by the problems' sizes: asked for once (a call of the library takes a microsecond or two).
+@functools.lru_cache(maxsize=4096)
+def _scan_bytes(n, s, d, dtype, mode, call):
+    """Bytes of the workspace of a call, or (None) rows of kept states."""
+    p, got = Scan(n, s, d, dtype, mode, 64, None, d, None, d, None, None), ctypes.c_int64()
+    if call is None:
+        _check(_lib().ccdpp_scan_kept(ctypes.byref(p), ctypes.byref(got)))
+        return got.value // (4 * d)
+    _check(_lib().ccdpp_scan_workspace(ctypes.byref(p), call, ctypes.byref(got)))
+    return got.value
+
+
 def _kept_rows(p):
-    n = ctypes.c_int64()
-    _check(_lib().ccdpp_scan_kept(ctypes.byref(p), ctypes.byref(n)))
-    return n.value // (4 * p.d)
+    return _scan_bytes(p.n, p.s, p.d, p.dtype, p.mode, None)
 
 
 def _scan_workspace(p, call, device):
-    n = ctypes.c_int64()
-    _check(_lib().ccdpp_scan_workspace(ctypes.byref(p), call, ctypes.byref(n)))
-    return torch.empty(n.value, dtype=torch.uint8, device=device), n
+    n = _scan_bytes(p.n, p.s, p.d, p.dtype, p.mode, call)
+    return torch.empty(n, dtype=torch.uint8, device=device), n
 
 
 def gated_scan(x, gate, *, starts, initial=None, mode="sigmoid", keep=False, y=None):
@@ -182,6 +191,13 @@ def _count(a, name):
     return a
 
 
+@functools.lru_cache(maxsize=4096)
+def _beam_bytes(g, v, b, k, dtype):
+    p, got = Beam(g, v, b, k, dtype, 0, None, v, None, None, None, -1), ctypes.c_int64()
+    _check(_lib().ccdpp_beam_workspace(ctypes.byref(p), ctypes.byref(got)))
+    return got.value
+
+
 def beam_select(logits, score, k, *, offset=None, done=None, end=None):
     """(score, parent, item, done): the k best continuations of each group of beams, in descending order.  score: float32, g x b;
     logits: (g b) x v, the beams' rows one group after another (float32, bfloat16 or float16; rows may lie apart).  Beam b
@@ -213,12 +229,10 @@ def beam_select(logits, score, k, *, offset=None, done=None, end=None):
     p = Beam(g, v, _count(b, "beams"), _count(k, "k"), _DTYPES[logits.dtype], 0, logits.data_ptr(), ld, s, o, f, -1 if end is None else end)
     L, device = _lib(), logits.device
     with _On(index):
-        n = ctypes.c_int64()
-        _check(L.ccdpp_beam_workspace(ctypes.byref(p), ctypes.byref(n)))
-        ws = torch.empty(n.value, dtype=torch.uint8, device=device)
+        n = _beam_bytes(g, v, b, k, p.dtype)
+        ws = torch.empty(n, dtype=torch.uint8, device=device)
         out = torch.empty((g, k), dtype=torch.float32, device=device)
-        parent = torch.empty((g, k), dtype=torch.int64, device=device)
-        item = torch.empty((g, k), dtype=torch.int64, device=device)
+        parent, item = torch.empty((2, g, k), dtype=torch.int64, device=device).unbind()
         ended = None if end is None else torch.empty((g, k), dtype=torch.bool, device=device)
         _check(L.ccdpp_beam_select(ctypes.byref(p), out.data_ptr(), parent.data_ptr(), item.data_ptr(), None if ended is None else ended.data_ptr(),
                                    ws.data_ptr(), n, _stream(index)))
@@ -247,13 +261,14 @@ def beam_reorder(parent, states, *, beams, out=None):
             raise TypeError("states must be tensors with a row for each beam")
         if a.get_device() != index or a.shape[0] != g * beams:
             raise ValueError(f"states must have {g * beams} rows, on the device of parent")
-        row = a.numel() // max(a.shape[0], 1) * a.element_size()
+        row = a.nbytes // max(a.shape[0], 1)
         if a.is_contiguous():
             strides.append(row)
         else:
-            if not a[0].is_contiguous() or a.stride(0) * a.element_size() < row:
+            apart = a.stride(0) * a.element_size()
+            if not a[0].is_contiguous() or apart < row:
                 raise ValueError("rows of states must be contiguous")
-            strides.append(a.stride(0) * a.element_size())
+            strides.append(apart)
         sizes.append(row)
     with _On(index):
         got = [torch.empty((g * k, *a.shape[1:]), dtype=a.dtype, device=a.device) for a in states] if out is None else out
