@@ -43,7 +43,9 @@ enum ccdpp_scan_mode {
  *              ascend, results are undefined, but nothing else is read or written.)
  *   initial  : float, s rows of d, or NULL for zeros
  * States, products of decays and their gradients are held in 32 bits and rounded once to dtype.
- * A value that is not finite stays within its column and its sequence.
+ * (GIVEN decays above 1: also the product of those of any rows one after another has to lie
+ * within the range of 32 bits.)  A value that is not finite stays within its column and its
+ * sequence.
  */
 typedef struct ccdpp_scan {
     int64_t n, s;

@@ -2,6 +2,10 @@
 //
 // Beam b continued by item i has the score  s_b + z_bi - L_b,  L_b = log sum_j exp z_bj.  Within a beam the order is that of z, which is
 // exact in 32 bits: a row leaves its k greatest keys (z, then the lowest item).  Between beams scores are compared in 64 bits.
+//
+// Bound by reading the logits once where they are many: 512 rows of 624,961 floats with offsets 250 us (5.1 TB/s, a copy's rate).  Less of
+// them is bound by instructions and rounds to LDS one after another: 128 rows of 131,072 in bfloat16 23 us (14 without the selection; 6.5 would
+// be a read from the memory-side cache), then 9 for joining, most of it rounds to memory, and 4 for the states.
 #include <algorithm>
 #include <cmath>
 
@@ -14,6 +18,7 @@ namespace {
 constexpr int kMost = 64;             // beams of a group, and continuations
 constexpr int64_t kGrid = 1 << 20;    // blocks of a launch
 
+// (Taking a chunk's greatest values out one by one, up to k times a chunk, instead of comparing with a bound: 32 us for the 128 rows above.)
 constexpr int kEach = 32;             // logits of a lane in a chunk
 constexpr int kChunk = 64 * kEach;    // of a wave
 constexpr int kWaves = 4;             // of a block
@@ -160,8 +165,9 @@ struct Found {
 // lane's greatest logit so far (in 32 bits within a chunk, in 64 over them), then what may be among the k best is put aside.  Of a wave's
 // first chunk that is what is not below the k-th greatest of its lanes' greatest values; with values in any order little is found after that.
 // Where more than kAdded values pass (many equal or ascending ones), the k greatest of the chunk are taken out one by one.
+// (Registers for four waves a SIMD where a chunk of raw values takes 16.)
 template <class T, bool OFFSET>
-__global__ __launch_bounds__(64 * kWaves) void k_beam_rows(Beam a) {
+__global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 && !OFFSET ? 4 : 2) void k_beam_rows(Beam a) {
     typedef Chunk<T, OFFSET> C;
     __shared__ uint64_t keys[kWaves][kFound];
     __shared__ double sums[kWaves];
@@ -458,7 +464,9 @@ int check(const ccdpp_beam_t* p) {
     return CCDPP_OK;
 }
 
-// How a row is shared out among blocks, and where the shares' results lie in the workspace (from 0 on).
+// How a row is shared out among blocks, and where the shares' results lie in the workspace (from 0 on).  Three blocks a CU are wanted: a wave's
+// first chunk costs the most, so fewer shares are better for many rows (512 rows of 624,961 floats in one share each 250 us, in two 257, in
+// four 277), but too few leave waits bare (128 rows of 131,072 in bfloat16: 512 blocks 24.8, 768 23.4, 1,024 21.9, 256 34).
 struct Layout {
     int64_t shares, each, sums, tops, keys, bytes;
 };
@@ -466,7 +474,7 @@ struct Layout {
 Layout layout(const ccdpp_beam_t* p) {
     Layout l;
     const int64_t rows = p->groups * p->beams, chunks = (p->v + kChunk - 1) / kChunk;
-    const int64_t wanted = std::max<int64_t>(1, std::min<int64_t>(512 / std::max<int64_t>(rows, 1), 256));
+    const int64_t wanted = std::max<int64_t>(1, std::min<int64_t>(768 / std::max<int64_t>(rows, 1), 256));
     l.each = std::max<int64_t>(round_up((chunks + wanted - 1) / wanted, kWaves), kWaves);
     l.shares = (chunks + l.each - 1) / l.each;
     l.sums = 0;

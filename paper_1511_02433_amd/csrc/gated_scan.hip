@@ -2,6 +2,17 @@
 //
 //   h_t = a_t h_(t-1) + u_t;   GIVEN: a = gate, u = x;   SIGMOID: a = 1 / (1 + e^-gate), u = (1 - a) x
 //   l_t = dy_t + a_(t+1) l_(t+1);   dx_t = l_t (times 1 - a_t),  dgate_t = l_t h_(t-1)  (or l_t (h_(t-1) - x_t) a_t (1 - a_t))
+//
+// Bound by memory where there is much: rows are read once and written once.  A row's state is A h + H of the state h before a chain of
+// rows, whatever those rows are, so chains are joined: a thread takes W columns of a chunk of kRows rows into registers, the groups of a
+// block, a chunk each, pass their (A, H) on through LDS, and a block goes on by `groups` chunks at a time down a share of the rows (up,
+// for the gradients), with the next chunks' loads in flight.  Shares of a strip of columns are as many as blocks fill the device.  A
+// sequence that goes on from one share to the next has its rows there read a second time, by a launch before, for their (A, H); so
+// shares begin where a sequence does if one does nearby.  Lengths are known to the device alone: every rule here holds for any of them.
+//
+// 32,768 x 4,096 bfloat16 in 16 sequences: 182 us forward (4.5 TB/s), 302 for the gradients (4.6), of a copy's 5.13; vector
+// instructions are issued in three cycles of four (a value takes some 30 forward, 45 back).  1,000,209 x 40 floats in 6,041 sequences
+// 123 + 22 us; one sequence of 65,537 x 100 bfloat16 19 + 9, which is what the rounds to memory of a block take one after another.
 #include <algorithm>
 #include <type_traits>
 
@@ -11,7 +22,11 @@
 namespace ccdops {
 namespace {
 
-constexpr int kRows = 8;       // of a chunk; one state of a chunk is kept
+// kRows: of a chunk, of which one state is kept for the gradients (half a byte a value).  With 16 the gradients' registers leave one block
+// a CU: 416 us in place of 305 for 32,768 x 4,096 bfloat16, the histories above 153 in place of 122.
+// kThreads: with 256 a block has half the chunks side by side and twice the steps: 10,007 x 777 half precision, both ways, 105 us in
+// place of 91, the long sequence 34 in place of 29, 32,768 x 4,096 the same (499 and 497).
+constexpr int kRows = 8;
 constexpr int kThreads = 512;  // of a block
 constexpr int kLanes = 64;     // of a group, at most
 
@@ -98,6 +113,7 @@ struct Share {
 };
 // kRows rows of a chunk: the sequence of the first one (-1 or s: none), and a bit for each row that begins a sequence (or the rows
 // behind all), bit kRows for the row after the chunk.  kSkips: sequences without rows begin in it, too; of_row says which begin there.
+constexpr uint32_t kSkips = 1u << 31;
 struct Chunk {
     int32_t q;
     uint32_t begins;
@@ -139,8 +155,7 @@ __device__ int64_t find_start(const Scan& a, int64_t row) {
     return lo;
 }
 
-// Share p begins at row p * rows, or where a sequence does if that is near: what goes on from one
-// share to the next costs a second pass over its rows.
+// Share p begins at row p * rows, or where a sequence does if that is near (3 / 8 of a share: shares stay a quarter of one at least).
 __device__ Share share_of(const Scan& a, int64_t p) {
     if (p <= 0) return {0, 0, 0, -1};
     if (p >= a.shares) return {a.n, 0, 0, -1};
@@ -154,7 +169,6 @@ __device__ Share share_of(const Scan& a, int64_t p) {
 
 // What a chain of rows does to the state before it: A state + H; where a sequence begins in it the state behind it is H, whatever
 // was before (A is kReset then, a bit pattern that no product has: products have no signalling NaN).
-constexpr uint32_t kSkips = 1u << 31;
 constexpr uint32_t kReset = 0x7F800001u;
 
 // A thread's place: `lanes` lanes side by side take the columns of a strip, W each, and `groups` of them a chunk each, one after
@@ -208,10 +222,10 @@ __device__ __forceinline__ void leave(Exchange<W>& e, const Scan& a, const Place
         for (int w = 0; w < W; ++w) e.behind[(step + 1) & 1][at.lane][w] = h[w];
 }
 
-// The same over all groups: c goes in as the state before them and out as that behind.
+// The same over all groups: c goes in as the state before them and out as that behind; `all` takes the product of their A.
 template <int W>
 __device__ __forceinline__ void join_all(const Scan& a, Exchange<W>& e, const Place<W>& at, int step, const float (&A)[W], const float (&H)[W], bool reset,
-                                         float (&c)[W]) {
+                                         float (&c)[W], float (&all)[W]) {
     typename Exchange<W>::Link* const of = e.of[step & 1];
     typename Exchange<W>::Link own;
 #pragma unroll
@@ -223,11 +237,11 @@ __device__ __forceinline__ void join_all(const Scan& a, Exchange<W>& e, const Pl
         const typename Exchange<W>::Link one = of[g * a.lanes + at.lane];
         const bool begins = __float_as_uint(one.A[0]) == kReset;
 #pragma unroll
-        for (int w = 0; w < W; ++w) c[w] = begins ? one.H[w] : fmaf(one.A[w], c[w], one.H[w]);
+        for (int w = 0; w < W; ++w) c[w] = begins ? one.H[w] : fmaf(one.A[w], c[w], one.H[w]), all[w] *= one.A[w];
     }
 }
 
-// The address of the next row from that of this one: sixteen multiples of every stride at once would not stay in registers.
+// The address of the next row from that of this one: eight multiples of every stride at once would not stay in registers.
 template <class T>
 __device__ __forceinline__ void next(T*& at, int64_t ld) {
     at += ld;
@@ -347,15 +361,7 @@ __global__ __launch_bounds__(kThreads) void k_scan_first(Scan a) {
                     ph[w] = GRAD ? d[i][w] * (u[i][w] + ph[w]) : fmaf(d[i][w], ph[w], u[i][w]);
                 }
             }
-            float all[W];
-#pragma unroll
-            for (int w = 0; w < W; ++w) all[w] = 1.f;
-            join_all<W>(a, e, at, (int)step, pa, ph, false, C);
-            for (int g = 0; g < a.groups; ++g)
-#pragma unroll
-                for (int w = 0; w < W; ++w) all[w] *= e.of[step & 1][g * a.lanes + at.lane].A[w];
-#pragma unroll
-            for (int w = 0; w < W; ++w) A[w] *= all[w];
+            join_all<W>(a, e, at, (int)step, pa, ph, false, C, A);
         }
         if (at.group == 0) {
             float* out = a.carry + ((int64_t)p * a.d + at.col) * 2;
@@ -455,10 +461,12 @@ __device__ void carry_in(const Scan& a, Exchange<W>& e, const Place<W>& at, int 
                 }
         }
     }
-    join_all<W>(a, e, at, 0, A, H, at.works && from == 0 && to > 0, c);
+    float all[W] = {};
+    join_all<W>(a, e, at, 0, A, H, at.works && from == 0 && to > 0, c, all);
     __syncthreads();
 }
 
+// A chunk whose rows are all of one sequence, and neither its first nor its last, takes the plain way; the other does each row by what it is.
 template <class T, int W, bool SIGMOID>
 __global__ __launch_bounds__(kThreads) void k_scan(Scan a) {
     __shared__ Exchange<W> e;
@@ -558,6 +566,8 @@ __global__ __launch_bounds__(kThreads) void k_scan(Scan a) {
     }
 }
 
+// Up the rows.  Each chunk's states are computed once more from the one that was kept, which gives what l is multiplied by for dgate; then
+// l goes through it as the state does forward, from the last row to the first.
 template <class T, int W, bool SIGMOID>
 __global__ __launch_bounds__(kThreads) void k_scan_grad(Scan a) {
     __shared__ Exchange<W> e;
@@ -698,7 +708,8 @@ __global__ __launch_bounds__(kThreads) void k_scan_grad(Scan a) {
     }
 }
 
-// A thread takes eight columns of a row.
+// A thread takes eight columns of a row.  Bound by memory, or by the call where there is little: 512 x 4,096 bfloat16 6.8 us (one column a
+// thread 8.0), 64 x 40 floats 2.6.
 constexpr int kStepColumns = 8;
 template <class T, bool SIGMOID>
 __global__ __launch_bounds__(256) void k_step(int64_t n, int d, const T* x, int64_t ldx, const T* gate, int64_t ldg, float* state, int64_t lds, T* y,
@@ -761,11 +772,19 @@ struct Layout {
     int64_t share, chunk, of_row, carry, bytes;
 };
 
-constexpr int64_t kLeastBlocks = 512, kMostBlocks = 512;
+// Blocks of a launch: two of 512 threads a CU are at work at once.  (Histories of 1,000,209 x 40 floats: 1,024 blocks 116 + 32 us in place of
+// 122 + 24, as more sequences go on from share to share; 256 132 + 27.  10,007 x 777 half precision, both ways: 256 blocks 102 in place of 91.)
+constexpr int64_t kBlocks = 512;
+// Bytes of a row that the lanes of a group take at least: with 128, 32,768 x 4,096 bfloat16 takes 203 us forward in place of 187, and 390 in
+// place of 332 for the gradients.
+constexpr int kPiece = 256;
+// Values from which on the gradients take two columns a thread: 305 us in place of 326 for 32,768 x 4,096 bfloat16, where their instructions
+// bound them; one column leaves registers for twice the waves, which wait less: 35 in place of 41 for 10,007 x 777 half precision.
+constexpr int64_t kMuch = 1 << 25;
 
-Layout layout(const ccdpp_scan_t* p) {
+Layout layout(const ccdpp_scan_t* p, int32_t call) {
     Layout l;
-    l.width = p->d >= 2 ? 2 : 1;
+    l.width = p->d >= 2 && (call == CCDPP_SCAN_FORWARD || p->n * p->d >= kMuch) ? 2 : 1;
     const int lanes = (p->d + l.width - 1) / l.width;
     l.chunks = (p->n + kRows - 1) / kRows;
     int64_t shares = 1;
@@ -773,10 +792,8 @@ Layout layout(const ccdpp_scan_t* p) {
         l.strips = (lanes + widest - 1) / widest;
         l.lanes = (lanes + l.strips - 1) / l.strips;
         l.groups = std::min(kThreads / l.lanes, 64);
-        const int64_t most = std::max<int64_t>(1, kMostBlocks / l.strips), least = std::max<int64_t>(1, kLeastBlocks / l.strips);
-        shares = std::min(std::max(p->s, least), most);
-        shares = std::max<int64_t>(1, std::min(shares, l.chunks / l.groups));
-        if (l.strips * shares >= kMostBlocks || widest * l.width * (p->dtype == CCDPP_F32 ? 4 : 2) <= 256) break;
+        shares = std::max<int64_t>(1, std::min(kBlocks / l.strips, l.chunks / l.groups));
+        if (l.strips * shares >= kBlocks || widest * l.width * (p->dtype == CCDPP_F32 ? 4 : 2) <= kPiece) break;
     }
     l.rows = round_up((std::max<int64_t>(p->n, 1) + shares - 1) / shares, kRows);
     l.shares = (int)((std::max<int64_t>(p->n, 1) + l.rows - 1) / l.rows);
@@ -788,7 +805,7 @@ Layout layout(const ccdpp_scan_t* p) {
     return l;
 }
 
-int64_t workspace(const ccdpp_scan_t* p, int32_t) { return layout(p).bytes; }
+int64_t workspace(const ccdpp_scan_t* p, int32_t call) { return layout(p, call).bytes; }
 
 void set(Scan& a, const ccdpp_scan_t* p, const Layout& l, void* ws) {
     a.n = p->n, a.s = p->s, a.ldx = p->ldx, a.ldg = p->ldg, a.d = p->d, a.bits = p->starts_bits;
@@ -852,7 +869,7 @@ int ccdpp_gated_scan(const ccdpp_scan_t* p, void* y, int64_t ldy, float* last, v
     if (ldy < p->d) return fail(CCDPP_EINVAL, "ldy must be at least d");
     if (misaligned(y, p->dtype == CCDPP_F32 ? 4 : 2) || misaligned(last, 4)) return fail(CCDPP_EINVAL, "pointers must be aligned to their types");
     if (int rc = check_device()) return rc;
-    const Layout l = layout(p);
+    const Layout l = layout(p, CCDPP_SCAN_FORWARD);
     Scan a = {};
     set(a, p, l, ws);
     a.y = y, a.ldy = ldy, a.last = last, a.keep = (float*)kept;
@@ -870,7 +887,7 @@ int ccdpp_gated_scan_grad(const ccdpp_scan_t* p, const void* dy, int64_t lddy, c
     if (misaligned(dy, es) || misaligned(dx, es) || misaligned(dgate, es) || misaligned(dlast, 4) || misaligned(dinitial, 4))
         return fail(CCDPP_EINVAL, "pointers must be aligned to their types");
     if (int rc = check_device()) return rc;
-    const Layout l = layout(p);
+    const Layout l = layout(p, CCDPP_SCAN_GRAD);
     Scan a = {};
     set(a, p, l, ws);
     a.y = const_cast<void*>(dy), a.ldy = lddy, a.dlast = dlast, a.kept = (const float*)kept;

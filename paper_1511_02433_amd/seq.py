@@ -126,7 +126,8 @@ def _scan_workspace(p, call, device):
 
 def gated_scan(x, gate, *, starts, initial=None, mode="sigmoid", keep=False, y=None):
     """(y, last), or (y, last, kept) with `keep`: h_t = a_t h_(t-1) + u_t along each sequence of rows, every column by itself.
-    mode 'sigmoid': a = sigmoid(gate), u = (1 - a) x; 'given': a = gate, u = x.  x, gate: n x d (float32, bfloat16 or float16;
+    mode 'sigmoid': a = sigmoid(gate), u = (1 - a) x; 'given': a = gate, u = x (decays above 1 as long as products of any that follow
+    one another stay within float32's range).  x, gate: n x d (float32, bfloat16 or float16;
     rows may lie apart).  starts: s + 1 ascending int32 or int64 values: sequence q has rows starts[q] to starts[q + 1] - 1; rows
     outside of all are not read and 0 in y.  initial: float32, s x d, the states before the sequences' first rows, or None for
     zeros.  y has x's type (or may be given to write to); last: float32, s x d, the states behind the last rows; kept: what

@@ -153,6 +153,53 @@ def test_long(n, d, s, mode):
     close(di, wi, ei, "dinitial")
 
 
+@pytest.mark.parametrize("seed", range(24))
+def test_random_problems(seed):
+    """Sizes, types, layouts and lengths at random: sequences by a power law, some without rows, rows before and behind them."""
+    rng = np.random.default_rng(1000 + seed)
+    n, s = int(2 ** rng.uniform(3, 13.5)), int(2 ** rng.uniform(0, 8))
+    d = int(2 ** rng.uniform(0, 9 if n < 2000 else 5.5))
+    dtype, mode = ("f32", "bf16", "f16")[seed % 3], ("sigmoid", "given")[seed % 2]
+    share = (rng.random(s) + 0.01) ** -1.5 * (rng.random(s) > 0.1)
+    share[rng.integers(s)] += 1e-9
+    L = np.floor(share / share.sum() * n).astype(np.int64)
+    lead, behind = int(rng.integers(0, 40)) * (seed % 4 == 0), int(rng.integers(0, 400)) * (seed % 4 == 1)
+    starts = np.concatenate([[0], np.cumsum(L)]) + lead
+    n = int(starts[-1]) + behind
+    gen = torch.Generator().manual_seed(seed)
+    pad = int(rng.integers(0, 4))
+
+    def rows(f):
+        return f(torch.randn(n, d + pad, generator=gen)).to(DT[dtype]).cuda()[:, :d]
+
+    x, dy = rows(lambda a: a), rows(lambda a: a)
+    gate = rows(lambda a: a * 2 + 2 if mode == "sigmoid" else torch.sigmoid(a * 2 + 2))
+    first = torch.randn(s, d, generator=gen).cuda() if rng.random() < 0.6 else None
+    dl = torch.randn(s, d, generator=gen).cuda() if rng.random() < 0.6 else None
+    at = torch.from_numpy(starts).cuda().to(torch.int32 if seed % 5 == 0 else torch.int64)
+    y, last, kept = seq().gated_scan(x, gate, starts=at, initial=first, mode=mode, keep=True)
+    dx, dg, di = seq().gated_scan_grad(x, gate, dy, kept, starts=at, initial=first, mode=mode, dlast=dl)
+    I, D = None if first is None else to64(first), None if dl is None else to64(dl)
+    wy, wl, before, ey, el, eb = forward(to64(x), to64(gate), starts, I, mode)
+    close(y, wy, ey, "y")
+    close(last, wl, el, "last")
+    wx, wg, wi, ex, eg, ei = backward(to64(x), to64(gate), to64(dy), D, starts, before, eb, mode)
+    close(dx, wx, ex, "dx")
+    close(dg, wg, eg, "dgate")
+    if first is not None:
+        close(di, wi, ei, "dinitial")
+
+
+@pytest.mark.parametrize("n", [0, 1, 700])
+def test_rows_without_any_sequence(n):
+    x, at = torch.full((n, 9), float("nan"), device="cuda"), torch.tensor([min(n, 3)], device="cuda")
+    y, last, kept = seq().gated_scan(x, x, starts=at, keep=True)
+    dx, dg, di = seq().gated_scan_grad(x, x, x, kept, starts=at, initial=torch.empty(0, 9, device="cuda"))
+    assert last.shape == di.shape == (0, 9)
+    for a in (y, dx, dg):
+        assert torch.equal(a, torch.zeros(n, 9, device="cuda"))
+
+
 @pytest.mark.parametrize("mode", ["sigmoid", "given"])
 def test_gradients_against_differences(mode):
     """Central differences of the sum in 64 bits: what they leave out is of the order of 1e-8 of the terms here, and they round
