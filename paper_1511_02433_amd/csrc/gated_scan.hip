@@ -308,65 +308,63 @@ __global__ __launch_bounds__(kThreads) void k_scan_first(Scan a) {
         if (edge.q < 0) return;
         const int64_t lo = GRAD ? at_begin.begin : max(at_begin.begin, edge.prev), hi = GRAD ? min(at_end.begin, edge.next) : at_end.begin;
         const Place<W> at(a, strip);
-        const int64_t c0 = lo / kRows, c1 = (hi + kRows - 1) / kRows;
-        float A[W], C[W];  // of all rows so far
-#pragma unroll
-        for (int w = 0; w < W; ++w) A[w] = 1.f, C[w] = 0.f;
+        // A group takes `per` chunks one after another, so that the groups join once.
+        const int64_t c0 = lo / kRows, c1 = (hi + kRows - 1) / kRows, per = (c1 - c0 + a.groups - 1) / a.groups;
+        const int64_t from = at.group * per, to = at.works ? min(from + per, c1 - c0) : 0;
         Rows<T, W> x, gate;  // x: dy for the gradients
-        const auto chunk_of = [&](int64_t step) { return GRAD ? c1 - 1 - step * a.groups - at.group : c0 + step * a.groups + at.group; };
-        const auto load = [&](int64_t step) {
-            const int64_t c = chunk_of(step);
-            if (!at.works || c < c0 || c >= c1) return;
-            gate.load(a.gate, a.ldg, c * kRows, a.n, at.col);
-            if (GRAD) x.load(a.y, a.ldy, c * kRows, a.n, at.col);
-            else x.load(a.x, a.ldx, c * kRows, a.n, at.col);
+        const auto chunk_of = [&](int64_t i) { return GRAD ? c1 - 1 - i : c0 + i; };
+        const auto load = [&](int64_t i) {
+            if (i >= to) return;
+            gate.load(a.gate, a.ldg, chunk_of(i) * kRows, a.n, at.col);
+            if (GRAD) x.load(a.y, a.ldy, chunk_of(i) * kRows, a.n, at.col);
+            else x.load(a.x, a.ldx, chunk_of(i) * kRows, a.n, at.col);
         };
-        float first[W];  // the state before a sequence's first row, or behind its last one
+        load(from);
+        float first[W], A[W], H[W], C[W], all[W];  // first: the state before a sequence's first row, or behind its last one
         const bool ends = GRAD ? edge.next <= at_end.begin : edge.prev >= at_begin.begin;
-        const float* from = GRAD ? a.dlast : a.initial;
+        const float* states = GRAD ? a.dlast : a.initial;
 #pragma unroll
-        for (int w = 0; w < W; ++w) first[w] = ends && from ? from[edge.q * a.d + at.col + w] : 0.f;
-        load(0);
-        const int64_t steps = (c1 - c0 + a.groups - 1) / a.groups;
-        for (int64_t step = 0; step < steps; ++step) {
-            const int64_t c = chunk_of(step);
-            const uint32_t in = at.works && c >= c0 && c < c1 ? rows_within(c * kRows, lo, hi) : 0u;
+        for (int w = 0; w < W; ++w) {
+            first[w] = ends && states ? states[edge.q * a.d + at.col + w] : 0.f;
+            A[w] = all[w] = 1.f, H[w] = C[w] = 0.f;
+        }
+        for (int64_t i = from; i < to; ++i) {
+            const int64_t row = chunk_of(i) * kRows;
+            const uint32_t in = rows_within(row, lo, hi);
             float d[kRows][W], u[kRows][W];
 #pragma unroll
-            for (int i = 0; i < kRows; ++i)
+            for (int k = 0; k < kRows; ++k)
 #pragma unroll
                 for (int w = 0; w < W; ++w) {
-                    const Terms m = terms_of<SIGMOID && !GRAD>(x.v[i].get(w), gate.v[i].get(w));
-                    d[i][w] = GRAD && SIGMOID ? sigmoid_of(gate.v[i].get(w)).a : m.a, u[i][w] = m.u;
+                    const Terms m = terms_of<SIGMOID && !GRAD>(x.v[k].get(w), gate.v[k].get(w));
+                    d[k][w] = GRAD && SIGMOID ? sigmoid_of(gate.v[k].get(w)).a : m.a, u[k][w] = m.u;
                 }
+            load(i + 1);
             if (in != kAll) {
 #pragma unroll
-                for (int i = 0; i < kRows; ++i)
+                for (int k = 0; k < kRows; ++k)
 #pragma unroll
                     for (int w = 0; w < W; ++w)
-                        if (!(in >> i & 1)) d[i][w] = 1.f, u[i][w] = 0.f;
+                        if (!(in >> k & 1)) d[k][w] = 1.f, u[k][w] = 0.f;
             }
-            load(step + 1);
-            float pa[W], ph[W];
-            // (The state that comes in at lo, or at hi - 1, is put into that row: nothing comes before it.)
-            const int64_t mark = in ? (GRAD ? hi - 1 : lo) - c * kRows : -1;
+            // (The state that comes in at lo, or at hi - 1, is put in before the chunk: the chunk's rows before it are none.)
+            if (GRAD ? hi - 1 - row < kRows && hi > row : lo >= row)
 #pragma unroll
-            for (int w = 0; w < W; ++w) {
-                pa[w] = 1.f, ph[w] = 0.f;
+                for (int w = 0; w < W; ++w) H[w] = first[w];
 #pragma unroll
-                for (int k = 0; k < kRows; ++k) {
-                    const int i = GRAD ? kRows - 1 - k : k;
-                    if (i == mark) ph[w] = first[w];
-                    pa[w] *= d[i][w];
-                    ph[w] = GRAD ? d[i][w] * (u[i][w] + ph[w]) : fmaf(d[i][w], ph[w], u[i][w]);
+            for (int k = 0; k < kRows; ++k)
+#pragma unroll
+                for (int w = 0; w < W; ++w) {
+                    const int r = GRAD ? kRows - 1 - k : k;
+                    A[w] *= d[r][w];
+                    H[w] = GRAD ? d[r][w] * (u[r][w] + H[w]) : fmaf(d[r][w], H[w], u[r][w]);
                 }
-            }
-            join_all<W>(a, e, at, (int)step, pa, ph, false, C, A);
         }
+        join_all<W>(a, e, at, 0, A, H, false, C, all);
         if (at.group == 0) {
             float* out = a.carry + ((int64_t)p * a.d + at.col) * 2;
 #pragma unroll
-            for (int w = 0; w < W; ++w) out[2 * w] = A[w], out[2 * w + 1] = C[w];
+            for (int w = 0; w < W; ++w) out[2 * w] = all[w], out[2 * w + 1] = C[w];
         }
         return;
     }
