@@ -164,7 +164,8 @@ struct Found {
 // One block for each share of a row.  Its waves take chunks in turn; a chunk is read once: its exponentials are added up relative to the
 // lane's greatest logit so far (in 32 bits within a chunk, in 64 over them), then what may be among the k best is put aside.  Of a wave's
 // first chunk that is what is not below the k-th greatest of its lanes' greatest values; with values in any order little is found after that.
-// Where more than kAdded values pass (many equal or ascending ones), the k greatest of the chunk are taken out one by one.
+// Where more than kAdded values pass, a bound is looked for that at least k and no more than kAdded pass; where there is none (many equal
+// ones), the k greatest of the chunk are taken out one by one.
 // (Registers for four waves a SIMD where a chunk of raw values takes 16.)
 template <class T, bool OFFSET>
 __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 && !OFFSET ? 4 : 2) void k_beam_rows(Beam a) {
@@ -241,6 +242,22 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 && !OFFSET ? 4 : 2) voi
                 passing = 0;
 #pragma unroll
                 for (int e = 0; e < kEach; ++e) passing += __popcll(__ballot(z[e] >= bound));
+            }
+            if (passing > kAdded) {  // (halving what lies between the bound and the greatest value, up to 32 times)
+                uint32_t low = order_of(bound + 0.f), high = order_of(wave_max(m) + 0.f) + 1;  // too many are not below low, none not below high
+                while (high - low > 1) {
+                    const uint32_t mid = low + (high - low) / 2;
+                    const float v = value_of(mid);
+                    int n = 0;
+#pragma unroll
+                    for (int e = 0; e < kEach; ++e) n += __popcll(__ballot(z[e] >= v));
+                    if (n > kAdded) low = mid;
+                    else if (n < a.k) high = mid;
+                    else {
+                        bound = raised = v, passing = n;
+                        break;
+                    }
+                }
             }
             if (found.n + min(passing, kAdded) > kFound) found.prune(a.k);
             if (passing <= kAdded) {
@@ -542,6 +559,7 @@ int ccdpp_beam_reorder(int64_t groups, int32_t beams, int32_t k, const int64_t* 
     for (int32_t i = 0; i < n; ++i) {
         if (row_bytes[i] < 0 || in_stride[i] < row_bytes[i]) return fail(CCDPP_EINVAL, "row_bytes must be >= 0, and rows no less apart");
         if (groups > 0 && row_bytes[i] > 0 && (!in[i] || !out[i])) return fail(CCDPP_EINVAL, "a tensor is NULL");
+        if (groups > 0 && row_bytes[i] > 0 && in[i] == out[i]) return fail(CCDPP_EINVAL, "an output must not be an input");
     }
     if (int rc = check_device()) return rc;
     if (groups == 0) return CCDPP_OK;

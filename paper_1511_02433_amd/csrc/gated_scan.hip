@@ -370,11 +370,8 @@ __global__ __launch_bounds__(kThreads) void k_scan_first(Scan a) {
     }
     block -= a.sums;
     if (block < a.tables) {
-        const int64_t c = block * (int64_t)blockDim.x + threadIdx.x;
-        if (c >= a.chunks) return;
-        // The first start from `row` on.
-        const auto find = [&](int64_t row, int64_t lo) {
-            int64_t hi = a.s + 1;
+        // The first start from `row` on, in [lo, hi].
+        const auto find = [&](int64_t row, int64_t lo, int64_t hi) {
             while (lo < hi) {
                 const int64_t mid = (lo + hi) / 2;
                 if (start_of(a, mid) < row) lo = mid + 1;
@@ -382,8 +379,11 @@ __global__ __launch_bounds__(kThreads) void k_scan_first(Scan a) {
             }
             return lo;
         };
-        const int64_t row = c * kRows;
-        int64_t j = find(row, 0), r = -1;
+        // A wave looks for its first chunk's row together, and each lane for its own among the next 64 starts, where they go that far.
+        const int64_t c = block * (int64_t)blockDim.x + threadIdx.x, row = c * kRows, row0 = (c - (threadIdx.x & 63)) * kRows;
+        const int64_t j0 = find_start(a, row0), near = min(j0 + 64, a.s + 1);
+        if (c >= a.chunks) return;
+        int64_t j = find(row, j0, near > a.s || start_of(a, near) >= row0 + 64 * kRows ? near : a.s + 1), r = -1;
         Chunk k = {(int32_t)(j - 1), 0u};
         int64_t q = j - 1;  // the last sequence so far
         while (j <= a.s) {
@@ -391,7 +391,7 @@ __global__ __launch_bounds__(kThreads) void k_scan_first(Scan a) {
             if (begin < row || begin > row + kRows || begin <= r) break;
             r = begin;
             const bool more = j < a.s && start_of(a, j + 1) == r;  // sequences without rows begin there, too
-            j = more ? find(r + 1, j + 1) : j + 1;
+            j = more ? find(r + 1, j + 1, a.s + 1) : j + 1;
             k.begins |= 1u << (r - row);
             if (r == row) k.q = (int32_t)(j - 1), q = j - 1;
             else if (j - 1 != ++q) k.begins |= kSkips, q = j - 1;
@@ -865,6 +865,7 @@ int ccdpp_gated_scan(const ccdpp_scan_t* p, void* y, int64_t ldy, float* last, v
     if (int rc = check_pointers(p, kept, ws, ws_bytes, workspace(p, CCDPP_SCAN_FORWARD))) return rc;
     if (p->n > 0 && !y) return fail(CCDPP_EINVAL, "y must be non-NULL");
     if (ldy < p->d) return fail(CCDPP_EINVAL, "ldy must be at least d");
+    if (p->n > 0 && (y == p->x || y == p->gate)) return fail(CCDPP_EINVAL, "an output must not be an input");
     if (misaligned(y, p->dtype == CCDPP_F32 ? 4 : 2) || misaligned(last, 4)) return fail(CCDPP_EINVAL, "pointers must be aligned to their types");
     if (int rc = check_device()) return rc;
     const Layout l = layout(p, CCDPP_SCAN_FORWARD);
@@ -881,6 +882,8 @@ int ccdpp_gated_scan_grad(const ccdpp_scan_t* p, const void* dy, int64_t lddy, c
     if (int rc = check_pointers(p, kept, ws, ws_bytes, workspace(p, CCDPP_SCAN_GRAD))) return rc;
     if (p->n > 0 && (!dy || !kept || !dx || !dgate)) return fail(CCDPP_EINVAL, "dy, kept, dx and dgate must be non-NULL");
     if (lddy < p->d || lddx < p->d || lddg < p->d) return fail(CCDPP_EINVAL, "lddy, lddx and lddg must be at least d");
+    if (p->n > 0 && (dx == p->x || dx == p->gate || dx == dy || dgate == p->x || dgate == p->gate || dgate == dy || dx == dgate))
+        return fail(CCDPP_EINVAL, "an output must not be an input");
     const uintptr_t es = p->dtype == CCDPP_F32 ? 4 : 2;
     if (misaligned(dy, es) || misaligned(dx, es) || misaligned(dgate, es) || misaligned(dlast, 4) || misaligned(dinitial, 4))
         return fail(CCDPP_EINVAL, "pointers must be aligned to their types");

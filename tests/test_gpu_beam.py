@@ -151,6 +151,25 @@ def test_what_is_not_finite():
     check(logits, score, 5)
 
 
+@pytest.mark.parametrize("score", [math.inf, 3.0e38, -3.0e38])
+def test_scores_at_the_ends_of_their_range(score):
+    _, logits, s = make(2, 3, 700, "f32", 4)
+    s[0, 1] = score
+    s[1] = score
+    check(logits, s, 7)
+
+
+@pytest.mark.parametrize("k", [1, 8, 64])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_many_large_values_side_by_side(k, dtype):
+    """A run of items far above the others, more than are put aside at a time, some of them equal."""
+    gen, logits, score = make(1, 2, 20_000, dtype, k)
+    logits[0, 4000:6500] += 30
+    logits[1, 9000:9300] = 25.0
+    logits[1, 15_000:15_100] = 26.0
+    check(logits, score, k)
+
+
 @pytest.mark.parametrize("low", [-1e30, -1e38, -3.0e38])
 def test_masks_of_very_low_values_are_not_exclusions(low):
     """A mask that is finite takes part where nothing else is left."""

@@ -287,6 +287,45 @@ def test_given_outputs_are_written_with_their_strides():
         assert bool((a[:, :5] == 7).all()) and bool((a[:, 26:] == 7).all())
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_rows_aligned_to_their_type_alone(dtype):
+    n, starts, gen, rows = problem("around", 37, dtype, 4, pad=6)
+    x, gate, dy = rows(lambda a: a), rows(lambda a: a), rows(lambda a: a)
+    at = torch.from_numpy(starts).cuda()
+    y, last, kept = seq().gated_scan(x, gate, starts=at, keep=True)
+    want = (y, last) + seq().gated_scan_grad(x, gate, dy, kept, starts=at)[:2]
+
+    def moved(a):
+        wide = torch.zeros(n, 50, dtype=a.dtype, device="cuda")
+        wide[:, 1:38] = a
+        return wide[:, 1:38]
+
+    y, last, kept = seq().gated_scan(moved(x), moved(gate), starts=at, keep=True, y=moved(x))
+    got = (y, last) + seq().gated_scan_grad(moved(x), moved(gate), moved(dy), kept, starts=at, dx=moved(x), dgate=moved(x))[:2]
+    for a, b in zip(want, got):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("n, empties", [(5000, 400), (3000, 3000), (70_000, 9000)])
+def test_many_sequences_without_rows_and_short_ones(n, empties):
+    """Starts that lie close together and far apart in the same tables: sequences of one row, and runs of none, at random places."""
+    rng = np.random.default_rng(n)
+    at = np.sort(np.concatenate([rng.integers(0, n + 1, empties // 2), rng.integers(n // 3, n // 3 + 20, empties // 2), [0, n]]))
+    s, d = len(at) - 1, 3
+    gen = torch.Generator().manual_seed(n)
+    x, gate = torch.randn(n, d, generator=gen).cuda(), torch.randn(n, d, generator=gen).cuda()
+    first = torch.randn(s, d, generator=gen).cuda()
+    y, last, kept = seq().gated_scan(x, gate, starts=torch.from_numpy(at).cuda(), initial=first, keep=True)
+    dx, dg, di = seq().gated_scan_grad(x, gate, x, kept, starts=torch.from_numpy(at).cuda(), initial=first, dlast=first)
+    wy, wl, before, ey, el, eb = forward(to64(x), to64(gate), at, to64(first), "sigmoid")
+    close(y, wy, ey, "y")
+    close(last, wl, el, "last")
+    wx, wg, wi, ex, eg, ei = backward(to64(x), to64(gate), to64(x), to64(first), at, before, eb, "sigmoid")
+    close(dx, wx, ex, "dx")
+    close(dg, wg, eg, "dgate")
+    close(di, wi, ei, "dinitial")
+
+
 def test_offsets_beyond_32_bits():
     """Rows more than 2^31 values apart."""
     d, ld = 40, (1 << 31) + 64

@@ -73,10 +73,10 @@ def test_scan_refuses_bad_calls():
         assert L.ccdpp_scan_workspace(B(scan()), call, B(n)) == 0
         need[call] = n.value
     for args, msg in (((None, 8, 256, 256, 256, 1 << 40), "y must"), ((256, 7, 256, 256, 256, 1 << 40), "ldy"), ((258, 8, 256, 256, 256, 1 << 40), "aligned"),
-                      ((256, 8, 258, 256, 256, 1 << 40), "aligned"), ((256, 8, 256, 264, 256, 1 << 40), "aligned"), ((256, 8, 256, 256, None, 1 << 40), "workspace"),
-                      ((256, 8, 256, 256, 264, 1 << 40), "workspace"), ((256, 8, 256, 256, 256, need[0] - 1), "workspace")):
+                      ((512, 8, 258, 256, 256, 1 << 40), "aligned"), ((512, 8, 256, 264, 256, 1 << 40), "aligned"), ((512, 8, 256, 256, None, 1 << 40), "workspace"),
+                      ((512, 8, 256, 256, 264, 1 << 40), "workspace"), ((512, 8, 256, 256, 256, need[0] - 1), "workspace")):
         assert L.ccdpp_gated_scan(B(scan()), *args, None) == E and said(L, msg), args
-    good = [256, 8, 256, 256, 256, 8, 256, 8, 256, 256, 1 << 40]
+    good = [768, 8, 256, 256, 1024, 8, 1280, 8, 256, 256, 1 << 40]
     for at, value, msg in ((0, None, "non-NULL"), (1, 7, "lddy"), (2, 258, "aligned"), (3, None, "non-NULL"), (3, 264, "aligned"), (4, None, "non-NULL"), (4, 258, "aligned"),
                            (5, 7, "lddx"), (6, None, "non-NULL"), (7, 7, "lddg"), (8, 258, "aligned"), (9, None, "workspace"), (10, need[1] - 1, "workspace")):
         args = list(good)
@@ -88,6 +88,19 @@ def test_scan_refuses_bad_calls():
         args = list(good)
         args[at] = value
         assert L.ccdpp_gated_scan_step(*args, None) == E and said(L, msg), (at, value)
+
+
+def test_outputs_that_are_inputs_are_refused():
+    """The same pointer; other overlaps are the caller's to avoid.  (Dropout and the step may write in place.)"""
+    L = _lib_or_skip()
+    p = scan(x=256, gate=512, starts=1024)
+    W = (2048, 1 << 40, None)
+    for y in (256, 512):
+        assert L.ccdpp_gated_scan(B(p), y, 8, 4096, None, *W) == E and said(L, "must not be an input")
+    for dx, dg in ((256, 8192), (512, 8192), (4096, 8192), (8192, 256), (8192, 512), (8192, 4096), (8192, 8192)):
+        assert L.ccdpp_gated_scan_grad(B(p), 4096, 8, None, 16384, dx, 8, dg, 8, None, *W) == E and said(L, "must not be an input"), (dx, dg)
+    one, sz = (ctypes.c_void_p * 1)(256), (ctypes.c_int64 * 1)(8)
+    assert L.ccdpp_beam_reorder(2, 3, 4, 256, 1, one, sz, one, sz, None) == E and said(L, "must not be an input")
 
 
 def test_kept_states_and_workspaces_are_small():
@@ -131,8 +144,8 @@ def test_beam_refuses_bad_calls():
                           (dict(), (256, 256, 256, None, None, 1 << 40), "workspace"), (dict(), (256, 256, 256, None, 264, 1 << 40), "workspace"),
                           (dict(), (256, 256, 256, None, 256, n.value - 1), "workspace")):
         assert L.ccdpp_beam_select(B(beam(**kw)), *args, None) == E and said(L, msg), (kw, args)
-    one, sz = (ctypes.c_void_p * 1)(256), (ctypes.c_int64 * 1)(8)
-    good = [2, 3, 4, 256, 1, one, sz, one, sz]
+    one, two, sz = (ctypes.c_void_p * 1)(256), (ctypes.c_void_p * 1)(512), (ctypes.c_int64 * 1)(8)
+    good = [2, 3, 4, 256, 1, one, sz, two, sz]
     for at, value, msg in ((0, -1, "groups"), (1, 0, "beams"), (1, 65, "beams"), (2, 0, "beams"), (2, 65, "beams"), (3, None, "parent"), (3, 260, "parent"), (4, -1, "n must"),
                            (5, None, "tables"), (6, None, "tables"), (7, None, "tables"), (8, None, "tables"), (5, (ctypes.c_void_p * 1)(None), "NULL"),
                            (7, (ctypes.c_void_p * 1)(None), "NULL"), (6, (ctypes.c_int64 * 1)(7), "row_bytes"), (8, (ctypes.c_int64 * 1)(-1), "row_bytes")):
@@ -159,12 +172,12 @@ def test_without_a_device_calls_report_edevice():
     if torch.cuda.is_available():
         pytest.skip("a GPU is present")
     D = C.CCDPP_EDEVICE
-    assert L.ccdpp_gated_scan(B(scan()), 256, 8, 256, 256, 256, 1 << 40, None) == D
-    assert L.ccdpp_gated_scan_grad(B(scan()), 256, 8, 256, 256, 256, 8, 256, 8, 256, 256, 1 << 40, None) == D
+    assert L.ccdpp_gated_scan(B(scan()), 512, 8, 256, 256, 256, 1 << 40, None) == D
+    assert L.ccdpp_gated_scan_grad(B(scan()), 768, 8, 256, 256, 1024, 8, 1280, 8, 256, 256, 1 << 40, None) == D
     assert L.ccdpp_gated_scan_step(4, 8, 0, 1, 256, 8, 256, 8, 256, 8, 256, 8, None) == D
     assert L.ccdpp_beam_select(B(beam()), 256, 256, 256, None, 256, 1 << 40, None) == D
-    one, sz = (ctypes.c_void_p * 1)(256), (ctypes.c_int64 * 1)(8)
-    assert L.ccdpp_beam_reorder(2, 3, 4, 256, 1, one, sz, one, sz, None) == D
+    one, two, sz = (ctypes.c_void_p * 1)(256), (ctypes.c_void_p * 1)(512), (ctypes.c_int64 * 1)(8)
+    assert L.ccdpp_beam_reorder(2, 3, 4, 256, 1, one, sz, two, sz, None) == D
     assert L.ccdpp_dropout(4, 8, 0, 256, 8, None, 0, 1024, 8, 0.1, 7, None, 0, None) == D
     assert L.ccdpp_ops_last_error()
 
