@@ -85,7 +85,10 @@ def _states(a, name, s, d, index):
 
 
 def _given(a, name, x):
-    return (torch.empty(x.shape, dtype=x.dtype, device=x.device) if a is None else a), (max(x.shape[1], 1) if a is None else _alike(a, name, x))
+    """What is written to, given or new, and its row stride."""
+    if a is None:
+        return torch.empty_like(x) if x.is_contiguous() else torch.empty(x.shape, dtype=x.dtype, device=x.device), max(x.shape[1], 1)
+    return a, _alike(a, name, x)
 
 
 def _sequences(x, gate, starts, initial, mode):
@@ -94,9 +97,9 @@ def _sequences(x, gate, starts, initial, mode):
     n, d = x.shape
     if d > 65536:
         raise ValueError("d must be in [1, 65536]")
-    if not isinstance(starts, torch.Tensor) or starts.dim() != 1 or starts.numel() < 1:
+    s = (starts.numel() if isinstance(starts, torch.Tensor) else 0) - 1
+    if s < 0:
         raise ValueError("starts must be a vector with at least one value")
-    s = starts.numel() - 1
     at = _vector(starts, "starts", s + 1, _INTS, index)
     first = None if initial is None else _states(initial, "initial", s, d, index)
     return Scan(n, s, d, _DTYPES[x.dtype], _mode(mode), 64 if starts.dtype == torch.int64 else 32, x.data_ptr(), ldx,
