@@ -464,7 +464,10 @@ __device__ void carry_in(const Scan& a, Exchange<W>& e, const Place<W>& at, int 
     __syncthreads();
 }
 
-// A chunk whose rows are all of one sequence, and neither its first nor its last, takes the plain way; the other does each row by what it is.
+// A chunk whose rows are all of one sequence, and neither its first nor its last, can take the plain way; the other does each row by what it
+// is.  A wave takes one of them for all its chunks: both would take the time of both.
+__device__ __forceinline__ bool all_plain(bool here, uint32_t in, uint32_t ends) { return !__ballot(here && (in != kAll || ends)); }
+
 template <class T, int W, bool SIGMOID>
 __global__ __launch_bounds__(kThreads) void k_scan(Scan a) {
     __shared__ Exchange<W> e;
@@ -491,7 +494,7 @@ __global__ __launch_bounds__(kThreads) void k_scan(Scan a) {
         const bool here = at.works && c < c1;
         const uint32_t mine = here ? rows_within(row, begin, end) : 0u, in = here ? rows_within(row, lo, hi) : 0u;
         const uint32_t firsts = here ? k.begins & mine : 0u, lasts = here ? k.begins >> 1 & in : 0u;
-        const bool plain = in == kAll && !(firsts | lasts);
+        const bool plain = here && all_plain(here, in, firsts | lasts), other = here && !plain;
         const Chunk now = k;
         float d[kRows][W], u[kRows][W];
 #pragma unroll
@@ -510,7 +513,7 @@ __global__ __launch_bounds__(kThreads) void k_scan(Scan a) {
             for (int i = 0; i < kRows; ++i)
 #pragma unroll
                 for (int w = 0; w < W; ++w) A[w] *= d[i][w], H[w] = fmaf(d[i][w], H[w], u[i][w]);
-        } else {
+        } else if (other) {
 #pragma unroll
             for (int i = 0; i < kRows; ++i) {
                 const bool inside = in >> i & 1, first = firsts >> i & 1;
@@ -541,7 +544,7 @@ __global__ __launch_bounds__(kThreads) void k_scan(Scan a) {
                 r.store(y);
                 next(y, a.ldy);
             }
-        } else {
+        } else if (other) {
 #pragma unroll
             for (int i = 0; i < kRows; ++i) {
                 const bool inside = in >> i & 1, first = firsts >> i & 1;
@@ -595,7 +598,7 @@ __global__ __launch_bounds__(kThreads) void k_scan_grad(Scan a) {
         const bool here = at.works && c >= c0;
         const uint32_t mine = here ? rows_within(row, begin, end) : 0u, in = here ? rows_within(row, lo, hi) : 0u;
         const uint32_t firsts = here ? k.begins & in : 0u, lasts = here ? k.begins >> 1 & in : 0u;
-        const bool plain = in == kAll && !(firsts | lasts);
+        const bool plain = here && all_plain(here, in, firsts | lasts), other = here && !plain;
         const Chunk now = k;
         // Kept in registers from the pass down the rows for the two up: a, 1 - a, what l is multiplied by for dgate, and dy as it is.
         float d[kRows][W], rest[kRows][W], f[kRows][W];
@@ -617,7 +620,7 @@ __global__ __launch_bounds__(kThreads) void k_scan_grad(Scan a) {
 #pragma unroll
                 for (int w = 0; w < W; ++w) down(i, w, x.v[i], gate.v[i], h[w]);
             }
-        } else {
+        } else if (other) {
 #pragma unroll
             for (int i = 0; i < kRows; ++i) {
                 if (firsts >> i & 1) {
@@ -642,7 +645,7 @@ __global__ __launch_bounds__(kThreads) void k_scan_grad(Scan a) {
                 for (int w = 0; w < W; ++w) {
                     A[w] *= d[i][w], H[w] = d[i][w] * (g.v[i].get(w) + H[w]);
                 }
-        } else {
+        } else if (other) {
 #pragma unroll
             for (int i = kRows - 1; i >= 0; --i) {
                 if (lasts >> i & 1) {
@@ -676,7 +679,7 @@ __global__ __launch_bounds__(kThreads) void k_scan_grad(Scan a) {
                 r.store(dx), t.store(dg);
                 next(dx, -a.lddx), next(dg, -a.lddg);
             }
-        } else {
+        } else if (other) {
 #pragma unroll
             for (int i = kRows - 1; i >= 0; --i) {
                 if (lasts >> i & 1) {
