@@ -12,7 +12,7 @@
 //
 // 32,768 x 4,096 bfloat16 in 16 sequences: 181 us forward (4.6 TB/s with the kept states), 303 for the gradients (4.6), of a copy's 5.13;
 // vector instructions are issued in 74% and 55% of the cycles (a value takes some 30 forward, 40 back).  1,000,209 x 40 floats in 6,041 sequences
-// 122 + 17 us; one sequence of 65,537 x 100 bfloat16 19 + 8, which is what the rounds to memory of a block take one after another.
+// 106 + 22 us; one sequence of 65,537 x 100 bfloat16 18 + 8, which is what the rounds to memory of a block take one after another.
 #include <algorithm>
 #include <type_traits>
 
@@ -22,10 +22,11 @@
 namespace ccdops {
 namespace {
 
-// kRows: of a chunk, of which one state is kept for the gradients (half a byte a value).  With 16 the gradients' registers leave one block
-// a CU: 416 us in place of 305 for 32,768 x 4,096 bfloat16, the histories above 153 in place of 122.
-// kThreads: with 256 a block has half the chunks side by side and twice the steps: 10,007 x 777 half precision, both ways, 105 us in
-// place of 91, the long sequence 34 in place of 29, 32,768 x 4,096 the same (499 and 497).
+// kRows: of a chunk, of which one state is kept for the gradients (half a byte a value).  With 16 the gradients' registers leave fewer waves:
+// 345 us in place of 303 for 32,768 x 4,096 bfloat16; the histories above take 118 + 21 in place of 106 + 22, 10,007 x 777 half precision, both
+// ways, 108 in place of 78.
+// kThreads: with 256 a block has half the chunks side by side and twice the steps: 10,007 x 777 half precision 85 us in place of 78, the histories
+// 133 in place of 128, 32,768 x 4,096 both ways 505 in place of 494.
 constexpr int kRows = 8;
 constexpr int kThreads = 512;  // of a block
 constexpr int kLanes = 64;     // of a group, at most
@@ -775,14 +776,15 @@ struct Layout {
     int64_t share, chunk, of_row, carry, bytes;
 };
 
-// Blocks of a launch: two of 512 threads a CU are at work at once.  (Histories of 1,000,209 x 40 floats: 1,024 blocks 116 + 32 us in place of
-// 122 + 24, as more sequences go on from share to share; 256 132 + 27.  10,007 x 777 half precision, both ways: 256 blocks 102 in place of 91.)
+// Blocks of a launch: two of 512 threads a CU.  1,024 split more sequences: 32,768 x 4,096 bfloat16 in 16, both ways, 612 us in place of 494,
+// 10,007 x 777 half precision 88 in place of 78.  256 would take 460 and 83 there, as nothing is split, but sequences' ends and shares of unlike
+// lengths weigh more: 16,000 x 4,096 bfloat16 in 4,000 sequences 190 in place of 160 forward, 65,000 x 1,000 in 64, both ways, 414 in place of 393.
 constexpr int64_t kBlocks = 512;
-// Bytes of a row that the lanes of a group take at least: with 128, 32,768 x 4,096 bfloat16 takes 203 us forward in place of 187, and 390 in
-// place of 332 for the gradients.
+// Bytes of a row that the lanes of a group take at least, where strips are made narrower for more blocks: 32,768 x 4,096 bfloat16 in strips of 128
+// bytes takes 203 us forward in place of 187, and 390 in place of 332 for the gradients.
 constexpr int kPiece = 256;
-// Values from which on the gradients take two columns a thread: 305 us in place of 326 for 32,768 x 4,096 bfloat16, where their instructions
-// bound them; one column leaves registers for twice the waves, which wait less: 35 in place of 41 for 10,007 x 777 half precision.
+// Values from which on the gradients take two columns a thread: 303 us in place of 325 for 32,768 x 4,096 bfloat16, where their instructions
+// bound them; one column leaves registers for twice the waves, which wait less: 31.7 in place of 32.5 for 10,007 x 777 half precision.
 constexpr int64_t kMuch = 1 << 25;
 
 Layout layout(const ccdpp_scan_t* p, int32_t call) {
