@@ -777,9 +777,16 @@ struct Layout {
 };
 
 // Blocks of a launch: two of 512 threads a CU.  1,024 split more sequences: 32,768 x 4,096 bfloat16 in 16, both ways, 612 us in place of 494,
-// 10,007 x 777 half precision 88 in place of 78.  256 would take 460 and 83 there, as nothing is split, but sequences' ends and shares of unlike
-// lengths weigh more: 16,000 x 4,096 bfloat16 in 4,000 sequences 190 in place of 160 forward, 65,000 x 1,000 in 64, both ways, 414 in place of 393.
+// 10,007 x 777 half precision 88 in place of 78.
 constexpr int64_t kBlocks = 512;
+// One block a CU where rows are wide, which leaves fewer sequences that go on from share to share and starts each block once: 32,768 x 4,096
+// bfloat16, both ways, in 16 sequences 460 us in place of 490, in 8 459 in place of 620, in 30 of unlike lengths 528 in place of 624; floats 781 in
+// place of 811, 65,536 x 1,024 in 500 479 in place of 523.  Not for 16-bit rows below 8 KB (40,000 x 2,500 in 20 639 in place of 626, 65,000 x
+// 1,000 in 64 414 in place of 393) or in short sequences (32,768 x 4,096 in 512 697 in place of 655), whose instructions need the waves, nor for
+// floats below 4 KB (300,000 x 200 in 50 799 in place of 740).
+bool one_block_a_cu(const ccdpp_scan_t* p) {
+    return p->dtype == CCDPP_F32 ? p->d >= 1024 : p->d >= 4096 && p->n / 256 >= p->s;
+}
 // Bytes of a row that the lanes of a group take at least, where strips are made narrower for more blocks: 32,768 x 4,096 bfloat16 in strips of 128
 // bytes takes 203 us forward in place of 187, and 390 in place of 332 for the gradients.
 constexpr int kPiece = 256;
@@ -792,13 +799,14 @@ Layout layout(const ccdpp_scan_t* p, int32_t call) {
     l.width = p->d >= 2 && (call == CCDPP_SCAN_FORWARD || p->n * p->d >= kMuch) ? 2 : 1;
     const int lanes = (p->d + l.width - 1) / l.width;
     l.chunks = (p->n + kRows - 1) / kRows;
+    const int64_t blocks = one_block_a_cu(p) ? kBlocks / 2 : kBlocks;
     int64_t shares = 1;
     for (int widest = kLanes;; widest /= 2) {
         l.strips = (lanes + widest - 1) / widest;
         l.lanes = (lanes + l.strips - 1) / l.strips;
         l.groups = std::min(kThreads / l.lanes, 64);
-        shares = std::max<int64_t>(1, std::min(kBlocks / l.strips, l.chunks / l.groups));
-        if (l.strips * shares >= kBlocks || widest * l.width * (p->dtype == CCDPP_F32 ? 4 : 2) <= kPiece) break;
+        shares = std::max<int64_t>(1, std::min(blocks / l.strips, l.chunks / l.groups));
+        if (l.strips * shares >= blocks || widest * l.width * (p->dtype == CCDPP_F32 ? 4 : 2) <= kPiece) break;
     }
     l.rows = round_up((std::max<int64_t>(p->n, 1) + shares - 1) / shares, kRows);
     l.shares = (int)((std::max<int64_t>(p->n, 1) + l.rows - 1) / l.rows);
