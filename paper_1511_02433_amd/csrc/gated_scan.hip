@@ -10,8 +10,8 @@
 // sequence that goes on from one share to the next has its rows there read a second time, by a launch before, for their (A, H); so
 // shares begin where a sequence does if one does nearby.  Lengths are known to the device alone: every rule here holds for any of them.
 //
-// 32,768 x 4,096 bfloat16 in 16 sequences: 181 us forward (4.6 TB/s with the kept states), 303 for the gradients (4.6), of a copy's 5.13;
-// vector instructions are issued in 74% and 55% of the cycles (a value takes some 30 forward, 40 back).  1,000,209 x 40 floats in 6,041 sequences
+// 32,768 x 4,096 bfloat16 in 16 sequences: 180 us forward (4.6 TB/s with the kept states), 280 for the gradients (4.9), of a copy's 5.13;
+// vector instructions are issued in 75% and 59% of the cycles (a value takes some 30 forward, 40 back).  1,000,209 x 40 floats in 6,041 sequences
 // 106 + 22 us; one sequence of 65,537 x 100 bfloat16 18 + 8, which is what the rounds to memory of a block take one after another.
 #include <algorithm>
 #include <type_traits>
