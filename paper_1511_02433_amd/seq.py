@@ -235,7 +235,7 @@ def beam_select(logits, score, k, *, offset=None, done=None, end=None):
     with _On(index):
         n = _beam_bytes(g, v, b, k, p.dtype)
         ws = torch.empty(n, dtype=torch.uint8, device=device)
-        out = torch.empty((g, k), dtype=torch.float32, device=device)
+        out = torch.empty_like(score) if k == b else torch.empty((g, k), dtype=torch.float32, device=device)
         parent, item = torch.empty((2, g, k), dtype=torch.int64, device=device).unbind()
         ended = None if end is None else torch.empty((g, k), dtype=torch.bool, device=device)
         _check(L.ccdpp_beam_select(ctypes.byref(p), out.data_ptr(), parent.data_ptr(), item.data_ptr(), None if ended is None else ended.data_ptr(),
@@ -259,27 +259,33 @@ def beam_reorder(parent, states, *, beams, out=None):
         out = list(out)
         if len(out) != n:
             raise ValueError("out must have one tensor for each state")
-    strides, sizes = [], []
-    for a in states:
-        if not isinstance(a, torch.Tensor) or a.dim() < 1:
-            raise TypeError("states must be tensors with a row for each beam")
-        if a.get_device() != index or a.shape[0] != g * beams:
-            raise ValueError(f"states must have {g * beams} rows, on the device of parent")
-        row = a.nbytes // max(a.shape[0], 1)
-        if a.is_contiguous():
-            strides.append(row)
-        else:
-            apart = a.stride(0) * a.element_size()
-            if not a[0].is_contiguous() or apart < row:
-                raise ValueError("rows of states must be contiguous")
-            strides.append(apart)
-        sizes.append(row)
+    rows, to = g * beams, g * k
     with _On(index):
-        got = [torch.empty((g * k, *a.shape[1:]), dtype=a.dtype, device=a.device) for a in states] if out is None else out
-        for a, o in zip(states, got):
-            if out is not None and (not isinstance(o, torch.Tensor) or o.shape != (g * k, *a.shape[1:]) or o.dtype != a.dtype
-                                    or o.get_device() != index or not o.is_contiguous()):
-                raise ValueError("out must be contiguous, with the states' type and row shape, and a row for each continuation")
+        strides, sizes, got = [], [], []
+        for a in states:
+            if not isinstance(a, torch.Tensor) or a.dim() < 1:
+                raise TypeError("states must be tensors with a row for each beam")
+            if a.get_device() != index or a.shape[0] != rows:
+                raise ValueError(f"states must have {rows} rows, on the device of parent")
+            row = a.nbytes // max(rows, 1)
+            sizes.append(row)
+            if a.is_contiguous():
+                strides.append(row)
+                if out is None:
+                    got.append(torch.empty_like(a) if to == rows else a.new_empty((to, *a.shape[1:])))
+            else:
+                apart = a.stride(0) * a.element_size()
+                if not a[0].is_contiguous() or apart < row:
+                    raise ValueError("rows of states must be contiguous")
+                strides.append(apart)
+                if out is None:
+                    got.append(a.new_empty((to, *a.shape[1:])))
+        if out is not None:
+            got = out
+            for a, o in zip(states, out):
+                if (not isinstance(o, torch.Tensor) or o.shape != (to, *a.shape[1:]) or o.dtype != a.dtype or o.get_device() != index
+                        or not o.is_contiguous()):
+                    raise ValueError("out must be contiguous, with the states' type and row shape, and a row for each continuation")
         P, N = ctypes.c_void_p * n, ctypes.c_int64 * n
         _check(_lib().ccdpp_beam_reorder(g, beams, k, parent.data_ptr(), n, P(*[a.data_ptr() for a in states]), N(*strides),
                                          P(*[o.data_ptr() for o in got]), N(*sizes), _stream(index)))
