@@ -12,6 +12,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+from operator import index as _whole
 
 import torch
 
@@ -190,6 +191,7 @@ def gated_scan_step(x, gate, state, *, mode="sigmoid", y=None):
 
 
 def _count(a, name):
+    a = _whole(a)
     if not 1 <= a <= 64:
         raise ValueError(f"{name} must be in [1, 64], not {a}")
     return a
@@ -214,6 +216,8 @@ def beam_select(logits, score, k, *, offset=None, done=None, end=None):
     if not isinstance(score, torch.Tensor) or score.dim() != 2:
         raise TypeError("score must be a matrix (a two-dimensional tensor)")
     g, b = score.shape
+    _count(b, "beams")
+    k = _count(k, "k")
     rows, v = logits.shape
     if rows != g * b:
         raise ValueError(f"logits must have a row for each of the {g} x {b} beams, not {rows}")
@@ -228,9 +232,11 @@ def beam_select(logits, score, k, *, offset=None, done=None, end=None):
         if done.shape != score.shape or not done.is_contiguous() or done.get_device() != index:
             raise ValueError("done must be contiguous, with the shape and device of score")
         f = done.data_ptr()
-    if end is not None and not 0 <= end < v:
-        raise ValueError(f"end must be an item, in [0, {v})")
-    p = Beam(g, v, _count(b, "beams"), _count(k, "k"), _DTYPES[logits.dtype], 0, logits.data_ptr(), ld, s, o, f, -1 if end is None else end)
+    if end is not None:
+        end = _whole(end)
+        if not 0 <= end < v:
+            raise ValueError(f"end must be an item, in [0, {v})")
+    p = Beam(g, v, b, k, _DTYPES[logits.dtype], 0, logits.data_ptr(), ld, s, o, f, -1 if end is None else end)
     L, device = _lib(), logits.device
     with _On(index):
         n = _beam_bytes(g, v, b, k, p.dtype)
@@ -251,7 +257,7 @@ def beam_reorder(parent, states, *, beams, out=None):
         raise TypeError("parent must be a matrix of int64")
     g, k = parent.shape
     index, states = parent.get_device(), list(states)
-    _count(beams, "beams"), _count(k, "k")
+    beams, k = _count(beams, "beams"), _count(k, "k")
     if index < 0 or not parent.is_contiguous():
         raise ValueError("parent must be contiguous, in device memory")
     n = len(states)
@@ -307,8 +313,11 @@ def dropout(x, p, seed, *, first_row=0, residual=None, out=None):
         if seed.dtype != torch.int64 or seed.numel() != 1 or seed.get_device() != index:
             raise ValueError("a seed in device memory must be one int64 value on the device of x")
         at, seed = seed.data_ptr(), 0
-    elif not -2 ** 63 <= seed < 2 ** 64:
-        raise ValueError("seed must fit 64 bits")
+    else:
+        seed = _whole(seed)
+        if not -2 ** 63 <= seed < 2 ** 64:
+            raise ValueError("seed must fit 64 bits")
+    first_row = _whole(first_row)
     if not 0 <= first_row < 2 ** 63:
         raise ValueError("first_row must be in [0, 2^63)")
     with _On(index):

@@ -82,7 +82,7 @@ def make(g, b, v, dtype, seed, pad=0, spread=2.0):
 @pytest.mark.parametrize("g, b, k, v, pad", [
     (1, 1, 1, 1, 0), (1, 1, 4, 2, 0), (2, 3, 5, 7, 1), (1, 4, 4, 63, 0), (3, 2, 8, 64, 3), (1, 8, 8, 65, 0), (2, 5, 3, 255, 0), (2, 5, 3, 257, 2),
     (1, 4, 4, 1000, 0), (4, 4, 4, 4097, 1), (2, 16, 16, 2049, 0), (1, 64, 64, 300, 5), (3, 7, 64, 1023, 0), (1, 64, 1, 5000, 1), (1, 1, 64, 10_001, 0),
-    (5, 8, 8, 17_770, 0), (1, 2, 10, 140_003, 1)])
+    (5, 8, 8, 17_770, 0), (1, 2, 10, 140_003, 1), (1, 1, 8, 624_961, 0), (1, 3, 64, 600_001, 1), (40, 16, 4, 5000, 0)])
 def test_select(g, b, k, v, pad, dtype):
     _, logits, score = make(g, b, v, dtype, g * 1000 + v, pad)
     check(logits, score, k)
@@ -193,6 +193,29 @@ def test_offsets_beyond_32_bits():
     big.copy_(logits)
     for a, b in zip(seq().beam_select(logits, score, 4)[:3], seq().beam_select(big, score, 4)[:3]):
         assert torch.equal(a, b)
+
+
+def test_refusals():
+    _, logits, score = make(2, 3, 50, "f32", 1)
+    good = dict(logits=logits, score=score, k=2)
+    for kw, error in ((dict(k=0), ValueError), (dict(k=65), ValueError), (dict(k=2 ** 32 + 2), ValueError), (dict(score=score[:1]), ValueError),
+                      (dict(score=score.double()), TypeError), (dict(score=score.cpu()), ValueError), (dict(logits=logits[:, ::2]), ValueError),
+                      (dict(offset=torch.zeros(49, device="cuda")), ValueError), (dict(done=torch.zeros(2, 3, dtype=torch.bool, device="cuda")), ValueError),
+                      (dict(done=torch.zeros(2, 2, dtype=torch.bool, device="cuda"), end=1), ValueError), (dict(end=50), ValueError), (dict(end=-1), ValueError),
+                      (dict(done=torch.zeros(2, 3, device="cuda"), end=1), TypeError)):
+        args = {**good, **kw}
+        with pytest.raises(error):
+            seq().beam_select(args.pop("logits"), args.pop("score"), args.pop("k"), **args)
+    parent = torch.zeros(2, 3, dtype=torch.int64, device="cuda")
+    state = torch.randn(6, 4, device="cuda")
+    for kw, error in ((dict(states=[state[:5]]), ValueError), (dict(states=[state.cpu()]), ValueError), (dict(states=[state[:, ::2]]), ValueError),
+                      (dict(beams=0), ValueError), (dict(beams=65), ValueError), (dict(parent=parent.int()), TypeError), (dict(parent=parent.T), ValueError),
+                      (dict(out=[]), ValueError), (dict(out=[state[:5].clone()]), ValueError), (dict(out=[state.double()]), ValueError), (dict(states=[1.0]), TypeError)):
+        args = {"parent": parent, "states": [state], "beams": 3, **kw}
+        with pytest.raises(error):
+            seq().beam_reorder(args.pop("parent"), args.pop("states"), **args)
+    with pytest.raises(Exception, match="must not be an input"):
+        seq().beam_reorder(parent, [state], beams=3, out=[state])
 
 
 def test_no_groups():

@@ -47,7 +47,8 @@ def check(n, d, dtype, p, seed, first_row=0, residual=False, pad=0):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("n, d, pad", [(0, 5, 0), (1, 1, 0), (1, 4, 0), (3, 5, 0), (7, 3, 2), (64, 40, 0), (5, 63, 1), (33, 129, 0), (1024, 40, 0),
-                                       (17, 777, 0), (11, 1000, 3), (4, 4096, 0), (2, 65_537, 0), (1, 100_001, 0), (20_000, 2, 0), (3001, 9, 0)])
+                                       (17, 777, 0), (11, 1000, 3), (4, 4096, 0), (2, 65_537, 0), (1, 100_001, 0), (20_000, 2, 0), (3001, 9, 0),
+                                       (2, 4_300_001, 0)])
 def test_values(n, d, pad, dtype):
     check(n, d, dtype, 0.1, 12345678901234567, pad=pad, residual=(n + d) % 2 == 0)
     check(n, d, dtype, 0.5, 7, pad=pad, residual=(n + d) % 2 == 1)
@@ -72,6 +73,22 @@ def test_counters(seed, first_row):
 def test_a_negative_seed_is_its_64_bits():
     x = torch.randn(10, 30, device="cuda")
     assert torch.equal(seq().dropout(x, 0.5, -5), seq().dropout(x, 0.5, 2 ** 64 - 5))
+
+
+def test_what_is_no_whole_number_of_64_bits_is_refused():
+    x = torch.randn(4, 8, device="cuda")
+    assert torch.equal(seq().dropout(x, 0.5, np.int64(7), first_row=np.int32(3)), seq().dropout(x, 0.5, 7, first_row=3))
+    for kw in (dict(seed=2 ** 64), dict(seed=-2 ** 63 - 1), dict(first_row=-1), dict(first_row=2 ** 63)):
+        with pytest.raises(ValueError):
+            seq().dropout(x, 0.5, **{"seed": 1, **kw})
+    for kw in (dict(seed=1.0), dict(first_row=0.5)):
+        with pytest.raises(TypeError):
+            seq().dropout(x, 0.5, **{"seed": 1, **kw})
+    for seed in (torch.tensor(1), torch.tensor([1, 2], device="cuda"), torch.tensor([1], device="cuda", dtype=torch.int32)):
+        with pytest.raises(ValueError):
+            seq().dropout(x, 0.5, seed)
+    with pytest.raises(Exception, match="p must"):
+        seq().dropout(x, 1.5, 1)
 
 
 def test_the_mask_is_of_the_row_and_column_alone():

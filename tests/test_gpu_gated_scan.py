@@ -153,6 +153,40 @@ def test_long(n, d, s, mode):
     close(di, wi, ei, "dinitial")
 
 
+@pytest.mark.parametrize("mode", ["sigmoid", "given"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("n, d, s", [(8_300, 4097, 9), (8_300, 4097, 700), (900, 40_000, 3), (300_000, 130, 40)])
+def test_much(n, d, s, dtype, mode):
+    """Sizes from which the gradients take two columns a thread, and wide rows one block a CU; columns here and there against 64 bits."""
+    rng = np.random.default_rng(n + s)
+    starts = np.sort(np.concatenate([[0], rng.integers(0, n - 20, s - 1), [n - 20]])).astype(np.int64)
+    gen = torch.Generator(device="cuda").manual_seed(s)
+
+    def rows(scale=1.0, add=0.0):
+        return torch.randn(n, d, generator=gen, device="cuda").mul_(scale).add_(add).to(DT[dtype])
+
+    x, gate, dy = rows(), rows(2.0, 2.0), rows()
+    if mode == "given":
+        gate = torch.sigmoid(gate.float()).to(gate.dtype)
+    first, dl = (torch.randn(s, d, generator=gen, device="cuda") for _ in range(2))
+    at = torch.from_numpy(starts).cuda()
+    y, last, kept = seq().gated_scan(x, gate, starts=at, initial=first, mode=mode, keep=True)
+    dx, dg, di = seq().gated_scan_grad(x, gate, dy, kept, starts=at, initial=first, mode=mode, dlast=dl)
+    for a in (y, dx, dg):
+        assert bool((a[n - 20:] == 0).all()) and bool(torch.isfinite(a).all())
+    some = torch.tensor([0, 1, 2, 127, d // 2, d // 2 + 1, d - 3, d - 2, d - 1]).cuda()
+    if n > 100_000:
+        some = some[[1, 5, 8]]
+    X, G, D, I, L = (to64(a[:, some]) for a in (x, gate, dy, first, dl))
+    wy, wl, before, ey, el, eb = forward(X, G, starts, I, mode)
+    close(y[:, some], wy, ey, "y")
+    close(last[:, some], wl, el, "last")
+    wx, wg, wi, ex, eg, ei = backward(X, G, D, L, starts, before, eb, mode)
+    close(dx[:, some], wx, ex, "dx")
+    close(dg[:, some], wg, eg, "dgate")
+    close(di[:, some], wi, ei, "dinitial")
+
+
 @pytest.mark.parametrize("seed", range(24))
 def test_random_problems(seed):
     """Sizes, types, layouts and lengths at random: sequences by a power law, some without rows, rows before and behind them."""
@@ -266,6 +300,33 @@ def test_steps_are_the_scan(mode):
     _, _, _, ey, el, _ = forward(to64(x), to64(gate), [0, n], to64(first), mode)
     close(got, to64(y), 2 * ey, "y")
     close(state, to64(last), 2 * el, "last")
+
+
+def test_refusals():
+    x, gate, at = torch.randn(6, 4, device="cuda"), torch.randn(6, 4, device="cuda"), torch.tensor([0, 2, 6], device="cuda")
+    _, _, kept = seq().gated_scan(x, gate, starts=at, keep=True)
+    for kw, error in ((dict(gate=gate[:5]), ValueError), (dict(gate=gate.half()), ValueError), (dict(gate=gate.cpu()), ValueError), (dict(x=x.T), ValueError),
+                      (dict(starts=at.float()), TypeError), (dict(starts=at[:0]), ValueError), (dict(starts=[0, 6]), ValueError), (dict(starts=at.cpu()), ValueError),
+                      (dict(mode="tanh"), ValueError), (dict(initial=torch.zeros(3, 4, device="cuda")), ValueError),
+                      (dict(initial=torch.zeros(2, 4, device="cuda").half()), TypeError), (dict(y=x[:5].clone()), ValueError), (dict(y=x.half()), ValueError)):
+        args = {"x": x, "gate": gate, "starts": at, **kw}
+        with pytest.raises(error):
+            seq().gated_scan(args.pop("x"), args.pop("gate"), **args)
+    for kw, error in ((dict(kept=kept[:, :3]), ValueError), (dict(kept=torch.zeros(2, 4, device="cuda")), ValueError), (dict(dy=x[:5]), ValueError),
+                      (dict(dlast=torch.zeros(1, 4, device="cuda")), ValueError), (dict(dx=x.half()), ValueError), (dict(dgate=x[:3]), ValueError)):
+        args = {"dy": x, "kept": kept, "starts": at, **kw}
+        with pytest.raises(error):
+            seq().gated_scan_grad(x, gate, args.pop("dy"), args.pop("kept"), **args)
+    for kw in (dict(y=x), dict(y=gate)):
+        with pytest.raises(Exception, match="must not be an input"):
+            seq().gated_scan(x, gate, starts=at, **kw)
+    same = torch.empty_like(x)
+    for kw in (dict(dx=x), dict(dgate=gate), dict(dx=same, dgate=same)):
+        with pytest.raises(Exception, match="must not be an input"):
+            seq().gated_scan_grad(x, gate, torch.randn_like(x), kept, starts=at, **kw)
+    for state in (torch.zeros(6, 4, device="cuda").half(), torch.zeros(5, 4, device="cuda"), torch.zeros(1, 4, device="cuda").expand(6, 4)):
+        with pytest.raises(Exception):
+            seq().gated_scan_step(x, gate, state)
 
 
 def test_given_outputs_are_written_with_their_strides():

@@ -198,3 +198,7 @@ def test_the_binding_refuses():
         seq.beam_reorder(torch.zeros(1, 2, dtype=torch.int64), [x], beams=2)
     with pytest.raises(ValueError):
         seq.dropout(x, 0.5, 1)
+    with pytest.raises(ValueError):  # before the tensors' device is looked at
+        seq._count(65, "k")
+    with pytest.raises(TypeError):
+        seq._count(2.0, "k")
