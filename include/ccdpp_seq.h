@@ -100,9 +100,12 @@ int ccdpp_gated_scan_step(int64_t n, int32_t d, int32_t dtype, int32_t mode, con
 /*
  * The best continuations of beams.  Each of `groups` groups has `beams` beams with a score;
  * beam b continued by item i has the score
- *   score_b + z_bi - log sum_j exp z_bj,   z_bi = logits_bi + offset_i (in 32 bits),
- * in 64 bits, rounded once.  The k greatest of a group are taken, in descending order; of
- * equal ones the lowest beam goes first, and of a beam the greatest z, then the lowest item.
+ *   score_b + z_bi - log sum_j exp z_bj,   z_bi = logits_bi + offset_i (in 32 bits).
+ * The exponentials and parts of their sums have 32 bits, and the log sum is within 2^-17 of the
+ * exact one; all else is in 64 bits, and scores are rounded once.  The k greatest of a group are taken,
+ * in descending order; of equal ones the lowest beam goes first, and of a beam the greatest z, then the
+ * lowest item.  The order within a beam is exact; of beams whose exact scores differ by less
+ * than their log sums may be off, either may go first.
  *   groups, beams, k, v : 0 <= groups < 2^24, 1 <= beams <= 64, 1 <= k <= 64, 1 <= v < 2^28
  *   logits, ld : groups * beams rows of v values of dtype, ld >= v values apart
  *   score  : float per beam; -inf: there is no such beam, and its logits are not read

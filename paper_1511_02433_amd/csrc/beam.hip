@@ -84,7 +84,7 @@ struct Beam {
     int64_t *parent, *item;
     uint8_t* out_done;
     double* sums;      // of exponentials over a share, relative to
-    float* tops;       // its greatest logit
+    float* refs;       // about its greatest logit; inf where that is inf or NaN, -inf where nothing takes part
     uint64_t* keys;    // k of each share, descending; 0: none
 };
 
@@ -161,8 +161,12 @@ struct Found {
     }
 };
 
-// One block for each share of a row.  Its waves take chunks in turn; a chunk is read once: its exponentials are added up relative to the
-// lane's greatest logit so far (in 32 bits within a chunk, in 64 over them), then what may be among the k best is put aside.  Of a wave's
+// One block for each share of a row.  Its waves take chunks in turn; a chunk is read once: its exponentials are added up relative to about the
+// lane's greatest logit so far (in 32 bits within a chunk, in 64 over them), then what may be among the k best is put aside.
+// What they are relative to is raised only where a logit is more than 1 above it, so a term that ends D below it is rounded for D + 3 raises at
+// most, however long the row is.  With u = 2^-24 (half a step of 32 bits): 2 u each and 2.3 u for each 1 of D, in the exponential and the
+// raises together; 2 u for the exponential, 9 u for its chunk's sum: (4.3 D + 20) u.  Of fewer than 2^28 terms the mean D by weight is below
+// 16, so the sum is within 90 u < 2^-17 of itself.  (Raised with every new maximum, the log sum of 2^28 ascending floats was 2^-14 off.)  Of a wave's
 // first chunk that is what is not below the k-th greatest of its lanes' greatest values; with values in any order little is found after that.
 // Where more than kAdded values pass, a bound is looked for that at least k and no more than kAdded pass; where there is none (many equal
 // ones), the k greatest of the chunk are taken out one by one.
@@ -172,7 +176,7 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 && !OFFSET ? 4 : 2) voi
     typedef Chunk<T, OFFSET> C;
     __shared__ uint64_t keys[kWaves][kFound];
     __shared__ double sums[kWaves];
-    __shared__ float tops[kWaves];
+    __shared__ float refs[kWaves];
     __shared__ int counts[kWaves];
     __shared__ uint32_t known;  // the order of a value that k of the block's are not below
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -188,7 +192,7 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 && !OFFSET ? 4 : 2) voi
         if (threadIdx.x == 0) known = 0;
         __syncthreads();
         Found found = {keys[wave], 0, -INFINITY};
-        float top = -INFINITY;  // of the lane
+        float ref = -INFINITY;  // of the lane
         double sum = 0.0;
         for (int64_t c = begin + wave; c < end; c += kWaves) {
             float z[kEach];
@@ -209,20 +213,20 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 && !OFFSET ? 4 : 2) voi
                 return m;
             };
             float m = greatest();
-            const float was = top;
-            top = fmaxf(top, m);
-            const float ref = top == -INFINITY ? 0.f : top;
+            const float was = ref;
+            ref = m > ref + 1.f ? m : ref;
+            const float to = ref == -INFINITY ? 0.f : ref;
             float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int e = 0; e < kEach; ++e) part[e & 3] += __builtin_amdgcn_exp2f((z[e] - ref) * kLog2e);
+            for (int e = 0; e < kEach; ++e) part[e & 3] += __builtin_amdgcn_exp2f((z[e] - to) * kLog2e);
             const float parts = (part[0] + part[1]) + (part[2] + part[3]);
             if (__ballot(parts != parts)) {  // NaN (or infinity less infinity): NaN counts as infinity
 #pragma unroll
                 for (int e = 0; e < kEach; ++e) z[e] = z[e] != z[e] ? INFINITY : z[e];
                 m = greatest();
-                top = fmaxf(top, m);
+                if (m == INFINITY) ref = m;
             }
-            sum = sum * (was == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((was - ref) * kLog2e)) + (double)parts;
+            sum = sum * (was == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((was - to) * kLog2e)) + (double)parts;
             // At least `bound`: above own, and not below what others know.
             const auto bound_of = [&] { return value_of(max(order_of(found.own + 0.f) + 1, all_know)); };
             float bound = bound_of();
@@ -314,10 +318,10 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 && !OFFSET ? 4 : 2) voi
             if (found.own > before && lane == 0) atomicMax(&known, order_of(found.own + 0.f));
         }
         found.prune(a.k);
-        const float all = wave_max(top);
-        if (top != all) sum *= top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((top - all) * kLog2e);
+        const float all = wave_max(ref);
+        if (ref != all) sum *= ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((ref - all) * kLog2e);
         for (int k = 32; k > 0; k >>= 1) sum += __shfl_xor(sum, k);
-        if (lane == 0) sums[wave] = sum, tops[wave] = all, counts[wave] = found.n;
+        if (lane == 0) sums[wave] = sum, refs[wave] = all, counts[wave] = found.n;
         __syncthreads();
         // Places among all waves' keys.
         const uint64_t mine = lane < found.n ? keys[wave][lane] : 0;
@@ -336,12 +340,12 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 && !OFFSET ? 4 : 2) voi
         if (wave == 0) {
             if (lane >= total && lane < a.k) a.keys[item * a.k + lane] = 0;
             if (lane == 0) {
-                float t = tops[0];
-                for (int w = 1; w < kWaves; ++w) t = fmaxf(t, tops[w]);
+                float t = refs[0];
+                for (int w = 1; w < kWaves; ++w) t = fmaxf(t, refs[w]);
                 double s = 0.0;
                 for (int w = 0; w < kWaves; ++w)
-                    if (tops[w] != -INFINITY) s += sums[w] * (double)__builtin_amdgcn_exp2f((tops[w] - t) * kLog2e);
-                a.sums[item] = s, a.tops[item] = t;
+                    if (refs[w] != -INFINITY) s += sums[w] * (double)__builtin_amdgcn_exp2f((refs[w] - t) * kLog2e);
+                a.sums[item] = s, a.refs[item] = t;
             }
         }
     }
@@ -359,16 +363,16 @@ __global__ __launch_bounds__(1024) void k_beam_join(Beam a) {
         for (int b = wave; b < a.beams; b += waves) {
             const int64_t row = g * a.beams + b;
             const int64_t first = row * a.shares;
-            // What most rows need is asked for at once: the first lists, tops and sums.  (Where the beam is none or done they hold nothing.)
+            // What most rows need is asked for at once: the first lists, references and sums.  (Where the beam is none or done they hold nothing.)
             constexpr int kAtOnce = 8;
             uint64_t other[kAtOnce];
             const auto ask = [&](int s) {
 #pragma unroll
                 for (int u = 0; u < kAtOnce; ++u) other[u] = lane < a.k && s + u < a.shares ? a.keys[(first + s + u) * a.k + lane] : 0;
             };
-            float my_top = -INFINITY;
+            float my_ref = -INFINITY;
             double my_sum = 0.0;
-            if (lane < a.shares) my_top = a.tops[first + lane], my_sum = a.sums[first + lane];
+            if (lane < a.shares) my_ref = a.refs[first + lane], my_sum = a.sums[first + lane];
             ask(0);
             if (lane_of(my_score, b) == -INFINITY || __ballot(my_done) >> b & 1) continue;
             Best best = {other[0]};
@@ -386,19 +390,19 @@ __global__ __launch_bounds__(1024) void k_beam_join(Beam a) {
                 ask(s);
             }
             for (int s = lane + 64; s < a.shares; s += 64) {
-                const float t = a.tops[first + s], more = fmaxf(my_top, t);
+                const float t = a.refs[first + s], more = fmaxf(my_ref, t);
                 if (t == -INFINITY) continue;
-                my_sum = my_sum * (my_top == -INFINITY ? 0.0 : exp((double)my_top - more)) + a.sums[first + s] * exp((double)t - more);
-                my_top = more;
+                my_sum = my_sum * (my_ref == -INFINITY ? 0.0 : exp((double)my_ref - more)) + a.sums[first + s] * exp((double)t - more);
+                my_ref = more;
             }
-            const float top = wave_max(my_top);
+            const float ref = wave_max(my_ref);
             double sum = my_sum;
             if (a.shares > 1) {
-                sum = my_top == -INFINITY ? 0.0 : my_sum * exp((double)my_top - top);
+                sum = my_ref == -INFINITY ? 0.0 : my_sum * exp((double)my_ref - ref);
                 for (int k = 32; k > 0; k >>= 1) sum += __shfl_xor(sum, k);
             }
             if (lane < a.k) lists[b][lane] = best.key;
-            if (lane == 0) logs[b] = top == INFINITY ? (double)NAN : top + log(sum);
+            if (lane == 0) logs[b] = ref == INFINITY ? (double)NAN : ref + log(sum);
         }
         __syncthreads();
         if (wave == 0) {
@@ -485,7 +489,7 @@ int check(const ccdpp_beam_t* p) {
 // first chunk costs the most, so fewer shares are better for many rows (512 rows of 624,961 floats in one share each 250 us, in two 257, in
 // four 277), but too few leave waits bare (128 rows of 131,072 in bfloat16: 512 blocks 24.8, 768 23.4, 1,024 21.9, 256 34).
 struct Layout {
-    int64_t shares, each, sums, tops, keys, bytes;
+    int64_t shares, each, sums, refs, keys, bytes;
 };
 
 Layout layout(const ccdpp_beam_t* p) {
@@ -495,8 +499,8 @@ Layout layout(const ccdpp_beam_t* p) {
     l.each = std::max<int64_t>(round_up((chunks + wanted - 1) / wanted, kWaves), kWaves);
     l.shares = (chunks + l.each - 1) / l.each;
     l.sums = 0;
-    l.tops = round_up(rows * l.shares * 8, 256);
-    l.keys = l.tops + round_up(rows * l.shares * 4, 256);
+    l.refs = round_up(rows * l.shares * 8, 256);
+    l.keys = l.refs + round_up(rows * l.shares * 4, 256);
     l.bytes = l.keys + round_up(rows * l.shares * p->k * 8, 256) + 256;
     return l;
 }
@@ -533,7 +537,7 @@ int ccdpp_beam_select(const ccdpp_beam_t* p, float* out_score, int64_t* parent, 
     a.groups = p->groups, a.v = p->v, a.ld = p->ld, a.end = p->end, a.beams = p->beams, a.k = p->k, a.shares = (int)l.shares, a.each = l.each;
     a.logits = p->logits, a.score = p->score, a.offset = p->offset, a.done = p->done;
     a.out_score = out_score, a.parent = parent, a.item = item, a.out_done = out_done;
-    a.sums = (double*)((char*)ws + l.sums), a.tops = (float*)((char*)ws + l.tops), a.keys = (uint64_t*)((char*)ws + l.keys);
+    a.sums = (double*)((char*)ws + l.sums), a.refs = (float*)((char*)ws + l.refs), a.keys = (uint64_t*)((char*)ws + l.keys);
     hipStream_t st = (hipStream_t)stream;
     const unsigned blocks = (unsigned)std::min<int64_t>(rows * l.shares, kGrid);
     const auto rows_of = [&](auto z) {

@@ -207,8 +207,8 @@ def _beam_bytes(g, v, b, k, dtype):
 def beam_select(logits, score, k, *, offset=None, done=None, end=None):
     """(score, parent, item, done): the k best continuations of each group of beams, in descending order.  score: float32, g x b;
     logits: (g b) x v, the beams' rows one group after another (float32, bfloat16 or float16; rows may lie apart).  Beam b
-    continued by item i has the score score_b + z_i - log sum exp z, z = logits + offset; of equal ones the lowest beam and then
-    the lowest item goes first.  offset: float32 per item; -inf (or below -1e38) excludes it.  A beam with score -inf is none.  done:
+    continued by item i has the score score_b + z_i - log sum exp z, z = logits + offset (in 32 bits; the log sum within 2^-17); of equal
+    ones the lowest beam goes first, and of a beam the greatest z, then the lowest item.  offset: float32 per item; -inf (or below -1e38) excludes it.  A beam with score -inf is none.  done:
     bool, g x b: such a beam is at its end and goes on as itself, with the item `end`.  parent (the beam within the group) and item:
     int64, g x k, and score; -1, -1 and -inf where there are fewer than k.  done is None where `end` is."""
     ld = _matrix(logits, "logits")
