@@ -268,11 +268,13 @@ def beam_reorder(parent, states, *, beams, out=None):
     rows, to = g * beams, g * k
     with _On(index):
         strides, sizes, got = [], [], []
-        for a in states:
+        for i, a in enumerate(states):
             if not isinstance(a, torch.Tensor) or a.dim() < 1:
                 raise TypeError("states must be tensors with a row for each beam")
             if a.get_device() != index or a.shape[0] != rows:
                 raise ValueError(f"states must have {rows} rows, on the device of parent")
+            if a.is_conj() or a.is_neg():  # views whose memory holds other values than they stand for
+                a = states[i] = a.resolve_conj().resolve_neg()
             row = a.nbytes // max(rows, 1)
             sizes.append(row)
             if a.is_contiguous():
@@ -290,8 +292,8 @@ def beam_reorder(parent, states, *, beams, out=None):
             got = out
             for a, o in zip(states, out):
                 if (not isinstance(o, torch.Tensor) or o.shape != (to, *a.shape[1:]) or o.dtype != a.dtype or o.get_device() != index
-                        or not o.is_contiguous()):
-                    raise ValueError("out must be contiguous, with the states' type and row shape, and a row for each continuation")
+                        or not o.is_contiguous() or o.is_conj() or o.is_neg()):
+                    raise ValueError("out must be contiguous (no conjugate), with the states' type and row shape, and a row for each continuation")
         P, N = ctypes.c_void_p * n, ctypes.c_int64 * n
         _check(_lib().ccdpp_beam_reorder(g, beams, k, parent.data_ptr(), n, P(*[a.data_ptr() for a in states]), N(*strides),
                                          P(*[o.data_ptr() for o in got]), N(*sizes), _stream(index)))
