@@ -107,10 +107,12 @@ template <> struct Few<__bf16, 2> : Pair<__bf16> {};
 template <> struct Few<_Float16, 2> : Pair<_Float16> {};
 
 // Where a share of rows begins.  q >= 0: within sequence q, which has rows prev to next - 1; else where a sequence begins, or in no
-// sequence at all.
+// sequence at all.  The rows of all sequences lie in [start0, start_s), which the table of shares has beside each, so that a block has them with
+// its share's begin.
 struct Share {
     int64_t begin, prev, next;
     int64_t q;
+    int64_t start0, start_s;
 };
 // kRows rows of a chunk: the sequence of the first one (-1 or s: none), and a bit for each row that begins a sequence (or the rows
 // behind all), bit kRows for the row after the chunk.  kSkips: sequences without rows begin in it, too; of_row says which begin there.
@@ -254,16 +256,16 @@ __device__ __forceinline__ void next(T*& at, int64_t ld) {
 template <class T, int W>
 struct Rows {
     Few<T, W> v[kRows];
-    // Those of a chunk; rows from n on are not read.
-    __device__ __forceinline__ void load(const void* base, int64_t ld, int64_t row, int64_t n, int col) {
+    // Those of a chunk that lie in [lo, hi): no other row is read.
+    __device__ __forceinline__ void load(const void* base, int64_t ld, int64_t row, int64_t lo, int64_t hi, int col) {
         const T* at = (const T*)base + row * ld + col;
-        if (row + kRows <= n) {
+        if (row >= lo && row + kRows <= hi) {
 #pragma unroll
             for (int i = 0; i < kRows; ++i) v[i].load(at), next(at, ld);
         } else {
 #pragma unroll
             for (int i = 0; i < kRows; ++i) {
-                if (row + i < n) v[i].load(at);
+                if (row + i >= lo && row + i < hi) v[i].load(at);
                 next(at, ld);
             }
         }
@@ -318,9 +320,9 @@ __global__ __launch_bounds__(kThreads) void k_scan_first(Scan a) {
         const auto chunk_of = [&](int64_t i) { return GRAD ? c1 - 1 - i : c0 + i; };
         const auto load = [&](int64_t i) {
             if (i >= to) return;
-            gate.load(a.gate, a.ldg, chunk_of(i) * kRows, a.n, at.col);
-            if (GRAD) x.load(a.y, a.ldy, chunk_of(i) * kRows, a.n, at.col);
-            else x.load(a.x, a.ldx, chunk_of(i) * kRows, a.n, at.col);
+            gate.load(a.gate, a.ldg, chunk_of(i) * kRows, lo, hi, at.col);
+            if (GRAD) x.load(a.y, a.ldy, chunk_of(i) * kRows, lo, hi, at.col);
+            else x.load(a.x, a.ldx, chunk_of(i) * kRows, lo, hi, at.col);
         };
         load(from);
         float first[W], A[W], H[W], C[W], all[W];  // first: the state before a sequence's first row, or behind its last one
@@ -407,7 +409,8 @@ __global__ __launch_bounds__(kThreads) void k_scan_first(Scan a) {
     if (block < a.marks) {
         const int p = block * waves + wave;
         if (p > a.shares) return;
-        const Share s = share_of(a, p);
+        Share s = share_of(a, p);
+        s.start0 = a.s ? start_of(a, 0) : a.n, s.start_s = start_of(a, a.s);
         if ((threadIdx.x & 63) == 0) a.share[p] = s;
         return;
     }
@@ -471,6 +474,36 @@ __device__ void carry_in(const Scan& a, Exchange<W>& e, const Place<W>& at, int 
 // is.  A wave takes one of them for all its chunks: both would take the time of both.
 __device__ __forceinline__ bool all_plain(bool here, uint32_t in, uint32_t ends) { return !__ballot(here && (in != kAll || ends)); }
 
+// The chunks of a share, and those of them that have rows of sequences ([lo, hi)): only these are read and stepped through.
+// (65,536 x 4,096 bfloat16 of which 8 rows are in sequences: 163 us forward and 207 for the gradients, mostly zeros; stepped through like others they
+// take 504 and 723, more than rows of sequences do, which take 322 and 568.)
+struct Range {
+    int64_t c0, c1, all0, all1;
+    __device__ Range(int64_t begin, int64_t end, int64_t lo, int64_t hi) {
+        all0 = begin / kRows, all1 = (end + kRows - 1) / kRows;
+        c0 = lo < hi ? lo / kRows : all1, c1 = lo < hi ? (hi + kRows - 1) / kRows : all1;
+    }
+    // body(chunk) for the others, a group each.
+    template <int W, class F>
+    __device__ __forceinline__ void others(const Scan& a, const Place<W>& at, F&& body) const {
+        if (!at.works) return;
+        for (int64_t c = all0 + at.group; c < c0; c += a.groups) body(c);
+        for (int64_t c = c1 + at.group; c < all1; c += a.groups) body(c);
+    }
+};
+template <class T, int W>
+__device__ __forceinline__ void clear_rows(void* base, int64_t ld, int64_t row, uint32_t which, int col) {
+    const float zero[W] = {};
+    Few<T, W> r;
+    r.set(zero);
+    T* at = (T*)base + row * ld + col;
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        if (which >> i & 1) r.store(at);
+        next(at, ld);
+    }
+}
+
 template <class T, int W, bool SIGMOID>
 __global__ __launch_bounds__(kThreads) void k_scan(Scan a) {
     __shared__ Exchange<W> e;
@@ -478,16 +511,17 @@ __global__ __launch_bounds__(kThreads) void k_scan(Scan a) {
     const Place<W> at(a, strip);
     const Share share = a.share[p];
     const int64_t begin = share.begin, end = a.share[p + 1].begin;
-    const int64_t lo = a.s ? max(start_of(a, 0), begin) : end, hi = a.s ? min(start_of(a, a.s), end) : end;  // rows of sequences
-    const int64_t c0 = begin / kRows, c1 = (end + kRows - 1) / kRows, steps = (c1 - c0 + a.groups - 1) / a.groups;
+    const int64_t lo = max(share.start0, begin), hi = min(share.start_s, end);  // rows of sequences
+    const Range range(begin, end, lo, hi);
+    const int64_t c0 = range.c0, c1 = range.c1, steps = (c1 - c0 + a.groups - 1) / a.groups;
     Rows<T, W> x, gate;
     Chunk k;
     const auto load = [&](int64_t step) {
         const int64_t c = c0 + step * a.groups + at.group;
         if (!at.works || c >= c1) return;
         k = a.chunk[c];
-        x.load(a.x, a.ldx, c * kRows, a.n, at.col);
-        gate.load(a.gate, a.ldg, c * kRows, a.n, at.col);
+        x.load(a.x, a.ldx, c * kRows, share.start0, share.start_s, at.col);
+        gate.load(a.gate, a.ldg, c * kRows, share.start0, share.start_s, at.col);
     };
     load(0);
     float carry[W];
@@ -568,6 +602,11 @@ __global__ __launch_bounds__(kThreads) void k_scan(Scan a) {
         }
         leave<W>(e, a, at, (int)step, h);
     }
+    range.others<W>(a, at, [&](int64_t c) {
+        const uint32_t mine = rows_within(c * kRows, begin, end);
+        clear_rows<T, W>(a.y, a.ldy, c * kRows, mine, at.col);
+        if (a.keep && (mine & 1)) clear_rows<float, W>(a.keep, a.d, c, 1, at.col);
+    });
 }
 
 // Up the rows.  Each chunk's states are computed once more from the one that was kept, which gives what l is multiplied by for dgate; then
@@ -579,8 +618,9 @@ __global__ __launch_bounds__(kThreads) void k_scan_grad(Scan a) {
     const Place<W> at(a, strip);
     const Share share = a.share[p + 1];
     const int64_t begin = a.share[p].begin, end = share.begin;
-    const int64_t lo = a.s ? max(start_of(a, 0), begin) : end, hi = a.s ? min(start_of(a, a.s), end) : end;
-    const int64_t c0 = begin / kRows, c1 = (end + kRows - 1) / kRows, steps = (c1 - c0 + a.groups - 1) / a.groups;
+    const int64_t lo = max(share.start0, begin), hi = min(share.start_s, end);
+    const Range range(begin, end, lo, hi);
+    const int64_t c0 = range.c0, c1 = range.c1, steps = (c1 - c0 + a.groups - 1) / a.groups;
     Rows<T, W> x, gate, dy;
     Few<float, W> h0;
     Chunk k;
@@ -589,9 +629,9 @@ __global__ __launch_bounds__(kThreads) void k_scan_grad(Scan a) {
         if (!at.works || c < c0) return;
         k = a.chunk[c];
         h0.load(a.kept + c * a.d + at.col);
-        x.load(a.x, a.ldx, c * kRows, a.n, at.col);
-        gate.load(a.gate, a.ldg, c * kRows, a.n, at.col);
-        dy.load(a.y, a.ldy, c * kRows, a.n, at.col);
+        x.load(a.x, a.ldx, c * kRows, share.start0, share.start_s, at.col);
+        gate.load(a.gate, a.ldg, c * kRows, share.start0, share.start_s, at.col);
+        dy.load(a.y, a.ldy, c * kRows, share.start0, share.start_s, at.col);
     };
     load(0);
     float carry[W];
@@ -710,6 +750,11 @@ __global__ __launch_bounds__(kThreads) void k_scan_grad(Scan a) {
         }
         leave<W>(e, a, at, (int)step, m);
     }
+    range.others<W>(a, at, [&](int64_t c) {
+        const uint32_t mine = rows_within(c * kRows, begin, end);
+        clear_rows<T, W>(a.dx, a.lddx, c * kRows, mine, at.col);
+        clear_rows<T, W>(a.dgate, a.lddg, c * kRows, mine, at.col);
+    });
 }
 
 // A thread takes eight columns of a row.  Bound by memory, or by the call where there is little: 512 x 4,096 bfloat16 6.8 us (one column a
