@@ -44,8 +44,9 @@ enum ccdpp_scan_mode {
  *   initial  : float, s rows of d, or NULL for zeros
  * States, products of decays and their gradients are held in 32 bits and rounded once to dtype.
  * (GIVEN decays above 1: also the product of those of any rows one after another has to lie
- * within the range of 32 bits.)  A value that is not finite stays within its column and its
- * sequence.
+ * within the range of 32 bits.  Where that of many rows is below it, what the state before them
+ * adds behind them may be 0, and NaN where the state is infinite.)  A value that is not finite stays
+ * within its column and its sequence.
  */
 typedef struct ccdpp_scan {
     int64_t n, s;
@@ -74,7 +75,7 @@ int ccdpp_scan_kept(const ccdpp_scan_t *p, int64_t *bytes);
 /* y_t = h_t, and last_q = the state behind sequence q's last row (its initial state where it
  * has none).
  *   y, ldy : n rows of d values of dtype, ldy >= d values apart
- *   last   : float, s rows of d, or NULL
+ *   last   : float, s rows of d, or NULL; not `initial` itself
  *   kept   : ccdpp_scan_kept bytes, aligned to 16, or NULL: one state in 8 rows */
 int ccdpp_gated_scan(const ccdpp_scan_t *p, void *y, int64_t ldy, float *last, void *kept,
                      void *workspace, int64_t workspace_bytes, void *stream);
@@ -86,7 +87,7 @@ int ccdpp_gated_scan(const ccdpp_scan_t *p, void *y, int64_t ldy, float *last, v
  *   dinitial_q = a l of the first row (dlast_q where there is none)
  *   dy, lddy : n rows likewise;  dlast : float, s rows of d, or NULL for zeros
  *   kept     : what ccdpp_gated_scan left for the same problem
- *   dx, dgate : n rows likewise;  dinitial : float, s rows of d, or NULL */
+ *   dx, dgate : n rows likewise;  dinitial : float, s rows of d, or NULL; not `dlast` itself */
 int ccdpp_gated_scan_grad(const ccdpp_scan_t *p, const void *dy, int64_t lddy, const float *dlast,
                           const void *kept, void *dx, int64_t lddx, void *dgate, int64_t lddg,
                           float *dinitial, void *workspace, int64_t workspace_bytes, void *stream);

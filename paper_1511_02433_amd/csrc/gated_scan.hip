@@ -926,6 +926,8 @@ int ccdpp_gated_scan(const ccdpp_scan_t* p, void* y, int64_t ldy, float* last, v
     if (p->n > 0 && !y) return fail(CCDPP_EINVAL, "y must be non-NULL");
     if (ldy < p->d) return fail(CCDPP_EINVAL, "ldy must be at least d");
     if (p->n > 0 && (y == p->x || y == p->gate)) return fail(CCDPP_EINVAL, "an output must not be an input");
+    // (Not in place: the block that has a sequence's first row reads its initial state, and the one that has its last row writes the last.)
+    if (last && last == p->initial && p->s > 0) return fail(CCDPP_EINVAL, "last must not be initial");
     if (misaligned(y, p->dtype == CCDPP_F32 ? 4 : 2) || misaligned(last, 4)) return fail(CCDPP_EINVAL, "pointers must be aligned to their types");
     if (int rc = check_device()) return rc;
     const Layout l = layout(p, CCDPP_SCAN_FORWARD);
@@ -948,6 +950,7 @@ int ccdpp_gated_scan_grad(const ccdpp_scan_t* p, const void* dy, int64_t lddy, c
     if (misaligned(dy, es) || misaligned(dx, es) || misaligned(dgate, es) || misaligned(dlast, 4) || misaligned(dinitial, 4))
         return fail(CCDPP_EINVAL, "pointers must be aligned to their types");
     if (int rc = check_device()) return rc;
+    if (dinitial && dinitial == dlast && p->s > 0) return fail(CCDPP_EINVAL, "dinitial must not be dlast");  // as for last and initial
     const Layout l = layout(p, CCDPP_SCAN_GRAD);
     Scan a = {};
     set(a, p, l, ws);

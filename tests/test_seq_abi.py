@@ -202,3 +202,11 @@ def test_the_binding_refuses():
         seq._count(65, "k")
     with pytest.raises(TypeError):
         seq._count(2.0, "k")
+
+
+def test_states_in_place_are_refused():
+    """A sequence's first row, where its initial state is read, and its last one, where the last state is written, may be different blocks'."""
+    L = _lib_or_skip()
+    for initial in (4096, 8192):
+        p = scan(x=256, gate=512, starts=1024, initial=initial)
+        assert L.ccdpp_gated_scan(B(p), 2048, 8, initial, None, 16384, 1 << 40, None) == E and said(L, "last must not be initial")
