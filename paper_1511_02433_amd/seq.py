@@ -319,6 +319,10 @@ def dropout(x, p, seed, *, first_row=0, residual=None, out=None):
         seed = _whole(seed)
         if not -2 ** 63 <= seed < 2 ** 64:
             raise ValueError("seed must fit 64 bits")
+    try:
+        p = ctypes.c_double(p)  # (what is no number is a TypeError)
+    except OverflowError:
+        raise ValueError("p must be in [0, 1]") from None
     first_row = _whole(first_row)
     if not 0 <= first_row < 2 ** 63:
         raise ValueError("first_row must be in [0, 2^63)")

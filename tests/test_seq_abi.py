@@ -210,3 +210,12 @@ def test_states_in_place_are_refused():
     for initial in (4096, 8192):
         p = scan(x=256, gate=512, starts=1024, initial=initial)
         assert L.ccdpp_gated_scan(B(p), 2048, 8, initial, None, 16384, 1 << 40, None) == E and said(L, "last must not be initial")
+
+
+@pytest.mark.parametrize("p, error", [("a", TypeError), ("0.1", TypeError), (None, TypeError), ([0.1], TypeError), (1j, TypeError),
+                                      pytest.param(10 ** 400, ValueError, id="huge")])
+def test_dropout_refuses_what_is_no_probability(p, error, monkeypatch):
+    """With the errors that the module names, before the tensors' device is used."""
+    monkeypatch.setattr(seq, "_matrix", lambda a, name: 3)
+    with pytest.raises(error):
+        seq.dropout(torch.ones(2, 3), p, 1)
