@@ -42,7 +42,8 @@ enum ccdpp_scan_mode {
  *              outputs are 0 there.  (Values are held within [0, n]; where they do not
  *              ascend, results are undefined, but nothing else is read or written.)
  *   initial  : float, s rows of d, or NULL for zeros
- * States, products of decays and their gradients are held in 32 bits and rounded once to dtype.
+ * States, products of decays and their gradients are held in 32 bits and rounded once to dtype;
+ * SIGMOID has a and 1 - a to some 2^-21 of themselves.
  * (GIVEN decays above 1: also the product of those of any rows one after another has to lie
  * within the range of 32 bits.  Where that of many rows is below it, what the state before them
  * adds behind them may be 0, and NaN where the state is infinite.)  A value that is not finite stays
@@ -148,9 +149,10 @@ int ccdpp_beam_reorder(int64_t groups, int32_t beams, int32_t k, const int64_t *
                        const void *const *in, const int64_t *in_stride, void *const *out,
                        const int64_t *row_bytes, void *stream);
 
-/* y = [residual +] x * [r >= p 2^32] / (1 - p), rounded once; r is word j mod 4 of Philox4x32
- * with 7 rounds (Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011)
- * of counter (j / 4, i, i >> 32, 0) and key (seed, seed >> 32), for column j and row
+/* y = [residual +] x * [r >= p 2^32] / (1 - p): 1 / (1 - p), its product with x and the sum with the
+ * residual are rounded to 32 bits each, and y to dtype.  r is word j mod 4 of Philox4x32 with
+ * 7 rounds (Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011) of
+ * counter (j / 4, i, i >> 32, 0) and key (seed, seed >> 32), for column j and row
  * i = first_row + the row's number: the mask is never stored, and the gradient is the same call
  * on dy.  Values that are dropped go nowhere, whatever they hold.
  *   n, d   : 0 <= n < 2^31, 1 <= d < 2^31;  x, residual (or NULL), y : n rows, ld* >= d apart
