@@ -3,9 +3,10 @@
 // Beam b continued by item i has the score  s_b + z_bi - L_b,  L_b = log sum_j exp z_bj.  Within a beam the order is that of z, which is
 // exact in 32 bits: a row leaves its k greatest keys (z, then the lowest item).  Between beams scores are compared in 64 bits.
 //
-// Bound by reading the logits once where they are many: 512 rows of 624,961 floats with offsets 250 us (5.1 TB/s, a copy's rate).  Less of
-// them is bound by instructions and rounds to LDS one after another: 128 rows of 131,072 in bfloat16 23 us (14 without the selection; 6.5 would
-// be a read from the memory-side cache), then 9 for joining, most of it rounds to memory, and 4 for the states.
+// Bound by reading the logits once where they are many: 512 rows of 624,961 floats with offsets 248 us (5.2 TB/s, a copy's rate; streams that
+// are only read reach 6.5 to 6.8).  Less of them is bound by instructions and rounds to LDS one after another: 128 rows of 131,072 in bfloat16
+// 24 us (14 without the selection; 5.2 would be a read from the memory-side cache), then 9 for joining, most of it rounds to memory, and 4 for
+// the states.
 #include <algorithm>
 #include <cmath>
 
@@ -18,7 +19,8 @@ namespace {
 constexpr int kMost = 64;             // beams of a group, and continuations
 constexpr int64_t kGrid = 1 << 20;    // blocks of a launch
 
-// (Taking a chunk's greatest values out one by one, up to k times a chunk, instead of comparing with a bound: 32 us for the 128 rows above.)
+// (The kernel before this one, which took a chunk's greatest values out one by one, up to k times a chunk, instead of comparing with a bound: 32
+// us for the 128 rows above.)
 constexpr int kEach = 32;             // logits of a lane in a chunk
 constexpr int kChunk = 64 * kEach;    // of a wave
 constexpr int kWaves = 4;             // of a block
@@ -486,8 +488,12 @@ int check(const ccdpp_beam_t* p) {
 }
 
 // How a row is shared out among blocks, and where the shares' results lie in the workspace (from 0 on).  Three blocks a CU are wanted: a wave's
-// first chunk costs the most, so fewer shares are better for many rows (512 rows of 624,961 floats in one share each 250 us, in two 257, in
-// four 277), but too few leave waits bare (128 rows of 131,072 in bfloat16: 512 blocks 24.8, 768 23.4, 1,024 21.9, 256 34).
+// first chunk costs the most, so fewer shares are better for many rows, but too few leave waits bare.  Whole calls, microseconds with 512, 768 and
+// 1,024 blocks wanted:
+//   131,072 bfloat16: 128 rows 33.6, 34.3, 32.2 (256 blocks 39.1); 256 46.3, 43.3, 42.3; 384 64.2, 50.0, 49.9; 400 64.1, 64.4, 52.9; 512 65.6, 65.6,
+//                     54.3; 768 72.0, 71.9, 71.7
+//   624,961 floats:   400 rows 230, 231, 252; 504 247, 247, 261; 512 258, 258, 270
+// So 768 is the best for many logits (385 to 767 rows get one share each), and up to a fifth behind 1,024 for as many rows of fewer logits.
 struct Layout {
     int64_t shares, each, sums, refs, keys, bytes;
 };

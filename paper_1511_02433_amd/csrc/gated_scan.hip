@@ -10,9 +10,11 @@
 // sequence that goes on from one share to the next has its rows there read a second time, by a launch before, for their (A, H); so
 // shares begin where a sequence does if one does nearby.  Lengths are known to the device alone: every rule here holds for any of them.
 //
-// 32,768 x 4,096 bfloat16 in 16 sequences: 180 us forward (4.6 TB/s with the kept states), 280 for the gradients (4.9), of a copy's 5.13;
-// vector instructions are issued in 75% and 59% of the cycles (a value takes some 30 forward, 40 back).  1,000,209 x 40 floats in 6,041 sequences
-// 106 + 22 us; one sequence of 65,537 x 100 bfloat16 18 + 8, which is what the rounds to memory of a block take one after another.
+// 32,768 x 4,096 bfloat16 in 16 sequences: 457 us both ways one after the other; the forward call alone, again and again, 193 (872 MB with the
+// kept states, 4.5 TB/s), that of the gradients 289 (1,409 MB, 4.9), of a copy's 5.13; vector instructions are issued in 75% and 60% of the
+// cycles (a value takes some 30 forward, 40 back).  1,000,209 x 40 floats in 6,041 sequences 108 + 22 us (22: the launch before); one sequence of
+// 65,537 x 100 bfloat16 18.5 + 7.5, which is what the rounds to memory of a block take one after another.
+// Times at the choices below are of calls, again and again, in one run that had both sides in turn (histories: the 1,000,209 x 40 floats).
 #include <algorithm>
 #include <type_traits>
 
@@ -23,10 +25,10 @@ namespace ccdops {
 namespace {
 
 // kRows: of a chunk, of which one state is kept for the gradients (half a byte a value).  With 16 the gradients' registers leave fewer waves:
-// 345 us in place of 303 for 32,768 x 4,096 bfloat16; the histories above take 118 + 21 in place of 106 + 22, 10,007 x 777 half precision, both
-// ways, 108 in place of 78.
-// kThreads: with 256 a block has half the chunks side by side and twice the steps: 10,007 x 777 half precision 85 us in place of 78, the histories
-// 133 in place of 128, 32,768 x 4,096 both ways 505 in place of 494.
+// 312 us in place of 289 for 32,768 x 4,096 bfloat16; the histories take 143 in place of 134, 10,007 x 777 half precision, both ways, 110 in
+// place of 78.
+// kThreads: with 256 a block has half the chunks side by side and twice the steps: 10,007 x 777 half precision 86 us in place of 78, the histories
+// 138 in place of 134, 32,768 x 4,096 both ways 547 in place of 454; one long sequence takes the same.
 constexpr int kRows = 8;
 constexpr int kThreads = 512;  // of a block
 constexpr int kLanes = 64;     // of a group, at most
@@ -159,8 +161,8 @@ __device__ int64_t find_start(const Scan& a, int64_t row) {
 }
 
 // Share p begins at row p * rows, or where a sequence does if that is near: within 3 / 16 of a share.  (Blocks wait for the longest share, so
-// shares of unlike lengths cost more than rows read twice: with 3 / 8, 65,000 x 1,000 bfloat16 in 64 sequences by a power law 169 us in
-// place of 154, the histories above 135 in place of 129; with 1 / 8, 32,768 x 4,096 in 16 such sequences both ways 653 in place of 624.)
+// shares of unlike lengths cost more than rows read twice: with 3 / 8, 65,000 x 1,000 bfloat16 in 64 sequences by a power law 173 us in
+// place of 155, 32,768 x 4,096 in 16 such sequences both ways 640 in place of 613.  With 1 / 8 157 and 613, and the histories 130 in place of 134.)
 __device__ Share share_of(const Scan& a, int64_t p) {
     if (p <= 0) return {0, 0, 0, -1};
     if (p >= a.shares) return {a.n, 0, 0, -1};
@@ -757,8 +759,8 @@ __global__ __launch_bounds__(kThreads) void k_scan_grad(Scan a) {
     });
 }
 
-// A thread takes eight columns of a row.  Bound by memory, or by the call where there is little: 512 x 4,096 bfloat16 6.8 us (one column a
-// thread 8.0), 64 x 40 floats 2.6.
+// A thread takes eight columns of a row.  Bound by memory, or by the call where there is little: 512 x 4,096 bfloat16 6.6 us (the first
+// kernel, one column a thread, 8.0), 64 x 40 floats 2.4.
 constexpr int kStepColumns = 8;
 template <class T, bool SIGMOID>
 __global__ __launch_bounds__(256) void k_step(int64_t n, int d, const T* x, int64_t ldx, const T* gate, int64_t ldg, float* state, int64_t lds, T* y,
@@ -821,22 +823,28 @@ struct Layout {
     int64_t share, chunk, of_row, carry, bytes;
 };
 
-// Blocks of a launch: two of 512 threads a CU.  1,024 split more sequences: 32,768 x 4,096 bfloat16 in 16, both ways, 612 us in place of 494,
-// 10,007 x 777 half precision 88 in place of 78.
+// Blocks of a launch: two of 512 threads a CU.  Twice as many split more sequences: 32,768 x 4,096 bfloat16 in 16, both ways, 481 us in place of 454,
+// 10,007 x 777 half precision 90 in place of 78, one sequence of 65,537 x 100 36.0 in place of 28.3; the histories alone gain, 131 in place of 134.
 constexpr int64_t kBlocks = 512;
-// One block a CU where rows are wide, which leaves fewer sequences that go on from share to share and starts each block once: 32,768 x 4,096
-// bfloat16, both ways, in 16 sequences 460 us in place of 490, in 8 459 in place of 620, in 30 of unlike lengths 528 in place of 624; floats 781 in
-// place of 811, 65,536 x 1,024 in 500 479 in place of 523.  Not for 16-bit rows below 8 KB (40,000 x 2,500 in 20 639 in place of 626, 65,000 x
-// 1,000 in 64 414 in place of 393) or in short sequences (32,768 x 4,096 in 512 697 in place of 655), whose instructions need the waves, nor for
-// floats below 4 KB (300,000 x 200 in 50 799 in place of 740).
+// One block a CU where rows are wide, which leaves fewer sequences that go on from share to share and starts each block once.  Both ways,
+// microseconds with it and without; "ragged": lengths by a power law.
+//   bfloat16, taken:  32,768 x 4,096 in 16 454 and 483, in 8 451 and 620, in 30 ragged 525 and 620; 40,000 rows in 16: 4,096 wide 556 and 557, 6,000
+//                     1,081 and 1,196, 8,192 1,087 and 1,109; 5,000 wide in 20 ragged 1,020 and 1,168
+//   not taken:        short sequences, whose instructions need the waves (32,768 x 4,096 in 512 702 and 650, ragged 623 and 565); rows below 8 KB,
+//                     where it depends on the lengths: 65,000 x 1,000 in 64 ragged 412 and 394, 40,000 x 2,500 in 20 ragged 629 and 625, but
+//                     3,500 789 and 855, and in 16 alike 2,048 wide 289 and 381, 2,500 555 and 618, 3,500 723 and 843, 4,000 759 and 777
+//   floats, taken:    65,536 x 1,024 in 16 532 and 592, in 500 426 and 454, in 8,000 ragged 498 and 531; 32,768 x 2,048 in 4,000 469 and 475, ragged 493
+//                     and 510; 32,768 x 4,096 in 16 796 and 813 (in 512 842 and 828)
+//   not taken:        300,000 x 200 in 50 750 and 733; but 65,536 x 512 in 50 288 and 307, 800 wide 486 and 566
 bool one_block_a_cu(const ccdpp_scan_t* p) {
     return p->dtype == CCDPP_F32 ? p->d >= 1024 : p->d >= 4096 && p->n / 256 >= p->s;
 }
-// Bytes of a row that the lanes of a group take at least, where strips are made narrower for more blocks: 32,768 x 4,096 bfloat16 in strips of 128
-// bytes takes 203 us forward in place of 187, and 390 in place of 332 for the gradients.
+// Bytes of a row that the lanes of a group take at least, where strips are made narrower for more blocks.  With 128 bytes 10,007 x 777 half precision
+// takes 36.2 us forward in place of 34.2, 1,000 x 4,096 bfloat16 23.8 in place of 21.9, 4,000 x 200 floats 21.6 in place of 17.1; the fewest rows
+// gain (256 x 4,096 bfloat16 11.7 in place of 14.2).
 constexpr int kPiece = 256;
-// Values from which on the gradients take two columns a thread: 303 us in place of 325 for 32,768 x 4,096 bfloat16, where their instructions
-// bound them; one column leaves registers for twice the waves, which wait less: 31.7 in place of 32.5 for 10,007 x 777 half precision.
+// Values from which on the gradients take two columns a thread: 289 us in place of 375 for 32,768 x 4,096 bfloat16, where their instructions
+// bound them; one column leaves registers for twice the waves, which wait less: 44.7 in place of 46.3 for 10,007 x 777 half precision.
 constexpr int64_t kMuch = 1 << 25;
 
 Layout layout(const ccdpp_scan_t* p, int32_t call) {
